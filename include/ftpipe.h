@@ -62,7 +62,8 @@ typedef enum {
 
 enum { FTP_CONV1D = 0, FTP_CONV2D = 1, FTP_DWCONV3x3 = 2, FTP_BN = 3, FTP_ACT = 4, FTP_ADD_RESIDUAL = 5,
        FTP_MAXPOOL2 = 6, FTP_GAP = 7, FTP_FC = 8, FTP_SOFTMAX_CE = 9 };
-enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2 };
+/* GELU (z Phi(z), the error-function form) and SILU (z / (1 + e^-z)): the feed-forward operators below; a layer list takes 0..2 */
+enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2, FTP_ACT_GELU = 3, FTP_ACT_SILU = 4 };
 enum { FTP_FP32 = 0, FTP_BF16 = 1 };
 /* selector of ftp_get_tensor / ftp_set_tensor */
 enum { FTP_T_WEIGHTS = 0, FTP_T_GRADS = 1, FTP_T_MOMENTUM = 2, FTP_T_STATE = 3 };
@@ -391,6 +392,73 @@ ftp_status ftp_trace_read(ftp_model* m, ftp_trace_rec* out, int32_t max, int32_t
 const char* ftp_kernel_name(int32_t kernel);
 /* Number of kernel launches issued by this model since it was built. */
 ftp_status ftp_launch_count(const ftp_model* m, int64_t* launches);
+
+/* ---- feed-forward operators -----------------------------------------------------------------
+ * (The paper trains convolutional networks; these are the token-wise layers of a stage of a language model, for callers
+ * that string a stage's operators together themselves.)  A batch is `rows` tokens of `cin` channels, row-major; a weight
+ * matrix is [cin][cout] as in the canonical parameter order; biases and their gradients are float; everything else has
+ * the type `precision` names, with float accumulation.  Calls are asynchronous on the stream, launch on the current
+ * device, allocate nothing and give the same bits for the same inputs.  They may be recorded into a CUDA graph.  A call
+ * needs a workspace of its own for as long as it runs (in a graph: for as long as the graph may be replayed).
+ *
+ * What a backward pass needs of its forward pass is kept by the caller, in the tensors' type or as an 8-bit image
+ * (FTP_STASH_8BIT, and x_8bit for the input), which takes 33/32 byte per value: per row and 32 columns one scale s, the
+ * power of two 2^(floor(log2 max|v|) - 6), at least 2^-126, and codes q = v / s rounded to the nearest integer (ties to
+ * even), limited to -127..127.  q s is exact in bf16.  A block that holds a NaN or an infinity reads as NaN throughout.
+ * Layout of the image of rows x cols: rows of pitch = cols rounded up to 32 codes (int8), then pitch / 32 scale bytes per
+ * row (biased exponent of s; 255: NaN), rounded up to 256 bytes; a gated call's image has two such parts, gate then up. */
+enum { FTP_STASH_NONE = 0, FTP_STASH_FULL = 1, FTP_STASH_8BIT = 2 };
+
+typedef struct {
+    int64_t rows;         /* tokens, >= 0 (0: outputs without rows are untouched, weight and bias gradients become 0) */
+    int32_t cin, cout;
+    int32_t precision;    /* FTP_FP32 or FTP_BF16 */
+    int32_t act;          /* FTP_ACT_* */
+    int32_t stash;        /* FTP_STASH_*: form of the kept values before the activation */
+    int32_t x_8bit;       /* backward: x is an 8-bit image of rows x cin */
+    int32_t dw_f32;       /* FTP_BF16: the weight gradients are float instead of bf16 */
+    int32_t unaligned;    /* 1: some operand does not start on a 16-byte boundary (the workspace then holds copies) */
+    /* elements between rows, 0 = no gap: x; w (both matrices of a gated call); y / dy or h / dh; residual or
+     * dx_addend; dx; dw.  Kept values and images have no gaps. */
+    int64_t ldx, ldw, ldy, ldr, lddx, lddw;
+} ftp_ffn_desc;
+
+/* Bytes of workspace of the calls below with this descriptor (0 is possible).  Pure host arithmetic. */
+ftp_status ftp_linear_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, size_t* bytes);
+ftp_status ftp_gated_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, size_t* bytes);
+
+/* z = x w + bias;  y = act(z) + residual;  z is kept in `stash` (rows x cout) as d->stash says.
+ * bias, residual: nullable.  residual may be y. */
+ftp_status ftp_linear_forward(const ftp_ffn_desc* d, const void* x, const void* w, const float* bias, const void* residual, void* y,
+                              void* stash, void* ws, size_t ws_bytes, void* stream);
+/* dz = dy * act'(z);  dx = dz w^T + dx_addend;  dw = x^T dz;  dbias = column sums of dz.  (The residual's gradient is dy.)
+ * Each of dx, dw, dbias may be NULL; dx_addend (a gradient that reaches x another way) is nullable and may be dx.
+ * stash: the kept values (NULL iff act is FTP_ACT_NONE).  dz is rounded to bf16 once before the products when precision
+ * is FTP_BF16; dbias is summed from the unrounded values. */
+ftp_status ftp_linear_backward(const ftp_ffn_desc* d, const void* x, const void* w, const void* stash, const void* dy, const void* dx_addend,
+                               void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* g = x w_gate;  u = x w_up;  h = act(g) * u, one kernel; g and u are kept in `stash` (two planes of rows x cout, or
+ * the two parts of an image).  h may be NULL when only the kept values are wanted. */
+ftp_status ftp_gated_forward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h, void* stash, void* ws,
+                             size_t ws_bytes, void* stream);
+/* dg = dh * u * act'(g);  du = dh * act(g);  dx = dg w_gate^T + du w_up^T + dx_addend;  dw_gate = x^T dg;  dw_up = x^T du.
+ * Each of dx and the pair dw_gate, dw_up may be NULL.  With d->stash == FTP_STASH_NONE (stash NULL) g and u are computed
+ * again from x, or from its 8-bit image. */
+ftp_status ftp_gated_backward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* stash, const void* dh,
+                              const void* dx_addend, void* dx, void* dw_gate, void* dw_up, void* ws, size_t ws_bytes, void* stream);
+
+/* 8-bit images: bytes of one with `parts` parts, and the conversions of one part (ld: elements between rows, 0 = cols). */
+ftp_status ftp_checkpoint_bytes(int64_t rows, int32_t cols, int32_t parts, size_t* bytes);
+ftp_status ftp_checkpoint_pack(const void* x, int64_t rows, int32_t cols, int64_t ld, int32_t precision, void* image, int32_t part,
+                               void* stream);
+ftp_status ftp_checkpoint_unpack(const void* image, int32_t part, int64_t rows, int32_t cols, int32_t precision, void* x, int64_t ld,
+                                 void* stream);
+
+/* Waits for the stream, reads the device word in which a feed-forward kernel leaves a code when one of its bounded waits
+ * ran out, and clears it: FTP_OK or FTP_ETIMEOUT.  After a timeout the results of every feed-forward call on this device
+ * since the last check are invalid.  FTP_ESTATE while the stream is being captured. */
+ftp_status ftp_check_op_status(void* stream);
 
 /* ---- for callers that cannot allocate ------------------------------------------------------------
  * (The paper has no counterpart: this is a packaging variant of the weight-gradient step of

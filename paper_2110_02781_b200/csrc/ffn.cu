@@ -1,0 +1,646 @@
+// Feed-forward operators: the kernels around the products (8-bit images, gradients through the activation, operand
+// planes, bias gradients, the few-token products) and the C entry points.
+#include <algorithm>
+#include <atomic>
+#include "ffn_math.cuh"
+#include "kernels.h"
+#include "launch.cuh"
+
+namespace ftp {
+namespace ffn {
+namespace {
+
+typedef __nv_bfloat16 bf16;
+constexpr int SMS = 148;
+
+__device__ int g_op_status;                  // set by a kernel whose bounded wait ran out; cleared by ftp_check_op_status
+std::atomic<int*> g_status_addr[64] = {};
+
+// ---- eight consecutive elements ----
+__device__ __forceinline__ void load8(const float* p, int valid, bool vec, float (&v)[8]) {
+    if (vec && valid >= 8) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+}
+__device__ __forceinline__ void load8(const bf16* p, int valid, bool vec, float (&v)[8]) {
+    if (vec && valid >= 8) {
+        const uint4 t = *reinterpret_cast<const uint4*>(p);
+        const unsigned u[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(u[i]); v[2 * i + 1] = bf_hi(u[i]); }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < valid ? __bfloat162float(p[i]) : 0.f;
+}
+__device__ __forceinline__ void store8(float* p, int valid, bool vec, const float (&v)[8]) {
+    if (vec && valid >= 8) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < valid) p[i] = v[i];
+}
+__device__ __forceinline__ void store8(bf16* p, int valid, bool vec, const float (&v)[8]) {
+    if (vec && valid >= 8) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(bf_pack(v[0], v[1]), bf_pack(v[2], v[3]), bf_pack(v[4], v[5]), bf_pack(v[6], v[7]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < valid) p[i] = __float2bfloat16(v[i]);
+}
+
+// One plane (bf16 rounding) or three (24 mantissa bits) of eight values; rows of a plane start on 16 bytes.
+// A float is its nearest bf16, the nearest bf16 of the rest and the rest of that; both subtractions are exact.  A value
+// that rounds beyond the largest bf16 is cut instead of rounded; an infinity or NaN goes to the first plane alone.
+__device__ __forceinline__ void store_planes(bf16* p, long long plane, int planes, const float (&v)[8]) {
+    unsigned o[4];
+    if (planes == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = bf_pack(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
+        return;
+    }
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v[i];
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+        float h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = __bfloat162float(__float2bfloat16(r[i]));
+            if (s == 0) {
+                const bool fin = (__float_as_uint(r[i]) & 0x7f800000u) != 0x7f800000u;
+                if (fin && (__float_as_uint(h[i]) & 0x7fffffffu) == 0x7f800000u) h[i] = __uint_as_float(__float_as_uint(r[i]) & 0xffff0000u);
+                r[i] = fin ? r[i] - h[i] : 0.f;
+            } else
+                r[i] -= h[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = bf_pack(h[2 * i], h[2 * i + 1]);
+        *reinterpret_cast<uint4*>(p + s * plane) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// ---- operand planes: copies of bf16 rows at an aligned pitch, or the three planes of float rows ----
+template <typename T>
+__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ x, long long rows, int cols, long long ld, bool vec, bf16* __restrict__ out,
+                                                     long long plane, int planes) {
+    grid_dep_sync();
+    const int groups = (cols + 7) / 8;
+    const long long total = rows * groups, pitch = 8ll * groups;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+        const long long r = i / groups;
+        const int c = (int)(i - r * groups) * 8;
+        float v[8];
+        load8(x + r * ld + c, cols - c, vec, v);
+        store_planes(out + r * pitch + c, plane, planes, v);
+    }
+}
+
+// ---- 8-bit images ----
+// A thread holds eight columns, four neighbouring threads a block of 32.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, long long rows, int cols, long long ld, bool vec, const Image im) {
+    grid_dep_sync();
+    const int groups = (int)(im.pitch / 8);                          // a multiple of 4: a block never straddles the end of a row
+    const long long total = rows * groups;
+    for (long long i0 = blockIdx.x * 256ll; i0 < total; i0 += (long long)gridDim.x * 256) {
+        const long long i = i0 + threadIdx.x;
+        const bool on = i < total;
+        const long long r = on ? i / groups : 0;
+        const int c = on ? (int)(i - r * groups) * 8 : 0;
+        float v[8];
+        load8(x + r * ld + c, on ? max(0, cols - c) : 0, vec, v);
+        unsigned top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const unsigned e = img_exp(top);
+        const float inv = img_inv(e);
+        if (on) {
+            int q[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) q[k] = img_code(v[k], inv);
+            *reinterpret_cast<uint2*>(im.q + r * im.pitch + c) = make_uint2(pack_codes(q[0], q[1], q[2], q[3]), pack_codes(q[4], q[5], q[6], q[7]));
+            if ((threadIdx.x & 3) == 0) im.e[r * (im.pitch / IMG_BLOCK) + c / IMG_BLOCK] = (uint8_t)e;
+        }
+    }
+}
+
+__device__ __forceinline__ void img_load8(const Image& im, long long r, int c, float (&v)[8]) {
+    const uint2 q = *reinterpret_cast<const uint2*>(im.q + r * im.pitch + c);
+    const float s = img_scale(im.e[r * (im.pitch / IMG_BLOCK) + c / IMG_BLOCK]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[k] = (float)(int8_t)(q.x >> (8 * k)) * s;
+        v[4 + k] = (float)(int8_t)(q.y >> (8 * k)) * s;
+    }
+}
+
+// out: `ld` elements between rows
+template <typename T>
+__global__ void __launch_bounds__(256) unpack_kernel(const Image im, long long rows, int cols, T* __restrict__ out, long long ld, bool vec) {
+    grid_dep_sync();
+    const int groups = (cols + 7) / 8;
+    const long long total = rows * groups;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+        const long long r = i / groups;
+        const int c = (int)(i - r * groups) * 8;
+        float v[8];
+        img_load8(im, r, c, v);
+        store8(out + r * ld + c, cols - c, vec, v);
+    }
+}
+
+// ---- gradients through the activation ----
+struct GradArgs {
+    const void* dy; long long lddy; int vec_dy;
+    const void* pre[2]; int vec_pre;         // STASH_FULL: `cols` elements between rows
+    Image img[2];
+    int kind, act;                           // kind: STASH_* (STASH_NONE: the gradient passes unchanged)
+    long long rows; int cols;
+    bf16* out[2]; long long plane; int planes;   // nullable; pitch = cols rounded up to 8
+    float* sums;                             // nullable: [gridDim.y][cols] column sums of this block row
+    int rows_per_block;
+};
+
+// linear: dz = dy act'(z).  gated: dg = dy u act'(g), du = dy act(g).  A thread keeps eight columns and walks down
+// rows_per_block / 8 rows, so the column sums of dz cost registers only; they are added up in float over at most
+// rows_per_block values and then across blocks in double, in a fixed order.
+template <typename T, bool GATED>
+__global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradArgs p) {
+    grid_dep_sync();
+    constexpr bool FAST = sizeof(T) == 2;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (blockIdx.x * 32 + tx) * 8, valid = p.cols - c;
+    const long long pitch = (p.cols + 7) / 8 * 8, r0 = (long long)blockIdx.y * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (valid > 0) {
+#pragma unroll 2
+        for (long long r = r0 + ty; r < r1; r += 8) {
+            float d[8], z[8], u[8], o[8];
+            load8(static_cast<const T*>(p.dy) + r * p.lddy + c, valid, p.vec_dy, d);
+            if (p.kind == STASH_FULL) {
+                load8(static_cast<const T*>(p.pre[0]) + r * p.cols + c, valid, p.vec_pre, z);
+                if (GATED) load8(static_cast<const T*>(p.pre[1]) + r * p.cols + c, valid, p.vec_pre, u);
+            } else if (p.kind == STASH_8BIT) {
+                img_load8(p.img[0], r, c, z);
+                if (GATED) img_load8(p.img[1], r, c, u);
+            }
+            if (GATED) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    float a, da;
+                    act_both<FAST>(z[k], p.act, a, da);
+                    o[k] = d[k] * u[k] * da;
+                    d[k] *= a;
+                }
+                if (valid < 8)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) if (k >= valid) o[k] = d[k] = 0.f;
+                store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, o);
+                store_planes(p.out[1] + r * pitch + c, p.plane, p.planes, d);
+            } else {
+                if (p.kind != STASH_NONE) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float a, da;
+                        act_both<FAST>(z[k], p.act, a, da);
+                        d[k] *= da;
+                    }
+                }
+                if (valid < 8)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) if (k >= valid) d[k] = 0.f;
+                if (p.out[0]) store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, d);
+                if (p.sums) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[k] += d[k];
+                }
+            }
+        }
+    }
+    if (!GATED && p.sums) {
+        __shared__ float red[8][32 * 8 + 8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) red[ty][tx * 8 + k] = sum[k];
+        __syncthreads();
+        const int col = blockIdx.x * 256 + threadIdx.x;
+        if (col < p.cols) {
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
+            p.sums[(long long)blockIdx.y * p.cols + col] = s;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) sums_kernel(const float* __restrict__ part, int chunks, int cols, float* __restrict__ out) {
+    grid_dep_sync();
+    __shared__ double red[8][33];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+    double s = 0.0;
+    if (c < cols)
+        for (int i = ty; i < chunks; i += 8) s += (double)part[(long long)i * cols + c];
+    red[ty][tx] = s;
+    __syncthreads();
+    if (ty == 0 && c < cols) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s += red[k][tx];
+        out[c] = (float)s;
+    }
+}
+
+// ---- the workspace ----
+struct Carve {
+    char* base; size_t off = 0, size;
+    bool dry() const { return base == nullptr; }
+    void* take(size_t bytes) {
+        void* p = base ? base + off : nullptr;
+        off = (off + bytes + 255) / 256 * 256;
+        return p;
+    }
+};
+
+inline long long up8(long long n) { return (n + 7) / 8 * 8; }
+
+// `rows` x `cols` of type T at `src` as an operand.  bf16 rows on 16 bytes are read in place, others copied; float rows
+// become three planes.
+template <typename T>
+ftp_status make_operand(Operand* o, const void* src, long long rows, long long cols, long long ld, bool unaligned, Carve& ws, cudaStream_t st, const char* who) {
+    const bool f32 = sizeof(T) == 4;
+    if (rows == 1) ld = up8(cols);                                   // never stepped over
+    if (!f32 && !unaligned && ld % 8 == 0) {
+        if (!ws.dry()) FTP_REQUIRE(aligned(src, 16), FTP_ERANGE, "%s: an operand does not start on a 16-byte boundary (set `unaligned`)", who);
+        *o = Operand{static_cast<const bf16*>(src), rows, cols, ld, 0, 1};
+        return FTP_OK;
+    }
+    const int planes = f32 ? 3 : 1;
+    const long long pitch = up8(cols), plane = rows * pitch;
+    bf16* p = static_cast<bf16*>(ws.take((size_t)plane * planes * 2));
+    *o = Operand{p, rows, cols, pitch, plane, planes};
+    if (ws.dry()) return FTP_OK;
+    const bool vec = aligned(src, 16) && (ld * (long long)sizeof(T)) % 16 == 0;
+    const long long blocks = (rows * (pitch / 8) + 255) / 256;
+    launch(planes_kernel<T>, dim3((unsigned)std::min<long long>(blocks, SMS * 16)), dim3(256), 0, st, static_cast<const T*>(src), rows, (int)cols, ld, vec, p,
+           plane, planes);
+    return FTP_OK;
+}
+
+// the values of an 8-bit image as an operand: one bf16 plane, exact
+ftp_status image_operand(Operand* o, const void* image, long long rows, long long cols, Carve& ws, cudaStream_t st) {
+    const long long pitch = up8(cols);
+    bf16* p = static_cast<bf16*>(ws.take((size_t)(rows * pitch) * 2));
+    *o = Operand{p, rows, cols, pitch, rows * pitch, 1};
+    if (ws.dry()) return FTP_OK;
+    const Image im = image_at(const_cast<void*>(image), rows, cols, 0);
+    const long long blocks = (rows * (pitch / 8) + 255) / 256;
+    launch(unpack_kernel<bf16>, dim3((unsigned)std::min<long long>(blocks, SMS * 16)), dim3(256), 0, st, im, rows, (int)cols, p, pitch, true);
+    return FTP_OK;
+}
+
+ftp_status check_desc(const ftp_ffn_desc* d, const char* who) {
+    FTP_REQUIRE(d, FTP_EINVAL, "%s: null descriptor", who);
+    FTP_REQUIRE(d->precision == FTP_FP32 || d->precision == FTP_BF16, FTP_EINVAL, "%s: unknown precision %d", who, d->precision);
+    FTP_REQUIRE(d->act >= FTP_ACT_NONE && d->act <= FTP_ACT_SILU, FTP_EINVAL, "%s: unknown activation %d", who, d->act);
+    FTP_REQUIRE(d->stash >= STASH_NONE && d->stash <= STASH_8BIT, FTP_EINVAL, "%s: unknown form of kept values %d", who, d->stash);
+    FTP_REQUIRE(d->rows >= 0 && d->cin >= 1 && d->cout >= 1, FTP_EINVAL, "%s: rows must not be negative, cin and cout must be positive", who);
+    FTP_REQUIRE(d->rows < (1ll << 31) - 256 && d->cin < (1 << 30) && d->cout < (1 << 30), FTP_ERANGE, "%s: tensor too large", who);
+    const long long mx = std::max<long long>(d->cin, d->cout), most = 1ll << 38;
+    FTP_REQUIRE(d->rows * mx <= most && (long long)d->cin * d->cout <= most, FTP_ERANGE, "%s: tensor too large", who);
+    FTP_REQUIRE((d->ldx == 0 || d->ldx >= d->cin) && (d->lddx == 0 || d->lddx >= d->cin) && (d->ldw == 0 || d->ldw >= d->cout) &&
+                    (d->lddw == 0 || d->lddw >= d->cout) && (d->ldy == 0 || d->ldy >= d->cout), FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
+    FTP_REQUIRE(d->ldx < (1ll << 35) && d->lddx < (1ll << 35) && d->ldw < (1ll << 35) && d->lddw < (1ll << 35) && d->ldy < (1ll << 35) && d->ldr >= 0 &&
+                    d->ldr < (1ll << 35), FTP_ERANGE, "%s: pitch too large", who);
+    return FTP_OK;
+}
+
+template <typename T> bool vec4_ok(const void* p, long long ld) { return aligned(p, 4 * sizeof(T)) && ld % 4 == 0; }
+
+template <typename T>
+void set_out(Epi& e, void* y, long long ldy, const void* add, long long ldadd) {
+    e.y = y; e.ldy = ldy; e.vec_y = vec4_ok<T>(y, ldy);
+    e.add = add; e.ldadd = ldadd; e.vec_add = add && vec4_ok<T>(add, ldadd);
+}
+template <typename T>
+void set_stash(Epi& e, int kind, void* stash, long long rows, long long cols, int parts) {
+    e.stash_kind = kind;
+    for (int i = 0; i < parts; ++i) {
+        if (kind == STASH_FULL) e.stash[i] = static_cast<T*>(stash) + (long long)i * rows * cols;
+        if (kind == STASH_8BIT) e.img[i] = image_at(stash, rows, cols, i);
+    }
+    e.ldstash = cols;
+    e.vec_stash = kind == STASH_FULL && vec4_ok<T>(stash, cols) && (parts == 1 || vec4_ok<T>(e.stash[1], cols));
+}
+
+ftp_status check_stash(const ftp_ffn_desc* d, const void* stash, const char* who) {
+    FTP_REQUIRE((d->stash != STASH_NONE) == (stash != nullptr), FTP_EINVAL, "%s: the descriptor and the pointer disagree on whether values are kept", who);
+    FTP_REQUIRE(d->stash != STASH_8BIT || aligned(stash, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
+    return FTP_OK;
+}
+ftp_status check_ws(const Carve& need, const void* ws, size_t ws_bytes, const char* who) {
+    FTP_REQUIRE(need.off == 0 || (ws && ws_bytes >= need.off), FTP_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need.off);
+    FTP_REQUIRE(need.off == 0 || aligned(ws, 256), FTP_ERANGE, "%s: workspace must start on a 256-byte boundary", who);
+    return FTP_OK;
+}
+ftp_status launched(const char* who) {
+    const cudaError_t e = cudaGetLastError();
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+
+// ---- forward of both operators (w[1]: the gated operator's second matrix) ----
+template <typename T, bool GATED>
+ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, const float* bias, const void* residual, void* y, int stash_kind, void* stash,
+                   Carve& ws, cudaStream_t st, const char* who, const Operand* given_x = nullptr, const Operand* given_w = nullptr) {
+    Product p{};
+    const long long ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
+    if (given_x) p.A[0] = *given_x;
+    else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, st, who)) return s;
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+        if (given_w) p.B[i] = given_w[i];
+        else if (ftp_status s = make_operand<T>(&p.B[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, st, who)) return s;
+    }
+    if (ws.dry()) return FTP_OK;
+    p.parts = GATED ? 2 : 1;
+    p.b_mn = 1;
+    p.M = d->rows; p.N = d->cout; p.K = d->cin;
+    p.epi = GATED ? EPI_GATED : EPI_LINEAR;
+    p.out_f32 = sizeof(T) == 4;
+    p.e[0].bias = bias; p.e[0].act = d->act;
+    set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
+    set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, p.parts);
+    p.err = status_word();
+    FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);
+    return run_product(p, st, who);
+}
+
+constexpr int GRAD_ROWS = 64, GRAD_CHUNKS = 1024;
+int grad_rows_per_block(long long rows) { return (int)std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8); }
+
+// ---- backward of both operators ----
+template <typename T, bool GATED>
+ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, const void* stash, const void* dy, const void* addend, void* dx,
+                    void* const* dw, float* dbias, Carve& ws, cudaStream_t st, const char* who) {
+    const long long M = d->rows, ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
+    const bool dry = ws.dry(), f32 = sizeof(T) == 4, want_dw = dry || dw[0], want_dx = dry || dx, recompute = GATED && d->stash == STASH_NONE;
+    Operand X{}, W[2] = {}, G[2] = {};
+    if (want_dw || recompute) {
+        const ftp_status s = d->x_8bit ? image_operand(&X, x, M, d->cin, ws, st) : make_operand<T>(&X, x, M, d->cin, ldx, d->unaligned, ws, st, who);
+        if (s) return s;
+    }
+    if (want_dx || recompute)
+        for (int i = 0; i < (GATED ? 2 : 1); ++i)
+            if (ftp_status s = make_operand<T>(&W[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, st, who)) return s;
+    int kind = d->stash;
+    if (recompute) {
+        stash = ws.take((size_t)(2 * M * d->cout) * sizeof(T));
+        kind = STASH_FULL;
+        if (!dry)
+            if (ftp_status s = forward<T, GATED>(d, nullptr, nullptr, nullptr, nullptr, nullptr, STASH_FULL, const_cast<void*>(stash), ws, st, who, &X, W)) return s;
+    }
+    // the gradient at the products' outputs
+    GradArgs g{};
+    const long long pitch = up8(d->cout);
+    const bool direct = !GATED && !f32 && kind == STASH_NONE && !d->unaligned && (ldy % 8 == 0 || M == 1);
+    g.planes = f32 ? 3 : 1;
+    g.plane = M * pitch;
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+        if (direct) G[i] = Operand{static_cast<const bf16*>(dy), M, d->cout, M == 1 ? pitch : ldy, 0, 1};
+        else {
+            g.out[i] = static_cast<bf16*>(ws.take((size_t)g.plane * g.planes * 2));
+            G[i] = Operand{g.out[i], M, d->cout, pitch, g.plane, g.planes};
+        }
+    }
+    g.rows_per_block = grad_rows_per_block(M);
+    const int chunks = (int)((M + g.rows_per_block - 1) / g.rows_per_block);
+    float* sums = GATED ? nullptr : static_cast<float*>(ws.take((size_t)chunks * d->cout * 4));
+    if (dry) return FTP_OK;
+    if (direct) FTP_REQUIRE(aligned(dy, 16), FTP_ERANGE, "%s: an operand does not start on a 16-byte boundary (set `unaligned`)", who);
+    if (!direct || dbias) {
+        g.dy = dy; g.lddy = ldy;
+        g.vec_dy = aligned(dy, 16) && (ldy * (long long)sizeof(T)) % 16 == 0;
+        g.kind = kind; g.act = d->act;
+        g.rows = M; g.cols = d->cout;
+        for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+            if (kind == STASH_FULL) g.pre[i] = static_cast<const T*>(stash) + (long long)i * M * d->cout;
+            if (kind == STASH_8BIT) g.img[i] = image_at(const_cast<void*>(stash), M, d->cout, i);
+        }
+        g.vec_pre = kind == STASH_FULL && aligned(g.pre[0], 16) && ((long long)d->cout * (long long)sizeof(T)) % 16 == 0 && (!GATED || aligned(g.pre[1], 16));
+        g.sums = dbias ? sums : nullptr;
+        launch(grad_kernel<T, GATED>, dim3((d->cout + 255) / 256, chunks), dim3(256), 0, st, g);
+        if (dbias) launch(sums_kernel, dim3((d->cout + 31) / 32), dim3(256), 0, st, (const float*)sums, chunks, (int)d->cout, dbias);
+        if (ftp_status s = launched(who)) return s;
+    }
+    Product p{};
+    p.err = status_word();
+    FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);
+    p.epi = EPI_STORE;
+    p.parts = GATED ? 2 : 1;
+    if (dx) {
+        p.cat_k = GATED;
+        p.A[0] = G[0]; p.A[1] = G[1]; p.B[0] = W[0]; p.B[1] = W[1];
+        p.M = M; p.N = d->cin; p.K = d->cout;
+        p.out_f32 = f32;
+        set_out<T>(p.e[0], dx, d->lddx ? d->lddx : d->cin, addend, d->ldr ? d->ldr : d->cin);
+        if (ftp_status s = run_product(p, st, who)) return s;
+    }
+    if (dw[0]) {
+        p.cat_k = 0;
+        p.a_mn = p.b_mn = 1;
+        p.A[0] = X; p.B[0] = G[0]; p.B[1] = G[1];
+        p.M = d->cin; p.N = d->cout; p.K = M;
+        p.out_f32 = f32 || d->dw_f32;
+        const long long lddw = d->lddw ? d->lddw : d->cout;
+        for (int i = 0; i < p.parts; ++i) {
+            if (p.out_f32) set_out<float>(p.e[i], dw[i], lddw, nullptr, 0);
+            else set_out<bf16>(p.e[i], dw[i], lddw, nullptr, 0);
+        }
+        if (ftp_status s = run_product(p, st, who)) return s;
+    }
+    return FTP_OK;
+}
+
+ftp_status zero_gradients(const ftp_ffn_desc* d, void* const* dw, int n, float* dbias, cudaStream_t st, const char* who) {
+    const size_t e = d->precision == FTP_FP32 || d->dw_f32 ? 4 : 2, pitch = (size_t)(d->lddw ? d->lddw : d->cout) * e;
+    for (int i = 0; i < n; ++i)
+        if (dw[i]) FTP_REQUIRE(cudaMemset2DAsync(dw[i], pitch, 0, (size_t)d->cout * e, d->cin, st) == cudaSuccess, FTP_ECUDA, "%s: memset failed", who);
+    if (dbias) FTP_REQUIRE(cudaMemsetAsync(dbias, 0, (size_t)d->cout * 4, st) == cudaSuccess, FTP_ECUDA, "%s: memset failed", who);
+    return FTP_OK;
+}
+
+template <bool GATED>
+ftp_status workspace_bytes(const ftp_ffn_desc* d, int32_t back, size_t* bytes, const char* who) {
+    if (ftp_status s = check_desc(d, who)) return s;
+    FTP_REQUIRE(bytes, FTP_EINVAL, "%s: null argument", who);
+    Carve c{nullptr, 0, 0};
+    const void* w[2] = {nullptr, nullptr};
+    void* dw[2] = {nullptr, nullptr};
+    if (d->rows > 0) {
+        if (back) d->precision == FTP_FP32 ? backward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, who)
+                                           : backward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, who);
+        else d->precision == FTP_FP32 ? forward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, who)
+                                      : forward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, who);
+    }
+    *bytes = c.off;
+    return FTP_OK;
+}
+
+template <bool GATED>
+ftp_status check_and_forward(const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const float* bias, const void* residual, void* y, void* stash,
+                             void* ws, size_t ws_bytes, cudaStream_t st, const char* who) {
+    size_t need = 0;
+    if (ftp_status s = workspace_bytes<GATED>(d, 0, &need, who)) return s;
+    FTP_REQUIRE(d->ldr == 0 || !residual || d->ldr >= d->cout, FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
+    FTP_REQUIRE(!d->x_8bit, FTP_EUNSUPPORTED, "%s: the forward pass takes x in its own type", who);
+    if (d->rows == 0) return FTP_OK;
+    FTP_REQUIRE(x && w0 && (!GATED || w1) && (y || (GATED && stash)), FTP_EINVAL, "%s: null buffer", who);
+    if (ftp_status s = check_stash(d, stash, who)) return s;
+    Carve c{nullptr, need, 0};
+    if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
+    Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
+    const void* w[2] = {w0, w1};
+    const ftp_status s = d->precision == FTP_FP32 ? forward<float, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, st, who)
+                                                  : forward<bf16, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, st, who);
+    return s ? s : launched(who);
+}
+
+template <bool GATED>
+ftp_status check_and_backward(const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const void* stash, const void* dy, const void* addend, void* dx,
+                              void* dw0, void* dw1, float* dbias, void* ws, size_t ws_bytes, cudaStream_t st, const char* who) {
+    size_t need = 0;
+    if (ftp_status s = workspace_bytes<GATED>(d, 1, &need, who)) return s;
+    FTP_REQUIRE(d->ldr == 0 || !addend || d->ldr >= d->cin, FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
+    FTP_REQUIRE(!GATED || (dw0 != nullptr) == (dw1 != nullptr), FTP_EINVAL, "%s: both weight gradients or neither", who);
+    FTP_REQUIRE(!addend || dx, FTP_EINVAL, "%s: dx_addend without dx", who);
+    void* dw[2] = {dw0, dw1};
+    if (d->rows == 0) return zero_gradients(d, dw, GATED ? 2 : 1, dbias, st, who);
+    const bool recompute = GATED && d->stash == STASH_NONE;
+    FTP_REQUIRE(dy && ((!dw0 && !recompute) || x) && ((!dx && !recompute) || (w0 && (!GATED || w1))), FTP_EINVAL, "%s: null buffer", who);
+    FTP_REQUIRE(GATED || (d->act == FTP_ACT_NONE) == (d->stash == STASH_NONE), FTP_EINVAL, "%s: an activation's backward pass needs the kept values, and only that does", who);
+    if (ftp_status s = check_stash(d, stash, who)) return s;
+    FTP_REQUIRE(!d->x_8bit || !x || aligned(x, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
+    Carve c{nullptr, need, 0};
+    if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
+    Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
+    const void* w[2] = {w0, w1};
+    const ftp_status s = d->precision == FTP_FP32 ? backward<float, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, st, who)
+                                                  : backward<bf16, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, st, who);
+    return s ? s : launched(who);
+}
+
+}  // namespace
+
+// In host code the word's name is only a handle; the address a kernel may use has to be asked for, once per device.
+int* status_word() {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    int* p = g_status_addr[dev].load(std::memory_order_acquire);
+    if (!p) {
+        void* a = nullptr;
+        if (cudaGetSymbolAddress(&a, g_op_status) != cudaSuccess || !a) return nullptr;
+        p = static_cast<int*>(a);
+        g_status_addr[dev].store(p, std::memory_order_release);
+    }
+    return p;
+}
+
+}  // namespace ffn
+}  // namespace ftp
+
+using namespace ftp::ffn;
+
+extern "C" {
+
+ftp_status ftp_linear_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, size_t* bytes) {
+    return workspace_bytes<false>(d, backward, bytes, "linear_workspace_bytes");
+}
+ftp_status ftp_gated_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, size_t* bytes) {
+    return workspace_bytes<true>(d, backward, bytes, "gated_workspace_bytes");
+}
+
+ftp_status ftp_linear_forward(const ftp_ffn_desc* d, const void* x, const void* w, const float* bias, const void* residual, void* y, void* stash, void* ws,
+                              size_t ws_bytes, void* stream) {
+    return check_and_forward<false>(d, x, w, nullptr, bias, residual, y, stash, ws, ws_bytes, static_cast<cudaStream_t>(stream), "linear_forward");
+}
+ftp_status ftp_gated_forward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h, void* stash, void* ws, size_t ws_bytes,
+                             void* stream) {
+    return check_and_forward<true>(d, x, w_gate, w_up, nullptr, nullptr, h, stash, ws, ws_bytes, static_cast<cudaStream_t>(stream), "gated_forward");
+}
+
+ftp_status ftp_linear_backward(const ftp_ffn_desc* d, const void* x, const void* w, const void* stash, const void* dy, const void* dx_addend, void* dx, void* dw,
+                               float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    return check_and_backward<false>(d, x, w, nullptr, stash, dy, dx_addend, dx, dw, nullptr, dbias, ws, ws_bytes, static_cast<cudaStream_t>(stream),
+                                     "linear_backward");
+}
+ftp_status ftp_gated_backward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* stash, const void* dh,
+                              const void* dx_addend, void* dx, void* dw_gate, void* dw_up, void* ws, size_t ws_bytes, void* stream) {
+    return check_and_backward<true>(d, x, w_gate, w_up, stash, dh, dx_addend, dx, dw_gate, dw_up, nullptr, ws, ws_bytes, static_cast<cudaStream_t>(stream),
+                                    "gated_backward");
+}
+
+ftp_status ftp_checkpoint_bytes(int64_t rows, int32_t cols, int32_t parts, size_t* bytes) {
+    FTP_REQUIRE(bytes && rows >= 0 && cols >= 1 && parts >= 1, FTP_EINVAL, "checkpoint_bytes: bad argument");
+    FTP_REQUIRE(rows * (long long)cols <= (1ll << 38) && rows < (1ll << 38) && parts <= 64 && cols < (1 << 30), FTP_ERANGE, "checkpoint_bytes: tensor too large");
+    *bytes = (size_t)parts * image_part_bytes(rows, cols);
+    return FTP_OK;
+}
+
+static ftp_status check_checkpoint(const void* x, const void* image, int64_t rows, int32_t cols, int64_t* ld, int32_t precision, int32_t part, const char* who) {
+    FTP_REQUIRE(precision == FTP_FP32 || precision == FTP_BF16, FTP_EINVAL, "%s: unknown precision %d", who, precision);
+    size_t bytes;
+    FTP_REQUIRE(part >= 0 && part < 64, FTP_EINVAL, "%s: bad part %d", who, part);
+    if (ftp_status s = ftp_checkpoint_bytes(rows, cols, 1, &bytes)) return s;
+    if (*ld == 0) *ld = cols;
+    FTP_REQUIRE(*ld >= cols && *ld < (1ll << 35), FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
+    FTP_REQUIRE(rows == 0 || (x && image), FTP_EINVAL, "%s: null buffer", who);
+    FTP_REQUIRE(aligned(image, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
+    return FTP_OK;
+}
+
+ftp_status ftp_checkpoint_pack(const void* x, int64_t rows, int32_t cols, int64_t ld, int32_t precision, void* image, int32_t part, void* stream) {
+    if (ftp_status s = check_checkpoint(x, image, rows, cols, &ld, precision, part, "checkpoint_pack")) return s;
+    if (rows == 0) return FTP_OK;
+    const Image im = image_at(image, rows, cols, part);
+    const unsigned blocks = (unsigned)std::min<long long>((rows * (im.pitch / 8) + 255) / 256, SMS * 16);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (precision == FTP_FP32) ftp::launch(pack_kernel<float>, dim3(blocks), dim3(256), 0, st, static_cast<const float*>(x), (long long)rows, (int)cols, (long long)ld, aligned(x, 16) && ld % 4 == 0, im);
+    else ftp::launch(pack_kernel<bf16>, dim3(blocks), dim3(256), 0, st, static_cast<const bf16*>(x), (long long)rows, (int)cols, (long long)ld, aligned(x, 16) && ld % 8 == 0, im);
+    return launched("checkpoint_pack");
+}
+
+ftp_status ftp_checkpoint_unpack(const void* image, int32_t part, int64_t rows, int32_t cols, int32_t precision, void* x, int64_t ld, void* stream) {
+    if (ftp_status s = check_checkpoint(x, image, rows, cols, &ld, precision, part, "checkpoint_unpack")) return s;
+    if (rows == 0) return FTP_OK;
+    const Image im = image_at(const_cast<void*>(image), rows, cols, part);
+    const unsigned blocks = (unsigned)std::min<long long>((rows * (long long)((cols + 7) / 8) + 255) / 256, SMS * 16);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (precision == FTP_FP32) ftp::launch(unpack_kernel<float>, dim3(blocks), dim3(256), 0, st, im, (long long)rows, (int)cols, static_cast<float*>(x), (long long)ld, aligned(x, 16) && ld % 4 == 0);
+    else ftp::launch(unpack_kernel<bf16>, dim3(blocks), dim3(256), 0, st, im, (long long)rows, (int)cols, static_cast<bf16*>(x), (long long)ld, aligned(x, 16) && ld % 8 == 0);
+    return launched("checkpoint_unpack");
+}
+
+ftp_status ftp_check_op_status(void* stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    FTP_REQUIRE(cudaStreamIsCapturing(st, &cap) == cudaSuccess, FTP_ECUDA, "check_op_status: bad stream");
+    FTP_REQUIRE(cap == cudaStreamCaptureStatusNone, FTP_ESTATE, "check_op_status: the stream is being captured");
+    int* word = status_word();
+    FTP_REQUIRE(word, FTP_ECUDA, "check_op_status: no status word on this device");
+    int code = 0;
+    cudaError_t e = cudaMemcpyAsync(&code, word, sizeof code, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && code) e = cudaMemsetAsync(word, 0, sizeof code, st);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "check_op_status: %s", cudaGetErrorString(e));
+    FTP_REQUIRE(code == 0, FTP_ETIMEOUT, "a bounded wait of a feed-forward kernel ran out (code %d)", code);
+    return FTP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,94 @@
+// Activations, their derivatives, 8-bit blocks and four-element accesses of the feed-forward kernels.
+#pragma once
+#include "ffn.h"
+
+namespace ftp {
+namespace ffn {
+
+// exp and the division at float accuracy for float tensors; for bf16 tensors the hardware approximations, whose error
+// (2^-21 relative) is far below the rounding of the result to 8 bits of mantissa.
+template <bool FAST> __device__ __forceinline__ float exp_t(float x) { return FAST ? __expf(x) : expf(x); }
+template <bool FAST> __device__ __forceinline__ float sigmoid_t(float z) {
+    return FAST ? __fdividef(1.f, 1.f + __expf(-z)) : 1.f / (1.f + expf(-z));
+}
+
+// NaN passes through every branch.
+template <bool FAST>
+__device__ __forceinline__ float act_value(float z, int act) {
+    switch (act) {
+        case FTP_ACT_RELU: return z < 0.f ? 0.f : z;
+        case FTP_ACT_RELU6: return z < 0.f ? 0.f : (z > 6.f ? 6.f : z);
+        case FTP_ACT_GELU: return z * (0.5f + 0.5f * erff(z * 0.70710678118654752f));
+        case FTP_ACT_SILU: return z * sigmoid_t<FAST>(z);
+        default: return z;
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ void act_both(float z, int act, float& v, float& d) {
+    switch (act) {
+        case FTP_ACT_RELU: v = z < 0.f ? 0.f : z; d = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z); break;
+        case FTP_ACT_RELU6: v = z < 0.f ? 0.f : (z > 6.f ? 6.f : z); d = z > 0.f && z < 6.f ? 1.f : (z == z ? 0.f : z); break;
+        case FTP_ACT_GELU: {
+            const float p = 0.5f + 0.5f * erff(z * 0.70710678118654752f);
+            v = z * p;
+            // for |z| beyond 14 the density is 0 in float; z * 0 at z = +-inf would be NaN
+            d = p + (fabsf(z) > 14.f ? 0.f : z * exp_t<FAST>(-0.5f * z * z) * 0.39894228040143268f);
+            break;
+        }
+        case FTP_ACT_SILU: {
+            const float s = sigmoid_t<FAST>(z);
+            v = z * s;
+            d = s + (s == 0.f || s == 1.f ? 0.f : v * (1.f - s));
+            break;
+        }
+        default: v = z; d = 1.f;
+    }
+}
+
+// ---- four consecutive elements ----
+__device__ __forceinline__ float bf_lo(unsigned u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf_hi(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ unsigned bf_pack(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const unsigned*>(&h);
+}
+__device__ __forceinline__ void load4(const float* p, int valid, bool vec, float (&v)[4]) {
+    if (vec && valid >= 4) { const float4 t = *reinterpret_cast<const float4*>(p); v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; return; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < valid ? p[i] : 0.f;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, int valid, bool vec, float (&v)[4]) {
+    if (vec && valid >= 4) { const uint2 t = *reinterpret_cast<const uint2*>(p); v[0] = bf_lo(t.x); v[1] = bf_hi(t.x); v[2] = bf_lo(t.y); v[3] = bf_hi(t.y); return; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < valid ? __bfloat162float(p[i]) : 0.f;
+}
+__device__ __forceinline__ void store4(float* p, int valid, bool vec, const float (&v)[4]) {
+    if (vec && valid >= 4) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); return; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < valid) p[i] = v[i];
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int valid, bool vec, const float (&v)[4]) {
+    if (vec && valid >= 4) { *reinterpret_cast<uint2*>(p) = make_uint2(bf_pack(v[0], v[1]), bf_pack(v[2], v[3])); return; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < valid) p[i] = __float2bfloat16(v[i]);
+}
+
+// ---- 8-bit blocks ----
+// Byte of the scale from the bits of the block's largest magnitude: exponent - 6 (so that the largest code is 64..127),
+// at least that of 2^-126, 255 where the block holds a NaN or an infinity.
+__device__ __forceinline__ unsigned img_exp(unsigned amax_bits) {
+    const int be = (int)(amax_bits >> 23);
+    return be == 255 ? 255u : (unsigned)max(be - 6, 1);
+}
+__device__ __forceinline__ float img_scale(unsigned e) { return e == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(e << 23); }
+// 1 / scale = 2^(127 - byte): exact, a subnormal for byte 254 at most (bytes end at 248)
+__device__ __forceinline__ float img_inv(unsigned e) { return e == 255u ? 0.f : __uint_as_float((254u - e) << 23); }
+__device__ __forceinline__ int img_code(float v, float inv) {
+    return __float2int_rn(fminf(fmaxf(v * inv, -127.f), 127.f));     // a NaN (byte 255) becomes some code that no reader uses
+}
+__device__ __forceinline__ unsigned pack_codes(int a, int b, int c, int d) {
+    return (a & 255) | (b & 255) << 8 | (c & 255) << 16 | (unsigned)d << 24;
+}
+
+}  // namespace ffn
+}  // namespace ftp

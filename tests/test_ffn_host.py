@@ -1,0 +1,96 @@
+"""Host side of the feed-forward operators: sizes and refusals, decided before anything is launched (no GPU)."""
+import ctypes as C
+
+import pytest
+
+F = pytest.importorskip("paper_2110_02781_b200")
+FAKE = 1 << 20                 # a 256-byte aligned address that is never dereferenced: every call below is refused on the host
+
+
+def desc(rows=8, cin=64, cout=48, prec=1, act=0, stash=0, x8=0, f32=0, unaligned=0, ldx=0, ldw=0, ldy=0, ldr=0, lddx=0, lddw=0):
+    return F.FfnDesc(rows, cin, cout, prec, act, stash, x8, f32, unaligned, ldx, ldw, ldy, ldr, lddx, lddw)
+
+
+def size(fn, d, back):
+    n = C.c_size_t()
+    st = fn(C.byref(d), back, C.byref(n))
+    return st, n.value
+
+
+def up(n, a):
+    return -(-n // a) * a
+
+
+@pytest.mark.parametrize("rows,cols,parts", [(0, 5, 1), (1, 1, 1), (3, 32, 2), (7, 33, 1), (1000, 1283, 2)])
+def test_image_size_follows_the_documented_layout(rows, cols, parts):
+    pitch = up(cols, 32)
+    assert F.ftp_checkpoint_bytes(rows, cols, parts) == parts * up(rows * (pitch + pitch // 32), 256)
+
+
+def test_image_size_refusals():
+    for a in ((-1, 4, 1), (1, 0, 1), (1, 4, 0), (1 << 40, 4, 1), (1, 1, 65), (1 << 37, 1 << 20, 1)):
+        with pytest.raises(F.FtpError):
+            F.ftp_checkpoint_bytes(*a)
+
+
+def test_workspace_sizes():
+    lin, gat = F.lib.ftp_linear_workspace_bytes, F.lib.ftp_gated_workspace_bytes
+    assert size(lin, desc(), 0) == (0, 0) and size(gat, desc(), 0) == (0, 0)                      # bf16 read in place
+    assert size(lin, desc(rows=0), 1) == (0, 0)
+    assert size(lin, desc(ldx=65), 0)[1] == up(8 * 64 * 2, 256)                                   # a copy of x
+    assert size(lin, desc(cout=47), 0)[1] == up(64 * 48 * 2, 256)                                 # a copy of w
+    assert size(lin, desc(unaligned=1), 0)[1] == up(8 * 64 * 2, 256) + up(64 * 48 * 2, 256)
+    assert size(lin, desc(prec=0), 0)[1] == up(3 * 8 * 64 * 2, 256) + up(3 * 64 * 48 * 2, 256)    # three planes of each
+    assert size(lin, desc(), 1)[1] == up(48 * 4, 256)                                             # sums of the bias gradient
+    assert size(lin, desc(act=3, stash=1), 1)[1] == up(8 * 48 * 2, 256) + up(48 * 4, 256)
+    assert size(gat, desc(act=4, stash=1), 1)[1] == 2 * up(8 * 48 * 2, 256)
+    assert size(gat, desc(act=4, stash=0), 1)[1] == up(2 * 8 * 48 * 2, 256) + 2 * up(8 * 48 * 2, 256)
+    assert size(lin, desc(x8=1), 1)[1] == up(8 * 64 * 2, 256) + up(48 * 4, 256)
+    big = size(gat, desc(rows=1 << 20, cin=8192, cout=16384, prec=0, stash=2, act=4), 1)
+    assert big[0] == 0 and big[1] > 1 << 36
+
+
+@pytest.mark.parametrize("kw,status", [(dict(rows=-1), 1), (dict(cin=0), 1), (dict(cout=-3), 1), (dict(prec=2), 1), (dict(act=5), 1), (dict(act=-1), 1),
+                                       (dict(stash=3), 1), (dict(ldx=63), 1), (dict(ldw=47), 1), (dict(ldy=1), 1), (dict(lddx=63), 1), (dict(lddw=4), 1),
+                                       (dict(rows=(1 << 31) - 1), 2), (dict(cin=1 << 30), 2), (dict(rows=1 << 30, cin=1 << 20), 2), (dict(ldx=1 << 36), 2), (dict(ldr=-1), 2)])
+def test_descriptors_that_are_refused(kw, status):
+    for fn in (F.lib.ftp_linear_workspace_bytes, F.lib.ftp_gated_workspace_bytes):
+        assert size(fn, desc(**kw), 0)[0] == status and size(fn, desc(**kw), 1)[0] == status
+    assert F.lib.ftp_linear_forward(C.byref(desc(**kw)), FAKE, FAKE, None, None, FAKE, None, None, 0, None) == status
+
+
+def test_calls_that_are_refused():
+    ok, L = desc(), F.lib
+    ref = C.byref
+    P = FAKE
+    assert L.ftp_linear_forward(None, P, P, None, None, P, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(ok), None, P, None, None, P, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(ok), P, P, None, None, None, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(ok), P, P, None, None, P, P, None, 0, None) == 1                      # kept values without a form
+    assert L.ftp_linear_forward(ref(desc(stash=1)), P, P, None, None, P, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(desc(stash=2)), P, P, None, None, P, P + 8, None, 0, None) == 2       # image not on 32 bytes
+    assert L.ftp_linear_forward(ref(desc(x8=1)), P, P, None, None, P, None, None, 0, None) == 7
+    assert L.ftp_linear_forward(ref(desc(ldr=40)), P, P, None, P, P, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, None, 0, None) == 3         # no workspace
+    assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, P, 100, None) == 3
+    assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, P + 16, 1 << 30, None) == 2
+    assert L.ftp_linear_forward(ref(ok), P + 2, P, None, None, P, None, None, 0, None) == 2               # not on 16 bytes, and not said so
+    assert L.ftp_linear_backward(ref(desc(act=3)), P, P, None, P, None, P, P, None, P, 1 << 30, None) == 1
+    assert L.ftp_linear_backward(ref(desc(stash=1)), P, P, P, P, None, P, P, None, P, 1 << 30, None) == 1
+    assert L.ftp_linear_backward(ref(ok), P, P, None, None, None, P, P, None, P, 1 << 30, None) == 1
+    assert L.ftp_linear_backward(ref(ok), None, P, None, P, None, None, P, None, P, 1 << 30, None) == 1   # dw without x
+    assert L.ftp_linear_backward(ref(ok), P, None, None, P, None, P, None, None, P, 1 << 30, None) == 1   # dx without w
+    assert L.ftp_linear_backward(ref(ok), P, P, None, P, P, None, P, None, P, 1 << 30, None) == 1         # addend without dx
+    assert L.ftp_linear_backward(ref(desc(ldr=63)), P, P, None, P, P, P, P, None, P, 1 << 30, None) == 1
+    assert L.ftp_linear_backward(ref(desc(x8=1)), P + 4, P, None, P, None, P, P, None, P, 1 << 30, None) == 2
+    assert L.ftp_gated_forward(ref(ok), P, P, None, P, None, None, 0, None) == 1
+    assert L.ftp_gated_forward(ref(ok), P, P, P, None, None, None, 0, None) == 1
+    assert L.ftp_gated_backward(ref(ok), P, P, P, None, P, None, P, P, None, P, 1 << 30, None) == 1       # one weight gradient
+    assert L.ftp_gated_backward(ref(ok), None, P, P, None, P, None, P, None, None, P, 1 << 30, None) == 1 # nothing to compute the products from
+    assert L.ftp_checkpoint_pack(P, 4, 4, 3, 1, P, 0, None) == 1
+    assert L.ftp_checkpoint_pack(P, 4, 4, 0, 1, P + 1, 0, None) == 2
+    assert L.ftp_checkpoint_pack(None, 4, 4, 0, 1, P, 0, None) == 1
+    assert L.ftp_checkpoint_pack(P, 4, 4, 0, 2, P, 0, None) == 1
+    assert L.ftp_checkpoint_unpack(P, -1, 4, 4, 1, P, 0, None) == 1
+    assert L.ftp_checkpoint_pack(None, 0, 4, 0, 1, None, 0, None) == 0                                    # no rows: nothing to do
+    assert L.ftp_linear_forward(ref(desc(rows=0)), None, None, None, None, None, None, None, 0, None) == 0
