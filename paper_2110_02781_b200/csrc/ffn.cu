@@ -322,12 +322,15 @@ ftp_status check_desc(const ftp_ffn_desc* d, const char* who) {
     return FTP_OK;
 }
 
-template <typename T> bool vec4_ok(const void* p, long long ld) { return aligned(p, 4 * sizeof(T)) && ld % 4 == 0; }
+template <typename T> int access_of(const void* p, long long ld) {
+    if (aligned(p, 16) && ld * (long long)sizeof(T) % 16 == 0) return 2;
+    return aligned(p, 4 * sizeof(T)) && ld % 4 == 0 ? 1 : 0;
+}
 
 template <typename T>
 void set_out(Epi& e, void* y, long long ldy, const void* add, long long ldadd) {
-    e.y = y; e.ldy = ldy; e.vec_y = vec4_ok<T>(y, ldy);
-    e.add = add; e.ldadd = ldadd; e.vec_add = add && vec4_ok<T>(add, ldadd);
+    e.y = y; e.ldy = ldy; e.vec_y = access_of<T>(y, ldy);
+    e.add = add; e.ldadd = ldadd; e.vec_add = add ? access_of<T>(add, ldadd) : 0;
 }
 template <typename T>
 void set_stash(Epi& e, int kind, void* stash, long long rows, long long cols, int parts) {
@@ -337,7 +340,7 @@ void set_stash(Epi& e, int kind, void* stash, long long rows, long long cols, in
         if (kind == STASH_8BIT) e.img[i] = image_at(stash, rows, cols, i);
     }
     e.ldstash = cols;
-    e.vec_stash = kind == STASH_FULL && vec4_ok<T>(stash, cols) && (parts == 1 || vec4_ok<T>(e.stash[1], cols));
+    if (kind == STASH_FULL) e.vec_stash = std::min(access_of<T>(stash, cols), parts == 1 ? 2 : access_of<T>(e.stash[1], cols));
 }
 
 ftp_status check_stash(const ftp_ffn_desc* d, const void* stash, const char* who) {

@@ -38,7 +38,8 @@ enum { EPI_STORE = 0, EPI_LINEAR = 1, EPI_GATED = 2 };
 //   EPI_STORE   y = a + add
 //   EPI_LINEAR  z = a + bias, kept in `stash`;  y = act(z) + add
 //   EPI_GATED   a and b kept in `stash`;  y = act(a) * b
-// Pitches in elements; vec_*: the pointer and the pitch allow four elements per access.
+// Pitches in elements; vec_*: what the pointer and the pitch allow at columns that are multiples of an access: 2 = 16
+// bytes, 1 = four elements, 0 = single elements.
 struct Epi {
     void* y; long long ldy;
     const void* add; long long ldadd;

@@ -1,0 +1,419 @@
+// Products of the feed-forward operators on CTA pairs: 256 x BN tiles, persistent.
+//
+// Two CTAs of a cluster work on one tile: each holds 128 rows of A and half of B's columns in its shared memory and 128
+// rows of the accumulator in its tensor memory, and one tcgen05.mma.cta_group::2 of 256 x BN x 16 reads both, so every
+// operand byte that a CTA loads is used for twice as many products as in a tile of its own -- which is what bounds large
+// products: at 256 x 256 a pair needs 64 KB per 8.4 MFLOP from L2.
+//
+// Warp 0 (one thread, each CTA) streams its operand tiles with TMA; the bytes of both CTAs are counted on the first
+// CTA's barrier.  Warp 1 of the first CTA issues the MMAs and hands stages and accumulators on with commits that signal
+// both CTAs.  Warps 2-9 empty the accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
+// accumulator is double (2 x BN columns), so the epilogue of a tile -- bias, activation, kept values, residual -- runs
+// beside the MMAs of the next.  Finished pieces of 32 x 32 go through 4 KB of shared memory per warp, so that a global
+// access covers whole 64- or 128-byte pieces of a row whatever its pitch.
+//
+// Float results are summed in registers chunk by chunk (see CHUNK).  Every wait is bounded; see gemm_tc.cu for the error
+// protocol.
+#include "ffn_gemm.cuh"
+
+namespace ftp {
+namespace ffn {
+namespace {
+
+constexpr int PAIR_THREADS = 64 + 8 * 32;
+constexpr int SMS = 148;
+template <int BN> constexpr int PAIR_STAGES = BN == 256 ? 6 : 8;
+template <int BN> constexpr uint32_t PAIR_RING = PAIR_STAGES<BN> * (128 * BK * 2 + BN / 2 * BK * 2);
+template <int BN> constexpr uint32_t PAIR_SMEM = PAIR_RING<BN> + 8 * 4096 + 1024;
+
+// The mbarrier may be the other CTA's of the pair.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// signals the barrier at this offset in both CTAs once the MMAs issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// tile number -> row tile and column tile: bands of 8 row tiles, column by column, so that the tiles in flight at one time
+// share operands in L2
+__device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+    constexpr int BAND = 8;
+    const int per = BAND * tiles_n, band = t / per, in = t - band * per, rows = min(BAND, tiles_m - band * BAND);
+    tn = in / rows;
+    tm = band * BAND + in - tn * rows;
+}
+
+// A 32 x 32 piece in a warp's shared memory: rows of 128 (float) or 64 (bf16) bytes, 16-byte parts exchanged within the
+// row so that both the per-row and the per-part accesses of a quarter-warp hit all banks.
+template <typename T> __device__ __forceinline__ uint32_t piece_at(int row, int part) {
+    return sizeof(T) == 4 ? row * 128 + ((part ^ (row & 7)) << 4) : row * 64 + ((part ^ ((row >> 1) & 3)) << 4);
+}
+template <typename T> __device__ __forceinline__ void piece_put(uint8_t* buf, int row, const float (&v)[32]) {
+#pragma unroll
+    for (int g = 0; g < (int)sizeof(T) * 2; ++g) {
+        uint4 o;
+        if (sizeof(T) == 4) o = make_uint4(__float_as_uint(v[4 * g]), __float_as_uint(v[4 * g + 1]), __float_as_uint(v[4 * g + 2]), __float_as_uint(v[4 * g + 3]));
+        else {
+            constexpr int W = sizeof(T) == 4 ? 0 : 8;
+            o = make_uint4(bf_pack(v[(W * g) & 31], v[(W * g + 1) & 31]), bf_pack(v[(W * g + 2) & 31], v[(W * g + 3) & 31]), bf_pack(v[(W * g + 4) & 31], v[(W * g + 5) & 31]),
+                           bf_pack(v[(W * g + 6) & 31], v[(W * g + 7) & 31]));
+        }
+        *reinterpret_cast<uint4*>(buf + piece_at<T>(row, g)) = o;
+    }
+}
+template <typename T> __device__ __forceinline__ void piece_get(const uint8_t* buf, int row, float (&v)[32]) {
+#pragma unroll
+    for (int g = 0; g < (int)sizeof(T) * 2; ++g) {
+        const uint4 o = *reinterpret_cast<const uint4*>(buf + piece_at<T>(row, g));
+        const unsigned u[4] = {o.x, o.y, o.z, o.w};
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[(4 * g + i) & 31] = __uint_as_float(u[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[(8 * g + 2 * i) & 31] = bf_lo(u[i]); v[(8 * g + 2 * i + 1) & 31] = bf_hi(u[i]); }
+        }
+    }
+}
+// The piece against rows m0.., columns n0.. of a matrix (ld elements between rows, cut at M x N); vec as in Epi.
+template <typename T, bool STORE>
+__device__ __forceinline__ void piece_move(uint8_t* buf, T* p, long long ld, int vec, long long m0, int n0, long long M, int N) {
+    constexpr int PARTS = sizeof(T) * 2, EL = 16 / sizeof(T), ROWS = 32 / PARTS;        // parts of a row, elements of a part, rows per access
+    const int lane = threadIdx.x & 31, part = lane % PARTS, n = n0 + part * EL;
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += ROWS) {
+        const int r = r0 + lane / PARTS;
+        const long long m = m0 + r;
+        if (m < M && n < N) {
+            T* g = p + m * ld + n;
+            uint4* s = reinterpret_cast<uint4*>(buf + piece_at<T>(r, part));
+            if (vec == 2 && n + EL <= N) {
+                if (STORE) *reinterpret_cast<uint4*>(g) = *s;
+                else *s = *reinterpret_cast<const uint4*>(g);
+            } else if (sizeof(T) == 2 && vec == 1 && n + EL <= N) {  // rows on 8 bytes
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (STORE) reinterpret_cast<uint2*>(g)[h] = reinterpret_cast<const uint2*>(s)[h];
+                    else reinterpret_cast<uint2*>(s)[h] = reinterpret_cast<const uint2*>(g)[h];
+                }
+            } else {
+                T* e = reinterpret_cast<T*>(s);
+                for (int i = 0; i < EL && n + i < N; ++i) {
+                    if (STORE) g[i] = e[i];
+                    else e[i] = g[i];
+                }
+            }
+        }
+    }
+}
+
+// one row's 32 columns of an 8-bit image, all in this thread
+__device__ __forceinline__ void img_store32(const Image& im, long long m, int n, const float (&v)[32]) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    const unsigned e = img_exp(top);
+    const float inv = img_inv(e);
+    uint4* q = reinterpret_cast<uint4*>(im.q + m * im.pitch + n);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = pack_codes(img_code(v[h * 16 + 4 * i], inv), img_code(v[h * 16 + 4 * i + 1], inv), img_code(v[h * 16 + 4 * i + 2], inv), img_code(v[h * 16 + 4 * i + 3], inv));
+        q[h] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    im.e[m * (im.pitch / IMG_BLOCK) + n / IMG_BLOCK] = (uint8_t)e;
+}
+
+// The epilogue on 32 columns n.. of 32 rows m.. (this thread: row m + lane); buf: the warp's 4 KB.
+template <typename T, int EPI>
+__device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long long m, int n, long long M, int N, float (&a)[32], float (&b)[32]) {
+    const int lane = threadIdx.x & 31;
+    constexpr bool FAST = sizeof(T) == 2;
+    if (n >= N || m >= M) return;                                    // the whole piece lies outside
+    auto put = [&](void* p, long long ld, int vec, const float (&v)[32]) {
+        piece_put<T>(buf, lane, v);
+        __syncwarp();
+        piece_move<T, true>(buf, static_cast<T*>(p), ld, vec, m, n, M, N);
+        __syncwarp();
+    };
+    if (EPI == EPI_LINEAR && e.bias) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) if (n + i < N) a[i] += __ldg(e.bias + n + i);
+    }
+    if (EPI != EPI_STORE && e.stash_kind == STASH_FULL) {
+        put(e.stash[0], e.ldstash, e.vec_stash, a);
+        if (EPI == EPI_GATED) put(e.stash[1], e.ldstash, e.vec_stash, b);
+    } else if (EPI != EPI_STORE && e.stash_kind == STASH_8BIT && m + lane < M) {
+        // columns past the end are zero products (their operand tiles are filled with zeros): no effect on a block's maximum
+        img_store32(e.img[0], m + lane, n, a);
+        if (EPI == EPI_GATED) img_store32(e.img[1], m + lane, n, b);
+    }
+    if (!e.y) return;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        if (EPI == EPI_LINEAR) a[i] = act_value<FAST>(a[i], e.act);
+        if (EPI == EPI_GATED) a[i] = act_value<FAST>(a[i], e.act) * b[i];
+    }
+    if (EPI != EPI_GATED && e.add) {
+        piece_move<T, false>(buf, const_cast<T*>(static_cast<const T*>(e.add)), e.ldadd, e.vec_add, m, n, M, N);
+        __syncwarp();
+        float r[32];
+        piece_get<T>(buf, lane, r);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) a[i] += r[i];
+        __syncwarp();
+    }
+    put(e.y, e.ldy, e.vec_y, a);
+}
+
+// EPI_GATED: the tile's first BN / 2 columns are A B[0] (the first CTA's half of B), the others A B[1].
+template <typename T, int BN, bool AMN, bool BMN, int EPI>
+__global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
+                                                                   const __grid_constant__ CUtensorMap mapB0, const __grid_constant__ CUtensorMap mapB1,
+                                                                   const __grid_constant__ KArgs p) {
+    constexpr int STAGES = PAIR_STAGES<BN>;
+    constexpr bool CHUNKED = sizeof(T) == 4;
+    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2, B_BYTES = BN / 2 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+    constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;             // output columns of a tile
+    constexpr int WC = BN / 2;                                       // accumulator columns of an epilogue warp
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 4];
+    __shared__ uint32_t tmem_base;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+    const int tn_all = p.tiles_n * p.parts_n, tiles = p.tiles_m * tn_all, all_kb = p.kb_part * p.parts_k;
+    const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[STAGES]), accf0 = smem_u32(&bars[2 * STAGES]), acce0 = accf0 + 16;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&mapA0); tma_prefetch_map(&mapB0);
+        if (p.parts_k > 1) tma_prefetch_map(&mapA1);
+        if (p.parts_k > 1 || p.parts_n > 1 || EPI == EPI_GATED) tma_prefetch_map(&mapB1);
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, 16); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"((uint32_t)(2 * BN)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync_all();                                              // the barriers of both CTAs exist
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    grid_dep_sync();
+
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---- producer ----
+            long long it = 0;
+            const uint32_t lead_full0 = map_rank(full0, 0);
+            for (int t = cluster; t < tiles && ok; t += clusters) {
+                int tm, tn;
+                tile_at(t, p.tiles_m, tn_all, tm, tn);
+                const int out = tn / p.tiles_n;
+                const int m0 = tm * 256 + (int)rank * 128, n0 = (tn - out * p.tiles_n) * OUTC + (EPI == EPI_GATED ? 0 : (int)rank * (BN / 2));
+                for (int kb = 0; kb < all_kb && ok; ++kb) {
+                    const int part = kb / p.kb_part, k = (kb - part * p.kb_part) * BK;
+                    const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+                    const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
+                    for (int z = p.np - 1; z >= 0; --z, ++it) {
+                        const int s = (int)(it % STAGES);
+                        if (it >= STAGES && !mbar_wait(empty0 + 8 * s, ((uint32_t)(it / STAGES) & 1) ^ 1, p.err, 1)) { ok = false; break; }
+                        const uint32_t sa = smem_u32(smem + s * STAGE_BYTES), sb = sa + A_BYTES, bar = lead_full0 + 8 * s;
+                        if (rank == 0) mbar_expect_tx(full0 + 8 * s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
+                        if (z < p.pa) {
+                            if (AMN) {
+#pragma unroll
+                                for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
+                            } else
+                                tma_load_3d_pair(sa, ma, k, m0, z, bar);
+                        }
+                        if (z < p.pb) {
+                            if (BMN) {
+#pragma unroll
+                                for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
+                            } else
+                                tma_load_3d_pair(sb, mb, k, n0, z, bar);
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            // ---- MMA issuer ----
+            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
+                                       ((uint32_t)(256 >> 4) << 24);
+            long long it = 0;
+            int chunk = 0;                                           // accumulators handed on so far
+            for (int t = cluster; t < tiles && ok; t += clusters) {
+                bool first = true;
+                for (int kb = 0; kb < all_kb && ok; ++kb) {
+                    const int b = chunk & 1;
+                    if (kb == 0 || (CHUNKED && kb % p.chunk == 0)) {
+                        if (chunk >= 2 && !mbar_wait(acce0 + 8 * b, ((chunk >> 1) & 1) ^ 1, p.err, 4)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        first = true;
+                    }
+                    const long long it0 = it;                        // slot of plane np - 1 - i: it0 + i
+                    for (int z = p.np - 1; z >= 0; --z, ++it) {
+                        ok = mbar_wait(full0 + 8 * (int)(it % STAGES), (uint32_t)(it / STAGES) & 1, p.err, 2);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        plane_products(z, p, [&](int za, int zb) {
+                            const uint32_t sa = smem_u32(smem + (int)((it0 + p.np - 1 - za) % STAGES) * STAGE_BYTES);
+                            const uint32_t sb = smem_u32(smem + (int)((it0 + p.np - 1 - zb) % STAGES) * STAGE_BYTES) + A_BYTES;
+                            const uint64_t ad = AMN ? desc_mn(sa, SLAB) : umma_desc_k_sw128(sa), bd = BMN ? desc_mn(sb, SLAB) : umma_desc_k_sw128(sb);
+#pragma unroll
+                            for (int k = 0; k < BK / 16; ++k) {
+                                umma_bf16_pair(tmem + (uint32_t)(b * BN), ad + (uint64_t)(k * (AMN ? 128 : 2)), bd + (uint64_t)(k * (BMN ? 128 : 2)), idesc,
+                                               first ? 0u : 1u);
+                                first = false;
+                            }
+                        });
+                    }
+                    if (!ok) break;
+                    for (long long i = it0; i < it; ++i) umma_commit_pair(empty0 + 8 * (int)(i % STAGES));
+                    if (kb + 1 == all_kb || (CHUNKED && (kb + 1) % p.chunk == 0)) { umma_commit_pair(accf0 + 8 * b); ++chunk; }
+                }
+            }
+        }
+    } else {
+        // ---- epilogue ----
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        uint8_t* buf = smem + PAIR_RING<BN> + (warp - 2) * 4096;
+        const uint32_t lead_acce0 = map_rank(acce0, 0), lanes = tmem + ((uint32_t)(q * 32) << 16);
+        // accumulator columns of this warp: linear and plain half * WC ..; gated: half * WC / 2 .. of either product
+        const int col0 = EPI == EPI_GATED ? half * (WC / 2) : half * WC;
+        constexpr int PIECES = (EPI == EPI_GATED ? WC / 2 : WC) / 32;
+        int chunk = 0;
+        for (int t = cluster; t < tiles && ok; t += clusters) {
+            int tm, tn;
+            tile_at(t, p.tiles_m, tn_all, tm, tn);
+            const int out = tn / p.tiles_n;
+            const long long m0 = (long long)tm * 256 + rank * 128 + q * 32;
+            const int n0 = (tn - out * p.tiles_n) * OUTC + col0;
+            if (CHUNKED) {
+                float acc[WC];
+#pragma unroll
+                for (int i = 0; i < WC; ++i) acc[i] = 0.f;
+                const int chunks = (all_kb + p.chunk - 1) / p.chunk;
+                for (int c = 0; c < chunks; ++c, ++chunk) {
+                    const int b = chunk & 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int g = 0; g < WC / 32; ++g) {
+                        const int col = EPI == EPI_GATED ? (g < WC / 64 ? col0 + g * 32 : BN / 2 + col0 + (g - WC / 64) * 32) : col0 + g * 32;
+                        uint32_t r[32];
+                        tmem_ld32(lanes + (uint32_t)(b * BN + col), r);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[g * 32 + i] += __uint_as_float(r[i]);
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(lead_acce0 + 8 * b);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int g = 0; g < PIECES; ++g) {
+                    float a[32], b2[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) { a[i] = acc[g * 32 + i]; b2[i] = EPI == EPI_GATED ? acc[(WC / 2 + g * 32 + i) % WC] : 0.f; }
+                    finish_piece<T, EPI>(p.e[out], buf, m0, n0 + g * 32, p.M, p.N, a, b2);
+                }
+            } else {
+                const int b = chunk & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                for (int g = 0; g < PIECES; ++g) {
+                    float a[32], b2[32];
+                    uint32_t r[32];
+                    tmem_ld32(lanes + (uint32_t)(b * BN + col0 + g * 32), r);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) a[i] = __uint_as_float(r[i]);
+                    if (EPI == EPI_GATED) {
+                        tmem_ld32(lanes + (uint32_t)(b * BN + BN / 2 + col0 + g * 32), r);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) b2[i] = __uint_as_float(r[i]);
+                    }
+                    if (g == PIECES - 1) {                           // the accumulator is in registers: the tile after next may overwrite it
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(lead_acce0 + 8 * b);
+                    }
+                    finish_piece<T, EPI>(p.e[out], buf, m0, n0 + g * 32, p.M, p.N, a, b2);
+                }
+                ++chunk;
+            }
+        }
+    }
+    if (!ok) {
+        // error path: time for the copies and MMAs already issued, which touch both CTAs, before either may leave
+        const unsigned long long t0 = gtime();
+        while (gtime() - t0 < 1000000ull) __nanosleep(1000);
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync_all();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)) : "memory");
+}
+
+template <typename T, int BN, bool AMN, bool BMN, int EPI>
+ftp_status launch_pair(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
+    Maps m;
+    FTP_REQUIRE(make_maps(m, p, 128, BN / 2), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
+    auto kern = ffn_pair_kernel<T, BN, AMN, BMN, EPI>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PAIR_SMEM<BN>);
+    const long long tiles = (long long)k.tiles_m * k.tiles_n * k.parts_n;
+    FTP_REQUIRE(tiles < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    if (e == cudaSuccess) e = launch_cluster(kern, 2 * (unsigned)std::min<long long>(tiles, SMS / 2), PAIR_THREADS, PAIR_SMEM<BN>, 2, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+template <int BN, bool AMN, bool BMN, int EPI>
+ftp_status pair_typed(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
+    if constexpr (BN == 128)                                         // 256 float sums per thread row do not fit into registers
+        if (p.out_f32) return launch_pair<float, BN, AMN, BMN, EPI>(p, k, st, who);
+    return launch_pair<__nv_bfloat16, BN, AMN, BMN, EPI>(p, k, st, who);
+}
+template <int BN>
+ftp_status pair_kind(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
+    if (p.epi == EPI_GATED) return pair_typed<BN, false, true, EPI_GATED>(p, k, st, who);
+    if (p.epi == EPI_LINEAR) return pair_typed<BN, false, true, EPI_LINEAR>(p, k, st, who);
+    if (p.a_mn) return pair_typed<BN, true, true, EPI_STORE>(p, k, st, who);
+    return pair_typed<BN, false, false, EPI_STORE>(p, k, st, who);
+}
+
+}  // namespace
+
+ftp_status run_product_pair(const Product& p, const KArgs& base, bool wide, cudaStream_t st, const char* who) {
+    KArgs k = base;
+    wide = wide && !p.out_f32;
+    const int bn = wide ? 256 : 128, outc = p.epi == EPI_GATED ? bn / 2 : bn;
+    k.tiles_m = (int)((p.M + 255) / 256);
+    k.tiles_n = (p.N + outc - 1) / outc;
+    return wide ? pair_kind<256>(p, k, st, who) : pair_kind<128>(p, k, st, who);
+}
+
+}  // namespace ffn
+}  // namespace ftp

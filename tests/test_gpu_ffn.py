@@ -84,13 +84,17 @@ LINEAR = [  # rows, cin, cout, gap, off
     (16, 2048, 128, 0, 0), (31, 33, 35, 1, 1), (128, 128, 128, 0, 0), (129, 65, 129, 0, 8), (200, 1283, 517, 0, 0), (257, 320, 1280, 0, 0),
     (300, 8, 1000, 4, 2), (513, 777, 264, 0, 0)]
 
+# enough output tiles for CTA pairs: forward, input gradient, weight gradient; odd edges, several tiles per pair
+LARGE = [(1000, 330, 2300, 0, 0), (1100, 72, 2104, 8, 0), (3001, 40, 2300, 0, 0), (1000, 2300, 330, 0, 0), (330, 1000, 2300, 0, 0), (70, 1100, 2104, 0, 8),
+         (1023, 2049, 33, 0, 0), (2305, 64, 1025, 0, 0)]
+
 
 def linear_case(seed, rows, cin, cout, dt, gap, off):
     x, w = dev(rnd(seed, rows, cin), dt, gap, off), dev(rnd(seed + 1, cin, cout, scale=cin ** -0.5), dt, gap, off)
     return x, w
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + LARGE)
 @pytest.mark.parametrize("dt,name,bias,res,keep", [(BF, "gelu", 1, 1, "full"), (BF, "none", 0, 0, None), (FP, "silu", 1, 1, "8bit"), (FP, "relu6", 0, 1, "full"),
                                                    (BF, "silu", 1, 0, None), (FP, "gelu", 1, 1, None), (BF, "relu", 0, 1, "8bit")])
 def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
@@ -121,7 +125,7 @@ def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
         assert_within(out, z, ez + top / 64, "stash")
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)])
+@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)] + LARGE)
 @pytest.mark.parametrize("dt,name,x8,keep,wide", [(BF, "gelu", 0, "full", 0), (BF, "none", 0, None, 1), (FP, "silu", 0, "full", 0), (FP, "none", 1, None, 0),
                                                   (BF, "relu6", 1, "8bit", 1), (FP, "gelu", 1, "8bit", 0)])
 def test_linear_backward(rows, cin, cout, gap, off, dt, name, x8, keep, wide):
@@ -162,7 +166,8 @@ def test_linear_backward(rows, cin, cout, gap, off, dt, name, x8, keep, wide):
 
 # ---- gated --------------------------------------------------------------------------------------------------
 GATED = [(1, 64, 64, 0, 0), (1, 1, 1, 0, 0), (1, 1000, 333, 0, 0), (4, 130, 200, 0, 0), (8, 512, 96, 8, 0), (33, 100, 31, 1, 1), (128, 256, 128, 0, 0),
-         (130, 72, 136, 0, 0), (257, 1283, 320, 0, 0), (300, 64, 1000, 0, 8)]
+         (130, 72, 136, 0, 0), (257, 1283, 320, 0, 0), (300, 64, 1000, 0, 8), (1000, 330, 1150, 0, 0), (1100, 72, 1048, 8, 0), (70, 1100, 1052, 0, 0),
+         (1025, 2049, 33, 0, 0)]
 
 
 def kept_pair(keep, rows, cout, dt, seed):
