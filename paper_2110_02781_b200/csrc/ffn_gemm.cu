@@ -76,14 +76,15 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
         if (lane == 0) {
             // ---- producer ----
             int it = 0;
+            Slot<STAGES> sl;
             bool ok = true;
             for (int kb = kb0; kb < kb1 && ok; ++kb) {
                 const int part = kb / p.kb_part, k = (kb - part * p.kb_part) * BK;
                 const CUtensorMap* ma = part ? &mapA1 : &mapA0;
                 const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
-                for (int z = p.np - 1; z >= 0; --z, ++it) {
-                    const int s = it % STAGES;
-                    if (it >= STAGES && !mbar_wait(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, p.err, 1)) { ok = false; break; }
+                for (int z = p.np - 1; z >= 0; --z, ++it, sl.next()) {
+                    const int s = sl.s;
+                    if (!wait_for(empty0 + 8 * s, sl.parity ^ 1, p.err, 1)) { ok = false; break; }          // at once for a slot never used
                     const uint32_t sa = smem_u32(smem + s * STAGE_BYTES), sb = sa + A_BYTES, bar = full0 + 8 * s;
                     mbar_expect_tx(bar, (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0));
                     if (z < p.pa) {
@@ -115,39 +116,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            // ---- MMA issuer ----
-            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
-                                       ((uint32_t)(128 >> 4) << 24);
-            int it = 0, chunk = 0;
-            bool ok = true, first = true;
-            for (int kb = kb0; kb < kb1 && ok; ++kb) {
-                const int b = CHUNKED ? chunk & 1 : 0;
-                if (CHUNKED && (kb - kb0) % p.chunk == 0) {
-                    if (chunk >= 2 && !mbar_wait(acce0 + 8 * b, ((chunk >> 1) & 1) ^ 1, p.err, 4)) break;     // the chunk before last has been read
-                    first = true;
-                }
-                const int it0 = it;                          // slot of plane np - 1 - i: it0 + i
-                for (int z = p.np - 1; z >= 0; --z, ++it) {
-                    ok = mbar_wait(full0 + 8 * (it % STAGES), (it / STAGES) & 1, p.err, 2);
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    plane_products(z, p, [&](int za, int zb) {
-                        const uint32_t sa = smem_u32(smem + (it0 + p.np - 1 - za) % STAGES * STAGE_BYTES);
-                        const uint32_t sb = smem_u32(smem + (it0 + p.np - 1 - zb) % STAGES * STAGE_BYTES) + A_BYTES;
-                        const uint64_t ad = AMN ? desc_mn(sa, SLAB) : umma_desc_k_sw128(sa), bd = BMN ? desc_mn(sb, SLAB) : umma_desc_k_sw128(sb);
-#pragma unroll
-                        for (int k = 0; k < BK / 16; ++k) {  // 16 elements further: 32 bytes along a K-major row, 16 rows of an MN-major slab
-                            umma_bf16(tmem + (uint32_t)(b * BN), ad + (uint64_t)(k * (AMN ? 128 : 2)), bd + (uint64_t)(k * (BMN ? 128 : 2)), idesc, first ? 0u : 1u);
-                            first = false;
-                        }
-                    });
-                }
-                if (!ok) break;
-                for (int i = it0; i < it; ++i) umma_commit(empty0 + 8 * (i % STAGES));
-                if (kb + 1 == kb1 || (CHUNKED && (kb + 1 - kb0) % p.chunk == 0)) { umma_commit(accf0 + 8 * b); ++chunk; }
-            }
-        }
+        mma_warp<1, BN, STAGES, STAGE_BYTES, AMN, BMN, CHUNKED, BUFS>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, 1, kb1 - kb0, p);
     } else {
         // ---- accumulator -> shared memory (the ring is free once the last MMA has completed) ----
         const int q = warp & 3;
@@ -161,7 +130,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
             const int chunks = (kb1 - kb0 + p.chunk - 1) / p.chunk;
             for (int c = 0; c < chunks && have; ++c) {
                 const int b = c & 1;
-                have = __all_sync(0xffffffffu, mbar_wait(accf0 + 8 * b, (c >> 1) & 1, p.err, 3));
+                have = __all_sync(0xffffffffu, wait_for(accf0 + 8 * b, (c >> 1) & 1, p.err, 3));
                 if (!have) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -179,7 +148,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
                 for (int g = 0; g < BN / 4; ++g) *reinterpret_cast<float4*>(row + g * 4) = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
             }
         } else {
-            have = __all_sync(0xffffffffu, kb1 > kb0 ? mbar_wait(accf0, 0, p.err, 3) : true);
+            have = __all_sync(0xffffffffu, kb1 > kb0 ? wait_for(accf0, 0, p.err, 3) : true);
             if (have) {
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1

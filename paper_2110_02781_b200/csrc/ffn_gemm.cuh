@@ -117,19 +117,130 @@ __device__ __forceinline__ void finish4(const Epi& e, long long m, int n, int N,
     }
 }
 
-// The MMAs of a block that its plane z completes; ad / bd: descriptors of the operand tiles of plane 0, 1, 2.
-// mma(ad, bd) issues the four 16-element steps.
-template <typename F>
-__device__ __forceinline__ void plane_products(int z, const KArgs& p, F&& mma) {
-    if (p.np == 1) { mma(0, 0); return; }
-    if (z == 1 && p.pa > 1 && p.pb > 1) mma(1, 1);
-    if (z == 0) {
-        if (p.pb > 2) mma(0, 2);
-        if (p.pa > 2) mma(2, 0);
-        if (p.pb > 1) mma(0, 1);
-        if (p.pa > 1) mma(1, 0);
-        mma(0, 0);
+// Bounded wait: as mbar_wait, but the clock and the error word are looked at only once a wait has lasted for 256 tests.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* err, int code) {
+    unsigned long long t0 = 0;
+    for (unsigned it = 1;; ++it) {
+        if (mbar_test(bar, parity)) return true;
+        if ((it & 255u) == 0u) {
+            if (*((volatile int*)err) != 0) return false;             // another role already gave up
+            const unsigned long long t = gtime();
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > TC_WAIT_NS) { atomicCAS(err, 0, code); return false; }
+        }
     }
+}
+// the same answer for the whole warp
+__device__ __forceinline__ bool warp_wait_for(uint32_t bar, uint32_t parity, int* err, int code) {
+    return __all_sync(0xffffffffu, wait_for(bar, parity, err, code));
+}
+// one thread of a converged warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(ok));
+    return ok != 0;
+}
+
+// A position in the ring of operand tiles: the slot and the parity of its use.  
+template <int STAGES>
+struct Slot {
+    int s = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) { s = 0; parity ^= 1; }
+    }
+};
+
+__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// signals the barrier at this offset in both CTAs once the MMAs issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+// The MMA warp of either kernel: `blocks` 64-wide blocks per tile, one tile (tile kernel) or `tiles` of them in turn.  The
+// whole warp walks the loop and one elected thread issues, so that descriptors and addresses stay in uniform registers: with the
+// loop inside a single-thread branch four MMAs and a commit took 1300 cycles to issue, more than they take to run.
+//   full / empty: ring barriers; accf / acce: accumulator complete / read, BUFS of them in turn.
+template <int CG, int BN, int STAGES, uint32_t STAGE_BYTES, bool AMN, bool BMN, bool CHUNKED, int BUFS>
+__device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t empty0, uint32_t accf0, uint32_t acce0, uint32_t tmem, int tiles, int blocks,
+                                         const KArgs& p) {
+    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2;
+    constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
+                               ((uint32_t)(CG * 128 >> 4) << 24);
+    const uint64_t a0 = AMN ? desc_mn(ring, SLAB) : umma_desc_k_sw128(ring), b0 = BMN ? desc_mn(ring + A_BYTES, SLAB) : umma_desc_k_sw128(ring + A_BYTES);
+    Slot<STAGES> sl;
+    int chunk = 0;
+    bool first = true;
+    uint32_t d = tmem;
+    auto four = [&](int sa, int sb) {                                // a block of the planes in slots sa and sb; one thread
+        const uint64_t ad = a0 + (uint64_t)((uint32_t)sa * (STAGE_BYTES >> 4)), bd = b0 + (uint64_t)((uint32_t)sb * (STAGE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) {                          // 16 elements further: 32 bytes along a K-major row, 16 rows of an MN-major slab
+            const uint32_t acc = first && k == 0 ? 0u : 1u;
+            if (CG == 2) umma_bf16_pair(d, ad + (uint64_t)(k * (AMN ? 128 : 2)), bd + (uint64_t)(k * (BMN ? 128 : 2)), idesc, acc);
+            else umma_bf16(d, ad + (uint64_t)(k * (AMN ? 128 : 2)), bd + (uint64_t)(k * (BMN ? 128 : 2)), idesc, acc);
+        }
+        first = false;
+    };
+    auto commit = [&](uint32_t bar) { if (CG == 2) umma_commit_pair(bar); else umma_commit(bar); };
+    for (int t = 0; t < tiles; ++t) {
+        int left = 0;
+        for (int kb = 0; kb < blocks; ++kb) {
+            if (left == 0) {                                         // a new accumulation
+                const int b = BUFS == 1 ? 0 : chunk & 1;
+                if (chunk >= BUFS && !warp_wait_for(acce0 + 8 * b, ((BUFS == 1 ? chunk : chunk >> 1) & 1) ^ 1, p.err, 4)) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                d = tmem + (uint32_t)(b * BN);
+                first = true;
+                left = CHUNKED ? min(p.chunk, blocks - kb) : blocks;
+            }
+            --left;
+            if (!CHUNKED || p.np == 1) {
+                if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (elect_one()) {
+                    four(sl.s, sl.s);
+                    commit(empty0 + 8 * sl.s);
+                    if (left == 0) commit(accf0 + 8 * (BUFS == 1 ? 0 : chunk & 1));
+                }
+                first = false;
+                sl.next();
+            } else {
+                const int s2 = sl.s;
+                if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
+                sl.next();
+                const int s1 = sl.s;
+                if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
+                sl.next();
+                const bool mid = p.pa > 1 && p.pb > 1;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (mid && elect_one()) four(s1, s1);
+                if (mid) first = false;
+                const int s0 = sl.s;
+                if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
+                sl.next();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (elect_one()) {
+                    if (p.pb > 2) four(s0, s2);
+                    if (p.pa > 2) four(s2, s0);
+                    if (p.pb > 1) four(s0, s1);
+                    if (p.pa > 1) four(s1, s0);
+                    four(s0, s0);
+                    commit(empty0 + 8 * s2);
+                    commit(empty0 + 8 * s1);
+                    commit(empty0 + 8 * s0);
+                    if (left == 0) commit(accf0 + 8 * (BUFS == 1 ? 0 : chunk & 1));
+                }
+                first = false;
+            }
+            __syncwarp();
+            if (left == 0) ++chunk;
+        }
+    }
+    return true;
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------

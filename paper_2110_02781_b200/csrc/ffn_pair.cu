@@ -31,14 +31,6 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// signals the barrier at this offset in both CTAs once the MMAs issued so far have completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -219,80 +211,48 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
 
     bool ok = true;
     if (warp == 0) {
-        if (lane == 0) {
-            // ---- producer ----
-            long long it = 0;
-            const uint32_t lead_full0 = map_rank(full0, 0);
-            for (int t = cluster; t < tiles && ok; t += clusters) {
-                int tm, tn;
-                tile_at(t, p.tiles_m, tn_all, tm, tn);
-                const int out = tn / p.tiles_n;
-                const int m0 = tm * 256 + (int)rank * 128, n0 = (tn - out * p.tiles_n) * OUTC + (EPI == EPI_GATED ? 0 : (int)rank * (BN / 2));
-                for (int kb = 0; kb < all_kb && ok; ++kb) {
-                    const int part = kb / p.kb_part, k = (kb - part * p.kb_part) * BK;
-                    const CUtensorMap* ma = part ? &mapA1 : &mapA0;
-                    const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
-                    for (int z = p.np - 1; z >= 0; --z, ++it) {
-                        const int s = (int)(it % STAGES);
-                        if (it >= STAGES && !mbar_wait(empty0 + 8 * s, ((uint32_t)(it / STAGES) & 1) ^ 1, p.err, 1)) { ok = false; break; }
-                        const uint32_t sa = smem_u32(smem + s * STAGE_BYTES), sb = sa + A_BYTES, bar = lead_full0 + 8 * s;
-                        if (rank == 0) mbar_expect_tx(full0 + 8 * s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
-                        if (z < p.pa) {
-                            if (AMN) {
+        // ---- producer ----
+        Slot<STAGES> sl;
+        const uint32_t lead_full0 = map_rank(full0, 0), ring = smem_u32(smem);
+        for (int t = cluster; t < tiles && ok; t += clusters) {
+            int tm, tn;
+            tile_at(t, p.tiles_m, tn_all, tm, tn);
+            const int out = tn / p.tiles_n;
+            const int m0 = tm * 256 + (int)rank * 128, n0 = (tn - out * p.tiles_n) * OUTC + (EPI == EPI_GATED ? 0 : (int)rank * (BN / 2));
+            for (int part = 0; part < p.parts_k && ok; ++part) {
+                const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+                const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
+                for (int kb = 0, k = 0; kb < p.kb_part && ok; ++kb, k += BK) {
+                    for (int z = p.np - 1; z >= 0; --z, sl.next()) {
+                        ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
+                        if (!ok) break;
+                        if (elect_one()) {
+                            const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = lead_full0 + 8 * sl.s;
+                            if (rank == 0) mbar_expect_tx(full0 + 8 * sl.s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
+                            if (z < p.pa) {
+                                if (AMN) {
 #pragma unroll
-                                for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
-                            } else
-                                tma_load_3d_pair(sa, ma, k, m0, z, bar);
-                        }
-                        if (z < p.pb) {
-                            if (BMN) {
+                                    for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
+                                } else
+                                    tma_load_3d_pair(sa, ma, k, m0, z, bar);
+                            }
+                            if (z < p.pb) {
+                                if (BMN) {
 #pragma unroll
-                                for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
-                            } else
-                                tma_load_3d_pair(sb, mb, k, n0, z, bar);
+                                    for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
+                                } else
+                                    tma_load_3d_pair(sb, mb, k, n0, z, bar);
+                            }
                         }
+                        __syncwarp();
                     }
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            // ---- MMA issuer ----
-            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
-                                       ((uint32_t)(256 >> 4) << 24);
-            long long it = 0;
-            int chunk = 0;                                           // accumulators handed on so far
-            for (int t = cluster; t < tiles && ok; t += clusters) {
-                bool first = true;
-                for (int kb = 0; kb < all_kb && ok; ++kb) {
-                    const int b = chunk & 1;
-                    if (kb == 0 || (CHUNKED && kb % p.chunk == 0)) {
-                        if (chunk >= 2 && !mbar_wait(acce0 + 8 * b, ((chunk >> 1) & 1) ^ 1, p.err, 4)) { ok = false; break; }
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        first = true;
-                    }
-                    const long long it0 = it;                        // slot of plane np - 1 - i: it0 + i
-                    for (int z = p.np - 1; z >= 0; --z, ++it) {
-                        ok = mbar_wait(full0 + 8 * (int)(it % STAGES), (uint32_t)(it / STAGES) & 1, p.err, 2);
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        plane_products(z, p, [&](int za, int zb) {
-                            const uint32_t sa = smem_u32(smem + (int)((it0 + p.np - 1 - za) % STAGES) * STAGE_BYTES);
-                            const uint32_t sb = smem_u32(smem + (int)((it0 + p.np - 1 - zb) % STAGES) * STAGE_BYTES) + A_BYTES;
-                            const uint64_t ad = AMN ? desc_mn(sa, SLAB) : umma_desc_k_sw128(sa), bd = BMN ? desc_mn(sb, SLAB) : umma_desc_k_sw128(sb);
-#pragma unroll
-                            for (int k = 0; k < BK / 16; ++k) {
-                                umma_bf16_pair(tmem + (uint32_t)(b * BN), ad + (uint64_t)(k * (AMN ? 128 : 2)), bd + (uint64_t)(k * (BMN ? 128 : 2)), idesc,
-                                               first ? 0u : 1u);
-                                first = false;
-                            }
-                        });
-                    }
-                    if (!ok) break;
-                    for (long long i = it0; i < it; ++i) umma_commit_pair(empty0 + 8 * (int)(i % STAGES));
-                    if (kb + 1 == all_kb || (CHUNKED && (kb + 1) % p.chunk == 0)) { umma_commit_pair(accf0 + 8 * b); ++chunk; }
-                }
-            }
+        if (rank == 0) {
+            const int mine = cluster < tiles ? (tiles - cluster + clusters - 1) / clusters : 0;
+            ok = mma_warp<2, BN, STAGES, STAGE_BYTES, AMN, BMN, CHUNKED, 2>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, mine, all_kb, p);
         }
     } else {
         // ---- epilogue ----
@@ -316,7 +276,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
                 const int chunks = (all_kb + p.chunk - 1) / p.chunk;
                 for (int c = 0; c < chunks; ++c, ++chunk) {
                     const int b = chunk & 1;
-                    ok = __all_sync(0xffffffffu, mbar_wait(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                    ok = __all_sync(0xffffffffu, wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -341,7 +301,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
                 }
             } else {
                 const int b = chunk & 1;
-                ok = __all_sync(0xffffffffu, mbar_wait(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                ok = __all_sync(0xffffffffu, wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
