@@ -378,6 +378,7 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     p.epi = GATED ? EPI_GATED : EPI_LINEAR;
     p.out_f32 = sizeof(T) == 4;
     p.e[0].bias = bias; p.e[0].act = d->act;
+    p.e[0].vec_bias = bias && aligned(bias, 16);
     set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
     set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, p.parts);
     p.err = status_word();

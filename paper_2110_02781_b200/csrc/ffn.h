@@ -47,7 +47,7 @@ struct Epi {
     void* stash[2]; long long ldstash;      // STASH_FULL: one plane per product
     Image img[2];                           // STASH_8BIT
     int stash_kind, act;
-    int vec_y, vec_add, vec_stash;
+    int vec_y, vec_add, vec_stash, vec_bias;
 };
 
 // One operand of a product as the tensor cores read it: bf16 planes whose sum is the operand (1 for bf16 tensors and

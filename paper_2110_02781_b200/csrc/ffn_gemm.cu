@@ -234,8 +234,8 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who) {
     const long long pair_m = (p.M + 255) / 256;
     auto pair_tiles = [&](int bn) { return pair_m * ((p.N + bn / gated - 1) / (bn / gated)) * k.parts_n; };
     if (pair_tiles(128) >= SMS / 2 - 10) {
-        // waves of the 74 pairs times the columns of a tile
-        auto cost = [&](int bn) { return ((pair_tiles(bn) + SMS / 2 - 1) / (SMS / 2)) * bn; };
+        // waves of the 74 pairs times a block's time: 256 x 128 takes 0.78 of 256 x 256 (8192 x 4096 x 4096 bf16: 281 against 180 us)
+        auto cost = [&](int bn) { return ((pair_tiles(bn) + SMS / 2 - 1) / (SMS / 2)) * (bn == 256 ? 100 : 78); };
         return run_product_pair(p, k, cost(256) <= cost(128), st, who);
     }
     auto tiles = [&](int outc) { return (long long)k.tiles_m * ((p.N + outc - 1) / outc) * k.parts_n; };

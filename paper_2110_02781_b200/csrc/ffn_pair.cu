@@ -5,9 +5,10 @@
 // operand byte that a CTA loads is used for twice as many products as in a tile of its own -- which is what bounds large
 // products: at 256 x 256 a pair needs 64 KB per 8.4 MFLOP from L2.
 //
-// Warp 0 (one thread, each CTA) streams its operand tiles with TMA; the bytes of both CTAs are counted on the first
-// CTA's barrier.  Warp 1 of the first CTA issues the MMAs and hands stages and accumulators on with commits that signal
-// both CTAs.  Warps 2-9 empty the accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
+// Warps 0 and 2 (one thread each, in each CTA) stream the tiles of A and of B with TMA (one warp for both takes 550 cycles a
+// block, more than the 512 of its MMAs); the bytes of both CTAs are counted on the first CTA's barrier.  Warp 1 of the first
+// CTA issues the MMAs and hands stages and accumulators on with commits that signal both CTAs.  Warps 4-11 empty the
+// accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
 // accumulator is double (2 x BN columns), so the epilogue of a tile -- bias, activation, kept values, residual -- runs
 // beside the MMAs of the next.  Finished pieces of 32 x 32 go through 4 KB of shared memory per warp, so that a global
 // access covers whole 64- or 128-byte pieces of a row whatever its pitch.
@@ -20,7 +21,7 @@ namespace ftp {
 namespace ffn {
 namespace {
 
-constexpr int PAIR_THREADS = 64 + 8 * 32;
+constexpr int PAIR_THREADS = 12 * 32;
 constexpr int SMS = 148;
 template <int BN> constexpr int PAIR_STAGES = BN == 256 ? 6 : 8;
 template <int BN> constexpr uint32_t PAIR_RING = PAIR_STAGES<BN> * (128 * BK * 2 + BN / 2 * BK * 2);
@@ -127,9 +128,49 @@ __device__ __forceinline__ void img_store32(const Image& im, long long m, int n,
     im.e[m * (im.pitch / IMG_BLOCK) + n / IMG_BLOCK] = (uint8_t)e;
 }
 
-// The epilogue on 32 columns n.. of 32 rows m.. (this thread: row m + lane); buf: the warp's 4 KB.
+// act of 32 values: the choice outside the loop, so that the values' instruction chains interleave
+template <bool FAST>
+__device__ __forceinline__ void act_32(float (&a)[32], int act) {
+    switch (act) {
+        case FTP_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU);
+            break;
+        case FTP_ACT_RELU6:
+#pragma unroll
+            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU6);
+            break;
+        case FTP_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_GELU);
+            break;
+        case FTP_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_SILU);
+            break;
+        default: break;
+    }
+}
+
+// The addend of a 32 x 32 bf16 piece on its way from memory, 16 bytes per access: four accesses per lane, begun before the
+// piece's accumulator is read.
+struct Ahead { uint4 v[4]; };
+__device__ __forceinline__ bool ahead_ok(const Epi& e, long long m, int n, long long M, int N) { return e.add && e.vec_add == 2 && n + 32 <= N && m < M; }
+__device__ __forceinline__ void ahead_load(Ahead& h, const Epi& e, long long m, int n, long long M) {
+    const int lane = threadIdx.x & 31, part = lane & 3;
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(e.add) + n + part * 8;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const long long r = m + k * 8 + (lane >> 2);
+        h.v[k] = r < M ? *reinterpret_cast<const uint4*>(p + r * e.ldadd) : make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// The epilogue on 32 columns n.. of 32 rows m.. (this thread: row m + lane); buf: the warp's 4 KB; ahead: the piece's
+// addend if it was begun (bf16).
 template <typename T, int EPI>
-__device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long long m, int n, long long M, int N, float (&a)[32], float (&b)[32]) {
+__device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long long m, int n, long long M, int N, float (&a)[32], float (&b)[32], bool have_ahead,
+                                             const Ahead& ahead) {
     const int lane = threadIdx.x & 31;
     constexpr bool FAST = sizeof(T) == 2;
     if (n >= N || m >= M) return;                                    // the whole piece lies outside
@@ -140,8 +181,16 @@ __device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long lo
         __syncwarp();
     };
     if (EPI == EPI_LINEAR && e.bias) {
+        if (e.vec_bias && n + 32 <= N) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) if (n + i < N) a[i] += __ldg(e.bias + n + i);
+            for (int i = 0; i < 8; ++i) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(e.bias + n) + i);
+                a[4 * i] += v.x; a[4 * i + 1] += v.y; a[4 * i + 2] += v.z; a[4 * i + 3] += v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) if (n + i < N) a[i] += __ldg(e.bias + n + i);
+        }
     }
     if (EPI != EPI_STORE && e.stash_kind == STASH_FULL) {
         put(e.stash[0], e.ldstash, e.vec_stash, a);
@@ -152,13 +201,17 @@ __device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long lo
         if (EPI == EPI_GATED) img_store32(e.img[1], m + lane, n, b);
     }
     if (!e.y) return;
+    if (EPI != EPI_STORE) act_32<FAST>(a, e.act);
+    if (EPI == EPI_GATED) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        if (EPI == EPI_LINEAR) a[i] = act_value<FAST>(a[i], e.act);
-        if (EPI == EPI_GATED) a[i] = act_value<FAST>(a[i], e.act) * b[i];
+        for (int i = 0; i < 32; ++i) a[i] *= b[i];
     }
     if (EPI != EPI_GATED && e.add) {
-        piece_move<T, false>(buf, const_cast<T*>(static_cast<const T*>(e.add)), e.ldadd, e.vec_add, m, n, M, N);
+        if (sizeof(T) == 2 && have_ahead) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(buf + piece_at<T>(k * 8 + (lane >> 2), lane & 3)) = ahead.v[k];
+        } else
+            piece_move<T, false>(buf, const_cast<T*>(static_cast<const T*>(e.add)), e.ldadd, e.vec_add, m, n, M, N);
         __syncwarp();
         float r[32];
         piece_get<T>(buf, lane, r);
@@ -210,8 +263,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     grid_dep_sync();
 
     bool ok = true;
-    if (warp == 0) {
-        // ---- producer ----
+    if (warp == 0 || warp == 2) {
+        // ---- producers: A by warp 0, B by warp 2 ----
         Slot<STAGES> sl;
         const uint32_t lead_full0 = map_rank(full0, 0), ring = smem_u32(smem);
         for (int t = cluster; t < tiles && ok; t += clusters) {
@@ -228,15 +281,16 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
                         if (!ok) break;
                         if (elect_one()) {
                             const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = lead_full0 + 8 * sl.s;
-                            if (rank == 0) mbar_expect_tx(full0 + 8 * sl.s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
-                            if (z < p.pa) {
-                                if (AMN) {
+                            if (warp == 0) {
+                                if (rank == 0) mbar_expect_tx(full0 + 8 * sl.s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
+                                if (z < p.pa) {
+                                    if (AMN) {
 #pragma unroll
-                                    for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
-                                } else
-                                    tma_load_3d_pair(sa, ma, k, m0, z, bar);
-                            }
-                            if (z < p.pb) {
+                                        for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
+                                    } else
+                                        tma_load_3d_pair(sa, ma, k, m0, z, bar);
+                                }
+                            } else if (z < p.pb) {
                                 if (BMN) {
 #pragma unroll
                                     for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
@@ -254,10 +308,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
             const int mine = cluster < tiles ? (tiles - cluster + clusters - 1) / clusters : 0;
             ok = mma_warp<2, BN, STAGES, STAGE_BYTES, AMN, BMN, CHUNKED, 2>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, mine, all_kb, p);
         }
-    } else {
+    } else if (warp >= 4) {
         // ---- epilogue ----
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        uint8_t* buf = smem + PAIR_RING<BN> + (warp - 2) * 4096;
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        uint8_t* buf = smem + PAIR_RING<BN> + (warp - 4) * 4096;
         const uint32_t lead_acce0 = map_rank(acce0, 0), lanes = tmem + ((uint32_t)(q * 32) << 16);
         // accumulator columns of this warp: linear and plain half * WC ..; gated: half * WC / 2 .. of either product
         const int col0 = EPI == EPI_GATED ? half * (WC / 2) : half * WC;
@@ -276,7 +330,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
                 const int chunks = (all_kb + p.chunk - 1) / p.chunk;
                 for (int c = 0; c < chunks; ++c, ++chunk) {
                     const int b = chunk & 1;
-                    ok = __all_sync(0xffffffffu, wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                    ok = warp_wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -297,31 +351,36 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
                     float a[32], b2[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) { a[i] = acc[g * 32 + i]; b2[i] = EPI == EPI_GATED ? acc[(WC / 2 + g * 32 + i) % WC] : 0.f; }
-                    finish_piece<T, EPI>(p.e[out], buf, m0, n0 + g * 32, p.M, p.N, a, b2);
+                    finish_piece<T, EPI>(p.e[out], buf, m0, n0 + g * 32, p.M, p.N, a, b2, false, Ahead());
                 }
             } else {
                 const int b = chunk & 1;
-                ok = __all_sync(0xffffffffu, wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3));
+                const Epi& e = p.e[out];
+                Ahead ahead;
+                bool have = EPI != EPI_GATED && ahead_ok(e, m0, n0, p.M, p.N);
+                if (have) ahead_load(ahead, e, m0, n0, p.M);
+                ok = warp_wait_for(accf0 + 8 * b, (chunk >> 1) & 1, p.err, 3);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
                 for (int g = 0; g < PIECES; ++g) {
                     float a[32], b2[32];
-                    uint32_t r[32];
-                    tmem_ld32(lanes + (uint32_t)(b * BN + col0 + g * 32), r);
+                    uint32_t r[32], r2[32];
+                    tmem_ld32_issue(lanes + (uint32_t)(b * BN + col0 + g * 32), r);
+                    if (EPI == EPI_GATED) tmem_ld32_issue(lanes + (uint32_t)(b * BN + BN / 2 + col0 + g * 32), r2);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) a[i] = __uint_as_float(r[i]);
-                    if (EPI == EPI_GATED) {
-                        tmem_ld32(lanes + (uint32_t)(b * BN + BN / 2 + col0 + g * 32), r);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) b2[i] = __uint_as_float(r[i]);
-                    }
+                    for (int i = 0; i < 32; ++i) { a[i] = __uint_as_float(r[i]); b2[i] = EPI == EPI_GATED ? __uint_as_float(r2[i]) : 0.f; }
                     if (g == PIECES - 1) {                           // the accumulator is in registers: the tile after next may overwrite it
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(lead_acce0 + 8 * b);
                     }
-                    finish_piece<T, EPI>(p.e[out], buf, m0, n0 + g * 32, p.M, p.N, a, b2);
+                    const Ahead now = ahead;
+                    const bool have_now = have;
+                    have = EPI != EPI_GATED && g + 1 < PIECES && ahead_ok(e, m0, n0 + (g + 1) * 32, p.M, p.N);
+                    if (have) ahead_load(ahead, e, m0, n0 + (g + 1) * 32, p.M);
+                    finish_piece<T, EPI>(e, buf, m0, n0 + g * 32, p.M, p.N, a, b2, have_now, now);
                 }
                 ++chunk;
             }
