@@ -204,7 +204,8 @@ ftp_status launch_tile(const Product& p, KArgs& k, int S, cudaStream_t st, const
     Maps m;
     FTP_REQUIRE(make_maps(m, p, 128, BN), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
     auto kern = ffn_tile_kernel<T, BN, AMN, BMN, EPI>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TILE_SMEM<BN>);
+    static std::atomic<unsigned long long> asked{0};
+    cudaError_t e = allow_smem(asked, kern, (int)TILE_SMEM<BN>);
     if (e == cudaSuccess) e = launch_cluster(kern, (unsigned)((long long)k.tiles_m * k.tiles_n * k.parts_n * S), TILE_THREADS, TILE_SMEM<BN>, S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;

@@ -1,6 +1,7 @@
 // What the two product kernels share: operand order, epilogue pieces, tensor maps, launches with clusters.
 #pragma once
 #include <algorithm>
+#include <atomic>
 #include "ffn_math.cuh"
 #include "gemm_tc_common.cuh"
 
@@ -266,12 +267,26 @@ bool make_map(CUtensorMap* map, const Operand& o, int box_x, int box_y) {
 
 struct Maps { CUtensorMap a[2], b[2]; };
 bool make_maps(Maps& m, const Product& p, int a_rows, int b_rows) {
-    for (int i = 0; i < 2; ++i) {
-        const Operand& A = p.A[(p.parts > 1 && p.cat_k) ? i : 0];
-        const Operand& B = p.B[p.parts > 1 ? i : 0];
-        if (!make_map(&m.a[i], A, 64, p.a_mn ? BK : a_rows) || !make_map(&m.b[i], B, 64, p.b_mn ? BK : b_rows)) return false;
-    }
+    const int na = p.parts > 1 && p.cat_k ? 2 : 1, nb = p.parts > 1 ? 2 : 1;
+    for (int i = 0; i < na; ++i) if (!make_map(&m.a[i], p.A[i], 64, p.a_mn ? BK : a_rows)) return false;
+    for (int i = 0; i < nb; ++i) if (!make_map(&m.b[i], p.B[i], 64, p.b_mn ? BK : b_rows)) return false;
+    if (na == 1) m.a[1] = m.a[0];
+    if (nb == 1) m.b[1] = m.b[0];
     return true;
+}
+
+// More than 48 KB of dynamic shared memory has to be asked for, once per kernel and device (done: the kernel's, one bit per
+// device).
+template <typename K>
+cudaError_t allow_smem(std::atomic<unsigned long long>& done, K kern, int bytes) {
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 template <typename... KA, typename... A>

@@ -402,7 +402,8 @@ ftp_status launch_pair(const Product& p, const KArgs& k, cudaStream_t st, const 
     Maps m;
     FTP_REQUIRE(make_maps(m, p, 128, BN / 2), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
     auto kern = ffn_pair_kernel<T, BN, AMN, BMN, EPI>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PAIR_SMEM<BN>);
+    static std::atomic<unsigned long long> asked{0};
+    cudaError_t e = allow_smem(asked, kern, (int)PAIR_SMEM<BN>);
     const long long tiles = (long long)k.tiles_m * k.tiles_n * k.parts_n;
     FTP_REQUIRE(tiles < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     if (e == cudaSuccess) e = launch_cluster(kern, 2 * (unsigned)std::min<long long>(tiles, SMS / 2), PAIR_THREADS, PAIR_SMEM<BN>, 2, st, m.a[0], m.a[1], m.b[0], m.b[1], k);

@@ -349,91 +349,126 @@ def _bad(who, why):
     raise FtpError(1, f"{who}: {why}")
 
 
-def _rows(who, name, t, cols, prec=None):
-    """(rows, elements between rows) of t seen as rows x cols; checks type, device and layout."""
-    if not t.is_cuda or t.get_device() != _device():
-        _bad(who, f"{name} must live on the current CUDA device")
-    dt = t.dtype
-    if prec is not None and dt != prec:
-        _bad(who, f"{name} must be {prec}, got {dt}")
-    shape, dim = t.shape, t.dim()
-    if dim < 1 or shape[-1] != cols:
-        _bad(who, f"{name} must have {cols} columns, got {tuple(shape)}")
-    if dim == 2:
-        st = t.stride()
-        if cols > 1 and st[1] != 1:
-            _bad(who, f"{name}: a row must be contiguous")
-        ld = st[0]
-        if shape[0] > 1 and ld < cols:
-            _bad(who, f"{name}: rows overlap")
-        return shape[0], (ld if shape[0] > 1 else cols)
-    if t.is_contiguous():
-        return t.numel() // cols, cols
-    _bad(who, f"{name}: only a two-dimensional tensor may have gaps between its rows")
-
-
-def _device():
+def _current():
+    """Index of the current CUDA device."""
     import torch
     return torch.cuda.current_device()
 
 
-def _image(who, name, t, rows, cols, parts):
-    if not t.is_cuda or t.get_device() != _device() or not t.is_contiguous():
-        _bad(who, f"{name}: an 8-bit image is a contiguous uint8 tensor on the current CUDA device")
-    need = ftp_checkpoint_bytes(rows, cols, parts)
-    if t.numel() < need:
-        _bad(who, f"{name}: an image of {rows} x {cols} ({parts} parts) takes {need} bytes, got {t.numel()}")
+def _raw_stream(stream, cur):
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(cur)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
-def _workspace(who, size_of, d, backward, ws, stream):
-    """(address, bytes, tensor to keep alive until the launches are queued)."""
-    import torch
-    n = _sz()
-    _check(size_of(C.byref(d), backward, C.byref(n)))
-    if n.value == 0:
-        return None, 0, None
-    if ws is None:
-        if stream is None:
-            ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
-        else:
-            with torch.cuda.stream(stream if not isinstance(stream, int) else torch.cuda.ExternalStream(stream)):
-                ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
-    elif not ws.is_cuda or ws.get_device() != _device() or not ws.is_contiguous():
-        _bad(who, "ws must be a contiguous tensor on the current CUDA device")
-    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+def _rows(who, name, t, cols, dtype, cur):
+    """(rows, elements between rows) of t seen as rows x cols; checks type, device and layout."""
+    if t.dtype is not dtype:
+        _bad(who, f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != cur:
+        _bad(who, f"{name} must live on the current CUDA device")
+    if t.dim() == 2:
+        rows, c = t.shape
+        s0, s1 = t.stride()
+        if c == cols:
+            if s1 != 1 and cols > 1:
+                _bad(who, f"{name}: a row must be contiguous")
+            if rows <= 1:
+                return rows, cols
+            if s0 < cols:
+                _bad(who, f"{name}: rows overlap")
+            return rows, s0
+    if t.dim() < 1 or t.shape[-1] != cols:
+        _bad(who, f"{name} must have {cols} columns, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        _bad(who, f"{name}: only a two-dimensional tensor may have gaps between its rows")
+    return t.numel() // cols, cols
+
+
+def _same_rows(who, name, t, rows, cols, dtype, cur):
+    """Elements between the rows of t, which has to be rows x cols."""
+    r, ld = _rows(who, name, t, cols, dtype, cur)
+    if r != rows:
+        _bad(who, f"{name} must have {rows} rows, got {r}")
+    return ld
 
 
 def _precision(who, t):
     import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return FP32
     _bad(who, f"tensors are float32 or bfloat16, got {t.dtype}")
 
 
-def _vector(who, name, t, n):
+def _vector(who, name, t, n, cur):
     import torch
-    if not t.is_cuda or t.get_device() != _device() or t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
+    if t.get_device() != cur or t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() != n:
         _bad(who, f"{name} must be {n} contiguous float32 values on the current CUDA device")
     return t.data_ptr()
 
 
-def _off16(*ptrs):
-    return int(any(p is not None and p & 15 for p in ptrs))
-
-
-def _kept(who, stash, rows, cols, parts, dtype):
-    """Form of the kept values from the tensor's type: STASH_*."""
+def _is_image(t):
     import torch
+    return t.dtype is torch.uint8
+
+
+def _image(who, name, t, rows, cols, parts, cur):
+    if t.get_device() != cur or not _is_image(t) or not t.is_contiguous():
+        _bad(who, f"{name}: an 8-bit image is a contiguous uint8 tensor on the current CUDA device")
+    pitch = (cols + 31) // 32 * 32
+    need = parts * ((rows * (pitch + pitch // 32) + 255) // 256 * 256)
+    if t.numel() < need:
+        _bad(who, f"{name}: an image of {rows} x {cols} ({parts} parts) takes {need} bytes, got {t.numel()}")
+
+
+def _kept(who, stash, rows, cols, parts, dtype, cur):
+    """Form of the kept values from the tensor's type: STASH_*."""
     if stash is None:
         return STASH_NONE
-    if stash.dtype == torch.uint8:
-        _image(who, "stash", stash, rows, cols, parts)
+    if _is_image(stash):
+        _image(who, "stash", stash, rows, cols, parts, cur)
         return STASH_8BIT
-    if stash.dtype != dtype or not stash.is_cuda or stash.get_device() != _device() or not stash.is_contiguous() or stash.numel() != parts * rows * cols:
+    if stash.dtype is not dtype or stash.get_device() != cur or not stash.is_contiguous() or stash.numel() != parts * rows * cols:
         _bad(who, f"stash must be a contiguous {dtype} tensor of {parts} x {rows} x {cols} values, or an 8-bit image")
     return STASH_FULL
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+_PLANS = {}            # sizes and options of a call -> its descriptor and workspace size
+
+
+def _plan(size_of, backward, *fields):
+    key = (size_of is lib.ftp_gated_workspace_bytes, backward) + fields
+    p = _PLANS.get(key)
+    if p is None:
+        d, n = FfnDesc(*fields), _sz()
+        _check(size_of(C.byref(d), backward, C.byref(n)))
+        if len(_PLANS) >= 4096:
+            _PLANS.clear()
+        p = _PLANS[key] = (C.byref(d), n.value)
+    return p
+
+
+def _workspace(who, need, ws, stream, cur):
+    """(address, bytes, tensor to keep alive until the launches are queued)."""
+    if need == 0:
+        return None, 0, None
+    if ws is None:
+        import torch
+        if stream is None:
+            ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+                ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    elif ws.get_device() != cur or not ws.is_contiguous():
+        _bad(who, "ws must be a contiguous tensor on the current CUDA device")
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
 def ftp_checkpoint_bytes(rows, cols, parts=1):
@@ -444,164 +479,132 @@ def ftp_checkpoint_bytes(rows, cols, parts=1):
 
 def ftp_checkpoint_pack(x, image, part=0, stream=None):
     """8-bit image of x (tokens x channels) into part `part` of `image`; see include/ftpipe.h for the format."""
-    who = "checkpoint_pack"
+    who, cur, cols = "checkpoint_pack", _current(), x.shape[-1]
     prec = _precision(who, x)
-    rows, ld = _rows(who, "x", x, x.shape[-1])
-    _image(who, "image", image, rows, x.shape[-1], part + 1)
-    _check(lib.ftp_checkpoint_pack(x.data_ptr(), rows, x.shape[-1], ld, prec, image.data_ptr(), part, _stream(stream)))
+    rows, ld = _rows(who, "x", x, cols, x.dtype, cur)
+    _image(who, "image", image, rows, cols, part + 1, cur)
+    _check(lib.ftp_checkpoint_pack(x.data_ptr(), rows, cols, ld, prec, image.data_ptr(), part, _raw_stream(stream, cur)))
 
 
 def ftp_checkpoint_unpack(image, out, part=0, stream=None):
     """The values of part `part` of an 8-bit image into out (tokens x channels)."""
-    who = "checkpoint_unpack"
+    who, cur, cols = "checkpoint_unpack", _current(), out.shape[-1]
     prec = _precision(who, out)
-    rows, ld = _rows(who, "out", out, out.shape[-1])
-    _image(who, "image", image, rows, out.shape[-1], part + 1)
-    _check(lib.ftp_checkpoint_unpack(image.data_ptr(), part, rows, out.shape[-1], prec, out.data_ptr(), ld, _stream(stream)))
+    rows, ld = _rows(who, "out", out, cols, out.dtype, cur)
+    _image(who, "image", image, rows, cols, part + 1, cur)
+    _check(lib.ftp_checkpoint_unpack(image.data_ptr(), part, rows, cols, prec, out.data_ptr(), ld, _raw_stream(stream, cur)))
 
 
-def _ffn_weights(who, ws, dtype):
-    """cin, cout, elements between rows of one or two weight matrices [cin][cout]."""
-    if ws[0].dim() != 2:
+def _weight(who, w, dtype, cur):
+    """cin, cout, elements between rows of a weight matrix [cin][cout]."""
+    if w.dim() != 2:
         _bad(who, "a weight matrix is [cin][cout]")
-    cin, cout = ws[0].shape
-    lds = []
-    for w in ws:
-        rows, ld = _rows(who, "w", w, cout, dtype)
-        if rows != cin:
-            _bad(who, "both weight matrices must have one shape")
-        lds.append(ld)
-    if cin > 1 and len(set(lds)) > 1:
-        _bad(who, "both weight matrices must have the same gap between rows")
-    return cin, cout, lds[0]
+    cin, cout = w.shape
+    return cin, cout, _rows(who, "w", w, cout, dtype, cur)[1]
+
+
+def _weight_pair(who, a, b, dtype, cur):
+    cin, cout, ld = _weight(who, a, dtype, cur)
+    if _weight(who, b, dtype, cur) != (cin, cout, ld):
+        _bad(who, "both weight matrices must have one shape and one gap between rows")
+    return cin, cout, ld
 
 
 def ftp_linear_forward(x, w, y, bias=None, residual=None, act=ACT_NONE, stash=None, ws=None, stream=None):
     """y = act(x w + bias) + residual.  stash: keeps x w + bias, in a tensor like y or as an 8-bit image (uint8)."""
-    who = "linear_forward"
-    prec, dt = _precision(who, x), x.dtype
-    cin, cout, ldw = _ffn_weights(who, (w,), dt)
-    rows, ldx = _rows(who, "x", x, cin, dt)
-    ry, ldy = _rows(who, "y", y, cout, dt)
-    ldr, pr = 0, None
-    if residual is not None:
-        rr, ldr = _rows(who, "residual", residual, cout, dt)
-        pr = residual.data_ptr()
-        if rr != rows:
-            _bad(who, "residual must have as many rows as x")
-    if ry != rows:
-        _bad(who, "y must have as many rows as x")
-    kind = _kept(who, stash, rows, cout, 1, dt)
-    pb = None if bias is None else _vector(who, "bias", bias, cout)
+    who, cur, dt = "linear_forward", _current(), x.dtype
+    prec = _precision(who, x)
+    cin, cout, ldw = _weight(who, w, dt, cur)
+    rows, ldx = _rows(who, "x", x, cin, dt, cur)
+    ldy = _same_rows(who, "y", y, rows, cout, dt, cur)
+    ldr = 0 if residual is None else _same_rows(who, "residual", residual, rows, cout, dt, cur)
+    kind = _kept(who, stash, rows, cout, 1, dt, cur)
+    pb = None if bias is None else _vector(who, "bias", bias, cout, cur)
     px, pw = x.data_ptr(), w.data_ptr()
-    d = FfnDesc(rows, cin, cout, prec, act, kind, 0, 0, _off16(px, pw), ldx, ldw, ldy, ldr, 0, 0)
-    pws, nws, keep = _workspace(who, lib.ftp_linear_workspace_bytes, d, 0, ws, stream)
-    _check(lib.ftp_linear_forward(C.byref(d), px, pw, pb, pr, y.data_ptr(), None if stash is None else stash.data_ptr(), pws, nws, _stream(stream)))
+    d, need = _plan(lib.ftp_linear_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int((px | pw) & 15 != 0), ldx, ldw, ldy, ldr, 0, 0)
+    pws, nws, keep = _workspace(who, need, ws, stream, cur)
+    _check(lib.ftp_linear_forward(d, px, pw, pb, _addr(residual), y.data_ptr(), _addr(stash), pws, nws, _raw_stream(stream, cur)))
 
 
-def _ffn_input(who, x, rows, cin, dtype):
+def _ffn_input(who, x, rows, cin, dtype, cur):
     """(is an image, elements between rows) of a backward pass's x."""
-    import torch
     if x is None:
         return 0, 0
-    if x.dtype == torch.uint8:
-        _image(who, "x", x, rows, cin, 1)
+    if _is_image(x):
+        _image(who, "x", x, rows, cin, 1, cur)
         return 1, 0
-    rx, ldx = _rows(who, "x", x, cin, dtype)
-    if rx != rows:
-        _bad(who, "x must have as many rows as the incoming gradient")
-    return 0, ldx
+    return 0, _same_rows(who, "x", x, rows, cin, dtype, cur)
 
 
-def _ffn_dx(who, dx, dx_addend, rows, cin, dtype):
-    lddx = ldr = 0
-    if dx is not None:
-        r, lddx = _rows(who, "dx", dx, cin, dtype)
-        if r != rows:
-            _bad(who, "dx must have as many rows as the incoming gradient")
-    if dx_addend is not None:
-        r, ldr = _rows(who, "dx_addend", dx_addend, cin, dtype)
-        if r != rows:
-            _bad(who, "dx_addend must have as many rows as the incoming gradient")
-    return lddx, ldr
+def _ffn_dx(who, dx, dx_addend, rows, cin, dtype, cur):
+    return (0 if dx is None else _same_rows(who, "dx", dx, rows, cin, dtype, cur),
+            0 if dx_addend is None else _same_rows(who, "dx_addend", dx_addend, rows, cin, dtype, cur))
 
 
-def _ffn_dw(who, dws, cin, cout, dtype):
+def _ffn_dw(who, dw, cin, cout, dtype, cur):
     """(elements between rows, gradients are float although the tensors are bf16)."""
     import torch
-    if dws[0] is None:
+    if dw is None:
         return 0, 0
-    f32 = dws[0].dtype == torch.float32
-    lds = []
-    for t in dws:
-        r, ld = _rows(who, "dw", t, cout, torch.float32 if f32 else dtype)
-        if r != cin:
-            _bad(who, f"dw must be {cin} x {cout}")
-        lds.append(ld)
-    if cin > 1 and len(set(lds)) > 1:
-        _bad(who, "both weight gradients must have the same gap between rows")
-    return lds[0], int(f32 and dtype == torch.bfloat16)
-
-
-def _addr(t):
-    return None if t is None else t.data_ptr()
+    f32 = dw.dtype is torch.float32
+    return _same_rows(who, "dw", dw, cin, cout, torch.float32 if f32 else dtype, cur), int(f32 and dtype is torch.bfloat16)
 
 
 def ftp_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, stash=None, dx_addend=None, ws=None, stream=None):
     """Gradients of ftp_linear_forward from dy: dx = dz w^T + dx_addend, dw = x^T dz, dbias = column sums of
     dz = dy act'(stash).  x: the input, or its 8-bit image; dw: x's type or float32.  Each output may be left out."""
-    who = "linear_backward"
-    prec, dt = _precision(who, dy), dy.dtype
-    cin, cout, ldw = _ffn_weights(who, (w,), dt)
-    rows, ldy = _rows(who, "dy", dy, cout, dt)
-    x8, ldx = _ffn_input(who, x, rows, cin, dt)
-    lddx, ldr = _ffn_dx(who, dx, dx_addend, rows, cin, dt)
-    lddw, f32 = _ffn_dw(who, (dw,), cin, cout, dt)
-    kind = _kept(who, stash, rows, cout, 1, dt)
-    pb = None if dbias is None else _vector(who, "dbias", dbias, cout)
+    who, cur, dt = "linear_backward", _current(), dy.dtype
+    prec = _precision(who, dy)
+    cin, cout, ldw = _weight(who, w, dt, cur)
+    rows, ldy = _rows(who, "dy", dy, cout, dt, cur)
+    x8, ldx = _ffn_input(who, x, rows, cin, dt, cur)
+    lddx, ldr = _ffn_dx(who, dx, dx_addend, rows, cin, dt, cur)
+    lddw, f32 = _ffn_dw(who, dw, cin, cout, dt, cur)
+    kind = _kept(who, stash, rows, cout, 1, dt, cur)
+    pb = None if dbias is None else _vector(who, "dbias", dbias, cout, cur)
     px, pw, pdy = _addr(x), w.data_ptr(), dy.data_ptr()
-    d = FfnDesc(rows, cin, cout, prec, act, kind, x8, f32, _off16(px, pw, pdy), ldx, ldw, ldy, ldr, lddx, lddw)
-    pws, nws, keep = _workspace(who, lib.ftp_linear_workspace_bytes, d, 1, ws, stream)
-    _check(lib.ftp_linear_backward(C.byref(d), px, pw, _addr(stash), pdy, _addr(dx_addend), _addr(dx), _addr(dw), pb, pws, nws, _stream(stream)))
+    d, need = _plan(lib.ftp_linear_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(((px or 0) | pw | pdy) & 15 != 0), ldx, ldw, ldy, ldr, lddx,
+                    lddw)
+    pws, nws, keep = _workspace(who, need, ws, stream, cur)
+    _check(lib.ftp_linear_backward(d, px, pw, _addr(stash), pdy, _addr(dx_addend), _addr(dx), _addr(dw), pb, pws, nws, _raw_stream(stream, cur)))
 
 
 def ftp_gated_forward(x, w_gate, w_up, h=None, act=ACT_SILU, stash=None, ws=None, stream=None):
     """h = act(x w_gate) * (x w_up).  stash: keeps both products, in a tensor (2, rows, cout) or as an 8-bit image of two
     parts (uint8)."""
-    who = "gated_forward"
-    prec, dt = _precision(who, x), x.dtype
-    cin, cout, ldw = _ffn_weights(who, (w_gate, w_up), dt)
-    rows, ldx = _rows(who, "x", x, cin, dt)
-    ldy = 0
-    if h is not None:
-        rh, ldy = _rows(who, "h", h, cout, dt)
-        if rh != rows:
-            _bad(who, "h must have as many rows as x")
-    kind = _kept(who, stash, rows, cout, 2, dt)
+    who, cur, dt = "gated_forward", _current(), x.dtype
+    prec = _precision(who, x)
+    cin, cout, ldw = _weight_pair(who, w_gate, w_up, dt, cur)
+    rows, ldx = _rows(who, "x", x, cin, dt, cur)
+    ldy = 0 if h is None else _same_rows(who, "h", h, rows, cout, dt, cur)
+    kind = _kept(who, stash, rows, cout, 2, dt, cur)
     px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
-    d = FfnDesc(rows, cin, cout, prec, act, kind, 0, 0, _off16(px, pg, pu), ldx, ldw, ldy, 0, 0, 0)
-    pws, nws, keep = _workspace(who, lib.ftp_gated_workspace_bytes, d, 0, ws, stream)
-    _check(lib.ftp_gated_forward(C.byref(d), px, pg, pu, _addr(h), _addr(stash), pws, nws, _stream(stream)))
+    d, need = _plan(lib.ftp_gated_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int((px | pg | pu) & 15 != 0), ldx, ldw, ldy, 0, 0, 0)
+    pws, nws, keep = _workspace(who, need, ws, stream, cur)
+    _check(lib.ftp_gated_forward(d, px, pg, pu, _addr(h), _addr(stash), pws, nws, _raw_stream(stream, cur)))
 
 
 def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, act=ACT_SILU, stash=None, dx_addend=None, ws=None, stream=None):
     """Gradients of ftp_gated_forward from dh.  x: the input, or its 8-bit image; stash: what the forward pass kept (None:
     both products are computed again from x); dw_gate, dw_up: x's type or float32.  dx or the pair may be left out."""
-    who = "gated_backward"
-    prec, dt = _precision(who, dh), dh.dtype
+    who, cur, dt = "gated_backward", _current(), dh.dtype
+    prec = _precision(who, dh)
     if (dw_gate is None) != (dw_up is None):
         _bad(who, "both weight gradients or neither")
-    cin, cout, ldw = _ffn_weights(who, (w_gate, w_up), dt)
-    rows, ldy = _rows(who, "dh", dh, cout, dt)
-    x8, ldx = _ffn_input(who, x, rows, cin, dt)
-    lddx, ldr = _ffn_dx(who, dx, dx_addend, rows, cin, dt)
-    lddw, f32 = _ffn_dw(who, (dw_gate, dw_up), cin, cout, dt)
-    kind = _kept(who, stash, rows, cout, 2, dt)
-    px, pg, pu, pdh = _addr(x), w_gate.data_ptr(), w_up.data_ptr(), dh.data_ptr()
-    d = FfnDesc(rows, cin, cout, prec, act, kind, x8, f32, _off16(px, pg, pu), ldx, ldw, ldy, ldr, lddx, lddw)
-    pws, nws, keep = _workspace(who, lib.ftp_gated_workspace_bytes, d, 1, ws, stream)
-    _check(lib.ftp_gated_backward(C.byref(d), px, pg, pu, _addr(stash), pdh, _addr(dx_addend), _addr(dx), _addr(dw_gate), _addr(dw_up), pws, nws,
-                                  _stream(stream)))
+    cin, cout, ldw = _weight_pair(who, w_gate, w_up, dt, cur)
+    rows, ldy = _rows(who, "dh", dh, cout, dt, cur)
+    x8, ldx = _ffn_input(who, x, rows, cin, dt, cur)
+    lddx, ldr = _ffn_dx(who, dx, dx_addend, rows, cin, dt, cur)
+    lddw, f32 = _ffn_dw(who, dw_gate, cin, cout, dt, cur)
+    if dw_up is not None and _ffn_dw(who, dw_up, cin, cout, dt, cur) != (lddw, f32):
+        _bad(who, "both weight gradients must have one type and one gap between rows")
+    kind = _kept(who, stash, rows, cout, 2, dt, cur)
+    px, pg, pu = _addr(x), w_gate.data_ptr(), w_up.data_ptr()
+    d, need = _plan(lib.ftp_gated_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(((px or 0) | pg | pu) & 15 != 0), ldx, ldw, ldy, ldr, lddx,
+                    lddw)
+    pws, nws, keep = _workspace(who, need, ws, stream, cur)
+    _check(lib.ftp_gated_backward(d, px, pg, pu, _addr(stash), dh.data_ptr(), _addr(dx_addend), _addr(dx), _addr(dw_gate), _addr(dw_up), pws, nws,
+                                  _raw_stream(stream, cur)))
 
 
 def ftp_check_op_status(stream=None):
