@@ -365,6 +365,12 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
                    Carve& ws, cudaStream_t st, const char* who, const Operand* given_x = nullptr, const Operand* given_w = nullptr) {
     Product p{};
     const long long ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
+    p.e[0].bias = bias; p.e[0].act = d->act;
+    p.e[0].vec_bias = bias && aligned(bias, 16);
+    set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
+    set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, GATED ? 2 : 1);
+    if (!given_x && few_tokens(d->rows, d->cin))
+        return ws.dry() ? FTP_OK : run_few(x, ldx, w, ldw, GATED ? 2 : 1, (int)d->rows, d->cin, d->cout, sizeof(T) == 4, p.e[0], st, who);
     if (given_x) p.A[0] = *given_x;
     else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, st, who)) return s;
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
@@ -377,10 +383,6 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     p.M = d->rows; p.N = d->cout; p.K = d->cin;
     p.epi = GATED ? EPI_GATED : EPI_LINEAR;
     p.out_f32 = sizeof(T) == 4;
-    p.e[0].bias = bias; p.e[0].act = d->act;
-    p.e[0].vec_bias = bias && aligned(bias, 16);
-    set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
-    set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, p.parts);
     p.err = status_word();
     FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);
     return run_product(p, st, who);

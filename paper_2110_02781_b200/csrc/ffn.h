@@ -76,6 +76,12 @@ struct Product {
 };
 ftp_status run_product(const Product& p, cudaStream_t st, const char* who);
 
+// Products of a few tokens, read from the tensors as they are (ffn_few.cu).
+constexpr int FEW_ROWS = 8, FEW_SMEM = 128 * 1024;
+bool few_tokens(long long rows, long long cin);
+ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, cudaStream_t st,
+                   const char* who);
+
 int* status_word();                         // device word that a kernel whose bounded wait ran out writes a code to
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

@@ -349,15 +349,20 @@ def _bad(who, why):
     raise FtpError(1, f"{who}: {why}")
 
 
+torch = None
+
+
 def _current():
-    """Index of the current CUDA device."""
-    import torch
+    """Index of the current CUDA device.  (torch is loaded with the first operator call.)"""
+    global torch
+    if torch is None:
+        import torch as module
+        torch = module
     return torch.cuda.current_device()
 
 
 def _raw_stream(stream, cur):
     if stream is None:
-        import torch
         return torch._C._cuda_getCurrentRawStream(cur)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
@@ -395,7 +400,6 @@ def _same_rows(who, name, t, rows, cols, dtype, cur):
 
 
 def _precision(who, t):
-    import torch
     if t.dtype is torch.bfloat16:
         return BF16
     if t.dtype is torch.float32:
@@ -404,14 +408,12 @@ def _precision(who, t):
 
 
 def _vector(who, name, t, n, cur):
-    import torch
     if t.get_device() != cur or t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() != n:
         _bad(who, f"{name} must be {n} contiguous float32 values on the current CUDA device")
     return t.data_ptr()
 
 
 def _is_image(t):
-    import torch
     return t.dtype is torch.uint8
 
 
@@ -460,7 +462,6 @@ def _workspace(who, need, ws, stream, cur):
     if need == 0:
         return None, 0, None
     if ws is None:
-        import torch
         if stream is None:
             ws = torch.empty(need, dtype=torch.uint8, device="cuda")
         else:
@@ -543,7 +544,6 @@ def _ffn_dx(who, dx, dx_addend, rows, cin, dtype, cur):
 
 def _ffn_dw(who, dw, cin, cout, dtype, cur):
     """(elements between rows, gradients are float although the tensors are bf16)."""
-    import torch
     if dw is None:
         return 0, 0
     f32 = dw.dtype is torch.float32

@@ -84,6 +84,8 @@ LINEAR = [  # rows, cin, cout, gap, off
     (16, 2048, 128, 0, 0), (31, 33, 35, 1, 1), (128, 128, 128, 0, 0), (129, 65, 129, 0, 8), (200, 1283, 517, 0, 0), (257, 320, 1280, 0, 0),
     (300, 8, 1000, 4, 2), (513, 777, 264, 0, 0)]
 
+# a few tokens: long and short reductions, strips of columns that end early, rows of w on odd addresses
+FEW = [(1, 4096, 256, 0, 0), (2, 1024, 70, 0, 0), (4, 520, 129, 0, 1), (5, 2000, 33, 8, 0), (7, 31, 300, 3, 0), (1, 30000, 40, 0, 0), (8, 9000, 72, 0, 0)]
 # enough output tiles for CTA pairs: forward, input gradient, weight gradient; odd edges, several tiles per pair
 LARGE = [(1000, 330, 2300, 0, 0), (1100, 72, 2104, 8, 0), (3001, 40, 2300, 0, 0), (1000, 2300, 330, 0, 0), (330, 1000, 2300, 0, 0), (70, 1100, 2104, 0, 8),
          (1023, 2049, 33, 0, 0), (2305, 64, 1025, 0, 0)]
@@ -94,7 +96,7 @@ def linear_case(seed, rows, cin, cout, dt, gap, off):
     return x, w
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + LARGE)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + FEW + LARGE)
 @pytest.mark.parametrize("dt,name,bias,res,keep", [(BF, "gelu", 1, 1, "full"), (BF, "none", 0, 0, None), (FP, "silu", 1, 1, "8bit"), (FP, "relu6", 0, 1, "full"),
                                                    (BF, "silu", 1, 0, None), (FP, "gelu", 1, 1, None), (BF, "relu", 0, 1, "8bit")])
 def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
@@ -181,7 +183,7 @@ def kept_pair(keep, rows, cout, dt, seed):
     return img, torch.stack([through_8_bits(ref(gu[i])) for i in range(2)])
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", GATED)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", GATED + FEW)
 @pytest.mark.parametrize("dt,name,keep", [(BF, "silu", None), (BF, "gelu", "full"), (FP, "silu", "8bit"), (FP, "none", None), (BF, "relu", "8bit"), (FP, "gelu", "full")])
 def test_gated_forward(rows, cin, cout, gap, off, dt, name, keep):
     x, wg = linear_case(30, rows, cin, cout, dt, gap, off)
