@@ -369,7 +369,7 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     p.e[0].vec_bias = bias && aligned(bias, 16);
     set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
     set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, GATED ? 2 : 1);
-    if (!given_x && few_tokens(d->rows, d->cin))
+    if (!given_x && few_tokens(d->rows, d->cin, sizeof(T) == 4, GATED ? 2 : 1))
         return ws.dry() ? FTP_OK : run_few(x, ldx, w, ldw, GATED ? 2 : 1, (int)d->rows, d->cin, d->cout, sizeof(T) == 4, p.e[0], st, who);
     if (given_x) p.A[0] = *given_x;
     else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, st, who)) return s;

@@ -77,8 +77,8 @@ struct Product {
 ftp_status run_product(const Product& p, cudaStream_t st, const char* who);
 
 // Products of a few tokens, read from the tensors as they are (ffn_few.cu).
-constexpr int FEW_ROWS = 8, FEW_SMEM = 128 * 1024;
-bool few_tokens(long long rows, long long cin);
+constexpr int FEW_SMEM = 96 * 1024;          // of it for the tokens
+bool few_tokens(long long rows, long long cin, bool f32, int products);
 ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, cudaStream_t st,
                    const char* who);
 

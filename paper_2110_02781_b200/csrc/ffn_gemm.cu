@@ -5,8 +5,8 @@
 // float tensor comes as three bf16 planes (8 mantissa bits each, 24 together) and a product of two of them as the six
 // plane products that matter; the dropped ones are below 2^-24 of the result.
 //
-// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warp 0 (one thread) streams operand tiles with TMA
-// into a ring in shared memory, warp 1 (one thread) issues the MMAs, warps 2-5 move the accumulator to shared memory.
+// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warps 0 and 2 (one thread each) stream the tiles of A and
+// of B with TMA into a ring in shared memory, warp 1 (one thread) issues the MMAs, warps 4-7 move the accumulator to shared memory.
 // The slices of one tile form a cluster: each CTA then adds up the rows rank, rank + S, ... of the tile over the
 // cluster's shared memory, always in rank order, and finishes them (bias, activation, residual, kept values), so a
 // product with few tiles still uses the whole GPU, needs no workspace, and gives the same bits every time.
@@ -19,22 +19,28 @@ namespace ffn {
 namespace {
 
 // ---- one CTA per tile and reduction slice ---------------------------------------------------------------------------
-constexpr int TILE_THREADS = 192;
-template <int BN> constexpr int TILE_STAGES = BN == 128 ? 6 : 8;
-template <int BN> constexpr uint32_t TILE_SMEM = TILE_STAGES<BN> * (128 * BK * 2 + BN * BK * 2) + 1024;
+constexpr int TILE_THREADS = 256;
+// bf16: two CTAs on an SM, one's epilogue beside the other's products; float (three operand tiles a block): one.
+// AR = 32: at most 32 rows of A are loaded, into the first 32 of the 128 rows that the MMA reads.  The other rows are whatever
+// lies behind them in shared memory (inside the allocation, see the 12 KB at its end); they only reach accumulator rows
+// that nobody reads.  A stage is then mostly B, which is what a product of a few tokens has to stream.
+template <int BN, bool F32, int AR> constexpr uint32_t TILE_STAGE = AR * BK * 2 + BN * BK * 2;
+template <int BN, bool F32, int AR> constexpr int TILE_STAGES = F32 ? (BN == 128 ? 6 : 8) : AR == 32 ? (BN == 128 ? 4 : 8) : (BN == 128 ? 3 : 4);
+template <int BN, bool F32, int AR> constexpr uint32_t TILE_SMEM = TILE_STAGES<BN, F32, AR> * TILE_STAGE<BN, F32, AR> + (128 - AR) * 128 + 1024;
 
 // AMN / BMN: the operand is MN-major.  EPI_GATED: the tile's first BN / 2 columns are A B[0], the others A B[1].
-template <typename T, int BN, bool AMN, bool BMN, int EPI>
-__global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
+template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR>
+__global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 1 : 2) ffn_tile_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
                                                                    const __grid_constant__ CUtensorMap mapB0, const __grid_constant__ CUtensorMap mapB1,
                                                                    const __grid_constant__ KArgs p) {
-    constexpr int STAGES = TILE_STAGES<BN>;
     constexpr bool CHUNKED = sizeof(T) == 4;
+    constexpr int STAGES = TILE_STAGES<BN, CHUNKED, AR>;
     constexpr int BUFS = CHUNKED ? 2 : 1;                            // accumulators in tensor memory
-    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = AR * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
     constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;             // output columns of a tile
     constexpr int PITCH = BN + 4;                                    // floats between rows of the staged accumulator: 16-byte accesses of 8 lanes hit all banks
-    static_assert(128 * PITCH * 4 <= STAGES * STAGE_BYTES, "the staged accumulator reuses the operand ring");
+    static_assert(AR == 128 || (!AMN && !CHUNKED), "");
+    static_assert(AR * PITCH * 4 <= STAGES * STAGE_BYTES, "the staged accumulator reuses the operand ring");
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS];
@@ -72,29 +78,30 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
     const uint32_t tmem = tmem_base;
     grid_dep_sync();
 
-    if (warp == 0) {
-        if (lane == 0) {
-            // ---- producer ----
-            int it = 0;
-            Slot<STAGES> sl;
-            bool ok = true;
-            for (int kb = kb0; kb < kb1 && ok; ++kb) {
-                const int part = kb / p.kb_part, k = (kb - part * p.kb_part) * BK;
-                const CUtensorMap* ma = part ? &mapA1 : &mapA0;
-                const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
-                for (int z = p.np - 1; z >= 0; --z, ++it, sl.next()) {
-                    const int s = sl.s;
-                    if (!wait_for(empty0 + 8 * s, sl.parity ^ 1, p.err, 1)) { ok = false; break; }          // at once for a slot never used
-                    const uint32_t sa = smem_u32(smem + s * STAGE_BYTES), sb = sa + A_BYTES, bar = full0 + 8 * s;
-                    mbar_expect_tx(bar, (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0));
-                    if (z < p.pa) {
-                        if (AMN) {
+    if (warp == 0 || warp == 2) {
+        // ---- producers: A by warp 0, B by warp 2 ----
+        Slot<STAGES> sl;
+        const uint32_t ring = smem_u32(smem);
+        bool ok = true;
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+            const int part = kb >= p.kb_part, k = (kb - part * p.kb_part) * BK;
+            const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+            const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
+            for (int z = p.np - 1; z >= 0; --z, sl.next()) {
+                ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = full0 + 8 * sl.s;
+                    if (warp == 0) {
+                        mbar_expect_tx(bar, (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0));
+                        if (z < p.pa) {
+                            if (AMN) {
 #pragma unroll
-                            for (int t = 0; t < 2; ++t) tma_load_3d(sa + t * SLAB, ma, (int)m0 + 64 * t, k, z, bar);
-                        } else
-                            tma_load_3d(sa, ma, k, (int)m0, z, bar);
-                    }
-                    if (z < p.pb) {
+                                for (int t = 0; t < 2; ++t) tma_load_3d(sa + t * SLAB, ma, (int)m0 + 64 * t, k, z, bar);
+                            } else
+                                tma_load_3d(sa, ma, k, (int)m0, z, bar);
+                        }
+                    } else if (z < p.pb) {
                         if (EPI == EPI_GATED) {
 #pragma unroll
                             for (int t = 0; t < BN / 64; ++t)
@@ -106,18 +113,17 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
                             tma_load_3d(sb, mb, k, n0, z, bar);
                     }
                 }
-            }
-            if (!ok || *((volatile int*)p.err) != 0) {
-                // error path: let the copies already issued land before the block's memory is released
-                for (int k = max(0, it - STAGES); k < it; ++k) {
-                    const unsigned long long t0 = gtime();
-                    while (!mbar_test(full0 + 8 * (k % STAGES), (k / STAGES) & 1) && gtime() - t0 < 1000000ull) __nanosleep(128);
-                }
+                __syncwarp();
             }
         }
+        if (!ok) {
+            // error path: time for the copies already issued to land before the block's memory is released
+            const unsigned long long t0 = gtime();
+            while (gtime() - t0 < 1000000ull) __nanosleep(1000);
+        }
     } else if (warp == 1) {
-        mma_warp<1, BN, STAGES, STAGE_BYTES, AMN, BMN, CHUNKED, BUFS>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, 1, kb1 - kb0, p);
-    } else {
+        mma_warp<1, BN, STAGES, STAGE_BYTES, A_BYTES, AMN, BMN, CHUNKED, BUFS>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, 1, kb1 - kb0, p);
+    } else if (warp >= 4 && (AR == 128 || (warp & 3) == 0)) {
         // ---- accumulator -> shared memory (the ring is free once the last MMA has completed) ----
         const int q = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
@@ -199,21 +205,24 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ffn_tile_kernel(const __grid_
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
-template <typename T, int BN, bool AMN, bool BMN, int EPI>
+template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR>
 ftp_status launch_tile(const Product& p, KArgs& k, int S, cudaStream_t st, const char* who) {
     Maps m;
-    FTP_REQUIRE(make_maps(m, p, 128, BN), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
-    auto kern = ffn_tile_kernel<T, BN, AMN, BMN, EPI>;
+    FTP_REQUIRE(make_maps(m, p, AR, BN), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
+    auto kern = ffn_tile_kernel<T, BN, AMN, BMN, EPI, AR>;
     static std::atomic<unsigned long long> asked{0};
-    cudaError_t e = allow_smem(asked, kern, (int)TILE_SMEM<BN>);
-    if (e == cudaSuccess) e = launch_cluster(kern, (unsigned)((long long)k.tiles_m * k.tiles_n * k.parts_n * S), TILE_THREADS, TILE_SMEM<BN>, S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
+    cudaError_t e = allow_smem(asked, kern, (int)TILE_SMEM<BN, sizeof(T) == 4, AR>);
+    if (e == cudaSuccess) e = launch_cluster(kern, dim3((unsigned)((long long)k.tiles_m * k.tiles_n * k.parts_n * S)), TILE_THREADS, TILE_SMEM<BN, sizeof(T) == 4, AR>, S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
 
 template <int BN, bool AMN, bool BMN, int EPI>
 ftp_status tile_typed(const Product& p, KArgs& k, int S, cudaStream_t st, const char* who) {
-    return p.out_f32 ? launch_tile<float, BN, AMN, BMN, EPI>(p, k, S, st, who) : launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI>(p, k, S, st, who);
+    if (p.out_f32) return launch_tile<float, BN, AMN, BMN, EPI, 128>(p, k, S, st, who);
+    if constexpr (!AMN)
+        if (p.M <= 32) return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, 32>(p, k, S, st, who);
+    return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, 128>(p, k, S, st, who);
 }
 
 }  // namespace
@@ -244,10 +253,11 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who) {
     const bool narrow = p.epi != EPI_GATED && (p.N <= 64 || tiles(outc128) < SMS);
     const int outc = narrow ? 64 : outc128;
     k.tiles_n = (p.N + outc - 1) / outc;
-    // slices of the reduction: as many as fill the SMs once, each at least four blocks long
+    // slices of the reduction: as many as fill the SMs once (bf16: with two CTAs each), each at least four blocks long
+    const int room = p.out_f32 ? SMS : 2 * SMS;
     const long long t = tiles(outc), blocks = (long long)k.kb_part * k.parts_k * k.np * k.np;
     int S = 1;
-    while (S < 8 && t * S * 2 <= SMS && blocks / (S * 2) >= 4 && (long long)k.kb_part * k.parts_k >= S * 2) S *= 2;
+    while (S < 8 && t * S * 2 <= room && blocks / (S * 2) >= 4 && (long long)k.kb_part * k.parts_k >= S * 2) S *= 2;
     FTP_REQUIRE(t * S < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     if (p.epi == EPI_GATED) return tile_typed<128, false, true, EPI_GATED>(p, k, S, st, who);
     if (p.epi == EPI_LINEAR) return narrow ? tile_typed<64, false, true, EPI_LINEAR>(p, k, S, st, who) : tile_typed<128, false, true, EPI_LINEAR>(p, k, S, st, who);

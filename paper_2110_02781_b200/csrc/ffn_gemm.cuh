@@ -174,10 +174,10 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
 // whole warp walks the loop and one elected thread issues, so that descriptors and addresses stay in uniform registers: with the
 // loop inside a single-thread branch four MMAs and a commit took 1300 cycles to issue, more than they take to run.
 //   full / empty: ring barriers; accf / acce: accumulator complete / read, BUFS of them in turn.
-template <int CG, int BN, int STAGES, uint32_t STAGE_BYTES, bool AMN, bool BMN, bool CHUNKED, int BUFS>
+template <int CG, int BN, int STAGES, uint32_t STAGE_BYTES, uint32_t A_BYTES, bool AMN, bool BMN, bool CHUNKED, int BUFS>
 __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t empty0, uint32_t accf0, uint32_t acce0, uint32_t tmem, int tiles, int blocks,
                                          const KArgs& p) {
-    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2;
+    constexpr uint32_t SLAB = 64 * BK * 2;
     constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
                                ((uint32_t)(CG * 128 >> 4) << 24);
     const uint64_t a0 = AMN ? desc_mn(ring, SLAB) : umma_desc_k_sw128(ring), b0 = BMN ? desc_mn(ring + A_BYTES, SLAB) : umma_desc_k_sw128(ring + A_BYTES);
@@ -290,9 +290,9 @@ cudaError_t allow_smem(std::atomic<unsigned long long>& done, K kern, int bytes)
 }
 
 template <typename... KA, typename... A>
-cudaError_t launch_cluster(void (*kern)(KA...), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, A&&... args) {
+cudaError_t launch_cluster(void (*kern)(KA...), dim3 grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, A&&... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     } else if (warp == 1) {
         if (rank == 0) {
             const int mine = cluster < tiles ? (tiles - cluster + clusters - 1) / clusters : 0;
-            ok = mma_warp<2, BN, STAGES, STAGE_BYTES, AMN, BMN, CHUNKED, 2>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, mine, all_kb, p);
+            ok = mma_warp<2, BN, STAGES, STAGE_BYTES, A_BYTES, AMN, BMN, CHUNKED, 2>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, mine, all_kb, p);
         }
     } else if (warp >= 4) {
         // ---- epilogue ----
@@ -406,7 +406,7 @@ ftp_status launch_pair(const Product& p, const KArgs& k, cudaStream_t st, const 
     cudaError_t e = allow_smem(asked, kern, (int)PAIR_SMEM<BN>);
     const long long tiles = (long long)k.tiles_m * k.tiles_n * k.parts_n;
     FTP_REQUIRE(tiles < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-    if (e == cudaSuccess) e = launch_cluster(kern, 2 * (unsigned)std::min<long long>(tiles, SMS / 2), PAIR_THREADS, PAIR_SMEM<BN>, 2, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
+    if (e == cudaSuccess) e = launch_cluster(kern, dim3(2 * (unsigned)std::min<long long>(tiles, SMS / 2)), PAIR_THREADS, PAIR_SMEM<BN>, 2, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }

@@ -7,7 +7,7 @@ F = pytest.importorskip("paper_2110_02781_b200")
 FAKE = 1 << 20                 # a 256-byte aligned address that is never dereferenced: every call below is refused on the host
 
 
-def desc(rows=12, cin=64, cout=48, prec=1, act=0, stash=0, x8=0, f32=0, unaligned=0, ldx=0, ldw=0, ldy=0, ldr=0, lddx=0, lddw=0):
+def desc(rows=40, cin=64, cout=48, prec=1, act=0, stash=0, x8=0, f32=0, unaligned=0, ldx=0, ldw=0, ldy=0, ldr=0, lddx=0, lddw=0):
     return F.FfnDesc(rows, cin, cout, prec, act, stash, x8, f32, unaligned, ldx, ldw, ldy, ldr, lddx, lddw)
 
 
@@ -37,16 +37,16 @@ def test_workspace_sizes():
     lin, gat = F.lib.ftp_linear_workspace_bytes, F.lib.ftp_gated_workspace_bytes
     assert size(lin, desc(), 0) == (0, 0) and size(gat, desc(), 0) == (0, 0)                      # bf16 read in place
     assert size(lin, desc(rows=0), 1) == (0, 0)
-    assert size(lin, desc(ldx=65), 0)[1] == up(12 * 64 * 2, 256)                                   # a copy of x
+    assert size(lin, desc(ldx=65), 0)[1] == up(40 * 64 * 2, 256)                                   # a copy of x
     assert size(lin, desc(cout=47), 0)[1] == up(64 * 48 * 2, 256)                                 # a copy of w
-    assert size(lin, desc(unaligned=1), 0)[1] == up(12 * 64 * 2, 256) + up(64 * 48 * 2, 256)
-    assert size(lin, desc(prec=0), 0)[1] == up(3 * 12 * 64 * 2, 256) + up(3 * 64 * 48 * 2, 256)    # three planes of each
+    assert size(lin, desc(unaligned=1), 0)[1] == up(40 * 64 * 2, 256) + up(64 * 48 * 2, 256)
+    assert size(lin, desc(prec=0), 0)[1] == up(3 * 40 * 64 * 2, 256) + up(3 * 64 * 48 * 2, 256)    # three planes of each
     assert size(lin, desc(), 1)[1] == up(48 * 4, 256)                                             # sums of the bias gradient
-    assert size(lin, desc(act=3, stash=1), 1)[1] == up(12 * 48 * 2, 256) + up(48 * 4, 256)
-    assert size(gat, desc(act=4, stash=1), 1)[1] == 2 * up(12 * 48 * 2, 256)
-    assert size(gat, desc(act=4, stash=0), 1)[1] == up(2 * 12 * 48 * 2, 256) + 2 * up(12 * 48 * 2, 256)
-    assert size(lin, desc(x8=1), 1)[1] == up(12 * 64 * 2, 256) + up(48 * 4, 256)
-    assert size(lin, desc(rows=8, prec=0, ldx=65), 0) == (0, 0)                                   # a few tokens: read as they are
+    assert size(lin, desc(act=3, stash=1), 1)[1] == up(40 * 48 * 2, 256) + up(48 * 4, 256)
+    assert size(gat, desc(act=4, stash=1), 1)[1] == 2 * up(40 * 48 * 2, 256)
+    assert size(gat, desc(act=4, stash=0), 1)[1] == up(2 * 40 * 48 * 2, 256) + 2 * up(40 * 48 * 2, 256)
+    assert size(lin, desc(x8=1), 1)[1] == up(40 * 64 * 2, 256) + up(48 * 4, 256)
+    assert size(lin, desc(rows=4, prec=0, ldx=65), 0) == (0, 0)                                   # a few tokens: read as they are
     big = size(gat, desc(rows=1 << 20, cin=8192, cout=16384, prec=0, stash=2, act=4), 1)
     assert big[0] == 0 and big[1] > 1 << 36
 

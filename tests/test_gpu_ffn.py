@@ -85,7 +85,9 @@ LINEAR = [  # rows, cin, cout, gap, off
     (300, 8, 1000, 4, 2), (513, 777, 264, 0, 0)]
 
 # a few tokens: long and short reductions, strips of columns that end early, rows of w on odd addresses
-FEW = [(1, 4096, 256, 0, 0), (2, 1024, 70, 0, 0), (4, 520, 129, 0, 1), (5, 2000, 33, 8, 0), (7, 31, 300, 3, 0), (1, 30000, 40, 0, 0), (8, 9000, 72, 0, 0)]
+FEW = [(1, 4096, 256, 0, 0), (2, 1024, 70, 0, 0), (4, 520, 129, 0, 1), (5, 2000, 33, 8, 0), (7, 31, 300, 3, 0), (1, 30000, 40, 0, 0), (8, 9000, 72, 0, 0),
+       (13, 600, 100, 0, 0), (16, 1025, 36, 0, 1), (17, 300, 65, 0, 0), (29, 2100, 40, 4, 0), (32, 64, 33, 0, 0), (30, 9000, 24, 0, 0), (1, 2000, 72, 0, 0),
+       (2, 640, 64, 8, 8), (3, 1300, 200, 0, 0), (4, 130, 1000, 0, 0), (6, 2048, 104, 0, 0), (47, 500, 68, 0, 0), (48, 72, 260, 0, 0), (49, 72, 260, 0, 0)]
 # enough output tiles for CTA pairs: forward, input gradient, weight gradient; odd edges, several tiles per pair
 LARGE = [(1000, 330, 2300, 0, 0), (1100, 72, 2104, 8, 0), (3001, 40, 2300, 0, 0), (1000, 2300, 330, 0, 0), (330, 1000, 2300, 0, 0), (70, 1100, 2104, 0, 8),
          (1023, 2049, 33, 0, 0), (2305, 64, 1025, 0, 0)]
