@@ -349,21 +349,27 @@ def _bad(who, why):
     raise FtpError(1, f"{who}: {why}")
 
 
-torch = None
+torch = _device = _raw_current = None
+
+
+def _load_torch():
+    """torch is loaded with the first operator call."""
+    global torch, _device, _raw_current
+    import torch as module
+    module.cuda.init()
+    torch, _device, _raw_current = module, module._C._cuda_getDevice, module._C._cuda_getCurrentRawStream
 
 
 def _current():
-    """Index of the current CUDA device.  (torch is loaded with the first operator call.)"""
-    global torch
+    """Index of the current CUDA device."""
     if torch is None:
-        import torch as module
-        torch = module
-    return torch.cuda.current_device()
+        _load_torch()
+    return _device()
 
 
 def _raw_stream(stream, cur):
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(cur)
+        return _raw_current(cur)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -442,25 +448,30 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-_PLANS = {}            # sizes and options of a call -> its descriptor and workspace size
+# What a call's checks depend on (device, types, shapes, gaps, alignment, options: nothing of an address but whether it
+# lies on 16 bytes, nothing of the values) -> its descriptor and workspace size, so that a call like an earlier one is not
+# checked again
+_PLANS = {}
 
 
-def _plan(size_of, backward, *fields):
-    key = (size_of is lib.ftp_gated_workspace_bytes, backward) + fields
-    p = _PLANS.get(key)
-    if p is None:
-        d, n = FfnDesc(*fields), _sz()
-        _check(size_of(C.byref(d), backward, C.byref(n)))
-        if len(_PLANS) >= 4096:
-            _PLANS.clear()
-        p = _PLANS[key] = (C.byref(d), n.value)
+def _sig(t):
+    return None if t is None else (t.dtype, t.get_device(), t.shape, t.stride())
+
+
+def _plan(key, size_of, backward, *fields):
+    d, n = FfnDesc(*fields), _sz()
+    _check(size_of(C.byref(d), backward, C.byref(n)))
+    if len(_PLANS) >= 4096:
+        _PLANS.clear()
+    p = _PLANS[key] = (C.byref(d), n.value)
     return p
+
+
+_NO_WS = (None, 0, None)
 
 
 def _workspace(who, need, ws, stream, cur):
     """(address, bytes, tensor to keep alive until the launches are queued)."""
-    if need == 0:
-        return None, 0, None
     if ws is None:
         if stream is None:
             ws = torch.empty(need, dtype=torch.uint8, device="cuda")
@@ -478,22 +489,35 @@ def ftp_checkpoint_bytes(rows, cols, parts=1):
     return n.value
 
 
+def _plan_checkpoint(key, cur, who, name, x, image, part):
+    cols = x.shape[-1]
+    prec = _precision(who, x)
+    rows, ld = _rows(who, name, x, cols, x.dtype, cur)
+    _image(who, "image", image, rows, cols, part + 1, cur)
+    if len(_PLANS) >= 4096:
+        _PLANS.clear()
+    p = _PLANS[key] = (rows, cols, ld, prec)
+    return p
+
+
 def ftp_checkpoint_pack(x, image, part=0, stream=None):
     """8-bit image of x (tokens x channels) into part `part` of `image`; see include/ftpipe.h for the format."""
-    who, cur, cols = "checkpoint_pack", _current(), x.shape[-1]
-    prec = _precision(who, x)
-    rows, ld = _rows(who, "x", x, cols, x.dtype, cur)
-    _image(who, "image", image, rows, cols, part + 1, cur)
-    _check(lib.ftp_checkpoint_pack(x.data_ptr(), rows, cols, ld, prec, image.data_ptr(), part, _raw_stream(stream, cur)))
+    cur = _current()
+    key = (4, cur, part, x.dtype, x.get_device(), x.shape, x.stride(), _sig(image))
+    rows, cols, ld, prec = _PLANS.get(key) or _plan_checkpoint(key, cur, "checkpoint_pack", "x", x, image, part)
+    st = lib.ftp_checkpoint_pack(x.data_ptr(), rows, cols, ld, prec, image.data_ptr(), part, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
 def ftp_checkpoint_unpack(image, out, part=0, stream=None):
     """The values of part `part` of an 8-bit image into out (tokens x channels)."""
-    who, cur, cols = "checkpoint_unpack", _current(), out.shape[-1]
-    prec = _precision(who, out)
-    rows, ld = _rows(who, "out", out, cols, out.dtype, cur)
-    _image(who, "image", image, rows, cols, part + 1, cur)
-    _check(lib.ftp_checkpoint_unpack(image.data_ptr(), part, rows, cols, prec, out.data_ptr(), ld, _raw_stream(stream, cur)))
+    cur = _current()
+    key = (5, cur, part, out.dtype, out.get_device(), out.shape, out.stride(), _sig(image))
+    rows, cols, ld, prec = _PLANS.get(key) or _plan_checkpoint(key, cur, "checkpoint_unpack", "out", out, image, part)
+    st = lib.ftp_checkpoint_unpack(image.data_ptr(), part, rows, cols, prec, out.data_ptr(), ld, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
 def _weight(who, w, dtype, cur):
@@ -511,20 +535,31 @@ def _weight_pair(who, a, b, dtype, cur):
     return cin, cout, ld
 
 
-def ftp_linear_forward(x, w, y, bias=None, residual=None, act=ACT_NONE, stash=None, ws=None, stream=None):
-    """y = act(x w + bias) + residual.  stash: keeps x w + bias, in a tensor like y or as an 8-bit image (uint8)."""
-    who, cur, dt = "linear_forward", _current(), x.dtype
+def _plan_linear_forward(key, cur, x, w, y, bias, residual, act, stash, off):
+    who, dt = "linear_forward", x.dtype
     prec = _precision(who, x)
     cin, cout, ldw = _weight(who, w, dt, cur)
     rows, ldx = _rows(who, "x", x, cin, dt, cur)
     ldy = _same_rows(who, "y", y, rows, cout, dt, cur)
     ldr = 0 if residual is None else _same_rows(who, "residual", residual, rows, cout, dt, cur)
     kind = _kept(who, stash, rows, cout, 1, dt, cur)
-    pb = None if bias is None else _vector(who, "bias", bias, cout, cur)
+    if bias is not None:
+        _vector(who, "bias", bias, cout, cur)
+    return _plan(key, lib.ftp_linear_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int(off), ldx, ldw, ldy, ldr, 0, 0)
+
+
+def ftp_linear_forward(x, w, y, bias=None, residual=None, act=ACT_NONE, stash=None, ws=None, stream=None):
+    """y = act(x w + bias) + residual.  stash: keeps x w + bias, in a tensor like y or as an 8-bit image (uint8)."""
+    cur = _current()
     px, pw = x.data_ptr(), w.data_ptr()
-    d, need = _plan(lib.ftp_linear_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int((px | pw) & 15 != 0), ldx, ldw, ldy, ldr, 0, 0)
-    pws, nws, keep = _workspace(who, need, ws, stream, cur)
-    _check(lib.ftp_linear_forward(d, px, pw, pb, _addr(residual), y.data_ptr(), _addr(stash), pws, nws, _raw_stream(stream, cur)))
+    off = (px | pw) & 15 != 0
+    key = (0, cur, act, off, x.dtype, x.get_device(), x.shape, x.stride(), w.dtype, w.get_device(), w.shape, w.stride(), y.dtype, y.get_device(), y.shape,
+           y.stride(), _sig(bias), _sig(residual), _sig(stash))
+    d, need = _PLANS.get(key) or _plan_linear_forward(key, cur, x, w, y, bias, residual, act, stash, off)
+    pws, nws, keep = _workspace("linear_forward", need, ws, stream, cur) if need else _NO_WS
+    st = lib.ftp_linear_forward(d, px, pw, _addr(bias), _addr(residual), y.data_ptr(), _addr(stash), pws, nws, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
 def _ffn_input(who, x, rows, cin, dtype, cur):
@@ -550,10 +585,8 @@ def _ffn_dw(who, dw, cin, cout, dtype, cur):
     return _same_rows(who, "dw", dw, cin, cout, torch.float32 if f32 else dtype, cur), int(f32 and dtype is torch.bfloat16)
 
 
-def ftp_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, stash=None, dx_addend=None, ws=None, stream=None):
-    """Gradients of ftp_linear_forward from dy: dx = dz w^T + dx_addend, dw = x^T dz, dbias = column sums of
-    dz = dy act'(stash).  x: the input, or its 8-bit image; dw: x's type or float32.  Each output may be left out."""
-    who, cur, dt = "linear_backward", _current(), dy.dtype
+def _plan_linear_backward(key, cur, x, w, dy, dx, dw, dbias, act, stash, dx_addend, off):
+    who, dt = "linear_backward", dy.dtype
     prec = _precision(who, dy)
     cin, cout, ldw = _weight(who, w, dt, cur)
     rows, ldy = _rows(who, "dy", dy, cout, dt, cur)
@@ -561,33 +594,53 @@ def ftp_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, st
     lddx, ldr = _ffn_dx(who, dx, dx_addend, rows, cin, dt, cur)
     lddw, f32 = _ffn_dw(who, dw, cin, cout, dt, cur)
     kind = _kept(who, stash, rows, cout, 1, dt, cur)
-    pb = None if dbias is None else _vector(who, "dbias", dbias, cout, cur)
+    if dbias is not None:
+        _vector(who, "dbias", dbias, cout, cur)
+    return _plan(key, lib.ftp_linear_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(off), ldx, ldw, ldy, ldr, lddx, lddw)
+
+
+def ftp_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, act=ACT_NONE, stash=None, dx_addend=None, ws=None, stream=None):
+    """Gradients of ftp_linear_forward from dy: dx = dz w^T + dx_addend, dw = x^T dz, dbias = column sums of
+    dz = dy act'(stash).  x: the input, or its 8-bit image; dw: x's type or float32.  Each output may be left out."""
+    cur = _current()
     px, pw, pdy = _addr(x), w.data_ptr(), dy.data_ptr()
-    d, need = _plan(lib.ftp_linear_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(((px or 0) | pw | pdy) & 15 != 0), ldx, ldw, ldy, ldr, lddx,
-                    lddw)
-    pws, nws, keep = _workspace(who, need, ws, stream, cur)
-    _check(lib.ftp_linear_backward(d, px, pw, _addr(stash), pdy, _addr(dx_addend), _addr(dx), _addr(dw), pb, pws, nws, _raw_stream(stream, cur)))
+    off = ((px or 0) | pw | pdy) & 15 != 0
+    key = (1, cur, act, off, _sig(x), w.dtype, w.get_device(), w.shape, w.stride(), dy.dtype, dy.get_device(), dy.shape, dy.stride(), _sig(dx), _sig(dw),
+           _sig(dbias), _sig(stash), _sig(dx_addend))
+    d, need = _PLANS.get(key) or _plan_linear_backward(key, cur, x, w, dy, dx, dw, dbias, act, stash, dx_addend, off)
+    pws, nws, keep = _workspace("linear_backward", need, ws, stream, cur) if need else _NO_WS
+    st = lib.ftp_linear_backward(d, px, pw, _addr(stash), pdy, _addr(dx_addend), _addr(dx), _addr(dw), _addr(dbias), pws, nws, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
-def ftp_gated_forward(x, w_gate, w_up, h=None, act=ACT_SILU, stash=None, ws=None, stream=None):
-    """h = act(x w_gate) * (x w_up).  stash: keeps both products, in a tensor (2, rows, cout) or as an 8-bit image of two
-    parts (uint8)."""
-    who, cur, dt = "gated_forward", _current(), x.dtype
+def _plan_gated_forward(key, cur, x, w_gate, w_up, h, act, stash, off):
+    who, dt = "gated_forward", x.dtype
     prec = _precision(who, x)
     cin, cout, ldw = _weight_pair(who, w_gate, w_up, dt, cur)
     rows, ldx = _rows(who, "x", x, cin, dt, cur)
     ldy = 0 if h is None else _same_rows(who, "h", h, rows, cout, dt, cur)
     kind = _kept(who, stash, rows, cout, 2, dt, cur)
+    return _plan(key, lib.ftp_gated_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int(off), ldx, ldw, ldy, 0, 0, 0)
+
+
+def ftp_gated_forward(x, w_gate, w_up, h=None, act=ACT_SILU, stash=None, ws=None, stream=None):
+    """h = act(x w_gate) * (x w_up).  stash: keeps both products, in a tensor (2, rows, cout) or as an 8-bit image of two
+    parts (uint8)."""
+    cur = _current()
     px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
-    d, need = _plan(lib.ftp_gated_workspace_bytes, 0, rows, cin, cout, prec, act, kind, 0, 0, int((px | pg | pu) & 15 != 0), ldx, ldw, ldy, 0, 0, 0)
-    pws, nws, keep = _workspace(who, need, ws, stream, cur)
-    _check(lib.ftp_gated_forward(d, px, pg, pu, _addr(h), _addr(stash), pws, nws, _raw_stream(stream, cur)))
+    off = (px | pg | pu) & 15 != 0
+    key = (2, cur, act, off, x.dtype, x.get_device(), x.shape, x.stride(), w_gate.dtype, w_gate.get_device(), w_gate.shape, w_gate.stride(), _sig(w_up), _sig(h),
+           _sig(stash))
+    d, need = _PLANS.get(key) or _plan_gated_forward(key, cur, x, w_gate, w_up, h, act, stash, off)
+    pws, nws, keep = _workspace("gated_forward", need, ws, stream, cur) if need else _NO_WS
+    st = lib.ftp_gated_forward(d, px, pg, pu, _addr(h), _addr(stash), pws, nws, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
-def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, act=ACT_SILU, stash=None, dx_addend=None, ws=None, stream=None):
-    """Gradients of ftp_gated_forward from dh.  x: the input, or its 8-bit image; stash: what the forward pass kept (None:
-    both products are computed again from x); dw_gate, dw_up: x's type or float32.  dx or the pair may be left out."""
-    who, cur, dt = "gated_backward", _current(), dh.dtype
+def _plan_gated_backward(key, cur, x, w_gate, w_up, dh, dx, dw_gate, dw_up, act, stash, dx_addend, off):
+    who, dt = "gated_backward", dh.dtype
     prec = _precision(who, dh)
     if (dw_gate is None) != (dw_up is None):
         _bad(who, "both weight gradients or neither")
@@ -599,12 +652,23 @@ def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, a
     if dw_up is not None and _ffn_dw(who, dw_up, cin, cout, dt, cur) != (lddw, f32):
         _bad(who, "both weight gradients must have one type and one gap between rows")
     kind = _kept(who, stash, rows, cout, 2, dt, cur)
+    return _plan(key, lib.ftp_gated_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(off), ldx, ldw, ldy, ldr, lddx, lddw)
+
+
+def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, act=ACT_SILU, stash=None, dx_addend=None, ws=None, stream=None):
+    """Gradients of ftp_gated_forward from dh.  x: the input, or its 8-bit image; stash: what the forward pass kept (None:
+    both products are computed again from x); dw_gate, dw_up: x's type or float32.  dx or the pair may be left out."""
+    cur = _current()
     px, pg, pu = _addr(x), w_gate.data_ptr(), w_up.data_ptr()
-    d, need = _plan(lib.ftp_gated_workspace_bytes, 1, rows, cin, cout, prec, act, kind, x8, f32, int(((px or 0) | pg | pu) & 15 != 0), ldx, ldw, ldy, ldr, lddx,
-                    lddw)
-    pws, nws, keep = _workspace(who, need, ws, stream, cur)
-    _check(lib.ftp_gated_backward(d, px, pg, pu, _addr(stash), dh.data_ptr(), _addr(dx_addend), _addr(dx), _addr(dw_gate), _addr(dw_up), pws, nws,
-                                  _raw_stream(stream, cur)))
+    off = ((px or 0) | pg | pu) & 15 != 0
+    key = (3, cur, act, off, _sig(x), w_gate.dtype, w_gate.get_device(), w_gate.shape, w_gate.stride(), _sig(w_up), dh.dtype, dh.get_device(), dh.shape,
+           dh.stride(), _sig(dx), _sig(dw_gate), _sig(dw_up), _sig(stash), _sig(dx_addend))
+    d, need = _PLANS.get(key) or _plan_gated_backward(key, cur, x, w_gate, w_up, dh, dx, dw_gate, dw_up, act, stash, dx_addend, off)
+    pws, nws, keep = _workspace("gated_backward", need, ws, stream, cur) if need else _NO_WS
+    st = lib.ftp_gated_backward(d, px, pg, pu, _addr(stash), dh.data_ptr(), _addr(dx_addend), _addr(dx), _addr(dw_gate), _addr(dw_up), pws, nws,
+                                _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
 def ftp_check_op_status(stream=None):
