@@ -88,141 +88,345 @@ __device__ __forceinline__ void store_planes(bf16* p, long long plane, int plane
     }
 }
 
+// Kernels that walk a matrix in groups of eight columns: EIGHT_U groups per thread and trip, their loads in flight together;
+// group numbers have 32 bits (larger matrices are cut into launches of whole rows, see by_rows).
+constexpr int EIGHT_U = 4;
+struct Groups { unsigned total, per_row; };
+template <typename F> __device__ __forceinline__ void group_at(const Groups& g, unsigned i, F&& f) {
+    const unsigned r = i / g.per_row;
+    f((long long)r, (int)(i - r * g.per_row) * 8);
+}
+
 // ---- operand planes: copies of bf16 rows at an aligned pitch, or the three planes of float rows ----
 template <typename T>
-__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ x, long long rows, int cols, long long ld, bool vec, bf16* __restrict__ out,
+__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, bool vec, bf16* __restrict__ out,
                                                      long long plane, int planes) {
     grid_dep_sync();
-    const int groups = (cols + 7) / 8;
-    const long long total = rows * groups, pitch = 8ll * groups;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long r = i / groups;
-        const int c = (int)(i - r * groups) * 8;
-        float v[8];
-        load8(x + r * ld + c, cols - c, vec, v);
-        store_planes(out + r * pitch + c, plane, planes, v);
+    const long long pitch = 8ll * g.per_row;
+    for (unsigned i0 = blockIdx.x * 256 * EIGHT_U + threadIdx.x; i0 < g.total; i0 += gridDim.x * 256 * EIGHT_U) {
+        float v[EIGHT_U][8];
+#pragma unroll
+        for (int u = 0; u < EIGHT_U; ++u)
+            if (i0 + u * 256 < g.total) group_at(g, i0 + u * 256, [&](long long r, int c) { load8(x + r * ld + c, cols - c, vec, v[u]); });
+#pragma unroll
+        for (int u = 0; u < EIGHT_U; ++u)
+            if (i0 + u * 256 < g.total) group_at(g, i0 + u * 256, [&](long long r, int c) { store_planes(out + r * pitch + c, plane, planes, v[u]); });
     }
 }
 
 // ---- 8-bit images ----
-// A thread holds eight columns, four neighbouring threads a block of 32.
+// Sixteen values as they are in memory, zeros behind `valid`; vec: rows on 16 bytes.
+template <typename T> struct Raw16 { uint4 q[sizeof(T)]; };
 template <typename T>
-__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, long long rows, int cols, long long ld, bool vec, const Image im) {
-    grid_dep_sync();
-    const int groups = (int)(im.pitch / 8);                          // a multiple of 4: a block never straddles the end of a row
-    const long long total = rows * groups;
-    for (long long i0 = blockIdx.x * 256ll; i0 < total; i0 += (long long)gridDim.x * 256) {
-        const long long i = i0 + threadIdx.x;
-        const bool on = i < total;
-        const long long r = on ? i / groups : 0;
-        const int c = on ? (int)(i - r * groups) * 8 : 0;
-        float v[8];
-        load8(x + r * ld + c, on ? max(0, cols - c) : 0, vec, v);
-        unsigned top = 0;
+__device__ __forceinline__ Raw16<T> fetch16(const T* p, int valid, bool vec) {
+    Raw16<T> r;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const unsigned e = img_exp(top);
-        const float inv = img_inv(e);
-        if (on) {
-            int q[8];
+    for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (vec && valid >= 16) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) q[k] = img_code(v[k], inv);
-            *reinterpret_cast<uint2*>(im.q + r * im.pitch + c) = make_uint2(pack_codes(q[0], q[1], q[2], q[3]), pack_codes(q[4], q[5], q[6], q[7]));
-            if ((threadIdx.x & 3) == 0) im.e[r * (im.pitch / IMG_BLOCK) + c / IMG_BLOCK] = (uint8_t)e;
+        for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
+    } else {
+        T* e = reinterpret_cast<T*>(r.q);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) if (k < valid) e[k] = p[k];
+    }
+    return r;
+}
+__device__ __forceinline__ unsigned top16(const Raw16<float>& r) {   // bits of the largest magnitude, as a float's
+    unsigned m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = max(max(max(r.q[k].x & 0x7fffffffu, r.q[k].y & 0x7fffffffu), max(r.q[k].z & 0x7fffffffu, r.q[k].w & 0x7fffffffu)), m);
+    return m;
+}
+__device__ __forceinline__ unsigned top16(const Raw16<bf16>& r) {
+    unsigned m = 0;                                                  // two at a time: magnitudes of bf16 compare as 16-bit integers
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        m = __vmaxu2(m, __vmaxu2(r.q[k].x & 0x7fff7fffu, r.q[k].y & 0x7fff7fffu));
+        m = __vmaxu2(m, __vmaxu2(r.q[k].z & 0x7fff7fffu, r.q[k].w & 0x7fff7fffu));
+    }
+    return max(m << 16, m & 0xffff0000u);
+}
+__device__ __forceinline__ void values16(const Raw16<float>& r, float (&v)[16]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[4 * k] = __uint_as_float(r.q[k].x); v[4 * k + 1] = __uint_as_float(r.q[k].y);
+        v[4 * k + 2] = __uint_as_float(r.q[k].z); v[4 * k + 3] = __uint_as_float(r.q[k].w);
+    }
+}
+__device__ __forceinline__ void values16(const Raw16<bf16>& r, float (&v)[16]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const unsigned u[4] = {r.q[k].x, r.q[k].y, r.q[k].z, r.q[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[8 * k + 2 * i] = bf_lo(u[i]); v[8 * k + 2 * i + 1] = bf_hi(u[i]); }
+    }
+}
+
+// A thread holds 16 columns, two neighbouring threads a block of 32; PACK_U such pieces in flight.  Bound by instructions
+// as much as by memory (8 columns, integer conversions and a piece at a time: 55 us for 16384 x 4096 bf16).
+constexpr int PACK_U = 4;
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, bool vec, const Image im) {
+    grid_dep_sync();                                                 // g: groups of 16 columns here
+    for (unsigned b0 = blockIdx.x * 256 * PACK_U; b0 < g.total; b0 += gridDim.x * 256 * PACK_U) {
+        Raw16<T> raw[PACK_U];
+        unsigned row[PACK_U], col[PACK_U];
+#pragma unroll
+        for (int u = 0; u < PACK_U; ++u) {
+            const unsigned i = min(b0 + threadIdx.x + u * 256, g.total - 1);       // whole warps take part in the exchange below
+            row[u] = i / g.per_row;
+            col[u] = (i - row[u] * g.per_row) * 16;
+            raw[u] = fetch16<T>(x + (long long)row[u] * ld + col[u], max(0, cols - (int)col[u]), vec);
+        }
+#pragma unroll
+        for (int u = 0; u < PACK_U; ++u) {
+            unsigned top = top16(raw[u]);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            const unsigned e = img_exp(top);
+            const float inv = img_inv(e);
+            float v[16];
+            values16(raw[u], v);
+            unsigned w[4];
+            if (__uint_as_float(top) * inv < 127.5f) {               // no code is cut to 127
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[k] = pack_codes(__float_as_uint(fmaf(v[4 * k], inv, IMG_MAGIC)), __float_as_uint(fmaf(v[4 * k + 1], inv, IMG_MAGIC)),
+                                      __float_as_uint(fmaf(v[4 * k + 2], inv, IMG_MAGIC)), __float_as_uint(fmaf(v[4 * k + 3], inv, IMG_MAGIC)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = pack_codes(img_code(v[4 * k], inv), img_code(v[4 * k + 1], inv), img_code(v[4 * k + 2], inv), img_code(v[4 * k + 3], inv));
+            }
+            if (b0 + threadIdx.x + u * 256 < g.total) {
+                *reinterpret_cast<uint4*>(im.q + row[u] * im.pitch + col[u]) = make_uint4(w[0], w[1], w[2], w[3]);
+                if ((threadIdx.x & 1) == 0) im.e[row[u] * (im.pitch / IMG_BLOCK) + col[u] / IMG_BLOCK] = (uint8_t)e;
+            }
         }
     }
 }
 
-__device__ __forceinline__ void img_load8(const Image& im, long long r, int c, float (&v)[8]) {
-    const uint2 q = *reinterpret_cast<const uint2*>(im.q + r * im.pitch + c);
-    const float s = img_scale(im.e[r * (im.pitch / IMG_BLOCK) + c / IMG_BLOCK]);
+struct Img8 { uint2 q; unsigned e; };
+__device__ __forceinline__ Img8 img_fetch8(const Image& im, long long r, int c) {
+    return Img8{*reinterpret_cast<const uint2*>(im.q + r * im.pitch + c), im.e[r * (im.pitch / IMG_BLOCK) + c / IMG_BLOCK]};
+}
+__device__ __forceinline__ void img_values8(const Img8& i, float (&v)[8]) {
+    const float s = img_scale(i.e);
+    float a[4], b[4];
+    unpack_codes(i.q.x, s, a);
+    unpack_codes(i.q.y, s, b);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        v[k] = (float)(int8_t)(q.x >> (8 * k)) * s;
-        v[4 + k] = (float)(int8_t)(q.y >> (8 * k)) * s;
+    for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
+}
+
+__device__ __forceinline__ void store16(float* p, int valid, bool vec, const float (&v)[16]) {
+    if (vec && valid >= 16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) reinterpret_cast<float4*>(p)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) if (i < valid) p[i] = v[i];
+}
+__device__ __forceinline__ void store16(bf16* p, int valid, bool vec, const float (&v)[16]) {
+    if (vec && valid >= 16) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            reinterpret_cast<uint4*>(p)[k] = make_uint4(bf_pack(v[8 * k], v[8 * k + 1]), bf_pack(v[8 * k + 2], v[8 * k + 3]), bf_pack(v[8 * k + 4], v[8 * k + 5]),
+                                                        bf_pack(v[8 * k + 6], v[8 * k + 7]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) if (i < valid) p[i] = __float2bfloat16(v[i]);
+}
+
+// out: `ld` elements between rows; g: groups of 16 columns
+template <typename T>
+__global__ void __launch_bounds__(256) unpack_kernel(const Image im, const Groups g, int cols, T* __restrict__ out, long long ld, bool vec) {
+    grid_dep_sync();
+    for (unsigned b0 = blockIdx.x * 256 * PACK_U; b0 < g.total; b0 += gridDim.x * 256 * PACK_U) {
+        uint4 q[PACK_U];
+        unsigned e[PACK_U], row[PACK_U], col[PACK_U];
+#pragma unroll
+        for (int u = 0; u < PACK_U; ++u) {
+            const unsigned i = min(b0 + threadIdx.x + u * 256, g.total - 1);
+            row[u] = i / g.per_row;
+            col[u] = (i - row[u] * g.per_row) * 16;
+            q[u] = *reinterpret_cast<const uint4*>(im.q + row[u] * im.pitch + col[u]);
+            e[u] = im.e[row[u] * (im.pitch / IMG_BLOCK) + col[u] / IMG_BLOCK];
+        }
+#pragma unroll
+        for (int u = 0; u < PACK_U; ++u) {
+            if (b0 + threadIdx.x + u * 256 >= g.total) break;
+            const float s = img_scale(e[u]);
+            const unsigned w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float f[4];
+                unpack_codes(w[k], s, f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[4 * k + i] = f[i];
+            }
+            store16(out + (long long)row[u] * ld + col[u], cols - (int)col[u], vec, v);
+        }
     }
 }
 
-// out: `ld` elements between rows
-template <typename T>
-__global__ void __launch_bounds__(256) unpack_kernel(const Image im, long long rows, int cols, T* __restrict__ out, long long ld, bool vec) {
-    grid_dep_sync();
-    const int groups = (cols + 7) / 8;
-    const long long total = rows * groups;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long r = i / groups;
-        const int c = (int)(i - r * groups) * 8;
-        float v[8];
-        img_load8(im, r, c, v);
-        store8(out + r * ld + c, cols - c, vec, v);
+// launch(first row, Groups, blocks) for pieces of at most 2^30 groups
+template <typename F>
+void by_rows(long long rows, long long per_row, F&& launch_piece) {
+    const long long most = std::max<long long>(1, (1ll << 30) / per_row);
+    for (long long r = 0; r < rows; r += most) {
+        const long long n = std::min(most, rows - r), total = n * per_row;
+        const long long blocks = (total + 256 * EIGHT_U - 1) / (256 * EIGHT_U);
+        launch_piece(r, Groups{(unsigned)total, (unsigned)per_row}, dim3((unsigned)std::min<long long>(blocks, SMS * 64)));
     }
+}
+template <typename T>
+void launch_planes(const T* x, long long rows, long long cols, long long ld, bf16* out, long long plane, int planes, cudaStream_t st) {
+    const bool vec = aligned(x, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    const long long pitch = (cols + 7) / 8 * 8;
+    by_rows(rows, pitch / 8, [&](long long r, Groups g, dim3 blocks) {
+        launch(planes_kernel<T>, blocks, dim3(256), 0, st, x + r * ld, g, (int)cols, ld, vec, out + r * pitch, plane, planes);
+    });
+}
+inline Image image_from(const Image& im, long long r) { return Image{im.q + r * im.pitch, im.e + r * (im.pitch / IMG_BLOCK), im.pitch}; }
+template <typename T>
+void launch_pack(const T* x, long long rows, long long cols, long long ld, const Image& im, cudaStream_t st) {
+    const bool vec = aligned(x, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    by_rows(rows, im.pitch / 16, [&](long long r, Groups g, dim3 blocks) { launch(pack_kernel<T>, blocks, dim3(256), 0, st, x + r * ld, g, (int)cols, ld, vec, image_from(im, r)); });
+}
+template <typename T>
+void launch_unpack(const Image& im, long long rows, long long cols, T* out, long long ld, cudaStream_t st) {
+    const bool vec = aligned(out, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    by_rows(rows, (cols + 15) / 16, [&](long long r, Groups g, dim3 blocks) { launch(unpack_kernel<T>, blocks, dim3(256), 0, st, image_from(im, r), g, (int)cols, out + r * ld, ld, vec); });
 }
 
 // ---- gradients through the activation ----
 struct GradArgs {
-    const void* dy; long long lddy; int vec_dy;
-    const void* pre[2]; int vec_pre;         // STASH_FULL: `cols` elements between rows
+    const void* dy; long long lddy;
+    const void* pre[2];                      // STASH_FULL: `cols` elements between rows
     Image img[2];
-    int kind, act;                           // kind: STASH_* (STASH_NONE: the gradient passes unchanged)
+    int act;
     long long rows; int cols;
     bf16* out[2]; long long plane; int planes;   // nullable; pitch = cols rounded up to 8
     float* sums;                             // nullable: [gridDim.y][cols] column sums of this block row
     int rows_per_block;
 };
 
-// linear: dz = dy act'(z).  gated: dg = dy u act'(g), du = dy act(g).  A thread keeps eight columns and walks down
-// rows_per_block / 8 rows, so the column sums of dz cost registers only; they are added up in float over at most
-// rows_per_block values and then across blocks in double, in a fixed order.
-template <typename T, bool GATED>
+// Eight values as they are in memory.  VEC: every access fits; otherwise element by element, zeros behind `valid`.
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> fetch8(const T* p, int valid) {
+    Raw8<T> r;
+    if (VEC) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.q[k] = __ldcs(reinterpret_cast<const uint4*>(p) + k);
+    } else {
+        T* e = reinterpret_cast<T*>(r.q);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = k < valid ? p[k] : T(0.f);
+    }
+    return r;
+}
+__device__ __forceinline__ void values8(const Raw8<float>& r, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        v[4 * k] = __uint_as_float(r.q[k].x); v[4 * k + 1] = __uint_as_float(r.q[k].y);
+        v[4 * k + 2] = __uint_as_float(r.q[k].z); v[4 * k + 3] = __uint_as_float(r.q[k].w);
+    }
+}
+__device__ __forceinline__ void values8(const Raw8<bf16>& r, float (&v)[8]) {
+    const unsigned u[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(u[i]); v[2 * i + 1] = bf_hi(u[i]); }
+}
+
+// act and its derivative at eight values, the choice outside the loop
+template <bool FAST>
+__device__ __forceinline__ void act_both8(const float (&z)[8], int act, float (&a)[8], float (&d)[8]) {
+    switch (act) {
+        case FTP_ACT_RELU:
+#pragma unroll
+            for (int k = 0; k < 8; ++k) act_both<FAST>(z[k], FTP_ACT_RELU, a[k], d[k]);
+            break;
+        case FTP_ACT_RELU6:
+#pragma unroll
+            for (int k = 0; k < 8; ++k) act_both<FAST>(z[k], FTP_ACT_RELU6, a[k], d[k]);
+            break;
+        case FTP_ACT_GELU:
+#pragma unroll
+            for (int k = 0; k < 8; ++k) act_both<FAST>(z[k], FTP_ACT_GELU, a[k], d[k]);
+            break;
+        case FTP_ACT_SILU:
+#pragma unroll
+            for (int k = 0; k < 8; ++k) act_both<FAST>(z[k], FTP_ACT_SILU, a[k], d[k]);
+            break;
+        default:
+#pragma unroll
+            for (int k = 0; k < 8; ++k) act_both<FAST>(z[k], FTP_ACT_NONE, a[k], d[k]);
+    }
+}
+
+// linear: dz = dy act'(z).  gated: dg = dy u act'(g), du = dy act(g).  KIND: form of z or of g and u (STASH_NONE: the
+// gradient passes unchanged).  A thread keeps eight columns and walks down rows_per_block / 8 rows, R of them in flight,
+// so the column sums of dz cost registers only; they are added up in float over at most rows_per_block values and then
+// across blocks in double, in a fixed order.  With one row in flight 2.3 TB/s at 8192 x 12288 bf16.
+template <typename T, bool GATED, int KIND, bool VEC>
 __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradArgs p) {
     grid_dep_sync();
     constexpr bool FAST = sizeof(T) == 2;
+    constexpr int R = sizeof(T) == 2 ? 4 : 2, P = GATED ? 2 : 1;
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (blockIdx.x * 32 + tx) * 8, valid = p.cols - c;
     const long long pitch = (p.cols + 7) / 8 * 8, r0 = (long long)blockIdx.y * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (valid > 0) {
-#pragma unroll 2
-        for (long long r = r0 + ty; r < r1; r += 8) {
-            float d[8], z[8], u[8], o[8];
-            load8(static_cast<const T*>(p.dy) + r * p.lddy + c, valid, p.vec_dy, d);
-            if (p.kind == STASH_FULL) {
-                load8(static_cast<const T*>(p.pre[0]) + r * p.cols + c, valid, p.vec_pre, z);
-                if (GATED) load8(static_cast<const T*>(p.pre[1]) + r * p.cols + c, valid, p.vec_pre, u);
-            } else if (p.kind == STASH_8BIT) {
-                img_load8(p.img[0], r, c, z);
-                if (GATED) img_load8(p.img[1], r, c, u);
+        for (long long rb = r0 + ty; rb < r1; rb += 8 * R) {
+            Raw8<T> dy[R], pre[P][R];
+            Img8 img[P][R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const long long r = min(rb + 8 * i, r1 - 1);
+                dy[i] = fetch8<T, VEC>(static_cast<const T*>(p.dy) + r * p.lddy + c, valid);
+#pragma unroll
+                for (int q = 0; q < P; ++q) {
+                    if (KIND == STASH_FULL) pre[q][i] = fetch8<T, VEC>(static_cast<const T*>(p.pre[q]) + r * p.cols + c, valid);
+                    if (KIND == STASH_8BIT) img[q][i] = img_fetch8(p.img[q], r, c);
+                }
             }
-            if (GATED) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float a, da;
-                    act_both<FAST>(z[k], p.act, a, da);
-                    o[k] = d[k] * u[k] * da;
-                    d[k] *= a;
-                }
-                if (valid < 8)
+            for (int i = 0; i < R; ++i) {
+                const long long r = rb + 8 * i;
+                if (r >= r1) break;
+                float d[8], z[8], a[8], da[8];
+                values8(dy[i], d);
+                if (KIND == STASH_FULL) values8(pre[0][i], z);
+                if (KIND == STASH_8BIT) img_values8(img[0][i], z);
+                if (KIND != STASH_NONE) act_both8<FAST>(z, p.act, a, da);
+                if (GATED) {
+                    float u[8], o[8];
+                    if (KIND == STASH_FULL) values8(pre[P - 1][i], u);
+                    if (KIND == STASH_8BIT) img_values8(img[P - 1][i], u);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) if (k >= valid) o[k] = d[k] = 0.f;
-                store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, o);
-                store_planes(p.out[1] + r * pitch + c, p.plane, p.planes, d);
-            } else {
-                if (p.kind != STASH_NONE) {
+                    for (int k = 0; k < 8; ++k) { o[k] = d[k] * u[k] * da[k]; d[k] *= a[k]; }
+                    if (!VEC)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float a, da;
-                        act_both<FAST>(z[k], p.act, a, da);
-                        d[k] *= da;
+                        for (int k = 0; k < 8; ++k) if (k >= valid) o[k] = d[k] = 0.f;
+                    store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, o);
+                    store_planes(p.out[1] + r * pitch + c, p.plane, p.planes, d);
+                } else {
+                    if (KIND != STASH_NONE) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) d[k] *= da[k];
                     }
-                }
-                if (valid < 8)
+                    if (!VEC)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) if (k >= valid) d[k] = 0.f;
-                if (p.out[0]) store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, d);
-                if (p.sums) {
+                        for (int k = 0; k < 8; ++k) if (k >= valid) d[k] = 0.f;
+                    if (p.out[0]) store_planes(p.out[0] + r * pitch + c, p.plane, p.planes, d);
+                    if (p.sums) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) sum[k] += d[k];
+                        for (int k = 0; k < 8; ++k) sum[k] += d[k];
+                    }
                 }
             }
         }
@@ -240,6 +444,10 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradA
             p.sums[(long long)blockIdx.y * p.cols + col] = s;
         }
     }
+}
+template <typename T, bool GATED, int KIND>
+void launch_grad(const GradArgs& g, bool vec, int chunks, cudaStream_t st) {
+    launch(vec ? grad_kernel<T, GATED, KIND, true> : grad_kernel<T, GATED, KIND, false>, dim3((g.cols + 255) / 256, chunks), dim3(256), 0, st, g);
 }
 
 __global__ void __launch_bounds__(256) sums_kernel(const float* __restrict__ part, int chunks, int cols, float* __restrict__ out) {
@@ -287,10 +495,7 @@ ftp_status make_operand(Operand* o, const void* src, long long rows, long long c
     bf16* p = static_cast<bf16*>(ws.take((size_t)plane * planes * 2));
     *o = Operand{p, rows, cols, pitch, plane, planes};
     if (ws.dry()) return FTP_OK;
-    const bool vec = aligned(src, 16) && (ld * (long long)sizeof(T)) % 16 == 0;
-    const long long blocks = (rows * (pitch / 8) + 255) / 256;
-    launch(planes_kernel<T>, dim3((unsigned)std::min<long long>(blocks, SMS * 16)), dim3(256), 0, st, static_cast<const T*>(src), rows, (int)cols, ld, vec, p,
-           plane, planes);
+    launch_planes(static_cast<const T*>(src), rows, cols, ld, p, plane, planes, st);
     return FTP_OK;
 }
 
@@ -300,9 +505,7 @@ ftp_status image_operand(Operand* o, const void* image, long long rows, long lon
     bf16* p = static_cast<bf16*>(ws.take((size_t)(rows * pitch) * 2));
     *o = Operand{p, rows, cols, pitch, rows * pitch, 1};
     if (ws.dry()) return FTP_OK;
-    const Image im = image_at(const_cast<void*>(image), rows, cols, 0);
-    const long long blocks = (rows * (pitch / 8) + 255) / 256;
-    launch(unpack_kernel<bf16>, dim3((unsigned)std::min<long long>(blocks, SMS * 16)), dim3(256), 0, st, im, rows, (int)cols, p, pitch, true);
+    launch_unpack(image_at(const_cast<void*>(image), rows, cols, 0), rows, cols, p, pitch, st);
     return FTP_OK;
 }
 
@@ -389,7 +592,8 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
 }
 
 constexpr int GRAD_ROWS = 64, GRAD_CHUNKS = 1024;
-int grad_rows_per_block(long long rows) { return (int)std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8); }
+// up to 256 rows in one block row, whose sums then are the bias gradient (a launch less)
+int grad_rows_per_block(long long rows) { return rows <= 256 ? 256 : (int)std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8); }
 
 // ---- backward of both operators ----
 template <typename T, bool GATED>
@@ -427,22 +631,23 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
     }
     g.rows_per_block = grad_rows_per_block(M);
     const int chunks = (int)((M + g.rows_per_block - 1) / g.rows_per_block);
-    float* sums = GATED ? nullptr : static_cast<float*>(ws.take((size_t)chunks * d->cout * 4));
+    float* sums = GATED || chunks == 1 ? nullptr : static_cast<float*>(ws.take((size_t)chunks * d->cout * 4));
     if (dry) return FTP_OK;
     if (direct) FTP_REQUIRE(aligned(dy, 16), FTP_ERANGE, "%s: an operand does not start on a 16-byte boundary (set `unaligned`)", who);
     if (!direct || dbias) {
         g.dy = dy; g.lddy = ldy;
-        g.vec_dy = aligned(dy, 16) && (ldy * (long long)sizeof(T)) % 16 == 0;
-        g.kind = kind; g.act = d->act;
+        g.act = d->act;
         g.rows = M; g.cols = d->cout;
         for (int i = 0; i < (GATED ? 2 : 1); ++i) {
             if (kind == STASH_FULL) g.pre[i] = static_cast<const T*>(stash) + (long long)i * M * d->cout;
             if (kind == STASH_8BIT) g.img[i] = image_at(const_cast<void*>(stash), M, d->cout, i);
         }
-        g.vec_pre = kind == STASH_FULL && aligned(g.pre[0], 16) && ((long long)d->cout * (long long)sizeof(T)) % 16 == 0 && (!GATED || aligned(g.pre[1], 16));
-        g.sums = dbias ? sums : nullptr;
-        launch(grad_kernel<T, GATED>, dim3((d->cout + 255) / 256, chunks), dim3(256), 0, st, g);
-        if (dbias) launch(sums_kernel, dim3((d->cout + 31) / 32), dim3(256), 0, st, (const float*)sums, chunks, (int)d->cout, dbias);
+        const bool vec = d->cout % 8 == 0 && aligned(dy, 16) && ldy * (long long)sizeof(T) % 16 == 0 && aligned(g.pre[0], 16) && aligned(g.pre[1], 16);
+        g.sums = dbias ? (chunks == 1 ? dbias : sums) : nullptr;
+        if (kind == STASH_FULL) launch_grad<T, GATED, STASH_FULL>(g, vec, chunks, st);
+        else if (kind == STASH_8BIT) launch_grad<T, GATED, STASH_8BIT>(g, vec, chunks, st);
+        else if constexpr (!GATED) launch_grad<T, false, STASH_NONE>(g, vec, chunks, st);
+        if (dbias && chunks > 1) launch(sums_kernel, dim3((d->cout + 31) / 32), dim3(256), 0, st, (const float*)sums, chunks, (int)d->cout, dbias);
         if (ftp_status s = launched(who)) return s;
     }
     Product p{};
@@ -615,10 +820,9 @@ ftp_status ftp_checkpoint_pack(const void* x, int64_t rows, int32_t cols, int64_
     if (ftp_status s = check_checkpoint(x, image, rows, cols, &ld, precision, part, "checkpoint_pack")) return s;
     if (rows == 0) return FTP_OK;
     const Image im = image_at(image, rows, cols, part);
-    const unsigned blocks = (unsigned)std::min<long long>((rows * (im.pitch / 8) + 255) / 256, SMS * 16);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (precision == FTP_FP32) ftp::launch(pack_kernel<float>, dim3(blocks), dim3(256), 0, st, static_cast<const float*>(x), (long long)rows, (int)cols, (long long)ld, aligned(x, 16) && ld % 4 == 0, im);
-    else ftp::launch(pack_kernel<bf16>, dim3(blocks), dim3(256), 0, st, static_cast<const bf16*>(x), (long long)rows, (int)cols, (long long)ld, aligned(x, 16) && ld % 8 == 0, im);
+    if (precision == FTP_FP32) launch_pack(static_cast<const float*>(x), rows, cols, ld, im, st);
+    else launch_pack(static_cast<const bf16*>(x), rows, cols, ld, im, st);
     return launched("checkpoint_pack");
 }
 
@@ -626,10 +830,9 @@ ftp_status ftp_checkpoint_unpack(const void* image, int32_t part, int64_t rows, 
     if (ftp_status s = check_checkpoint(x, image, rows, cols, &ld, precision, part, "checkpoint_unpack")) return s;
     if (rows == 0) return FTP_OK;
     const Image im = image_at(const_cast<void*>(image), rows, cols, part);
-    const unsigned blocks = (unsigned)std::min<long long>((rows * (long long)((cols + 7) / 8) + 255) / 256, SMS * 16);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (precision == FTP_FP32) ftp::launch(unpack_kernel<float>, dim3(blocks), dim3(256), 0, st, im, (long long)rows, (int)cols, static_cast<float*>(x), (long long)ld, aligned(x, 16) && ld % 4 == 0);
-    else ftp::launch(unpack_kernel<bf16>, dim3(blocks), dim3(256), 0, st, im, (long long)rows, (int)cols, static_cast<bf16*>(x), (long long)ld, aligned(x, 16) && ld % 8 == 0);
+    if (precision == FTP_FP32) launch_unpack(im, rows, cols, static_cast<float*>(x), ld, st);
+    else launch_unpack(im, rows, cols, static_cast<bf16*>(x), ld, st);
     return launched("checkpoint_unpack");
 }
 

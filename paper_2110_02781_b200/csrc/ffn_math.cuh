@@ -7,17 +7,19 @@ namespace ffn {
 
 // exp and the division at float accuracy for float tensors; for bf16 tensors the hardware approximations, whose error
 // (2^-21 relative) is far below the rounding of the result to 8 bits of mantissa.
-template <bool FAST> __device__ __forceinline__ float exp_t(float x) { return FAST ? __expf(x) : expf(x); }
+__device__ __forceinline__ float rcp_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float ex2_fast(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+constexpr float LOG2E = 1.4426950408889634f;
+template <bool FAST> __device__ __forceinline__ float exp_t(float x) { return FAST ? ex2_fast(x * LOG2E) : expf(x); }
 template <bool FAST> __device__ __forceinline__ float sigmoid_t(float z) {
-    return FAST ? __fdividef(1.f, 1.f + __expf(-z)) : 1.f / (1.f + expf(-z));
+    return FAST ? rcp_fast(1.f + ex2_fast(z * -LOG2E)) : 1.f / (1.f + expf(-z));
 }
 
 // For bf16 tensors: Phi(z) without a branch from e^(-z^2/2) and the rational approximation 7.1.26 of Abramowitz and Stegun,
 // Handbook of Mathematical Functions (1964), of erfc: |error| <= 1.5e-7, a 1/26000 of bf16's half step at 1.  erff takes
 // both sides of a branch in almost every warp and twice the instructions.  e: e^(-z^2/2), shared with the density.
 __device__ __forceinline__ float phi_fast(float z, float e) {
-    const float x = fabsf(z) * 0.70710678118654752f;
-    const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+    const float t = rcp_fast(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
     const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);   // Phi(-|z|)
     return z > 0.f ? 1.f - q : q;
 }
@@ -28,7 +30,7 @@ __device__ __forceinline__ float act_value(float z, int act) {
     switch (act) {
         case FTP_ACT_RELU: return z < 0.f ? 0.f : z;
         case FTP_ACT_RELU6: return z < 0.f ? 0.f : (z > 6.f ? 6.f : z);
-        case FTP_ACT_GELU: return z * (FAST ? phi_fast(z, __expf(-0.5f * z * z)) : 0.5f + 0.5f * erff(z * 0.70710678118654752f));
+        case FTP_ACT_GELU: return z * (FAST ? phi_fast(z, ex2_fast(z * z * (-0.5f * LOG2E))) : 0.5f + 0.5f * erff(z * 0.70710678118654752f));
         case FTP_ACT_SILU: return z * sigmoid_t<FAST>(z);
         default: return z;
     }
@@ -39,7 +41,7 @@ __device__ __forceinline__ void act_both(float z, int act, float& v, float& d) {
         case FTP_ACT_RELU: v = z < 0.f ? 0.f : z; d = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z); break;
         case FTP_ACT_RELU6: v = z < 0.f ? 0.f : (z > 6.f ? 6.f : z); d = z > 0.f && z < 6.f ? 1.f : (z == z ? 0.f : z); break;
         case FTP_ACT_GELU: {
-            const float e = exp_t<FAST>(-0.5f * z * z), p = FAST ? phi_fast(z, e) : 0.5f + 0.5f * erff(z * 0.70710678118654752f);
+            const float e = FAST ? ex2_fast(z * z * (-0.5f * LOG2E)) : expf(-0.5f * z * z), p = FAST ? phi_fast(z, e) : 0.5f + 0.5f * erff(z * 0.70710678118654752f);
             v = z * p;
             // for |z| beyond 14 the density is 0 in float; z * 0 at z = +-inf would be NaN
             d = p + (fabsf(z) > 14.f ? 0.f : z * e * 0.39894228040143268f);
@@ -93,11 +95,24 @@ __device__ __forceinline__ unsigned img_exp(unsigned amax_bits) {
 __device__ __forceinline__ float img_scale(unsigned e) { return e == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(e << 23); }
 // 1 / scale = 2^(127 - byte): exact, a subnormal for byte 254 at most (bytes end at 248)
 __device__ __forceinline__ float img_inv(unsigned e) { return e == 255u ? 0.f : __uint_as_float((254u - e) << 23); }
-__device__ __forceinline__ int img_code(float v, float inv) {
-    return __float2int_rn(fminf(fmaxf(v * inv, -127.f), 127.f));     // a NaN (byte 255) becomes some code that no reader uses
+// Codes without a conversion instruction (a quarter of the rate of an addition): v * inv is exact, and adding 1.5 * 2^23
+// rounds it to the nearest integer, ties to even, which then is the low byte of the sum's bits.
+constexpr float IMG_MAGIC = 12582912.f;
+__device__ __forceinline__ unsigned img_code(float v, float inv) {
+    // a NaN (byte 255) becomes some code that no reader uses
+    return __float_as_uint(fminf(fmaxf(v * inv, -127.f), 127.f) + IMG_MAGIC);
 }
-__device__ __forceinline__ unsigned pack_codes(int a, int b, int c, int d) {
-    return (a & 255) | (b & 255) << 8 | (c & 255) << 16 | (unsigned)d << 24;
+// low bytes of four words
+__device__ __forceinline__ unsigned pack_codes(unsigned a, unsigned b, unsigned c, unsigned d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// the four codes of a word as floats: code + 128 under the exponent of 2^23, less 2^23 + 128
+__device__ __forceinline__ void unpack_codes(unsigned q, float scale, float (&v)[4]) {
+    const unsigned u = q ^ 0x80808080u;
+    v[0] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - 8388736.f) * scale;
+    v[1] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - 8388736.f) * scale;
+    v[2] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - 8388736.f) * scale;
+    v[3] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - 8388736.f) * scale;
 }
 
 }  // namespace ffn

@@ -41,11 +41,12 @@ def test_workspace_sizes():
     assert size(lin, desc(cout=47), 0)[1] == up(64 * 48 * 2, 256)                                 # a copy of w
     assert size(lin, desc(unaligned=1), 0)[1] == up(40 * 64 * 2, 256) + up(64 * 48 * 2, 256)
     assert size(lin, desc(prec=0), 0)[1] == up(3 * 40 * 64 * 2, 256) + up(3 * 64 * 48 * 2, 256)    # three planes of each
-    assert size(lin, desc(), 1)[1] == up(48 * 4, 256)                                             # sums of the bias gradient
-    assert size(lin, desc(act=3, stash=1), 1)[1] == up(40 * 48 * 2, 256) + up(48 * 4, 256)
+    assert size(lin, desc(), 1) == (0, 0)
+    assert size(lin, desc(rows=300), 1)[1] == up(5 * 48 * 4, 256)                                 # sums of the bias gradient, 64 rows each
+    assert size(lin, desc(act=3, stash=1), 1)[1] == up(40 * 48 * 2, 256)
     assert size(gat, desc(act=4, stash=1), 1)[1] == 2 * up(40 * 48 * 2, 256)
     assert size(gat, desc(act=4, stash=0), 1)[1] == up(2 * 40 * 48 * 2, 256) + 2 * up(40 * 48 * 2, 256)
-    assert size(lin, desc(x8=1), 1)[1] == up(40 * 64 * 2, 256) + up(48 * 4, 256)
+    assert size(lin, desc(x8=1), 1)[1] == up(40 * 64 * 2, 256)
     assert size(lin, desc(rows=4, prec=0, ldx=65), 0) == (0, 0)                                   # a few tokens: read as they are
     big = size(gat, desc(rows=1 << 20, cin=8192, cout=16384, prec=0, stash=2, act=4), 1)
     assert big[0] == 0 and big[1] > 1 << 36
