@@ -37,23 +37,6 @@ __device__ __forceinline__ void load8(const bf16* p, int valid, bool vec, float 
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < valid ? __bfloat162float(p[i]) : 0.f;
 }
-__device__ __forceinline__ void store8(float* p, int valid, bool vec, const float (&v)[8]) {
-    if (vec && valid >= 8) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < valid) p[i] = v[i];
-}
-__device__ __forceinline__ void store8(bf16* p, int valid, bool vec, const float (&v)[8]) {
-    if (vec && valid >= 8) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(bf_pack(v[0], v[1]), bf_pack(v[2], v[3]), bf_pack(v[4], v[5]), bf_pack(v[6], v[7]));
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < valid) p[i] = __float2bfloat16(v[i]);
-}
 
 // One plane (bf16 rounding) or three (24 mantissa bits) of eight values; rows of a plane start on 16 bytes.
 // A float is its nearest bf16, the nearest bf16 of the rest and the rest of that; both subtractions are exact.  A value
@@ -302,6 +285,61 @@ void launch_unpack(const Image& im, long long rows, long long cols, T* out, long
     by_rows(rows, (cols + 15) / 16, [&](long long r, Groups g, dim3 blocks) { launch(unpack_kernel<T>, blocks, dim3(256), 0, st, image_from(im, r), g, (int)cols, out + r * ld, ld, vec); });
 }
 
+// ---- operands of the products, made in one launch ----
+// Up to three matrices that have to be copied, split into planes or unpacked before a product can read them; as blocks of
+// their own in one kernel, or behind the blocks of the gradient kernel: a small call costs its launches.
+enum { JOB_PLANES = 0, JOB_IMAGE = 1 };
+struct Job {
+    const void* src; long long ld; int vec;  // JOB_PLANES
+    Image im;                                // JOB_IMAGE
+    bf16* out; long long plane; int planes, cols, kind;
+    Groups g;                                // groups of eight columns
+    unsigned blocks;
+};
+struct Jobs { Job job[3]; int n; unsigned blocks; };
+
+template <typename T>
+__device__ __forceinline__ void run_jobs(const Jobs& all, unsigned block) {
+    int j = 0;
+    while (block >= all.job[j].blocks) block -= all.job[j++].blocks;
+    const Job& p = all.job[j];
+    const long long pitch = 8ll * p.g.per_row;
+    for (unsigned i0 = block * 256 * EIGHT_U + threadIdx.x; i0 < p.g.total; i0 += p.blocks * 256 * EIGHT_U) {
+        float v[EIGHT_U][8];
+#pragma unroll
+        for (int u = 0; u < EIGHT_U; ++u)
+            if (i0 + u * 256 < p.g.total)
+                group_at(p.g, i0 + u * 256, [&](long long r, int c) {
+                    if (p.kind == JOB_PLANES) load8(static_cast<const T*>(p.src) + r * p.ld + c, p.cols - c, p.vec, v[u]);
+                    else img_values8(img_fetch8(p.im, r, c), v[u]);
+                });
+#pragma unroll
+        for (int u = 0; u < EIGHT_U; ++u)
+            if (i0 + u * 256 < p.g.total) group_at(p.g, i0 + u * 256, [&](long long r, int c) { store_planes(p.out + r * pitch + c, p.plane, p.planes, v[u]); });
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) jobs_kernel(const __grid_constant__ Jobs jobs) {
+    grid_dep_sync();
+    run_jobs<T>(jobs, blockIdx.x);
+}
+// false: too large for 32-bit group numbers
+inline bool add_job(Jobs& all, Job j, long long rows, long long cols) {
+    const long long per_row = (cols + 7) / 8, total = rows * per_row;
+    if (total > 1 << 30 || all.n == 3) return false;
+    j.cols = (int)cols;
+    j.g = Groups{(unsigned)total, (unsigned)per_row};
+    j.blocks = (unsigned)std::min<long long>((total + 256 * EIGHT_U - 1) / (256 * EIGHT_U), SMS * 16);
+    all.job[all.n++] = j;
+    all.blocks += j.blocks;
+    return true;
+}
+template <typename T>
+void run_now(Jobs& all, cudaStream_t st) {
+    if (all.n) launch(jobs_kernel<T>, dim3(all.blocks), dim3(256), 0, st, all);
+    all = Jobs{};
+}
+
 // ---- gradients through the activation ----
 struct GradArgs {
     const void* dy; long long lddy;
@@ -310,8 +348,9 @@ struct GradArgs {
     int act;
     long long rows; int cols;
     bf16* out[2]; long long plane; int planes;   // nullable; pitch = cols rounded up to 8
-    float* sums;                             // nullable: [gridDim.y][cols] column sums of this block row
+    float* sums;                             // nullable: [block rows][cols] column sums of a block row
     int rows_per_block;
+    unsigned blocks_x, blocks;               // of the gradient itself: along the columns, all; the blocks behind them run the jobs
 };
 
 // Eight values as they are in memory.  VEC: every access fits; otherwise element by element, zeros behind `valid`.
@@ -373,12 +412,14 @@ __device__ __forceinline__ void act_both8(const float (&z)[8], int act, float (&
 // so the column sums of dz cost registers only; they are added up in float over at most rows_per_block values and then
 // across blocks in double, in a fixed order.  With one row in flight 2.3 TB/s at 8192 x 12288 bf16.
 template <typename T, bool GATED, int KIND, bool VEC>
-__global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradArgs p) {
+__global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradArgs p, const __grid_constant__ Jobs jobs) {
     grid_dep_sync();
+    if (blockIdx.x >= p.blocks) { run_jobs<T>(jobs, blockIdx.x - p.blocks); return; }
+    const int by = blockIdx.x / p.blocks_x, bx = blockIdx.x - by * p.blocks_x;
     constexpr bool FAST = sizeof(T) == 2;
     constexpr int R = sizeof(T) == 2 ? 4 : 2, P = GATED ? 2 : 1;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (blockIdx.x * 32 + tx) * 8, valid = p.cols - c;
-    const long long pitch = (p.cols + 7) / 8 * 8, r0 = (long long)blockIdx.y * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (bx * 32 + tx) * 8, valid = p.cols - c;
+    const long long pitch = (p.cols + 7) / 8 * 8, r0 = (long long)by * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (valid > 0) {
         for (long long rb = r0 + ty; rb < r1; rb += 8 * R) {
@@ -436,18 +477,21 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradA
 #pragma unroll
         for (int k = 0; k < 8; ++k) red[ty][tx * 8 + k] = sum[k];
         __syncthreads();
-        const int col = blockIdx.x * 256 + threadIdx.x;
+        const int col = bx * 256 + threadIdx.x;
         if (col < p.cols) {
             float s = 0.f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
-            p.sums[(long long)blockIdx.y * p.cols + col] = s;
+            p.sums[(long long)by * p.cols + col] = s;
         }
     }
 }
 template <typename T, bool GATED, int KIND>
-void launch_grad(const GradArgs& g, bool vec, int chunks, cudaStream_t st) {
-    launch(vec ? grad_kernel<T, GATED, KIND, true> : grad_kernel<T, GATED, KIND, false>, dim3((g.cols + 255) / 256, chunks), dim3(256), 0, st, g);
+void launch_grad(GradArgs& g, bool vec, int chunks, Jobs& jobs, cudaStream_t st) {
+    g.blocks_x = (unsigned)((g.cols + 255) / 256);
+    g.blocks = g.blocks_x * chunks;
+    launch(vec ? grad_kernel<T, GATED, KIND, true> : grad_kernel<T, GATED, KIND, false>, dim3(g.blocks + jobs.blocks), dim3(256), 0, st, g, jobs);
+    jobs = Jobs{};
 }
 
 __global__ void __launch_bounds__(256) sums_kernel(const float* __restrict__ part, int chunks, int cols, float* __restrict__ out) {
@@ -482,7 +526,7 @@ inline long long up8(long long n) { return (n + 7) / 8 * 8; }
 // `rows` x `cols` of type T at `src` as an operand.  bf16 rows on 16 bytes are read in place, others copied; float rows
 // become three planes.
 template <typename T>
-ftp_status make_operand(Operand* o, const void* src, long long rows, long long cols, long long ld, bool unaligned, Carve& ws, cudaStream_t st, const char* who) {
+ftp_status make_operand(Operand* o, const void* src, long long rows, long long cols, long long ld, bool unaligned, Carve& ws, Jobs& jobs, cudaStream_t st, const char* who) {
     const bool f32 = sizeof(T) == 4;
     if (rows == 1) ld = up8(cols);                                   // never stepped over
     if (!f32 && !unaligned && ld % 8 == 0) {
@@ -495,17 +539,25 @@ ftp_status make_operand(Operand* o, const void* src, long long rows, long long c
     bf16* p = static_cast<bf16*>(ws.take((size_t)plane * planes * 2));
     *o = Operand{p, rows, cols, pitch, plane, planes};
     if (ws.dry()) return FTP_OK;
-    launch_planes(static_cast<const T*>(src), rows, cols, ld, p, plane, planes, st);
+    Job j{};
+    j.kind = JOB_PLANES;
+    j.src = src; j.ld = ld; j.vec = aligned(src, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    j.out = p; j.plane = plane; j.planes = planes;
+    if (!add_job(jobs, j, rows, cols)) launch_planes(static_cast<const T*>(src), rows, cols, ld, p, plane, planes, st);
     return FTP_OK;
 }
 
 // the values of an 8-bit image as an operand: one bf16 plane, exact
-ftp_status image_operand(Operand* o, const void* image, long long rows, long long cols, Carve& ws, cudaStream_t st) {
+ftp_status image_operand(Operand* o, const void* image, long long rows, long long cols, Carve& ws, Jobs& jobs, cudaStream_t st) {
     const long long pitch = up8(cols);
     bf16* p = static_cast<bf16*>(ws.take((size_t)(rows * pitch) * 2));
     *o = Operand{p, rows, cols, pitch, rows * pitch, 1};
     if (ws.dry()) return FTP_OK;
-    launch_unpack(image_at(const_cast<void*>(image), rows, cols, 0), rows, cols, p, pitch, st);
+    Job j{};
+    j.kind = JOB_IMAGE;
+    j.im = image_at(const_cast<void*>(image), rows, cols, 0);
+    j.out = p; j.plane = rows * pitch; j.planes = 1;
+    if (!add_job(jobs, j, rows, cols)) launch_unpack(j.im, rows, cols, p, pitch, st);
     return FTP_OK;
 }
 
@@ -574,13 +626,15 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, GATED ? 2 : 1);
     if (!given_x && few_tokens(d->rows, d->cin, sizeof(T) == 4, GATED ? 2 : 1))
         return ws.dry() ? FTP_OK : run_few(x, ldx, w, ldw, GATED ? 2 : 1, (int)d->rows, d->cin, d->cout, sizeof(T) == 4, p.e[0], st, who);
+    Jobs jobs{};
     if (given_x) p.A[0] = *given_x;
-    else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, st, who)) return s;
+    else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, jobs, st, who)) return s;
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
         if (given_w) p.B[i] = given_w[i];
-        else if (ftp_status s = make_operand<T>(&p.B[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, st, who)) return s;
+        else if (ftp_status s = make_operand<T>(&p.B[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, jobs, st, who)) return s;
     }
     if (ws.dry()) return FTP_OK;
+    run_now<T>(jobs, st);
     p.parts = GATED ? 2 : 1;
     p.b_mn = 1;
     p.M = d->rows; p.N = d->cout; p.K = d->cin;
@@ -602,17 +656,19 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
     const long long M = d->rows, ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
     const bool dry = ws.dry(), f32 = sizeof(T) == 4, want_dw = dry || dw[0], want_dx = dry || dx, recompute = GATED && d->stash == STASH_NONE;
     Operand X{}, W[2] = {}, G[2] = {};
+    Jobs jobs{};
     if (want_dw || recompute) {
-        const ftp_status s = d->x_8bit ? image_operand(&X, x, M, d->cin, ws, st) : make_operand<T>(&X, x, M, d->cin, ldx, d->unaligned, ws, st, who);
+        const ftp_status s = d->x_8bit ? image_operand(&X, x, M, d->cin, ws, jobs, st) : make_operand<T>(&X, x, M, d->cin, ldx, d->unaligned, ws, jobs, st, who);
         if (s) return s;
     }
     if (want_dx || recompute)
         for (int i = 0; i < (GATED ? 2 : 1); ++i)
-            if (ftp_status s = make_operand<T>(&W[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, st, who)) return s;
+            if (ftp_status s = make_operand<T>(&W[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, jobs, st, who)) return s;
     int kind = d->stash;
     if (recompute) {
         stash = ws.take((size_t)(2 * M * d->cout) * sizeof(T));
         kind = STASH_FULL;
+        if (!dry) run_now<T>(jobs, st);
         if (!dry)
             if (ftp_status s = forward<T, GATED>(d, nullptr, nullptr, nullptr, nullptr, nullptr, STASH_FULL, const_cast<void*>(stash), ws, st, who, &X, W)) return s;
     }
@@ -644,12 +700,13 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
         }
         const bool vec = d->cout % 8 == 0 && aligned(dy, 16) && ldy * (long long)sizeof(T) % 16 == 0 && aligned(g.pre[0], 16) && aligned(g.pre[1], 16);
         g.sums = dbias ? (chunks == 1 ? dbias : sums) : nullptr;
-        if (kind == STASH_FULL) launch_grad<T, GATED, STASH_FULL>(g, vec, chunks, st);
-        else if (kind == STASH_8BIT) launch_grad<T, GATED, STASH_8BIT>(g, vec, chunks, st);
-        else if constexpr (!GATED) launch_grad<T, false, STASH_NONE>(g, vec, chunks, st);
+        if (kind == STASH_FULL) launch_grad<T, GATED, STASH_FULL>(g, vec, chunks, jobs, st);
+        else if (kind == STASH_8BIT) launch_grad<T, GATED, STASH_8BIT>(g, vec, chunks, jobs, st);
+        else if constexpr (!GATED) launch_grad<T, false, STASH_NONE>(g, vec, chunks, jobs, st);
         if (dbias && chunks > 1) launch(sums_kernel, dim3((d->cout + 31) / 32), dim3(256), 0, st, (const float*)sums, chunks, (int)d->cout, dbias);
-        if (ftp_status s = launched(who)) return s;
     }
+    run_now<T>(jobs, st);                                            // nothing left of them after the gradient kernel
+    if (ftp_status s = launched(who)) return s;
     Product p{};
     p.err = status_word();
     FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);

@@ -82,30 +82,37 @@ template <typename T, bool STORE>
 __device__ __forceinline__ void piece_move(uint8_t* buf, T* p, long long ld, int vec, long long m0, int n0, long long M, int N) {
     constexpr int PARTS = sizeof(T) * 2, EL = 16 / sizeof(T), ROWS = 32 / PARTS;        // parts of a row, elements of a part, rows per access
     const int lane = threadIdx.x & 31, part = lane % PARTS, n = n0 + part * EL;
+    if (vec != 0 && n0 + 32 <= N) {
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += ROWS) {
-        const int r = r0 + lane / PARTS;
-        const long long m = m0 + r;
-        if (m < M && n < N) {
-            T* g = p + m * ld + n;
-            uint4* s = reinterpret_cast<uint4*>(buf + piece_at<T>(r, part));
-            if (vec == 2 && n + EL <= N) {
-                if (STORE) *reinterpret_cast<uint4*>(g) = *s;
-                else *s = *reinterpret_cast<const uint4*>(g);
-            } else if (sizeof(T) == 2 && vec == 1 && n + EL <= N) {  // rows on 8 bytes
+        for (int r0 = 0; r0 < 32; r0 += ROWS) {
+            const int r = r0 + lane / PARTS;
+            const long long m = m0 + r;
+            if (m < M) {
+                T* g = p + m * ld + n;
+                uint4* s = reinterpret_cast<uint4*>(buf + piece_at<T>(r, part));
+                if (vec == 2) {
+                    if (STORE) *reinterpret_cast<uint4*>(g) = *s;
+                    else *s = *reinterpret_cast<const uint4*>(g);
+                } else {                                             // bf16 rows on 8 bytes
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (STORE) reinterpret_cast<uint2*>(g)[h] = reinterpret_cast<const uint2*>(s)[h];
-                    else reinterpret_cast<uint2*>(s)[h] = reinterpret_cast<const uint2*>(g)[h];
-                }
-            } else {
-                T* e = reinterpret_cast<T*>(s);
-                for (int i = 0; i < EL && n + i < N; ++i) {
-                    if (STORE) g[i] = e[i];
-                    else e[i] = g[i];
+                    for (int h = 0; h < 2; ++h) {
+                        if (STORE) reinterpret_cast<uint2*>(g)[h] = reinterpret_cast<const uint2*>(s)[h];
+                        else reinterpret_cast<uint2*>(s)[h] = reinterpret_cast<const uint2*>(g)[h];
+                    }
                 }
             }
         }
+    } else {
+        // rows anywhere, or cut: an element per lane, so that an access still covers neighbouring bytes
+        const bool on = n0 + lane < N;
+        T* g = p + m0 * ld + n0 + lane;
+#pragma unroll 4
+        for (int r = 0; r < 32; ++r)
+            if (on && m0 + r < M) {
+                T* s = reinterpret_cast<T*>(buf + piece_at<T>(r, lane / EL)) + lane % EL;
+                if (STORE) g[r * ld] = *s;
+                else *s = g[r * ld];
+            }
     }
 }
 
