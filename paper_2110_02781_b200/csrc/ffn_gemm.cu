@@ -5,8 +5,8 @@
 // float tensor comes as three bf16 planes (8 mantissa bits each, 24 together) and a product of two of them as the six
 // plane products that matter; the dropped ones are below 2^-24 of the result.
 //
-// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warps 0 and 2 (one thread each) stream the tiles of A and
-// of B with TMA into a ring in shared memory, warp 1 (one thread) issues the MMAs, warps 4-7 move the accumulator to shared memory.
+// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warps 0, 2 and 3 (one thread each) stream operand tiles with
+// TMA into a ring in shared memory, warp 1 (one thread) issues the MMAs, warps 4-7 move the accumulator to shared memory.
 // The slices of one tile form a cluster: each CTA then adds up the rows rank, rank + S, ... of the tile over the
 // cluster's shared memory, always in rank order, and finishes them (bias, activation, residual, kept values), so a
 // product with few tiles still uses the whole GPU, needs no workspace, and gives the same bits every time.
@@ -20,26 +20,28 @@ namespace {
 
 // ---- one CTA per tile and reduction slice ---------------------------------------------------------------------------
 constexpr int TILE_THREADS = 256;
-// bf16: two CTAs on an SM, one's epilogue beside the other's products; float (three operand tiles a block): one.
+// DEEP: a ring that fills an SM's shared memory, for launches of one CTA an SM or fewer (a block's turn through a short ring
+// takes a load's latency divided by its slots); otherwise two CTAs share an SM, one's epilogue beside the other's products.
+// Float results (three operand tiles a block) always take the long one.
 // AR = 32: at most 32 rows of A are loaded, into the first 32 of the 128 rows that the MMA reads.  The other rows are whatever
 // lies behind them in shared memory (inside the allocation, see the 12 KB at its end); they only reach accumulator rows
 // that nobody reads.  A stage is then mostly B, which is what a product of a few tokens has to stream.
-template <int BN, bool F32, int AR> constexpr uint32_t TILE_STAGE = AR * BK * 2 + BN * BK * 2;
-template <int BN, bool F32, int AR> constexpr int TILE_STAGES = F32 ? (BN == 128 ? 6 : 8) : AR == 32 ? (BN == 128 ? 4 : 8) : (BN == 128 ? 3 : 4);
-template <int BN, bool F32, int AR> constexpr uint32_t TILE_SMEM = TILE_STAGES<BN, F32, AR> * TILE_STAGE<BN, F32, AR> + (128 - AR) * 128 + 1024;
+template <int BN, int AR> constexpr uint32_t TILE_STAGE = AR * BK * 2 + BN * BK * 2;
+template <int BN, int AR, bool DEEP> constexpr int TILE_STAGES = (DEEP ? 196608 : 98304) / TILE_STAGE<BN, AR>;
+template <int BN, int AR, bool DEEP> constexpr uint32_t TILE_SMEM = TILE_STAGES<BN, AR, DEEP> * TILE_STAGE<BN, AR> + (128 - AR) * 128 + 1024;
 
 // AMN / BMN: the operand is MN-major.  EPI_GATED: the tile's first BN / 2 columns are A B[0], the others A B[1].
-template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR>
-__global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 1 : 2) ffn_tile_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
+template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR, bool DEEP>
+__global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
                                                                    const __grid_constant__ CUtensorMap mapB0, const __grid_constant__ CUtensorMap mapB1,
                                                                    const __grid_constant__ KArgs p) {
     constexpr bool CHUNKED = sizeof(T) == 4;
-    constexpr int STAGES = TILE_STAGES<BN, CHUNKED, AR>;
+    constexpr int STAGES = TILE_STAGES<BN, AR, DEEP>;
     constexpr int BUFS = CHUNKED ? 2 : 1;                            // accumulators in tensor memory
     constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = AR * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
     constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;             // output columns of a tile
     constexpr int PITCH = BN + 4;                                    // floats between rows of the staged accumulator: 16-byte accesses of 8 lanes hit all banks
-    static_assert(AR == 128 || (!AMN && !CHUNKED), "");
+    static_assert((AR == 128 || (!AMN && !CHUNKED)) && (DEEP || !CHUNKED), "");
     static_assert(AR * PITCH * 4 <= STAGES * STAGE_BYTES, "the staged accumulator reuses the operand ring");
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -78,43 +80,43 @@ __global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 1 : 2) ffn_tile
     const uint32_t tmem = tmem_base;
     grid_dep_sync();
 
-    if (warp == 0 || warp == 2) {
-        // ---- producers: A by warp 0, B by warp 2 ----
+    if (warp < 4 && warp != 1) {
+        // ---- producers ----
         Slot<STAGES> sl;
         const uint32_t ring = smem_u32(smem);
+        const int me = producer_of(warp), z = p.np == 1 ? 0 : p.np - 1 - me, step = p.np == 1 ? PRODUCERS : 1;
+        const uint32_t bytes = (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0);
         bool ok = true;
-        for (int kb = kb0; kb < kb1 && ok; ++kb) {
-            const int part = kb >= p.kb_part, k = (kb - part * p.kb_part) * BK;
-            const CUtensorMap* ma = part ? &mapA1 : &mapA0;
-            const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
-            for (int z = p.np - 1; z >= 0; --z, sl.next()) {
-                ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
-                if (!ok) break;
-                if (elect_one()) {
-                    const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = full0 + 8 * sl.s;
-                    if (warp == 0) {
-                        mbar_expect_tx(bar, (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0));
-                        if (z < p.pa) {
-                            if (AMN) {
+        sl.ahead(me);
+        for (int kb = kb0 + (p.np == 1 ? me : 0); kb < kb1; kb += step, sl.ahead(PRODUCERS)) {
+            const int part = kb >= p.kb_part, k = (kb - (part ? p.kb_part : 0)) * BK;
+            ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                          // at once for a slot never used
+            if (!ok) break;
+            if (elect_one()) {
+                const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+                const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
+                const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = full0 + 8 * sl.s;
+                mbar_expect_tx(bar, bytes);
+                if (z < p.pa) {
+                    if (AMN) {
 #pragma unroll
-                                for (int t = 0; t < 2; ++t) tma_load_3d(sa + t * SLAB, ma, (int)m0 + 64 * t, k, z, bar);
-                            } else
-                                tma_load_3d(sa, ma, k, (int)m0, z, bar);
-                        }
-                    } else if (z < p.pb) {
-                        if (EPI == EPI_GATED) {
-#pragma unroll
-                            for (int t = 0; t < BN / 64; ++t)
-                                tma_load_3d(sb + t * SLAB, t < BN / 128 ? &mapB0 : &mapB1, n0 + 64 * (t & (BN / 128 - 1)), k, z, bar);
-                        } else if (BMN) {
-#pragma unroll
-                            for (int t = 0; t < BN / 64; ++t) tma_load_3d(sb + t * SLAB, mb, n0 + 64 * t, k, z, bar);
-                        } else
-                            tma_load_3d(sb, mb, k, n0, z, bar);
-                    }
+                        for (int t = 0; t < 2; ++t) tma_load_3d(sa + t * SLAB, ma, (int)m0 + 64 * t, k, z, bar);
+                    } else
+                        tma_load_3d(sa, ma, k, (int)m0, z, bar);
                 }
-                __syncwarp();
+                if (z < p.pb) {
+                    if (EPI == EPI_GATED) {
+#pragma unroll
+                        for (int t = 0; t < BN / 64; ++t)
+                            tma_load_3d(sb + t * SLAB, t < BN / 128 ? &mapB0 : &mapB1, n0 + 64 * (t & (BN / 128 - 1)), k, z, bar);
+                    } else if (BMN) {
+#pragma unroll
+                        for (int t = 0; t < BN / 64; ++t) tma_load_3d(sb + t * SLAB, mb, n0 + 64 * t, k, z, bar);
+                    } else
+                        tma_load_3d(sb, mb, k, n0, z, bar);
+                }
             }
+            __syncwarp();
         }
         if (!ok) {
             // error path: time for the copies already issued to land before the block's memory is released
@@ -205,24 +207,29 @@ __global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 1 : 2) ffn_tile
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
-template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR>
+template <typename T, int BN, bool AMN, bool BMN, int EPI, int AR, bool DEEP>
 ftp_status launch_tile(const Product& p, KArgs& k, int S, cudaStream_t st, const char* who) {
     Maps m;
     FTP_REQUIRE(make_maps(m, p, AR, BN), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
-    auto kern = ffn_tile_kernel<T, BN, AMN, BMN, EPI, AR>;
+    auto kern = ffn_tile_kernel<T, BN, AMN, BMN, EPI, AR, DEEP>;
     static std::atomic<unsigned long long> asked{0};
-    cudaError_t e = allow_smem(asked, kern, (int)TILE_SMEM<BN, sizeof(T) == 4, AR>);
-    if (e == cudaSuccess) e = launch_cluster(kern, dim3((unsigned)((long long)k.tiles_m * k.tiles_n * k.parts_n * S)), TILE_THREADS, TILE_SMEM<BN, sizeof(T) == 4, AR>, S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
+    cudaError_t e = allow_smem(asked, kern, (int)TILE_SMEM<BN, AR, DEEP>);
+    if (e == cudaSuccess) e = launch_cluster(kern, dim3((unsigned)((long long)k.tiles_m * k.tiles_n * k.parts_n * S)), TILE_THREADS, TILE_SMEM<BN, AR, DEEP>, S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
 
+template <int BN, bool AMN, bool BMN, int EPI, int AR>
+ftp_status tile_deep(const Product& p, KArgs& k, int S, cudaStream_t st, const char* who) {
+    if ((long long)k.tiles_m * k.tiles_n * k.parts_n * S <= 148) return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, AR, true>(p, k, S, st, who);
+    return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, AR, false>(p, k, S, st, who);
+}
 template <int BN, bool AMN, bool BMN, int EPI>
 ftp_status tile_typed(const Product& p, KArgs& k, int S, cudaStream_t st, const char* who) {
-    if (p.out_f32) return launch_tile<float, BN, AMN, BMN, EPI, 128>(p, k, S, st, who);
+    if (p.out_f32) return launch_tile<float, BN, AMN, BMN, EPI, 128, true>(p, k, S, st, who);
     if constexpr (!AMN)
-        if (p.M <= 32) return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, 32>(p, k, S, st, who);
-    return launch_tile<__nv_bfloat16, BN, AMN, BMN, EPI, 128>(p, k, S, st, who);
+        if (p.M <= 32) return tile_deep<BN, AMN, BMN, EPI, 32>(p, k, S, st, who);
+    return tile_deep<BN, AMN, BMN, EPI, 128>(p, k, S, st, who);
 }
 
 }  // namespace

@@ -156,10 +156,18 @@ template <int STAGES>
 struct Slot {
     int s = 0;
     uint32_t parity = 0;
-    __device__ __forceinline__ void next() {
-        if (++s == STAGES) { s = 0; parity ^= 1; }
+    __device__ __forceinline__ void next() { ahead(1); }
+    __device__ __forceinline__ void ahead(int n) {                   // n <= STAGES
+        s += n;
+        if (s >= STAGES) { s -= STAGES; parity ^= 1; }
     }
 };
+
+// The copies are issued by PRODUCERS warps that take the slots in turn (a slot's wait, count and copies take a warp about
+// 600 cycles, the MMAs of a slot 256 to 512).  Producer j's slots are those of number j, j + PRODUCERS, ... over all tiles;
+// with three planes a producer always fetches the same one.
+constexpr int PRODUCERS = 3;
+__device__ __forceinline__ int producer_of(int warp) { return warp == 0 ? 0 : warp - 1; }           // warps 0, 2, 3
 
 __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
@@ -209,15 +217,28 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
             }
             --left;
             if (!CHUNKED || p.np == 1) {
-                if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
+                const int s0 = sl.s;
+                if (!warp_wait_for(full0 + 8 * s0, sl.parity, p.err, 2)) return false;
+                sl.next();
+                const bool two = STAGES >= 6 && left > 0;            // two blocks a trip where the ring is long
+                const int s1 = sl.s;
+                if (two) {
+                    if (!warp_wait_for(full0 + 8 * s1, sl.parity, p.err, 2)) return false;
+                    sl.next();
+                    --left;
+                    ++kb;
+                }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (elect_one()) {
-                    four(sl.s, sl.s);
-                    commit(empty0 + 8 * sl.s);
+                    four(s0, s0);
+                    commit(empty0 + 8 * s0);
+                    if (two) {
+                        four(s1, s1);
+                        commit(empty0 + 8 * s1);
+                    }
                     if (left == 0) commit(accf0 + 8 * (BUFS == 1 ? 0 : chunk & 1));
                 }
                 first = false;
-                sl.next();
             } else {
                 const int s2 = sl.s;
                 if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;

@@ -5,10 +5,9 @@
 // operand byte that a CTA loads is used for twice as many products as in a tile of its own -- which is what bounds large
 // products: at 256 x 256 a pair needs 64 KB per 8.4 MFLOP from L2.
 //
-// Warps 0 and 2 (one thread each, in each CTA) stream the tiles of A and of B with TMA (one warp for both takes 550 cycles a
-// block, more than the 512 of its MMAs); the bytes of both CTAs are counted on the first CTA's barrier.  Warp 1 of the first
-// CTA issues the MMAs and hands stages and accumulators on with commits that signal both CTAs.  Warps 4-11 empty the
-// accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
+// Warps 0, 2 and 3 (one thread each, in each CTA) stream the operand tiles with TMA; the bytes of both CTAs are counted on the
+// first CTA's barrier.  Warp 1 of the first CTA issues the MMAs and hands stages and accumulators on with commits that
+// signal both CTAs.  Warps 4-11 empty the accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
 // accumulator is double (2 x BN columns), so the epilogue of a tile -- bias, activation, kept values, residual -- runs
 // beside the MMAs of the next.  Finished pieces of 32 x 32 go through 4 KB of shared memory per warp, so that a global
 // access covers whole 64- or 128-byte pieces of a row whatever its pitch.
@@ -270,44 +269,44 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     grid_dep_sync();
 
     bool ok = true;
-    if (warp == 0 || warp == 2) {
-        // ---- producers: A by warp 0, B by warp 2 ----
+    if (warp < 4 && warp != 1) {
+        // ---- producers ----
         Slot<STAGES> sl;
         const uint32_t lead_full0 = map_rank(full0, 0), ring = smem_u32(smem);
-        for (int t = cluster; t < tiles && ok; t += clusters) {
+        const int me = producer_of(warp), z = p.np == 1 ? 0 : p.np - 1 - me, step = p.np == 1 ? PRODUCERS : 1;
+        const uint32_t bytes = (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0);
+        int kb = p.np == 1 ? me : 0;                                 // runs on over the tiles: slots are numbered through
+        sl.ahead(me);
+        for (int t = cluster; t < tiles && ok; t += clusters, kb -= all_kb) {
             int tm, tn;
             tile_at(t, p.tiles_m, tn_all, tm, tn);
             const int out = tn / p.tiles_n;
             const int m0 = tm * 256 + (int)rank * 128, n0 = (tn - out * p.tiles_n) * OUTC + (EPI == EPI_GATED ? 0 : (int)rank * (BN / 2));
-            for (int part = 0; part < p.parts_k && ok; ++part) {
-                const CUtensorMap* ma = part ? &mapA1 : &mapA0;
-                const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
-                for (int kb = 0, k = 0; kb < p.kb_part && ok; ++kb, k += BK) {
-                    for (int z = p.np - 1; z >= 0; --z, sl.next()) {
-                        ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
-                        if (!ok) break;
-                        if (elect_one()) {
-                            const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = lead_full0 + 8 * sl.s;
-                            if (warp == 0) {
-                                if (rank == 0) mbar_expect_tx(full0 + 8 * sl.s, (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0));
-                                if (z < p.pa) {
-                                    if (AMN) {
+            for (; kb < all_kb; kb += step, sl.ahead(PRODUCERS)) {
+                const int part = kb >= p.kb_part, k = (kb - (part ? p.kb_part : 0)) * BK;
+                ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
+                if (!ok) break;
+                if (elect_one()) {
+                    const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+                    const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
+                    const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = lead_full0 + 8 * sl.s;
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * sl.s, bytes);
+                    if (z < p.pa) {
+                        if (AMN) {
 #pragma unroll
-                                        for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
-                                    } else
-                                        tma_load_3d_pair(sa, ma, k, m0, z, bar);
-                                }
-                            } else if (z < p.pb) {
-                                if (BMN) {
+                            for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, m0 + 64 * u, k, z, bar);
+                        } else
+                            tma_load_3d_pair(sa, ma, k, m0, z, bar);
+                    }
+                    if (z < p.pb) {
+                        if (BMN) {
 #pragma unroll
-                                    for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
-                                } else
-                                    tma_load_3d_pair(sb, mb, k, n0, z, bar);
-                            }
-                        }
-                        __syncwarp();
+                            for (int u = 0; u < BN / 128; ++u) tma_load_3d_pair(sb + u * SLAB, mb, n0 + 64 * u, k, z, bar);
+                        } else
+                            tma_load_3d_pair(sb, mb, k, n0, z, bar);
                     }
                 }
+                __syncwarp();
             }
         }
     } else if (warp == 1) {
