@@ -12,6 +12,7 @@
 // product with few tiles still uses the whole GPU, needs no workspace, and gives the same bits every time.
 //
 // Every wait is bounded; see gemm_tc.cu for the error protocol.
+#include <cmath>
 #include "ffn_gemm.cuh"
 
 namespace ftp {
@@ -38,6 +39,7 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
     constexpr bool CHUNKED = sizeof(T) == 4;
     constexpr int STAGES = TILE_STAGES<BN, AR, DEEP>;
     constexpr int BUFS = CHUNKED ? 2 : 1;                            // accumulators in tensor memory
+    constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN, TMEM_COLS = BUFS * ACC;
     constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = AR * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
     constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;             // output columns of a tile
     constexpr int PITCH = BN + 4;                                    // floats between rows of the staged accumulator: 16-byte accesses of 8 lanes hit all banks
@@ -71,7 +73,7 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"((uint32_t)(BN * BUFS)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -142,12 +144,7 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
                 if (!have) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int g = 0; g < BN / 32; ++g) {
-                    uint32_t r[32];
-                    tmem_ld32(lanes + (uint32_t)(b * BN + g * 32), r);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) acc[g * 32 + i] += __uint_as_float(r[i]);
-                }
+                for (int g = 0; g < BN / 32; ++g) add_acc(lanes + (uint32_t)b * ACC + g * 32, BN, p.np > 1, acc + g * 32);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 if (lane == 0) mbar_arrive_one(acce0 + 8 * b);
             }
@@ -176,7 +173,7 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(BN * BUFS)) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     if (S > 1) cluster_sync_all();
 
     // ---- rows rank, rank + S, ... of the tile, added over the slices in rank order ----
@@ -234,42 +231,58 @@ ftp_status tile_typed(const Product& p, KArgs& k, int S, cudaStream_t st, const 
 
 }  // namespace
 
+// What a form of a product takes, in microseconds, up to what all forms share.  From launches timed one form at a time
+// (64..4096 tokens, 512..4096 channels, all three products, both types): c = a 64-wide block of one tile, base = launch,
+// first loads and last epilogue, epi = a tile's epilogue where the reduction is too short to hide it, share(S) = the cluster
+// and its exchange.  A wave is 74 pairs or 148 CTAs; clusters of four and eight do not fill every group of SMs.
+struct Form { bool pair; int cols, S; double cost; };
+static Form choose_form(const KArgs& k, const Product& p) {
+    const bool f32 = p.out_f32 && k.np > 1;
+    const int gated = p.epi == EPI_GATED ? 2 : 1;
+    const double blocks = (double)k.kb_part * k.parts_k;
+    auto tiles = [&](int rows, int cols) { return (double)((p.M + rows - 1) / rows) * ((p.N + cols / gated - 1) / (cols / gated)) * k.parts_n; };
+    Form best{true, 256, 1, 1e30};
+    auto take = [&](const Form& f) { if (f.cost < best.cost) best = f; };
+    auto pair = [&](int cols, double c, double base, double epi) { take({true, cols, 1, base + std::ceil(tiles(256, cols) / 74) * std::max(c * blocks, epi)}); };
+    if (f32 || p.out_f32) pair(128, f32 ? 0.97 : 0.2, 5.4, 3.0);
+    else {
+        pair(256, 0.29, 7.1, 4.0);
+        pair(128, 0.166, 5.4, 2.9);
+    }
+    static constexpr double share[9] = {0, 0, 1.5, 2.1, 2.7, 3.1, 3.4, 3.8, 4.2};
+    auto tile = [&](int cols, double c, double base, double epi) {
+        for (int S = 1; S <= 8 && S <= blocks; ++S) {
+            const double room = S <= 2 ? 148 : S <= 4 ? 132 : 104;
+            const double waves = std::ceil(tiles(128, cols) * S / room);
+            take({false, cols, S, base + share[S] + waves * c * std::ceil(blocks / S) + (waves - 1) * epi});
+        }
+    };
+    tile(128, f32 ? 1.3 : 0.353, 3.6, 3.0);
+    if (gated == 1) tile(64, f32 ? 1.05 : 0.275, 3.1, 2.8);
+    return best;
+}
+
 ftp_status run_product(const Product& p, cudaStream_t st, const char* who) {
-    constexpr int SMS = 148;
     KArgs k{};
     k.e[0] = p.e[0]; k.e[1] = p.e[1];
     k.M = p.M; k.N = p.N; k.err = p.err;
     k.pa = p.A[0].planes; k.pb = p.B[0].planes;
     k.np = std::max(k.pa, k.pb);
-    k.chunk = k.np > 1 ? 1 : CHUNK;
+    k.chunk = CHUNK;
     k.kb_part = (int)((p.K + BK - 1) / BK);
     k.parts_k = (p.parts > 1 && p.cat_k) ? 2 : 1;
     k.parts_n = (p.parts > 1 && !p.cat_k && p.epi != EPI_GATED) ? 2 : 1;
+    const Form f = choose_form(k, p);
+    if (f.pair) return run_product_pair(p, k, f.cols == 256, st, who);
     k.tiles_m = (int)((p.M + 127) / 128);
-    const int gated = p.epi == EPI_GATED ? 2 : 1;
-    // CTA pairs where their 256 x 128 tiles cover most of the pairs at least once
-    const long long pair_m = (p.M + 255) / 256;
-    auto pair_tiles = [&](int bn) { return pair_m * ((p.N + bn / gated - 1) / (bn / gated)) * k.parts_n; };
-    if (pair_tiles(128) >= SMS / 2 - 10) {
-        // waves of the 74 pairs times a block's time: 256 x 128 takes 0.78 of 256 x 256 (8192 x 4096 x 4096 bf16: 281 against 180 us)
-        auto cost = [&](int bn) { return ((pair_tiles(bn) + SMS / 2 - 1) / (SMS / 2)) * (bn == 256 ? 100 : 78); };
-        return run_product_pair(p, k, cost(256) <= cost(128), st, who);
-    }
-    auto tiles = [&](int outc) { return (long long)k.tiles_m * ((p.N + outc - 1) / outc) * k.parts_n; };
-    const int outc128 = 128 / gated;
-    const bool narrow = p.epi != EPI_GATED && (p.N <= 64 || tiles(outc128) < SMS);
-    const int outc = narrow ? 64 : outc128;
+    const int outc = p.epi == EPI_GATED ? f.cols / 2 : f.cols;
     k.tiles_n = (p.N + outc - 1) / outc;
-    // slices of the reduction: as many as fill the SMs once (bf16: with two CTAs each), each at least four blocks long
-    const int room = p.out_f32 ? SMS : 2 * SMS;
-    const long long t = tiles(outc), blocks = (long long)k.kb_part * k.parts_k * k.np * k.np;
-    int S = 1;
-    while (S < 8 && t * S * 2 <= room && blocks / (S * 2) >= 4 && (long long)k.kb_part * k.parts_k >= S * 2) S *= 2;
-    FTP_REQUIRE(t * S < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-    if (p.epi == EPI_GATED) return tile_typed<128, false, true, EPI_GATED>(p, k, S, st, who);
-    if (p.epi == EPI_LINEAR) return narrow ? tile_typed<64, false, true, EPI_LINEAR>(p, k, S, st, who) : tile_typed<128, false, true, EPI_LINEAR>(p, k, S, st, who);
-    if (p.a_mn) return narrow ? tile_typed<64, true, true, EPI_STORE>(p, k, S, st, who) : tile_typed<128, true, true, EPI_STORE>(p, k, S, st, who);
-    return narrow ? tile_typed<64, false, false, EPI_STORE>(p, k, S, st, who) : tile_typed<128, false, false, EPI_STORE>(p, k, S, st, who);
+    FTP_REQUIRE((long long)k.tiles_m * k.tiles_n * k.parts_n * f.S < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    const bool narrow = f.cols == 64;
+    if (p.epi == EPI_GATED) return tile_typed<128, false, true, EPI_GATED>(p, k, f.S, st, who);
+    if (p.epi == EPI_LINEAR) return narrow ? tile_typed<64, false, true, EPI_LINEAR>(p, k, f.S, st, who) : tile_typed<128, false, true, EPI_LINEAR>(p, k, f.S, st, who);
+    if (p.a_mn) return narrow ? tile_typed<64, true, true, EPI_STORE>(p, k, f.S, st, who) : tile_typed<128, true, true, EPI_STORE>(p, k, f.S, st, who);
+    return narrow ? tile_typed<64, false, false, EPI_STORE>(p, k, f.S, st, who) : tile_typed<128, false, false, EPI_STORE>(p, k, f.S, st, who);
 }
 
 }  // namespace ffn

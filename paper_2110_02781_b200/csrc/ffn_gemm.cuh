@@ -10,14 +10,14 @@ using namespace tc;
 namespace ffn {
 
 constexpr int BK = 64;                       // reduction elements per stage: one 128-byte swizzle row
-// Operand tiles arrive one plane of A and of B at a time, the smallest planes of a block first; once the main planes are
-// there, the products of the block that matter are issued small terms first, each plane read from memory once:
+// Operand tiles arrive one plane of A and of B at a time, the smallest planes of a block first, each read from memory once;
+// the products that matter are issued as soon as their planes are there:
 //   plane 1: A1 B1    plane 0: A0 B2, A2 B0, A0 B1, A1 B0, A0 B0
 // (those with planes that exist).  Dropped: A1 B2, A2 B1, A2 B2, below 2^-24 of the result.
 //
 // Float results: the tensor cores cut their accumulator instead of rounding it, an error that grows with the number of
-// steps (measured 3.5e-5 of the result after 2048 steps of 16 elements).  So it is emptied into registers, which add with
-// rounding, after every block of a product of planes and every CHUNK blocks of a product of bf16 tensors.
+// steps (measured 3.5e-5 of the result after 2048 steps of 16 elements).  So the products of the main planes have an
+// accumulator of their own, and every CHUNK blocks both are emptied into registers, which add with rounding.
 constexpr int CHUNK = 4;
 
 struct KArgs {
@@ -47,6 +47,20 @@ __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32
         : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// 32 columns of an accumulator, and of its small terms `small` columns further, added to acc[0..31]
+__device__ __forceinline__ void add_acc(uint32_t taddr, uint32_t small, bool both, float* acc) {
+    uint32_t r[32], q[32];
+    tmem_ld32_issue(taddr, r);
+    if (both) tmem_ld32_issue(taddr + small, q);
+    tmem_ld_wait();
+    if (both) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[i] += __uint_as_float(r[i]) + __uint_as_float(q[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[i] += __uint_as_float(r[i]);
+    }
+}
 // MN-major operand: slabs of 64 reduction rows x 64 elements (128-byte rows, 128-byte swizzle), slab_bytes apart
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t slab_bytes) {
     return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)((slab_bytes >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
@@ -190,10 +204,13 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
                                ((uint32_t)(CG * 128 >> 4) << 24);
     const uint64_t a0 = AMN ? desc_mn(ring, SLAB) : umma_desc_k_sw128(ring), b0 = BMN ? desc_mn(ring + A_BYTES, SLAB) : umma_desc_k_sw128(ring + A_BYTES);
     Slot<STAGES> sl;
+    // float results: an accumulator is BN columns for the products of the main planes and BN for all the small ones, so that
+    // adding those costs the sum no accuracy
+    constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN;
     int chunk = 0;
-    bool first = true;
-    uint32_t d = tmem;
-    auto four = [&](int sa, int sb) {                                // a block of the planes in slots sa and sb; one thread
+    bool first = true, first_small = true;
+    uint32_t d0 = tmem;
+    auto four = [&](uint32_t d, bool& first, int sa, int sb) {       // a block of the planes in slots sa and sb; one thread
         const uint64_t ad = a0 + (uint64_t)((uint32_t)sa * (STAGE_BYTES >> 4)), bd = b0 + (uint64_t)((uint32_t)sb * (STAGE_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < BK / 16; ++k) {                          // 16 elements further: 32 bytes along a K-major row, 16 rows of an MN-major slab
@@ -211,8 +228,8 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
                 const int b = BUFS == 1 ? 0 : chunk & 1;
                 if (chunk >= BUFS && !warp_wait_for(acce0 + 8 * b, ((BUFS == 1 ? chunk : chunk >> 1) & 1) ^ 1, p.err, 4)) return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                d = tmem + (uint32_t)(b * BN);
-                first = true;
+                d0 = tmem + (uint32_t)b * ACC;
+                first = first_small = true;
                 left = CHUNKED ? min(p.chunk, blocks - kb) : blocks;
             }
             --left;
@@ -230,10 +247,10 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
                 }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (elect_one()) {
-                    four(s0, s0);
+                    four(d0, first, s0, s0);
                     commit(empty0 + 8 * s0);
                     if (two) {
-                        four(s1, s1);
+                        four(d0, first, s1, s1);
                         commit(empty0 + 8 * s1);
                     }
                     if (left == 0) commit(accf0 + 8 * (BUFS == 1 ? 0 : chunk & 1));
@@ -248,24 +265,24 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
                 sl.next();
                 const bool mid = p.pa > 1 && p.pb > 1;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (mid && elect_one()) four(s1, s1);
-                if (mid) first = false;
+                if (mid && elect_one()) four(d0 + BN, first_small, s1, s1);
+                if (mid) first_small = false;
                 const int s0 = sl.s;
                 if (!warp_wait_for(full0 + 8 * sl.s, sl.parity, p.err, 2)) return false;
                 sl.next();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (elect_one()) {
-                    if (p.pb > 2) four(s0, s2);
-                    if (p.pa > 2) four(s2, s0);
-                    if (p.pb > 1) four(s0, s1);
-                    if (p.pa > 1) four(s1, s0);
-                    four(s0, s0);
+                    if (p.pb > 2) four(d0 + BN, first_small, s0, s2);
+                    if (p.pa > 2) four(d0 + BN, first_small, s2, s0);
+                    if (p.pb > 1) four(d0 + BN, first_small, s0, s1);
+                    if (p.pa > 1) four(d0 + BN, first_small, s1, s0);
+                    four(d0, first, s0, s0);
                     commit(empty0 + 8 * s2);
                     commit(empty0 + 8 * s1);
                     commit(empty0 + 8 * s0);
                     if (left == 0) commit(accf0 + 8 * (BUFS == 1 ? 0 : chunk & 1));
                 }
-                first = false;
+                first = first_small = false;
             }
             __syncwarp();
             if (left == 0) ++chunk;

@@ -238,6 +238,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2, B_BYTES = BN / 2 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
     constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;             // output columns of a tile
     constexpr int WC = BN / 2;                                       // accumulator columns of an epilogue warp
+    constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN, TMEM_COLS = 2 * ACC;
+    static_assert(TMEM_COLS <= 512, "tensor memory");
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) unsigned long long bars[2 * STAGES + 4];
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"((uint32_t)(2 * BN)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -342,10 +344,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
 #pragma unroll
                     for (int g = 0; g < WC / 32; ++g) {
                         const int col = EPI == EPI_GATED ? (g < WC / 64 ? col0 + g * 32 : BN / 2 + col0 + (g - WC / 64) * 32) : col0 + g * 32;
-                        uint32_t r[32];
-                        tmem_ld32(lanes + (uint32_t)(b * BN + col), r);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[g * 32 + i] += __uint_as_float(r[i]);
+                        add_acc(lanes + (uint32_t)b * ACC + col, BN, p.np > 1, acc + g * 32);
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
@@ -400,7 +399,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     cluster_sync_all();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
 }
 
 template <typename T, int BN, bool AMN, bool BMN, int EPI>
