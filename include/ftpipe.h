@@ -18,6 +18,7 @@
  *     the loss stay float).
  *   - Canonical parameter order of a unit: its ops in order; per op
  *       CONV1D/CONV2D/FC : W[kh][kw][cin][cout] then bias[cout] if has_bias
+ *       LINEAR           : W[cin][cout] then bias[cout] if has_bias;  GATED: W_gate[cin][cout], W_up[cin][cout]
  *       DWCONV3x3        : W[3][3][c]
  *       BN               : gamma[c], beta[c]      (state: running_mean[c], running_var[c])
  *   - Ownership: the CALLER allocates every device and pinned-host buffer, including the
@@ -61,8 +62,14 @@ typedef enum {
 } ftp_status;
 
 enum { FTP_CONV1D = 0, FTP_CONV2D = 1, FTP_DWCONV3x3 = 2, FTP_BN = 3, FTP_ACT = 4, FTP_ADD_RESIDUAL = 5,
-       FTP_MAXPOOL2 = 6, FTP_GAP = 7, FTP_FC = 8, FTP_SOFTMAX_CE = 9 };
-/* GELU (z Phi(z), the error-function form) and SILU (z / (1 + e^-z)): the feed-forward operators below; a layer list takes 0..2 */
+       FTP_MAXPOOL2 = 6, FTP_GAP = 7, FTP_FC = 8, FTP_SOFTMAX_CE = 9,
+       /* token-wise feed-forward layers (see "feed-forward operators"), applied at every position of an (N, H, W, C) tensor:
+        *   LINEAR: act(x W + bias) + output of op residual_src (-1: none; within the unit, or its input)
+        *   GATED : act(x W_gate) * (x W_up)
+        * k is the form in which the values before the activation wait for the backward pass: 0 the tensors' type, 8 an
+        * 8-bit image, which halves (bf16) or quarters (float) what a batch in flight holds of them. */
+       FTP_LINEAR = 10, FTP_GATED = 11 };
+/* GELU (z Phi(z), the error-function form) and SILU (z / (1 + e^-z)): LINEAR and GATED only */
 enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2, FTP_ACT_GELU = 3, FTP_ACT_SILU = 4 };
 enum { FTP_FP32 = 0, FTP_BF16 = 1 };
 /* selector of ftp_get_tensor / ftp_set_tensor */
@@ -70,13 +77,13 @@ enum { FTP_T_WEIGHTS = 0, FTP_T_GRADS = 1, FTP_T_MOMENTUM = 2, FTP_T_STATE = 3 }
 
 typedef struct {
     int32_t unit;         /* partition unit of this op; non-decreasing along the list */
-    int32_t kind;         /* FTP_CONV1D ... FTP_SOFTMAX_CE */
+    int32_t kind;         /* FTP_CONV1D ... FTP_GATED */
     int32_t cin, cout;    /* channels in / out (BN, pools, ADD: cin == cout) */
-    int32_t k;            /* kernel size (CONV1D: 1 x k; CONV2D: k x k; DW: 3; FC: 1) */
+    int32_t k;            /* kernel size (CONV1D: 1 x k; CONV2D: k x k; DW: 3; FC: 1); LINEAR, GATED: 0 or 8 */
     int32_t stride, pad;
-    int32_t act;          /* activation applied to this op's output (CONV*, FC, BN, ACT) */
+    int32_t act;          /* activation applied to this op's output (CONV*, FC, BN, ACT, LINEAR, GATED) */
     int32_t has_bias;
-    int32_t residual_src; /* ADD_RESIDUAL: index of the op whose output is added; -1 otherwise */
+    int32_t residual_src; /* ADD_RESIDUAL, LINEAR: index of the op whose output is added; -1 otherwise */
 } ftp_layer_desc;
 
 typedef struct {
@@ -394,12 +401,13 @@ const char* ftp_kernel_name(int32_t kernel);
 ftp_status ftp_launch_count(const ftp_model* m, int64_t* launches);
 
 /* ---- feed-forward operators -----------------------------------------------------------------
- * (The paper trains convolutional networks; these are the token-wise layers of a stage of a language model, for callers
- * that string a stage's operators together themselves.)  A batch is `rows` tokens of `cin` channels, row-major; a weight
+ * (The paper trains convolutional networks; these are the token-wise layers of a stage of a language model: the layer kinds
+ * LINEAR and GATED, and the same for callers that string a stage's operators together themselves.)  A batch is `rows` tokens of `cin` channels, row-major; a weight
  * matrix is [cin][cout] as in the canonical parameter order; biases and their gradients are float; everything else has
  * the type `precision` names, with float accumulation.  Calls are asynchronous on the stream, launch on the current
  * device, allocate nothing and give the same bits for the same inputs.  They may be recorded into a CUDA graph.  A call
- * needs a workspace of its own for as long as it runs (in a graph: for as long as the graph may be replayed).
+ * needs a workspace of its own for as long as it runs (in a graph: for as long as the graph may be replayed).  Outputs may
+ * not overlap inputs or each other, but for the two cases named below.
  *
  * What a backward pass needs of its forward pass is kept by the caller, in the tensors' type or as an 8-bit image
  * (FTP_STASH_8BIT, and x_8bit for the input), which takes 33/32 byte per value: per row and 32 columns one scale s, the

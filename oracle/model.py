@@ -9,7 +9,7 @@ Sec. III-E (a replica is a copy of a stage's weights).
 import numpy as np
 from . import ops
 
-CONV1D, CONV2D, DW, BN, ACT, ADD, MAXPOOL, GAP, FC, CE = range(10)
+CONV1D, CONV2D, DW, BN, ACT, ADD, MAXPOOL, GAP, FC, CE, LINEAR, GATED = range(12)
 
 
 def round_bf16(x):
@@ -70,6 +70,20 @@ class OracleModel:
                     pre = self.q(pre)
                 self.saved[i] = pre
                 y = ops.act_fwd(pre, l.act)
+            elif l.kind in (LINEAR, GATED):
+                # weights as the tensor cores read them; what the backward pass gets of the values before the activation is
+                # what was kept: the tensors' type, or 8 bits; the result is rounded once, after the product or the residual
+                keep = ops.through_8_bits if l.k == 8 else self.q
+                pre = [x @ self.q(w) for w in (self.p[i] if l.kind == GATED else self.p[i][:1])]
+                if l.kind == LINEAR and l.has_bias:
+                    pre[0] = pre[0] + self.p[i][1]
+                y = ops.act_fwd(pre[0], l.act)
+                if l.kind == GATED:
+                    y = y * pre[1]
+                elif l.residual_src >= 0:
+                    y = y + self.out[l.residual_src]
+                y = self.q(y)
+                self.saved[i] = [keep(v) for v in pre] if l.kind == GATED or l.act else None
             elif l.kind == DW:
                 y = self.q(ops.dwconv_fwd(x, self.p[i][0], l.stride, l.pad))
             elif l.kind == BN:
@@ -131,6 +145,20 @@ class OracleModel:
                 if l.has_bias:
                     self.g[i][1] = db
                 acc(i - 1, dx)
+            elif l.kind in (LINEAR, GATED):
+                if l.kind == LINEAR:
+                    if l.residual_src >= 0:
+                        acc(l.residual_src, d)
+                    dz = [ops.act_bwd(self.saved[i][0], d, l.act) if l.act else d]
+                else:
+                    g, u = self.saved[i]
+                    dz = [ops.act_bwd(g, d * u, l.act), d * ops.act_fwd(g, l.act)]
+                if l.kind == LINEAR and l.has_bias:
+                    self.g[i][1] = dz[0].reshape(-1, l.cout).sum(axis=0)
+                dz = [self.q(v) for v in dz]                     # the products read it in the tensors' type
+                for k, v in enumerate(dz):
+                    self.g[i][k] = x.reshape(-1, l.cin).T @ v.reshape(-1, l.cout)
+                acc(i - 1, sum(v @ self.q(self.p[i][k]).T for k, v in enumerate(dz)))
             elif l.kind == DW:
                 dx, dw = ops.dwconv_bwd(x, self.p[i][0], d, l.stride, l.pad)
                 self.g[i][0] = dw
@@ -180,9 +208,11 @@ class OracleModel:
                 each.append((i, float(gap.min() / max(np.abs(x).max(), 1e-300))))
                 worst = min(worst, each[-1][1])
                 continue
-            if l.act == 0 or l.kind == CE:
-                continue
-            if l.kind in (CONV1D, CONV2D, FC):
+            if l.act not in (1, 2) or l.kind == CE:
+                continue                                         # the other activations are smooth
+            if l.kind in (LINEAR, GATED):
+                z = self.saved[i][0]
+            elif l.kind in (CONV1D, CONV2D, FC):
                 z = self.saved[i]
             elif l.kind == BN:
                 z = self.saved[i][0]

@@ -7,6 +7,8 @@ standard ones of that setting: cross-correlation with zero padding, batch normal
 training mode with biased batch variance, ReLU6 = min(max(z, 0), 6), mean-reduced softmax
 cross-entropy.  Activations are (N, H, W, C).
 """
+import math
+
 import numpy as np
 
 __all__ = ["conv_fwd", "conv_bwd", "dwconv_fwd", "dwconv_bwd", "bn_fwd", "bn_bwd", "act_fwd",
@@ -106,7 +108,18 @@ def act_fwd(z, act):
         return np.maximum(z, 0.0)
     if act == 2:
         return np.minimum(np.maximum(z, 0.0), 6.0)
+    if act == 3:
+        return z * normal_cdf(z)
+    if act == 4:
+        return z / (1.0 + np.exp(-z))
     return z
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+
+
+def normal_cdf(z):
+    return 0.5 * (1.0 + _erf(z / np.sqrt(2.0)))
 
 
 def act_bwd(z_pre, dout, act):
@@ -115,7 +128,25 @@ def act_bwd(z_pre, dout, act):
         return dout * (z_pre > 0.0)
     if act == 2:
         return dout * ((z_pre > 0.0) & (z_pre < 6.0))
+    if act == 3:
+        return dout * (normal_cdf(z_pre) + z_pre * np.exp(-0.5 * z_pre * z_pre) / np.sqrt(2.0 * np.pi))
+    if act == 4:
+        p = 1.0 / (1.0 + np.exp(-z_pre))
+        return dout * p * (1.0 + z_pre * (1.0 - p))
     return dout
+
+
+def through_8_bits(x):
+    """What the 8-bit image of x reads as: per 32 channels whole multiples, -127..127, of the power of two six binary orders
+    below the one at or under the largest magnitude."""
+    out = np.empty_like(x)
+    for a in range(0, x.shape[-1], 32):
+        v = x[..., a:a + 32]
+        top = np.abs(v).max(axis=-1, keepdims=True)
+        _, e = np.frexp(top)                                     # top = m 2^e, 0.5 <= m < 1
+        s = np.ldexp(1.0, np.where(top > 0, np.maximum(e - 7, -126), -126))
+        out[..., a:a + 32] = np.clip(np.rint(v / s), -127, 127) * s
+    return out
 
 
 def maxpool_fwd(x):

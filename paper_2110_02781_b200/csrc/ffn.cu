@@ -13,6 +13,12 @@ namespace {
 typedef __nv_bfloat16 bf16;
 constexpr int SMS = 148;
 
+template <typename... A>
+void launch(A&&... args) {
+    ++launches();
+    ftp::launch(std::forward<A>(args)...);
+}
+
 __device__ int g_op_status;                  // set by a kernel whose bounded wait ran out; cleared by ftp_check_op_status
 std::atomic<int*> g_status_addr[64] = {};
 
@@ -617,15 +623,19 @@ ftp_status launched(const char* who) {
 // ---- forward of both operators (w[1]: the gated operator's second matrix) ----
 template <typename T, bool GATED>
 ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, const float* bias, const void* residual, void* y, int stash_kind, void* stash,
-                   Carve& ws, cudaStream_t st, const char* who, const Operand* given_x = nullptr, const Operand* given_w = nullptr) {
+                   Carve& ws, int* err, cudaStream_t st, const char* who, const Operand* given_x = nullptr, const Operand* given_w = nullptr) {
     Product p{};
     const long long ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
     p.e[0].bias = bias; p.e[0].act = d->act;
     p.e[0].vec_bias = bias && aligned(bias, 16);
     set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
     set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, GATED ? 2 : 1);
-    if (!given_x && few_tokens(d->rows, d->cin, sizeof(T) == 4, GATED ? 2 : 1))
-        return ws.dry() ? FTP_OK : run_few(x, ldx, w, ldw, GATED ? 2 : 1, (int)d->rows, d->cin, d->cout, sizeof(T) == 4, p.e[0], st, who);
+    if (!given_x && few_tokens(d->rows, d->cin, sizeof(T) == 4, GATED ? 2 : 1)) {
+        if (ws.dry()) return FTP_OK;
+        if (!err) err = status_word();
+        FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+        return run_few(x, ldx, w, ldw, GATED ? 2 : 1, (int)d->rows, d->cin, d->cout, sizeof(T) == 4, p.e[0], err, st, who);
+    }
     Jobs jobs{};
     if (given_x) p.A[0] = *given_x;
     else if (ftp_status s = make_operand<T>(&p.A[0], x, d->rows, d->cin, ldx, d->unaligned, ws, jobs, st, who)) return s;
@@ -634,14 +644,15 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
         else if (ftp_status s = make_operand<T>(&p.B[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, jobs, st, who)) return s;
     }
     if (ws.dry()) return FTP_OK;
+    if (!err) err = status_word();
+    FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     run_now<T>(jobs, st);
     p.parts = GATED ? 2 : 1;
     p.b_mn = 1;
     p.M = d->rows; p.N = d->cout; p.K = d->cin;
     p.epi = GATED ? EPI_GATED : EPI_LINEAR;
     p.out_f32 = sizeof(T) == 4;
-    p.err = status_word();
-    FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);
+    p.err = err;
     return run_product(p, st, who);
 }
 
@@ -652,9 +663,11 @@ int grad_rows_per_block(long long rows) { return rows <= 256 ? 256 : (int)std::m
 // ---- backward of both operators ----
 template <typename T, bool GATED>
 ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, const void* stash, const void* dy, const void* addend, void* dx,
-                    void* const* dw, float* dbias, Carve& ws, cudaStream_t st, const char* who) {
+                    void* const* dw, float* dbias, Carve& ws, int* err, cudaStream_t st, const char* who) {
     const long long M = d->rows, ldx = d->ldx ? d->ldx : d->cin, ldw = d->ldw ? d->ldw : d->cout, ldy = d->ldy ? d->ldy : d->cout;
     const bool dry = ws.dry(), f32 = sizeof(T) == 4, want_dw = dry || dw[0], want_dx = dry || dx, recompute = GATED && d->stash == STASH_NONE;
+    // a gradient that passes unchanged is read in place
+    const bool direct = !GATED && !f32 && d->stash == STASH_NONE && !d->unaligned && (ldy % 8 == 0 || M == 1);
     Operand X{}, W[2] = {}, G[2] = {};
     Jobs jobs{};
     if (want_dw || recompute) {
@@ -664,18 +677,22 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
     if (want_dx || recompute)
         for (int i = 0; i < (GATED ? 2 : 1); ++i)
             if (ftp_status s = make_operand<T>(&W[i], w[i], d->cin, d->cout, ldw, d->unaligned, ws, jobs, st, who)) return s;
+    if (!dry) {
+        if (direct) FTP_REQUIRE(aligned(dy, 16), FTP_ERANGE, "%s: an operand does not start on a 16-byte boundary (set `unaligned`)", who);
+        if (!err) err = status_word();
+        FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    }
     int kind = d->stash;
     if (recompute) {
         stash = ws.take((size_t)(2 * M * d->cout) * sizeof(T));
         kind = STASH_FULL;
         if (!dry) run_now<T>(jobs, st);
         if (!dry)
-            if (ftp_status s = forward<T, GATED>(d, nullptr, nullptr, nullptr, nullptr, nullptr, STASH_FULL, const_cast<void*>(stash), ws, st, who, &X, W)) return s;
+            if (ftp_status s = forward<T, GATED>(d, nullptr, nullptr, nullptr, nullptr, nullptr, STASH_FULL, const_cast<void*>(stash), ws, err, st, who, &X, W)) return s;
     }
     // the gradient at the products' outputs
     GradArgs g{};
     const long long pitch = up8(d->cout);
-    const bool direct = !GATED && !f32 && kind == STASH_NONE && !d->unaligned && (ldy % 8 == 0 || M == 1);
     g.planes = f32 ? 3 : 1;
     g.plane = M * pitch;
     for (int i = 0; i < (GATED ? 2 : 1); ++i) {
@@ -689,7 +706,6 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
     const int chunks = (int)((M + g.rows_per_block - 1) / g.rows_per_block);
     float* sums = GATED || chunks == 1 ? nullptr : static_cast<float*>(ws.take((size_t)chunks * d->cout * 4));
     if (dry) return FTP_OK;
-    if (direct) FTP_REQUIRE(aligned(dy, 16), FTP_ERANGE, "%s: an operand does not start on a 16-byte boundary (set `unaligned`)", who);
     if (!direct || dbias) {
         g.dy = dy; g.lddy = ldy;
         g.act = d->act;
@@ -708,8 +724,7 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
     run_now<T>(jobs, st);                                            // nothing left of them after the gradient kernel
     if (ftp_status s = launched(who)) return s;
     Product p{};
-    p.err = status_word();
-    FTP_REQUIRE(p.err, FTP_ECUDA, "%s: no status word on this device", who);
+    p.err = err;
     p.epi = EPI_STORE;
     p.parts = GATED ? 2 : 1;
     if (dx) {
@@ -752,10 +767,10 @@ ftp_status workspace_bytes(const ftp_ffn_desc* d, int32_t back, size_t* bytes, c
     const void* w[2] = {nullptr, nullptr};
     void* dw[2] = {nullptr, nullptr};
     if (d->rows > 0) {
-        if (back) d->precision == FTP_FP32 ? backward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, who)
-                                           : backward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, who);
-        else d->precision == FTP_FP32 ? forward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, who)
-                                      : forward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, who);
+        if (back) d->precision == FTP_FP32 ? backward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, nullptr, who)
+                                           : backward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, nullptr, dw, nullptr, c, nullptr, nullptr, who);
+        else d->precision == FTP_FP32 ? forward<float, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, nullptr, who)
+                                      : forward<bf16, GATED>(d, nullptr, w, nullptr, nullptr, nullptr, 0, nullptr, c, nullptr, nullptr, who);
     }
     *bytes = c.off;
     return FTP_OK;
@@ -763,7 +778,7 @@ ftp_status workspace_bytes(const ftp_ffn_desc* d, int32_t back, size_t* bytes, c
 
 template <bool GATED>
 ftp_status check_and_forward(const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const float* bias, const void* residual, void* y, void* stash,
-                             void* ws, size_t ws_bytes, cudaStream_t st, const char* who) {
+                             void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who) {
     size_t need = 0;
     if (ftp_status s = workspace_bytes<GATED>(d, 0, &need, who)) return s;
     FTP_REQUIRE(d->ldr == 0 || !residual || d->ldr >= d->cout, FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
@@ -775,14 +790,14 @@ ftp_status check_and_forward(const ftp_ffn_desc* d, const void* x, const void* w
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
-    const ftp_status s = d->precision == FTP_FP32 ? forward<float, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, st, who)
-                                                  : forward<bf16, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, st, who);
+    const ftp_status s = d->precision == FTP_FP32 ? forward<float, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, err, st, who)
+                                                  : forward<bf16, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, err, st, who);
     return s ? s : launched(who);
 }
 
 template <bool GATED>
 ftp_status check_and_backward(const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const void* stash, const void* dy, const void* addend, void* dx,
-                              void* dw0, void* dw1, float* dbias, void* ws, size_t ws_bytes, cudaStream_t st, const char* who) {
+                              void* dw0, void* dw1, float* dbias, void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who) {
     size_t need = 0;
     if (ftp_status s = workspace_bytes<GATED>(d, 1, &need, who)) return s;
     FTP_REQUIRE(d->ldr == 0 || !addend || d->ldr >= d->cin, FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
@@ -799,12 +814,30 @@ ftp_status check_and_backward(const ftp_ffn_desc* d, const void* x, const void* 
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
-    const ftp_status s = d->precision == FTP_FP32 ? backward<float, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, st, who)
-                                                  : backward<bf16, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, st, who);
+    const ftp_status s = d->precision == FTP_FP32 ? backward<float, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, err, st, who)
+                                                  : backward<bf16, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, err, st, who);
     return s ? s : launched(who);
 }
 
 }  // namespace
+
+unsigned& launches() {
+    static thread_local unsigned n = 0;
+    return n;
+}
+ftp_status op_workspace(bool gated, const ftp_ffn_desc* d, bool backward, size_t* bytes, const char* who) {
+    return gated ? workspace_bytes<true>(d, backward, bytes, who) : workspace_bytes<false>(d, backward, bytes, who);
+}
+ftp_status op_forward(bool gated, const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const float* bias, const void* residual, void* y,
+                      void* stash, void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who) {
+    return gated ? check_and_forward<true>(d, x, w0, w1, bias, residual, y, stash, ws, ws_bytes, err, st, who)
+                 : check_and_forward<false>(d, x, w0, w1, bias, residual, y, stash, ws, ws_bytes, err, st, who);
+}
+ftp_status op_backward(bool gated, const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const void* stash, const void* dy, const void* addend,
+                       void* dx, void* dw0, void* dw1, float* dbias, void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who) {
+    return gated ? check_and_backward<true>(d, x, w0, w1, stash, dy, addend, dx, dw0, dw1, dbias, ws, ws_bytes, err, st, who)
+                 : check_and_backward<false>(d, x, w0, w1, stash, dy, addend, dx, dw0, dw1, dbias, ws, ws_bytes, err, st, who);
+}
 
 // In host code the word's name is only a handle; the address a kernel may use has to be asked for, once per device.
 int* status_word() {
@@ -836,21 +869,21 @@ ftp_status ftp_gated_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, si
 
 ftp_status ftp_linear_forward(const ftp_ffn_desc* d, const void* x, const void* w, const float* bias, const void* residual, void* y, void* stash, void* ws,
                               size_t ws_bytes, void* stream) {
-    return check_and_forward<false>(d, x, w, nullptr, bias, residual, y, stash, ws, ws_bytes, static_cast<cudaStream_t>(stream), "linear_forward");
+    return check_and_forward<false>(d, x, w, nullptr, bias, residual, y, stash, ws, ws_bytes, nullptr, static_cast<cudaStream_t>(stream), "linear_forward");
 }
 ftp_status ftp_gated_forward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h, void* stash, void* ws, size_t ws_bytes,
                              void* stream) {
-    return check_and_forward<true>(d, x, w_gate, w_up, nullptr, nullptr, h, stash, ws, ws_bytes, static_cast<cudaStream_t>(stream), "gated_forward");
+    return check_and_forward<true>(d, x, w_gate, w_up, nullptr, nullptr, h, stash, ws, ws_bytes, nullptr, static_cast<cudaStream_t>(stream), "gated_forward");
 }
 
 ftp_status ftp_linear_backward(const ftp_ffn_desc* d, const void* x, const void* w, const void* stash, const void* dy, const void* dx_addend, void* dx, void* dw,
                                float* dbias, void* ws, size_t ws_bytes, void* stream) {
-    return check_and_backward<false>(d, x, w, nullptr, stash, dy, dx_addend, dx, dw, nullptr, dbias, ws, ws_bytes, static_cast<cudaStream_t>(stream),
+    return check_and_backward<false>(d, x, w, nullptr, stash, dy, dx_addend, dx, dw, nullptr, dbias, ws, ws_bytes, nullptr, static_cast<cudaStream_t>(stream),
                                      "linear_backward");
 }
 ftp_status ftp_gated_backward(const ftp_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, const void* stash, const void* dh,
                               const void* dx_addend, void* dx, void* dw_gate, void* dw_up, void* ws, size_t ws_bytes, void* stream) {
-    return check_and_backward<true>(d, x, w_gate, w_up, stash, dh, dx_addend, dx, dw_gate, dw_up, nullptr, ws, ws_bytes, static_cast<cudaStream_t>(stream),
+    return check_and_backward<true>(d, x, w_gate, w_up, stash, dh, dx_addend, dx, dw_gate, dw_up, nullptr, ws, ws_bytes, nullptr, static_cast<cudaStream_t>(stream),
                                     "gated_backward");
 }
 

@@ -79,10 +79,18 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who);
 // Products of a few tokens, read from the tensors as they are (ffn_few.cu).
 constexpr int FEW_SMEM = 96 * 1024;          // of it for the tokens
 bool few_tokens(long long rows, long long cin, bool f32, int products);
-ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, cudaStream_t st,
-                   const char* who);
+ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, int* err,
+                   cudaStream_t st, const char* who);
 
 int* status_word();                         // device word that a kernel whose bounded wait ran out writes a code to
+
+// The entry points' work for callers inside the library: `err` is the status word that a timed-out wait writes to.
+ftp_status op_workspace(bool gated, const ftp_ffn_desc* d, bool backward, size_t* bytes, const char* who);
+ftp_status op_forward(bool gated, const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const float* bias, const void* residual, void* y,
+                      void* stash, void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who);
+ftp_status op_backward(bool gated, const ftp_ffn_desc* d, const void* x, const void* w0, const void* w1, const void* stash, const void* dy, const void* addend,
+                       void* dx, void* dw0, void* dw1, float* dbias, void* ws, size_t ws_bytes, int* err, cudaStream_t st, const char* who);
+unsigned& launches();                       // kernel launches of this thread so far
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 

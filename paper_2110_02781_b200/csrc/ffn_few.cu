@@ -453,8 +453,8 @@ bool few_tokens(long long rows, long long cin, bool f32, int products) {
     return rows <= (f32 ? (products == 2 ? 16 : 32) : (products == 2 ? 2 : 4)) && few_smem(rows, (cin + 7) / 8, f32, products) <= FEW_SMEM;
 }
 
-ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, cudaStream_t st,
-                   const char* who) {
+ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, int* err,
+                   cudaStream_t st, const char* who) {
     constexpr int SMS = 148;
     FewArgs a{};
     a.x = x; a.ldx = ldx; a.ldw = ldw;
@@ -462,8 +462,7 @@ ftp_status run_few(const void* x, long long ldx, const void* const* w, long long
     a.vec_w = aligned(w[0], 16) && (products == 1 || aligned(w[1], 16)) && ldw * (f32 ? 4 : 2) % 16 == 0;
     a.vec_x = aligned(x, 16) && (rows == 1 || ldx * (f32 ? 4 : 2) % 16 == 0);
     a.e = e;
-    a.err = status_word();
-    FTP_REQUIRE(a.err, FTP_ECUDA, "%s: no status word on this device", who);
+    a.err = err;
     a.rows = rows; a.K = K; a.N = N;
     // Up to 4 MB of w the loads into registers are quicker, whose kernel begins and ends faster (one token, 1024 x 1024 bf16:
     // 3.6 against 4.6 us; 4096 x 4096 float: 14.2 against 13.1; the gated 4096 x 12288 bf16: 45 against 34.6)

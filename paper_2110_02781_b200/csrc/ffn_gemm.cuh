@@ -329,6 +329,7 @@ cudaError_t allow_smem(std::atomic<unsigned long long>& done, K kern, int bytes)
 
 template <typename... KA, typename... A>
 cudaError_t launch_cluster(void (*kern)(KA...), dim3 grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, A&&... args) {
+    ++launches();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(block);

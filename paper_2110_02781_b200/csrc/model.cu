@@ -7,6 +7,7 @@
 #include <cstring>
 #include <new>
 #include <type_traits>
+#include "ffn.h"
 #include "model.h"
 
 using namespace ftp;
@@ -41,7 +42,7 @@ const char* kKernelNames[K_COUNT] = {
     "bn_bwd_finalize", "bn_bwd_apply", "act_bias_bwd", "dw_fwd", "dw_dgrad", "dw_wgrad", "maxpool_fwd", "maxpool_bwd",
     "gap_fwd", "gap_bwd", "softmax_ce", "sgd", "act_fwd", "act_bwd", "copy", "tc_gemm_bf16_fwd", "tc_gemm_bf16_dgrad",
     "tc_gemm_bf16_wgrad", "conv_fwd_bf16_simt", "conv_dgrad_bf16_simt", "conv_wgrad_bf16_simt",
-    "tc_gemm_tf32x3_fwd", "tc_gemm_tf32x3_dgrad", "tc_gemm_tf32x3_wgrad"};
+    "tc_gemm_tf32x3_fwd", "tc_gemm_tf32x3_dgrad", "tc_gemm_tf32x3_wgrad", "linear_fwd", "linear_bwd", "gated_fwd", "gated_bwd"};
 
 // Brackets one launcher call with events when tracing is on.
 struct Scope {
@@ -65,6 +66,7 @@ struct Scope {
 };
 
 bool is_contraction(int kind) { return kind == FTP_CONV1D || kind == FTP_CONV2D || kind == FTP_FC; }
+bool is_ffn(int kind) { return kind == FTP_LINEAR || kind == FTP_GATED; }
 bool is_pointwise_op(const Op& o);
 bool is_3x3_op(const Op& o);
 
@@ -98,7 +100,7 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
         o.w_cnt = o.b_cnt = 0;
         o.gslot = -1; o.galias = i; o.addend_of = -1;
         o.Ho = H; o.Wo = W; o.Co = C;
-        FTP_REQUIRE(d.act >= 0 && d.act <= 2, FTP_EINVAL, "build_model: op %d: unknown activation %d", i, d.act);
+        FTP_REQUIRE(d.act >= 0 && d.act <= (is_ffn(d.kind) ? FTP_ACT_SILU : FTP_ACT_RELU6), FTP_EINVAL, "build_model: op %d: unknown activation %d", i, d.act);
         switch (d.kind) {
             case FTP_CONV1D: case FTP_CONV2D: case FTP_FC: {
                 FTP_REQUIRE(d.cin == C && d.cout >= 1, FTP_EINVAL, "build_model: op %d: cin %d does not match the incoming %d channels", i, d.cin, C);
@@ -112,6 +114,22 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
                 o.g = ConvGeom{N, H, W, C, o.Ho, o.Wo, o.Co, kh, kw, st, ph, pw};
                 o.w_off = poff; o.w_cnt = (long long)kh * kw * C * d.cout; poff += o.w_cnt;
                 if (d.has_bias) { o.b_off = poff; o.b_cnt = d.cout; poff += o.b_cnt; }
+                break;
+            }
+            case FTP_LINEAR: case FTP_GATED: {
+                FTP_REQUIRE(d.cin == C && d.cout >= 1, FTP_EINVAL, "build_model: op %d: cin %d does not match the incoming %d channels", i, d.cin, C);
+                FTP_REQUIRE(d.k == 0 || d.k == 8, FTP_EINVAL, "build_model: op %d: k is the form of the kept values, 0 or 8 bits", i);
+                FTP_REQUIRE(d.stride == 1 && d.pad == 0, FTP_EINVAL, "build_model: op %d: a token-wise op has stride 1 and no padding", i);
+                o.Co = d.cout;
+                o.w_off = poff; o.w_cnt = (d.kind == FTP_GATED ? 2LL : 1LL) * C * d.cout; poff += o.w_cnt;
+                FTP_REQUIRE(d.kind == FTP_LINEAR || (!d.has_bias && d.residual_src < 0), FTP_EUNSUPPORTED, "build_model: op %d: GATED has neither bias nor residual", i);
+                if (d.has_bias) { o.b_off = poff; o.b_cnt = d.cout; poff += o.b_cnt; }
+                if (d.residual_src >= 0) {
+                    const int s = d.residual_src;
+                    FTP_REQUIRE(s < i, FTP_EINVAL, "build_model: op %d: residual_src %d out of range", i, s);
+                    FTP_REQUIRE(s >= m.unit_first.back() - 1, FTP_EINVAL, "build_model: op %d: a residual connection may not cross a unit edge", i);
+                    FTP_REQUIRE(m.ops[s].Ho == H && m.ops[s].Wo == W && m.ops[s].Co == d.cout, FTP_EINVAL, "build_model: op %d: residual shapes differ", i);
+                }
                 break;
             }
             case FTP_DWCONV3x3:
@@ -193,7 +211,7 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
         const Op& c = m.ops[i + 1];
         if (o.d.kind != FTP_BN || o.fused_add || c.d.unit != o.d.unit) continue;
         bool other_reader = false;
-        for (int j = i + 2; j < n; ++j) other_reader |= m.ops[j].d.kind == FTP_ADD_RESIDUAL && m.ops[j].d.residual_src == i;
+        for (int j = i + 1; j < n; ++j) other_reader |= (m.ops[j].d.kind == FTP_ADD_RESIDUAL || m.ops[j].d.kind == FTP_LINEAR) && m.ops[j].d.residual_src == i;
         if (other_reader || (double)o.out_elems * m.esize > fuse_max_bytes) continue;
         void* const al = reinterpret_cast<void*>(256);
         if (c.d.kind == FTP_DWCONV3x3) o.defer = (fuse & 1) != 0 || ((fuse & 4) != 0 && c.g.stride == 2);
@@ -234,6 +252,12 @@ ftp_status plan_gradients(ftp_model& m, int* n_slots) {
             if (s >= 0) refc[s] += 1;                   // readers: op i-1 (already counted as op i's read) and the addend user
             continue;
         }
+        if (o.d.kind == FTP_LINEAR && o.d.residual_src >= 0) {   // the residual's gradient is this op's output gradient
+            const int src = o.d.residual_src;
+            FTP_REQUIRE(pending[src + 1] < 0, FTP_EUNSUPPORTED, "build_model: op %d: two residual adds share one source", i);
+            pending[src + 1] = k;
+            if (s >= 0) refc[s] += 1;
+        }
         if (i > 0) {
             m.ops[i - 1].gslot = alloc();
             if (pending[i] >= 0) o.addend_of = pending[i];
@@ -244,6 +268,18 @@ ftp_status plan_gradients(ftp_model& m, int* n_slots) {
     }
     *n_slots = (int)refc.size();
     return FTP_OK;
+}
+
+// descriptor of a token-wise op: tokens = all positions of the batch
+ftp_ffn_desc ffn_desc(const ftp_model& m, const Op& o) {
+    ftp_ffn_desc d{};
+    d.rows = (long long)o.N * o.H * o.W;
+    d.cin = o.C; d.cout = o.Co;
+    d.precision = m.cfg.precision; d.act = o.d.act;
+    d.dw_f32 = m.cfg.precision == FTP_BF16;
+    // what the backward pass needs of the values before the activation: nothing of a linear op without one
+    d.stash = o.d.kind == FTP_LINEAR && o.d.act == FTP_ACT_NONE ? FTP_STASH_NONE : o.d.k == 8 ? FTP_STASH_8BIT : FTP_STASH_FULL;
+    return d;
 }
 
 // ---- memory layout inside the workspace --------------------------------------------------------------
@@ -285,7 +321,7 @@ ftp_status layout(ftp_model& m, char* dev_base, size_t* dev_total, size_t* pinne
     }
     m.grad = (float*)bp.take((size_t)m.P * 4);
     m.state_backup = (float*)bp.take((size_t)std::max<long long>(m.R, 1) * 4);
-    size_t max_act = 0, red = 0, dwp = 0, foldd = 0, dpre = 0, finp = 64, finc = 1, fcin = 64;
+    size_t max_act = 0, red = 0, dwp = 0, foldd = 0, dpre = 0, finp = 64, finc = 1, fcin = 64, ffn = 0;
     for (int i = 0; i < n; ++i) {
         Op& o = m.ops[i];
         const size_t obytes = (size_t)o.out_elems * (o.out_f32 ? 4 : es);
@@ -315,6 +351,17 @@ ftp_status layout(ftp_model& m, char* dev_base, size_t* dev_total, size_t* pinne
             if (o.d.act != FTP_ACT_NONE || o.d.has_bias) foldd = std::max(foldd, fold_partial_doubles(o.fold));
             if (o.d.act != FTP_ACT_NONE) dpre = std::max(dpre, obytes);
             if (o.d.kind == FTP_FC) fcin = std::max(fcin, (size_t)o.in_elems);
+        } else if (is_ffn(o.d.kind)) {
+            const bool gated = o.d.kind == FTP_GATED;
+            ftp_ffn_desc d = ffn_desc(m, o);
+            o.keep = d.stash == FTP_STASH_NONE ? nullptr
+                     : bp.take(d.stash == FTP_STASH_8BIT ? (gated ? 2 : 1) * ffn::image_part_bytes(Mout, o.Co) : (gated ? 2 : 1) * obytes);
+            d.unaligned = 1;                                           // what any boundary buffer needs
+            for (int back = 0; back < 2; ++back) {
+                size_t need = 0;
+                if (ftp_status st = ffn::op_workspace(gated, &d, back, &need, "build_model")) return st;
+                ffn = std::max(ffn, need);
+            }
         } else if (o.d.kind == FTP_DWCONV3x3) {
             red = std::max(red, dwconv_wgrad_scratch_floats(o.g));
             dwp = std::max(dwp, dwconv_wgrad_scratch_floats(o.g));
@@ -334,6 +381,7 @@ ftp_status layout(ftp_model& m, char* dev_base, size_t* dev_total, size_t* pinne
     m.fold_doubles = std::max<size_t>(foldd, 64); m.fold_scratch = (double*)bp.take(m.fold_doubles * 8);
     m.dpre_bytes = std::max<size_t>(dpre, 256); m.dpre = bp.take(m.dpre_bytes);
     m.tc_err = (int*)bp.take(256);
+    m.ffn_ws_bytes = ffn; m.ffn_ws = ffn ? bp.take(ffn) : nullptr;
     m.fc_in = (float*)bp.take(fcin * 4); m.fc_din = (float*)bp.take(fcin * 4);
     m.fin.part = (double*)bp.take(finp * 8);
     m.fin_counter_bytes = finc * 4; m.fin.counters = (unsigned*)bp.take(m.fin_counter_bytes);
@@ -387,6 +435,11 @@ ftp_status check_launches(const char* where) {
 
 inline bool a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+
+// the weights as the linear and gated operators read them
+template <typename T> const T* ffn_weights(const Arena& ar);
+template <> const float* ffn_weights<float>(const Arena& ar) { return ar.w; }
+template <> const __nv_bfloat16* ffn_weights<__nv_bfloat16>(const Arena& ar) { return ar.wb; }
 
 // ---- forward of a unit range ------------------------------------------------------------------------------
 template <typename T>
@@ -444,6 +497,22 @@ ftp_status fwd_range(ftp_model* m, int a, int b, const void* act_in, void* act_o
                         if (!tc) conv_fwd_bf16_simt((const T*)in, ar.wb + o.w_off, o.b_off >= 0 ? ar.w + o.b_off : nullptr, (T*)out, o.g, o.d.act, st);
                     }
                 }
+                break;
+            }
+            case FTP_LINEAR: case FTP_GATED: {
+                const bool gated = o.d.kind == FTP_GATED;
+                ftp_ffn_desc d = ffn_desc(*m, o);
+                const T* w = ffn_weights<T>(ar) + o.w_off;
+                const T* w1 = gated ? w + o.w_cnt / 2 : nullptr;
+                const void* res = o.d.residual_src < 0 ? nullptr : o.d.residual_src < first ? act_in : m->cur_out[o.d.residual_src];
+                d.unaligned = !a16(in) || !a16(w) || (gated && !a16(w1));
+                const double kept = d.stash == FTP_STASH_NONE ? 0.0 : (gated ? 2.0 : 1.0) * (d.stash == FTP_STASH_8BIT ? 33.0 / 32.0 : es) * o.out_elems;
+                const unsigned before = ffn::launches();
+                Scope sc(m, st, gated ? K_GATED_FWD : K_LINEAR_FWD, u, i, 0, (o.in_elems + o.out_elems * (res ? 2.0 : 1.0) + o.w_cnt) * es + kept, 2.0 * Mout * o.w_cnt, 0);
+                const ftp_status s = ffn::op_forward(gated, &d, in, w, w1, o.b_off >= 0 ? ar.w + o.b_off : nullptr, res, out, o.keep, m->ffn_ws, m->ffn_ws_bytes,
+                                                     m->tc_err, st, "forward");
+                g_launches += ffn::launches() - before;
+                if (s != FTP_OK) return s;
                 break;
             }
             case FTP_DWCONV3x3: {
@@ -646,6 +715,23 @@ ftp_status bwd_range(ftp_model* m, int a, int b, const void* grad_out, void* gra
                         if (!tc) conv_dgrad_bf16_simt(d, ar.wb + o.w_off, (const T*)addend, (T*)gi, o.g, st);
                     }
                 }
+                break;
+            }
+            case FTP_LINEAR: case FTP_GATED: {
+                const bool gated = o.d.kind == FTP_GATED;
+                ftp_ffn_desc d = ffn_desc(*m, o);
+                const T* w = ffn_weights<T>(ar) + o.w_off;
+                const T* w1 = gated ? w + o.w_cnt / 2 : nullptr;
+                d.unaligned = !a16(in) || !a16(w) || !a16(go) || (gated && !a16(w1));
+                const double kept = d.stash == FTP_STASH_NONE ? 0.0 : (gated ? 2.0 : 1.0) * (d.stash == FTP_STASH_8BIT ? 33.0 / 32.0 : es) * o.out_elems;
+                const unsigned before = ffn::launches();
+                Scope sc(m, st, gated ? K_GATED_BWD : K_LINEAR_BWD, u, i, 1, (o.in_elems * (gi ? (addend ? 3.0 : 2.0) : 1.0) + o.out_elems + o.w_cnt) * es + o.w_cnt * 4.0 + kept,
+                         2.0 * Mout * o.w_cnt * (gi ? 2.0 : 1.0), 0);
+                float* dw1 = gated ? gr + o.w_off + o.w_cnt / 2 : nullptr;
+                const ftp_status s = ffn::op_backward(gated, &d, in, w, w1, o.keep, go, gi ? addend : nullptr, gi, gr + o.w_off, dw1, o.b_off >= 0 ? gr + o.b_off : nullptr,
+                                                      m->ffn_ws, m->ffn_ws_bytes, m->tc_err, st, "backward");
+                g_launches += ffn::launches() - before;
+                if (s != FTP_OK) return s;
                 break;
             }
             case FTP_DWCONV3x3: {

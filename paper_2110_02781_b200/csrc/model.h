@@ -12,7 +12,8 @@ enum KernelId {
     K_CONV_FWD_F32 = 0, K_CONV_DGRAD_F32, K_CONV_WGRAD_F32, K_BN_STATS, K_BN_FINALIZE, K_BN_APPLY, K_BN_BWD_REDUCE,
     K_BN_BWD_FINALIZE, K_BN_BWD_APPLY, K_ACT_BIAS_BWD, K_DW_FWD, K_DW_DGRAD, K_DW_WGRAD, K_MAXPOOL_FWD,
     K_MAXPOOL_BWD, K_GAP_FWD, K_GAP_BWD, K_SOFTMAX_CE, K_SGD, K_ACT_FWD, K_ACT_BWD, K_COPY, K_GEMM_BF16_FWD,
-    K_GEMM_BF16_DGRAD, K_GEMM_BF16_WGRAD, K_CONV_FWD_BF16_SIMT, K_CONV_DGRAD_BF16_SIMT, K_CONV_WGRAD_BF16_SIMT, K_TC32_FWD, K_TC32_DGRAD, K_TC32_WGRAD, K_COUNT
+    K_GEMM_BF16_DGRAD, K_GEMM_BF16_WGRAD, K_CONV_FWD_BF16_SIMT, K_CONV_DGRAD_BF16_SIMT, K_CONV_WGRAD_BF16_SIMT, K_TC32_FWD, K_TC32_DGRAD, K_TC32_WGRAD,
+    K_LINEAR_FWD, K_LINEAR_BWD, K_GATED_FWD, K_GATED_BWD, K_COUNT
 };
 
 struct Op {
@@ -33,6 +34,7 @@ struct Op {
     bool defer;              // BN whose normalised output is never stored: the next op of the unit applies it to what it loads
     int gslot;               // slot holding the gradient w.r.t. this op's output (-1 none, -2 dlogits)
     int galias;              // op whose output-gradient buffer this op's output gradient shares
+    void* keep;              // linear / gated: the values before the activation, kept for the backward pass
     int addend_of;           // when writing the gradient of this op's input, add the gradient buffer of that op's output
 };
 
@@ -84,6 +86,7 @@ struct ftp_model {
     ftp::TransposeEntryDev* tp_dev;
     void* dpre; size_t dpre_bytes;
     int* tc_err;                                  // device word set by a tensor-core kernel whose bounded wait ran out
+    void* ffn_ws; size_t ffn_ws_bytes;            // workspace of the linear and gated operators
     float* fc_in; float* fc_din;                  // bf16 models: the classifier's input and input gradient widened to float
     float* dlogits; float* per_sample; float* loss_dev; int32_t* labels_dev; void* input_dev; float* state_backup;
     float* pinned; size_t pinned_bytes;

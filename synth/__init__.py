@@ -5,9 +5,9 @@ random streams and the input / initial-weight generators.  It contains none of t
 method's arithmetic: no forward, backward, optimiser, partition or snapshot code.
 """
 from .nets import (Layer, KIND, ACT, har_cnn, mobilenetv2, vgg16, tiny_mbv2, tiny_vgg, continual_mbv2,
-                   param_shapes, state_shapes, num_units, config)
+                   token_ffn, param_shapes, state_shapes, num_units, config)
 from .inputs import rng_stream, make_batch, init_params, init_state, flat_unit_params
 
-__all__ = ["Layer", "KIND", "ACT", "har_cnn", "mobilenetv2", "vgg16", "tiny_mbv2", "tiny_vgg", "continual_mbv2",
+__all__ = ["Layer", "KIND", "ACT", "har_cnn", "mobilenetv2", "vgg16", "tiny_mbv2", "tiny_vgg", "continual_mbv2", "token_ffn",
            "param_shapes", "state_shapes", "num_units", "config", "rng_stream", "make_batch",
            "init_params", "init_state", "flat_unit_params"]

@@ -38,6 +38,8 @@ def init_params(config_index, layers):
             arrs.append((g.standard_normal(s) * np.sqrt(2.0 / fan_in)).astype(np.float32))
             for b in shapes[1:]:
                 arrs.append(np.zeros(b, np.float32))
+        elif l.kind in (KIND["LINEAR"], KIND["GATED"]):
+            arrs = [(g.standard_normal(s) * np.sqrt(2.0 / l.cin)).astype(np.float32) if len(s) == 2 else np.zeros(s, np.float32) for s in shapes]
         elif l.kind == KIND["BN"]:
             arrs = [np.ones(shapes[0], np.float32), np.zeros(shapes[1], np.float32)]
         out.append(arrs)

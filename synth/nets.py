@@ -9,14 +9,15 @@ Canonical parameter order inside an op (an interface convention, restated on eac
   CONV1D / CONV2D / FC : W[kh][kw][cin][cout] (FC: kh = kw = 1), then bias[cout] if has_bias
   DWCONV3x3           : W[3][3][c]
   BN                  : gamma[c], beta[c]           (state: running_mean[c], running_var[c])
+  LINEAR              : W[cin][cout], then bias[cout] if has_bias;  GATED: W_gate[cin][cout], W_up[cin][cout]
 """
 from collections import namedtuple
 
 Layer = namedtuple("Layer", "unit kind cin cout k stride pad act has_bias residual_src")
 
 KIND = dict(CONV1D=0, CONV2D=1, DWCONV3x3=2, BN=3, ACT=4, ADD_RESIDUAL=5, MAXPOOL2=6, GAP=7, FC=8,
-            SOFTMAX_CE=9)
-ACT = dict(NONE=0, RELU=1, RELU6=2)
+            SOFTMAX_CE=9, LINEAR=10, GATED=11)
+ACT = dict(NONE=0, RELU=1, RELU6=2, GELU=3, SILU=4)
 
 
 def _L(unit, kind, cin=0, cout=0, k=0, stride=1, pad=0, act="NONE", has_bias=0, residual_src=-1):
@@ -122,6 +123,22 @@ def tiny_vgg(batch=4, hw=4, n_classes=3, precision=0):
     return vgg16(batch, hw, n_classes, precision, plan=[8, "M", 8, "M"], momentum=0.9)
 
 
+def token_ffn(batch=4, tokens=12, in_c=16, d=32, f=48, blocks=2, n_classes=5, precision=0, kept=0, act="SILU", lr=0.01, momentum=0.9,
+              weight_decay=4e-5):
+    """A feed-forward network over tokens: [linear + bias + GELU], then blocks of [BN, gated block, linear + residual], global
+    average pooling, FC.  `kept`: form of the values before the activations (0: the tensors' type, 8: 8 bits)."""
+    ls = [_L(0, "LINEAR", in_c, d, kept, act="GELU", has_bias=1)]
+    for u in range(1, blocks + 1):
+        src = len(ls) - 1
+        ls.append(_L(u, "BN", d, d))
+        ls.append(_L(u, "GATED", d, f, kept, act=act))
+        ls.append(_L(u, "LINEAR", f, d, kept, has_bias=1, residual_src=src))
+    ls.append(_L(blocks + 1, "GAP", d, d))
+    ls.append(_L(blocks + 1, "FC", d, n_classes, 1, 1, 0, "NONE", 1))
+    ls.append(_L(blocks + 1, "SOFTMAX_CE", n_classes, n_classes))
+    return ls, config(batch, in_c, 1, tokens, n_classes, precision, lr=lr, momentum=momentum, weight_decay=weight_decay)
+
+
 def param_shapes(l):
     """Shapes of the trainable arrays of one op, in canonical order."""
     k = l.kind
@@ -135,6 +152,10 @@ def param_shapes(l):
         return [(3, 3, l.cin)]
     elif k == KIND["BN"]:
         return [(l.cin,), (l.cin,)]
+    elif k == KIND["LINEAR"]:
+        s = [(l.cin, l.cout)]
+    elif k == KIND["GATED"]:
+        return [(l.cin, l.cout), (l.cin, l.cout)]
     else:
         return []
     if l.has_bias:

@@ -96,3 +96,25 @@ def test_calls_that_are_refused():
     assert L.ftp_checkpoint_unpack(P, -1, 4, 4, 1, P, 0, None) == 1
     assert L.ftp_checkpoint_pack(None, 0, 4, 0, 1, None, 0, None) == 0                                    # no rows: nothing to do
     assert L.ftp_linear_forward(ref(desc(rows=0)), None, None, None, None, None, None, None, 0, None) == 0
+
+
+# ---- the layer kinds -----------------------------------------------------------------------------------------------
+def test_layer_lists_that_are_refused():
+    import synth
+    L, K = synth.Layer, synth.KIND
+    tail = [L(1, K["GAP"], 8, 8, 0, 1, 0, 0, 0, -1), L(1, K["FC"], 8, 3, 1, 1, 0, 0, 1, -1), L(1, K["SOFTMAX_CE"], 3, 3, 0, 1, 0, 0, 0, -1)]
+    cfg = synth.config(2, 8, 1, 6, 3)
+    lin = L(0, K["LINEAR"], 8, 8, 0, 1, 0, 3, 1, -1)
+    F.ftp_workspace_bytes([lin] + tail, cfg)
+    F.ftp_workspace_bytes([lin, lin._replace(act=0, residual_src=0)] + tail, cfg)
+    F.ftp_workspace_bytes([lin, L(0, K["GATED"], 8, 8, 8, 1, 0, 4, 0, -1)] + tail, cfg)
+    bad = [[lin._replace(cin=7)], [lin._replace(k=4)], [lin._replace(stride=2)], [lin._replace(pad=1)], [lin._replace(act=5)], [lin._replace(cout=0)],
+           [lin, lin._replace(residual_src=1)], [lin, lin._replace(cout=8, residual_src=5)], [lin, lin._replace(kind=K["GATED"], has_bias=1)],
+           [lin, lin._replace(kind=K["GATED"], has_bias=0, residual_src=0)],
+           [lin._replace(cout=16), L(0, K["LINEAR"], 16, 8, 0, 1, 0, 0, 0, 0)],                       # residual of another width
+           [L(0, K["ACT"], 8, 8, 0, 1, 0, 4, 0, -1)],                                                  # SILU is for the new kinds only
+           [L(0, 12, 8, 8, 0, 1, 0, 0, 0, -1)]]
+    for ls in bad:
+        with pytest.raises(F.FtpError):
+            F.ftp_workspace_bytes(ls + tail, cfg)
+            pytest.fail(str(ls))

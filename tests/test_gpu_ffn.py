@@ -549,6 +549,7 @@ def test_a_word_left_by_a_timed_out_wait_is_reported_once():
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         g.capture_begin()
+        torch.zeros(1, device="cuda")
         with pytest.raises(F.FtpError) as e:
             F.ftp_check_op_status()
         g.capture_end()
