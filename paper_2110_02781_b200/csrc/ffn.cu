@@ -630,7 +630,7 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     p.e[0].vec_bias = bias && aligned(bias, 16);
     set_out<T>(p.e[0], y, ldy, residual, d->ldr ? d->ldr : d->cout);
     set_stash<T>(p.e[0], stash_kind, stash, d->rows, d->cout, GATED ? 2 : 1);
-    if (!given_x && few_tokens(d->rows, d->cin, sizeof(T) == 4, GATED ? 2 : 1)) {
+    if (!given_x && few_tokens(d->rows, d->cin, d->cout, sizeof(T) == 4, GATED ? 2 : 1)) {
         if (ws.dry()) return FTP_OK;
         if (!err) err = status_word();
         FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);

@@ -78,7 +78,7 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who);
 
 // Products of a few tokens, read from the tensors as they are (ffn_few.cu).
 constexpr int FEW_SMEM = 96 * 1024;          // of it for the tokens
-bool few_tokens(long long rows, long long cin, bool f32, int products);
+bool few_tokens(long long rows, long long cin, long long cout, bool f32, int products);
 ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, int* err,
                    cudaStream_t st, const char* who);
 

@@ -223,17 +223,19 @@ __device__ __forceinline__ void finish_few(const FewArgs& p, const Part& t, floa
 }
 
 // MR: tokens (rounded up); P: products (2: gated).
-// Rows of w and of x on 16 bytes: one thread streams boxes of 64 rows x 128 bytes of w, and the tokens' values for those rows,
-// with TMA into a ring in shared memory; eight warps multiply, eight rows of a box each.  The ring keeps 96 KB per CTA, two
+// Rows of w and of x on 16 bytes: one thread streams boxes of 128 rows x 128 bytes of w (gated: 64 of either), and the tokens'
+// values for those rows, with TMA into a ring in shared memory; eight warps multiply, an eighth of the rows each.  The ring keeps 96 KB per CTA, two
 // CTAs an SM, on their way from memory all the time, which loads into registers do not (4.0 TB/s of 6.5 with eight in flight
 // per thread).
-constexpr int RING_ROWS = 64, RING_BYTES = 96 * 1024, RING_THREADS = FEW_THREADS + 32;
+constexpr int RING_BYTES = 96 * 1024, RING_THREADS = FEW_THREADS + 32;
+template <int P> constexpr int RING_ROWS = 128 / P;                  // rows of a box: 16 KB of weights a stage (8 KB: 25 us instead of 20 for 4096 x 12288)
 template <typename T, int MR, int P>
 __global__ void __launch_bounds__(RING_THREADS, MR * P * Wide<T>::V <= 32 ? 2 : 1)
 ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_constant__ CUtensorMap map1, const __grid_constant__ CUtensorMap mapx,
                     const __grid_constant__ FewArgs p) {
     constexpr int V = Wide<T>::V, CW = 8 * V;
-    constexpr uint32_t BOX = RING_ROWS * 128, XBOX = MR * RING_ROWS * sizeof(T), STAGE = P * BOX + (XBOX + 127) / 128 * 128;
+    constexpr int ROWS = RING_ROWS<P>, STEPS = ROWS / 32;            // a warp takes ROWS / 8 rows, four a step
+    constexpr uint32_t BOX = ROWS * 128, XBOX = MR * ROWS * sizeof(T), STAGE = P * BOX + (XBOX + 127) / 128 * 128;
     constexpr int STAGES = RING_BYTES / STAGE;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));   // at the end [FEW_WARPS][P][MR][CW]
@@ -242,7 +244,7 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Part t = my_part<CW, MR>(p);
-    const int boxes = (t.klen + RING_ROWS - 1) / RING_ROWS;
+    const int boxes = (t.klen + ROWS - 1) / ROWS;
     const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[STAGES]);
     if (threadIdx.x == 0) {
         tma_prefetch_map(&map0); tma_prefetch_map(&mapx);
@@ -254,8 +256,8 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
     // The first boxes of w on their way into L2 while the kernel before this one still runs (a hint: nothing is read yet)
     if (warp == FEW_WARPS && elect_one())
         for (int b = 0; b < min(boxes, STAGES); ++b) {
-            prefetch_2d(&map0, t.n0, t.k0 + b * RING_ROWS);
-            if (P == 2) prefetch_2d(&map1, t.n0, t.k0 + b * RING_ROWS);
+            prefetch_2d(&map0, t.n0, t.k0 + b * ROWS);
+            if (P == 2) prefetch_2d(&map1, t.n0, t.k0 + b * ROWS);
         }
     __syncthreads();
     grid_dep_sync();
@@ -276,7 +278,7 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
             if (!ok) break;
             if (elect_one()) {
                 const uint32_t dst = smem_u32(ring) + (uint32_t)sl.s * STAGE, bar = full0 + 8 * sl.s;
-                const int k = t.k0 + b * RING_ROWS;
+                const int k = t.k0 + b * ROWS;
                 mbar_expect_tx(bar, P * BOX + XBOX);
                 tma_load_2d(dst, &map0, t.n0, k, bar);
                 if (P == 2) tma_load_2d(dst + BOX, &map1, t.n0, k, bar);
@@ -291,16 +293,16 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
             if (!ok) break;
             // rows behind the end of the reduction are zeros in w and in x; shares are whole boxes
             const uint8_t* stage = ring + (uint32_t)sl.s * STAGE;
-            const int row = warp * 8 + (lane >> 3);
+            const int row = warp * (ROWS / 8) + (lane >> 3);
             const T* xk = reinterpret_cast<const T*>(stage + P * BOX) + row;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < STEPS; ++u) {
                 float f[P][V];
 #pragma unroll
                 for (int q = 0; q < P; ++q) unpack<T>(*reinterpret_cast<const uint4*>(stage + q * BOX + (row + 4 * u) * 128 + (lane & 7) * 16), f[q]);
 #pragma unroll
                 for (int m = 0; m < MR; ++m) {
-                    const float xv = to_f(xk[m * RING_ROWS + 4 * u]);
+                    const float xv = to_f(xk[m * ROWS + 4 * u]);
 #pragma unroll
                     for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -408,8 +410,8 @@ ftp_status launch_few(const FewArgs& a, int S, cudaStream_t st, const char* who)
         constexpr int V = 16 / (int)sizeof(T), B = 128 / (int)sizeof(T);
         CUtensorMap m0, m1, mx;
         const long long ldx = a.rows == 1 ? (a.K + V - 1) / V * V : a.ldx;       // one row: never stepped over
-        FTP_REQUIRE(make_ring_map<T>(&m0, a.w[0], a.N, a.K, a.ldw, B, RING_ROWS) && (P == 1 || make_ring_map<T>(&m1, a.w[1], a.N, a.K, a.ldw, B, RING_ROWS)) &&
-                        make_ring_map<T>(&mx, a.x, a.K, a.rows, ldx, RING_ROWS, MR), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
+        FTP_REQUIRE(make_ring_map<T>(&m0, a.w[0], a.N, a.K, a.ldw, B, RING_ROWS<P>) && (P == 1 || make_ring_map<T>(&m1, a.w[1], a.N, a.K, a.ldw, B, RING_ROWS<P>)) &&
+                        make_ring_map<T>(&mx, a.x, a.K, a.rows, ldx, RING_ROWS<P>, MR), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
         if (P == 1) m1 = m0;
         static_assert(FEW_WARPS * P * MR * CW * 4 <= RING_BYTES / 2, "the warps' sums reuse the ring");
         auto kern = ffn_few_ring_kernel<T, MR, P>;
@@ -441,16 +443,18 @@ ftp_status few_rows(const FewArgs& a, int S, cudaStream_t st, const char* who) {
 // bytes of shared memory that the tokens of a group take beside `k` rows of w
 long long few_smem(long long rows, long long k, bool f32, int products) {
     const int group = rows <= 2 ? (int)rows : rows <= 4 || !f32 ? 4 : rows <= 8 || products == 2 ? 8 : 16;
-    return (k + RING_ROWS) * (group <= 4 ? group : group + 4) * 4;
+    return (k + 2 * FEW_STEP) * (group <= 4 ? group : group + 4) * 4;
 }
 
 }  // namespace
 
-// The tokens of a CTA's share of the reduction (an eighth at least) have to fit into its shared memory.  bf16: the sums of
-// four tokens (gated: two) fit into the registers of two CTAs an SM, beyond that the tensor cores are faster.  float: up to
-// 32 (gated: 16), since the tensor cores would first need the planes of w, five times its bytes.
-bool few_tokens(long long rows, long long cin, bool f32, int products) {
-    return rows <= (f32 ? (products == 2 ? 16 : 32) : (products == 2 ? 2 : 4)) && few_smem(rows, (cin + 7) / 8, f32, products) <= FEW_SMEM;
+// The tokens of a CTA's share of the reduction (an eighth at least) have to fit into its shared memory.  bf16: two tokens, or
+// four of a small linear op; beyond that the tensor cores are faster (four tokens, 4096 x 12288: 28.0 against 21.2 us).
+// float: up to 32 tokens (gated: 16), since the tensor cores would first need the planes of w, five times its bytes (16
+// tokens, 4096 x 4096: 30 against 55 us).
+bool few_tokens(long long rows, long long cin, long long cout, bool f32, int products) {
+    const long long most = f32 ? (products == 2 ? 16 : 32) : (products == 1 && cin * cout <= 2 << 20 ? 4 : 2);
+    return rows <= most && few_smem(rows, (cin + 7) / 8, f32, products) <= FEW_SMEM;
 }
 
 ftp_status run_few(const void* x, long long ldx, const void* const* w, long long ldw, int products, int rows, int K, int N, bool f32, const Epi& e, int* err,
@@ -472,10 +476,11 @@ ftp_status run_few(const void* x, long long ldx, const void* const* w, long long
     const long long strips = (N + (f32 ? 32 : 64) - 1) / (f32 ? 32 : 64), groups = rows <= 4 ? 1 : rows <= 8 || products == 2 ? (rows + 7) / 8 : (rows + 15) / 16;
     const int room = !a.ring ? 4 : (f32 && rows * products > 8 ? 1 : 2);
     int S = (int)std::max<long long>(1, std::min<long long>(8, room * SMS / (strips * groups)));
-    while (S > 1 && K / S < 2 * RING_ROWS) --S;
+    const int box = a.ring ? 128 / products : FEW_STEP * 2;
+    while (S > 1 && K / S < 128) --S;
     if (!a.ring)
         while (S < 8 && few_smem(rows, (K + S - 1) / S, f32, products) > FEW_SMEM) ++S;
-    a.kper = ((K + S - 1) / S + RING_ROWS - 1) / RING_ROWS * RING_ROWS;
+    a.kper = ((K + S - 1) / S + box - 1) / box * box;
     if (f32) return products == 2 ? few_rows<float, 2>(a, S, st, who) : few_rows<float, 1>(a, S, st, who);
     return products == 2 ? few_rows<__nv_bfloat16, 2>(a, S, st, who) : few_rows<__nv_bfloat16, 1>(a, S, st, who);
 }

@@ -88,12 +88,15 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
         const uint32_t ring = smem_u32(smem);
         const int me = producer_of(warp), z = p.np == 1 ? 0 : p.np - 1 - me, step = p.np == 1 ? PRODUCERS : 1;
         const uint32_t bytes = (z < p.pa ? A_BYTES : 0) + (z < p.pb ? B_BYTES : 0);
-        bool ok = true;
+        bool ok = true, peek = false;
         sl.ahead(me);
         for (int kb = kb0 + (p.np == 1 ? me : 0); kb < kb1; kb += step, sl.ahead(PRODUCERS)) {
             const int part = kb >= p.kb_part, k = (kb - (part ? p.kb_part : 0)) * BK;
-            ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                          // at once for a slot never used
+            ok = warp_ready(peek, empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                       // at once for a slot never used
             if (!ok) break;
+            Slot<STAGES> then = sl;
+            then.ahead(PRODUCERS);
+            peek = mbar_peek(empty0 + 8 * then.s, then.parity ^ 1);  // of this warp's next slot, see mma_warp
             if (elect_one()) {
                 const CUtensorMap* ma = part ? &mapA1 : &mapA0;
                 const CUtensorMap* mb = (part || out) ? &mapB1 : &mapB0;
@@ -232,33 +235,50 @@ ftp_status tile_typed(const Product& p, KArgs& k, int S, cudaStream_t st, const 
 }  // namespace
 
 // What a form of a product takes, in microseconds, up to what all forms share.  From launches timed one form at a time
-// (64..4096 tokens, 512..4096 channels, all three products, both types): c = a 64-wide block of one tile, base = launch,
-// first loads and last epilogue, epi = a tile's epilogue where the reduction is too short to hide it, share(S) = the cluster
-// and its exchange.  A wave is 74 pairs or 148 CTAs; clusters of four and eight do not fill every group of SMs.
+// (5..4096 tokens, 512..12288 channels, all three products, both types): c = a 64-wide block of one tile (c2 with two CTAs
+// on an SM), base = launch, first loads and last epilogue, epi = a tile's epilogue where nothing hides it, share(S) = the
+// cluster and its exchange, and what reading the operands from memory takes at the rate the form reaches.  A wave is 74
+// pairs, 148 CTAs or twice that; clusters of four and eight do not fill every group of SMs.
 struct Form { bool pair; int cols, S; double cost; };
 static Form choose_form(const KArgs& k, const Product& p) {
     const bool f32 = p.out_f32 && k.np > 1;
     const int gated = p.epi == EPI_GATED ? 2 : 1;
     const double blocks = (double)k.kb_part * k.parts_k;
+    const double mbytes = 2e-6 * blocks * 64 * ((double)p.M * k.pa + (double)p.N * gated * k.parts_n * k.pb);
     auto tiles = [&](int rows, int cols) { return (double)((p.M + rows - 1) / rows) * ((p.N + cols / gated - 1) / (cols / gated)) * k.parts_n; };
     Form best{true, 256, 1, 1e30};
     auto take = [&](const Form& f) { if (f.cost < best.cost) best = f; };
-    auto pair = [&](int cols, double c, double base, double epi) { take({true, cols, 1, base + std::ceil(tiles(256, cols) / 74) * std::max(c * blocks, epi)}); };
-    if (f32 || p.out_f32) pair(128, f32 ? 0.97 : 0.2, 5.4, 3.0);
+    auto pair = [&](int cols, double c, double base, double epi) {
+        take({true, cols, 1, base + std::max(std::ceil(tiles(256, cols) / 74) * std::max(c * blocks, epi), mbytes / 4.0)});
+    };
+    if (f32 || p.out_f32) pair(128, f32 ? 0.82 : 0.2, 5.4, 3.0);
     else {
         pair(256, 0.29, 7.1, 4.0);
-        pair(128, 0.166, 5.4, 2.9);
+        pair(128, 0.15, 5.6, 2.9);
     }
     static constexpr double share[9] = {0, 0, 1.5, 2.1, 2.7, 3.1, 3.4, 3.8, 4.2};
-    auto tile = [&](int cols, double c, double base, double epi) {
+    auto tile = [&](int cols, double c, double c2, double base, double epi) {
         for (int S = 1; S <= 8 && S <= blocks; ++S) {
-            const double room = S <= 2 ? 148 : S <= 4 ? 132 : 104;
-            const double waves = std::ceil(tiles(128, cols) * S / room);
-            take({false, cols, S, base + share[S] + waves * c * std::ceil(blocks / S) + (waves - 1) * epi});
+            const double room = S <= 2 ? 148 : S <= 4 ? 132 : 104, n = tiles(128, cols) * S, len = std::ceil(blocks / S);
+            double t;
+            if (n <= room) t = c * len;
+            else {
+                const double waves = std::ceil(n / (c2 > 0 ? 2 * room : room));
+                t = waves * (c2 > 0 ? c2 : c) * len + (waves - 1) * epi;
+            }
+            take({false, cols, S, base + share[S] + std::max(t, mbytes / 5.2)});
         }
     };
-    tile(128, f32 ? 1.3 : 0.353, 3.6, 3.0);
-    if (gated == 1) tile(64, f32 ? 1.05 : 0.275, 3.1, 2.8);
+    if (f32) {
+        tile(128, 1.3, 0, 3.6, 3.0);
+        if (gated == 1) tile(64, 1.0, 0, 3.1, 2.8);
+    } else if (p.out_f32) {
+        tile(128, 0.4, 0, 3.6, 3.0);
+        if (gated == 1) tile(64, 0.3, 0, 3.1, 2.8);
+    } else {
+        tile(128, 0.325, 0.6, 4.2, 6.0);
+        if (gated == 1) tile(64, 0.253, 0.36, 3.8, 4.7);
+    }
     return best;
 }
 

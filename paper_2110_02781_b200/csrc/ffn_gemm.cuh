@@ -158,6 +158,16 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* err
 __device__ __forceinline__ bool warp_wait_for(uint32_t bar, uint32_t parity, int* err, int code) {
     return __all_sync(0xffffffffu, wait_for(bar, parity, err, code));
 }
+// a test that does not suspend the thread
+__device__ __forceinline__ bool mbar_peek(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// the same for a barrier that was tested before
+__device__ __forceinline__ bool warp_ready(bool seen, uint32_t bar, uint32_t parity, int* err, int code) {
+    return __all_sync(0xffffffffu, seen) || warp_wait_for(bar, parity, err, code);
+}
 // one thread of a converged warp
 __device__ __forceinline__ bool elect_one() {
     uint32_t ok;
@@ -208,7 +218,7 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
     // adding those costs the sum no accuracy
     constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN;
     int chunk = 0;
-    bool first = true, first_small = true;
+    bool first = true, first_small = true, peek0 = false, peek1 = false;
     uint32_t d0 = tmem;
     auto four = [&](uint32_t d, bool& first, int sa, int sb) {       // a block of the planes in slots sa and sb; one thread
         const uint64_t ad = a0 + (uint64_t)((uint32_t)sa * (STAGE_BYTES >> 4)), bd = b0 + (uint64_t)((uint32_t)sb * (STAGE_BYTES >> 4));
@@ -233,17 +243,25 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
                 left = CHUNKED ? min(p.chunk, blocks - kb) : blocks;
             }
             --left;
+            // The barriers of the slots to come are tested before this block's MMAs are issued (a test of a barrier that is
+            // complete still takes over a hundred cycles), so that the wait for them usually costs a vote.
             if (!CHUNKED || p.np == 1) {
                 const int s0 = sl.s;
-                if (!warp_wait_for(full0 + 8 * s0, sl.parity, p.err, 2)) return false;
+                if (!warp_ready(peek0, full0 + 8 * s0, sl.parity, p.err, 2)) return false;
                 sl.next();
                 const bool two = STAGES >= 6 && left > 0;            // two blocks a trip where the ring is long
                 const int s1 = sl.s;
                 if (two) {
-                    if (!warp_wait_for(full0 + 8 * s1, sl.parity, p.err, 2)) return false;
+                    if (!warp_ready(peek1, full0 + 8 * s1, sl.parity, p.err, 2)) return false;
                     sl.next();
                     --left;
                     ++kb;
+                }
+                peek0 = mbar_peek(full0 + 8 * sl.s, sl.parity);
+                if (STAGES >= 6) {
+                    Slot<STAGES> then = sl;
+                    then.next();
+                    peek1 = mbar_peek(full0 + 8 * then.s, then.parity);
                 }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (elect_one()) {

@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
         const int me = producer_of(warp), z = p.np == 1 ? 0 : p.np - 1 - me, step = p.np == 1 ? PRODUCERS : 1;
         const uint32_t bytes = (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0);
         int kb = p.np == 1 ? me : 0;                                 // runs on over the tiles: slots are numbered through
+        bool peek = false;
         sl.ahead(me);
         for (int t = cluster; t < tiles && ok; t += clusters, kb -= all_kb) {
             int tm, tn;
@@ -286,8 +287,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
             const int m0 = tm * 256 + (int)rank * 128, n0 = (tn - out * p.tiles_n) * OUTC + (EPI == EPI_GATED ? 0 : (int)rank * (BN / 2));
             for (; kb < all_kb; kb += step, sl.ahead(PRODUCERS)) {
                 const int part = kb >= p.kb_part, k = (kb - (part ? p.kb_part : 0)) * BK;
-                ok = warp_wait_for(empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                      // at once for a slot never used
+                ok = warp_ready(peek, empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                       // at once for a slot never used
                 if (!ok) break;
+                Slot<STAGES> then = sl;
+                then.ahead(PRODUCERS);
+                peek = mbar_peek(empty0 + 8 * then.s, then.parity ^ 1);  // of this warp's next slot, see mma_warp
                 if (elect_one()) {
                     const CUtensorMap* ma = part ? &mapA1 : &mapA0;
                     const CUtensorMap* mb = (EPI == EPI_GATED ? rank != 0 : (part || out)) ? &mapB1 : &mapB0;
