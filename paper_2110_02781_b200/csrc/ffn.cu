@@ -152,24 +152,25 @@ __device__ __forceinline__ void values16(const Raw16<bf16>& r, float (&v)[16]) {
     }
 }
 
-// A thread holds 16 columns, two neighbouring threads a block of 32; PACK_U such pieces in flight.  Bound by instructions
-// as much as by memory (8 columns, integer conversions and a piece at a time: 55 us for 16384 x 4096 bf16).
+// A thread holds 16 columns, two neighbouring threads a block of 32; U such pieces in flight: PACK_U, or one where that
+// many would leave multiprocessors without a block.  Bound by instructions as much as by memory (8 columns, integer
+// conversions and a piece at a time: 55 us for 16384 x 4096 bf16).
 constexpr int PACK_U = 4;
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, bool vec, const Image im) {
     grid_dep_sync();                                                 // g: groups of 16 columns here
-    for (unsigned b0 = blockIdx.x * 256 * PACK_U; b0 < g.total; b0 += gridDim.x * 256 * PACK_U) {
-        Raw16<T> raw[PACK_U];
-        unsigned row[PACK_U], col[PACK_U];
+    for (unsigned b0 = blockIdx.x * 256 * U; b0 < g.total; b0 += gridDim.x * 256 * U) {
+        Raw16<T> raw[U];
+        unsigned row[U], col[U];
 #pragma unroll
-        for (int u = 0; u < PACK_U; ++u) {
+        for (int u = 0; u < U; ++u) {
             const unsigned i = min(b0 + threadIdx.x + u * 256, g.total - 1);       // whole warps take part in the exchange below
             row[u] = i / g.per_row;
             col[u] = (i - row[u] * g.per_row) * 16;
             raw[u] = fetch16<T>(x + (long long)row[u] * ld + col[u], max(0, cols - (int)col[u]), vec);
         }
 #pragma unroll
-        for (int u = 0; u < PACK_U; ++u) {
+        for (int u = 0; u < U; ++u) {
             unsigned top = top16(raw[u]);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             const unsigned e = img_exp(top);
@@ -228,15 +229,14 @@ __device__ __forceinline__ void store16(bf16* p, int valid, bool vec, const floa
     for (int i = 0; i < 16; ++i) if (i < valid) p[i] = __float2bfloat16(v[i]);
 }
 
-// out: `ld` elements between rows; g: groups of 16 columns
-template <typename T>
-__global__ void __launch_bounds__(256) unpack_kernel(const Image im, const Groups g, int cols, T* __restrict__ out, long long ld, bool vec) {
-    grid_dep_sync();
-    for (unsigned b0 = blockIdx.x * 256 * PACK_U; b0 < g.total; b0 += gridDim.x * 256 * PACK_U) {
-        uint4 q[PACK_U];
-        unsigned e[PACK_U], row[PACK_U], col[PACK_U];
+// out: `ld` elements between rows; g: groups of 16 columns; block `block` of `blocks`
+template <typename T, int U>
+__device__ __forceinline__ void unpack_blocks(const Image& im, const Groups& g, int cols, T* __restrict__ out, long long ld, bool vec, unsigned block, unsigned blocks) {
+    for (unsigned b0 = block * 256 * U; b0 < g.total; b0 += blocks * 256 * U) {
+        uint4 q[U];
+        unsigned e[U], row[U], col[U];
 #pragma unroll
-        for (int u = 0; u < PACK_U; ++u) {
+        for (int u = 0; u < U; ++u) {
             const unsigned i = min(b0 + threadIdx.x + u * 256, g.total - 1);
             row[u] = i / g.per_row;
             col[u] = (i - row[u] * g.per_row) * 16;
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(256) unpack_kernel(const Image im, const Group
             e[u] = im.e[row[u] * (im.pitch / IMG_BLOCK) + col[u] / IMG_BLOCK];
         }
 #pragma unroll
-        for (int u = 0; u < PACK_U; ++u) {
+        for (int u = 0; u < U; ++u) {
             if (b0 + threadIdx.x + u * 256 >= g.total) break;
             const float s = img_scale(e[u]);
             const unsigned w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
@@ -259,6 +259,11 @@ __global__ void __launch_bounds__(256) unpack_kernel(const Image im, const Group
             store16(out + (long long)row[u] * ld + col[u], cols - (int)col[u], vec, v);
         }
     }
+}
+template <typename T, int U>
+__global__ void __launch_bounds__(256) unpack_kernel(const Image im, const Groups g, int cols, T* __restrict__ out, long long ld, bool vec) {
+    grid_dep_sync();
+    unpack_blocks<T, U>(im, g, cols, out, ld, vec, blockIdx.x, gridDim.x);
 }
 
 // launch(first row, Groups, blocks) for pieces of at most 2^30 groups
@@ -280,15 +285,25 @@ void launch_planes(const T* x, long long rows, long long cols, long long ld, bf1
     });
 }
 inline Image image_from(const Image& im, long long r) { return Image{im.q + r * im.pitch, im.e + r * (im.pitch / IMG_BLOCK), im.pitch}; }
+// one piece per thread where four leave multiprocessors idle
+inline bool few_pieces(const Groups& g) { return g.total <= SMS * 256 * PACK_U; }
 template <typename T>
 void launch_pack(const T* x, long long rows, long long cols, long long ld, const Image& im, cudaStream_t st) {
     const bool vec = aligned(x, 16) && ld * (long long)sizeof(T) % 16 == 0;
-    by_rows(rows, im.pitch / 16, [&](long long r, Groups g, dim3 blocks) { launch(pack_kernel<T>, blocks, dim3(256), 0, st, x + r * ld, g, (int)cols, ld, vec, image_from(im, r)); });
+    by_rows(rows, im.pitch / 16, [&](long long r, Groups g, dim3 blocks) {
+        const T* from = x + r * ld;
+        if (few_pieces(g)) launch(pack_kernel<T, 1>, dim3((g.total + 255) / 256), dim3(256), 0, st, from, g, (int)cols, ld, vec, image_from(im, r));
+        else launch(pack_kernel<T, PACK_U>, blocks, dim3(256), 0, st, from, g, (int)cols, ld, vec, image_from(im, r));
+    });
 }
 template <typename T>
 void launch_unpack(const Image& im, long long rows, long long cols, T* out, long long ld, cudaStream_t st) {
     const bool vec = aligned(out, 16) && ld * (long long)sizeof(T) % 16 == 0;
-    by_rows(rows, (cols + 15) / 16, [&](long long r, Groups g, dim3 blocks) { launch(unpack_kernel<T>, blocks, dim3(256), 0, st, image_from(im, r), g, (int)cols, out + r * ld, ld, vec); });
+    by_rows(rows, (cols + 15) / 16, [&](long long r, Groups g, dim3 blocks) {
+        T* to = out + r * ld;
+        if (few_pieces(g)) launch(unpack_kernel<T, 1>, dim3((g.total + 255) / 256), dim3(256), 0, st, image_from(im, r), g, (int)cols, to, ld, vec);
+        else launch(unpack_kernel<T, PACK_U>, blocks, dim3(256), 0, st, image_from(im, r), g, (int)cols, to, ld, vec);
+    });
 }
 
 // ---- operands of the products, made in one launch ----
@@ -296,10 +311,11 @@ void launch_unpack(const Image& im, long long rows, long long cols, T* out, long
 // their own in one kernel, or behind the blocks of the gradient kernel: a small call costs its launches.
 enum { JOB_PLANES = 0, JOB_IMAGE = 1 };
 struct Job {
-    const void* src; long long ld; int vec;  // JOB_PLANES
+    const void* src; int vec;                // JOB_PLANES
     Image im;                                // JOB_IMAGE
+    long long ld;                            // elements between rows of src (JOB_IMAGE: of out)
     bf16* out; long long plane; int planes, cols, kind;
-    Groups g;                                // groups of eight columns
+    Groups g;                                // groups of eight columns (JOB_IMAGE: sixteen)
     unsigned blocks;
 };
 struct Jobs { Job job[3]; int n; unsigned blocks; };
@@ -309,16 +325,14 @@ __device__ __forceinline__ void run_jobs(const Jobs& all, unsigned block) {
     int j = 0;
     while (block >= all.job[j].blocks) block -= all.job[j++].blocks;
     const Job& p = all.job[j];
+    if (p.kind == JOB_IMAGE) { unpack_blocks<bf16, PACK_U>(p.im, p.g, p.cols, p.out, p.ld, true, block, p.blocks); return; }
     const long long pitch = 8ll * p.g.per_row;
     for (unsigned i0 = block * 256 * EIGHT_U + threadIdx.x; i0 < p.g.total; i0 += p.blocks * 256 * EIGHT_U) {
         float v[EIGHT_U][8];
 #pragma unroll
         for (int u = 0; u < EIGHT_U; ++u)
             if (i0 + u * 256 < p.g.total)
-                group_at(p.g, i0 + u * 256, [&](long long r, int c) {
-                    if (p.kind == JOB_PLANES) load8(static_cast<const T*>(p.src) + r * p.ld + c, p.cols - c, p.vec, v[u]);
-                    else img_values8(img_fetch8(p.im, r, c), v[u]);
-                });
+                group_at(p.g, i0 + u * 256, [&](long long r, int c) { load8(static_cast<const T*>(p.src) + r * p.ld + c, p.cols - c, p.vec, v[u]); });
 #pragma unroll
         for (int u = 0; u < EIGHT_U; ++u)
             if (i0 + u * 256 < p.g.total) group_at(p.g, i0 + u * 256, [&](long long r, int c) { store_planes(p.out + r * pitch + c, p.plane, p.planes, v[u]); });
@@ -331,7 +345,8 @@ __global__ void __launch_bounds__(256) jobs_kernel(const __grid_constant__ Jobs 
 }
 // false: too large for 32-bit group numbers
 inline bool add_job(Jobs& all, Job j, long long rows, long long cols) {
-    const long long per_row = (cols + 7) / 8, total = rows * per_row;
+    const int width = j.kind == JOB_IMAGE ? 16 : 8;
+    const long long per_row = (cols + width - 1) / width, total = rows * per_row;
     if (total > 1 << 30 || all.n == 3) return false;
     j.cols = (int)cols;
     j.g = Groups{(unsigned)total, (unsigned)per_row};
@@ -562,7 +577,7 @@ ftp_status image_operand(Operand* o, const void* image, long long rows, long lon
     Job j{};
     j.kind = JOB_IMAGE;
     j.im = image_at(const_cast<void*>(image), rows, cols, 0);
-    j.out = p; j.plane = rows * pitch; j.planes = 1;
+    j.out = p; j.ld = pitch; j.planes = 1;
     if (!add_job(jobs, j, rows, cols)) launch_unpack(j.im, rows, cols, p, pitch, st);
     return FTP_OK;
 }

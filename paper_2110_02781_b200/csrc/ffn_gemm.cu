@@ -5,10 +5,10 @@
 // float tensor comes as three bf16 planes (8 mantissa bits each, 24 together) and a product of two of them as the six
 // plane products that matter; the dropped ones are below 2^-24 of the result.
 //
-// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warps 0, 2 and 3 (one thread each) stream operand tiles with
-// TMA into a ring in shared memory, warp 1 (one thread) issues the MMAs, warps 4-7 move the accumulator to shared memory.
+// tile kernel: one CTA per 128 x BN tile and slice of the reduction.  Warps 0, 2 and 3 (one elected thread each) stream operand tiles
+// with TMA into a ring in shared memory, warp 1 issues the MMAs, warps 4-7 move the accumulator to shared memory.
 // The slices of one tile form a cluster: each CTA then adds up the rows rank, rank + S, ... of the tile over the
-// cluster's shared memory, always in rank order, and finishes them (bias, activation, residual, kept values), so a
+// cluster's shared memory, in an order that depends on the row alone, and finishes them (bias, activation, residual, kept values), so a
 // product with few tiles still uses the whole GPU, needs no workspace, and gives the same bits every time.
 //
 // Every wait is bounded; see gemm_tc.cu for the error protocol.
@@ -179,30 +179,10 @@ __global__ void __launch_bounds__(TILE_THREADS, DEEP ? 1 : 2) ffn_tile_kernel(co
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     if (S > 1) cluster_sync_all();
 
-    // ---- rows rank, rank + S, ... of the tile, added over the slices in rank order ----
+    // ---- rows rank, rank + S, ... of the tile, added over the slices ----
     bool ok = true;
     for (uint32_t k = 0; k < S; ++k) ok = ok && (S > 1 ? ld_cluster1(map_rank(smem_u32(&failed), k)) : failed) == 0;
-    if (ok) {
-        constexpr int LPR = OUTC / 4, RPW = 32 / LPR;                // lanes per row, rows per warp
-        const int rows = (int)min(128ll, p.M - m0), c = (lane % LPR) * 4;
-        const uint32_t base = smem_u32(smem);
-        for (int i = warp * RPW; i * (int)S + (int)rank < rows; i += (TILE_THREADS / 32) * RPW) {
-            const int r = (i + lane / LPR) * (int)S + (int)rank;
-            const bool row_ok = r < rows;
-            const uint32_t at = base + (uint32_t)((row_ok ? r : 0) * PITCH + c) * 4;
-            float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-            for (uint32_t k = 0; k < S; ++k) {
-                const uint32_t from = S > 1 ? map_rank(at, k) : at;
-                const float4 u = ld_cluster4(from);
-                a[0] += u.x; a[1] += u.y; a[2] += u.z; a[3] += u.w;
-                if (EPI == EPI_GATED) {
-                    const float4 w = ld_cluster4(from + OUTC * 4);
-                    b[0] += w.x; b[1] += w.y; b[2] += w.z; b[3] += w.w;
-                }
-            }
-            finish4<T, EPI>(p.e[out], m0 + r, n0 + c, p.N, row_ok, a, b);
-        }
-    }
+    if (ok) finish_rows<T, EPI, BN, PITCH>(p.e[out], smem_u32(smem), S, rank, 0, 1, m0, n0, p.M, p.N);
     if (S > 1) cluster_sync_all();                                   // nobody leaves while another CTA reads its shared memory
 }
 
@@ -248,15 +228,21 @@ static Form choose_form(const KArgs& k, const Product& p) {
     auto tiles = [&](int rows, int cols) { return (double)((p.M + rows - 1) / rows) * ((p.N + cols / gated - 1) / (cols / gated)) * k.parts_n; };
     Form best{true, 256, 1, 1e30};
     auto take = [&](const Form& f) { if (f.cost < best.cost) best = f; };
+    // results whose rows cannot be stored four elements at a time
+    const double ragged = k.e[0].vec_y ? 0 : 5.0;
+    static constexpr double share[9] = {0, 0, 1.5, 2.1, 2.7, 3.1, 3.4, 3.8, 4.2}, pair_share[5] = {0, 0, 2.1, 2.4, 2.8};
     auto pair = [&](int cols, double c, double base, double epi) {
-        take({true, cols, 1, base + std::max(std::ceil(tiles(256, cols) / 74) * std::max(c * blocks, epi), mbytes / 4.0)});
+        const double t = c * blocks, n = tiles(256, cols), waves = std::ceil(n / 74);
+        take({true, cols, 1, base + ragged + std::max(t + (waves - 1) * std::max(t, epi), mbytes / std::min(4.0, 0.085 * n))});
+        for (int S = 2; cols == 128 && S <= 4 && S <= blocks; ++S)   // one tile per cluster of four, six or eight CTAs
+            if (tiles(256, cols) * S <= (S == 2 ? 66 : S == 3 ? 60 : 52))
+                take({true, cols, S, base + pair_share[S] + ragged / S + std::max(c * std::ceil(blocks / S), mbytes / 5.2)});
     };
     if (f32 || p.out_f32) pair(128, f32 ? 0.82 : 0.2, 5.4, 3.0);
     else {
         pair(256, 0.29, 7.1, 4.0);
         pair(128, 0.15, 5.6, 2.9);
     }
-    static constexpr double share[9] = {0, 0, 1.5, 2.1, 2.7, 3.1, 3.4, 3.8, 4.2};
     auto tile = [&](int cols, double c, double c2, double base, double epi) {
         for (int S = 1; S <= 8 && S <= blocks; ++S) {
             const double room = S <= 2 ? 148 : S <= 4 ? 132 : 104, n = tiles(128, cols) * S, len = std::ceil(blocks / S);
@@ -266,7 +252,7 @@ static Form choose_form(const KArgs& k, const Product& p) {
                 const double waves = std::ceil(n / (c2 > 0 ? 2 * room : room));
                 t = waves * (c2 > 0 ? c2 : c) * len + (waves - 1) * epi;
             }
-            take({false, cols, S, base + share[S] + std::max(t, mbytes / 5.2)});
+            take({false, cols, S, base + share[S] + ragged / S + std::max(t, mbytes / 5.2)});
         }
     };
     if (f32) {
@@ -293,7 +279,7 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who) {
     k.parts_k = (p.parts > 1 && p.cat_k) ? 2 : 1;
     k.parts_n = (p.parts > 1 && !p.cat_k && p.epi != EPI_GATED) ? 2 : 1;
     const Form f = choose_form(k, p);
-    if (f.pair) return run_product_pair(p, k, f.cols == 256, st, who);
+    if (f.pair) return run_product_pair(p, k, f.cols == 256, f.S, st, who);
     k.tiles_m = (int)((p.M + 127) / 128);
     const int outc = p.epi == EPI_GATED ? f.cols / 2 : f.cols;
     k.tiles_n = (p.N + outc - 1) / outc;

@@ -104,40 +104,27 @@ __device__ __forceinline__ void img_store4(const Image& im, long long m, int n, 
     }
 }
 
-// The epilogue on four columns n.. of row m; a whole warp calls it (row_ok: this lane's row exists).
-template <typename T, int EPI>
-__device__ __forceinline__ void finish4(const Epi& e, long long m, int n, int N, bool row_ok, float (&a)[4], float (&b)[4]) {
-    const int valid = row_ok ? min(4, max(0, N - n)) : 0;
-    T* y = static_cast<T*>(e.y);
-    constexpr bool FAST = sizeof(T) == 2;
-    float add[4] = {0.f, 0.f, 0.f, 0.f};
-    if (EPI != EPI_GATED && e.add && valid) load4(static_cast<const T*>(e.add) + m * e.ldadd + n, valid, e.vec_add, add);
-    if (EPI == EPI_STORE) {
+// act of N values: the choice outside the loop, so that the values' instruction chains interleave
+template <bool FAST, int N>
+__device__ __forceinline__ void act_all(float (&a)[N], int act) {
+    switch (act) {
+        case FTP_ACT_RELU:
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] += add[i];
-        if (valid) store4(y + m * e.ldy + n, valid, e.vec_y, a);
-        return;
-    }
-    if (EPI == EPI_LINEAR && e.bias) {
+            for (int i = 0; i < N; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU);
+            break;
+        case FTP_ACT_RELU6:
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < valid) a[i] += __ldg(e.bias + n + i);
-    }
-    if (e.stash_kind == STASH_FULL && valid) {
-        store4(static_cast<T*>(e.stash[0]) + m * e.ldstash + n, valid, e.vec_stash, a);
-        if (EPI == EPI_GATED) store4(static_cast<T*>(e.stash[1]) + m * e.ldstash + n, valid, e.vec_stash, b);
-    } else if (e.stash_kind == STASH_8BIT) {
-        // columns past the end are zero products (their operand tiles are filled with zeros): no effect on a block's maximum
-        img_store4(e.img[0], m, n, a, row_ok);
-        if (EPI == EPI_GATED) img_store4(e.img[1], m, n, b, row_ok);
-    }
-    if (valid && y) {
-        float v[4];
+            for (int i = 0; i < N; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU6);
+            break;
+        case FTP_ACT_GELU:
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float f = act_value<FAST>(a[i], e.act);
-            v[i] = EPI == EPI_GATED ? f * b[i] : f + add[i];
-        }
-        store4(y + m * e.ldy + n, valid, e.vec_y, v);
+            for (int i = 0; i < N; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_GELU);
+            break;
+        case FTP_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_SILU);
+            break;
+        default: break;
     }
 }
 
@@ -197,9 +184,9 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, 
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// signals the barrier at this offset in both CTAs once the MMAs issued so far have completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+// signals the barrier at this offset in the CTAs of `mask` (both of the pair) once the MMAs issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t mask) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
 }
 
 // The MMA warp of either kernel: `blocks` 64-wide blocks per tile, one tile (tile kernel) or `tiles` of them in turn.  The
@@ -208,7 +195,7 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
 //   full / empty: ring barriers; accf / acce: accumulator complete / read, BUFS of them in turn.
 template <int CG, int BN, int STAGES, uint32_t STAGE_BYTES, uint32_t A_BYTES, bool AMN, bool BMN, bool CHUNKED, int BUFS>
 __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t empty0, uint32_t accf0, uint32_t acce0, uint32_t tmem, int tiles, int blocks,
-                                         const KArgs& p) {
+                                         const KArgs& p, uint16_t mask = 3) {
     constexpr uint32_t SLAB = 64 * BK * 2;
     constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
                                ((uint32_t)(CG * 128 >> 4) << 24);
@@ -230,7 +217,7 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
         }
         first = false;
     };
-    auto commit = [&](uint32_t bar) { if (CG == 2) umma_commit_pair(bar); else umma_commit(bar); };
+    auto commit = [&](uint32_t bar) { if (CG == 2) umma_commit_pair(bar, mask); else umma_commit(bar); };
     for (int t = 0; t < tiles; ++t) {
         int left = 0;
         for (int kb = 0; kb < blocks; ++kb) {
@@ -309,6 +296,90 @@ __device__ __forceinline__ bool mma_warp(uint32_t ring, uint32_t full0, uint32_t
     return true;
 }
 
+// Rows rank, rank + S, ... of a 128-row tile that the S CTAs `first`, `first` + stride, ... of the cluster have each staged in
+// shared memory (BN columns, PITCH floats between rows), added and finished.  All threads of the block; a thread takes four
+// columns of four rows at a time, so that their loads and activations overlap (a row at a time: 14.8 instead of 10.4 us for
+// 1024 x 1024 x 1024 on 128 x 128 tiles).  A CTA adds its own sums first and the others' in turn from there: an order that
+// depends on the row alone, and no two CTAs read the same one at a time (all from the first: 1.5 us more with S = 4).
+template <typename T, int EPI, int BN, int PITCH>
+__device__ __forceinline__ void finish_rows(const Epi& e, uint32_t base, uint32_t S, uint32_t rank, uint32_t first, uint32_t stride, long long m0, int n0, long long M,
+                                            int N) {
+    constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN, LPR = OUTC / 4, RPW = 32 / LPR, U = 4;      // lanes per row, rows per warp
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, step = (int)(blockDim.x >> 5) * RPW;
+    const int rows = (int)max(0ll, min(128ll, M - m0)), c = (lane % LPR) * 4, n = n0 + c, valid = min(4, max(0, N - n));
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (EPI == EPI_LINEAR && e.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (i < valid) bias[i] = __ldg(e.bias + n + i);
+    }
+#pragma unroll 1
+    for (int i0 = warp * RPW; i0 * (int)S + (int)rank < rows; i0 += step * U) {                      // whole warps: img_store4 exchanges
+        int r[U];
+        bool on[U];
+        float a[4 * U], b[4 * U], add[4 * U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = (i0 + u * step + lane / LPR) * (int)S + (int)rank;
+            on[u] = r[u] < rows;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { a[4 * u + i] = b[4 * u + i] = 0.f; add[4 * u + i] = bias[i]; }
+        }
+        for (uint32_t k = 0; k < S; ++k) {
+            const uint32_t turn = rank + k < S ? rank + k : rank + k - S;
+            const uint32_t there = S > 1 ? map_rank(base, first + turn * stride) : base;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!on[u]) continue;
+                const uint32_t from = there + (uint32_t)(r[u] * PITCH + c) * 4;
+                const float4 v = ld_cluster4(from);
+                a[4 * u] += v.x; a[4 * u + 1] += v.y; a[4 * u + 2] += v.z; a[4 * u + 3] += v.w;
+                if (EPI == EPI_GATED) {
+                    const float4 w = ld_cluster4(from + OUTC * 4);
+                    b[4 * u] += w.x; b[4 * u + 1] += w.y; b[4 * u + 2] += w.z; b[4 * u + 3] += w.w;
+                }
+            }
+        }
+        if (EPI == EPI_LINEAR) {
+#pragma unroll
+            for (int i = 0; i < 4 * U; ++i) a[i] += add[i];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float add4[4] = {0.f, 0.f, 0.f, 0.f};
+            if (EPI != EPI_GATED && e.add && on[u] && valid) load4(static_cast<const T*>(e.add) + (m0 + r[u]) * e.ldadd + n, valid, e.vec_add, add4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add[4 * u + i] = add4[i];
+        }
+        if (EPI != EPI_STORE && e.stash_kind != STASH_NONE) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long m = m0 + r[u];
+                float a4[4], b4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { a4[i] = a[4 * u + i]; b4[i] = b[4 * u + i]; }
+                if (e.stash_kind == STASH_FULL) {
+                    if (!on[u] || !valid) continue;
+                    store4(static_cast<T*>(e.stash[0]) + m * e.ldstash + n, valid, e.vec_stash, a4);
+                    if (EPI == EPI_GATED) store4(static_cast<T*>(e.stash[1]) + m * e.ldstash + n, valid, e.vec_stash, b4);
+                } else {
+                    // columns past the end are zero products (their operand tiles are filled with zeros): no effect on a block's maximum
+                    img_store4(e.img[0], m, n, a4, on[u]);
+                    if (EPI == EPI_GATED) img_store4(e.img[1], m, n, b4, on[u]);
+                }
+            }
+        }
+        if (!e.y) continue;
+        if (EPI != EPI_STORE) act_all<sizeof(T) == 2>(a, e.act);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = EPI == EPI_GATED ? a[4 * u + i] * b[4 * u + i] : a[4 * u + i] + add[4 * u + i];
+            if (on[u] && valid) store4(static_cast<T*>(e.y) + (m0 + r[u]) * e.ldy + n, valid, e.vec_y, v);
+        }
+    }
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------
 bool make_map(CUtensorMap* map, const Operand& o, int box_x, int box_y) {
     EncodeTiledFn fn = encode_fn();
@@ -366,8 +437,9 @@ cudaError_t launch_cluster(void (*kern)(KA...), dim3 grid, unsigned block, size_
 
 }  // namespace
 
-// products on CTA pairs (ffn_pair.cu); wide: 256 x 256 tiles instead of 256 x 128
-ftp_status run_product_pair(const Product& p, const KArgs& base, bool wide, cudaStream_t st, const char* who);
+// products on CTA pairs (ffn_pair.cu); wide: 256 x 256 tiles instead of 256 x 128; S > 1: pairs that share a 256 x 128 tile's
+// reduction
+ftp_status run_product_pair(const Product& p, const KArgs& base, bool wide, int S, cudaStream_t st, const char* who);
 
 }  // namespace ffn
 }  // namespace ftp

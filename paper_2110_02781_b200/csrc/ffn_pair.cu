@@ -5,7 +5,7 @@
 // operand byte that a CTA loads is used for twice as many products as in a tile of its own -- which is what bounds large
 // products: at 256 x 256 a pair needs 64 KB per 8.4 MFLOP from L2.
 //
-// Warps 0, 2 and 3 (one thread each, in each CTA) stream the operand tiles with TMA; the bytes of both CTAs are counted on the
+// Warps 0, 2 and 3 (one elected thread each, in each CTA) stream the operand tiles with TMA; the bytes of both CTAs are counted on the
 // first CTA's barrier.  Warp 1 of the first CTA issues the MMAs and hands stages and accumulators on with commits that
 // signal both CTAs.  Warps 4-11 empty the accumulator: warp w the 32 lanes of its quarter and one half of the columns.  The
 // accumulator is double (2 x BN columns), so the epilogue of a tile -- bias, activation, kept values, residual -- runs
@@ -134,30 +134,6 @@ __device__ __forceinline__ void img_store32(const Image& im, long long m, int n,
     im.e[m * (im.pitch / IMG_BLOCK) + n / IMG_BLOCK] = (uint8_t)e;
 }
 
-// act of 32 values: the choice outside the loop, so that the values' instruction chains interleave
-template <bool FAST>
-__device__ __forceinline__ void act_32(float (&a)[32], int act) {
-    switch (act) {
-        case FTP_ACT_RELU:
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU);
-            break;
-        case FTP_ACT_RELU6:
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_RELU6);
-            break;
-        case FTP_ACT_GELU:
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_GELU);
-            break;
-        case FTP_ACT_SILU:
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = act_value<FAST>(a[i], FTP_ACT_SILU);
-            break;
-        default: break;
-    }
-}
-
 // The addend of a 32 x 32 bf16 piece on its way from memory, 16 bytes per access: four accesses per lane, begun before the
 // piece's accumulator is read.
 struct Ahead { uint4 v[4]; };
@@ -207,7 +183,7 @@ __device__ __forceinline__ void finish_piece(const Epi& e, uint8_t* buf, long lo
         if (EPI == EPI_GATED) img_store32(e.img[1], m + lane, n, b);
     }
     if (!e.y) return;
-    if (EPI != EPI_STORE) act_32<FAST>(a, e.act);
+    if (EPI != EPI_STORE) act_all<FAST>(a, e.act);
     if (EPI == EPI_GATED) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) a[i] *= b[i];
@@ -406,6 +382,140 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
 }
 
+// Several pairs of a cluster share a 256 x 128 tile's reduction, for products with too few tiles for all pairs: every CTA
+// leaves its 128 rows of partial sums in shared memory (the ring is free by then), and the CTAs that hold the same rows add
+// and finish every S-th of them each (finish_rows): 1024 x 1024 x 1024 float 22 instead of 28 us, 512 x 11008 x 512 bf16 15
+// instead of 30.
+template <typename T, bool AMN, bool BMN, int EPI>
+__global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_split_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
+                                                                    const __grid_constant__ CUtensorMap mapB0, const __grid_constant__ CUtensorMap mapB1,
+                                                                    const __grid_constant__ KArgs p) {
+    constexpr int BN = 128, STAGES = PAIR_STAGES<BN>, WC = BN / 2, PITCH = BN + 4;
+    constexpr bool CHUNKED = sizeof(T) == 4;
+    constexpr int BUFS = CHUNKED ? 2 : 1;
+    constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2, B_BYTES = BN / 2 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+    constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN, TMEM_COLS = BUFS * ACC;
+    constexpr int OUTC = EPI == EPI_GATED ? BN / 2 : BN;
+    static_assert(128 * PITCH * 4 <= STAGES * STAGE_BYTES, "the staged sums reuse the operand ring");
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS];
+    __shared__ uint32_t tmem_base, failed;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t C;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
+    const uint32_t cta = cluster_rank(), side = cta & 1, slice = cta >> 1, S = C >> 1;
+    const int tn_all = p.tiles_n * p.parts_n, all_kb = p.kb_part * p.parts_k;
+    int tm, tn;
+    tile_at((int)(blockIdx.x / C), p.tiles_m, tn_all, tm, tn);
+    const int out = tn / p.tiles_n;
+    const long long m0 = (long long)tm * 256 + side * 128;
+    const int n0 = (tn - out * p.tiles_n) * OUTC;
+    const int kb0 = (int)((long long)all_kb * slice / S), kb1 = (int)((long long)all_kb * (slice + 1) / S);
+    const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[STAGES]), accf0 = smem_u32(&bars[2 * STAGES]), acce0 = accf0 + 8 * BUFS;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&mapA0); tma_prefetch_map(&mapB0);
+        if (p.parts_k > 1) tma_prefetch_map(&mapA1);
+        if (p.parts_k > 1 || p.parts_n > 1 || EPI == EPI_GATED) tma_prefetch_map(&mapB1);
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+        for (int b = 0; b < BUFS; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, 16); }
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync_all();                                              // the barriers of all CTAs exist
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    grid_dep_sync();
+
+    bool ok = true;
+    if (warp < 4 && warp != 1) {
+        // ---- producers ----
+        Slot<STAGES> sl;
+        const uint32_t lead_full0 = map_rank(full0, cta & ~1u), ring = smem_u32(smem);
+        const int me = producer_of(warp), z = p.np == 1 ? 0 : p.np - 1 - me, step = p.np == 1 ? PRODUCERS : 1;
+        const uint32_t bytes = (z < p.pa ? 2 * A_BYTES : 0) + (z < p.pb ? 2 * B_BYTES : 0);
+        const int nb = n0 + (EPI == EPI_GATED ? 0 : (int)side * (BN / 2));
+        bool peek = false;
+        sl.ahead(me);
+        for (int kb = kb0 + (p.np == 1 ? me : 0); kb < kb1; kb += step, sl.ahead(PRODUCERS)) {
+            const int part = kb >= p.kb_part, k = (kb - (part ? p.kb_part : 0)) * BK;
+            ok = warp_ready(peek, empty0 + 8 * sl.s, sl.parity ^ 1, p.err, 1);                       // at once for a slot never used
+            if (!ok) break;
+            Slot<STAGES> then = sl;
+            then.ahead(PRODUCERS);
+            peek = mbar_peek(empty0 + 8 * then.s, then.parity ^ 1);  // of this warp's next slot, see mma_warp
+            if (elect_one()) {
+                const CUtensorMap* ma = part ? &mapA1 : &mapA0;
+                const CUtensorMap* mb = (EPI == EPI_GATED ? side != 0 : (part || out)) ? &mapB1 : &mapB0;
+                const uint32_t sa = ring + (uint32_t)sl.s * STAGE_BYTES, sb = sa + A_BYTES, bar = lead_full0 + 8 * sl.s;
+                if (side == 0) mbar_expect_tx(full0 + 8 * sl.s, bytes);
+                if (z < p.pa) {
+                    if (AMN) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) tma_load_3d_pair(sa + u * SLAB, ma, (int)m0 + 64 * u, k, z, bar);
+                    } else
+                        tma_load_3d_pair(sa, ma, k, (int)m0, z, bar);
+                }
+                if (z < p.pb) {
+                    if (BMN) tma_load_3d_pair(sb, mb, nb, k, z, bar);
+                    else tma_load_3d_pair(sb, mb, k, nb, z, bar);
+                }
+            }
+            __syncwarp();
+        }
+    } else if (warp == 1) {
+        if (side == 0)
+            ok = mma_warp<2, BN, STAGES, STAGE_BYTES, A_BYTES, AMN, BMN, CHUNKED, BUFS>(smem_u32(smem), full0, empty0, accf0, acce0, tmem, 1, kb1 - kb0, p,
+                                                                                     (uint16_t)(3u << (cta & ~1u)));
+    } else if (warp >= 4) {
+        // ---- partial sums -> shared memory ----
+        const int q = warp & 3, col0 = ((warp - 4) >> 2) * WC;
+        const uint32_t lead_acce0 = map_rank(acce0, cta & ~1u), lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)col0;
+        float* row = reinterpret_cast<float*>(smem) + (q * 32 + lane) * PITCH + col0;
+        float acc[WC];
+#pragma unroll
+        for (int i = 0; i < WC; ++i) acc[i] = 0.f;
+        const int chunks = CHUNKED ? (kb1 - kb0 + p.chunk - 1) / p.chunk : 1;
+        for (int c = 0; c < chunks; ++c) {
+            const int b = CHUNKED ? c & 1 : 0;
+            ok = warp_wait_for(accf0 + 8 * b, CHUNKED ? (c >> 1) & 1 : 0, p.err, 3);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int g = 0; g < WC / 32; ++g) add_acc(lanes + (uint32_t)b * ACC + g * 32, BN, CHUNKED && p.np > 1, acc + g * 32);
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (CHUNKED && lane == 0) mbar_arrive_cluster(lead_acce0 + 8 * b);
+        }
+        if (ok) {                                                    // the last MMA of the tile has completed: the ring is free
+#pragma unroll
+            for (int g = 0; g < WC / 4; ++g) *reinterpret_cast<float4*>(row + g * 4) = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
+        }
+    }
+    if (!ok) {
+        if (lane == 0) failed = 1;
+        // error path: time for the copies and MMAs already issued, which touch both CTAs, before either may leave
+        const unsigned long long t0 = gtime();
+        while (gtime() - t0 < 1000000ull) __nanosleep(1000);
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync_all();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    bool all = true;
+    for (uint32_t k = 0; k < C; ++k) all = all && ld_cluster1(map_rank(smem_u32(&failed), k)) == 0;
+    if (all) finish_rows<T, EPI, BN, PITCH>(p.e[out], smem_u32(smem), S, slice, side, 2, m0, n0, p.M, p.N);
+    cluster_sync_all();                                              // nobody leaves while another CTA reads its shared memory
+}
+
 template <typename T, int BN, bool AMN, bool BMN, int EPI>
 ftp_status launch_pair(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
     Maps m;
@@ -419,29 +529,45 @@ ftp_status launch_pair(const Product& p, const KArgs& k, cudaStream_t st, const 
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
+template <typename T, bool AMN, bool BMN, int EPI>
+ftp_status launch_split(const Product& p, const KArgs& k, int S, cudaStream_t st, const char* who) {
+    Maps m;
+    FTP_REQUIRE(make_maps(m, p, 128, 64), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
+    auto kern = ffn_split_kernel<T, AMN, BMN, EPI>;
+    constexpr uint32_t SMEM = PAIR_RING<128> + 1024;
+    static std::atomic<unsigned long long> asked{0};
+    cudaError_t e = allow_smem(asked, kern, (int)SMEM);
+    const long long tiles = (long long)k.tiles_m * k.tiles_n * k.parts_n;
+    FTP_REQUIRE(tiles * 2 * S < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    if (e == cudaSuccess) e = launch_cluster(kern, dim3((unsigned)(tiles * 2 * S)), PAIR_THREADS, SMEM, 2 * S, st, m.a[0], m.a[1], m.b[0], m.b[1], k);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
 template <int BN, bool AMN, bool BMN, int EPI>
-ftp_status pair_typed(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
-    if constexpr (BN == 128)                                         // 256 float sums per thread row do not fit into registers
-        if (p.out_f32) return launch_pair<float, BN, AMN, BMN, EPI>(p, k, st, who);
+ftp_status pair_typed(const Product& p, const KArgs& k, int S, cudaStream_t st, const char* who) {
+    if constexpr (BN == 128) {                                       // 256 float sums per thread row do not fit into registers
+        if (p.out_f32) return S > 1 ? launch_split<float, AMN, BMN, EPI>(p, k, S, st, who) : launch_pair<float, BN, AMN, BMN, EPI>(p, k, st, who);
+        if (S > 1) return launch_split<__nv_bfloat16, AMN, BMN, EPI>(p, k, S, st, who);
+    }
     return launch_pair<__nv_bfloat16, BN, AMN, BMN, EPI>(p, k, st, who);
 }
 template <int BN>
-ftp_status pair_kind(const Product& p, const KArgs& k, cudaStream_t st, const char* who) {
-    if (p.epi == EPI_GATED) return pair_typed<BN, false, true, EPI_GATED>(p, k, st, who);
-    if (p.epi == EPI_LINEAR) return pair_typed<BN, false, true, EPI_LINEAR>(p, k, st, who);
-    if (p.a_mn) return pair_typed<BN, true, true, EPI_STORE>(p, k, st, who);
-    return pair_typed<BN, false, false, EPI_STORE>(p, k, st, who);
+ftp_status pair_kind(const Product& p, const KArgs& k, int S, cudaStream_t st, const char* who) {
+    if (p.epi == EPI_GATED) return pair_typed<BN, false, true, EPI_GATED>(p, k, S, st, who);
+    if (p.epi == EPI_LINEAR) return pair_typed<BN, false, true, EPI_LINEAR>(p, k, S, st, who);
+    if (p.a_mn) return pair_typed<BN, true, true, EPI_STORE>(p, k, S, st, who);
+    return pair_typed<BN, false, false, EPI_STORE>(p, k, S, st, who);
 }
 
 }  // namespace
 
-ftp_status run_product_pair(const Product& p, const KArgs& base, bool wide, cudaStream_t st, const char* who) {
+ftp_status run_product_pair(const Product& p, const KArgs& base, bool wide, int S, cudaStream_t st, const char* who) {
     KArgs k = base;
     wide = wide && !p.out_f32;
     const int bn = wide ? 256 : 128, outc = p.epi == EPI_GATED ? bn / 2 : bn;
     k.tiles_m = (int)((p.M + 255) / 256);
     k.tiles_n = (p.N + outc - 1) / outc;
-    return wide ? pair_kind<256>(p, k, st, who) : pair_kind<128>(p, k, st, who);
+    return wide ? pair_kind<256>(p, k, 1, st, who) : pair_kind<128>(p, k, S, st, who);
 }
 
 }  // namespace ffn

@@ -93,12 +93,17 @@ LARGE = [(1000, 330, 2300, 0, 0), (1100, 72, 2104, 8, 0), (3001, 40, 2300, 0, 0)
          (1023, 2049, 33, 0, 0), (2305, 64, 1025, 0, 0)]
 
 
+# few output tiles over a long reduction: clusters of CTA pairs that share tiles, in the forward pass or a gradient
+SHARED = [(130, 1283, 2050, 0, 0), (300, 4100, 1100, 0, 0), (300, 1100, 4100, 8, 0), (130, 1100, 4100, 0, 0), (2050, 4100, 200, 0, 8), (2050, 200, 4100, 0, 0),
+          (1290, 200, 2050, 0, 0)]
+
+
 def linear_case(seed, rows, cin, cout, dt, gap, off):
     x, w = dev(rnd(seed, rows, cin), dt, gap, off), dev(rnd(seed + 1, cin, cout, scale=cin ** -0.5), dt, gap, off)
     return x, w
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + FEW + LARGE)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + FEW + LARGE + SHARED)
 @pytest.mark.parametrize("dt,name,bias,res,keep", [(BF, "gelu", 1, 1, "full"), (BF, "none", 0, 0, None), (FP, "silu", 1, 1, "8bit"), (FP, "relu6", 0, 1, "full"),
                                                    (BF, "silu", 1, 0, None), (FP, "gelu", 1, 1, None), (BF, "relu", 0, 1, "8bit")])
 def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
@@ -129,7 +134,7 @@ def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
         assert_within(out, z, ez + top / 64, "stash")
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)] + LARGE)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)] + LARGE + SHARED)
 @pytest.mark.parametrize("dt,name,x8,keep,wide", [(BF, "gelu", 0, "full", 0), (BF, "none", 0, None, 1), (FP, "silu", 0, "full", 0), (FP, "none", 1, None, 0),
                                                   (BF, "relu6", 1, "8bit", 1), (FP, "gelu", 1, "8bit", 0)])
 def test_linear_backward(rows, cin, cout, gap, off, dt, name, x8, keep, wide):
@@ -171,7 +176,7 @@ def test_linear_backward(rows, cin, cout, gap, off, dt, name, x8, keep, wide):
 # ---- gated --------------------------------------------------------------------------------------------------
 GATED = [(1, 64, 64, 0, 0), (1, 1, 1, 0, 0), (1, 1000, 333, 0, 0), (4, 130, 200, 0, 0), (8, 512, 96, 8, 0), (33, 100, 31, 1, 1), (128, 256, 128, 0, 0),
          (130, 72, 136, 0, 0), (257, 1283, 320, 0, 0), (300, 64, 1000, 0, 8), (1000, 330, 1150, 0, 0), (1100, 72, 1048, 8, 0), (70, 1100, 1052, 0, 0),
-         (1025, 2049, 33, 0, 0)]
+         (1025, 2049, 33, 0, 0), (130, 4100, 700, 0, 0), (130, 1283, 1100, 0, 0), (300, 1100, 2050, 8, 0), (130, 1100, 1100, 0, 0), (2050, 700, 200, 0, 8)]
 
 
 def kept_pair(keep, rows, cout, dt, seed):
