@@ -2,6 +2,7 @@
 // planes, bias gradients, the few-token products) and the C entry points.
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 #include "ffn_math.cuh"
 #include "kernels.h"
 #include "launch.cuh"
@@ -624,6 +625,20 @@ ftp_status check_stash(const ftp_ffn_desc* d, const void* stash, const char* who
     FTP_REQUIRE(d->stash != STASH_8BIT || aligned(stash, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
     return FTP_OK;
 }
+// Addresses: multiples of their elements' size, and no output where an input or another output starts (further overlaps
+// cannot be told from columns of one matrix, which may be neighbours).
+ftp_status check_addresses(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins, const char* who) {
+    for (auto o = outs.begin(); o != outs.end(); ++o) {
+        if (!*o) continue;
+        for (const void* i : ins) FTP_REQUIRE(*o != i, FTP_EINVAL, "%s: an output lies on an input", who);
+        for (auto q = outs.begin(); q != o; ++q) FTP_REQUIRE(*o != *q, FTP_EINVAL, "%s: two outputs in one place", who);
+    }
+    return FTP_OK;
+}
+ftp_status check_elements(std::initializer_list<const void*> all, size_t bytes, const char* who) {
+    for (const void* p : all) FTP_REQUIRE(aligned(p, bytes), FTP_ERANGE, "%s: an address is not a multiple of its elements' size", who);
+    return FTP_OK;
+}
 ftp_status check_ws(const Carve& need, const void* ws, size_t ws_bytes, const char* who) {
     FTP_REQUIRE(need.off == 0 || (ws && ws_bytes >= need.off), FTP_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need.off);
     FTP_REQUIRE(need.off == 0 || aligned(ws, 256), FTP_ERANGE, "%s: workspace must start on a 256-byte boundary", who);
@@ -801,8 +816,13 @@ ftp_status check_and_forward(const ftp_ffn_desc* d, const void* x, const void* w
     if (d->rows == 0) return FTP_OK;
     FTP_REQUIRE(x && w0 && (!GATED || w1) && (y || (GATED && stash)), FTP_EINVAL, "%s: null buffer", who);
     if (ftp_status s = check_stash(d, stash, who)) return s;
+    const size_t e = d->precision == FTP_FP32 ? 4 : 2;
+    if (ftp_status s = check_elements({x, w0, w1, residual, y, d->stash == STASH_FULL ? stash : nullptr}, e, who)) return s;
+    if (ftp_status s = check_elements({bias}, 4, who)) return s;
     Carve c{nullptr, need, 0};
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
+    if (ftp_status s = check_addresses({y, stash}, {x, w0, w1, bias}, who)) return s;
+    if (ftp_status s = check_addresses({stash}, {residual}, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
     const ftp_status s = d->precision == FTP_FP32 ? forward<float, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, err, st, who)
@@ -825,8 +845,14 @@ ftp_status check_and_backward(const ftp_ffn_desc* d, const void* x, const void* 
     FTP_REQUIRE(GATED || (d->act == FTP_ACT_NONE) == (d->stash == STASH_NONE), FTP_EINVAL, "%s: an activation's backward pass needs the kept values, and only that does", who);
     if (ftp_status s = check_stash(d, stash, who)) return s;
     FTP_REQUIRE(!d->x_8bit || !x || aligned(x, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
+    const size_t e = d->precision == FTP_FP32 ? 4 : 2;
+    if (ftp_status s = check_elements({x, w0, w1, d->stash == STASH_FULL ? stash : nullptr, dy, addend, dx}, e, who)) return s;
+    if (ftp_status s = check_elements({dw0, dw1}, d->dw_f32 ? 4 : e, who)) return s;
+    if (ftp_status s = check_elements({dbias}, 4, who)) return s;
     Carve c{nullptr, need, 0};
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
+    if (ftp_status s = check_addresses({dx, dw0, dw1, dbias}, {x, w0, w1, stash, dy}, who)) return s;
+    if (ftp_status s = check_addresses({dw0, dw1, dbias}, {addend}, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
     const ftp_status s = d->precision == FTP_FP32 ? backward<float, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, err, st, who)
@@ -918,7 +944,8 @@ static ftp_status check_checkpoint(const void* x, const void* image, int64_t row
     FTP_REQUIRE(*ld >= cols && *ld < (1ll << 35), FTP_EINVAL, "%s: rows overlap (a pitch below the width)", who);
     FTP_REQUIRE(rows == 0 || (x && image), FTP_EINVAL, "%s: null buffer", who);
     FTP_REQUIRE(aligned(image, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
-    return FTP_OK;
+    FTP_REQUIRE(rows == 0 || x != image, FTP_EINVAL, "%s: the image lies on its values", who);
+    return check_elements({x}, precision == FTP_FP32 ? 4 : 2, who);
 }
 
 ftp_status ftp_checkpoint_pack(const void* x, int64_t rows, int32_t cols, int64_t ld, int32_t precision, void* image, int32_t part, void* stream) {

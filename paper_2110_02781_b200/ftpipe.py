@@ -390,7 +390,7 @@ def _rows(who, name, t, cols, dtype, cur):
             if s0 < cols:
                 _bad(who, f"{name}: rows overlap")
             return rows, s0
-    if t.dim() < 1 or t.shape[-1] != cols:
+    if t.dim() < 1 or cols < 1 or t.shape[-1] != cols:
         _bad(who, f"{name} must have {cols} columns, got {tuple(t.shape)}")
     if not t.is_contiguous():
         _bad(who, f"{name}: only a two-dimensional tensor may have gaps between its rows")
@@ -490,7 +490,7 @@ def ftp_checkpoint_bytes(rows, cols, parts=1):
 
 
 def _plan_checkpoint(key, cur, who, name, x, image, part):
-    cols = x.shape[-1]
+    cols = x.shape[-1] if x.dim() else 0
     prec = _precision(who, x)
     rows, ld = _rows(who, name, x, cols, x.dtype, cur)
     _image(who, "image", image, rows, cols, part + 1, cur)

@@ -64,7 +64,7 @@ def test_descriptors_that_are_refused(kw, status):
 def test_calls_that_are_refused():
     ok, L = desc(), F.lib
     ref = C.byref
-    P = FAKE
+    P, Q = FAKE, FAKE + 4096
     assert L.ftp_linear_forward(None, P, P, None, None, P, None, None, 0, None) == 1
     assert L.ftp_linear_forward(ref(ok), None, P, None, None, P, None, None, 0, None) == 1
     assert L.ftp_linear_forward(ref(ok), P, P, None, None, None, None, None, 0, None) == 1
@@ -76,7 +76,7 @@ def test_calls_that_are_refused():
     assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, None, 0, None) == 3         # no workspace
     assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, P, 100, None) == 3
     assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, None, P, None, P + 16, 1 << 30, None) == 2
-    assert L.ftp_linear_forward(ref(ok), P + 2, P, None, None, P, None, None, 0, None) == 2               # not on 16 bytes, and not said so
+    assert L.ftp_linear_forward(ref(ok), P + 2, P, None, None, Q, None, None, 0, None) == 2               # not on 16 bytes, and not said so
     assert L.ftp_linear_backward(ref(desc(act=3)), P, P, None, P, None, P, P, None, P, 1 << 30, None) == 1
     assert L.ftp_linear_backward(ref(desc(stash=1)), P, P, P, P, None, P, P, None, P, 1 << 30, None) == 1
     assert L.ftp_linear_backward(ref(ok), P, P, None, None, None, P, P, None, P, 1 << 30, None) == 1
@@ -85,6 +85,17 @@ def test_calls_that_are_refused():
     assert L.ftp_linear_backward(ref(ok), P, P, None, P, P, None, P, None, P, 1 << 30, None) == 1         # addend without dx
     assert L.ftp_linear_backward(ref(desc(ldr=63)), P, P, None, P, P, P, P, None, P, 1 << 30, None) == 1
     assert L.ftp_linear_backward(ref(desc(x8=1)), P + 4, P, None, P, None, P, P, None, P, 1 << 30, None) == 2
+    assert L.ftp_linear_forward(ref(ok), P + 1, P, None, None, Q, None, None, 0, None) == 2               # between elements
+    assert L.ftp_linear_forward(ref(ok), P, P, Q + 2, None, Q, None, None, 0, None) == 2
+    assert L.ftp_linear_forward(ref(desc(prec=0)), P, P, None, P + 2, Q, None, P, 1 << 30, None) == 2
+    assert L.ftp_linear_backward(ref(desc(f32=1)), P, P, None, P, None, None, Q + 2, None, P, 1 << 30, None) == 2
+    assert L.ftp_linear_forward(ref(ok), P, Q, None, None, P, None, None, 0, None) == 1                   # y on x, on w
+    assert L.ftp_linear_forward(ref(ok), P, Q, None, None, Q, None, None, 0, None) == 1
+    assert L.ftp_linear_forward(ref(desc(stash=1)), P, P, None, Q, Q, Q, None, 0, None) == 1              # kept values on y
+    assert L.ftp_linear_backward(ref(ok), P, P, None, P, None, Q, Q, None, P, 1 << 30, None) == 1         # dx and dw in one place
+    assert L.ftp_linear_backward(ref(ok), P, P, None, Q, None, Q, None, None, P, 1 << 30, None) == 1      # dx on dy
+    assert L.ftp_checkpoint_pack(P, 4, 4, 0, 1, P, 0, None) == 1
+    assert L.ftp_checkpoint_pack(P + 1, 4, 4, 0, 1, Q, 0, None) == 2
     assert L.ftp_gated_forward(ref(ok), P, P, None, P, None, None, 0, None) == 1
     assert L.ftp_gated_forward(ref(ok), P, P, P, None, None, None, 0, None) == 1
     assert L.ftp_gated_backward(ref(ok), P, P, P, None, P, None, P, P, None, P, 1 << 30, None) == 1       # one weight gradient

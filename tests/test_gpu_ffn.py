@@ -1,5 +1,8 @@
 """Feed-forward operators (linear, gated, 8-bit activation checkpoints) on the GPU against their float64 forms."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -510,6 +513,7 @@ def test_refusals():
     x, w, y = dev(rnd(220, 10, 32), BF), dev(rnd(221, 32, 24), BF), torch.empty(10, 24, dtype=BF, device="cuda")
     bias, dw, db = torch.zeros(24, device="cuda"), torch.empty_like(w), torch.empty(24, device="cuda")
     img = lambda *a: torch.empty(F.ftp_checkpoint_bytes(*a), dtype=torch.uint8, device="cuda")  # noqa: E731
+    r, both = torch.zeros_like(y), torch.zeros(2, 10, 24, dtype=BF, device="cuda")
     F.ftp_linear_forward(x, w, y, bias=bias)
     bad = [
         lambda: F.ftp_linear_forward(x.float(), w, y),                              # types differ
@@ -539,6 +543,16 @@ def test_refusals():
         lambda: F.ftp_linear_backward(x.float(), w.float(), y.float(), dw=dw.float(), ws=torch.empty(16, dtype=torch.uint8, device="cuda")),
         lambda: F.ftp_checkpoint_pack(x, img(9, 32)[:-300] if img(9, 32).numel() > 300 else img(1, 1)[:8]),
         lambda: F.ftp_checkpoint_pack(x.half(), img(10, 32)),
+        lambda: F.ftp_checkpoint_pack(x[0, 0], img(10, 32)),
+        lambda: F.ftp_linear_forward(x.new_empty(2, 5, 0), w[:0], y),
+        lambda: F.ftp_linear_forward(x, w[:, :8], x[:, :8]),                          # outputs on inputs or on each other
+        lambda: F.ftp_linear_forward(x, w, y, stash=y),
+        lambda: F.ftp_linear_forward(x, w, y, residual=r, stash=r),
+        lambda: F.ftp_linear_backward(x, w, y, dw=w),
+        lambda: F.ftp_linear_backward(x, w, y, dx=x),
+        lambda: F.ftp_linear_backward(x, w[:, :8], x[:, :8], dx=x),
+        lambda: F.ftp_gated_forward(x, w, w, both[0], stash=both),
+        lambda: F.ftp_gated_backward(x, w, w, y, dw_gate=dw, dw_up=dw),
         lambda: F.ftp_checkpoint_unpack(img(10, 32, 2)[1:-255], x),
     ]
     for k, call in enumerate(bad):
@@ -548,7 +562,7 @@ def test_refusals():
     F.ftp_check_op_status()
 
 
-def test_a_word_left_by_a_timed_out_wait_is_reported_once():
+def test_status_check_is_refused_while_the_stream_is_captured():
     F.ftp_check_op_status()
     g = torch.cuda.CUDAGraph()
     s = torch.cuda.Stream()
@@ -560,3 +574,32 @@ def test_a_word_left_by_a_timed_out_wait_is_reported_once():
         g.capture_end()
     assert e.value.status == 5
     F.ftp_check_op_status()
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    code = """
+import sys, torch
+import paper_2110_02781_b200 as F
+torch.manual_seed(0)
+for dt, rows in ((torch.bfloat16, 1), (torch.bfloat16, 300), (torch.float32, 700)):
+    x, w = torch.randn(rows, 72, device='cuda').to(dt), torch.randn(72, 136, device='cuda').to(dt)
+    y, h, dx, dw = (torch.empty(*s, dtype=dt, device='cuda') for s in ((rows, 136), (rows, 136), (rows, 72), (72, 136)))
+    img = torch.empty(F.ftp_checkpoint_bytes(rows, 72), dtype=torch.uint8, device='cuda')
+    def step():
+        F.ftp_linear_forward(x, w, y)
+        F.ftp_gated_forward(x, w, w, h)
+        F.ftp_checkpoint_pack(x, img)
+        F.ftp_linear_backward(img, w, h, dx=dx, dw=dw)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for t in (y, h, dx, dw):
+        t.zero_()
+    g.replay()
+    got = [t.clone() for t in (y, h, dx, dw)]
+    step()
+    F.ftp_check_op_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, (y, h, dx, dw)))
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
