@@ -11,6 +11,9 @@ def __getattr__(name):
         return importlib.import_module("." + name, __name__)
     ft = importlib.import_module(".ftpipe", __name__)      # raises if libftpipe.so is missing: there is no fallback
     try:
-        return getattr(ft, name)
+        value = getattr(ft, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
+    if callable(value) or isinstance(value, int):          # calls and constants: found at once from here on (1.5 us less a call)
+        globals()[name] = value
+    return value
