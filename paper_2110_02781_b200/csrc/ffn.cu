@@ -23,26 +23,66 @@ void launch(A&&... args) {
 __device__ int g_op_status;                  // set by a kernel whose bounded wait ran out; cleared by ftp_check_op_status
 std::atomic<int*> g_status_addr[64] = {};
 
-// ---- eight consecutive elements ----
-__device__ __forceinline__ void load8(const float* p, int valid, bool vec, float (&v)[8]) {
-    if (vec && valid >= 8) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+// ---- consecutive elements of rows that start anywhere ----
+// The bytes of a matrix, between which a whole 16-byte part may be read.
+struct Span { const char *lo, *hi; };
+template <typename T> Span span_of(const void* p, long long rows, long long cols, long long ld) {
+    return Span{static_cast<const char*>(p), static_cast<const char*>(p) + ((rows - 1) * ld + cols) * (long long)sizeof(T)};
 }
-__device__ __forceinline__ void load8(const bf16* p, int valid, bool vec, float (&v)[8]) {
-    if (vec && valid >= 8) {
-        const uint4 t = *reinterpret_cast<const uint4*>(p);
-        const unsigned u[4] = {t.x, t.y, t.z, t.w};
+// W words from p on, as the aligned 16-byte parts that cover them, of which neighbouring threads read the same ones, and how
+// far to shift them (element by element a copy of 4720 x 11570 bf16 ran at 2.4 TB/s).  `begin` has no branch in front of its
+// loads, so that those of several rows are in flight together; where a part reaches out of the matrix, the `valid` elements
+// are loaded one by one.  `end`: the words, zeros behind `valid`.
+template <typename T, int W> struct Words {
+    static constexpr int PER = 4 / (int)sizeof(T);
+    unsigned w[W + 4], sh;
+    __device__ __forceinline__ void begin(const T* p, int valid, const Span& all) {
+        sh = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15);
+        const char* from = reinterpret_cast<const char*>(p) - sh;
+        const bool ok = from >= all.lo && from + W * 4 + (sh ? 16 : 0) <= all.hi;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(u[i]); v[2 * i + 1] = bf_hi(u[i]); }
-        return;
+        for (int k = 0; k <= W / 4; ++k) {
+            const uint4 t = ok && (k < W / 4 || sh) ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+            w[4 * k] = t.x; w[4 * k + 1] = t.y; w[4 * k + 2] = t.z; w[4 * k + 3] = t.w;
+        }
+        if (!ok) {
+            sh = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                w[i] = 0u;
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (i * PER + e < valid) w[i] |= bits_of(p[i * PER + e]) << (16 * e);
+            }
+        }
     }
+    __device__ __forceinline__ void end(int valid, unsigned (&out)[W]) const {
+        unsigned a[W + 2], b[W + 1];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? __bfloat162float(p[i]) : 0.f;
+        for (int i = 0; i < W + 2; ++i) a[i] = sh & 8 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < W + 1; ++i) b[i] = sh & 4 ? a[i + 1] : a[i];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const unsigned v = sh & 2 ? __funnelshift_r(b[i], b[i + 1], 16) : b[i];
+            out[i] = i * PER >= valid ? 0u : PER == 2 && i * PER + 1 >= valid ? v & 0xffffu : v;
+        }
+    }
+    static __device__ __forceinline__ unsigned bits_of(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ unsigned bits_of(bf16 v) { return __bfloat16_as_ushort(v); }
+};
+template <typename T> using Words8 = Words<T, 2 * (int)sizeof(T)>;
+__device__ __forceinline__ void values8(const Words8<float>& r, int valid, float (&v)[8]) {
+    unsigned u[8];
+    r.end(valid, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+}
+__device__ __forceinline__ void values8(const Words8<bf16>& r, int valid, float (&v)[8]) {
+    unsigned u[4];
+    r.end(valid, u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(u[i]); v[2 * i + 1] = bf_hi(u[i]); }
 }
 
 // One plane (bf16 rounding) or three (24 mantissa bits) of eight values; rows of a plane start on 16 bytes.
@@ -89,39 +129,57 @@ template <typename F> __device__ __forceinline__ void group_at(const Groups& g, 
 
 // ---- operand planes: copies of bf16 rows at an aligned pitch, or the three planes of float rows ----
 template <typename T>
-__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, bool vec, bf16* __restrict__ out,
-                                                     long long plane, int planes) {
+__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, const Span all,
+                                                     bf16* __restrict__ out, long long plane, int planes) {
     grid_dep_sync();
     const long long pitch = 8ll * g.per_row;
     for (unsigned i0 = blockIdx.x * 256 * EIGHT_U + threadIdx.x; i0 < g.total; i0 += gridDim.x * 256 * EIGHT_U) {
-        float v[EIGHT_U][8];
+        Words8<T> raw[EIGHT_U];
 #pragma unroll
         for (int u = 0; u < EIGHT_U; ++u)
-            if (i0 + u * 256 < g.total) group_at(g, i0 + u * 256, [&](long long r, int c) { load8(x + r * ld + c, cols - c, vec, v[u]); });
+            if (i0 + u * 256 < g.total) group_at(g, i0 + u * 256, [&](long long r, int c) { raw[u].begin(x + r * ld + c, cols - c, all); });
 #pragma unroll
         for (int u = 0; u < EIGHT_U; ++u)
-            if (i0 + u * 256 < g.total) group_at(g, i0 + u * 256, [&](long long r, int c) { store_planes(out + r * pitch + c, plane, planes, v[u]); });
+            if (i0 + u * 256 < g.total)
+                group_at(g, i0 + u * 256, [&](long long r, int c) {
+                    float v[8];
+                    values8(raw[u], cols - c, v);
+                    store_planes(out + r * pitch + c, plane, planes, v);
+                });
     }
 }
 
 // ---- 8-bit images ----
-// Sixteen values as they are in memory, zeros behind `valid`; vec: rows on 16 bytes.
+// Sixteen values as they are in memory, zeros behind `valid`; VEC: rows on 16 bytes.
 template <typename T> struct Raw16 { uint4 q[sizeof(T)]; };
-template <typename T>
-__device__ __forceinline__ Raw16<T> fetch16(const T* p, int valid, bool vec) {
-    Raw16<T> r;
+template <typename T, bool VEC> struct Fetch16 {
+    Words<T, 4 * (int)sizeof(T)> r;
+    __device__ __forceinline__ void begin(const T* p, int valid, const Span& all) { r.begin(p, valid, all); }
+    __device__ __forceinline__ Raw16<T> end(int valid) const {
+        unsigned u[4 * sizeof(T)];
+        r.end(valid, u);
+        Raw16<T> o;
 #pragma unroll
-    for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = make_uint4(0u, 0u, 0u, 0u);
-    if (vec && valid >= 16) {
-#pragma unroll
-        for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
-    } else {
-        T* e = reinterpret_cast<T*>(r.q);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) if (k < valid) e[k] = p[k];
+        for (int k = 0; k < (int)sizeof(T); ++k) o.q[k] = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+        return o;
     }
-    return r;
-}
+};
+template <typename T> struct Fetch16<T, true> {
+    Raw16<T> r;
+    __device__ __forceinline__ void begin(const T* p, int valid, const Span&) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (valid >= 16) {
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
+        } else {
+            T* e = reinterpret_cast<T*>(r.q);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) if (k < valid) e[k] = p[k];
+        }
+    }
+    __device__ __forceinline__ Raw16<T> end(int) const { return r; }
+};
 __device__ __forceinline__ unsigned top16(const Raw16<float>& r) {   // bits of the largest magnitude, as a float's
     unsigned m = 0;
 #pragma unroll
@@ -157,27 +215,28 @@ __device__ __forceinline__ void values16(const Raw16<bf16>& r, float (&v)[16]) {
 // many would leave multiprocessors without a block.  Bound by instructions as much as by memory (8 columns, integer
 // conversions and a piece at a time: 55 us for 16384 x 4096 bf16).
 constexpr int PACK_U = 4;
-template <typename T, int U>
-__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, bool vec, const Image im) {
+template <typename T, int U, bool VEC>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, const Groups g, int cols, long long ld, const Span all, const Image im) {
     grid_dep_sync();                                                 // g: groups of 16 columns here
     for (unsigned b0 = blockIdx.x * 256 * U; b0 < g.total; b0 += gridDim.x * 256 * U) {
-        Raw16<T> raw[U];
+        Fetch16<T, VEC> got[U];
         unsigned row[U], col[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const unsigned i = min(b0 + threadIdx.x + u * 256, g.total - 1);       // whole warps take part in the exchange below
             row[u] = i / g.per_row;
             col[u] = (i - row[u] * g.per_row) * 16;
-            raw[u] = fetch16<T>(x + (long long)row[u] * ld + col[u], max(0, cols - (int)col[u]), vec);
+            got[u].begin(x + (long long)row[u] * ld + col[u], max(0, cols - (int)col[u]), all);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            unsigned top = top16(raw[u]);
+            const Raw16<T> raw = got[u].end(max(0, cols - (int)col[u]));
+            unsigned top = top16(raw);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             const unsigned e = img_exp(top);
             const float inv = img_inv(e);
             float v[16];
-            values16(raw[u], v);
+            values16(raw, v);
             unsigned w[4];
             if (__uint_as_float(top) * inv < 127.5f) {               // no code is cut to 127
 #pragma unroll
@@ -279,10 +338,9 @@ void by_rows(long long rows, long long per_row, F&& launch_piece) {
 }
 template <typename T>
 void launch_planes(const T* x, long long rows, long long cols, long long ld, bf16* out, long long plane, int planes, cudaStream_t st) {
-    const bool vec = aligned(x, 16) && ld * (long long)sizeof(T) % 16 == 0;
     const long long pitch = (cols + 7) / 8 * 8;
     by_rows(rows, pitch / 8, [&](long long r, Groups g, dim3 blocks) {
-        launch(planes_kernel<T>, blocks, dim3(256), 0, st, x + r * ld, g, (int)cols, ld, vec, out + r * pitch, plane, planes);
+        launch(planes_kernel<T>, blocks, dim3(256), 0, st, x + r * ld, g, (int)cols, ld, span_of<T>(x, rows, cols, ld), out + r * pitch, plane, planes);
     });
 }
 inline Image image_from(const Image& im, long long r) { return Image{im.q + r * im.pitch, im.e + r * (im.pitch / IMG_BLOCK), im.pitch}; }
@@ -291,10 +349,12 @@ inline bool few_pieces(const Groups& g) { return g.total <= SMS * 256 * PACK_U; 
 template <typename T>
 void launch_pack(const T* x, long long rows, long long cols, long long ld, const Image& im, cudaStream_t st) {
     const bool vec = aligned(x, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    const Span all = span_of<T>(x, rows, cols, ld);
     by_rows(rows, im.pitch / 16, [&](long long r, Groups g, dim3 blocks) {
         const T* from = x + r * ld;
-        if (few_pieces(g)) launch(pack_kernel<T, 1>, dim3((g.total + 255) / 256), dim3(256), 0, st, from, g, (int)cols, ld, vec, image_from(im, r));
-        else launch(pack_kernel<T, PACK_U>, blocks, dim3(256), 0, st, from, g, (int)cols, ld, vec, image_from(im, r));
+        const bool few = few_pieces(g);
+        auto kern = few ? (vec ? pack_kernel<T, 1, true> : pack_kernel<T, 1, false>) : (vec ? pack_kernel<T, PACK_U, true> : pack_kernel<T, PACK_U, false>);
+        launch(kern, few ? dim3((g.total + 255) / 256) : blocks, dim3(256), 0, st, from, g, (int)cols, ld, all, image_from(im, r));
     });
 }
 template <typename T>
@@ -312,7 +372,7 @@ void launch_unpack(const Image& im, long long rows, long long cols, T* out, long
 // their own in one kernel, or behind the blocks of the gradient kernel: a small call costs its launches.
 enum { JOB_PLANES = 0, JOB_IMAGE = 1 };
 struct Job {
-    const void* src; int vec;                // JOB_PLANES
+    const void* src; Span all;               // JOB_PLANES
     Image im;                                // JOB_IMAGE
     long long ld;                            // elements between rows of src (JOB_IMAGE: of out)
     bf16* out; long long plane; int planes, cols, kind;
@@ -329,14 +389,18 @@ __device__ __forceinline__ void run_jobs(const Jobs& all, unsigned block) {
     if (p.kind == JOB_IMAGE) { unpack_blocks<bf16, PACK_U>(p.im, p.g, p.cols, p.out, p.ld, true, block, p.blocks); return; }
     const long long pitch = 8ll * p.g.per_row;
     for (unsigned i0 = block * 256 * EIGHT_U + threadIdx.x; i0 < p.g.total; i0 += p.blocks * 256 * EIGHT_U) {
-        float v[EIGHT_U][8];
+        Words8<T> raw[EIGHT_U];
+#pragma unroll
+        for (int u = 0; u < EIGHT_U; ++u)
+            if (i0 + u * 256 < p.g.total) group_at(p.g, i0 + u * 256, [&](long long r, int c) { raw[u].begin(static_cast<const T*>(p.src) + r * p.ld + c, p.cols - c, p.all); });
 #pragma unroll
         for (int u = 0; u < EIGHT_U; ++u)
             if (i0 + u * 256 < p.g.total)
-                group_at(p.g, i0 + u * 256, [&](long long r, int c) { load8(static_cast<const T*>(p.src) + r * p.ld + c, p.cols - c, p.vec, v[u]); });
-#pragma unroll
-        for (int u = 0; u < EIGHT_U; ++u)
-            if (i0 + u * 256 < p.g.total) group_at(p.g, i0 + u * 256, [&](long long r, int c) { store_planes(p.out + r * pitch + c, p.plane, p.planes, v[u]); });
+                group_at(p.g, i0 + u * 256, [&](long long r, int c) {
+                    float v[8];
+                    values8(raw[u], p.cols - c, v);
+                    store_planes(p.out + r * pitch + c, p.plane, p.planes, v);
+                });
     }
 }
 template <typename T>
@@ -372,32 +436,31 @@ struct GradArgs {
     bf16* out[2]; long long plane; int planes;   // nullable; pitch = cols rounded up to 8
     float* sums;                             // nullable: [block rows][cols] column sums of a block row
     int rows_per_block;
+    Span all_dy, all_pre[2];                 // where whole parts of rows off 16 bytes may be read
     unsigned blocks_x, blocks;               // of the gradient itself: along the columns, all; the blocks behind them run the jobs
 };
 
-// Eight values as they are in memory.  VEC: every access fits; otherwise element by element, zeros behind `valid`.
+// Eight values as they are in memory, every access fits
 template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
-template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> fetch8(const T* p, int valid) {
+template <typename T, bool VEC> struct Fetch8 {
+    Words8<T> r;
+    __device__ __forceinline__ void begin(const T* p, int valid, const Span& all) { r.begin(p, valid, all); }
+};
+template <typename T> struct Fetch8<T, true> {
     Raw8<T> r;
-    if (VEC) {
+    __device__ __forceinline__ void begin(const T* p, int, const Span&) {
 #pragma unroll
         for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.q[k] = __ldcs(reinterpret_cast<const uint4*>(p) + k);
-    } else {
-        T* e = reinterpret_cast<T*>(r.q);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = k < valid ? p[k] : T(0.f);
     }
-    return r;
-}
-__device__ __forceinline__ void values8(const Raw8<float>& r, float (&v)[8]) {
+};
+__device__ __forceinline__ void values8(const Raw8<float>& r, int, float (&v)[8]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         v[4 * k] = __uint_as_float(r.q[k].x); v[4 * k + 1] = __uint_as_float(r.q[k].y);
         v[4 * k + 2] = __uint_as_float(r.q[k].z); v[4 * k + 3] = __uint_as_float(r.q[k].w);
     }
 }
-__device__ __forceinline__ void values8(const Raw8<bf16>& r, float (&v)[8]) {
+__device__ __forceinline__ void values8(const Raw8<bf16>& r, int, float (&v)[8]) {
     const unsigned u[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[2 * i] = bf_lo(u[i]); v[2 * i + 1] = bf_hi(u[i]); }
@@ -439,21 +502,21 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradA
     if (blockIdx.x >= p.blocks) { run_jobs<T>(jobs, blockIdx.x - p.blocks); return; }
     const int by = blockIdx.x / p.blocks_x, bx = blockIdx.x - by * p.blocks_x;
     constexpr bool FAST = sizeof(T) == 2;
-    constexpr int R = sizeof(T) == 2 ? 4 : 2, P = GATED ? 2 : 1;
+    constexpr int R = VEC && sizeof(T) == 2 ? 4 : 2, P = GATED ? 2 : 1;
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = (bx * 32 + tx) * 8, valid = p.cols - c;
     const long long pitch = (p.cols + 7) / 8 * 8, r0 = (long long)by * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (valid > 0) {
         for (long long rb = r0 + ty; rb < r1; rb += 8 * R) {
-            Raw8<T> dy[R], pre[P][R];
+            Fetch8<T, VEC> dy[R], pre[P][R];
             Img8 img[P][R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const long long r = min(rb + 8 * i, r1 - 1);
-                dy[i] = fetch8<T, VEC>(static_cast<const T*>(p.dy) + r * p.lddy + c, valid);
+                dy[i].begin(static_cast<const T*>(p.dy) + r * p.lddy + c, valid, p.all_dy);
 #pragma unroll
                 for (int q = 0; q < P; ++q) {
-                    if (KIND == STASH_FULL) pre[q][i] = fetch8<T, VEC>(static_cast<const T*>(p.pre[q]) + r * p.cols + c, valid);
+                    if (KIND == STASH_FULL) pre[q][i].begin(static_cast<const T*>(p.pre[q]) + r * p.cols + c, valid, p.all_pre[q]);
                     if (KIND == STASH_8BIT) img[q][i] = img_fetch8(p.img[q], r, c);
                 }
             }
@@ -462,13 +525,13 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradA
                 const long long r = rb + 8 * i;
                 if (r >= r1) break;
                 float d[8], z[8], a[8], da[8];
-                values8(dy[i], d);
-                if (KIND == STASH_FULL) values8(pre[0][i], z);
+                values8(dy[i].r, valid, d);
+                if (KIND == STASH_FULL) values8(pre[0][i].r, valid, z);
                 if (KIND == STASH_8BIT) img_values8(img[0][i], z);
                 if (KIND != STASH_NONE) act_both8<FAST>(z, p.act, a, da);
                 if (GATED) {
                     float u[8], o[8];
-                    if (KIND == STASH_FULL) values8(pre[P - 1][i], u);
+                    if (KIND == STASH_FULL) values8(pre[P - 1][i].r, valid, u);
                     if (KIND == STASH_8BIT) img_values8(img[P - 1][i], u);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) { o[k] = d[k] * u[k] * da[k]; d[k] *= a[k]; }
@@ -563,7 +626,8 @@ ftp_status make_operand(Operand* o, const void* src, long long rows, long long c
     if (ws.dry()) return FTP_OK;
     Job j{};
     j.kind = JOB_PLANES;
-    j.src = src; j.ld = ld; j.vec = aligned(src, 16) && ld * (long long)sizeof(T) % 16 == 0;
+    j.all = span_of<T>(src, rows, cols, ld);
+    j.src = src; j.ld = ld;
     j.out = p; j.plane = plane; j.planes = planes;
     if (!add_job(jobs, j, rows, cols)) launch_planes(static_cast<const T*>(src), rows, cols, ld, p, plane, planes, st);
     return FTP_OK;
@@ -740,8 +804,12 @@ ftp_status backward(const ftp_ffn_desc* d, const void* x, const void* const* w, 
         g.dy = dy; g.lddy = ldy;
         g.act = d->act;
         g.rows = M; g.cols = d->cout;
+        g.all_dy = span_of<T>(dy, M, d->cout, ldy);
         for (int i = 0; i < (GATED ? 2 : 1); ++i) {
-            if (kind == STASH_FULL) g.pre[i] = static_cast<const T*>(stash) + (long long)i * M * d->cout;
+            if (kind == STASH_FULL) {
+                g.pre[i] = static_cast<const T*>(stash) + (long long)i * M * d->cout;
+                g.all_pre[i] = span_of<T>(g.pre[i], M, d->cout, d->cout);
+            }
             if (kind == STASH_8BIT) g.img[i] = image_at(const_cast<void*>(stash), M, d->cout, i);
         }
         const bool vec = d->cout % 8 == 0 && aligned(dy, 16) && ldy * (long long)sizeof(T) % 16 == 0 && aligned(g.pre[0], 16) && aligned(g.pre[1], 16);

@@ -228,12 +228,13 @@ static Form choose_form(const KArgs& k, const Product& p) {
     auto tiles = [&](int rows, int cols) { return (double)((p.M + rows - 1) / rows) * ((p.N + cols / gated - 1) / (cols / gated)) * k.parts_n; };
     Form best{true, 256, 1, 1e30};
     auto take = [&](const Form& f) { if (f.cost < best.cost) best = f; };
-    // results whose rows cannot be stored four elements at a time
-    const double ragged = k.e[0].vec_y ? 0 : 5.0;
+    // rows that cannot be moved four elements at a time: of the result, and of what is read or kept beside it
+    const Epi& e = k.e[0];
+    const double ragged = e.vec_y ? 0 : 5.0, beside = (e.add && !e.vec_add ? 1 : 0) + (e.stash_kind == STASH_FULL && !e.vec_stash ? 1 : 0);
     static constexpr double share[9] = {0, 0, 1.5, 2.1, 2.7, 3.1, 3.4, 3.8, 4.2}, pair_share[5] = {0, 0, 2.1, 2.4, 2.8};
     auto pair = [&](int cols, double c, double base, double epi) {
         const double t = c * blocks, n = tiles(256, cols), waves = std::ceil(n / 74);
-        take({true, cols, 1, base + ragged + std::max(t + (waves - 1) * std::max(t, epi), mbytes / std::min(4.0, 0.085 * n))});
+        take({true, cols, 1, base + ragged + 7 * beside + std::max(t + (waves - 1) * std::max(t, epi + 5 * beside), mbytes / std::min(4.0, 0.085 * n))});
         for (int S = 2; cols == 128 && S <= 4 && S <= blocks; ++S)   // one tile per cluster of four, six or eight CTAs
             if (tiles(256, cols) * S <= (S == 2 ? 66 : S == 3 ? 60 : 52))
                 take({true, cols, S, base + pair_share[S] + ragged / S + std::max(c * std::ceil(blocks / S), mbytes / 5.2)});
