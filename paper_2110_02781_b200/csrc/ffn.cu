@@ -753,8 +753,8 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
 constexpr int GRAD_ROWS = 64, GRAD_CHUNKS = 1024;
 // up to 256 rows in one block row, whose sums then are the bias gradient (a launch less)
 int grad_rows_per_block(long long rows) { return rows <= 256 ? 256 : (int)std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8); }
-// without a bias gradient: enough blocks to fill the GPU four times over, 16 rows at least (246 x 576 x 1454 bf16 backward: 41 instead of 20 us with all rows
-// in one block row)
+// without a bias gradient: enough blocks to fill the GPU four times over, 16 rows at least (246 x 576 x 1454 bf16 backward:
+// 41 instead of 20 us with all rows in one block row)
 int grad_rows_per_block(long long rows, long long cols) {
     const long long chunks = std::max<long long>(1, 4 * SMS / ((cols + 255) / 256)), want = ((rows + chunks - 1) / chunks + 7) / 8 * 8;
     return std::max<int>(rows > GRAD_ROWS * GRAD_CHUNKS ? grad_rows_per_block(rows) : 16, (int)std::min<long long>(want, GRAD_ROWS));

@@ -94,6 +94,8 @@ FEW = [(1, 4096, 256, 0, 0), (2, 1024, 70, 0, 0), (4, 520, 129, 0, 1), (5, 2000,
 # enough output tiles for CTA pairs: forward, input gradient, weight gradient; odd edges, several tiles per pair
 LARGE = [(1000, 330, 2300, 0, 0), (1100, 72, 2104, 8, 0), (3001, 40, 2300, 0, 0), (1000, 2300, 330, 0, 0), (330, 1000, 2300, 0, 0), (70, 1100, 2104, 0, 8),
          (1023, 2049, 33, 0, 0), (2305, 64, 1025, 0, 0)]
+# the same with results, addends and kept values whose rows lie on 2, 4 or 8 bytes
+UNEVEN = [(2500, 300, 2051, 0, 0), (2500, 300, 2050, 0, 0), (1300, 500, 2053, 1, 2), (2500, 2051, 300, 0, 0), (2500, 2050, 300, 0, 1), (1400, 2060, 300, 0, 0)]
 
 
 # few output tiles over a long reduction: clusters of CTA pairs that share tiles, in the forward pass or a gradient
@@ -106,7 +108,7 @@ def linear_case(seed, rows, cin, cout, dt, gap, off):
     return x, w
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + FEW + LARGE + SHARED)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", LINEAR + FEW + LARGE + UNEVEN + SHARED + [(1100, 8000, 2051, 0, 0), (1100, 8000, 2050, 0, 0)])
 @pytest.mark.parametrize("dt,name,bias,res,keep", [(BF, "gelu", 1, 1, "full"), (BF, "none", 0, 0, None), (FP, "silu", 1, 1, "8bit"), (FP, "relu6", 0, 1, "full"),
                                                    (BF, "silu", 1, 0, None), (FP, "gelu", 1, 1, None), (BF, "relu", 0, 1, "8bit")])
 def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
@@ -137,7 +139,7 @@ def test_linear_forward(rows, cin, cout, gap, off, dt, name, bias, res, keep):
         assert_within(out, z, ez + top / 64, "stash")
 
 
-@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)] + LARGE + SHARED)
+@pytest.mark.parametrize("rows,cin,cout,gap,off", [c for c in LINEAR if c[0] != 16] + [(1100, 40, 56, 0, 0), (5000, 16, 16, 0, 0)] + LARGE + UNEVEN + SHARED)
 @pytest.mark.parametrize("dt,name,x8,keep,wide", [(BF, "gelu", 0, "full", 0), (BF, "none", 0, None, 1), (FP, "silu", 0, "full", 0), (FP, "none", 1, None, 0),
                                                   (BF, "relu6", 1, "8bit", 1), (FP, "gelu", 1, "8bit", 0)])
 def test_linear_backward(rows, cin, cout, gap, off, dt, name, x8, keep, wide):
