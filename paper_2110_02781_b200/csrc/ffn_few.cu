@@ -21,6 +21,7 @@ struct FewArgs {
     const void* x; long long ldx;
     const void* w[2]; long long ldw;
     int vec_w, vec_x, ring;                                          // rows of w / of x on 16 bytes; both
+    Span all[2];                                                     // the bytes of w
     Epi e;
     int* err;
     int rows, K, N, kper;                                            // kper: rows of w per CTA of a cluster
@@ -331,30 +332,47 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
 }
 
 // Any other rows of w: loads into registers, a batch of U steps ahead.
-template <typename T, int MR, int P>
+// Sixteen bytes of a row of w: EVEN: rows on 16 bytes, a strip's last columns element by element; otherwise the parts that cover
+// them (4096 x 12063 bf16, one token: 64 us element by element, 42 so).
+template <typename T, bool EVEN> struct Row16 {
+    uint4 q;
+    __device__ __forceinline__ void begin(const T* at, int valid, const Span&) {
+        q = valid <= 0 ? make_uint4(0u, 0u, 0u, 0u) : valid >= Wide<T>::V ? ld_stream(at) : ld_partial<T>(at, valid);
+    }
+    __device__ __forceinline__ uint4 end(int) const { return q; }
+};
+template <typename T> struct Row16<T, false> {
+    Words<T, 4> r;
+    __device__ __forceinline__ void begin(const T* at, int valid, const Span& all) { r.begin(at, valid, all); }
+    __device__ __forceinline__ uint4 end(int valid) const {
+        unsigned u[4];
+        r.end(valid, u);
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <typename T, int MR, int P, bool EVEN>
 __global__ void __launch_bounds__(FEW_THREADS) ffn_few_kernel(const __grid_constant__ FewArgs p) {
     constexpr int V = Wide<T>::V, CW = 8 * V, XP = FEW_PITCH<MR>;    // columns of a thread and of a block
-    constexpr int U = P * MR * V >= 128 ? 2 : 4;
+    constexpr int U = P * MR * V >= 128 || !EVEN ? 2 : 4;
     extern __shared__ __align__(16) float xs[];                      // [kper][XP], at the end [FEW_WARPS][P][MR][CW] in its place
     __shared__ float part[P * MR * CW];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Part t = my_part<CW, MR>(p);
     const int c = t.n0 + (lane & 7) * V, valid = p.N - c, row = warp * 4 + (lane >> 3);
-    const bool whole = p.vec_w && valid >= V;
     grid_dep_sync();
 
-    auto load = [&](uint4 (&w)[U][P], int kb) {
+    auto load = [&](Row16<T, EVEN> (&w)[U][P], int kb) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = kb + u * FEW_STEP + row;
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 const T* at = static_cast<const T*>(p.w[q]) + (long long)(t.k0 + k) * p.ldw + c;
-                w[u][q] = k >= t.klen || valid <= 0 ? make_uint4(0u, 0u, 0u, 0u) : whole ? ld_stream(at) : ld_partial<T>(at, valid);
+                w[u][q].begin(at, k < t.klen ? valid : 0, p.all[q]);
             }
         }
     };
-    uint4 w[U][P], next[U][P];
+    Row16<T, EVEN> w[U][P], next[U][P];
     load(w, 0);
     stage_x<T, MR>(xs, p, t, threadIdx.x, FEW_THREADS);
     __syncthreads();
@@ -374,7 +392,7 @@ __global__ void __launch_bounds__(FEW_THREADS) ffn_few_kernel(const __grid_const
             if (k < t.klen) {
                 float f[P][V];
 #pragma unroll
-                for (int q = 0; q < P; ++q) unpack<T>(w[u][q], f[q]);
+                for (int q = 0; q < P; ++q) unpack<T>(w[u][q].end(valid), f[q]);
                 multiply<V, MR, P>(acc, xs + k * XP, f);
             }
         }
@@ -420,9 +438,9 @@ ftp_status launch_few(const FewArgs& a, int S, cudaStream_t st, const char* who)
         if (e == cudaSuccess) e = launch_cluster(kern, grid, RING_THREADS, RING_BYTES + 128, S, st, m0, m1, mx, a);
     } else {
         const size_t x_bytes = (size_t)FEW_PITCH<MR> * a.kper * 4, red_bytes = (size_t)FEW_WARPS * P * MR * CW * 4;
-        auto kern = ffn_few_kernel<T, MR, P>;
-        static std::atomic<unsigned long long> asked{0};
-        e = allow_smem(asked, kern, FEW_SMEM);
+        auto kern = a.vec_w ? ffn_few_kernel<T, MR, P, true> : ffn_few_kernel<T, MR, P, false>;
+        static std::atomic<unsigned long long> asked[2] = {};
+        e = allow_smem(asked[a.vec_w ? 1 : 0], kern, FEW_SMEM);
         if (e == cudaSuccess) e = launch_cluster(kern, grid, FEW_THREADS, std::max(x_bytes, red_bytes), S, st, a);
     }
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
@@ -467,6 +485,7 @@ ftp_status run_few(const void* x, long long ldx, const void* const* w, long long
     a.vec_x = aligned(x, 16) && (rows == 1 || ldx * (f32 ? 4 : 2) % 16 == 0);
     a.e = e;
     a.err = err;
+    for (int i = 0; i < products; ++i) a.all[i] = f32 ? span_of<float>(w[i], K, N, ldw) : span_of<__nv_bfloat16>(w[i], K, N, ldw);
     a.rows = rows; a.K = K; a.N = N;
     // Up to 4 MB of w the loads into registers are quicker, whose kernel begins and ends faster (one token, 1024 x 1024 bf16:
     // 3.6 against 4.6 us; 4096 x 4096 float: 14.2 against 13.1; the gated 4096 x 12288 bf16: 45 against 34.6)

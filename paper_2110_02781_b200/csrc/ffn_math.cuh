@@ -115,5 +115,54 @@ __device__ __forceinline__ void unpack_codes(unsigned q, float scale, float (&v)
     v[3] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - 8388736.f) * scale;
 }
 
+// ---- consecutive elements of rows that start anywhere ----
+// The bytes of a matrix, between which a whole 16-byte part may be read.
+struct Span { const char *lo, *hi; };
+template <typename T> Span span_of(const void* p, long long rows, long long cols, long long ld) {
+    return Span{static_cast<const char*>(p), static_cast<const char*>(p) + ((rows - 1) * ld + cols) * (long long)sizeof(T)};
+}
+// W words from p on, as the aligned 16-byte parts that cover them, of which neighbouring threads read the same ones, and how
+// far to shift them (element by element a copy of 4720 x 11570 bf16 ran at 2.4 TB/s).  `begin` has no branch in front of its
+// loads, so that those of several rows are in flight together; where a part reaches out of the matrix, the `valid` elements
+// are loaded one by one.  `end`: the words, zeros behind `valid`.
+template <typename T, int W> struct Words {
+    static constexpr int PER = 4 / (int)sizeof(T);
+    unsigned w[W + 4], sh;
+    __device__ __forceinline__ void begin(const T* p, int valid, const Span& all) {
+        sh = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15);
+        const char* from = reinterpret_cast<const char*>(p) - sh;
+        const bool ok = from >= all.lo && from + W * 4 + (sh ? 16 : 0) <= all.hi;
+#pragma unroll
+        for (int k = 0; k <= W / 4; ++k) {
+            const uint4 t = ok && (k < W / 4 || sh) ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+            w[4 * k] = t.x; w[4 * k + 1] = t.y; w[4 * k + 2] = t.z; w[4 * k + 3] = t.w;
+        }
+        if (!ok) {
+            sh = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                w[i] = 0u;
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (i * PER + e < valid) w[i] |= bits_of(p[i * PER + e]) << (16 * e);
+            }
+        }
+    }
+    __device__ __forceinline__ void end(int valid, unsigned (&out)[W]) const {
+        unsigned a[W + 2], b[W + 1];
+#pragma unroll
+        for (int i = 0; i < W + 2; ++i) a[i] = sh & 8 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < W + 1; ++i) b[i] = sh & 4 ? a[i + 1] : a[i];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const unsigned v = sh & 2 ? __funnelshift_r(b[i], b[i + 1], 16) : b[i];
+            out[i] = i * PER >= valid ? 0u : PER == 2 && i * PER + 1 >= valid ? v & 0xffffu : v;
+        }
+    }
+    static __device__ __forceinline__ unsigned bits_of(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ unsigned bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+};
+
 }  // namespace ffn
 }  // namespace ftp
