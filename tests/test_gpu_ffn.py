@@ -3,6 +3,7 @@ import math
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -605,3 +606,41 @@ for dt, rows in ((torch.bfloat16, 1), (torch.bfloat16, 300), (torch.float32, 700
 """
     done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_calls_from_several_threads_at_once():
+    shapes = [(1, 640, 512), (300, 200, 136), (130, 1100, 1100), (777, 264, 517)]
+    cases = [(dev(rnd(300 + i, m, k), dt), dev(rnd(310 + i, k, n, scale=k ** -0.5), dt)) for i, (m, k, n) in enumerate(shapes) for dt in (BF, FP)]
+    dys = [dev(rnd(320 + i, x.shape[0], w.shape[1]), x.dtype) for i, (x, w) in enumerate(cases)]
+
+    def step(i):
+        x, w = cases[i]
+        y, h, dx, dw = x.new_empty(x.shape[0], w.shape[1]), x.new_empty(x.shape[0], w.shape[1]), torch.empty_like(x), torch.empty_like(w)
+        F.ftp_linear_forward(x, w, y, act=F.ACT_SILU)
+        F.ftp_gated_forward(x, w, w, h)
+        F.ftp_linear_backward(x, w, dys[i], dx=dx, dw=dw)
+        return y, h, dx, dw
+
+    want = [step(i) for i in range(len(cases))]
+    torch.cuda.synchronize()
+    got, failed = {}, []
+
+    def work(t):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(5):
+                    for i in range(t, len(cases), 4):
+                        got[t, i] = step(i)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(t,)) for t in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    F.ftp_check_op_status()
+    assert not failed, failed
+    assert len(got) == len(cases) and all(torch.equal(a, b) for (t, i), r in got.items() for a, b in zip(r, want[i]))
