@@ -64,7 +64,8 @@ typedef enum {
 enum { FTP_CONV1D = 0, FTP_CONV2D = 1, FTP_DWCONV3x3 = 2, FTP_BN = 3, FTP_ACT = 4, FTP_ADD_RESIDUAL = 5,
        FTP_MAXPOOL2 = 6, FTP_GAP = 7, FTP_FC = 8, FTP_SOFTMAX_CE = 9,
        /* token-wise feed-forward layers (see "feed-forward operators"), applied at every position of an (N, H, W, C) tensor:
-        *   LINEAR: act(x W + bias) + output of op residual_src (-1: none; within the unit, or its input)
+        *   LINEAR: act(x W + bias) + output of op residual_src (-1: none; within the unit, or its input; as for ADD_RESIDUAL not
+        *           a batch norm in front of an ADD_RESIDUAL, of which only the sum is stored: FTP_EUNSUPPORTED)
         *   GATED : act(x W_gate) * (x W_up)
         * k is the form in which the values before the activation wait for the backward pass: 0 the tensors' type, 8 an
         * 8-bit image, which halves (bf16) or quarters (float) what a batch in flight holds of them. */

@@ -71,6 +71,9 @@ bool is_pointwise_op(const Op& o);
 bool is_3x3_op(const Op& o);
 
 // ---- shapes, parameter offsets, validation ------------------------------------------------------
+// A batch norm in front of an ADD_RESIDUAL is folded into it: only the sum is stored, and only the sum's gradient has a buffer.
+bool folded_into_add(const ftp_layer_desc* layers, int n, int s) { return s >= 0 && s + 1 < n && layers[s + 1].kind == FTP_ADD_RESIDUAL; }
+
 ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cfg, ftp_model& m) {
     FTP_REQUIRE(layers && cfg, FTP_EINVAL, "build_model: null argument");
     FTP_REQUIRE(n >= 1, FTP_EINVAL, "build_model: empty layer list");
@@ -129,6 +132,7 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
                     FTP_REQUIRE(s < i, FTP_EINVAL, "build_model: op %d: residual_src %d out of range", i, s);
                     FTP_REQUIRE(s >= m.unit_first.back() - 1, FTP_EINVAL, "build_model: op %d: a residual connection may not cross a unit edge", i);
                     FTP_REQUIRE(m.ops[s].Ho == H && m.ops[s].Wo == W && m.ops[s].Co == d.cout, FTP_EINVAL, "build_model: op %d: residual shapes differ", i);
+                    FTP_REQUIRE(!folded_into_add(layers, n, s), FTP_EUNSUPPORTED, "build_model: op %d: residual_src %d is a batch norm in front of a residual add, whose own output is not stored", i, s);
                 }
                 break;
             }
@@ -152,6 +156,7 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
                 FTP_REQUIRE(s >= m.unit_first.back() - 1, FTP_EINVAL, "build_model: op %d: a residual connection may not cross a unit edge", i);
                 const int sh = s < 0 ? cfg->in_h : m.ops[s].Ho, sw = s < 0 ? cfg->in_w : m.ops[s].Wo, sc = s < 0 ? cfg->in_c : m.ops[s].Co;
                 FTP_REQUIRE(sh == H && sw == W && sc == C, FTP_EINVAL, "build_model: op %d: residual shapes differ", i);
+                FTP_REQUIRE(!folded_into_add(layers, n, s), FTP_EUNSUPPORTED, "build_model: op %d: residual_src %d is a batch norm in front of a residual add, whose own output is not stored", i, s);
                 FTP_REQUIRE(i >= 1 && layers[i - 1].kind == FTP_BN && layers[i - 1].act == FTP_ACT_NONE && layers[i - 1].unit == d.unit,
                             FTP_EUNSUPPORTED, "build_model: op %d: a residual add must follow a BN without activation", i);
                 break;

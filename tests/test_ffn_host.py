@@ -129,3 +129,21 @@ def test_layer_lists_that_are_refused():
         with pytest.raises(F.FtpError):
             F.ftp_workspace_bytes(ls + tail, cfg)
             pytest.fail(str(ls))
+
+
+@pytest.mark.parametrize("precision", [0, 1])
+def test_a_folded_batch_norm_is_no_residual_source(precision):
+    """A batch norm in front of an ADD_RESIDUAL leaves the sum, not its own output: nothing may read it as a residual."""
+    import synth
+    L, K = synth.Layer, synth.KIND
+    lin = L(0, K["LINEAR"], 8, 8, 0, 1, 0, 0, 0, -1)
+    bn, add = L(0, K["BN"], 8, 8, 0, 1, 0, 0, 0, -1), L(0, K["ADD_RESIDUAL"], 8, 8, 0, 1, 0, 0, 0, 0)
+    tail = [L(1, K["GAP"], 8, 8, 0, 1, 0, 0, 0, -1), L(1, K["FC"], 8, 3, 1, 1, 0, 0, 1, -1), L(1, K["SOFTMAX_CE"], 3, 3, 0, 1, 0, 0, 0, -1)]
+    cfg = synth.config(2, 8, 1, 6, 3, precision=precision)
+    folded = [lin, lin, bn, add]                                     # op 2 is folded into op 3
+    for src in (1, 3):                                               # what is stored may be read
+        F.ftp_workspace_bytes(folded + [lin._replace(residual_src=src)] + tail, cfg)
+    for reader in ([lin._replace(residual_src=2)], [lin, lin._replace(residual_src=2)], [lin, bn, add._replace(residual_src=2)]):
+        with pytest.raises(F.FtpError) as e:
+            F.ftp_workspace_bytes(folded + reader + tail, cfg)
+        assert e.value.status == 7
