@@ -47,7 +47,9 @@ __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32
         : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// 32 columns of an accumulator, and of its small terms `small` columns further, added to acc[0..31]
+// 32 columns of an accumulator, and of its small terms `small` columns further, added to acc[0..31].  Where an operand holds an
+// infinity or a NaN, its first plane alone carries it and the product of the first planes is what the operands' product is;
+// the small terms beside it are that infinity times what is left of the other operand, of either sign or 0: not added.
 __device__ __forceinline__ void add_acc(uint32_t taddr, uint32_t small, bool both, float* acc) {
     uint32_t r[32], q[32];
     tmem_ld32_issue(taddr, r);
@@ -55,7 +57,10 @@ __device__ __forceinline__ void add_acc(uint32_t taddr, uint32_t small, bool bot
     tmem_ld_wait();
     if (both) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) acc[i] += __uint_as_float(r[i]) + __uint_as_float(q[i]);
+        for (int i = 0; i < 32; ++i) {
+            const float v = __uint_as_float(r[i]);
+            acc[i] += fabsf(v) < __uint_as_float(0x7f800000u) ? v + __uint_as_float(q[i]) : v;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[i] += __uint_as_float(r[i]);

@@ -1,0 +1,76 @@
+"""Values of the feed-forward operators where an elementwise worst-case bound says nothing: infinities."""
+import math
+
+import pytest
+import torch
+
+from ffn_helpers import ACTS, act
+
+pytestmark = pytest.mark.gpu
+F = pytest.importorskip("paper_2110_02781_b200")
+BF, FP = torch.bfloat16, torch.float32
+
+
+def rnd(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def ref(t):
+    return t.double().cpu()
+
+
+def same_kinds(got, want):
+    """The same NaN and the same infinities."""
+    got, want = ref(got), ref(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    inf = torch.isinf(want)
+    assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf], want[inf])
+
+
+# ---- infinities: products of a few tokens, of one CTA a tile, of clusters of pairs, of pairs -------------------------------
+@pytest.mark.parametrize("rows,cin,cout", [(3, 200, 72), (20, 200, 72), (140, 200, 72), (140, 4100, 200), (1100, 72, 2104), (300, 4100, 1100)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("name", ["none", "relu6"])
+def test_infinities_reach_the_results_that_hold_them(rows, cin, cout, dt, name):
+    x, w = rnd(1, rows, cin), rnd(2, cin, cout)
+    w[5, :8] = torch.tensor([1.0, -1.0, 0.0, 0.5, 3.0, -2.0, -0.0, 1.5])     # values of one plane, and zeros
+    x[0, 5], x[1, 5] = math.inf, -math.inf
+    x[2, 5], x[2, 9] = math.inf, math.inf                                    # of either sign in one sum
+    w[7, 20], w[8, 21] = math.inf, -math.inf
+    x[rows - 1, 7] = 1.0
+    xd, wd = x.to(dt).cuda(), w.to(dt).cuda()
+    y = torch.empty(rows, cout, dtype=dt, device="cuda")
+    F.ftp_linear_forward(xd, wd, y, act=ACTS[name])
+    same_kinds(y, act(ref(xd) @ ref(wd), name))
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(3, 200, 72), (12, 200, 72), (140, 200, 72), (1100, 72, 1052), (130, 4100, 700)])
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_infinities_pass_through_the_gate(rows, cin, cout, dt):
+    x, wg, wu = rnd(3, rows, cin), rnd(4, cin, cout), rnd(5, cin, cout)
+    x[1, 5], x[rows - 1, 9] = math.inf, -math.inf
+    xd, gd, ud = x.to(dt).cuda(), wg.to(dt).cuda(), wu.to(dt).cuda()
+    h, kept = torch.empty(rows, cout, dtype=dt, device="cuda"), torch.empty(2, rows, cout, dtype=dt, device="cuda")
+    F.ftp_gated_forward(xd, gd, ud, h, act=F.ACT_RELU, stash=kept)
+    g, u = ref(xd) @ ref(gd), ref(xd) @ ref(ud)
+    same_kinds(kept, torch.stack((g, u)))
+    same_kinds(h, act(g, "relu") * u)
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(5, 200, 72), (140, 200, 72), (300, 1100, 900), (1100, 72, 2104)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("eight", [0, 1])
+def test_infinities_pass_through_the_gradients(rows, cin, cout, dt, eight):
+    x, w, dy = rnd(6, rows, cin), rnd(7, cin, cout), rnd(8, rows, cout)
+    dy[2, 3], dy[4, 30] = math.inf, -math.inf
+    xd, wd, dyd = x.to(dt).cuda(), w.to(dt).cuda(), dy.to(dt).cuda()
+    xin, xv = xd, ref(xd)
+    if eight:                                                                # one plane against three
+        xin, back = torch.empty(F.ftp_checkpoint_bytes(rows, cin), dtype=torch.uint8, device="cuda"), torch.empty_like(xd)
+        F.ftp_checkpoint_pack(xd, xin)
+        F.ftp_checkpoint_unpack(xin, back)
+        xv = ref(back)
+    dx, dw = torch.empty_like(xd), torch.empty_like(wd)
+    F.ftp_linear_backward(xin, wd, dyd, dx=dx, dw=dw)
+    same_kinds(dx, ref(dyd) @ ref(wd).T)
+    same_kinds(dw, xv.T @ ref(dyd))
