@@ -24,13 +24,16 @@ __device__ __forceinline__ float phi_fast(float z, float e) {
     return z > 0.f ? 1.f - q : q;
 }
 
+// For float tensors: from erfc, whose error is relative; 0.5 + 0.5 erf cancels for negative z (4 % of the result at z = -5).
+__device__ __forceinline__ float phi_exact(float z) { return 0.5f * erfcf(z * -0.70710678118654752f); }
+
 // NaN passes through every branch.
 template <bool FAST>
 __device__ __forceinline__ float act_value(float z, int act) {
     switch (act) {
         case FTP_ACT_RELU: return z < 0.f ? 0.f : z;
         case FTP_ACT_RELU6: return z < 0.f ? 0.f : (z > 6.f ? 6.f : z);
-        case FTP_ACT_GELU: return z * (FAST ? phi_fast(z, ex2_fast(z * z * (-0.5f * LOG2E))) : 0.5f + 0.5f * erff(z * 0.70710678118654752f));
+        case FTP_ACT_GELU: return z * (FAST ? phi_fast(z, ex2_fast(z * z * (-0.5f * LOG2E))) : phi_exact(z));
         case FTP_ACT_SILU: return z * sigmoid_t<FAST>(z);
         default: return z;
     }
@@ -41,7 +44,7 @@ __device__ __forceinline__ void act_both(float z, int act, float& v, float& d) {
         case FTP_ACT_RELU: v = z < 0.f ? 0.f : z; d = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z); break;
         case FTP_ACT_RELU6: v = z < 0.f ? 0.f : (z > 6.f ? 6.f : z); d = z > 0.f && z < 6.f ? 1.f : (z == z ? 0.f : z); break;
         case FTP_ACT_GELU: {
-            const float e = FAST ? ex2_fast(z * z * (-0.5f * LOG2E)) : expf(-0.5f * z * z), p = FAST ? phi_fast(z, e) : 0.5f + 0.5f * erff(z * 0.70710678118654752f);
+            const float e = FAST ? ex2_fast(z * z * (-0.5f * LOG2E)) : expf(-0.5f * z * z), p = FAST ? phi_fast(z, e) : phi_exact(z);
             v = z * p;
             // for |z| beyond 14 the density is 0 in float; z * 0 at z = +-inf would be NaN
             d = p + (fabsf(z) > 14.f ? 0.f : z * e * 0.39894228040143268f);

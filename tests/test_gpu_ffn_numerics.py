@@ -1,10 +1,11 @@
-"""Values of the feed-forward operators where an elementwise worst-case bound says nothing: infinities."""
+"""Values of the feed-forward operators where an elementwise worst-case bound says nothing: infinities, the
+far ends of the activations."""
 import math
 
 import pytest
 import torch
 
-from ffn_helpers import ACTS, act
+from ffn_helpers import ACTS, act, dact
 
 pytestmark = pytest.mark.gpu
 F = pytest.importorskip("paper_2110_02781_b200")
@@ -74,3 +75,26 @@ def test_infinities_pass_through_the_gradients(rows, cin, cout, dt, eight):
     F.ftp_linear_backward(xin, wd, dyd, dx=dx, dw=dw)
     same_kinds(dx, ref(dyd) @ ref(wd).T)
     same_kinds(dw, xv.T @ ref(dyd))
+
+
+# ---- GELU far from zero -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [3, 130])
+def test_float_gelu_holds_its_accuracy_for_negative_values(rows):
+    # z = x w with w the identity, exact.  Phi(z) = erfc(-z / sqrt 2) / 2: the argument is off by 2^-23 relative, which erfc turns
+    # into (z^2 + 1) 2^-23 of its value, erfc itself by 4 steps and the product by one: (z^2 + 6) 2^-23 of the result.
+    n = 64
+    z = torch.linspace(-11.5, 9.0, rows * n, dtype=torch.float64).view(rows, n).float().cuda()
+    eye = torch.eye(n, device="cuda")
+    y, kept, dx = torch.empty_like(z), torch.empty_like(z), torch.empty_like(z)
+    F.ftp_linear_forward(z, eye, y, act=F.ACT_GELU, stash=kept)
+    assert torch.equal(kept, z)
+    want = act(ref(z), "gelu")
+    over = (ref(y) - want).abs() / ((ref(z) ** 2 + 6) * 2.0 ** -23 * want.abs()).clamp(min=2.0 ** -149)
+    assert over.max() <= 1, (float(over.max()), float(ref(z).flatten()[over.argmax()]))
+    # the derivative Phi + z phi: exp(-z^2 / 2) is off by (z^2 / 2 + 2) 2^-23 and both terms by two roundings, on the sum of the
+    # magnitudes; its three planes hold it exactly
+    F.ftp_linear_backward(None, eye, torch.ones_like(z), dx=dx, act=F.ACT_GELU, stash=kept)
+    v = ref(z)
+    size = 0.5 * torch.special.erfc(-v / math.sqrt(2)) + (v * torch.exp(-v * v / 2)).abs() / math.sqrt(2 * math.pi)
+    over = (ref(dx) - dact(v, "gelu")).abs() / ((v ** 2 + 8) * 2.0 ** -23 * size)
+    assert over.max() <= 1, (float(over.max()), float(v.flatten()[over.argmax()]))
