@@ -446,8 +446,8 @@ __device__ __forceinline__ void act_both8(const float (&z)[8], int act, float (&
 
 // linear: dz = dy act'(z).  gated: dg = dy u act'(g), du = dy act(g).  KIND: form of z or of g and u (STASH_NONE: the
 // gradient passes unchanged).  A thread keeps eight columns and walks down rows_per_block / 8 rows, R of them in flight,
-// so the column sums of dz cost registers only; they are added up in float over at most rows_per_block values and then
-// across blocks in double, in a fixed order.  With one row in flight 2.3 TB/s at 8192 x 12288 bf16.
+// so the column sums of dz cost registers only; they are added up in float over at most 64 values and then across warps and
+// block rows in double, in a fixed order.  With one row in flight 2.3 TB/s at 8192 x 12288 bf16.
 template <typename T, bool GATED, int KIND, bool VEC>
 __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradArgs p, const __grid_constant__ Jobs jobs) {
     grid_dep_sync();
@@ -516,10 +516,10 @@ __global__ void __launch_bounds__(256) grad_kernel(const __grid_constant__ GradA
         __syncthreads();
         const int col = bx * 256 + threadIdx.x;
         if (col < p.cols) {
-            float s = 0.f;
+            double s = 0.0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += red[k][threadIdx.x];
-            p.sums[(long long)by * p.cols + col] = s;
+            for (int k = 0; k < 8; ++k) s += (double)red[k][threadIdx.x];
+            p.sums[(long long)by * p.cols + col] = (float)s;
         }
     }
 }
@@ -702,9 +702,14 @@ ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, c
     return run_product(p, st, who);
 }
 
-constexpr int GRAD_ROWS = 64, GRAD_CHUNKS = 1024;
+// Rows of a block row, an eighth of them to a thread: up to 1024 block rows of 64 rows, then longer ones, but never more than 64
+// float additions in a sum (rounding errors of terms of one sign add up: 1.3e-5 of the result with 8192 rows a block row).
+constexpr int GRAD_ROWS = 64, GRAD_CHUNKS = 1024, GRAD_MOST = 8 * 64;
 // up to 256 rows in one block row, whose sums then are the bias gradient (a launch less)
-int grad_rows_per_block(long long rows) { return rows <= 256 ? 256 : (int)std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8); }
+int grad_rows_per_block(long long rows) {
+    if (rows <= 256) return 256;
+    return (int)std::min<long long>(GRAD_MOST, std::max<long long>(GRAD_ROWS, (rows + GRAD_CHUNKS * 8 - 1) / (GRAD_CHUNKS * 8) * 8));
+}
 // without a bias gradient: enough blocks to fill the GPU four times over, 16 rows at least (246 x 576 x 1454 bf16 backward:
 // 41 instead of 20 us with all rows in one block row)
 int grad_rows_per_block(long long rows, long long cols) {

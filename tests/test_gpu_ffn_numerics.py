@@ -1,5 +1,5 @@
 """Values of the feed-forward operators where an elementwise worst-case bound says nothing: infinities, the
-far ends of the activations."""
+far ends of the activations, long sums."""
 import math
 
 import pytest
@@ -14,6 +14,10 @@ BF, FP = torch.bfloat16, torch.float32
 
 def rnd(seed, *shape):
     return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def positive(seed, *shape):
+    return 0.5 + torch.rand(*shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
 
 
 def ref(t):
@@ -98,3 +102,15 @@ def test_float_gelu_holds_its_accuracy_for_negative_values(rows):
     size = 0.5 * torch.special.erfc(-v / math.sqrt(2)) + (v * torch.exp(-v * v / 2)).abs() / math.sqrt(2 * math.pi)
     over = (ref(dx) - dact(v, "gelu")).abs() / ((v ** 2 + 8) * 2.0 ** -23 * size)
     assert over.max() <= 1, (float(over.max()), float(v.flatten()[over.argmax()]))
+
+
+# ---- long sums --------------------------------------------------------------------------------------------------------------
+def test_bias_gradient_of_a_very_long_batch():
+    # a column of one value each: rounding errors of a float sum do not cancel.  64 additions or fewer in float, the rest in double
+    rows, cout = 1 << 23, 24
+    c = positive(17, cout).float().cuda()
+    dy = c.expand(rows, cout).contiguous()
+    db = torch.empty(cout, device="cuda")
+    F.ftp_linear_backward(None, torch.zeros(8, cout, device="cuda"), dy, dbias=db)
+    err = (ref(db) / (rows * ref(c)) - 1).abs().max()
+    assert err <= 68 * 2.0 ** -24, float(err)
