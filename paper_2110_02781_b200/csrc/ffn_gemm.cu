@@ -220,7 +220,7 @@ ftp_status tile_typed(const Product& p, KArgs& k, int S, cudaStream_t st, const 
 // cluster and its exchange, and what reading the operands from memory takes at the rate the form reaches.  A wave is 74
 // pairs, 148 CTAs or twice that; clusters of four and eight do not fill every group of SMs.
 struct Form { bool pair; int cols, S; double cost; };
-static Form choose_form(const KArgs& k, const Product& p) {
+static Form choose_form(KArgs& k, const Product& p) {
     const bool f32 = p.out_f32 && k.np > 1;
     const int gated = p.epi == EPI_GATED ? 2 : 1;
     const double blocks = (double)k.kb_part * k.parts_k;
@@ -266,6 +266,14 @@ static Form choose_form(const KArgs& k, const Product& p) {
         tile(128, 0.325, 0.6, 4.2, 6.0);
         if (gated == 1) tile(64, 0.253, 0.36, 3.8, 4.7);
     }
+    if (!p.out_f32 && blocks > (double)LONG_SUM * best.S) {          // too long a sum for the accumulator: pairs that empty it
+        best.cost = 1e30;
+        const double n = tiles(256, 128);
+        for (int S = 1; S <= 4; ++S)
+            if (S == 1 || n * S <= (S == 2 ? 66 : S == 3 ? 60 : 52)) take({true, 128, S, pair_share[S] + 0.15 * std::ceil(blocks / S) * std::ceil(n * S / 74)});
+        k.long_sum = 1;
+        k.chunk = LONG_CHUNK;
+    }
     return best;
 }
 
@@ -275,9 +283,9 @@ ftp_status run_product(const Product& p, cudaStream_t st, const char* who) {
     k.M = p.M; k.N = p.N; k.err = p.err;
     k.pa = p.A[0].planes; k.pb = p.B[0].planes;
     k.np = std::max(k.pa, k.pb);
-    k.chunk = CHUNK;
     k.kb_part = (int)((p.K + BK - 1) / BK);
     k.parts_k = (p.parts > 1 && p.cat_k) ? 2 : 1;
+    k.chunk = CHUNK;
     k.parts_n = (p.parts > 1 && !p.cat_k && p.epi != EPI_GATED) ? 2 : 1;
     const Form f = choose_form(k, p);
     if (f.pair) return run_product_pair(p, k, f.cols == 256, f.S, st, who);

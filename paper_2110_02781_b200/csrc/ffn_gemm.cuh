@@ -19,6 +19,10 @@ constexpr int BK = 64;                       // reduction elements per stage: on
 // steps (measured 3.5e-5 of the result after 2048 steps of 16 elements).  So the products of the main planes have an
 // accumulator of their own, and every CHUNK blocks both are emptied into registers, which add with rounding.
 constexpr int CHUNK = 4;
+// bf16 results stay in the accumulator up to LONG_SUM blocks a slice (131072 terms): for terms of one sign that costs about 2^-24
+// of the result per step, 1/8 of bf16's half step at that length and twice the half step for 8M terms in eight slices.  Longer
+// slices are emptied every LONG_CHUNK blocks (200000 x 2048 x 2048 weight gradient: 1411 instead of 1118 us).
+constexpr int LONG_SUM = 2048, LONG_CHUNK = 64;
 
 struct KArgs {
     Epi e[2];
@@ -28,7 +32,8 @@ struct KArgs {
     int parts_n;                             // 2: the column tiles of output 1 follow those of output 0
     int tiles_m, tiles_n;                    // column tiles of one output
     int pa, pb, np;                          // planes of A and of B, the larger of the two
-    int chunk;                               // blocks per accumulation in the tensor cores (float results)
+    int chunk;                               // blocks per accumulation in the tensor cores (float results, long_sum)
+    int long_sum;                            // a bf16 result whose slices are longer than LONG_SUM blocks
     int* err;
 };
 

@@ -438,13 +438,13 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_pair_kernel(const __grid_
 // Several pairs of a cluster share a 256 x 128 tile's reduction, for products with too few tiles for all pairs: every CTA
 // leaves its 128 rows of partial sums in shared memory (the ring is free by then), and the CTAs that hold the same rows add
 // and finish every S-th of them each (finish_rows): 1024 x 1024 x 1024 float 22 instead of 28 us, 512 x 11008 x 512 bf16 15
-// instead of 30.
-template <typename T, bool AMN, bool BMN, int EPI>
+// instead of 30.  CHUNKED: the accumulator is emptied into registers every p.chunk blocks: float results, and long reductions of
+// bf16 ones (see LONG_SUM).
+template <typename T, bool AMN, bool BMN, int EPI, bool CHUNKED>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) ffn_split_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__ CUtensorMap mapA1,
                                                                     const __grid_constant__ CUtensorMap mapB0, const __grid_constant__ CUtensorMap mapB1,
                                                                     const __grid_constant__ KArgs p) {
     constexpr int BN = 128, STAGES = PAIR_STAGES<BN>, WC = BN / 2, PITCH = BN + 4;
-    constexpr bool CHUNKED = sizeof(T) == 4;
     constexpr int BUFS = CHUNKED ? 2 : 1;
     constexpr uint32_t SLAB = 64 * BK * 2, A_BYTES = 128 * BK * 2, B_BYTES = BN / 2 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
     constexpr uint32_t ACC = CHUNKED ? 2 * BN : BN, TMEM_COLS = BUFS * ACC;
@@ -592,11 +592,11 @@ ftp_status launch_either(const Product& p, const KArgs& k, cudaStream_t st, cons
     }
     return even ? launch_pair<T, BN, AMN, BMN, EPI, true>(p, k, st, who) : launch_pair<T, BN, AMN, BMN, EPI, false>(p, k, st, who);
 }
-template <typename T, bool AMN, bool BMN, int EPI>
+template <typename T, bool AMN, bool BMN, int EPI, bool CHUNKED = sizeof(T) == 4>
 ftp_status launch_split(const Product& p, const KArgs& k, int S, cudaStream_t st, const char* who) {
     Maps m;
     FTP_REQUIRE(make_maps(m, p, 128, 64), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
-    auto kern = ffn_split_kernel<T, AMN, BMN, EPI>;
+    auto kern = ffn_split_kernel<T, AMN, BMN, EPI, CHUNKED>;
     constexpr uint32_t SMEM = PAIR_RING<128> + 1024;
     static std::atomic<unsigned long long> asked{0};
     cudaError_t e = allow_smem(asked, kern, (int)SMEM);
@@ -610,6 +610,7 @@ template <int BN, bool AMN, bool BMN, int EPI>
 ftp_status pair_typed(const Product& p, const KArgs& k, int S, cudaStream_t st, const char* who) {
     if constexpr (BN == 128) {                                       // 256 float sums per thread row do not fit into registers
         if (p.out_f32) return S > 1 ? launch_split<float, AMN, BMN, EPI>(p, k, S, st, who) : launch_either<float, BN, AMN, BMN, EPI>(p, k, st, who);
+        if (k.long_sum) return launch_split<__nv_bfloat16, AMN, BMN, EPI, true>(p, k, S, st, who);
         if (S > 1) return launch_split<__nv_bfloat16, AMN, BMN, EPI>(p, k, S, st, who);
     }
     return launch_either<__nv_bfloat16, BN, AMN, BMN, EPI>(p, k, st, who);

@@ -114,3 +114,52 @@ def test_bias_gradient_of_a_very_long_batch():
     F.ftp_linear_backward(None, torch.zeros(8, cout, device="cuda"), dy, dbias=db)
     err = (ref(db) / (rows * ref(c)) - 1).abs().max()
     assert err <= 68 * 2.0 ** -24, float(err)
+
+
+def test_bf16_weight_gradient_of_a_very_long_batch():
+    # terms of one sign: what the accumulator of the tensor cores cuts adds up.  Half a step of bf16 and 2^-14 for the sum
+    rows, cin, cout = 1 << 23, 64, 72
+    g = torch.Generator(device="cuda").manual_seed(18)
+    make = lambda n: (0.5 + torch.rand(rows, n, generator=g, device="cuda")).to(BF)  # noqa: E731
+    x, dy = make(cin), make(cout)
+    dw = torch.empty(cin, cout, dtype=BF, device="cuda")
+    F.ftp_linear_backward(x, torch.zeros(cin, cout, dtype=BF, device="cuda"), dy, dw=dw)
+    want = sum(x[a:a + (1 << 20)].double().T @ dy[a:a + (1 << 20)].double() for a in range(0, rows, 1 << 20))
+    err = ((dw.double() - want) / want).abs().max()
+    assert err <= 2.0 ** -8 + 2.0 ** -14, float(err)
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(40, 1100000, 72), (300, 1100000, 392), (700, 300000, 1032), (700, 140000, 2304), (130, 70000, 72)])
+def test_bf16_products_over_long_reductions(rows, cin, cout):
+    # Sums too long for the accumulator, on one to four pairs a tile: forward, gated, input gradient (over cout), weight gradient
+    # (over rows).  A chunk is 256 steps, which cut at most 2^-23 of its magnitudes each; 300 float additions at most: 2^-14.
+    g = torch.Generator(device="cuda").manual_seed(19)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)  # noqa: E731
+    x, w, w2, res = make(rows, cin), make(cin, cout), make(cin, cout), make(rows, cout)
+    new = lambda *s: torch.empty(*s, dtype=BF, device="cuda")  # noqa: E731
+
+    def check(got, want, size, err=2.0 ** -14):
+        over = (got.double() - want).abs() - (2.0 ** -8 + 2.0 ** -20) * want.abs() - err * size
+        assert over.max() <= 0, float(over.max())
+    xd = x.double()
+    a, b, size = xd @ w.double(), xd @ w2.double(), xd.abs() @ torch.maximum(w.abs(), w2.abs()).double()
+    y, h, kept = new(rows, cout), new(rows, cout), new(2, rows, cout)
+    F.ftp_linear_forward(x, w, y, residual=res)
+    check(y, a + res.double(), size)
+    F.ftp_gated_forward(x, w, w2, h, act=F.ACT_NONE, stash=kept)
+    check(kept[0], a, size)
+    check(kept[1], b, size)
+    check(h, a * b, size * (a.abs() + b.abs() + 2.0 ** -14 * size))
+    # the same numbers as gradients: dx = dy w^T + addend, dw = x^T dy
+    dx, dw = new(rows, cout), new(rows, cout)
+    F.ftp_linear_backward(None, w.T.contiguous(), x, dx=dx, dx_addend=res)
+    check(dx, a + res.double(), size)
+    xt = x.T.contiguous()
+    F.ftp_linear_backward(xt, res, w, dw=dw)
+    check(dw, a, size)
+    # dg = dh u and du = dh g with dh = g = w and u = w2: products of bf16 values, rounded to bf16 once more before the product
+    grads = new(2, rows, cout)
+    F.ftp_gated_backward(xt, res, res, w, dw_gate=grads[0], dw_up=grads[1], act=F.ACT_NONE, stash=torch.stack((w, w2)))
+    for got, d in zip(grads, (w.double() * w2.double(), w.double() ** 2)):
+        check(got, xd @ d.to(BF).double(), xd.abs() @ d.abs())
+    F.ftp_check_op_status()
