@@ -439,11 +439,11 @@ ftp_status ftp_linear_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, s
 ftp_status ftp_gated_workspace_bytes(const ftp_ffn_desc* d, int32_t backward, size_t* bytes);
 
 /* z = x w + bias;  y = act(z) + residual;  z is kept in `stash` (rows x cout) as d->stash says.
- * bias, residual: nullable.  residual may be y. */
+ * bias, residual: nullable.  residual may be y, with its pitch. */
 ftp_status ftp_linear_forward(const ftp_ffn_desc* d, const void* x, const void* w, const float* bias, const void* residual, void* y,
                               void* stash, void* ws, size_t ws_bytes, void* stream);
 /* dz = dy * act'(z);  dx = dz w^T + dx_addend;  dw = x^T dz;  dbias = column sums of dz.  (The residual's gradient is dy.)
- * Each of dx, dw, dbias may be NULL; dx_addend (a gradient that reaches x another way) is nullable and may be dx.
+ * Each of dx, dw, dbias may be NULL; dx_addend (a gradient that reaches x another way) is nullable and may be dx, with its pitch.
  * stash: the kept values (NULL iff act is FTP_ACT_NONE).  dz is rounded to bf16 once before the products when precision
  * is FTP_BF16; dbias is summed from the unrounded values. */
 ftp_status ftp_linear_backward(const ftp_ffn_desc* d, const void* x, const void* w, const void* stash, const void* dy, const void* dx_addend,

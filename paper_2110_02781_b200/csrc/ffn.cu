@@ -651,6 +651,11 @@ ftp_status check_addresses(std::initializer_list<const void*> outs, std::initial
     }
     return FTP_OK;
 }
+// An addend may be the result itself, element by element: with another pitch a row would be read after it was overwritten.
+ftp_status check_in_place(const void* add, const void* out, int64_t ldadd, int64_t ldout, int64_t rows, int32_t cols, const char* who) {
+    FTP_REQUIRE(!add || add != out || rows == 1 || (ldadd ? ldadd : cols) == (ldout ? ldout : cols), FTP_EINVAL, "%s: an addend in place of its result with another pitch", who);
+    return FTP_OK;
+}
 ftp_status check_elements(std::initializer_list<const void*> all, size_t bytes, const char* who) {
     for (const void* p : all) FTP_REQUIRE(aligned(p, bytes), FTP_ERANGE, "%s: an address is not a multiple of its elements' size", who);
     return FTP_OK;
@@ -854,6 +859,7 @@ ftp_status check_and_forward(const ftp_ffn_desc* d, const void* x, const void* w
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
     if (ftp_status s = check_addresses({y, stash}, {x, w0, w1, bias}, who)) return s;
     if (ftp_status s = check_addresses({stash}, {residual}, who)) return s;
+    if (ftp_status s = check_in_place(residual, y, d->ldr, d->ldy, d->rows, d->cout, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
     const ftp_status s = d->precision == FTP_FP32 ? forward<float, GATED>(d, x, w, bias, residual, y, d->stash, stash, real, err, st, who)
@@ -884,6 +890,7 @@ ftp_status check_and_backward(const ftp_ffn_desc* d, const void* x, const void* 
     if (ftp_status s = check_ws(c, ws, ws_bytes, who)) return s;
     if (ftp_status s = check_addresses({dx, dw0, dw1, dbias}, {x, w0, w1, stash, dy}, who)) return s;
     if (ftp_status s = check_addresses({dw0, dw1, dbias}, {addend}, who)) return s;
+    if (ftp_status s = check_in_place(addend, dx, d->ldr, d->lddx, d->rows, d->cin, who)) return s;
     Carve real{static_cast<char*>(ws) + (ws ? 0 : 256), 0, ws_bytes};
     const void* w[2] = {w0, w1};
     const ftp_status s = d->precision == FTP_FP32 ? backward<float, GATED>(d, x, w, stash, dy, addend, dx, dw, dbias, real, err, st, who)

@@ -147,3 +147,13 @@ def test_a_folded_batch_norm_is_no_residual_source(precision):
         with pytest.raises(F.FtpError) as e:
             F.ftp_workspace_bytes(folded + reader + tail, cfg)
         assert e.value.status == 7
+
+
+def test_an_addend_in_place_has_the_pitch_of_its_result():
+    # residual == y and dx_addend == dx are allowed element by element: with another pitch a row would be added after it was overwritten
+    ref, L, P, Q, W = C.byref, F.lib, FAKE, FAKE + 4096, FAKE + 8192
+    for kw in (dict(ldr=64), dict(ldy=64), dict(ldy=64, ldr=48)):
+        assert L.ftp_linear_forward(ref(desc(**kw)), P, P, None, Q, Q, None, None, 0, None) == 1, kw
+    for kw in (dict(ldr=80), dict(lddx=80), dict(lddx=80, ldr=64)):
+        assert L.ftp_linear_backward(ref(desc(**kw)), None, P, None, P, Q, Q, None, None, W, 1 << 30, None) == 1, kw
+        assert L.ftp_gated_backward(ref(desc(stash=1, **kw)), None, P, P, P, P, Q, Q, None, None, W, 1 << 30, None) == 1, kw

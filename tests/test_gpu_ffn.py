@@ -644,3 +644,27 @@ def test_calls_from_several_threads_at_once():
     F.ftp_check_op_status()
     assert not failed, failed
     assert len(got) == len(cases) and all(torch.equal(a, b) for (t, i), r in got.items() for a, b in zip(r, want[i]))
+
+
+def test_an_addend_in_place_keeps_gaps_and_refuses_another_pitch():
+    rows, cin, cout = 130, 72, 200
+    x, w = linear_case(400, rows, cin, cout, BF, 0, 0)
+    r, a = rnd(401, rows, cout), rnd(402, rows, cin)
+    y, inplace = torch.empty(rows, cout, dtype=BF, device="cuda"), Guarded(rows, cout, BF, 24, fill=r)
+    F.ftp_linear_forward(x, w, y, residual=dev(r, BF), act=F.ACT_SILU)
+    F.ftp_linear_forward(x, w, inplace.t, residual=inplace.t, act=F.ACT_SILU)
+    dx, din = torch.empty(rows, cin, dtype=BF, device="cuda"), Guarded(rows, cin, BF, 16, fill=a)
+    F.ftp_linear_backward(None, w, y, dx=dx, dx_addend=dev(a, BF))
+    F.ftp_linear_backward(None, w, y, dx=din.t, dx_addend=din.t)
+    assert torch.equal(y, inplace.t) and torch.equal(dx, din.t) and inplace.untouched() and din.untouched()
+    wide = torch.zeros(2 * rows, cout, dtype=BF, device="cuda")
+    every_other, packed = wide.view(rows, 2 * cout)[:, :cout], wide[:rows]           # the same first row, other rows elsewhere
+    for res, out in ((every_other, packed), (packed, every_other)):
+        with pytest.raises(F.FtpError):
+            F.ftp_linear_forward(x, w, out, residual=res)
+    wide = torch.zeros(2 * rows, cin, dtype=BF, device="cuda")
+    with pytest.raises(F.FtpError):
+        F.ftp_linear_backward(None, w, y, dx=wide[:rows], dx_addend=wide.view(rows, 2 * cin)[:, :cin])
+    one = torch.zeros(1, cout, dtype=BF, device="cuda")
+    F.ftp_linear_forward(x[:1], w, one, residual=torch.as_strided(one, (1, cout), (2 * cout, 1)))       # one row has no pitch
+    F.ftp_check_op_status()
