@@ -168,3 +168,18 @@ def test_schedule_helpers_match_the_oracle():
             assert F.ftp_is_replication_iter(it, period) == (oracle.is_replication_iter(it, period) if it >= 0 else False)
     assert [it + 1 for it in range(450) if F.ftp_is_repartition_iter(it)] == [10, 100, 200, 300, 400]
     assert F.ftp_is_repartition_iter(6, 7, 5) and F.ftp_is_repartition_iter(9, 7, 5) and not F.ftp_is_repartition_iter(7, 7, 5)
+
+
+def test_a_name_replaced_in_the_binding_is_replaced_in_the_package(monkeypatch):
+    from paper_2110_02781_b200 import ftpipe
+    first = F.ftp_checkpoint_bytes
+    assert F.ftp_checkpoint_bytes is first and F.ACT_SILU == 4              # handed out, and handed out again
+    with monkeypatch.context() as m:
+        m.setattr(ftpipe, "ftp_checkpoint_bytes", lambda *a: 7)
+        m.setattr(ftpipe, "ACT_SILU", 44)
+        assert F.ftp_checkpoint_bytes(1, 1) == 7 and F.ACT_SILU == 44
+        m.delattr(ftpipe, "ftp_checkpoint_bytes")
+        with pytest.raises(AttributeError):
+            F.ftp_checkpoint_bytes
+    assert F.ftp_checkpoint_bytes is first and F.ACT_SILU == 4
+    assert F.__name__ == "paper_2110_02781_b200" and F.build.__name__.endswith(".build")
