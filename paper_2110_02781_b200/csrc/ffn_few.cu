@@ -419,30 +419,36 @@ bool make_ring_map(CUtensorMap* map, const void* base, long long cols, long long
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int MR, int CW>
+dim3 few_grid(const FewArgs& a, int S) { return dim3((unsigned)((a.N + CW - 1) / CW * S), (unsigned)((a.rows + MR - 1) / MR)); }
+
+template <typename T, int MR, int P>
+ftp_status launch_ring(const FewArgs& a, int S, cudaStream_t st, const char* who) {
+    constexpr int CW = 8 * Wide<T>::V, V = 16 / (int)sizeof(T), B = 128 / (int)sizeof(T);
+    CUtensorMap m0, m1, mx;
+    const long long ldx = a.rows == 1 ? (a.K + V - 1) / V * V : a.ldx;       // one row: never stepped over
+    FTP_REQUIRE(make_ring_map<T>(&m0, a.w[0], a.N, a.K, a.ldw, B, RING_ROWS<P>) && (P == 1 || make_ring_map<T>(&m1, a.w[1], a.N, a.K, a.ldw, B, RING_ROWS<P>)) &&
+                    make_ring_map<T>(&mx, a.x, a.K, a.rows, ldx, RING_ROWS<P>, MR), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
+    if (P == 1) m1 = m0;
+    static_assert(FEW_WARPS * P * MR * CW * 4 <= RING_BYTES / 2, "the warps' sums reuse the ring");
+    auto kern = ffn_few_ring_kernel<T, MR, P>;
+    static std::atomic<unsigned long long> asked{0};
+    cudaError_t e = allow_smem(asked, kern, RING_BYTES + 128);
+    if (e == cudaSuccess) e = launch_cluster(kern, few_grid<MR, CW>(a, S), RING_THREADS, RING_BYTES + 128, S, st, m0, m1, mx, a);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+
 template <typename T, int MR, int P>
 ftp_status launch_few(const FewArgs& a, int S, cudaStream_t st, const char* who) {
+    if constexpr (sizeof(T) == 4 || MR <= 2)                         // four bf16 tokens come with at most 4 MB of w (few_tokens)
+        if (a.ring) return launch_ring<T, MR, P>(a, S, st, who);
     constexpr int CW = 8 * Wide<T>::V;
-    const dim3 grid((unsigned)((a.N + CW - 1) / CW * S), (unsigned)((a.rows + MR - 1) / MR));
-    cudaError_t e;
-    if (a.ring) {
-        constexpr int V = 16 / (int)sizeof(T), B = 128 / (int)sizeof(T);
-        CUtensorMap m0, m1, mx;
-        const long long ldx = a.rows == 1 ? (a.K + V - 1) / V * V : a.ldx;       // one row: never stepped over
-        FTP_REQUIRE(make_ring_map<T>(&m0, a.w[0], a.N, a.K, a.ldw, B, RING_ROWS<P>) && (P == 1 || make_ring_map<T>(&m1, a.w[1], a.N, a.K, a.ldw, B, RING_ROWS<P>)) &&
-                        make_ring_map<T>(&mx, a.x, a.K, a.rows, ldx, RING_ROWS<P>, MR), FTP_ECUDA, "%s: cannot describe an operand to the copy engine", who);
-        if (P == 1) m1 = m0;
-        static_assert(FEW_WARPS * P * MR * CW * 4 <= RING_BYTES / 2, "the warps' sums reuse the ring");
-        auto kern = ffn_few_ring_kernel<T, MR, P>;
-        static std::atomic<unsigned long long> asked{0};
-        e = allow_smem(asked, kern, RING_BYTES + 128);
-        if (e == cudaSuccess) e = launch_cluster(kern, grid, RING_THREADS, RING_BYTES + 128, S, st, m0, m1, mx, a);
-    } else {
-        const size_t x_bytes = (size_t)FEW_PITCH<MR> * a.kper * 4, red_bytes = (size_t)FEW_WARPS * P * MR * CW * 4;
-        auto kern = a.vec_w ? ffn_few_kernel<T, MR, P, true> : ffn_few_kernel<T, MR, P, false>;
-        static std::atomic<unsigned long long> asked[2] = {};
-        e = allow_smem(asked[a.vec_w ? 1 : 0], kern, FEW_SMEM);
-        if (e == cudaSuccess) e = launch_cluster(kern, grid, FEW_THREADS, std::max(x_bytes, red_bytes), S, st, a);
-    }
+    const size_t x_bytes = (size_t)FEW_PITCH<MR> * a.kper * 4, red_bytes = (size_t)FEW_WARPS * P * MR * CW * 4;
+    auto kern = a.vec_w ? ffn_few_kernel<T, MR, P, true> : ffn_few_kernel<T, MR, P, false>;
+    static std::atomic<unsigned long long> asked[2] = {};
+    cudaError_t e = allow_smem(asked[a.vec_w ? 1 : 0], kern, FEW_SMEM);
+    if (e == cudaSuccess) e = launch_cluster(kern, few_grid<MR, CW>(a, S), FEW_THREADS, std::max(x_bytes, red_bytes), S, st, a);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
@@ -455,7 +461,8 @@ ftp_status few_rows(const FewArgs& a, int S, cudaStream_t st, const char* who) {
             if (a.rows > 8) return launch_few<T, 16, P>(a, S, st, who);
         if (a.rows > 4) return launch_few<T, 8, P>(a, S, st, who);
     }
-    return launch_few<T, 4, P>(a, S, st, who);
+    if constexpr (sizeof(T) == 4 || P == 1) return launch_few<T, 4, P>(a, S, st, who);
+    return fail(FTP_EUNSUPPORTED, "%s: no few-token form for %d tokens", who, a.rows);   // few_tokens sends none
 }
 
 // bytes of shared memory that the tokens of a group take beside `k` rows of w

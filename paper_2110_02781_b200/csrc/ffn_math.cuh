@@ -10,7 +10,6 @@ namespace ffn {
 __device__ __forceinline__ float rcp_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float ex2_fast(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 constexpr float LOG2E = 1.4426950408889634f;
-template <bool FAST> __device__ __forceinline__ float exp_t(float x) { return FAST ? ex2_fast(x * LOG2E) : expf(x); }
 template <bool FAST> __device__ __forceinline__ float sigmoid_t(float z) {
     return FAST ? rcp_fast(1.f + ex2_fast(z * -LOG2E)) : 1.f / (1.f + expf(-z));
 }
