@@ -5,7 +5,7 @@ import pytest
 
 import oracle
 import synth
-from helpers import TOL_BF16, TOL_FP32, gpu_step_split, make_gpu, rel_err, to_dev
+from helpers import TOL_BF16, TOL_FP32, clear_batch, gpu_step_split, make_gpu, rel_err, to_dev
 from oracle import schedule as S
 
 pytestmark = pytest.mark.gpu
@@ -173,3 +173,64 @@ def test_captured_step_traces_and_profile():
     for m in (a, b):
         m.ftp_check_guards()
         m.close()
+
+
+def mixed_net():
+    """Token-wise layers among the other kinds: with RELU and RELU6, and residuals from a convolution, a batch norm that a gated
+    block reads too, a linear op (read by an ADD_RESIDUAL), a sum and the unit's input."""
+    K, A, d = synth.KIND, synth.ACT, 20
+    L = lambda unit, kind, cin=d, cout=d, k=0, act="NONE", bias=0, src=-1, pad=0: synth.Layer(unit, K[kind], cin, cout, k, 1, pad, A[act], bias, src)  # noqa: E731
+    ls = [L(0, "CONV1D", 12, d, 3, pad=1, bias=1), L(0, "LINEAR", act="RELU", bias=1, src=0),
+          L(1, "BN"), L(1, "GATED", d, 36, act="RELU6"), L(1, "LINEAR", 36, d, src=2), L(1, "BN"), L(1, "ADD_RESIDUAL", src=4), L(1, "LINEAR", act="RELU6", src=6),
+          L(2, "LINEAR", act="GELU", src=7), L(2, "ACT", act="RELU"), L(2, "GATED", act="RELU"), L(2, "LINEAR", src=9, bias=1),
+          L(3, "GAP"), L(3, "FC", d, 5, 1, bias=1), L(3, "SOFTMAX_CE", 5, 5)]
+    return ls, synth.config(2, 12, 1, 6, 5)
+
+
+@pytest.mark.parametrize("points", [None, [0, 1, 2, 3, 4]])
+def test_residuals_from_layers_of_every_kind(points):
+    ls, cfg = mixed_net()
+    params, state = synth.init_params(73, ls), synth.init_state(ls)
+    probe = oracle.OracleModel(ls, cfg, params, state)
+    x, y, _ = clear_batch(probe, 73, cfg)
+    om = oracle.OracleModel(ls, cfg, params, state)
+    gm = F.Model(ls, cfg)
+    gm.load_params(params, state)
+    pts = points or [0, gm.L]
+    gm.ftp_set_partition(pts)
+    loss = gm.ftp_train_step(to_dev(x), to_dev(y), cfg["lr"])
+    ref = om.step(pts, x, y)
+    assert abs(loss - ref) <= TOL_FP32 * abs(ref)
+    for u in range(gm.L):
+        assert rel_err(gm.ftp_get_tensor(F.T_GRADS, u), om.unit_grads(u)) <= TOL_FP32, u
+        assert rel_err(gm.ftp_get_tensor(F.T_WEIGHTS, u), om.unit_params(u)) <= TOL_FP32, u
+    gm.ftp_check_guards()
+    gm.ftp_check_device_status()
+    gm.close()
+
+
+@pytest.mark.parametrize("kept,precision", [(8, 0), (0, 1), (8, 1)])
+def test_async_pipeline_with_values_kept_in_8_bits(kept, precision):
+    """Several micro-batches in flight.  A kept value next to a rounding border may land on the other side (1/64 of its block's
+    largest): held to the bf16 tolerance, and to the same bits when the run is repeated."""
+    import torch
+    from paper_2110_02781_b200.async_pipeline import AsyncPipeline
+    ls, cfg, params, state = nets(kept, precision, batch=2, tokens=6, in_c=16, d=24, f=40)
+    points, nb = [0, 1, 2, 4], 6
+    op = S.AsyncPipeline(ls, cfg, params, state, points, 1)
+    batches = [synth.make_batch(70, cfg, t) for t in range(nb)]
+    if precision:
+        batches = [(oracle.model.round_bf16(x), y) for x, y in batches]
+    ref = op.run(batches, cfg["lr"])
+    runs = []
+    for _ in range(2):
+        gp = AsyncPipeline(ls, cfg, points, params, state, 1)
+        got = gp.run([(to_dev(x, torch.bfloat16 if precision else None), to_dev(y)) for x, y in batches], cfg["lr"])
+        assert gp.log == op.log
+        for b in range(nb):
+            assert abs(got[b] - ref[b]) <= TOL_BF16 * abs(ref[b]), b
+        for u in range(gp.L):
+            assert rel_err(gp.master.ftp_get_tensor(F.T_WEIGHTS, u), op.master.unit_params(u)) <= TOL_BF16, u
+        runs.append((list(got), [gp.master.ftp_get_tensor(F.T_WEIGHTS, u) for u in range(gp.L)]))
+        gp.close()
+    assert runs[0][0] == runs[1][0] and all(np.array_equal(a, b) for a, b in zip(runs[0][1], runs[1][1]))

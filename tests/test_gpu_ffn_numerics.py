@@ -1,5 +1,5 @@
 """Values of the feed-forward operators where an elementwise worst-case bound says nothing: infinities, the
-far ends of the activations, long sums."""
+far ends of the activations, errors in the norm, sums of one sign, long sums."""
 import math
 
 import pytest
@@ -102,6 +102,55 @@ def test_float_gelu_holds_its_accuracy_for_negative_values(rows):
     size = 0.5 * torch.special.erfc(-v / math.sqrt(2)) + (v * torch.exp(-v * v / 2)).abs() / math.sqrt(2 * math.pi)
     over = (ref(dx) - dact(v, "gelu")).abs() / ((v ** 2 + 8) * 2.0 ** -23 * size)
     assert over.max() <= 1, (float(over.max()), float(v.flatten()[over.argmax()]))
+
+
+# ---- errors in the norm -----------------------------------------------------------------------------------------------------
+# A tile's accumulator takes 16 steps of 16 elements before it is added in float: every step cuts at most 2^-23, half of that on
+# average, of a sum that grows to the chunk's, which makes 5e-7 of the result for terms of one sign and less for random ones;
+# float additions of the chunks and the products left out (2^-24) add 2e-7.  Without the third plane it would be 3.5e-6, with
+# the whole reduction in the accumulator 3e-5 for 1024 steps of one sign.
+NORM = 1e-6
+
+
+def off(got, want):
+    return float((ref(got) - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(8, 9000, 72), (30, 9000, 24), (47, 5000, 68), (130, 16384, 140), (300, 4100, 1100), (1100, 4000, 2051), (200, 1283, 517),
+                                           (2305, 2050, 1025)])
+@pytest.mark.parametrize("make", [rnd, positive])
+def test_float_products_keep_24_bits(rows, cin, cout, make):
+    x, w, dy = make(11, rows, cin).float().cuda(), make(12, cin, cout).float().cuda(), make(13, rows, cout).float().cuda()
+    y, h, kept = torch.empty(rows, cout, device="cuda"), torch.empty(rows, cout, device="cuda"), torch.empty(2, rows, cout, device="cuda")
+    F.ftp_linear_forward(x, w, y)
+    want = ref(x) @ ref(w)
+    assert off(y, want) <= NORM
+    w2 = make(14, cin, cout).float().cuda()
+    F.ftp_gated_forward(x, w, w2, h, act=F.ACT_NONE, stash=kept)
+    up = ref(x) @ ref(w2)
+    assert off(kept[0], want) <= NORM and off(kept[1], up) <= NORM and off(h, want * up) <= 2 * NORM
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    F.ftp_linear_backward(x, w, dy, dx=dx, dw=dw)
+    assert off(dx, ref(dy) @ ref(w).T) <= NORM and off(dw, ref(x).T @ ref(dy)) <= NORM
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(5000, 136, 200), (16384, 130, 70), (9000, 1032, 520)])
+@pytest.mark.parametrize("make", [rnd, positive])
+@pytest.mark.parametrize("dt,eight", [(FP, 0), (FP, 1), (BF, 0)])
+def test_float_weight_gradients_of_long_batches(rows, cin, cout, make, dt, eight):
+    x, dy = make(15, rows, cin).to(dt).cuda(), make(16, rows, cout).to(dt).cuda()
+    w = torch.zeros(cin, cout, dtype=dt, device="cuda")
+    xin, xv = x, ref(x)
+    if eight:
+        xin, back = torch.empty(F.ftp_checkpoint_bytes(rows, cin), dtype=torch.uint8, device="cuda"), torch.empty_like(x)
+        F.ftp_checkpoint_pack(x, xin)
+        F.ftp_checkpoint_unpack(xin, back)
+        xv = ref(back)
+    dw, db = torch.empty(cin, cout, device="cuda"), torch.empty(cout, device="cuda")
+    F.ftp_linear_backward(xin, w, dy, dw=dw, dbias=db)
+    assert off(dw, xv.T @ ref(dy)) <= NORM
+    if make is positive:
+        assert off(db, ref(dy).sum(0)) <= NORM
 
 
 # ---- long sums --------------------------------------------------------------------------------------------------------------
