@@ -668,3 +668,32 @@ def test_an_addend_in_place_keeps_gaps_and_refuses_another_pitch():
     one = torch.zeros(1, cout, dtype=BF, device="cuda")
     F.ftp_linear_forward(x[:1], w, one, residual=torch.as_strided(one, (1, cout), (2 * cout, 1)))       # one row has no pitch
     F.ftp_check_op_status()
+
+
+@pytest.mark.parametrize("rows,cin,cout,gap,off", [(1, 64, 64, 0, 0), (3, 130, 200, 0, 0), (9, 72, 24, 8, 0), (33, 100, 31, 1, 1), (300, 64, 1000, 0, 8), (1000, 330, 1150, 0, 0),
+                                                   (130, 4100, 700, 0, 0)])
+@pytest.mark.parametrize("dt,name,x8,wide", [(BF, "gelu", 0, 1), (BF, "none", 1, 0), (FP, "relu6", 0, 0), (FP, "gelu", 1, 0), (BF, "silu", 1, 1), (FP, "silu", 0, 0)])
+def test_products_computed_again_over_shapes_and_activations(rows, cin, cout, gap, off, dt, name, x8, wide):
+    x, wg = linear_case(410, rows, cin, cout, dt, gap, off)
+    _, wu = linear_case(420, rows, cin, cout, dt, gap, off)
+    dh, add = dev(rnd(430, rows, cout), dt, gap, off), dev(rnd(431, rows, cin), dt, gap, off)
+    xin, xv = x, ref(x)
+    if x8:
+        xin, xv = torch.empty(F.ftp_checkpoint_bytes(rows, cin), dtype=torch.uint8, device="cuda"), through_8_bits(xv)
+        F.ftp_checkpoint_pack(x, xin)
+    dtw = FP if wide else dt
+    dx, dwg, dwu = Guarded(rows, cin, dt, gap, off), Guarded(cin, cout, dtw, gap, off), Guarded(cin, cout, dtw, gap, off)
+    F.ftp_gated_backward(xin, wg, wu, dh, dx=dx.t, dw_gate=dwg.t, dw_up=dwu.t, act=ACTS[name], dx_addend=add)
+    F.ftp_check_op_status()
+    g, u = xv @ ref(wg), xv @ ref(wu)
+    eg, eu = (product_err(xv.abs() @ ref(w).abs(), cin, dt) for w in (wg, wu))
+    eg, eu = eg + HALF[dt] * (g.abs() + eg), eu + HALF[dt] * (u.abs() + eu)       # kept in the tensors' type
+    dg, du, e_g, e_u = gated_bounds(xv, ref(wg), ref(wu), g, u, ref(dh), name, dt, eg, eu)
+    if name == "relu6":                                                             # a g that may lie on either side of a kink
+        near = (g.abs() <= eg) | ((g - 6).abs() <= eg)
+        e_g = e_g + torch.where(near, ref(dh).abs() * (u.abs() + eu), torch.zeros_like(u)) * (1 + HALF[dt])
+    check_gated_grads(xv, ref(wg), ref(wu), dg, du, e_g, e_u, ref(add), dx.t, (dwg.t, dwu.t), dt, dtw, rows, cout)
+    assert dx.untouched() and dwg.untouched() and dwu.untouched()
+    only = Guarded(rows, cin, dt, gap, off)                                        # one gradient alone, laid out alike: the same bits
+    F.ftp_gated_backward(xin, wg, wu, dh, dx=only.t, act=ACTS[name], dx_addend=add)
+    assert torch.equal(only.t, dx.t) and only.untouched()

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from ffn_helpers import ACTS, act, dact
+from ffn_helpers import ACTS, act, dact, product_err
 
 pytestmark = pytest.mark.gpu
 F = pytest.importorskip("paper_2110_02781_b200")
@@ -151,6 +151,21 @@ def test_float_weight_gradients_of_long_batches(rows, cin, cout, make, dt, eight
     assert off(dw, xv.T @ ref(dy)) <= NORM
     if make is positive:
         assert off(db, ref(dy).sum(0)) <= NORM
+
+
+@pytest.mark.parametrize("rows", [8, 140, 1100])
+@pytest.mark.parametrize("size", [-100, -115, -126, -135])
+def test_float_operands_next_to_the_smallest_numbers(rows, size):
+    # three planes end at bf16's smallest number, 2^-133: an operand is off by 2^-134 at most, times what it is multiplied with;
+    # results below 2^-126 by half of 2^-149 more
+    x, w = rnd(23, rows, 200).float(), rnd(24, 200, 300).float()
+    y = torch.empty(rows, 300, device="cuda")
+    for a, b in ((x * 2.0 ** size, w), (x, w * 2.0 ** size)):
+        F.ftp_linear_forward(a.cuda(), b.cuda(), y)
+        a, b = a.double(), b.double()
+        bound = 2.0 ** -134 * (b.abs().sum(0) if a.abs().max() < b.abs().max() else a.abs().sum(1, keepdim=True)) + product_err(a.abs() @ b.abs(), 200, FP) + 2.0 ** -149
+        over = (ref(y) - a @ b).abs() - bound
+        assert over.max() <= 0, float(over.max())
 
 
 # ---- long sums --------------------------------------------------------------------------------------------------------------
