@@ -333,7 +333,7 @@ ffn_few_ring_kernel(const __grid_constant__ CUtensorMap map0, const __grid_const
 
 // Any other rows of w: loads into registers, a batch of U steps ahead.
 // Sixteen bytes of a row of w: EVEN: rows on 16 bytes, a strip's last columns element by element; otherwise the parts that cover
-// them (4096 x 12063 bf16, one token: 64 us element by element, 42 so).
+// them (3952 x 12063 bf16, one token: 64 us element by element, 42 so).
 template <typename T, bool EVEN> struct Row16 {
     uint4 q;
     __device__ __forceinline__ void begin(const T* at, int valid, const Span&) {

@@ -15,8 +15,9 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_t(float z) {
 }
 
 // For bf16 tensors: Phi(z) without a branch from e^(-z^2/2) and the rational approximation 7.1.26 of Abramowitz and Stegun,
-// Handbook of Mathematical Functions (1964), of erfc: |error| <= 1.5e-7, a 1/26000 of bf16's half step at 1.  erff takes
-// both sides of a branch in almost every warp and twice the instructions.  e: e^(-z^2/2), shared with the density.
+// Handbook of Mathematical Functions (1964), of erfc: |error| <= 1.5e-7, a 1/26000 of bf16's half step at 1.  Relative to
+// Phi(z) itself 0.36 % at z = -6 (half a step of bf16), 1 % at -8, 3 % at -12.  erff takes both sides of a branch in almost
+// every warp and twice the instructions.  e: e^(-z^2/2), shared with the density.
 __device__ __forceinline__ float phi_fast(float z, float e) {
     const float t = rcp_fast(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
     const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);   // Phi(-|z|)
