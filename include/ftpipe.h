@@ -68,7 +68,8 @@ enum { FTP_CONV1D = 0, FTP_CONV2D = 1, FTP_DWCONV3x3 = 2, FTP_BN = 3, FTP_ACT = 
         *           a batch norm in front of an ADD_RESIDUAL, of which only the sum is stored: FTP_EUNSUPPORTED)
         *   GATED : act(x W_gate) * (x W_up)
         * k is the form in which the values before the activation wait for the backward pass: 0 the tensors' type, 8 an
-        * 8-bit image, which halves (bf16) or quarters (float) what a batch in flight holds of them. */
+        * 8-bit image, which halves (bf16) or quarters (float) what a batch in flight holds of them.
+        * (FC is computed in float: a bf16 model has it in front of SOFTMAX_CE only, FTP_EUNSUPPORTED elsewhere.) */
        FTP_LINEAR = 10, FTP_GATED = 11 };
 /* GELU (z Phi(z), the error-function form) and SILU (z / (1 + e^-z)): LINEAR and GATED only */
 enum { FTP_ACT_NONE = 0, FTP_ACT_RELU = 1, FTP_ACT_RELU6 = 2, FTP_ACT_GELU = 3, FTP_ACT_SILU = 4 };

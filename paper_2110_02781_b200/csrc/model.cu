@@ -110,7 +110,12 @@ ftp_status plan_ops(const ftp_layer_desc* layers, int n, const ftp_model_cfg* cf
                 int kh = 1, kw = 1, st = 1, ph = 0, pw = 0;
                 if (d.kind == FTP_CONV1D) { FTP_REQUIRE(H == 1, FTP_EINVAL, "build_model: op %d: CONV1D needs H == 1", i); kw = d.k; st = d.stride; pw = d.pad; }
                 else if (d.kind == FTP_CONV2D) { kh = kw = d.k; st = d.stride; ph = pw = d.pad; }
-                else FTP_REQUIRE(H == 1 && W == 1, FTP_EINVAL, "build_model: op %d: FC needs a 1x1 input (pool first)", i);
+                else {
+                    FTP_REQUIRE(H == 1 && W == 1, FTP_EINVAL, "build_model: op %d: FC needs a 1x1 input (pool first)", i);
+                    // computed in float: the buffers of a bf16 model hold such a result in front of the loss only
+                    FTP_REQUIRE(cfg->precision == FTP_FP32 || (i + 1 < n && layers[i + 1].kind == FTP_SOFTMAX_CE), FTP_EUNSUPPORTED,
+                                "build_model: op %d: in a bf16 model FC is the classifier in front of the loss (LINEAR elsewhere)", i);
+                }
                 FTP_REQUIRE(kw >= 1 && st >= 1 && pw >= 0, FTP_EINVAL, "build_model: op %d: bad kernel geometry", i);
                 o.Ho = (H + 2 * ph - kh) / st + 1; o.Wo = (W + 2 * pw - kw) / st + 1; o.Co = d.cout;
                 FTP_REQUIRE(H + 2 * ph >= kh && W + 2 * pw >= kw, FTP_EINVAL, "build_model: op %d: kernel larger than the padded input", i);

@@ -157,3 +157,20 @@ def test_an_addend_in_place_has_the_pitch_of_its_result():
     for kw in (dict(ldr=80), dict(lddx=80), dict(lddx=80, ldr=64)):
         assert L.ftp_linear_backward(ref(desc(**kw)), None, P, None, P, Q, Q, None, None, W, 1 << 30, None) == 1, kw
         assert L.ftp_gated_backward(ref(desc(stash=1, **kw)), None, P, P, P, P, Q, Q, None, None, W, 1 << 30, None) == 1, kw
+
+
+def test_an_inner_classifier_is_refused_in_bf16():
+    """FC computes in float: in a bf16 model only the one in front of the loss has a buffer that holds its result."""
+    import synth
+    L, K = synth.Layer, synth.KIND
+    lin, gap = L(0, K["LINEAR"], 8, 8, 0, 1, 0, 0, 0, -1), L(0, K["GAP"], 8, 8, 0, 1, 0, 0, 0, -1)
+    inner = L(0, K["FC"], 8, 8, 1, 1, 0, 0, 1, -1)
+    tail = [L(0, K["FC"], 8, 3, 1, 1, 0, 0, 1, -1), L(0, K["SOFTMAX_CE"], 3, 3, 0, 1, 0, 0, 0, -1)]
+    for ls in ([lin, gap, inner], [lin, gap, inner, lin], [lin, gap, lin]):
+        F.ftp_workspace_bytes(ls + tail, synth.config(2, 8, 1, 6, 3))
+        if inner not in ls:
+            F.ftp_workspace_bytes(ls + tail, synth.config(2, 8, 1, 6, 3, precision=1))
+            continue
+        with pytest.raises(F.FtpError) as e:
+            F.ftp_workspace_bytes(ls + tail, synth.config(2, 8, 1, 6, 3, precision=1))
+        assert e.value.status == 7
