@@ -271,6 +271,8 @@ ftp_status plan_gradients(ftp_model& m, int* n_slots) {
         if (i > 0) {
             m.ops[i - 1].gslot = alloc();
             if (pending[i] >= 0) o.addend_of = pending[i];
+            FTP_REQUIRE(o.addend_of < 0 || (o.d.kind != FTP_MAXPOOL2 && o.d.kind != FTP_GAP), FTP_EUNSUPPORTED,
+                        "build_model: op %d: a residual source feeding a pool is not supported", i);
         }
         // after op i has run: its own output gradient is consumed, and so is the addend it folded in
         if (s >= 0) release(s);

@@ -174,3 +174,17 @@ def test_an_inner_classifier_is_refused_in_bf16():
         with pytest.raises(F.FtpError) as e:
             F.ftp_workspace_bytes(ls + tail, synth.config(2, 8, 1, 6, 3, precision=1))
         assert e.value.status == 7
+
+
+@pytest.mark.parametrize("precision", [0, 1])
+def test_a_residual_source_in_front_of_a_pool_is_refused_when_the_model_is_planned(precision):
+    """The pool's backward pass adds no second gradient: found before a step, not in the middle of one."""
+    import synth
+    L, K = synth.Layer, synth.KIND
+    lin, gap = L(0, K["LINEAR"], 8, 8, 0, 1, 0, 0, 0, -1), L(0, K["GAP"], 8, 8, 0, 1, 0, 0, 0, -1)
+    tail = [L(0, K["FC"], 8, 3, 1, 1, 0, 0, 1, -1), L(0, K["SOFTMAX_CE"], 3, 3, 0, 1, 0, 0, 0, -1)]
+    cfg = synth.config(2, 8, 1, 1, 3, precision=precision)           # one position: the pool keeps the shape
+    F.ftp_workspace_bytes([lin, gap, lin._replace(residual_src=1)] + tail, cfg)
+    with pytest.raises(F.FtpError) as e:
+        F.ftp_workspace_bytes([lin, gap, lin._replace(residual_src=0)] + tail, cfg)
+    assert e.value.status == 7
