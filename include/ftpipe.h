@@ -411,8 +411,8 @@ ftp_status ftp_launch_count(const ftp_model* m, int64_t* launches);
  * laid out alike (rows off 16 bytes may be added up in another order). They may be recorded into a CUDA graph.  A call
  * needs a workspace of its own for as long as it runs (in a graph: for as long as the graph may be replayed).  Infinities
  * and NaN reach the results whose terms hold them, as in float arithmetic (beside an infinity in a float product of more
- * than a few tokens a factor below 2^-134 counts as 0).  Such products take a float operand with an error of up to 2^-134:
- * as it is from 2^-109 on.  Outputs may not overlap inputs or each other, but for the two cases named below (refused where
+ * than a few tokens a factor below 2^-134 counts as 0).  Such products hold a float operand to 24 bits or to 2^-134,
+ * whichever is coarser.  Outputs may not overlap inputs or each other, but for the two cases named below (refused where
  * two of them start at one address).
  *
  * What a backward pass needs of its forward pass is kept by the caller, in the tensors' type or as an 8-bit image
