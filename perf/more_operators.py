@@ -121,8 +121,8 @@ def work(case):
         return {"bytes": e * n * (5 + 2 * c["gated"]) + 2 * state + kept, "flops": 25.0 * n}
     n = c["rows"] * c["vocab"]
     if op == "logp_fwd":
-        return {"bytes": e * n + c["rows"] * (4 + 4 + 4 + 4 * c["entropy"] + 8 * c["top"]), "flops": 6.0 * n}
-    return {"bytes": 2 * e * n + c["rows"] * (12 + 8 * c["entropy"]), "flops": 6.0 * n}
+        return {"bytes": e * n + c["rows"] * (4 + 4 + 8 + 4 * c["entropy"] + 8 * c["top"]), "flops": 6.0 * n}
+    return {"bytes": 2 * e * n + c["rows"] * (16 + 8 * c["entropy"]), "flops": 6.0 * n}
 
 
 # ---- inputs -----------------------------------------------------------------------------------------
@@ -211,17 +211,17 @@ def prepare(case, seed):
     del z, noise
     if op == "logp_fwd":
         f32 = dict(dtype=torch.float32, device="cuda")
-        s["logp"], s["lse"] = torch.empty(m, **f32), torch.empty(m, **f32)
+        s["logp"], s["lse"] = torch.empty(m, **f32), torch.empty(m, 2, **f32)
         s["entropy"] = torch.empty(m, **f32) if c["entropy"] else None
         s["top"] = torch.empty(m, c["top"], dtype=torch.int32, **dev) if c["top"] else None
         s["top_logp"] = torch.empty(m, c["top"], **f32) if c["top"] else None
         return s
     z = s["logits"].double() * c["scale"]
-    s["lse"] = torch.logsumexp(z, 1)
-    lp = z - s["lse"][:, None]
+    top = z.amax(1, keepdim=True)
+    lp = z - torch.logsumexp(z, 1, keepdim=True)
+    s["lse"] = torch.cat([top / c["scale"], torch.logsumexp(z - top, 1, keepdim=True)], 1).float()           # the largest logit, and the rest of the sum
     s["entropy"] = -(lp.exp() * lp.clamp(min=-1e4)).sum(1).float() if c["entropy"] else None
-    s["lse"] = s["lse"].float()
-    del z, lp
+    del z, lp, top
     s["dlogp"] = normal(m) / m
     s["dentropy"] = normal(m, scale=0.01) / m if c["entropy"] else None
     s["dlogits"] = torch.empty_like(s["logits"])
@@ -413,7 +413,7 @@ def _plain_logp(s, c, t):
         e = torch.exp(z - top)
         total = e.sum(1, keepdim=True)
         lse = top + torch.log(total)
-        out = dict(logp=(z.gather(1, at) - lse)[:, 0], lse=lse[:, 0], entropy=None, top=None, top_logp=None)
+        out = dict(logp=(z.gather(1, at) - lse)[:, 0], lse=torch.cat([s["logits"].float().amax(1, keepdim=True), torch.log(total)], 1), entropy=None, top=None, top_logp=None)
         if c["entropy"]:
             low = torch.where(e > 0, z - lse, torch.zeros_like(z))
             out["entropy"] = -(e / total * low).sum(1)
@@ -421,7 +421,7 @@ def _plain_logp(s, c, t):
             value, index = torch.sort(z, dim=1, descending=True, stable=True)  # of equal ones the lowest token first
             out["top"], out["top_logp"] = index[:, :c["top"]].to(torch.int32), value[:, :c["top"]] - lse
         return out
-    lp = z - s["lse"][:, None]
+    lp = (s["logits"].float() - s["lse"][:, :1]) * c["scale"] - s["lse"][:, 1:]
     p = torch.exp(lp)
     d = -p * s["dlogp"][:, None]
     d.scatter_add_(1, at, s["dlogp"][:, None])
@@ -572,7 +572,7 @@ def _exact_logp(s, c):
     p = torch.exp(lp)
     plogp = torch.where(torch.isinf(lp), torch.zeros_like(p), p * lp)
     if c["op"] == "logp_fwd":
-        res = {"logp": lp[rows, s["targets"].long()], "lse": lse, "entropy": -plogp.sum(1) if c["entropy"] else None, "top": None, "top_logp": None}
+        res = {"logp": lp[rows, s["targets"].long()], "lse": torch.stack([s["logits"].double().max(1).values, lse - z.max(1).values], 1), "entropy": -plogp.sum(1) if c["entropy"] else None, "top": None, "top_logp": None}
         if c["top"]:
             index = torch.sort(-s["logits"].double(), dim=1, stable=True)[1][:, :c["top"]]
             res["top"], res["top_logp"] = index.to(torch.int32), torch.gather(lp, 1, index)
