@@ -474,6 +474,99 @@ ftp_status ftp_checkpoint_unpack(const void* image, int32_t part, int64_t rows, 
  * since the last check are invalid.  FTP_ESTATE while the stream is being captured. */
 ftp_status ftp_check_op_status(void* stream);
 
+/* ---- operators around the feed-forward products ---------------------------------------------------------------------
+ * (The paper's networks have no counterpart: these are what a stage of a language model needs beside its token-wise products.)
+ * Conventions as above: tokens are rows, vectors of weights and their gradients are float, everything else has the type
+ * `precision` names, pitches are elements between rows (0: no gap), sums, statistics and states are float or double.  The same
+ * inputs laid out alike give the same bits.  Outputs may not overlap inputs or each other but where a call says so. */
+
+/* Dropout.  A mask is never stored: whether an element stays is a function of two 64-bit words in device memory, rng[0] (key) and
+ * rng[1] (step), read when the kernel runs (a replayed graph takes the words of that moment), of `site` (0..2^24-1: which dropout
+ * of a step this is), of the row's number row0 + r and of the column; so cutting a batch into micro-batches, or a network into
+ * stages, or repeating a lost step, changes no bit.  Philox 4x32-10 with key {lo, hi of rng[0]} and counter {lo of n, (hi of n) |
+ * site << 8, lo, hi of rng[1]}, n = row * ceil(cols / 8) + column / 8, gives eight columns 16 bits each, the lowest of the first
+ * word first; a column stays where its bits are at least c = round(65536 dropout), and is multiplied by 65536 / (65536 - c). What
+ * does not stay is 0, whatever it was.  (dropout counts in steps of 2^-16; (row0 + rows) ceil(cols / 8) < 2^40.)
+ *
+ * y = x mask 65536 / (65536 - c).  The gradient is the same call on dy.  y may be x, with its pitch. */
+ftp_status ftp_dropout(const void* x, void* y, int64_t rows, int32_t cols, int64_t ldx, int64_t ldy, int32_t precision, double dropout,
+                       const void* rng, int32_t site, int64_t row0, void* stream);
+
+/* A block's result u joins the residual stream x, and the next block's input y is made of the sum:
+ *
+ *   s = alpha x + beta gate drop(post(u)),   y = pre(s)
+ *
+ * post, pre: FTP_NORM_NONE; FTP_NORM_RMS, v / sqrt(mean(v^2) + eps) * w + b; FTP_NORM_LAYER, (v - mean(v)) / sqrt(var(v) + eps) *
+ * w + b, over a row; w and b nullable (1 and 0).  gate: NULL (1); with gate_rows 0 a float vector of cols; else a matrix of the
+ * tensors' type with a row for every gate_rows tokens (the last may have fewer).  s is rounded to the tensors' type and y is
+ * made of the rounded s.  Rows hold up to 16384 columns. */
+enum { FTP_NORM_NONE = 0, FTP_NORM_RMS = 1, FTP_NORM_LAYER = 2 };
+typedef struct {
+    int64_t rows;
+    int32_t cols, precision;
+    int32_t post, pre;                    /* FTP_NORM_* */
+    float eps, alpha, beta;
+    int32_t site;                         /* dropout: see above; 0 dropout: rng may be NULL */
+    double dropout;
+    int64_t row0, gate_rows;
+    int64_t ldu, ldx, lds, ldy, ldg;      /* u, x, s, y and dy, gate */
+    int64_t lddu, ldds, lddx, lddg;       /* du, ds, dx, dgate */
+} ftp_join_desc;
+
+/* x may be NULL (no stream yet: its term is 0), s may be x, with its pitch.  u NULL: y = pre(x) alone (s NULL, alpha 1, no post, gate
+ * or dropout).  y is NULL iff pre is FTP_NORM_NONE.  stats (nullable): 4 x rows floats for the backward pass (mean, 1 / deviation
+ * of u; mean, 1 / deviation of s; only those of norms that are there are written, means of RMS norms are 0). */
+ftp_status ftp_join_forward(const ftp_join_desc* d, const void* u, const void* x, const float* w_post, const float* b_post, const void* gate,
+                            const float* w_pre, const float* b_pre, const void* rng, void* s, void* y, float* stats, void* stream);
+/* From dy and ds (the gradient that reaches s another way; nullable), with D = ds + (gradient of s through pre):  dx = alpha D,
+ * and du, the gradients of the weights and of the gate (a float vector, or of the gate's type) through beta gate drop(post(u)).
+ * Each output may be NULL; dx may be ds, with its pitch.  u may be NULL where post is FTP_NORM_NONE and dgate is NULL; s (for u
+ * NULL in the forward pass: x) where pre is FTP_NORM_NONE.  No rows: the vectors' gradients become 0. */
+ftp_status ftp_join_workspace_bytes(const ftp_join_desc* d, size_t* bytes);
+ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* s, const float* w_post, const float* b_post, const void* gate,
+                             const float* w_pre, const float* stats, const void* rng, const void* dy, const void* ds, void* du, void* dx,
+                             float* dw_post, float* db_post, float* dw_pre, float* db_pre, void* dgate, void* ws, size_t ws_bytes, void* stream);
+
+/* Gated linear recurrence over the steps of a sequence, every channel for itself:
+ *
+ *   a_t = 1 / (1 + e^-f_t),   h_t = a_t h_(t-1) + (1 - a_t) v_t   (coupled; else + v_t),   y_t = act(o_t) h_t   (o NULL: y = h)
+ *
+ * f, v, o, y are rows of `cols` channels, a row per step: sequence b of `seqs` holds rows b len .. b len + len - 1, or, with
+ * `offsets` (device, seqs + 1 ascending int32), rows offsets[b] .. offsets[b + 1] - 1 of `rows`, `len` of them at most (what is
+ * beyond either is cut off; other rows are left as they are).  Steps whose rows lie apart by more (time-major batches) are one
+ * sequence of seqs * cols channels.  h0, h1: state in front of the first and behind the last step, float [seqs][cols] (h0 NULL: 0;
+ * h1 may be h0); a sequence without steps passes it on.  One step a sequence is a serving program's call.
+ * states (nullable): the states that a backward pass starts from, in front of every 16th step: float [rows / 16 + seqs][cols],
+ * step t of sequence b at row (its first row) / 16 + b + t / 16; other rows are left as they are.
+ * Long sequences are cut among blocks, whose parts are joined in a fixed order; a state that is infinite or NaN makes all later
+ * ones of its channel infinite or NaN. */
+typedef struct {
+    int64_t seqs, len, rows;              /* rows: with offsets; else 0 or seqs * len */
+    int32_t cols, precision, act, coupled;
+    int64_t ldf, ldv, ldo, ldy;           /* ldy: y, or dy */
+    int64_t lddf, lddv, lddo;
+} ftp_recurrence_desc;
+ftp_status ftp_recurrence_states(const ftp_recurrence_desc* d, int64_t* rows);
+ftp_status ftp_recurrence_forward(const ftp_recurrence_desc* d, const void* f, const void* v, const void* o, const float* h0, const int32_t* offsets,
+                                  void* y, float* h1, float* states, void* stream);
+/* df, dv, dout (of o; NULL iff o is) and dh0 (nullable) from dy and dh1 (of h1; nullable); dh0 may be dh1.  states: what the forward pass kept. */
+ftp_status ftp_recurrence_backward(const ftp_recurrence_desc* d, const void* f, const void* v, const void* o, const float* states,
+                                   const int32_t* offsets, const void* dy, const float* dh1, void* df, void* dv, void* dout, float* dh0, void* stream);
+
+/* Log probabilities of given tokens under rows of logits, z = scale x over `vocab` columns:
+ *
+ *   logp = z_target - log sum e^z,   entropy = - sum p log p,   top: the k likeliest tokens, likeliest first (of equal ones the lowest)
+ *
+ * A target outside 0..vocab-1 is none: logp 0, and no gradient through it.  Logits of -infinity are tokens that cannot occur; a row
+ * of nothing else has logp -infinity, entropy 0 and gradient 0.  A row that holds a NaN or +infinity has NaN for results; its top
+ * tokens are some tokens of the row.  logp, entropy, top, top_logp nullable; top and top_logp are rows x k (k 0..32, at most vocab).
+ * lse (nullable; the backward pass reads it): per row two floats, the largest logit m and log sum e^(scale (x - m)). */
+ftp_status ftp_logprob_forward(const void* logits, int64_t rows, int32_t vocab, int64_t ldl, int32_t precision, float scale, const int32_t* targets,
+                               float* logp, float* entropy, float* lse, int32_t* top, float* top_logp, int32_t k, void* stream);
+/* dlogits from dlogp and dentropy (each nullable; entropy: the forward pass's, with dentropy).  dlogits may be logits, with its pitch. */
+ftp_status ftp_logprob_backward(const void* logits, int64_t rows, int32_t vocab, int64_t ldl, int32_t precision, float scale, const int32_t* targets,
+                                const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, void* stream);
+
 /* ---- for callers that cannot allocate ------------------------------------------------------------
  * (The paper has no counterpart: this is a packaging variant of the weight-gradient step of
  * run_stage's backward pass.)

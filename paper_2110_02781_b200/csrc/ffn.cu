@@ -6,6 +6,7 @@
 #include "ffn_math.cuh"
 #include "kernels.h"
 #include "launch.cuh"
+#include "op_checks.h"
 
 namespace ftp {
 namespace ffn {
@@ -641,36 +642,11 @@ ftp_status check_stash(const ftp_ffn_desc* d, const void* stash, const char* who
     FTP_REQUIRE(d->stash != STASH_8BIT || aligned(stash, 32), FTP_ERANGE, "%s: an image must start on a 32-byte boundary", who);
     return FTP_OK;
 }
-// Addresses: multiples of their elements' size, and no output where an input or another output starts (further overlaps
-// cannot be told from columns of one matrix, which may be neighbours).
-ftp_status check_addresses(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins, const char* who) {
-    for (auto o = outs.begin(); o != outs.end(); ++o) {
-        if (!*o) continue;
-        for (const void* i : ins) FTP_REQUIRE(*o != i, FTP_EINVAL, "%s: an output lies on an input", who);
-        for (auto q = outs.begin(); q != o; ++q) FTP_REQUIRE(*o != *q, FTP_EINVAL, "%s: two outputs in one place", who);
-    }
-    return FTP_OK;
-}
-// An addend may be the result itself, element by element: with another pitch a row would be read after it was overwritten.
-ftp_status check_in_place(const void* add, const void* out, int64_t ldadd, int64_t ldout, int64_t rows, int32_t cols, const char* who) {
-    FTP_REQUIRE(!add || add != out || rows == 1 || (ldadd ? ldadd : cols) == (ldout ? ldout : cols), FTP_EINVAL, "%s: an addend in place of its result with another pitch", who);
-    return FTP_OK;
-}
-ftp_status check_elements(std::initializer_list<const void*> all, size_t bytes, const char* who) {
-    for (const void* p : all) FTP_REQUIRE(aligned(p, bytes), FTP_ERANGE, "%s: an address is not a multiple of its elements' size", who);
-    return FTP_OK;
-}
 ftp_status check_ws(const Carve& need, const void* ws, size_t ws_bytes, const char* who) {
     FTP_REQUIRE(need.off == 0 || (ws && ws_bytes >= need.off), FTP_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need.off);
     FTP_REQUIRE(need.off == 0 || aligned(ws, 256), FTP_ERANGE, "%s: workspace must start on a 256-byte boundary", who);
     return FTP_OK;
 }
-ftp_status launched(const char* who) {
-    const cudaError_t e = cudaGetLastError();
-    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
-    return FTP_OK;
-}
-
 // ---- forward of both operators (w[1]: the gated operator's second matrix) ----
 template <typename T, bool GATED>
 ftp_status forward(const ftp_ffn_desc* d, const void* x, const void* const* w, const float* bias, const void* residual, void* y, int stash_kind, void* stash,
@@ -937,6 +913,8 @@ int* status_word() {
 }  // namespace ftp
 
 using namespace ftp::ffn;
+using ftp::check_elements;
+using ftp::launched;
 
 extern "C" {
 

@@ -1,0 +1,458 @@
+// Gated linear recurrence over the steps of a sequence: h_t = a_t h_(t-1) + b_t with a = 1 / (1 + e^-f), b = (1 - a) v or v, and
+// y = act(o) h; every channel for itself.
+//
+// Bound by memory: one pass over f, v, o and y (backward: f, v, o, dy in, df, dv, do out).  A step is the map h -> a h + b, and the
+// maps of a run of steps compose to one, h -> A h + B.  A thread holds a run of 16 steps of two neighbouring channels (bf16; one
+// float channel) in registers, all its loads in flight at once; a warp 32 threads of one run; a block up to eight runs after one
+// another, and a cluster of up to eight blocks the runs after those, so that a long sequence of few channels still fills the GPU.
+// The runs' maps go through shared memory, the blocks' through the cluster's, and are applied in the order of time, whatever
+// finishes first: one read of the data and the same bits every time.  The state and the maps are float.
+// The backward pass starts every run from the state that the forward pass kept in front of it, walks it forward once and then, with
+// q_t = a_t (g_t + q_(t+1)) (g: dy act(o), q_(t+1): what reaches h_t from behind), backward in the same way.
+#include <algorithm>
+#include "token.cuh"
+
+namespace ftp {
+namespace token {
+namespace {
+
+constexpr int RUN = 16, WARPS = 8;
+template <typename T> constexpr int LANES = 4 / (int)sizeof(T);      // channels of a thread
+template <typename T> constexpr int TILE = 32 * LANES<T>;            // of a block
+
+struct RecArgs {
+    const void *f, *v, *o, *dy;
+    void *y, *df, *dv, *dout;
+    const float *h0, *dh1;
+    float *h1, *dh0, *states;
+    const int32_t* offsets;
+    int64_t seqs, len, rows, ldf, ldv, ldo, ldy, lddf, lddv, lddo;
+    int cols, tiles, act, coupled;
+};
+
+// A thread's channels of one row.  VEC: neighbours; otherwise 32 apart.
+template <typename T, bool VEC> struct Lane {
+    int c;
+    __device__ __forceinline__ Lane(int tile) : c(tile * TILE<T> + (threadIdx.x & 31) * (VEC ? LANES<T> : 1)) {}
+    __device__ __forceinline__ int at(int j) const { return c + (VEC ? j : 32 * j); }
+    __device__ __forceinline__ unsigned get(const T* row, int cols) const {
+        if constexpr (sizeof(T) == 4) return c < cols ? __float_as_uint(row[c]) : 0u;
+        else if constexpr (VEC) return c < cols ? *reinterpret_cast<const unsigned*>(row + c) : 0u;
+        else return (c < cols ? bits_of(row[c]) : 0u) | (c + 32 < cols ? bits_of(row[c + 32]) << 16 : 0u);
+    }
+    __device__ __forceinline__ void put(T* row, int cols, const float (&v)[LANES<T>]) const {
+        if constexpr (sizeof(T) == 4) { if (c < cols) row[c] = v[0]; }
+        else if constexpr (VEC) { if (c < cols) *reinterpret_cast<unsigned*>(row + c) = bf_pack(v[0], v[1]); }
+        else {
+            if (c < cols) row[c] = __float2bfloat16(v[0]);
+            if (c + 32 < cols) row[c + 32] = __float2bfloat16(v[1]);
+        }
+    }
+    __device__ __forceinline__ void get_state(const float* row, int cols, float (&v)[LANES<T>]) const {
+#pragma unroll
+        for (int j = 0; j < LANES<T>; ++j) v[j] = row && at(j) < cols ? row[at(j)] : 0.f;
+    }
+    __device__ __forceinline__ void put_state(float* row, int cols, const float (&v)[LANES<T>]) const {
+#pragma unroll
+        for (int j = 0; j < LANES<T>; ++j) if (at(j) < cols) row[at(j)] = v[j];
+    }
+};
+template <typename T> __device__ __forceinline__ void split(unsigned w, float (&v)[LANES<T>]) {
+    if constexpr (sizeof(T) == 4) v[0] = __uint_as_float(w);
+    else { v[0] = bf_lo(w); v[1] = bf_hi(w); }
+}
+
+// The smaller of a = 1 / (1 + e^-f) and 1 - a, with the sign bit set where that is a: both then are exact to a rounding, next to 1 and
+// to 0 alike (0 and 1 at infinities).  bf16: hardware exponential and reciprocal, 2^-21 relative.
+template <typename T> __device__ __forceinline__ float gate(float f) {
+    const float e = sizeof(T) == 4 ? expf(-fabsf(f)) : ffn::ex2_fast(fabsf(f) * -ffn::LOG2E);
+    const float s = e * (sizeof(T) == 4 ? 1.f / (1.f + e) : ffn::rcp_fast(1.f + e));
+    return __uint_as_float(__float_as_uint(s) | (__float_as_uint(f) & 0x80000000u));
+}
+__device__ __forceinline__ void both(float s, float& a, float& other) {
+    const float small = fabsf(s), big = 1.f - small;
+    const bool low = __float_as_uint(s) >> 31;
+    a = low ? small : big;
+    other = low ? big : small;
+}
+
+// rows of sequence b
+struct Where { int64_t start, len; };
+__device__ __forceinline__ Where where(const RecArgs& a, int64_t b) {
+    if (!a.offsets) return Where{b * a.len, a.len};
+    const int64_t lo = min(max((int64_t)a.offsets[b], (int64_t)0), a.rows), hi = min(max((int64_t)a.offsets[b + 1], lo), a.rows);
+    return Where{lo, min(hi - lo, a.len)};
+}
+
+// Maps of the warps' runs joined: what reaches this warp's run and what leaves the cluster's last, from what reaches its first.
+// REVERSE: the last run comes first.  `maps`: [2][WARPS][32], `parts`: [2][8][32] in shared memory, used in turn.
+template <int N> struct Map { float a[N], b[N]; };
+template <int N, bool REVERSE> struct Join {
+    Map<N>*maps, *parts;
+    unsigned ranks, rank;
+    int turn, w, warps;
+    __device__ __forceinline__ void operator()(const Map<N>& mine, float (&carry)[N], float (&in)[N]) {
+        const int lane = threadIdx.x & 31;
+        Map<N>* m = maps + turn * WARPS * 32;
+        m[w * 32 + lane] = mine;
+        __syncthreads();
+        Map<N> pre, all;
+#pragma unroll
+        for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
+        for (int i = 0; i < warps; ++i) {
+            const int k = REVERSE ? warps - 1 - i : i;
+            if (k == w) pre = all;
+            const Map<N> n = m[k * 32 + lane];
+#pragma unroll
+            for (int j = 0; j < N; ++j) { all.b[j] = fmaf(n.a[j], all.b[j], n.b[j]); all.a[j] *= n.a[j]; }
+        }
+        if (ranks == 1) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) { in[j] = fmaf(pre.a[j], carry[j], pre.b[j]); carry[j] = fmaf(all.a[j], carry[j], all.b[j]); }
+        } else {
+            Map<N>* p = parts + turn * 8 * 32;
+            for (unsigned r = w; r < ranks; r += warps) {            // every warp tells some of the blocks
+                const unsigned to = on_rank(smem_at(p + rank * 32 + lane), r);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(to + 4 * j), "f"(all.a[j]) : "memory");
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(to + 4 * N + 4 * j), "f"(all.b[j]) : "memory");
+                }
+            }
+            cluster_sync();
+            for (unsigned i = 0; i < ranks; ++i) {
+                const unsigned k = REVERSE ? ranks - 1 - i : i;
+                if (k == rank)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) in[j] = fmaf(pre.a[j], carry[j], pre.b[j]);
+                const Map<N> n = p[k * 32 + lane];
+#pragma unroll
+                for (int j = 0; j < N; ++j) carry[j] = fmaf(n.a[j], carry[j], n.b[j]);
+            }
+        }
+        turn ^= 1;
+    }
+};
+
+// SHORT: sequences of at most one run, a warp each; otherwise a cluster per sequence and tile of channels
+template <typename T, bool VEC, bool SHORT>
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a) {
+    constexpr int N = LANES<T>;
+    __shared__ Map<N> maps[SHORT ? 1 : 2 * WARPS * 32], parts[SHORT ? 1 : 2 * 8 * 32];
+    grid_dep_sync();
+    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
+    unsigned ranks = 1, rank = 0;
+    if constexpr (!SHORT) {
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+        rank = cluster_rank();
+        if (ranks > 1) cluster_sync();                               // the other blocks' shared memory is there
+    }
+    const int64_t unit = SHORT ? (int64_t)blockIdx.x * warps + w : blockIdx.x / ranks, b = unit / a.tiles;
+    if (SHORT && b >= a.seqs) return;
+    const Lane<T, VEC> lane((int)(unit - b * a.tiles));
+    const Where seq = where(a, b);
+    float carry[N];
+    lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
+    Join<N, false> join{maps, parts, ranks, rank, 0, w, warps};
+    const int64_t stride = (int64_t)RUN * (SHORT ? 1 : warps * ranks);
+    for (int64_t t0 = SHORT ? 0 : (int64_t)RUN * (rank * warps + w), base = 0; base < seq.len; t0 += stride, base += stride) {
+        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
+        const int64_t row = seq.start + t0;
+        unsigned f[RUN], v[RUN], o[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            f[i] = i < n ? lane.get(static_cast<const T*>(a.f) + (row + i) * a.ldf, a.cols) : 0u;
+            v[i] = i < n ? lane.get(static_cast<const T*>(a.v) + (row + i) * a.ldv, a.cols) : 0u;
+            o[i] = i < n && a.o ? lane.get(static_cast<const T*>(a.o) + (row + i) * a.ldo, a.cols) : 0u;
+        }
+        float s[RUN][N];
+        Map<N> all;
+#pragma unroll
+        for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float ff[N], vv[N];
+            split<T>(f[i], ff);
+            split<T>(v[i], vv);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                s[i][j] = gate<T>(ff[j]);
+                if (i >= n) s[i][j] = 0.f;                           // a = 1, v = 0: passes the state on
+                if constexpr (!SHORT) {
+                    float x, y;
+                    both(s[i][j], x, y);
+                    all.b[j] = fmaf(x, all.b[j], (a.coupled ? y : 1.f) * vv[j]);
+                    all.a[j] *= x;
+                }
+            }
+        }
+        float h[N];
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) h[j] = carry[j];
+        } else join(all, carry, h);
+        if (a.states && n > 0) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float vv[N], oo[N];
+            split<T>(v[i], vv);
+            split<T>(o[i], oo);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float x, y;
+                both(s[i][j], x, y);
+                h[j] = fmaf(x, h[j], (a.coupled ? y : 1.f) * vv[j]);
+                oo[j] = a.o ? ffn::act_value<sizeof(T) == 2>(oo[j], a.act) * h[j] : h[j];
+            }
+            if (i < n) lane.put(static_cast<T*>(a.y) + (row + i) * a.ldy, a.cols, oo);
+        }
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) carry[j] = h[j];
+        }
+    }
+    if (a.h1 && (SHORT || (w == 0 && rank == 0))) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(const RecArgs a) {
+    constexpr int N = LANES<T>;
+    __shared__ Map<N> maps[2 * WARPS * 32], parts[2 * 8 * 32];
+    extern __shared__ float before[];                                // [RUN][threads][N]: h_(t-1) - v (coupled) or h_(t-1)
+    grid_dep_sync();
+    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
+    unsigned ranks, rank = cluster_rank();
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    if (ranks > 1) cluster_sync();
+    const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
+    const Lane<T, VEC> lane((int)(unit - b * a.tiles));
+    const Where seq = where(a, b);
+    float carry[N];
+    lane.get_state(a.dh1 ? a.dh1 + b * a.cols : nullptr, a.cols, carry);
+    Join<N, true> join{maps, parts, ranks, rank, 0, w, warps};
+    const int64_t stride = (int64_t)RUN * warps * ranks;
+    for (int64_t base = (seq.len + stride - 1) / stride * stride - stride; base >= 0; base -= stride) {
+        const int64_t t0 = base + (int64_t)RUN * (rank * warps + w);
+        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
+        const int64_t row = seq.start + t0;
+        unsigned f[RUN], v[RUN], o[RUN], dy[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            f[i] = i < n ? lane.get(static_cast<const T*>(a.f) + (row + i) * a.ldf, a.cols) : 0u;
+            v[i] = i < n ? lane.get(static_cast<const T*>(a.v) + (row + i) * a.ldv, a.cols) : 0u;
+            o[i] = i < n && a.o ? lane.get(static_cast<const T*>(a.o) + (row + i) * a.ldo, a.cols) : 0u;
+            dy[i] = i < n ? lane.get(static_cast<const T*>(a.dy) + (row + i) * a.ldy, a.cols) : 0u;
+        }
+        float h[N], s[RUN][N], g[RUN][N];
+        lane.get_state(n > 0 ? a.states + (seq.start / RUN + b + t0 / RUN) * a.cols : nullptr, a.cols, h);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float ff[N], vv[N], oo[N];
+            split<T>(f[i], ff);
+            split<T>(v[i], vv);
+            split<T>(o[i], oo);
+            split<T>(dy[i], g[i]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                s[i][j] = gate<T>(ff[j]);
+                if (i >= n) s[i][j] = 0.f;
+                float x, y;
+                both(s[i][j], x, y);
+                before[(i * blockDim.x + threadIdx.x) * N + j] = a.coupled ? h[j] - vv[j] : h[j];
+                h[j] = fmaf(x, h[j], (a.coupled ? y : 1.f) * vv[j]);
+                if (a.o) {
+                    float p, q;
+                    ffn::act_both<sizeof(T) == 2>(oo[j], a.act, p, q);
+                    oo[j] = g[i][j] * h[j] * q;
+                    g[i][j] *= p;
+                }
+            }
+            if (a.o && i < n) lane.put(static_cast<T*>(a.dout) + (row + i) * a.lddo, a.cols, oo);
+        }
+        Map<N> all;
+#pragma unroll
+        for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
+#pragma unroll
+        for (int i = RUN - 1; i >= 0; --i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float x, y;
+                both(s[i][j], x, y);
+                if (i >= n) g[i][j] = 0.f;
+                all.b[j] = x * (g[i][j] + all.b[j]);
+                all.a[j] *= x;
+            }
+        float q[N];
+        join(all, carry, q);
+#pragma unroll
+        for (int i = RUN - 1; i >= 0; --i) {
+            float df[N], dv[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float x, y;
+                both(s[i][j], x, y);
+                const float d = g[i][j] + q[j];
+                q[j] = x * d;
+                df[j] = q[j] * y * before[(i * blockDim.x + threadIdx.x) * N + j];
+                dv[j] = a.coupled ? d * y : d;
+            }
+            if (i < n) {
+                lane.put(static_cast<T*>(a.df) + (row + i) * a.lddf, a.cols, df);
+                lane.put(static_cast<T*>(a.dv) + (row + i) * a.lddv, a.cols, dv);
+            }
+        }
+    }
+    if (a.dh0 && w == 0 && rank == 0) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
+}
+
+// ---- host ----
+ftp_status check_desc(const ftp_recurrence_desc* d, const char* who) {
+    FTP_REQUIRE(d, FTP_EINVAL, "%s: null descriptor", who);
+    FTP_REQUIRE(d->precision == FTP_FP32 || d->precision == FTP_BF16, FTP_EINVAL, "%s: unknown precision %d", who, d->precision);
+    FTP_REQUIRE(d->act >= FTP_ACT_NONE && d->act <= FTP_ACT_SILU, FTP_EINVAL, "%s: unknown activation %d", who, d->act);
+    FTP_REQUIRE(d->seqs >= 0 && d->len >= 0 && d->rows >= 0 && d->cols >= 1, FTP_EINVAL, "%s: seqs, len and rows must not be negative, cols must be positive", who);
+    FTP_REQUIRE(d->seqs < (1ll << 31) && d->len < (1ll << 31) && d->rows < (1ll << 38) && d->cols < (1 << 30), FTP_ERANGE, "%s: tensor too large", who);
+    const double steps = d->rows ? (double)d->rows : (double)d->seqs * (double)d->len;
+    FTP_REQUIRE(steps * d->cols <= 274877906944.0 && (double)d->seqs * d->cols <= 274877906944.0, FTP_ERANGE, "%s: tensor too large", who);
+    return check_pitches({d->ldf, d->ldv, d->ldo, d->ldy, d->lddf, d->lddv, d->lddo}, d->cols, who);
+}
+ftp_status check_offsets(const ftp_recurrence_desc* d, const int32_t* offsets, const char* who) {
+    if (offsets) {
+        FTP_REQUIRE(d->rows < (1ll << 31), FTP_ERANGE, "%s: offsets have 32 bits", who);
+        return check_elements({offsets}, 4, who);
+    }
+    FTP_REQUIRE(d->rows == 0 || d->rows == d->seqs * d->len, FTP_EINVAL, "%s: rows must be seqs * len without offsets", who);
+    return FTP_OK;
+}
+void fill(RecArgs& a, const ftp_recurrence_desc* d, const int32_t* offsets) {
+    const auto ld = [&](int64_t v) { return v ? v : (int64_t)d->cols; };
+    a.seqs = d->seqs; a.len = d->len; a.rows = offsets ? d->rows : d->seqs * d->len;
+    a.cols = d->cols; a.act = d->act; a.coupled = d->coupled != 0;
+    a.ldf = ld(d->ldf); a.ldv = ld(d->ldv); a.ldo = ld(d->ldo); a.ldy = ld(d->ldy);
+    a.lddf = ld(d->lddf); a.lddv = ld(d->lddv); a.lddo = ld(d->lddo);
+    a.offsets = offsets;
+}
+// two bf16 channels in one access: even pitches, addresses on four bytes
+bool pairs(std::initializer_list<const void*> ps, std::initializer_list<int64_t> lds, int cols) {
+    for (const void* p : ps) if (!on_bytes(p, 4)) return false;
+    for (int64_t ld : lds) if (ld % 2) return false;
+    return cols % 2 == 0;
+}
+// Blocks of a cluster and runs of a block: the fewest turns of the resident blocks, a turn of a cluster a tenth longer for its barrier.
+void shape(const RecArgs& a, int per_sm, int* warps, int* ranks) {
+    const int64_t runs = (a.len + RUN - 1) / RUN, units = a.seqs * a.tiles;
+    *warps = 1;
+    while (*warps < WARPS && *warps < runs) *warps *= 2;
+    double best = 0;
+    *ranks = 0;
+    for (int s = 1; s <= 8; s *= 2) {
+        if (s > 1 && (int64_t)s * *warps / 2 >= runs) break;
+        const double turns = (double)((units * s + SMS * per_sm - 1) / (SMS * per_sm)), steps = (double)((runs + s * *warps - 1) / (s * *warps));
+        const double cost = turns * steps * (s > 1 ? 1.1 : 1.0);
+        if (!*ranks || cost < best) { best = cost; *ranks = s; }
+    }
+}
+
+template <typename T, bool VEC> ftp_status forward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    const int64_t units = a.seqs * a.tiles;
+    if (a.len <= RUN) {
+        FTP_REQUIRE((units + 3) / 4 < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+        launch(recurrence_forward_kernel<T, VEC, true>, dim3((unsigned)((units + 3) / 4)), dim3(128), 0, st, a);
+        return FTP_OK;
+    }
+    int warps, ranks;
+    shape(a, 2, &warps, &ranks);
+    FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, false>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+template <typename T, bool VEC> ftp_status backward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    const int64_t units = a.seqs * a.tiles;
+    int warps, ranks;
+    shape(a, 2, &warps, &ranks);
+    FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    const cudaError_t e = launch_cluster(recurrence_backward_kernel<T, VEC>, dim3((unsigned)(units * ranks)), 32 * warps, (size_t)RUN * 32 * warps * LANES<T> * 4, ranks, st, a);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+
+}  // namespace
+}  // namespace token
+}  // namespace ftp
+
+using namespace ftp;
+using namespace ftp::token;
+
+extern "C" {
+
+ftp_status ftp_recurrence_states(const ftp_recurrence_desc* d, int64_t* rows) {
+    const char* who = "recurrence_states";
+    if (ftp_status e = check_desc(d, who)) return e;
+    FTP_REQUIRE(rows, FTP_EINVAL, "%s: null argument", who);
+    *rows = (d->rows ? d->rows : d->seqs * d->len) / RUN + d->seqs;
+    return FTP_OK;
+}
+
+ftp_status ftp_recurrence_forward(const ftp_recurrence_desc* d, const void* f, const void* v, const void* o, const float* h0, const int32_t* offsets, void* y,
+                                  float* h1, float* states, void* stream) {
+    const char* who = "recurrence_forward";
+    if (ftp_status e = check_desc(d, who)) return e;
+    if (ftp_status e = check_offsets(d, offsets, who)) return e;
+    if (d->seqs == 0) return FTP_OK;
+    RecArgs a{};
+    fill(a, d, offsets);
+    const bool empty = a.len == 0 || a.rows == 0;
+    FTP_REQUIRE(empty || (f && v && y), FTP_EINVAL, "%s: null buffer", who);
+    FTP_REQUIRE(o || d->act == FTP_ACT_NONE, FTP_EINVAL, "%s: an activation without o", who);
+    if (ftp_status e = check_elements({f, v, o, y}, d->precision == FTP_FP32 ? 4 : 2, who)) return e;
+    if (ftp_status e = check_elements({h0, h1, states}, 4, who)) return e;
+    if (ftp_status e = check_addresses({y, h1, states}, {f, v, o, offsets}, who)) return e;
+    if (ftp_status e = check_addresses({y, states}, {h0}, who)) return e;
+    a.f = f; a.v = v; a.o = o; a.h0 = h0; a.y = y; a.h1 = h1; a.states = states;
+    if (empty) a.len = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ftp_status e;
+    if (d->precision == FTP_FP32) {
+        a.tiles = (a.cols + TILE<float> - 1) / TILE<float>;
+        e = forward_of<float, true>(a, st, who);
+    } else {
+        a.tiles = (a.cols + TILE<bf16> - 1) / TILE<bf16>;
+        e = pairs({f, v, o, y}, {a.ldf, a.ldv, o ? a.ldo : 0, a.ldy}, a.cols) ? forward_of<bf16, true>(a, st, who) : forward_of<bf16, false>(a, st, who);
+    }
+    return e ? e : launched(who);
+}
+
+ftp_status ftp_recurrence_backward(const ftp_recurrence_desc* d, const void* f, const void* v, const void* o, const float* states, const int32_t* offsets,
+                                   const void* dy, const float* dh1, void* df, void* dv, void* dout, float* dh0, void* stream) {
+    const char* who = "recurrence_backward";
+    if (ftp_status e = check_desc(d, who)) return e;
+    if (ftp_status e = check_offsets(d, offsets, who)) return e;
+    if (d->seqs == 0) return FTP_OK;
+    RecArgs a{};
+    fill(a, d, offsets);
+    const bool empty = a.len == 0 || a.rows == 0;
+    FTP_REQUIRE(empty || (f && v && states && dy && df && dv), FTP_EINVAL, "%s: null buffer", who);
+    FTP_REQUIRE((o != nullptr) == (dout != nullptr), FTP_EINVAL, "%s: the gradient of o goes with o", who);
+    FTP_REQUIRE(o || d->act == FTP_ACT_NONE, FTP_EINVAL, "%s: an activation without o", who);
+    if (ftp_status e = check_elements({f, v, o, dy, df, dv, dout}, d->precision == FTP_FP32 ? 4 : 2, who)) return e;
+    if (ftp_status e = check_elements({states, dh1, dh0}, 4, who)) return e;
+    if (ftp_status e = check_addresses({df, dv, dout, dh0}, {f, v, o, states, offsets, dy}, who)) return e;
+    if (ftp_status e = check_addresses({df, dv, dout}, {dh1}, who)) return e;
+    a.f = f; a.v = v; a.o = o; a.dy = dy; a.dh1 = dh1; a.df = df; a.dv = dv; a.dout = dout; a.dh0 = dh0;
+    a.states = const_cast<float*>(states);
+    if (empty) a.len = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ftp_status e;
+    if (d->precision == FTP_FP32) {
+        a.tiles = (a.cols + TILE<float> - 1) / TILE<float>;
+        e = backward_of<float, true>(a, st, who);
+    } else {
+        a.tiles = (a.cols + TILE<bf16> - 1) / TILE<bf16>;
+        e = pairs({f, v, o, dy, df, dv, dout}, {a.ldf, a.ldv, o ? a.ldo : 0, a.ldy, a.lddf, a.lddv, o ? a.lddo : 0}, a.cols) ? backward_of<bf16, true>(a, st, who)
+                                                                                                                             : backward_of<bf16, false>(a, st, who);
+    }
+    return e ? e : launched(who);
+}
+
+}  // extern "C"

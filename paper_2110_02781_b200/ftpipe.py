@@ -22,6 +22,7 @@ T_WEIGHTS, T_GRADS, T_MOMENTUM, T_STATE = 0, 1, 2, 3
 FP32, BF16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_GELU, ACT_SILU = 0, 1, 2, 3, 4
 STASH_NONE, STASH_FULL, STASH_8BIT = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 
 class LayerDesc(C.Structure):
@@ -48,6 +49,17 @@ class FfnDesc(C.Structure):
     _fields_ = [("rows", C.c_int64)] + [(n, C.c_int32) for n in ("cin", "cout", "precision", "act", "stash", "x_8bit", "dw_f32",
                                                                  "unaligned")] + \
                [(n, C.c_int64) for n in ("ldx", "ldw", "ldy", "ldr", "lddx", "lddw")]
+
+
+class JoinDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64)] + [(n, C.c_int32) for n in ("cols", "precision", "post", "pre")] + \
+               [(n, C.c_float) for n in ("eps", "alpha", "beta")] + [("site", C.c_int32), ("dropout", C.c_double)] + \
+               [(n, C.c_int64) for n in ("row0", "gate_rows", "ldu", "ldx", "lds", "ldy", "ldg", "lddu", "ldds", "lddx", "lddg")]
+
+
+class RecurrenceDesc(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("seqs", "len", "rows")] + [(n, C.c_int32) for n in ("cols", "precision", "act", "coupled")] + \
+               [(n, C.c_int64) for n in ("ldf", "ldv", "ldo", "ldy", "lddf", "lddv", "lddo")]
 
 
 PROBE_NORMAL, PROBE_RESTARTED, PROBE_SILENT = 0, 1, 2
@@ -117,6 +129,15 @@ _SIGS = {
     "ftp_checkpoint_pack": [_vp, _i64, _i32, _i64, _i32, _vp, _i32, _vp],
     "ftp_checkpoint_unpack": [_vp, _i32, _i64, _i32, _i32, _vp, _i64, _vp],
     "ftp_check_op_status": [_vp],
+    "ftp_dropout": [_vp, _vp, _i64, _i32, _i64, _i64, _i32, C.c_double, _vp, _i32, _i64, _vp],
+    "ftp_join_workspace_bytes": [_P(JoinDesc), _P(_sz)],
+    "ftp_join_forward": [_P(JoinDesc)] + [_vp] * 12,
+    "ftp_join_backward": [_P(JoinDesc)] + [_vp] * 18 + [_sz, _vp],
+    "ftp_recurrence_states": [_P(RecurrenceDesc), _P(_i64)],
+    "ftp_recurrence_forward": [_P(RecurrenceDesc)] + [_vp] * 9,
+    "ftp_recurrence_backward": [_P(RecurrenceDesc)] + [_vp] * 12,
+    "ftp_logprob_forward": [_vp, _i64, _i32, _i64, _i32, _f32] + [_vp] * 6 + [_i32, _vp],
+    "ftp_logprob_backward": [_vp, _i64, _i32, _i64, _i32, _f32] + [_vp] * 6 + [_i64, _vp],
     "ftp_conv_wgrad_static": [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp],
 }
 for _name, _args in _SIGS.items():
@@ -674,6 +695,266 @@ def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, a
 def ftp_check_op_status(stream=None):
     """Waits for the stream; raises FtpError if a bounded wait of a feed-forward kernel ran out since the last check."""
     _check(lib.ftp_check_op_status(_stream(stream)))
+
+
+# ---- operators around the feed-forward products --------------------------------------------------
+def _remember(key, plan):
+    if len(_PLANS) >= 4096:
+        _PLANS.clear()
+    _PLANS[key] = plan
+    return plan
+
+
+def _words(who, rng, dropout, cur):
+    """The generator's two words (int64: key, step) on the device."""
+    if rng is None:
+        if dropout:
+            _bad(who, "dropout without the generator's words")
+        return
+    if rng.get_device() != cur or rng.dtype is not torch.int64 or not rng.is_contiguous() or rng.numel() != 2:
+        _bad(who, "rng must be two contiguous int64 words (key, step) on the current CUDA device")
+
+
+def _floats(who, name, t, n, cur):
+    if t is not None:
+        _vector(who, name, t, n, cur)
+
+
+def _plan_dropout(key, cur, x, y, dropout, rng):
+    who, cols = "dropout", x.shape[-1] if x.dim() else 0
+    prec = _precision(who, x)
+    rows, ldx = _rows(who, "x", x, cols, x.dtype, cur)
+    ldy = _same_rows(who, "y", y, rows, cols, x.dtype, cur)
+    _words(who, rng, dropout, cur)
+    return _remember(key, (rows, cols, ldx, ldy, prec))
+
+
+def ftp_dropout(x, y, dropout, rng, site=0, row0=0, stream=None):
+    """y = x with elements dropped at the rate `dropout`, the others divided by what stays; the same call on dy gives the
+    gradient.  rng: int64 tensor (key, step) in device memory; site: which dropout of a step; row0: number of x's first row."""
+    cur = _current()
+    key = (6, cur, dropout != 0, _sig(x), _sig(y), _sig(rng))
+    rows, cols, ldx, ldy, prec = _PLANS.get(key) or _plan_dropout(key, cur, x, y, dropout, rng)
+    st = lib.ftp_dropout(x.data_ptr(), y.data_ptr(), rows, cols, ldx, ldy, prec, dropout, _addr(rng), site, row0, _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def _gate(who, name, gate, gate_rows, rows, cols, dt, cur):
+    """Elements between rows of a gate or its gradient (0: a vector)."""
+    if gate is None:
+        return 0
+    if gate_rows < 0:
+        _bad(who, "gate_rows must not be negative")
+    if gate_rows == 0:
+        _vector(who, name, gate, cols, cur)
+        return 0
+    return _same_rows(who, name, gate, -(-rows // gate_rows), cols, dt, cur)
+
+
+def _plan_join_forward(key, cur, u, x, s, y, post, pre, w_post, b_post, w_pre, b_pre, gate, gate_rows, alpha, beta, eps, dropout, rng, site, row0, stats):
+    who, one = "join_forward", u if u is not None else x
+    if one is None:
+        _bad(who, "u or x is needed")
+    dt, prec, cols = one.dtype, _precision(who, one), one.shape[-1] if one.dim() else 0
+    rows = _rows(who, "u" if u is not None else "x", one, cols, dt, cur)[0]
+    ldu, ldx, lds, ldy = (0 if t is None else _same_rows(who, n, t, rows, cols, dt, cur) for n, t in (("u", u), ("x", x), ("s", s), ("y", y)))
+    for n, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("b_pre", b_pre)):
+        _floats(who, n, t, cols, cur)
+    _floats(who, "stats", stats, 4 * rows, cur)
+    _words(who, rng, dropout, cur)
+    ldg = _gate(who, "gate", gate, gate_rows, rows, cols, dt, cur)
+    d = JoinDesc(rows, cols, prec, post, pre, eps, alpha, beta, site, dropout, row0, gate_rows, ldu, ldx, lds, ldy, ldg, 0, 0, 0, 0)
+    return _remember(key, (C.byref(d), 0))
+
+
+def ftp_join_forward(u, x, s, y=None, post=NORM_RMS, pre=NORM_RMS, w_post=None, b_post=None, w_pre=None, b_pre=None, gate=None, gate_rows=0, alpha=1.0,
+                     beta=1.0, eps=1e-6, dropout=0.0, rng=None, site=0, row0=0, stats=None, stream=None):
+    """s = alpha x + beta gate drop(post(u)), y = pre(s).  u None: y = pre(x) alone (s None).  gate: a float vector, or with
+    gate_rows a tensor like u with a row for every gate_rows tokens.  stats: float32, (4, rows), for the backward pass.  dropout, rng,
+    site, row0: as in ftp_dropout."""
+    cur = _current()
+    key = (7, cur, post, pre, gate_rows, alpha, beta, eps, dropout, site, row0, _sig(u), _sig(x), _sig(s), _sig(y), _sig(w_post), _sig(b_post), _sig(w_pre),
+           _sig(b_pre), _sig(gate), _sig(rng), _sig(stats))
+    d, _ = _PLANS.get(key) or _plan_join_forward(key, cur, u, x, s, y, post, pre, w_post, b_post, w_pre, b_pre, gate, gate_rows, alpha, beta, eps, dropout, rng,
+                                                 site, row0, stats)
+    st = lib.ftp_join_forward(d, _addr(u), _addr(x), _addr(w_post), _addr(b_post), _addr(gate), _addr(w_pre), _addr(b_pre), _addr(rng), _addr(s), _addr(y),
+                              _addr(stats), _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def _plan_join_backward(key, cur, u, s, dy, ds, stats, du, dx, dw_post, db_post, dw_pre, db_pre, dgate, post, pre, w_post, b_post, w_pre, gate, gate_rows, alpha,
+                        beta, dropout, rng, site, row0):
+    who, one = "join_backward", dy if dy is not None else ds
+    if one is None:
+        _bad(who, "no gradient comes in")
+    dt, prec, cols = one.dtype, _precision(who, one), one.shape[-1] if one.dim() else 0
+    rows = _rows(who, "dy" if dy is not None else "ds", one, cols, dt, cur)[0]
+    ldu, lds, ldy, ldds, lddu, lddx = (0 if t is None else _same_rows(who, n, t, rows, cols, dt, cur)
+                                       for n, t in (("u", u), ("s", s), ("dy", dy), ("ds", ds), ("du", du), ("dx", dx)))
+    for n, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("dw_post", dw_post), ("db_post", db_post), ("dw_pre", dw_pre), ("db_pre", db_pre)):
+        _floats(who, n, t, cols, cur)
+    _floats(who, "stats", stats, 4 * rows, cur)
+    _words(who, rng, dropout, cur)
+    ldg = _gate(who, "gate", gate, gate_rows, rows, cols, dt, cur)
+    lddg = _gate(who, "dgate", dgate, gate_rows, rows, cols, dt, cur)
+    d, n = JoinDesc(rows, cols, prec, post, pre, 0.0, alpha, beta, site, dropout, row0, gate_rows, ldu, 0, lds, ldy, ldg, lddu, ldds, lddx, lddg), _sz()
+    _check(lib.ftp_join_workspace_bytes(C.byref(d), C.byref(n)))
+    return _remember(key, (C.byref(d), n.value))
+
+
+def ftp_join_backward(u, s, dy, ds, stats, du=None, dx=None, dw_post=None, db_post=None, dw_pre=None, db_pre=None, dgate=None, post=NORM_RMS, pre=NORM_RMS,
+                      w_post=None, b_post=None, w_pre=None, gate=None, gate_rows=0, alpha=1.0, beta=1.0, dropout=0.0, rng=None, site=0, row0=0, ws=None,
+                      stream=None):
+    """Gradients of ftp_join_forward from dy and ds, with its other arguments (s: x where u was None).  Each output may be left out."""
+    cur = _current()
+    key = (8, cur, post, pre, gate_rows, alpha, beta, dropout, site, row0, _sig(u), _sig(s), _sig(dy), _sig(ds), _sig(stats), _sig(du), _sig(dx), _sig(dw_post),
+           _sig(db_post), _sig(dw_pre), _sig(db_pre), _sig(dgate), _sig(w_post), _sig(b_post), _sig(w_pre), _sig(gate), _sig(rng))
+    d, need = _PLANS.get(key) or _plan_join_backward(key, cur, u, s, dy, ds, stats, du, dx, dw_post, db_post, dw_pre, db_pre, dgate, post, pre, w_post, b_post, w_pre,
+                                                     gate, gate_rows, alpha, beta, dropout, rng, site, row0)
+    pws, nws, keep = _workspace("join_backward", need, ws, stream, cur) if need else _NO_WS
+    st = lib.ftp_join_backward(d, _addr(u), _addr(s), _addr(w_post), _addr(b_post), _addr(gate), _addr(w_pre), _addr(stats), _addr(rng), _addr(dy), _addr(ds),
+                               _addr(du), _addr(dx), _addr(dw_post), _addr(db_post), _addr(dw_pre), _addr(db_pre), _addr(dgate), pws, nws,
+                               _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def _steps(who, name, t, shape, dt, cur):
+    """Elements between the steps of t, whose shape must be `shape`: (rows, cols), or (seqs, len, cols) with one gap throughout."""
+    if tuple(t.shape) != tuple(shape):
+        _bad(who, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dim() == 3 and not t.is_contiguous():
+        if t.dtype is not dt or t.get_device() != cur:
+            _bad(who, f"{name} must be {dt} on the current CUDA device")
+        b, n, c = t.shape
+        s0, s1, s2 = t.stride()
+        if n == 1:
+            s1 = s0                                                  # a step each: the sequences' gap is the steps'
+        if (s2 != 1 and c > 1) or s1 < c or (b > 1 and s0 != n * s1):
+            _bad(who, f"{name}: steps must be contiguous inside and the same gap apart throughout")
+        return s1
+    return _rows(who, name, t, shape[-1], dt, cur)[1]
+
+
+def _recurrence_desc(who, cur, f, act, coupled, offsets, max_len, named, states, vectors):
+    """Descriptor from f's shape; named: (name, tensor) in the order of the descriptor's pitches."""
+    if f.dim() not in (2, 3):
+        _bad(who, "f is (steps, channels) or (sequences, steps, channels)")
+    dt, prec = f.dtype, _precision(who, f)
+    cols = f.shape[-1]
+    if offsets is None:
+        seqs, n, rows = (f.shape[0], f.shape[1], 0) if f.dim() == 3 else (1, f.shape[0], 0)
+    else:
+        if f.dim() != 2:
+            _bad(who, "with offsets f is (rows, channels)")
+        if offsets.get_device() != cur or offsets.dtype is not torch.int32 or not offsets.is_contiguous() or offsets.dim() != 1 or offsets.numel() < 1:
+            _bad(who, "offsets must be a contiguous int32 vector of sequences + 1 values on the current CUDA device")
+        seqs, rows = offsets.numel() - 1, f.shape[0]
+        n = rows if max_len is None else max_len
+    pitches = [0 if t is None else _steps(who, name, t, f.shape, dt, cur) for name, t in named]
+    d = RecurrenceDesc(seqs, n, rows, cols, prec, act, int(coupled), *pitches)
+    for name, t in vectors:
+        _floats(who, name, t, seqs * cols, cur)
+    if states is not None:
+        need = _i64()
+        _check(lib.ftp_recurrence_states(C.byref(d), C.byref(need)))
+        if states.get_device() != cur or states.dtype is not torch.float32 or not states.is_contiguous() or states.numel() < need.value * cols:
+            _bad(who, f"states must be contiguous float32 of {need.value} x {cols} values on the current CUDA device")
+    return d
+
+
+def ftp_recurrence_states(rows, seqs):
+    """Rows of the tensor of kept states for `rows` steps in all of `seqs` sequences."""
+    d, n = RecurrenceDesc(seqs, 0, rows, 1, 0, 0, 0), _i64()
+    _check(lib.ftp_recurrence_states(C.byref(d), C.byref(n)))
+    return n.value
+
+
+def ftp_recurrence_forward(f, v, y, o=None, h0=None, h1=None, states=None, act=ACT_SILU, coupled=True, offsets=None, max_len=None, stream=None):
+    """h_t = a_t h_(t-1) + (1 - a_t) v_t (coupled, else + v_t), a = sigmoid(f), y = act(o) h (o None: y = h).  f, v, o, y: (sequences,
+    steps, channels), or (rows, channels): one sequence, or those that offsets (int32, sequences + 1) cut out of the rows, max_len
+    steps at most.  h0, h1: float32 states (sequences, channels) before and behind, which may be one tensor; states: float32
+    (ftp_recurrence_states(rows, sequences), channels), kept for the backward pass."""
+    cur = _current()
+    if o is None:
+        act = ACT_NONE
+    key = (9, cur, act, bool(coupled), max_len, _sig(f), _sig(v), _sig(y), _sig(o), _sig(h0), _sig(h1), _sig(states), _sig(offsets))
+    d = _PLANS.get(key) or _remember(key, C.byref(_recurrence_desc("recurrence_forward", cur, f, act, coupled, offsets, max_len, (
+        ("f", f), ("v", v), ("o", o), ("y", y)), states, (("h0", h0), ("h1", h1)))))
+    st = lib.ftp_recurrence_forward(d, f.data_ptr(), v.data_ptr(), _addr(o), _addr(h0), _addr(offsets), y.data_ptr(), _addr(h1), _addr(states),
+                                    _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def ftp_recurrence_backward(f, v, dy, states, df, dv, o=None, do=None, dh1=None, dh0=None, act=ACT_SILU, coupled=True, offsets=None, max_len=None, stream=None):
+    """Gradients of ftp_recurrence_forward from dy and dh1 (of h1), with its other arguments and the states it kept.  dh0 may be dh1."""
+    cur = _current()
+    if o is None:
+        act = ACT_NONE
+    key = (10, cur, act, bool(coupled), max_len, _sig(f), _sig(v), _sig(dy), _sig(states), _sig(df), _sig(dv), _sig(o), _sig(do), _sig(dh1), _sig(dh0),
+           _sig(offsets))
+    d = _PLANS.get(key) or _remember(key, C.byref(_recurrence_desc("recurrence_backward", cur, f, act, coupled, offsets, max_len, (
+        ("f", f), ("v", v), ("o", o), ("dy", dy), ("df", df), ("dv", dv), ("do", do)), states, (("dh1", dh1), ("dh0", dh0)))))
+    st = lib.ftp_recurrence_backward(d, f.data_ptr(), v.data_ptr(), _addr(o), states.data_ptr(), _addr(offsets), dy.data_ptr(), _addr(dh1), df.data_ptr(),
+                                     dv.data_ptr(), _addr(do), _addr(dh0), _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def _integers(who, name, t, n, cur):
+    if t is not None and (t.get_device() != cur or t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() != n):
+        _bad(who, f"{name} must be {n} contiguous int32 values on the current CUDA device")
+
+
+def _plan_logprob_forward(key, cur, logits, targets, logp, entropy, lse, top, top_logp):
+    who, vocab = "logprob_forward", logits.shape[-1] if logits.dim() else 0
+    prec = _precision(who, logits)
+    rows, ld = _rows(who, "logits", logits, vocab, logits.dtype, cur)
+    k = 0 if top is None else top.shape[-1] if top.dim() else 0
+    if top is not None and k < 1:
+        _bad(who, "top must be rows x k")
+    _integers(who, "targets", targets, rows, cur)
+    _integers(who, "top", top, rows * k, cur)
+    for n, t, size in (("logp", logp, rows), ("entropy", entropy, rows), ("lse", lse, 2 * rows), ("top_logp", top_logp, rows * k)):
+        _floats(who, n, t, size, cur)
+    return _remember(key, (rows, vocab, ld, prec, k))
+
+
+def ftp_logprob_forward(logits, targets, logp=None, entropy=None, lse=None, top=None, top_logp=None, scale=1.0, stream=None):
+    """Log probabilities of the tokens `targets` (int32) under scale * logits (rows x vocab), the rows' entropies, the likeliest
+    tokens (top: int32, rows x k) with their log probabilities, and lse (rows x 2) for the backward pass; all float32, each may be left out."""
+    cur = _current()
+    key = (11, cur, _sig(logits), _sig(targets), _sig(logp), _sig(entropy), _sig(lse), _sig(top), _sig(top_logp))
+    rows, vocab, ld, prec, k = _PLANS.get(key) or _plan_logprob_forward(key, cur, logits, targets, logp, entropy, lse, top, top_logp)
+    st = lib.ftp_logprob_forward(logits.data_ptr(), rows, vocab, ld, prec, scale, _addr(targets), _addr(logp), _addr(entropy), _addr(lse), _addr(top),
+                                 _addr(top_logp), k, _raw_stream(stream, cur))
+    if st:
+        _check(st)
+
+
+def _plan_logprob_backward(key, cur, logits, targets, lse, dlogp, dlogits, entropy, dentropy):
+    who, vocab = "logprob_backward", logits.shape[-1] if logits.dim() else 0
+    prec = _precision(who, logits)
+    rows, ld = _rows(who, "logits", logits, vocab, logits.dtype, cur)
+    ldd = _same_rows(who, "dlogits", dlogits, rows, vocab, logits.dtype, cur)
+    _integers(who, "targets", targets, rows, cur)
+    for n, t, size in (("lse", lse, 2 * rows), ("dlogp", dlogp, rows), ("entropy", entropy, rows), ("dentropy", dentropy, rows)):
+        _floats(who, n, t, size, cur)
+    return _remember(key, (rows, vocab, ld, prec, ldd))
+
+
+def ftp_logprob_backward(logits, targets, lse, dlogp, dlogits, entropy=None, dentropy=None, scale=1.0, stream=None):
+    """Gradient of the logits from dlogp and dentropy (each may be None) with what ftp_logprob_forward left; dlogits may be logits."""
+    cur = _current()
+    key = (12, cur, _sig(logits), _sig(targets), _sig(lse), _sig(dlogp), _sig(dlogits), _sig(entropy), _sig(dentropy))
+    rows, vocab, ld, prec, ldd = _PLANS.get(key) or _plan_logprob_backward(key, cur, logits, targets, lse, dlogp, dlogits, entropy, dentropy)
+    st = lib.ftp_logprob_backward(logits.data_ptr(), rows, vocab, ld, prec, scale, _addr(targets), _addr(lse), _addr(entropy), _addr(dlogp), _addr(dentropy),
+                                  dlogits.data_ptr(), ldd, _raw_stream(stream, cur))
+    if st:
+        _check(st)
 
 
 def ftp_kernel_name(k):
