@@ -2,10 +2,11 @@
 // pass over the tokens each way; and dropout by itself.
 //
 // Bound by memory: the forward pass reads u, x and writes s, y; the backward pass reads u, s, dy, ds and writes du, dx.  A row lies
-// in the registers of 32 to 512 threads (16 bytes of columns each, one to eight times), a block of 512 threads holds one row or
-// several; every sum over a row is one exchange between its warps.  The column sums of the backward pass (gradients of the norms'
-// weights and of a gate that many rows share) grow in shared memory, each thread its own columns, over at most 64 rows, and a
-// second kernel adds the blocks' sums in double, in a fixed order.
+// in the registers of 32 to 512 threads, which take 16 bytes of columns one to eight times; a sum over a row is five shuffles, one
+// exchange between its warps and up to four shuffles more.  Threads with many columns make these cheap and leave more rows in flight;
+// a single row is spread over more threads.  The column sums of the backward pass (gradients of the norms' weights and of a gate that many
+// rows share) grow in shared memory, each thread its own columns, over at most 64 rows, and a second kernel adds the blocks' sums in
+// double, in a fixed order.
 #include <algorithm>
 #include "token.cuh"
 
@@ -13,7 +14,6 @@ namespace ftp {
 namespace token {
 namespace {
 
-constexpr int THREADS = 512;
 enum { SUM_W_PRE, SUM_B_PRE, SUM_W_POST, SUM_B_POST, SUM_GATE, SUMS };
 
 struct JoinArgs {
@@ -22,130 +22,210 @@ struct JoinArgs {
     const float *w_post, *b_post, *w_pre, *b_pre;
     float* stats;                            // four planes of `rows`: mean and 1 / deviation of u, of s
     int64_t rows, ldu, ldx, lds, ldy, ldg, lddu, ldds, lddx, lddg, gate_rows;
-    int cols, threads, post, pre;
+    int cols, threads, post, pre, full;          // full: no thread has columns behind the last one
     float eps, alpha, beta, per_col;         // per_col: 1 / cols
     Drop drop;
     // backward
     float *sums, *gate_sums, *spill;         // blocks' column sums; a shared gate's sums; the running sums where shared memory is too small
     float* out[SUMS];                        // where the column sums go when there is one block
     int at[SUMS], nsums, run;                // place of each sum or -1; rows of a run (the rows that one row's threads walk)
-    int64_t runs;
 };
 
+// A row; its number is the same in all threads of a block, so that its address stays in uniform registers.
+template <typename T> __device__ __forceinline__ const T* in_row(const void* base, int64_t ld, int64_t row) { return static_cast<const T*>(base) + row * ld; }
+template <typename T> __device__ __forceinline__ T* out_row(void* base, int64_t ld, int64_t row) { return static_cast<T*>(base) + row * ld; }
 // a row of the gate: a float vector, or a row of the tensors' type for every gate_rows rows
-template <typename T, bool VEC> __device__ __forceinline__ void gate_of(const JoinArgs& a, int64_t row, int t, int g, float (&v)[V<T>]) {
-    if (!a.gate || a.gate_rows == 0) fetch_vector<T, VEC>(static_cast<const float*>(a.gate), 1.f, t, a.threads, g, a.cols, v);
+template <typename T, bool VEC> __device__ __forceinline__ void gate_of(const JoinArgs& a, int64_t row, int t, int g, F2 (&v)[P<T>]) {
+    if (a.gate_rows == 0) fetch_vector<T, VEC>(static_cast<const float*>(a.gate), t, a.threads, g, a.cols, v);
     else decode<T>(fetch<T, VEC>(static_cast<const T*>(a.gate) + row / a.gate_rows * a.ldg, t, a.threads, g, a.cols), v);
 }
 
-// 1 / deviation and mean of the rows in v; what lies behind the last column is 0 and stays out of the sums
-template <typename T, int G, bool VEC> __device__ __forceinline__ float2 moments(const JoinArgs& a, int kind, const float (&v)[G][V<T>], int t, RowSum& sum) {
-    float mean = 0.f, q = 0.f;
+// What lies behind the last column becomes 0.
+template <typename T, bool VEC> __device__ __forceinline__ void clip(int t, int threads, int g, int cols, F2 (&v)[P<T>]) {
+    if constexpr (VEC) {
+        if (column<T, true>(t, threads, g, 0) >= cols)
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) v[j] = 0ull;
+    } else {
+#pragma unroll
+        for (int j = 0; j < P<T>; ++j) {
+            const float2 p = parts(v[j]);
+            v[j] = f2(column<T, false>(t, threads, g, 2 * j) < cols ? p.x : 0.f, column<T, false>(t, threads, g, 2 * j + 1) < cols ? p.y : 0.f);
+        }
+    }
+}
+
+template <typename T, int G, bool VEC> __device__ __forceinline__ void clip_row(const JoinArgs& a, int t, F2 (&v)[G][P<T>]) {
+    if (a.full) return;
+#pragma unroll
+    for (int g = 0; g < G; ++g) clip<T, VEC>(t, a.threads, g, a.cols, v[g]);
+}
+
+// mean and 1 / deviation of the rows in v (0 behind the last column)
+template <typename T, int G, bool VEC> __device__ __forceinline__ float2 moments(const JoinArgs& a, int kind, const F2 (&v)[G][P<T>], int t, RowSum& sum) {
+    float mean = 0.f;
+    F2 q = 0ull;
     if (kind == FTP_NORM_LAYER) {
-        float p = 0.f;
+        F2 p = 0ull;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int j = 0; j < V<T>; ++j) p += v[g][j];
-        mean = sum(p, 0.f).x * a.per_col;
+            for (int j = 0; j < P<T>; ++j) p = add2(p, v[g][j]);
+        mean = sum(sum2(p)) * a.per_col;
+        const F2 less = f2(-mean);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            F2 d[P<T>];
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) d[j] = add2(v[g][j], less);
+            if (!a.full) clip<T, VEC>(t, a.threads, g, a.cols, d);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) q = fma2(d[j], d[j], q);
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) q = fma2(v[g][j], v[g][j], q);
     }
+    return make_float2(mean, 1.f / sqrtf(fmaf(sum(sum2(q)), a.per_col, a.eps)));
+}
+// v * c or v + c over all groups of a row
+template <typename T, int G, bool VEC> __device__ __forceinline__ void scale_by(const JoinArgs& a, const float* w, int t, F2 (&v)[G][P<T>]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        F2 c[P<T>];
+        fetch_vector<T, VEC>(w, t, a.threads, g, a.cols, c);
+#pragma unroll
+        for (int j = 0; j < P<T>; ++j) v[g][j] = mul2(v[g][j], c[j]);
+    }
+}
+template <typename T, int G, bool VEC> __device__ __forceinline__ void shift_by(const JoinArgs& a, const float* b, int t, F2 (&v)[G][P<T>]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        F2 c[P<T>];
+        fetch_vector<T, VEC>(b, t, a.threads, g, a.cols, c);
+#pragma unroll
+        for (int j = 0; j < P<T>; ++j) v[g][j] = add2(v[g][j], c[j]);
+    }
+}
+template <typename T, int G, bool VEC> __device__ __forceinline__ void gate_by(const JoinArgs& a, int64_t row, int t, F2 (&v)[G][P<T>]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        F2 c[P<T>];
+        gate_of<T, VEC>(a, row, t, g, c);
+#pragma unroll
+        for (int j = 0; j < P<T>; ++j) v[g][j] = mul2(v[g][j], c[j]);
+    }
+}
+// (v - mean) / deviation * w + b
+template <typename T, int G, bool VEC>
+__device__ __forceinline__ void apply(const JoinArgs& a, float2 m, const float* w, const float* b, int t, F2 (&v)[G][P<T>]) {
+    const F2 r = f2(m.y), less = f2(-m.x * m.y);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int j = 0; j < V<T>; ++j) {
-            const float d = VEC ? (column<T, VEC>(t, a.threads, g, 0) < a.cols ? v[g][j] - mean : 0.f) : (column<T, VEC>(t, a.threads, g, j) < a.cols ? v[g][j] - mean : 0.f);
-            q = fmaf(d, d, q);
-        }
-    return make_float2(mean, 1.f / sqrtf(fmaf(sum(q, 0.f).x, a.per_col, a.eps)));
+        for (int j = 0; j < P<T>; ++j) v[g][j] = fma2(v[g][j], r, less);
+    if (w) scale_by<T, G, VEC>(a, w, t, v);
+    if (b) shift_by<T, G, VEC>(a, b, t, v);
+}
+template <typename T, int G, bool VEC>
+__device__ __forceinline__ void fetch_row(const JoinArgs& a, const T* row, int t, uint4 (&r)[G]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) r[g] = fetch<T, VEC>(row, t, a.threads, g, a.cols);
+}
+template <typename T, int G, bool VEC>
+__device__ __forceinline__ void put_row(const JoinArgs& a, T* row, int t, const F2 (&v)[G][P<T>]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) put<T, VEC>(row, t, a.threads, g, a.cols, encode<T>(v[g]));
+}
+template <typename T, int G> __device__ __forceinline__ void decode_row(const uint4 (&r)[G], F2 (&v)[G][P<T>]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) decode<T>(r[g], v[g]);
 }
 
+// Threads resident on a multiprocessor, by the columns of a thread: what their registers leave (64, 80 and 128 a thread).
+constexpr int forward_threads(int columns) { return columns <= 8 ? 1024 : columns <= 16 ? 768 : 512; }
+constexpr int backward_threads(int columns) { return columns <= 8 ? 1024 : 512; }
+
 template <typename T, int G, bool VEC>
-__global__ void __launch_bounds__(THREADS, G == 1 ? 3 : G == 2 ? 2 : 1) join_forward_kernel(const JoinArgs a) {
+__global__ void __launch_bounds__(forward_threads(G * V<T>)) join_forward_kernel(const JoinArgs a) {
     __shared__ float2 red[32];
+    __shared__ Rounds keys;
     grid_dep_sync();
-    Drop drop = a.drop;
-    drop.begin();
-    RowSum sum{red, a.threads, 0};
-    const int t = threadIdx.x & (a.threads - 1), slot = threadIdx.x / a.threads, slots = THREADS / a.threads;
-    for (int64_t r0 = (int64_t)blockIdx.x * slots; r0 < a.rows; r0 += (int64_t)gridDim.x * slots) {
-        const bool on = r0 + slot < a.rows;
-        const int64_t row = on ? r0 + slot : a.rows - 1;
-        float v[G][V<T>];
-        uint4 x[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            x[g] = a.x ? fetch<T, VEC>(static_cast<const T*>(a.x) + row * a.ldx, t, a.threads, g, a.cols) : make_uint4(0u, 0u, 0u, 0u);
-            decode<T>(a.u ? fetch<T, VEC>(static_cast<const T*>(a.u) + row * a.ldu, t, a.threads, g, a.cols) : x[g], v[g]);
-        }
+    const Dropping drop(a.drop, keys);
+    RowSum sum{red, 0};
+    const int t = threadIdx.x;
+    const F2 f = f2(drop.cut ? a.beta * a.drop.factor : a.beta), alpha = f2(a.alpha);
+    int64_t row = blockIdx.x;
+    const int64_t step = gridDim.x;
+    uint4 ru[G], rx[G];
+    if (a.u) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row), t, ru);
+    if (a.x) fetch_row<T, G, VEC>(a, in_row<T>(a.x, a.ldx, row), t, rx);
+    for (; row < a.rows; row += step) {
+        F2 v[G][P<T>];
+        const bool more = row + step < a.rows;                       // the next row's loads start as soon as this one's values are taken
         if (a.u) {
+            decode_row<T, G>(ru, v);
+            if (more) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row + step), t, ru);
+            clip_row<T, G, VEC>(a, t, v);
             if (a.post != FTP_NORM_NONE) {
                 const float2 m = moments<T, G, VEC>(a, a.post, v, t, sum);
-                if (a.stats && on && t == 0) { a.stats[row] = m.x; a.stats[a.rows + row] = m.y; }
+                if (a.stats && t == 0) { a.stats[row] = m.x; a.stats[a.rows + row] = m.y; }
+                apply<T, G, VEC>(a, m, a.w_post, a.b_post, t, v);
+            }
+            if (a.gate) gate_by<T, G, VEC>(a, row, t, v);
+            if (drop.cut) {
+                const unsigned long long first = drop.first_of(row, a.cols);
+#pragma unroll
+                for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(first, t, a.threads, g, v[g]);
+            }
+            if (a.x) {
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    float w[V<T>], b[V<T>];
-                    fetch_vector<T, VEC>(a.w_post, 1.f, t, a.threads, g, a.cols, w);
-                    fetch_vector<T, VEC>(a.b_post, 0.f, t, a.threads, g, a.cols, b);
+                    F2 r[P<T>];
+                    decode<T>(rx[g], r);
 #pragma unroll
-                    for (int j = 0; j < V<T>; ++j) v[g][j] = fmaf((v[g][j] - m.x) * m.y, w[j], b[j]);
+                    for (int j = 0; j < P<T>; ++j) v[g][j] = fma2(v[g][j], f, mul2(r[j], alpha));
                 }
-            }
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                float w[V<T>], r[V<T>];
-                gate_of<T, VEC>(a, row, t, g, w);
-                const unsigned keep = drop.cut ? drop.keep<T, VEC>(row, t, a.threads, g, a.cols) : ~0u;
-                const float f = drop.cut ? drop.factor : 1.f;
-                decode<T>(x[g], r);
-#pragma unroll
-                for (int j = 0; j < V<T>; ++j) {
-                    const float d = keep >> j & 1 ? v[g][j] * f : 0.f;
-                    v[g][j] = fmaf(a.beta, d * w[j], a.alpha * r[j]);
-                }
-                x[g] = encode<T>(v[g]);                              // the stream goes on in the tensors' type, here too
-                if (on) put<T, VEC>(static_cast<T*>(a.s) + row * a.lds, t, a.threads, g, a.cols, x[g]);
-                decode<T>(x[g], v[g]);
-            }
-        }
-        if (a.pre != FTP_NORM_NONE) {
-            if constexpr (VEC) {
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                    if (column<T, VEC>(t, a.threads, g, 0) >= a.cols)
-#pragma unroll
-                        for (int j = 0; j < V<T>; ++j) v[g][j] = 0.f;
+                if (more) fetch_row<T, G, VEC>(a, in_row<T>(a.x, a.ldx, row + step), t, rx);
             } else {
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int j = 0; j < V<T>; ++j)
-                        if (column<T, VEC>(t, a.threads, g, j) >= a.cols) v[g][j] = 0.f;
+                    for (int j = 0; j < P<T>; ++j) v[g][j] = mul2(v[g][j], f);
             }
-            const float2 m = moments<T, G, VEC>(a, a.pre, v, t, sum);
-            if (a.stats && on && t == 0) { a.stats[2 * a.rows + row] = m.x; a.stats[3 * a.rows + row] = m.y; }
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                float w[V<T>], b[V<T>];
-                fetch_vector<T, VEC>(a.w_pre, 1.f, t, a.threads, g, a.cols, w);
-                fetch_vector<T, VEC>(a.b_pre, 0.f, t, a.threads, g, a.cols, b);
-#pragma unroll
-                for (int j = 0; j < V<T>; ++j) w[j] = fmaf((v[g][j] - m.x) * m.y, w[j], b[j]);
-                if (on) put<T, VEC>(static_cast<T*>(a.y) + row * a.ldy, t, a.threads, g, a.cols, encode<T>(w));
+                const uint4 to = encode<T>(v[g]);                    // the stream goes on in the tensors' type, here too
+                put<T, VEC>(out_row<T>(a.s, a.lds, row), t, a.threads, g, a.cols, to);
+                decode<T>(to, v[g]);
             }
+        } else {
+            decode_row<T, G>(rx, v);
+            if (more) fetch_row<T, G, VEC>(a, in_row<T>(a.x, a.ldx, row + step), t, rx);
+        }
+        if (a.pre != FTP_NORM_NONE) {
+            clip_row<T, G, VEC>(a, t, v);
+            const float2 m = moments<T, G, VEC>(a, a.pre, v, t, sum);
+            if (a.stats && t == 0) { a.stats[2 * a.rows + row] = m.x; a.stats[3 * a.rows + row] = m.y; }
+            apply<T, G, VEC>(a, m, a.w_pre, a.b_pre, t, v);
+            put_row<T, G, VEC>(a, out_row<T>(a.y, a.ldy, row), t, v);
         }
     }
 }
 
-// A thread's running sum number `i` (of V columns): float4s that lie a block's width apart
+// A thread's running sum number `i` (of V columns): float4s that lie a block's width apart.  Only the widest rows may have theirs in
+// global memory.
 template <typename T> struct Running {
     float4* at;
-    __device__ __forceinline__ float4& q(int i, int k) const { return at[(i * (V<T> / 4) + k) * THREADS]; }
-    __device__ __forceinline__ void add(int i, const float (&v)[V<T>]) const {
+    __device__ __forceinline__ float4& q(int i, int k) const { return at[(unsigned)(i * (V<T> / 4) + k) * blockDim.x]; }
+    __device__ __forceinline__ void add(int i, const F2 (&v)[P<T>]) const {
 #pragma unroll
         for (int k = 0; k < V<T> / 4; ++k) {
-            float4 f = q(i, k);
-            f.x += v[4 * k]; f.y += v[4 * k + 1]; f.z += v[4 * k + 2]; f.w += v[4 * k + 3];
-            q(i, k) = f;
+            const float4 f = q(i, k);
+            const float2 x = parts(add2(f2(f.x, f.y), v[2 * k])), y = parts(add2(f2(f.z, f.w), v[2 * k + 1]));
+            q(i, k) = make_float4(x.x, x.y, y.x, y.y);
         }
     }
     __device__ __forceinline__ void get(int i, float (&v)[V<T>]) const {
@@ -161,24 +241,22 @@ template <typename T> struct Running {
 // D = ds + r (g - mean(g) - x^ mean(g x^)), g = dy w_pre, x^ = (s - mean) r  (mean(g) with the layer norm only)
 // dx = alpha D;  dv = beta D gate mask / (1 - p);  du from dv w_post in the same way;  dgate = beta D drop(v)
 template <typename T, int G, bool VEC>
-__global__ void __launch_bounds__(THREADS, G == 1 ? 2 : 1) join_backward_kernel(const JoinArgs a) {
+__global__ void __launch_bounds__(backward_threads(G * V<T>)) join_backward_kernel(const JoinArgs a) {
     extern __shared__ float4 dynamic[];
     __shared__ float2 red[32];
+    __shared__ Rounds keys;
     grid_dep_sync();
-    Drop drop = a.drop;
-    drop.begin();
-    RowSum sum{red, a.threads, 0};
-    const int t = threadIdx.x & (a.threads - 1), slot = threadIdx.x / a.threads, slots = THREADS / a.threads;
-    const int quads = G * (V<T> / 4);
-    const Running<T> run{(a.spill ? reinterpret_cast<float4*>(a.spill) + (size_t)blockIdx.x * a.nsums * quads * THREADS : dynamic) + threadIdx.x};
+    const Dropping drop(a.drop, keys);
+    RowSum sum{red, 0};
+    const int t = threadIdx.x;
+    Running<T> run{dynamic + t};
+    if (G * V<T> >= 32 && a.spill) run.at = reinterpret_cast<float4*>(a.spill) + (size_t)blockIdx.x * a.nsums * (G * (V<T> / 4)) * blockDim.x + t;
     for (int i = 0; i < a.nsums * G; ++i) run.clear(i);
-    const int64_t mine = (int64_t)blockIdx.x * slots + slot, first = mine * a.run;
+    const int64_t mine = blockIdx.x, first = mine * a.run, last = min(first + a.run, a.rows);
     int64_t group = a.gate_rows > 1 ? first / a.gate_rows : 0, next = a.gate_rows > 1 ? (group + 1) * a.gate_rows : 0;   // next: first row of the next group
-    for (int i = 0; i < a.run; ++i) {
-        const int64_t row = first + i;
-        const bool on = row < a.rows;
-        const int64_t safe = on ? row : a.rows - 1;
-        if (a.gate_sums && on && row == next) {                      // another group: its predecessor's sum is complete as far as this run goes
+    const F2 f = f2(drop.cut ? a.beta * a.drop.factor : a.beta), alpha = f2(a.alpha);
+    for (int64_t row = first; row < last; ++row) {
+        if (a.gate_sums && row == next) {                            // another group: its predecessor's sum is complete as far as this run goes
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float v[V<T>];
@@ -189,114 +267,125 @@ __global__ void __launch_bounds__(THREADS, G == 1 ? 2 : 1) join_backward_kernel(
             ++group;
             next += a.gate_rows;
         }
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
         uint4 ru[G], rs[G], rdy[G], rds[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            rs[g] = a.pre != FTP_NORM_NONE ? fetch<T, VEC>(static_cast<const T*>(a.s) + safe * a.lds, t, a.threads, g, a.cols) : zero;
-            rdy[g] = a.dy && on ? fetch<T, VEC>(static_cast<const T*>(a.dy) + safe * a.ldy, t, a.threads, g, a.cols) : zero;
-            rds[g] = a.ds && on ? fetch<T, VEC>(static_cast<const T*>(a.ds) + safe * a.ldds, t, a.threads, g, a.cols) : zero;
-            ru[g] = a.u ? fetch<T, VEC>(static_cast<const T*>(a.u) + safe * a.ldu, t, a.threads, g, a.cols) : zero;
-        }
-        float2 ms = make_float2(0.f, 0.f), mu = make_float2(0.f, 1.f), c = make_float2(0.f, 0.f);
-        if (a.post != FTP_NORM_NONE) mu = make_float2(a.stats[safe], a.stats[a.rows + safe]);
+        if (a.pre != FTP_NORM_NONE) fetch_row<T, G, VEC>(a, in_row<T>(a.s, a.lds, row), t, rs);
+        if (a.dy) fetch_row<T, G, VEC>(a, in_row<T>(a.dy, a.ldy, row), t, rdy);
+        if (a.ds) fetch_row<T, G, VEC>(a, in_row<T>(a.ds, a.ldds, row), t, rds);
+        if (a.u) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row), t, ru);
+        F2 d[G][P<T>], p[G][P<T>];
         if (a.pre != FTP_NORM_NONE) {
-            ms = make_float2(a.stats[2 * a.rows + safe], a.stats[3 * a.rows + safe]);
+            const float m = a.stats[2 * a.rows + row], r = a.stats[3 * a.rows + row];
+            const F2 rp = f2(r), lp = f2(-m * r);
+            F2 p1 = 0ull, p2 = 0ull;
+            decode_row<T, G>(rdy, d);
+            clip_row<T, G, VEC>(a, t, d);
+            if (a.at[SUM_B_PRE] >= 0)
+#pragma unroll
+                for (int g = 0; g < G; ++g) run.add(a.at[SUM_B_PRE] * G + g, d[g]);
+            decode_row<T, G>(rs, p);
+            if (a.at[SUM_W_PRE] >= 0)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    F2 h[P<T>];
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) h[j] = mul2(fma2(p[g][j], rp, lp), d[g][j]);
+                    run.add(a.at[SUM_W_PRE] * G + g, h);
+                }
+            if (a.w_pre) scale_by<T, G, VEC>(a, a.w_pre, t, d);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) {
+                    p[g][j] = fma2(p[g][j], rp, lp);
+                    p1 = add2(p1, d[g][j]);
+                    p2 = fma2(p[g][j], d[g][j], p2);
+                }
+            float2 c = make_float2(0.f, 0.f);
+            if (a.pre == FTP_NORM_LAYER) c = sum(sum2(p1), sum2(p2)); else c.y = sum(sum2(p2));
+            const F2 c1 = f2(-c.x * a.per_col), c2 = f2(-c.y * a.per_col);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                float s[V<T>], dy[V<T>], w[V<T>];
-                decode<T>(rs[g], s);
-                decode<T>(rdy[g], dy);
-                fetch_vector<T, VEC>(a.w_pre, 1.f, t, a.threads, g, a.cols, w);
-                if (a.at[SUM_B_PRE] >= 0 && on) run.add(a.at[SUM_B_PRE] * G + g, dy);
+                F2 e[P<T>] = {};
+                if (a.ds) decode<T>(rds[g], e);
 #pragma unroll
-                for (int j = 0; j < V<T>; ++j) {
-                    s[j] = (s[j] - ms.x) * ms.y;
-                    const float p = dy[j] * w[j];
-                    c.x += p;
-                    c.y = fmaf(p, s[j], c.y);
-                    s[j] *= dy[j];
-                }
-                if (a.at[SUM_W_PRE] >= 0 && on) run.add(a.at[SUM_W_PRE] * G + g, s);
+                for (int j = 0; j < P<T>; ++j) d[g][j] = fma2(rp, fma2(p[g][j], c2, add2(d[g][j], c1)), e[j]);
             }
-            c = sum(c.x, c.y);
-            c.x = a.pre == FTP_NORM_LAYER ? c.x * a.per_col : 0.f;
-            c.y *= a.per_col;
+        } else
+            decode_row<T, G>(rds, d);
+        clip_row<T, G, VEC>(a, t, d);
+        if (a.dx) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) p[g][j] = mul2(alpha, d[g][j]);
+            put_row<T, G, VEC>(a, out_row<T>(a.dx, a.lddx, row), t, p);
         }
-        float dv[G][V<T>];
-        float2 e = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            float d[V<T>], p[V<T>], q[V<T>];
-            decode<T>(rds[g], d);
-            if (a.pre != FTP_NORM_NONE) {
-                float w[V<T>];
-                decode<T>(rs[g], p);
-                decode<T>(rdy[g], q);
-                fetch_vector<T, VEC>(a.w_pre, 1.f, t, a.threads, g, a.cols, w);
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int j = 0; j < V<T>; ++j) d[j] = fmaf(ms.y, fmaf(q[j], w[j], -c.x) - (p[j] - ms.x) * ms.y * c.y, d[j]);
-            }
-            if (a.dx && on) {
+            for (int j = 0; j < P<T>; ++j) d[g][j] = mul2(d[g][j], f);
+        if (drop.cut) {
+            const unsigned long long n = drop.first_of(row, a.cols);
 #pragma unroll
-                for (int j = 0; j < V<T>; ++j) p[j] = a.alpha * d[j];
-                put<T, VEC>(static_cast<T*>(a.dx) + row * a.lddx, t, a.threads, g, a.cols, encode<T>(p));
-            }
-            const unsigned keep = drop.cut ? drop.keep<T, VEC>(safe, t, a.threads, g, a.cols) : ~0u;
-            const float f = drop.cut ? a.beta * drop.factor : a.beta;
-#pragma unroll
-            for (int j = 0; j < V<T>; ++j) d[j] = keep >> j & 1 ? d[j] * f : 0.f;      // beta D mask / (1 - p)
-            decode<T>(ru[g], q);
-#pragma unroll
-            for (int j = 0; j < V<T>; ++j) q[j] = (q[j] - mu.x) * mu.y;
-            if (a.dgate) {
-                float w[V<T>], b[V<T>];
-                fetch_vector<T, VEC>(a.w_post, 1.f, t, a.threads, g, a.cols, w);
-                fetch_vector<T, VEC>(a.b_post, 0.f, t, a.threads, g, a.cols, b);
-#pragma unroll
-                for (int j = 0; j < V<T>; ++j) p[j] = keep >> j & 1 ? d[j] * fmaf(q[j], w[j], b[j]) : 0.f;
-                if (a.gate_rows == 1) {
-                    if (on) put<T, VEC>(static_cast<T*>(a.dgate) + row * a.lddg, t, a.threads, g, a.cols, encode<T>(p));
-                } else if (on) run.add(a.at[SUM_GATE] * G + g, p);
-            }
-            gate_of<T, VEC>(a, safe, t, g, p);
-#pragma unroll
-            for (int j = 0; j < V<T>; ++j) d[j] *= p[j];
-            if (a.at[SUM_B_POST] >= 0 && on) run.add(a.at[SUM_B_POST] * G + g, d);
-            if (a.at[SUM_W_POST] >= 0 && on) {
-#pragma unroll
-                for (int j = 0; j < V<T>; ++j) p[j] = d[j] * q[j];
-                run.add(a.at[SUM_W_POST] * G + g, p);
-            }
-            if (a.post != FTP_NORM_NONE) {
-                fetch_vector<T, VEC>(a.w_post, 1.f, t, a.threads, g, a.cols, p);
-#pragma unroll
-                for (int j = 0; j < V<T>; ++j) {
-                    d[j] *= p[j];
-                    e.x += d[j];
-                    e.y = fmaf(d[j], q[j], e.y);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < V<T>; ++j) dv[g][j] = d[j];
+            for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(n, t, a.threads, g, d[g]);
         }
-        if (a.post != FTP_NORM_NONE && a.du) {
-            e = sum(e.x, e.y);
-            e.x = a.post == FTP_NORM_LAYER ? e.x * a.per_col : 0.f;
-            e.y *= a.per_col;
-        }
-        if (a.du && on) {
+        float m = 0.f, r = 1.f;
+        if (a.post != FTP_NORM_NONE) { m = a.stats[row]; r = a.stats[a.rows + row]; }
+        const F2 rn = f2(r), ln = f2(-m * r);
+        if (a.dgate) {
+            decode_row<T, G>(ru, p);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) p[g][j] = fma2(p[g][j], rn, ln);
+            if (a.w_post) scale_by<T, G, VEC>(a, a.w_post, t, p);
+            if (a.b_post) shift_by<T, G, VEC>(a, a.b_post, t, p);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                if (a.post != FTP_NORM_NONE) {
-                    float q[V<T>];
-                    decode<T>(ru[g], q);
 #pragma unroll
-                    for (int j = 0; j < V<T>; ++j) dv[g][j] = mu.y * (dv[g][j] - e.x - (q[j] - mu.x) * mu.y * e.y);
+                for (int j = 0; j < P<T>; ++j) p[g][j] = mul2(p[g][j], d[g][j]);
+                if (a.gate_rows != 1) run.add(a.at[SUM_GATE] * G + g, p[g]);
+            }
+            if (a.gate_rows == 1) put_row<T, G, VEC>(a, out_row<T>(a.dgate, a.lddg, row), t, p);
+        }
+        if (a.gate) gate_by<T, G, VEC>(a, row, t, d);
+        if (a.at[SUM_B_POST] >= 0)
+#pragma unroll
+            for (int g = 0; g < G; ++g) run.add(a.at[SUM_B_POST] * G + g, d[g]);
+        if (a.post != FTP_NORM_NONE) {
+            decode_row<T, G>(ru, p);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) p[g][j] = fma2(p[g][j], rn, ln);
+            if (a.at[SUM_W_POST] >= 0)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    F2 h[P<T>];
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) h[j] = mul2(p[g][j], d[g][j]);
+                    run.add(a.at[SUM_W_POST] * G + g, h);
                 }
-                put<T, VEC>(static_cast<T*>(a.du) + row * a.lddu, t, a.threads, g, a.cols, encode<T>(dv[g]));
+            if (a.w_post) scale_by<T, G, VEC>(a, a.w_post, t, d);
+            if (a.du) {
+                F2 q1 = 0ull, q2 = 0ull;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) {
+                        q1 = add2(q1, d[g][j]);
+                        q2 = fma2(p[g][j], d[g][j], q2);
+                    }
+                float2 e = make_float2(0.f, 0.f);
+                if (a.post == FTP_NORM_LAYER) e = sum(sum2(q1), sum2(q2)); else e.y = sum(sum2(q2));
+                const F2 e1 = f2(-e.x * a.per_col), e2 = f2(-e.y * a.per_col);
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) d[g][j] = mul2(rn, fma2(p[g][j], e2, add2(d[g][j], e1)));
             }
         }
+        if (a.du) put_row<T, G, VEC>(a, out_row<T>(a.du, a.lddu, row), t, d);
     }
     if (a.gate_sums && first < a.rows) {
 #pragma unroll
@@ -307,24 +396,18 @@ __global__ void __launch_bounds__(THREADS, G == 1 ? 2 : 1) join_backward_kernel(
         }
     }
     const int n = a.gate_sums ? a.nsums - 1 : a.nsums;               // a shared gate's sum comes last
-    if (!n) return;
-    __syncthreads();
-    // the block's rows joined: the threads of a row's slot take every slots-th piece
-    for (int i = slot; i < n * G; i += slots) {
-        float all[V<T>] = {};
-        for (int s = 0; s < slots; ++s) {
-            float v[V<T>];
-            Running<T>{run.at - threadIdx.x + s * a.threads + t}.get(i, v);
-#pragma unroll
-            for (int j = 0; j < V<T>; ++j) all[j] += v[j];
-        }
-        const int k = i / G;
+    for (int k = 0; k < n; ++k) {
         float* to = a.sums + ((size_t)blockIdx.x * n + k) * a.cols;
         if (gridDim.x == 1) {
 #pragma unroll
             for (int o = 0; o < SUMS; ++o) if (a.at[o] == k) to = a.out[o];
         }
-        put_vector<T, VEC>(to, t, a.threads, i - k * G, a.cols, all);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float v[V<T>];
+            run.get(k * G + g, v);
+            put_vector<T, VEC>(to, t, a.threads, g, a.cols, v);
+        }
     }
 }
 
@@ -360,9 +443,10 @@ __global__ void __launch_bounds__(128) join_gate_kernel(const float* part, int64
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) dropout_kernel(const T* x, T* y, int64_t rows, int cols, int64_t ldx, int64_t ldy, Drop drop) {
+__global__ void __launch_bounds__(256) dropout_kernel(const T* x, T* y, int64_t rows, int cols, int64_t ldx, int64_t ldy, const Drop d) {
+    __shared__ Rounds keys;
     grid_dep_sync();
-    drop.begin();
+    const Dropping drop(d, keys);
     const int t = threadIdx.x & 31;
     const unsigned per_row = (unsigned)((cols + 32 * V<T> - 1) / (32 * V<T>));           // pieces of a warp
     const int64_t total = rows * per_row;
@@ -385,12 +469,12 @@ __global__ void __launch_bounds__(256) dropout_kernel(const T* x, T* y, int64_t 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (row[u] >= rows) break;
-            float v[V<T>];
+            F2 v[P<T>];
             decode<T>(q[u], v);
             if (drop.cut) {
-                const unsigned keep = drop.keep<T, VEC>(row[u], t, 32, at[u], cols);
 #pragma unroll
-                for (int j = 0; j < V<T>; ++j) v[j] = keep >> j & 1 ? v[j] * drop.factor : 0.f;
+                for (int j = 0; j < P<T>; ++j) v[j] = mul2(v[j], f2(d.factor));
+                drop.template operator()<T, VEC>(drop.first_of(row[u], cols), t, 32, at[u], v);
             }
             put<T, VEC>(y + row[u] * ldy, t, 32, at[u], cols, encode<T>(v));
         }
@@ -419,6 +503,7 @@ void fill(JoinArgs& a, const ftp_join_desc* d) {
     a.lddu = ld(d->lddu); a.ldds = ld(d->ldds); a.lddx = ld(d->lddx); a.lddg = ld(d->lddg);
     a.gate_rows = d->gate_rows;
 }
+template <typename T> bool fills(const JoinArgs& a, int groups) { return (int64_t)a.threads * V<T> * groups == a.cols; }
 // every row of it starts on 16 bytes
 template <typename T> bool wide(const void* p, int64_t ld, int64_t rows) { return !p || (on_bytes(p, 16) && (rows <= 1 || ld * (int64_t)sizeof(T) % 16 == 0)); }
 bool wide_vectors(std::initializer_list<const void*> all) {
@@ -428,17 +513,22 @@ bool wide_vectors(std::initializer_list<const void*> all) {
 
 template <typename T, int G>
 void forward_of(const JoinArgs& a, bool vec, cudaStream_t st) {
-    const int slots = THREADS / a.threads, per_sm = G == 1 ? 3 : G == 2 ? 2 : 1;
-    const dim3 grid((unsigned)std::min<int64_t>((a.rows + slots - 1) / slots, SMS * per_sm));
-    if (vec) launch(join_forward_kernel<T, G, true>, grid, dim3(THREADS), 0, st, a);
-    else launch(join_forward_kernel<T, G, false>, grid, dim3(THREADS), 0, st, a);
+    const dim3 grid((unsigned)std::min<int64_t>(a.rows, SMS * std::min(32, forward_threads(G * V<T>) / a.threads)));
+    launch(vec ? join_forward_kernel<T, G, true> : join_forward_kernel<T, G, false>, grid, dim3(a.threads), 0, st, a);
+}
+// columns of a thread: as many groups as leave every multiprocessor 512 threads, up to 32 columns
+inline int groups_for(int64_t rows, int cols, int v) {
+    int most = 1;
+    while (most < 32 / v && rows * cols >= (int64_t)SMS * 512 * v * most * 2) most *= 2;
+    return most;
 }
 template <typename T>
 void run_forward(JoinArgs& a, cudaStream_t st) {
     int groups;
-    row_shape(a.cols, V<T>, &a.threads, &groups);
+    row_shape(a.cols, V<T>, groups_for(a.rows, a.cols, V<T>), &a.threads, &groups);
     const bool vec = a.cols % V<T> == 0 && wide<T>(a.u, a.ldu, a.rows) && wide<T>(a.x, a.ldx, a.rows) && wide<T>(a.s, a.lds, a.rows) && wide<T>(a.y, a.ldy, a.rows) &&
                      (a.gate_rows ? wide<T>(a.gate, a.ldg, 2) : on_bytes(a.gate, 16)) && wide_vectors({a.w_post, a.b_post, a.w_pre, a.b_pre});
+    a.full = fills<T>(a, groups);
     switch (groups) {
         case 1: forward_of<T, 1>(a, vec, st); break;
         case 2: forward_of<T, 2>(a, vec, st); break;
@@ -449,15 +539,14 @@ void run_forward(JoinArgs& a, cudaStream_t st) {
 
 // The backward pass's work on its rows: runs of up to 64 rows (the float additions of a running sum), short ones while there are
 // fewer than two blocks for every multiprocessor.
-struct JoinPlan { int threads, groups, slots, run; int64_t runs, blocks; };
+struct JoinPlan { int threads, groups, run; int64_t blocks; };
 JoinPlan plan_backward(const ftp_join_desc* d) {
     JoinPlan p;
-    row_shape(d->cols, d->precision == FTP_FP32 ? 4 : 8, &p.threads, &p.groups);
-    p.slots = THREADS / p.threads;
-    const int64_t want = (d->rows + (int64_t)p.slots * 2 * SMS - 1) / ((int64_t)p.slots * 2 * SMS);
-    p.run = (int)std::min<int64_t>(64, std::max<int64_t>(4, want));
-    p.runs = (d->rows + p.run - 1) / p.run;
-    p.blocks = (p.runs + p.slots - 1) / p.slots;
+    const int v = d->precision == FTP_FP32 ? 4 : 8;
+    row_shape(d->cols, v, d->cols <= 512 * v ? 1 : 16 / v, &p.threads, &p.groups);
+    const int64_t each = (int64_t)SMS * std::min(16, backward_threads(p.groups * v) / p.threads);
+    p.run = (int)std::min<int64_t>(64, std::max<int64_t>(4, (d->rows + each - 1) / each));
+    p.blocks = (d->rows + p.run - 1) / p.run;
     return p;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -465,27 +554,28 @@ constexpr size_t MOST_SMEM = 200 * 1024;
 struct JoinSpace { size_t sums, gate, spill, total; };
 JoinSpace space_of(const ftp_join_desc* d, const JoinPlan& p, int nsums) {
     const int v = d->precision == FTP_FP32 ? 4 : 8;
-    const size_t running = (size_t)nsums * p.groups * v * THREADS * 4;
+    const size_t running = (size_t)nsums * p.groups * v * p.threads * 4;
     JoinSpace s{};
     s.sums = p.blocks > 1 ? up256((size_t)p.blocks * nsums * d->cols * 4) : 0;
-    if (d->gate_rows > 1) s.gate = up256((size_t)(p.blocks * p.slots + (d->rows + d->gate_rows - 1) / d->gate_rows) * d->cols * 4);
+    if (d->gate_rows > 1) s.gate = up256((size_t)(p.blocks + (d->rows + d->gate_rows - 1) / d->gate_rows) * d->cols * 4);
     s.spill = running > MOST_SMEM ? up256((size_t)p.blocks * running) : 0;
     s.total = s.sums + s.gate + s.spill;
     return s;
 }
 
 template <typename T, int G>
-ftp_status backward_of(const JoinArgs& a, const JoinPlan& p, bool vec, cudaStream_t st, const char* who) {
-    const size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * THREADS * 4;
+ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, cudaStream_t st, const char* who) {
+    const size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * p.threads * 4;
     auto kern = vec ? join_backward_kernel<T, G, true> : join_backward_kernel<T, G, false>;
     if (smem > 40 * 1024)                                            // 48 KB with what the kernel holds beside it
         FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SMEM) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
-    launch(kern, dim3((unsigned)p.blocks), dim3(THREADS), smem, st, a);
+    launch(kern, dim3((unsigned)p.blocks), dim3(p.threads), smem, st, a);
     return FTP_OK;
 }
 template <typename T>
 ftp_status run_backward(JoinArgs& a, const JoinPlan& p, cudaStream_t st, const char* who) {
     a.threads = p.threads;
+    a.full = fills<T>(a, p.groups);
     const bool vec = a.cols % V<T> == 0 && wide<T>(a.u, a.ldu, a.rows) && wide<T>(a.s, a.lds, a.rows) && wide<T>(a.dy, a.ldy, a.rows) && wide<T>(a.ds, a.ldds, a.rows) &&
                      wide<T>(a.du, a.lddu, a.rows) && wide<T>(a.dx, a.lddx, a.rows) && (a.gate_rows ? wide<T>(a.gate, a.ldg, 2) : on_bytes(a.gate, 16)) &&
                      (a.gate_rows != 1 || wide<T>(a.dgate, a.lddg, a.rows)) && wide_vectors({a.w_post, a.b_post, a.w_pre, a.out[0], a.out[1], a.out[2], a.out[3], a.out[4]});
@@ -578,7 +668,7 @@ ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* 
     if (ftp_status r = drop_of(&a.drop, d->dropout, rng, d->site, d->row0, d->rows, d->cols, who)) return r;
     a.u = u; a.s = const_cast<void*>(s); a.gate = gate; a.dy = dy; a.ds = ds; a.du = du; a.dx = dx; a.dgate = dgate;
     a.w_post = w_post; a.b_post = b_post; a.w_pre = w_pre; a.stats = const_cast<float*>(stats);
-    a.run = p.run; a.runs = p.runs;
+    a.run = p.run;
     const bool shared_gate = dgate && d->gate_rows > 1;
     float* out[SUMS] = {dw_pre, db_pre, dw_post, db_post, d->gate_rows ? nullptr : static_cast<float*>(dgate)};
     JoinSums j{};

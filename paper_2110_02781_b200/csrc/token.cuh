@@ -72,24 +72,29 @@ __device__ __forceinline__ unsigned bits_of(bf16 v) { return __bfloat16_as_ushor
 __device__ __forceinline__ void from_bits(float* p, unsigned b) { *p = __uint_as_float(b); }
 __device__ __forceinline__ void from_bits(bf16* p, unsigned b) { *p = __ushort_as_bfloat16((unsigned short)b); }
 
+// Loads: a thread whose columns lie behind the last one gets others of the row (no load is conditional).
+template <typename T, bool VEC> __device__ __forceinline__ int column_in(int t, int threads, int g, int j, int cols) {
+    return min(column<T, VEC>(t, threads, g, j), VEC ? cols - V<T> + j : cols - 1);
+}
 template <typename T, bool VEC> __device__ __forceinline__ uint4 fetch(const T* row, int t, int threads, int g, int cols) {
     if constexpr (VEC) {
-        const int c = column<T, true>(t, threads, g, 0);
-        return c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-    } else {
+        // read once: kept out of the first cache, which is for the vectors that every row needs
+        uint4 r;
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                     : "l"(reinterpret_cast<const char*>(row) + (unsigned)column_in<T, true>(t, threads, g, 0, cols) * (unsigned)sizeof(T)) : "memory");
+        return r;
+    }
+    else {
         unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int j = 0; j < V<T>; ++j) {
-            const int c = column<T, false>(t, threads, g, j);
-            if (c < cols) w[j * (int)sizeof(T) / 4] |= bits_of(row[c]) << (sizeof(T) == 4 ? 0 : 16 * (j & 1));
-        }
+        for (int j = 0; j < V<T>; ++j) w[j * (int)sizeof(T) / 4] |= bits_of(row[column_in<T, false>(t, threads, g, j, cols)]) << (sizeof(T) == 4 ? 0 : 16 * (j & 1));
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 template <typename T, bool VEC> __device__ __forceinline__ void put(T* row, int t, int threads, int g, int cols, const uint4& r) {
     if constexpr (VEC) {
         const int c = column<T, true>(t, threads, g, 0);
-        if (c < cols) *reinterpret_cast<uint4*>(row + c) = r;
+        if (c < cols) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(row) + (unsigned)c * (unsigned)sizeof(T)) = r;
     } else {
         const unsigned w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -99,26 +104,18 @@ template <typename T, bool VEC> __device__ __forceinline__ void put(T* row, int 
         }
     }
 }
-// the same columns of a float vector; `other` where there is none, and behind the last column
-template <typename T, bool VEC> __device__ __forceinline__ void fetch_vector(const float* w, float other, int t, int threads, int g, int cols, float (&v)[V<T>]) {
-#pragma unroll
-    for (int j = 0; j < V<T>; ++j) v[j] = other;
-    if (!w) return;
+// the same columns of a float vector
+template <typename T, bool VEC> __device__ __forceinline__ void fetch_vector(const float* w, int t, int threads, int g, int cols, float (&v)[V<T>]) {
     if constexpr (VEC) {
-        const int c = column<T, true>(t, threads, g, 0);
-        if (c < cols) {
+        const char* at = reinterpret_cast<const char*>(w) + (unsigned)column_in<T, true>(t, threads, g, 0, cols) * 4u;
 #pragma unroll
-            for (int q = 0; q < V<T> / 4; ++q) {
-                const float4 f = *reinterpret_cast<const float4*>(w + c + 4 * q);
-                v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
-            }
+        for (int q = 0; q < V<T> / 4; ++q) {
+            const float4 f = reinterpret_cast<const float4*>(at)[q];
+            v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V<T>; ++j) {
-            const int c = column<T, false>(t, threads, g, j);
-            if (c < cols) v[j] = w[c];
-        }
+        for (int j = 0; j < V<T>; ++j) v[j] = w[column_in<T, false>(t, threads, g, j, cols)];
     }
 }
 template <typename T, bool VEC> __device__ __forceinline__ void put_vector(float* w, int t, int threads, int g, int cols, const float (&v)[V<T>]) {
@@ -137,38 +134,102 @@ template <typename T, bool VEC> __device__ __forceinline__ void put_vector(float
     }
 }
 
-// Sums over the `threads` (32 or a multiple) threads of a row; `red`: two places for a pair of floats per warp, used in turn, so
-// that one barrier a sum is enough.  The whole block takes part.  The order of additions depends on the thread alone.
+// Two floats at a time: the packed forms of sm_100 do an addition, product or fused product of both in one instruction.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float2 parts(F2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float sum2(F2 v) { const float2 p = parts(v); return p.x + p.y; }
+template <typename T> constexpr int P = V<T> / 2;                    // pairs of a group
+template <typename T> __device__ __forceinline__ void decode(const uint4& r, F2 (&v)[P<T>]) {
+    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+    if constexpr (sizeof(T) == 4) {
+        v[0] = f2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        v[1] = f2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2(bf_lo(w[i]), bf_hi(w[i]));
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 encode(const F2 (&v)[P<T>]) {
+    unsigned w[4];
+    if constexpr (sizeof(T) == 4) {
+        const float2 a = parts(v[0]), b = parts(v[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 a = parts(v[i]); w[i] = bf_pack(a.x, a.y); }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void fetch_vector(const float* w, int t, int threads, int g, int cols, F2 (&v)[P<T>]) {
+    float f[V<T>];
+    fetch_vector<T, VEC>(w, t, threads, g, cols, f);
+#pragma unroll
+    for (int j = 0; j < P<T>; ++j) v[j] = f2(f[2 * j], f[2 * j + 1]);
+}
+
+// Sums over the threads of a block (32 to 512, a power of two) that holds one row, through one place per warp; `red` holds two sets of
+// 16 places, used in turn, so that one barrier a sum is enough.  The order of additions depends on the thread alone.
 struct RowSum {
     float2* red;
-    int threads, turn;
+    int turn;
+    __device__ __forceinline__ float operator()(float a) {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+        const int n = blockDim.x >> 5, lane = threadIdx.x & 31;
+        if (n == 1) return a;
+        float2* at = red + turn * 16;
+        turn ^= 1;
+        if (lane == 0) at[threadIdx.x >> 5].x = a;
+        __syncthreads();
+        a = at[lane & (n - 1)].x;
+        for (int d = n >> 1; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+        return a;
+    }
     __device__ __forceinline__ float2 operator()(float a, float b) {
 #pragma unroll
         for (int d = 16; d; d >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, d);
             b += __shfl_xor_sync(0xffffffffu, b, d);
         }
-        if (threads == 32) return make_float2(a, b);
-        const int w = threadIdx.x >> 5, n = threads >> 5, first = w & ~(n - 1);
+        const int n = blockDim.x >> 5, lane = threadIdx.x & 31;
+        if (n == 1) return make_float2(a, b);
         float2* at = red + turn * 16;
         turn ^= 1;
-        if ((threadIdx.x & 31) == 0) at[w] = make_float2(a, b);
+        if (lane == 0) at[threadIdx.x >> 5] = make_float2(a, b);
         __syncthreads();
-        a = b = 0.f;
-        for (int i = 0; i < n; ++i) { a += at[first + i].x; b += at[first + i].y; }
+        const float2 q = at[lane & (n - 1)];
+        a = q.x; b = q.y;
+        for (int d = n >> 1; d; d >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, d);
+            b += __shfl_xor_sync(0xffffffffu, b, d);
+        }
         return make_float2(a, b);
     }
 };
 
 // ---- dropout ----
 // Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; SC 2011).
-__device__ __forceinline__ uint4 philox(uint4 c, unsigned k0, unsigned k1) {
+// A round: (x, y, z, w) -> (hi(z M1) ^ y ^ k0, lo(z M1), hi(x M0) ^ w ^ k1, lo(x M0)); the keys grow by a constant each.
+struct Rounds { uint4 k[5]; };                                       // the keys of two rounds each
+__device__ __forceinline__ void philox_keys(Rounds& r, int i, unsigned k0, unsigned k1) {   // those of rounds 2 i and 2 i + 1
+    k0 += 0x9E3779B9u * (2 * i);
+    k1 += 0xBB67AE85u * (2 * i);
+    r.k[i] = make_uint4(k0, k1, k0 + 0x9E3779B9u, k1 + 0xBB67AE85u);
+}
+__device__ __forceinline__ uint4 philox(uint4 c, const Rounds& r) {
 #pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        const unsigned h0 = __umulhi(c.x, 0xD2511F53u), l0 = c.x * 0xD2511F53u, h1 = __umulhi(c.z, 0xCD9E8D57u), l1 = c.z * 0xCD9E8D57u;
-        c = make_uint4(h1 ^ c.y ^ k0, l1, h0 ^ c.w ^ k1, l0);
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+    for (int i = 0; i < 5; ++i) {
+        const uint4 k = r.k[i];
+        unsigned long long p0 = (unsigned long long)c.x * 0xD2511F53u, p1 = (unsigned long long)c.z * 0xCD9E8D57u;
+        c = make_uint4((unsigned)(p1 >> 32) ^ c.y ^ k.x, (unsigned)p1, (unsigned)(p0 >> 32) ^ c.w ^ k.y, (unsigned)p0);
+        p0 = (unsigned long long)c.x * 0xD2511F53u;
+        p1 = (unsigned long long)c.z * 0xCD9E8D57u;
+        c = make_uint4((unsigned)(p1 >> 32) ^ c.y ^ k.z, (unsigned)p1, (unsigned)(p0 >> 32) ^ c.w ^ k.w, (unsigned)p0);
     }
     return c;
 }
@@ -176,35 +237,62 @@ __device__ __forceinline__ uint4 philox(uint4 c, unsigned k0, unsigned k1) {
 // least `cut`.
 struct Drop {
     const unsigned long long* rng;           // key, step
-    unsigned long long key, step;
     unsigned cut, site;
     float factor;
     int64_t row0;
-    __device__ __forceinline__ void begin() { if (cut) { key = rng[0]; step = rng[1]; } }
-    __device__ __forceinline__ unsigned keep8(unsigned long long group) const {
-        const uint4 r = philox(make_uint4((unsigned)group, (unsigned)(group >> 32) | site << 8, (unsigned)step, (unsigned)(step >> 32)), (unsigned)key,
-                               (unsigned)(key >> 32));
-        const unsigned w[4] = {r.x, r.y, r.z, r.w};
-        unsigned m = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m |= ((w[i] & 0xffffu) >= cut ? 1u : 0u) << (2 * i) | ((w[i] >> 16) >= cut ? 2u : 0u) << (2 * i);
-        return m;
+};
+// What a kernel makes of it: the rounds' keys wait in shared memory, where a call fetches them two rounds at a time (an addition
+// less per key than making them anew).
+struct Dropping {
+    const Rounds* keys;
+    unsigned long long step;
+    int64_t row0;
+    unsigned cut, site;
+    // the whole block takes part
+    __device__ __forceinline__ Dropping(const Drop& d, Rounds& shared) : keys(&shared), step(0), row0(d.row0), cut(d.cut), site(d.site << 8) {
+        if (!cut) return;
+        const unsigned long long key = d.rng[0];
+        step = d.rng[1];
+        if (threadIdx.x < 5) philox_keys(shared, threadIdx.x, (unsigned)key, (unsigned)(key >> 32));
+        __syncthreads();
     }
-    // bit j: column j of group g stays.  Whole warps, which hold columns of one row.
-    template <typename T, bool VEC> __device__ __forceinline__ unsigned keep(int64_t row, int t, int threads, int g, int cols) const {
-        const unsigned long long first = (unsigned long long)(row0 + row) * (unsigned)((cols + 7) / 8);
+    __device__ __forceinline__ uint4 bits(unsigned long long group) const {
+        return philox(make_uint4((unsigned)group, (unsigned)(group >> 32) | site, (unsigned)step, (unsigned)(step >> 32)), *keys);
+    }
+    // the number of a row's first group
+    __device__ __forceinline__ unsigned long long first_of(int64_t row, int cols) const { return (unsigned long long)(row0 + row) * (unsigned)((cols + 7) / 8); }
+    // v's columns of group g of the row whose first group of eight is number `first`: those that do not stay become 0.  Whole warps, which hold columns of one row.
+    template <typename T, bool VEC> __device__ __forceinline__ void operator()(unsigned long long first, int t, int threads, int g, F2 (&v)[P<T>]) const {
+        const unsigned high = cut << 16;                             
+        if (cut >> 16) {
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) v[j] = 0ull;
+            return;
+        }
         if constexpr (VEC) {
             const int c = column<T, true>(t, threads, g, 0);
-            const unsigned m = keep8(first + (unsigned)(c >> 3));
-            return V<T> == 8 ? m : m >> (c & 4);
+            const uint4 r = bits(first + (unsigned)(c >> 3));
+            unsigned w[4] = {r.x, r.y, r.z, r.w};
+            if (V<T> == 4 && (c & 4)) { w[0] = r.z; w[1] = r.w; }
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) {
+                const float2 p = parts(v[j]);
+                v[j] = f2((w[j] << 16) >= high ? p.x : 0.f, w[j] >= high ? p.y : 0.f);
+            }
         } else {
             // the warp's columns are V runs of 32, four groups of eight each: a lane makes one of these 4 V groups
             const int l = t & 31, base = t - l, lj = (l >> 2) & (V<T> - 1);
-            const unsigned mine = keep8(first + (unsigned)(((g * V<T> + lj) * threads + base) >> 3) + (l & 3));
-            unsigned m = 0;
+            const uint4 r = bits(first + (unsigned)(((g * V<T> + lj) * threads + base) >> 3) + (l & 3));
+            const unsigned w[4] = {r.x, r.y, r.z, r.w};
+            unsigned mine = 0;
 #pragma unroll
-            for (int j = 0; j < V<T>; ++j) m |= (__shfl_sync(0xffffffffu, mine, j * 4 + (l >> 3)) >> (l & 7) & 1u) << j;
-            return m;
+            for (int i = 0; i < 4; ++i) mine |= ((w[i] << 16) >= high ? 1u : 0u) << (2 * i) | (w[i] >= high ? 2u : 0u) << (2 * i);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) {
+                const unsigned a = __shfl_sync(0xffffffffu, mine, 8 * j + (l >> 3)), b = __shfl_sync(0xffffffffu, mine, 8 * j + 4 + (l >> 3));
+                const float2 p = parts(v[j]);
+                v[j] = f2(a >> (l & 7) & 1 ? p.x : 0.f, b >> (l & 7) & 1 ? p.y : 0.f);
+            }
         }
     }
 };
@@ -225,10 +313,10 @@ inline ftp_status drop_of(Drop* d, double p, const void* rng, int32_t site, int6
     return FTP_OK;
 }
 
-// threads of a row (32..512) and groups per thread for `cols` columns
-inline void row_shape(int cols, int v, int* threads, int* groups) {
+// threads of a row (32..512) and groups per thread (a power of two, `most` at most while that needs no more than 512 threads)
+inline void row_shape(int cols, int v, int most, int* threads, int* groups) {
     *threads = 32;
-    while (*threads < 512 && *threads * v < cols) *threads *= 2;
+    while (*threads < 512 && (int64_t)*threads * v * most < cols) *threads *= 2;
     *groups = 1;
     while ((int64_t)*threads * v * *groups < cols) *groups *= 2;
 }
