@@ -62,18 +62,19 @@ template <typename T> __device__ __forceinline__ void split(unsigned w, float (&
     else { v[0] = bf_lo(w); v[1] = bf_hi(w); }
 }
 
-// The smaller of a = 1 / (1 + e^-f) and 1 - a, with the sign bit set where that is a: both then are exact to a rounding, next to 1 and
-// to 0 alike (0 and 1 at infinities).  bf16: hardware exponential and reciprocal, 2^-21 relative.
-template <typename T> __device__ __forceinline__ float gate(float f) {
-    const float e = sizeof(T) == 4 ? expf(-fabsf(f)) : ffn::ex2_fast(fabsf(f) * -ffn::LOG2E);
-    const float s = e * (sizeof(T) == 4 ? 1.f / (1.f + e) : ffn::rcp_fast(1.f + e));
-    return __uint_as_float(__float_as_uint(s) | (__float_as_uint(f) & 0x80000000u));
+// a = 1 / (1 + e^-f) and 1 - a, each to a few roundings of itself, next to 1 and to 0 alike.  f below -79 counts as -79 (a 4e-35, 1 - a exactly
+// 1 in float), so that 0 times infinity does not arise.  bf16: hardware exponential and reciprocal, 2^-21 relative.
+template <typename T> __device__ __forceinline__ void gate(float f, float& a, float& other) {
+    float x = f * -ffn::LOG2E;
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(114.f));
+    const float e = sizeof(T) == 4 ? exp2f(x) : ffn::ex2_fast(x);
+    a = sizeof(T) == 4 ? 1.f / (1.f + e) : ffn::rcp_fast(1.f + e);
+    other = e * a;
 }
-__device__ __forceinline__ void both(float s, float& a, float& other) {
-    const float small = fabsf(s), big = 1.f - small;
-    const bool low = __float_as_uint(s) >> 31;
-    a = low ? small : big;
-    other = low ? big : small;
+// act(o): FORM 0 none, 1 SILU, 2 as `act` says
+template <typename T, int FORM> __device__ __forceinline__ float act_of(float o, int act) {
+    if (FORM == 0) return 1.f;
+    return FORM == 1 ? o * ffn::sigmoid_t<sizeof(T) == 2>(o) : ffn::act_value<sizeof(T) == 2>(o, act);
 }
 
 // rows of sequence b
@@ -134,39 +135,25 @@ template <int N, bool REVERSE> struct Join {
     }
 };
 
-// SHORT: sequences of at most one run, a warp each; otherwise a cluster per sequence and tile of channels
-template <typename T, bool VEC, bool SHORT>
-__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a) {
-    constexpr int N = LANES<T>;
-    __shared__ Map<N> maps[SHORT ? 1 : 2 * WARPS * 32], parts[SHORT ? 1 : 2 * 8 * 32];
-    grid_dep_sync();
-    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
-    unsigned ranks = 1, rank = 0;
-    if constexpr (!SHORT) {
-        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-        rank = cluster_rank();
-        if (ranks > 1) cluster_sync();                               // the other blocks' shared memory is there
-    }
-    const int64_t unit = SHORT ? (int64_t)blockIdx.x * warps + w : blockIdx.x / ranks, b = unit / a.tiles;
-    if (SHORT && b >= a.seqs) return;
-    const Lane<T, VEC> lane((int)(unit - b * a.tiles));
-    const Where seq = where(a, b);
-    float carry[N];
-    lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
-    Join<N, false> join{maps, parts, ranks, rank, 0, w, warps};
-    const int64_t stride = (int64_t)RUN * (SHORT ? 1 : warps * ranks);
-    for (int64_t t0 = SHORT ? 0 : (int64_t)RUN * (rank * warps + w), base = 0; base < seq.len; t0 += stride, base += stride) {
-        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
-        const int64_t row = seq.start + t0;
-        unsigned f[RUN], v[RUN], o[RUN];
+// The rows of a run.  WHOLE: all RUN of them are there.
+template <typename T, bool VEC, bool WHOLE>
+__device__ __forceinline__ void load_run(const void* base, int64_t row, int64_t ld, int n, const Lane<T, VEC>& lane, int cols, unsigned (&r)[RUN]) {
+    const T* p = static_cast<const T*>(base) + row * ld;
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            f[i] = i < n ? lane.get(static_cast<const T*>(a.f) + (row + i) * a.ldf, a.cols) : 0u;
-            v[i] = i < n ? lane.get(static_cast<const T*>(a.v) + (row + i) * a.ldv, a.cols) : 0u;
-            o[i] = i < n && a.o ? lane.get(static_cast<const T*>(a.o) + (row + i) * a.ldo, a.cols) : 0u;
-        }
-        float s[RUN][N];
-        Map<N> all;
+    for (int i = 0; i < RUN; ++i) r[i] = WHOLE || i < n ? lane.get(p + i * ld, cols) : 0u;
+}
+
+// One run forward: from what is loaded to its map, and from the state in front of it to its outputs.
+template <typename T, bool VEC, int FORM> struct Forward {
+    static constexpr int N = LANES<T>;
+    unsigned f[RUN], v[RUN], o[RUN];
+    float a[RUN][N], b[RUN][N];
+    template <bool WHOLE> __device__ __forceinline__ void load(const RecArgs& p, int64_t row, int n, const Lane<T, VEC>& lane) {
+        load_run<T, VEC, WHOLE>(p.f, row, p.ldf, n, lane, p.cols, f);
+        load_run<T, VEC, WHOLE>(p.v, row, p.ldv, n, lane, p.cols, v);
+        if (FORM) load_run<T, VEC, WHOLE>(p.o, row, p.ldo, n, lane, p.cols, o);
+    }
+    template <bool WHOLE> __device__ __forceinline__ void map(const RecArgs& p, int n, Map<N>& all) {
 #pragma unroll
         for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
 #pragma unroll
@@ -176,53 +163,183 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const
             split<T>(v[i], vv);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                s[i][j] = gate<T>(ff[j]);
-                if (i >= n) s[i][j] = 0.f;                           // a = 1, v = 0: passes the state on
-                if constexpr (!SHORT) {
-                    float x, y;
-                    both(s[i][j], x, y);
-                    all.b[j] = fmaf(x, all.b[j], (a.coupled ? y : 1.f) * vv[j]);
-                    all.a[j] *= x;
-                }
+                float other;
+                gate<T>(ff[j], a[i][j], other);
+                b[i][j] = p.coupled ? other * vv[j] : vv[j];
+                if (!WHOLE && i >= n) { a[i][j] = 1.f; b[i][j] = 0.f; }
+                all.b[j] = fmaf(a[i][j], all.b[j], b[i][j]);
+                all.a[j] *= a[i][j];
             }
-        }
-        float h[N];
-        if constexpr (SHORT) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) h[j] = carry[j];
-        } else join(all, carry, h);
-        if (a.states && n > 0) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h);
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            float vv[N], oo[N];
-            split<T>(v[i], vv);
-            split<T>(o[i], oo);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float x, y;
-                both(s[i][j], x, y);
-                h[j] = fmaf(x, h[j], (a.coupled ? y : 1.f) * vv[j]);
-                oo[j] = a.o ? ffn::act_value<sizeof(T) == 2>(oo[j], a.act) * h[j] : h[j];
-            }
-            if (i < n) lane.put(static_cast<T*>(a.y) + (row + i) * a.ldy, a.cols, oo);
-        }
-        if constexpr (SHORT) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) carry[j] = h[j];
         }
     }
-    if (a.h1 && (SHORT || (w == 0 && rank == 0))) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+    template <bool WHOLE> __device__ __forceinline__ void out(const RecArgs& p, int64_t row, int n, const Lane<T, VEC>& lane, float (&h)[N]) {
+        T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float oo[N];
+            if (FORM) split<T>(o[i], oo);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                h[j] = fmaf(a[i][j], h[j], b[i][j]);
+                oo[j] = FORM ? act_of<T, FORM>(oo[j], p.act) * h[j] : h[j];
+            }
+            if (WHOLE || i < n) lane.put(y + i * p.ldy, p.cols, oo);
+        }
+    }
+};
+
+// A cluster per sequence and tile of channels; `ranks` blocks of `warps` runs each walk down the sequence.
+template <typename T, bool VEC, int FORM>
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a) {
+    constexpr int N = LANES<T>;
+    __shared__ Map<N> maps[2 * WARPS * 32], parts[2 * 8 * 32];
+    grid_dep_sync();
+    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
+    unsigned ranks;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    const unsigned rank = cluster_rank();
+    if (ranks > 1) cluster_sync();                                   // the other blocks' shared memory is there
+    const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
+    const Lane<T, VEC> lane((int)(unit - b * a.tiles));
+    const Where seq = where(a, b);
+    float carry[N];
+    lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
+    Join<N, false> join{maps, parts, ranks, rank, 0, w, warps};
+    const int64_t stride = (int64_t)RUN * warps * ranks;
+    for (int64_t t0 = (int64_t)RUN * (rank * warps + w), base = 0; base < seq.len; t0 += stride, base += stride) {
+        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
+        const int64_t row = seq.start + t0;
+        Forward<T, VEC, FORM> r;
+        Map<N> all;
+        float h[N];
+        if (n == RUN) {
+            r.template load<true>(a, row, n, lane);
+            r.template map<true>(a, n, all);
+        } else {
+            r.template load<false>(a, row, n, lane);
+            r.template map<false>(a, n, all);
+        }
+        join(all, carry, h);
+        if (a.states && n > 0) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h);
+        if (n == RUN) r.template out<true>(a, row, n, lane, h); else r.template out<false>(a, row, n, lane, h);
+    }
+    if (a.h1 && w == 0 && rank == 0) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
 }
 
-template <typename T, bool VEC>
+// Sequences of at most one run, a warp each, a step at a time: a serving program's call.
+template <typename T, bool VEC, int FORM>
+__global__ void __launch_bounds__(128) recurrence_short_kernel(const RecArgs a) {
+    constexpr int N = LANES<T>;
+    grid_dep_sync();
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), b = unit / a.tiles;
+    if (b >= a.seqs) return;
+    const Lane<T, VEC> lane((int)(unit - b * a.tiles));
+    const Where seq = where(a, b);
+    float h[N];
+    lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, h);
+    if (a.states && seq.len > 0) lane.put_state(a.states + (seq.start / RUN + b) * a.cols, a.cols, h);
+    for (int64_t row = seq.start; row < seq.start + seq.len; ++row) {
+        float f[N], v[N], o[N];
+        split<T>(lane.get(static_cast<const T*>(a.f) + row * a.ldf, a.cols), f);
+        split<T>(lane.get(static_cast<const T*>(a.v) + row * a.ldv, a.cols), v);
+        if (FORM) split<T>(lane.get(static_cast<const T*>(a.o) + row * a.ldo, a.cols), o);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float x, other;
+            gate<T>(f[j], x, other);
+            h[j] = fmaf(x, h[j], a.coupled ? other * v[j] : v[j]);
+            o[j] = FORM ? act_of<T, FORM>(o[j], a.act) * h[j] : h[j];
+        }
+        lane.put(static_cast<T*>(a.y) + row * a.ldy, a.cols, o);
+    }
+    if (a.h1) lane.put_state(a.h1 + b * a.cols, a.cols, h);
+}
+
+// One run backward.  Between its two walks it keeps, per step, a and 1 - a's partner s (the smaller of both, sign bit set where it is a), the gradient g that
+// reaches h from its own output, and in shared memory h_(t-1) - v (coupled) or h_(t-1).
+template <typename T, bool VEC, int FORM> struct Backward {
+    static constexpr int N = LANES<T>;
+    unsigned f[RUN], v[RUN], o[RUN], dy[RUN];
+    float a[RUN][N], g[RUN][N];
+    template <bool WHOLE> __device__ __forceinline__ void load(const RecArgs& p, int64_t row, int n, const Lane<T, VEC>& lane) {
+        load_run<T, VEC, WHOLE>(p.f, row, p.ldf, n, lane, p.cols, f);
+        load_run<T, VEC, WHOLE>(p.v, row, p.ldv, n, lane, p.cols, v);
+        if (FORM) load_run<T, VEC, WHOLE>(p.o, row, p.ldo, n, lane, p.cols, o);
+        load_run<T, VEC, WHOLE>(p.dy, row, p.ldy, n, lane, p.cols, dy);
+    }
+    // forward through the run, then its map of what reaches it from behind
+    template <bool WHOLE> __device__ __forceinline__ void map(const RecArgs& p, int64_t row, int n, const Lane<T, VEC>& lane, float (&h)[N], float* before, Map<N>& all) {
+        T* to = static_cast<T*>(p.dout) + (FORM ? row * p.lddo : 0);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float ff[N], vv[N], oo[N];
+            split<T>(f[i], ff);
+            split<T>(v[i], vv);
+            if (FORM) split<T>(o[i], oo);
+            split<T>(dy[i], g[i]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float other;
+                gate<T>(ff[j], a[i][j], other);
+                // what the second walk multiplies by: (1 - a) (h - v), or (1 - a) h; coupled: 1 - a besides, without cancellation
+                before[(i * N + j) * (int)blockDim.x] = other * (p.coupled ? h[j] - vv[j] : h[j]);
+                if (p.coupled) before[((RUN + i) * N + j) * (int)blockDim.x] = other;
+                h[j] = fmaf(a[i][j], h[j], p.coupled ? other * vv[j] : vv[j]);
+                if (FORM == 1) {
+                    const float s = ffn::sigmoid_t<sizeof(T) == 2>(oo[j]), x = oo[j] * s;
+                    oo[j] = g[i][j] * h[j] * (s == 1.f ? 1.f : fmaf(x, 1.f - s, s));
+                    g[i][j] *= x;
+                } else if (FORM == 2) {
+                    float x, q;
+                    ffn::act_both<sizeof(T) == 2>(oo[j], p.act, x, q);
+                    oo[j] = g[i][j] * h[j] * q;
+                    g[i][j] *= x;
+                }
+                if (!WHOLE && i >= n) { a[i][j] = 1.f; g[i][j] = 0.f; }
+            }
+            if (FORM && (WHOLE || i < n)) lane.put(to + i * p.lddo, p.cols, oo);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
+#pragma unroll
+        for (int i = RUN - 1; i >= 0; --i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                all.b[j] = a[i][j] * (g[i][j] + all.b[j]);
+                all.a[j] *= a[i][j];
+            }
+    }
+    template <bool WHOLE> __device__ __forceinline__ void out(const RecArgs& p, int64_t row, int n, const Lane<T, VEC>& lane, const float* before, float (&q)[N]) {
+        T *to_f = static_cast<T*>(p.df) + row * p.lddf, *to_v = static_cast<T*>(p.dv) + row * p.lddv;
+#pragma unroll
+        for (int i = RUN - 1; i >= 0; --i) {
+            float df[N], dv[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float d = g[i][j] + q[j];
+                q[j] = a[i][j] * d;
+                df[j] = q[j] * before[(i * N + j) * (int)blockDim.x];
+                dv[j] = p.coupled ? d * before[((RUN + i) * N + j) * (int)blockDim.x] : d;
+            }
+            if (WHOLE || i < n) {
+                lane.put(to_f + i * p.lddf, p.cols, df);
+                lane.put(to_v + i * p.lddv, p.cols, dv);
+            }
+        }
+    }
+};
+
+template <typename T, bool VEC, int FORM>
 __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(const RecArgs a) {
     constexpr int N = LANES<T>;
     __shared__ Map<N> maps[2 * WARPS * 32], parts[2 * 8 * 32];
-    extern __shared__ float before[];                                // [RUN][threads][N]: h_(t-1) - v (coupled) or h_(t-1)
+    extern __shared__ float kept[];                                  // per step and channel of a thread one or two values
     grid_dep_sync();
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
-    unsigned ranks, rank = cluster_rank();
+    float* const before = kept + threadIdx.x;
+    unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    const unsigned rank = cluster_rank();
     if (ranks > 1) cluster_sync();
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const Lane<T, VEC> lane((int)(unit - b * a.tiles));
@@ -235,72 +352,19 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(cons
         const int64_t t0 = base + (int64_t)RUN * (rank * warps + w);
         const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
         const int64_t row = seq.start + t0;
-        unsigned f[RUN], v[RUN], o[RUN], dy[RUN];
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            f[i] = i < n ? lane.get(static_cast<const T*>(a.f) + (row + i) * a.ldf, a.cols) : 0u;
-            v[i] = i < n ? lane.get(static_cast<const T*>(a.v) + (row + i) * a.ldv, a.cols) : 0u;
-            o[i] = i < n && a.o ? lane.get(static_cast<const T*>(a.o) + (row + i) * a.ldo, a.cols) : 0u;
-            dy[i] = i < n ? lane.get(static_cast<const T*>(a.dy) + (row + i) * a.ldy, a.cols) : 0u;
-        }
-        float h[N], s[RUN][N], g[RUN][N];
-        lane.get_state(n > 0 ? a.states + (seq.start / RUN + b + t0 / RUN) * a.cols : nullptr, a.cols, h);
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            float ff[N], vv[N], oo[N];
-            split<T>(f[i], ff);
-            split<T>(v[i], vv);
-            split<T>(o[i], oo);
-            split<T>(dy[i], g[i]);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                s[i][j] = gate<T>(ff[j]);
-                if (i >= n) s[i][j] = 0.f;
-                float x, y;
-                both(s[i][j], x, y);
-                before[(i * blockDim.x + threadIdx.x) * N + j] = a.coupled ? h[j] - vv[j] : h[j];
-                h[j] = fmaf(x, h[j], (a.coupled ? y : 1.f) * vv[j]);
-                if (a.o) {
-                    float p, q;
-                    ffn::act_both<sizeof(T) == 2>(oo[j], a.act, p, q);
-                    oo[j] = g[i][j] * h[j] * q;
-                    g[i][j] *= p;
-                }
-            }
-            if (a.o && i < n) lane.put(static_cast<T*>(a.dout) + (row + i) * a.lddo, a.cols, oo);
-        }
+        Backward<T, VEC, FORM> r;
         Map<N> all;
-#pragma unroll
-        for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
-#pragma unroll
-        for (int i = RUN - 1; i >= 0; --i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float x, y;
-                both(s[i][j], x, y);
-                if (i >= n) g[i][j] = 0.f;
-                all.b[j] = x * (g[i][j] + all.b[j]);
-                all.a[j] *= x;
-            }
-        float q[N];
-        join(all, carry, q);
-#pragma unroll
-        for (int i = RUN - 1; i >= 0; --i) {
-            float df[N], dv[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float x, y;
-                both(s[i][j], x, y);
-                const float d = g[i][j] + q[j];
-                q[j] = x * d;
-                df[j] = q[j] * y * before[(i * blockDim.x + threadIdx.x) * N + j];
-                dv[j] = a.coupled ? d * y : d;
-            }
-            if (i < n) {
-                lane.put(static_cast<T*>(a.df) + (row + i) * a.lddf, a.cols, df);
-                lane.put(static_cast<T*>(a.dv) + (row + i) * a.lddv, a.cols, dv);
-            }
+        float h[N], q[N];
+        lane.get_state(n > 0 ? a.states + (seq.start / RUN + b + t0 / RUN) * a.cols : nullptr, a.cols, h);
+        if (n == RUN) {
+            r.template load<true>(a, row, n, lane);
+            r.template map<true>(a, row, n, lane, h, before, all);
+        } else {
+            r.template load<false>(a, row, n, lane);
+            r.template map<false>(a, row, n, lane, h, before, all);
         }
+        join(all, carry, q);
+        if (n == RUN) r.template out<true>(a, row, n, lane, before, q); else r.template out<false>(a, row, n, lane, before, q);
     }
     if (a.dh0 && w == 0 && rank == 0) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
 }
@@ -353,28 +417,37 @@ void shape(const RecArgs& a, int per_sm, int* warps, int* ranks) {
     }
 }
 
-template <typename T, bool VEC> ftp_status forward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+template <typename T, bool VEC, int FORM> ftp_status forward_as(const RecArgs& a, cudaStream_t st, const char* who) {
     const int64_t units = a.seqs * a.tiles;
     if (a.len <= RUN) {
         FTP_REQUIRE((units + 3) / 4 < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-        launch(recurrence_forward_kernel<T, VEC, true>, dim3((unsigned)((units + 3) / 4)), dim3(128), 0, st, a);
+        launch(recurrence_short_kernel<T, VEC, FORM>, dim3((unsigned)((units + 3) / 4)), dim3(128), 0, st, a);
         return FTP_OK;
     }
     int warps, ranks;
     shape(a, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, false>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a);
+    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, FORM>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
-template <typename T, bool VEC> ftp_status backward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& a, cudaStream_t st, const char* who) {
     const int64_t units = a.seqs * a.tiles;
     int warps, ranks;
     shape(a, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-    const cudaError_t e = launch_cluster(recurrence_backward_kernel<T, VEC>, dim3((unsigned)(units * ranks)), 32 * warps, (size_t)RUN * 32 * warps * LANES<T> * 4, ranks, st, a);
+    auto kern = recurrence_backward_kernel<T, VEC, FORM>;
+    const size_t smem = (size_t)(a.coupled ? 2 : 1) * RUN * 32 * warps * LANES<T> * 4;
+    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RUN * 32 * WARPS * LANES<T> * 4) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
+    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, a);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
+}
+template <typename T, bool VEC> ftp_status forward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    return !a.o ? forward_as<T, VEC, 0>(a, st, who) : a.act == FTP_ACT_SILU ? forward_as<T, VEC, 1>(a, st, who) : forward_as<T, VEC, 2>(a, st, who);
+}
+template <typename T, bool VEC> ftp_status backward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    return !a.o ? backward_as<T, VEC, 0>(a, st, who) : a.act == FTP_ACT_SILU ? backward_as<T, VEC, 1>(a, st, who) : backward_as<T, VEC, 2>(a, st, who);
 }
 
 }  // namespace
