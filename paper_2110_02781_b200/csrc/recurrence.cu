@@ -10,6 +10,8 @@
 // The backward pass starts every run from the state that the forward pass kept in front of it, walks it forward once and then, with
 // q_t = a_t (g_t + q_(t+1)) (g: dy act(o), q_(t+1): what reaches h_t from behind), backward in the same way.
 #include <algorithm>
+#include <type_traits>
+#include "gemm_tc_common.cuh"
 #include "token.cuh"
 
 namespace ftp {
@@ -48,6 +50,11 @@ template <typename T, bool VEC> struct Lane {
             if (c + 32 < cols) row[c + 32] = __float2bfloat16(v[1]);
         }
     }
+    // the word of two neighbours, of which the second may lie behind the last column
+    __device__ __forceinline__ void put_word(T* row, int cols, unsigned v) const {
+        if (c < cols) from_bits(row + c, v);
+        if (sizeof(T) == 2 && c + 1 < cols) from_bits(row + c + 1, v >> 16);
+    }
     __device__ __forceinline__ void get_state(const float* row, int cols, float (&v)[LANES<T>]) const {
 #pragma unroll
         for (int j = 0; j < LANES<T>; ++j) v[j] = row && at(j) < cols ? row[at(j)] : 0.f;
@@ -77,6 +84,41 @@ template <typename T, int FORM> __device__ __forceinline__ float act_of(float o,
     return FORM == 1 ? o * ffn::sigmoid_t<sizeof(T) == 2>(o) : ffn::act_value<sizeof(T) == 2>(o, act);
 }
 
+// ---- the streamed kernels: two bf16 channels of a thread in one register pair, or a float channel ----
+template <typename T> using Two = std::conditional_t<sizeof(T) == 4, float, F2>;
+using token::add2;
+using token::fma2;
+using token::mul2;
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul2(float a, float b) { return a * b; }
+__device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+template <typename T> __device__ __forceinline__ Two<T> splat(float v) { if constexpr (sizeof(T) == 4) return v; else return f2(v); }
+template <typename T> __device__ __forceinline__ Two<T> two_of(unsigned w) { if constexpr (sizeof(T) == 4) return __uint_as_float(w); else return f2(bf_lo(w), bf_hi(w)); }
+template <typename T> __device__ __forceinline__ unsigned word_of(Two<T> v) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(v);
+    else { const float2 p = parts(v); return bf_pack(p.x, p.y); }
+}
+template <typename T, typename F> __device__ __forceinline__ Two<T> each(Two<T> v, F&& f) {
+    if constexpr (sizeof(T) == 4) return f(v);
+    else { const float2 p = parts(v); return f2(f(p.x), f(p.y)); }
+}
+template <typename T> __device__ __forceinline__ Two<T> join_floats(const float (&v)[LANES<T>]) { if constexpr (sizeof(T) == 4) return v[0]; else return f2(v[0], v[1]); }
+template <typename T> __device__ __forceinline__ void to_floats(Two<T> v, float (&o)[LANES<T>]) {
+    if constexpr (sizeof(T) == 4) o[0] = v;
+    else { const float2 p = parts(v); o[0] = p.x; o[1] = p.y; }
+}
+// 1 / (1 + 2^x) and 2^x over the same
+template <typename T> __device__ __forceinline__ void sigmoids(Two<T> x, Two<T>& a, Two<T>& e) {
+    e = each<T>(x, [](float v) { return sizeof(T) == 4 ? exp2f(v) : ffn::ex2_fast(v); });
+    a = each<T>(add2(e, splat<T>(1.f)), [](float v) { return sizeof(T) == 4 ? 1.f / v : ffn::rcp_fast(v); });
+}
+template <typename T> __device__ __forceinline__ void gate2(Two<T> f, Two<T>& a, Two<T>& other) {
+    const Two<T> x = each<T>(mul2(f, splat<T>(-ffn::LOG2E)), [](float v) { asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(114.f)); return v; });
+    Two<T> e;
+    sigmoids<T>(x, a, e);
+    other = mul2(e, a);
+}
+
 // rows of sequence b
 struct Where { int64_t start, len; };
 __device__ __forceinline__ Where where(const RecArgs& a, int64_t b) {
@@ -86,7 +128,7 @@ __device__ __forceinline__ Where where(const RecArgs& a, int64_t b) {
 }
 
 // Maps of the warps' runs joined: what reaches this warp's run and what leaves the cluster's last, from what reaches its first.
-// REVERSE: the last run comes first.  `maps`: [2][WARPS][32], `parts`: [2][8][32] in shared memory, used in turn.
+// REVERSE: the last run comes first.  `maps`: [2][warps][32], `parts`: [2][ranks][32] in shared memory, used in turn.
 template <int N> struct Map { float a[N], b[N]; };
 template <int N, bool REVERSE> struct Join {
     Map<N>*maps, *parts;
@@ -94,7 +136,7 @@ template <int N, bool REVERSE> struct Join {
     int turn, w, warps;
     __device__ __forceinline__ void operator()(const Map<N>& mine, float (&carry)[N], float (&in)[N]) {
         const int lane = threadIdx.x & 31;
-        Map<N>* m = maps + turn * WARPS * 32;
+        Map<N>* m = maps + turn * warps * 32;
         m[w * 32 + lane] = mine;
         __syncthreads();
         Map<N> pre, all;
@@ -111,7 +153,7 @@ template <int N, bool REVERSE> struct Join {
 #pragma unroll
             for (int j = 0; j < N; ++j) { in[j] = fmaf(pre.a[j], carry[j], pre.b[j]); carry[j] = fmaf(all.a[j], carry[j], all.b[j]); }
         } else {
-            Map<N>* p = parts + turn * 8 * 32;
+            Map<N>* p = parts + turn * ranks * 32;
             for (unsigned r = w; r < ranks; r += warps) {            // every warp tells some of the blocks
                 const unsigned to = on_rank(smem_at(p + rank * 32 + lane), r);
 #pragma unroll
@@ -224,6 +266,298 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const
         if (n == RUN) r.template out<true>(a, row, n, lane, h); else r.template out<false>(a, row, n, lane, h);
     }
     if (a.h1 && w == 0 && rank == 0) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+}
+
+// ---- rows that start on 16 bytes: tiles through the copy engine ----
+// Every warp works on its own: its runs' 16 x 128-byte tiles come into its own part of shared memory, two iterations ahead, and its results
+// leave from there; loads hold no registers, addresses are constants, and the runs' compositions alone tie the warps together.  (Loads into
+// registers: 618 us for 65536 x 2048 bf16, 59 instructions an element, half of them addresses.)
+constexpr unsigned TILE_BYTES = RUN * 128;
+
+__device__ __forceinline__ void tile_in(unsigned to, const CUtensorMap* map, int c, int64_t row, unsigned bar) { tc::tma_load_2d(to, map, c, (int)row, bar); }
+__device__ __forceinline__ void tile_out(const CUtensorMap* map, int c, int64_t row, unsigned from) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" :: "l"(map), "r"(c), "r"((int)row), "r"(from) : "memory");
+}
+__device__ __forceinline__ void tiles_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void tiles_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }       // shared memory may be written again
+__device__ __forceinline__ void tiles_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void tiles_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+struct Maps4 { CUtensorMap m[4]; };
+
+template <typename T, int FORM>
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kernel(const __grid_constant__ Maps4 maps_in, const __grid_constant__ CUtensorMap map_y, const RecArgs a,
+                                                                                  int* err) {
+    constexpr int N = LANES<T>;
+    extern __shared__ unsigned char dynamic[];                       // per warp two stages of three tiles (f, v, o: where y is put); the maps
+    unsigned char* const smem = dynamic + (-smem_at(dynamic) & 127);
+    __shared__ uint64_t bars[WARPS][4];
+    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5, l = threadIdx.x & 31;
+    unsigned ranks;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    const unsigned rank = cluster_rank();
+    unsigned char* const mine = smem + w * 6 * TILE_BYTES;
+    Map<N>* const maps = reinterpret_cast<Map<N>*>(smem + warps * 6 * TILE_BYTES);
+    const unsigned bar = smem_at(bars[w]), tiles = smem_at(mine);
+    if (l == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tc::mbar_init(bar + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    grid_dep_sync();
+    if (ranks > 1) cluster_sync();                                   // the other blocks' shared memory is there
+    const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
+    const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
+    const Lane<T, true> lane(tile);
+    const Where seq = where(a, b);
+    float carry[N];
+    lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
+    Join<N, false> join{maps, maps + 2 * warps * 32, ranks, rank, 0, w, warps};
+    const int64_t stride = (int64_t)RUN * warps * ranks, own = (int64_t)RUN * (rank * warps + w);
+    const auto load_fv = [&](int64_t t0, int s) {
+        if (l || t0 >= seq.len) return;
+        tc::mbar_expect_tx(bar + 8 * s, 2 * TILE_BYTES);
+        tile_in(tiles + (3 * s) * TILE_BYTES, &maps_in.m[0], c, seq.start + t0, bar + 8 * s);
+        tile_in(tiles + (3 * s + 1) * TILE_BYTES, &maps_in.m[1], c, seq.start + t0, bar + 8 * s);
+    };
+    const auto load_o = [&](int64_t t0, int s) {
+        if (!FORM || l || t0 >= seq.len) return;
+        tc::mbar_expect_tx(bar + 16 + 8 * s, TILE_BYTES);
+        tile_in(tiles + (3 * s + 2) * TILE_BYTES, &maps_in.m[2], c, seq.start + t0, bar + 16 + 8 * s);
+    };
+    load_fv(own, 0);
+    load_o(own, 0);
+    load_fv(own + stride, 1);
+    bool ok = true;
+    int s = 0;
+    unsigned parity = 0;
+    for (int64_t t0 = own, base = 0; base < seq.len; t0 += stride, base += stride) {
+        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
+        const unsigned char* at = mine + 3 * s * TILE_BYTES + 4 * l;
+        Two<T> x[RUN], d[RUN];                                       // a and what is added
+        Two<T> all_a = splat<T>(1.f), all_b = splat<T>(0.f);
+        if (n > 0) {
+            ok = tc::mbar_wait(bar + 8 * s, parity, err, 0x501) && ok;
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                const Two<T> f = two_of<T>(*reinterpret_cast<const unsigned*>(at + 128 * i)), v = two_of<T>(*reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
+                Two<T> other;
+                gate2<T>(f, x[i], other);
+                d[i] = a.coupled ? mul2(other, v) : v;
+                if (i >= n) { x[i] = splat<T>(1.f); d[i] = splat<T>(0.f); }
+                all_b = fma2(x[i], all_b, d[i]);
+                all_a = mul2(all_a, x[i]);
+            }
+        }
+        __syncwarp();
+        load_fv(t0 + 2 * stride, s);
+        if (l == 0) tiles_read();                                    // the other stage's results have left
+        load_o(t0 + stride, s ^ 1);
+        Map<N> all;
+        to_floats<T>(all_a, all.a);
+        to_floats<T>(all_b, all.b);
+        float h0[N];
+        join(all, carry, h0);
+        if (n > 0) {
+            if (a.states && ok) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h0);
+            if (FORM) ok = tc::mbar_wait(bar + 16 + 8 * s, parity, err, 0x502) && ok;
+            unsigned char* const to = mine + (3 * s + 2) * TILE_BYTES + 4 * l;
+            Two<T> h = join_floats<T>(h0);
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                h = fma2(x[i], h, d[i]);
+                Two<T> y = h;
+                if (FORM) {
+                    const Two<T> o = two_of<T>(*reinterpret_cast<const unsigned*>(to + 128 * i));
+                    if (FORM == 1) {
+                        Two<T> p, e;
+                        sigmoids<T>(mul2(o, splat<T>(-ffn::LOG2E)), p, e);
+                        y = mul2(mul2(o, p), h);
+                    } else
+                        y = mul2(each<T>(o, [&](float v) { return ffn::act_value<sizeof(T) == 2>(v, a.act); }), h);
+                }
+                *reinterpret_cast<unsigned*>(to + 128 * i) = word_of<T>(y);
+            }
+            if (n == RUN) {
+                tiles_fence();
+                __syncwarp();
+                if (l == 0 && ok) { tile_out(&map_y, c, seq.start + t0, tiles + (3 * s + 2) * TILE_BYTES); tiles_commit(); }
+            } else if (ok)
+                for (int i = 0; i < n; ++i) lane.put_word(static_cast<T*>(a.y) + (seq.start + t0 + i) * a.ldy, a.cols, *reinterpret_cast<const unsigned*>(to + 128 * i));
+        }
+        parity ^= s;
+        s ^= 1;
+    }
+    if (a.h1 && w == 0 && rank == 0 && ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+    if (l == 0) tiles_done();
+}
+
+// The same backward.  Per step a thread keeps s, the smaller of a and 1 - a with the sign bit set where it is a (each of both is then exact to a
+// rounding), the gradient g that reaches h from its own output, and h_(t-1) - v (coupled) or h_(t-1).
+constexpr int BACK_WARPS = 4;
+template <typename T, int FORM>
+__global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream_kernel(const __grid_constant__ Maps4 maps_in, const __grid_constant__ Maps4 maps_out, const RecArgs a,
+                                                                                        int* err) {
+    constexpr int N = LANES<T>;
+    extern __shared__ unsigned char dynamic[];                       // per warp two stages of four tiles (f, v, o, dy: df, dv, do replace them); the maps
+    unsigned char* const smem = dynamic + (-smem_at(dynamic) & 127);
+    __shared__ uint64_t bars[BACK_WARPS][2];
+    const int warps = blockDim.x >> 5, w = threadIdx.x >> 5, l = threadIdx.x & 31;
+    unsigned ranks;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    const unsigned rank = cluster_rank();
+    unsigned char* const mine = smem + w * 8 * TILE_BYTES;
+    Map<N>* const maps = reinterpret_cast<Map<N>*>(smem + warps * 8 * TILE_BYTES);
+    const unsigned bar = smem_at(bars[w]), tiles = smem_at(mine);
+    if (l == 0) {
+        tc::mbar_init(bar, 1);
+        tc::mbar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    grid_dep_sync();
+    if (ranks > 1) cluster_sync();
+    const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
+    const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
+    const Lane<T, true> lane(tile);
+    const Where seq = where(a, b);
+    float carry[N];
+    lane.get_state(a.dh1 ? a.dh1 + b * a.cols : nullptr, a.cols, carry);
+    Join<N, true> join{maps, maps + 2 * warps * 32, ranks, rank, 0, w, warps};
+    const int64_t stride = (int64_t)RUN * warps * ranks, own = (int64_t)RUN * (rank * warps + w), last = (seq.len + stride - 1) / stride * stride - stride;
+    const auto load = [&](int64_t t0, int s) {
+        if (l || t0 < 0 || t0 >= seq.len) return;
+        tc::mbar_expect_tx(bar + 8 * s, (FORM ? 4 : 3) * TILE_BYTES);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (FORM || i != 2) tile_in(tiles + (4 * s + i) * TILE_BYTES, &maps_in.m[i], c, seq.start + t0, bar + 8 * s);
+    };
+    // only the first turn may find nothing of the sequence left for this warp: it then starts with the second
+    int64_t t0 = last + own;
+    int s = 0;
+    unsigned parity = 0;
+    const bool skip = t0 >= seq.len;
+    load(t0 - (skip ? stride : 0), 0);
+    load(t0 - (skip ? 2 : 1) * stride, 1);
+    bool ok = true;
+    for (int64_t base = last; base >= 0; base -= stride, t0 -= stride) {
+        const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
+        unsigned char* const at = mine + 4 * s * TILE_BYTES + 4 * l;
+        Two<T> k[RUN], g[RUN], d[RUN];
+        Two<T> all_a = splat<T>(1.f), all_b = splat<T>(0.f);
+        // a and 1 - a of s
+        const auto both2 = [&](Two<T> v, Two<T>& x, Two<T>& other) {
+            const Two<T> small = each<T>(v, [](float q) { return fabsf(q); }), big = add2(splat<T>(1.f), mul2(small, splat<T>(-1.f)));
+            if constexpr (N == 1) {
+                const bool low = __float_as_uint(v) >> 31;
+                x = low ? small : big;
+                other = low ? big : small;
+            } else {
+                const float2 q = parts(v), sm = parts(small), bg = parts(big);
+                const bool l0 = __float_as_uint(q.x) >> 31, l1 = __float_as_uint(q.y) >> 31;
+                x = f2(l0 ? sm.x : bg.x, l1 ? sm.y : bg.y);
+                other = f2(l0 ? bg.x : sm.x, l1 ? bg.y : sm.y);
+            }
+        };
+        if (n > 0) {
+            float h0[N];
+            lane.get_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h0);
+            Two<T> h = join_floats<T>(h0);
+            ok = tc::mbar_wait(bar + 8 * s, parity, err, 0x503) && ok;
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
+                const Two<T> f = two_of<T>(*reinterpret_cast<const unsigned*>(at + 128 * i)), v = two_of<T>(*reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
+                g[i] = two_of<T>(*reinterpret_cast<const unsigned*>(at + 3 * TILE_BYTES + 128 * i));
+                // e^-|f| / (1 + e^-|f|), with the sign of f
+                Two<T> p, e, x, other;
+                sigmoids<T>(each<T>(f, [](float q) { return fabsf(q) * -ffn::LOG2E; }), p, e);
+                p = mul2(p, e);
+                if constexpr (N == 1) k[i] = __uint_as_float(__float_as_uint(p) | (__float_as_uint(f) & 0x80000000u));
+                else {
+                    const float2 q = parts(p), r = parts(f);
+                    k[i] = f2(__uint_as_float(__float_as_uint(q.x) | (__float_as_uint(r.x) & 0x80000000u)), __uint_as_float(__float_as_uint(q.y) | (__float_as_uint(r.y) & 0x80000000u)));
+                }
+                both2(k[i], x, other);
+                d[i] = a.coupled ? fma2(v, splat<T>(-1.f), h) : h;
+                h = fma2(x, h, a.coupled ? mul2(other, v) : v);
+                if (FORM) {
+                    const Two<T> o = two_of<T>(*reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
+                    Two<T> val, slope;
+                    if (FORM == 1) {
+                        sigmoids<T>(mul2(o, splat<T>(-ffn::LOG2E)), p, e);
+                        val = mul2(o, p);
+                        slope = fma2(mul2(val, e), p, p);            // p + o p (1 - p); 1 - p = e p
+                        if constexpr (N == 1) { if (p == 1.f) slope = 1.f; if (p == 0.f) slope = 0.f; }
+                        else {
+                            const float2 q = parts(p), r = parts(slope);
+                            slope = f2(q.x == 1.f || q.x == 0.f ? q.x : r.x, q.y == 1.f || q.y == 0.f ? q.y : r.y);
+                        }
+                    } else {
+                        float oo[N], vv[N], ss[N];
+                        to_floats<T>(o, oo);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) ffn::act_both<sizeof(T) == 2>(oo[j], a.act, vv[j], ss[j]);
+                        val = join_floats<T>(vv);
+                        slope = join_floats<T>(ss);
+                    }
+                    *reinterpret_cast<unsigned*>(at + 2 * TILE_BYTES + 128 * i) = word_of<T>(mul2(mul2(g[i], h), slope));
+                    g[i] = mul2(g[i], val);
+                }
+                if (i >= n) { k[i] = splat<T>(0.f); g[i] = splat<T>(0.f); }
+            }
+#pragma unroll
+            for (int i = RUN - 1; i >= 0; --i) {
+                Two<T> x, other;
+                both2(k[i], x, other);
+                all_b = mul2(x, add2(g[i], all_b));
+                all_a = mul2(all_a, x);
+            }
+            if (FORM) tiles_fence();
+        }
+        __syncwarp();
+        if (l == 0) {
+            tiles_read();                                            // the other stage's results have left
+            if (base < last - (skip ? stride : 0)) load(t0 - stride, s ^ 1);
+            if (FORM && n == RUN && ok) { tile_out(&maps_out.m[2], c, seq.start + t0, tiles + (4 * s + 2) * TILE_BYTES); tiles_commit(); }
+        }
+        Map<N> all;
+        to_floats<T>(all_a, all.a);
+        to_floats<T>(all_b, all.b);
+        float q0[N];
+        join(all, carry, q0);
+        if (n > 0) {
+            Two<T> q = join_floats<T>(q0);
+#pragma unroll
+            for (int i = RUN - 1; i >= 0; --i) {
+                Two<T> x, other;
+                both2(k[i], x, other);
+                const Two<T> e = add2(g[i], q);
+                q = mul2(x, e);
+                *reinterpret_cast<unsigned*>(at + 128 * i) = word_of<T>(mul2(mul2(q, other), d[i]));
+                *reinterpret_cast<unsigned*>(at + TILE_BYTES + 128 * i) = word_of<T>(a.coupled ? mul2(e, other) : e);
+            }
+            if (n == RUN) {
+                tiles_fence();
+                __syncwarp();
+                if (l == 0 && ok) {
+                    tile_out(&maps_out.m[0], c, seq.start + t0, tiles + (4 * s) * TILE_BYTES);
+                    tile_out(&maps_out.m[1], c, seq.start + t0, tiles + (4 * s + 1) * TILE_BYTES);
+                    tiles_commit();
+                }
+            } else if (ok)
+                for (int i = 0; i < n; ++i) {
+                    const int64_t row = seq.start + t0 + i;
+                    lane.put_word(static_cast<T*>(a.df) + row * a.lddf, a.cols, *reinterpret_cast<const unsigned*>(at + 128 * i));
+                    lane.put_word(static_cast<T*>(a.dv) + row * a.lddv, a.cols, *reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
+                    if (FORM) lane.put_word(static_cast<T*>(a.dout) + row * a.lddo, a.cols, *reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
+                }
+            parity ^= s;
+            s ^= 1;
+        }
+    }
+    if (a.dh0 && w == 0 && rank == 0 && ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
+    if (l == 0) tiles_done();
 }
 
 // Sequences of at most one run, a warp each, a step at a time: a serving program's call.
@@ -402,11 +736,25 @@ bool pairs(std::initializer_list<const void*> ps, std::initializer_list<int64_t>
     for (int64_t ld : lds) if (ld % 2) return false;
     return cols % 2 == 0;
 }
+// every row of it starts on 16 bytes, where the copy engine can fetch tiles
+bool whole_rows(std::initializer_list<const void*> ps, std::initializer_list<int64_t> lds, size_t size, int64_t rows) {
+    for (const void* p : ps) if (!on_bytes(p, 16)) return false;
+    for (int64_t ld : lds) if (rows > 1 && ld * (int64_t)size % 16) return false;
+    return rows < (1ll << 31) - 64;
+}
+template <typename T> bool tile_map(CUtensorMap* map, const void* p, int64_t ld, const RecArgs& a) {
+    tc::EncodeTiledFn fn = tc::encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows}, strides[1] = {(cuuint64_t)((a.rows > 1 ? ld * (int64_t)sizeof(T) : (a.cols * (int64_t)sizeof(T) + 15) / 16 * 16))};
+    const cuuint32_t box[2] = {(cuuint32_t)TILE<T>, RUN}, one[2] = {1, 1};
+    return fn(map, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 // Blocks of a cluster and runs of a block: the fewest turns of the resident blocks, a turn of a cluster a tenth longer for its barrier.
-void shape(const RecArgs& a, int per_sm, int* warps, int* ranks) {
+void shape(const RecArgs& a, int most, int per_sm, int* warps, int* ranks) {
     const int64_t runs = (a.len + RUN - 1) / RUN, units = a.seqs * a.tiles;
     *warps = 1;
-    while (*warps < WARPS && *warps < runs) *warps *= 2;
+    while (*warps < most && *warps < runs) *warps *= 2;
     double best = 0;
     *ranks = 0;
     for (int s = 1; s <= 8; s *= 2) {
@@ -425,7 +773,7 @@ template <typename T, bool VEC, int FORM> ftp_status forward_as(const RecArgs& a
         return FTP_OK;
     }
     int warps, ranks;
-    shape(a, 2, &warps, &ranks);
+    shape(a, WARPS, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, FORM>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
@@ -434,7 +782,7 @@ template <typename T, bool VEC, int FORM> ftp_status forward_as(const RecArgs& a
 template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& a, cudaStream_t st, const char* who) {
     const int64_t units = a.seqs * a.tiles;
     int warps, ranks;
-    shape(a, 2, &warps, &ranks);
+    shape(a, WARPS, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     auto kern = recurrence_backward_kernel<T, VEC, FORM>;
     const size_t smem = (size_t)(a.coupled ? 2 : 1) * RUN * 32 * warps * LANES<T> * 4;
@@ -443,10 +791,51 @@ template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& 
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
+template <typename T, int FORM> ftp_status forward_stream(const RecArgs& a, cudaStream_t st, const char* who) {
+    const int64_t units = a.seqs * a.tiles;
+    int warps, ranks;
+    shape(a, WARPS, 2, &warps, &ranks);
+    FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    Maps4 in{};
+    CUtensorMap y;
+    FTP_REQUIRE(tile_map<T>(&in.m[0], a.f, a.ldf, a) && tile_map<T>(&in.m[1], a.v, a.ldv, a) && (!FORM || tile_map<T>(&in.m[2], a.o, a.ldo, a)) && tile_map<T>(&y, a.y, a.ldy, a),
+                FTP_ECUDA, "%s: cannot describe a tensor to the copy engine", who);
+    int* err = ffn::status_word();
+    FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    auto kern = recurrence_forward_stream_kernel<T, FORM>;
+    const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 6 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
+    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + 8))) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
+    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, y, a, err);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
+template <typename T, int FORM> ftp_status backward_stream(const RecArgs& a, cudaStream_t st, const char* who) {
+    const int64_t units = a.seqs * a.tiles;
+    int warps, ranks;
+    shape(a, BACK_WARPS, 3, &warps, &ranks);
+    FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    Maps4 in{}, out{};
+    FTP_REQUIRE(tile_map<T>(&in.m[0], a.f, a.ldf, a) && tile_map<T>(&in.m[1], a.v, a.ldv, a) && (!FORM || tile_map<T>(&in.m[2], a.o, a.ldo, a)) && tile_map<T>(&in.m[3], a.dy, a.ldy, a) &&
+                    tile_map<T>(&out.m[0], a.df, a.lddf, a) && tile_map<T>(&out.m[1], a.dv, a.lddv, a) && (!FORM || tile_map<T>(&out.m[2], a.dout, a.lddo, a)),
+                FTP_ECUDA, "%s: cannot describe a tensor to the copy engine", who);
+    int* err = ffn::status_word();
+    FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    auto kern = recurrence_backward_stream_kernel<T, FORM>;
+    const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 8 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
+    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + 8))) == cudaSuccess, FTP_ECUDA,
+                "%s: no shared memory", who);
+    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, out, a, err);
+    FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return FTP_OK;
+}
 template <typename T, bool VEC> ftp_status forward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    if (a.len > RUN && whole_rows({a.f, a.v, a.o, a.y}, {a.ldf, a.ldv, a.o ? a.ldo : 0, a.ldy}, sizeof(T), a.rows))
+        return !a.o ? forward_stream<T, 0>(a, st, who) : a.act == FTP_ACT_SILU ? forward_stream<T, 1>(a, st, who) : forward_stream<T, 2>(a, st, who);
     return !a.o ? forward_as<T, VEC, 0>(a, st, who) : a.act == FTP_ACT_SILU ? forward_as<T, VEC, 1>(a, st, who) : forward_as<T, VEC, 2>(a, st, who);
 }
 template <typename T, bool VEC> ftp_status backward_of(const RecArgs& a, cudaStream_t st, const char* who) {
+    if (a.len > 0 && whole_rows({a.f, a.v, a.o, a.dy, a.df, a.dv, a.dout}, {a.ldf, a.ldv, a.o ? a.ldo : 0, a.ldy, a.lddf, a.lddv, a.o ? a.lddo : 0}, sizeof(T), a.rows))
+        return !a.o ? backward_stream<T, 0>(a, st, who) : a.act == FTP_ACT_SILU ? backward_stream<T, 1>(a, st, who) : backward_stream<T, 2>(a, st, who);
     return !a.o ? backward_as<T, VEC, 0>(a, st, who) : a.act == FTP_ACT_SILU ? backward_as<T, VEC, 1>(a, st, who) : backward_as<T, VEC, 2>(a, st, who);
 }
 
