@@ -128,12 +128,37 @@ __device__ __forceinline__ Where where(const RecArgs& a, int64_t b) {
 }
 
 // Maps of the warps' runs joined: what reaches this warp's run and what leaves the cluster's last, from what reaches its first.
-// REVERSE: the last run comes first.  `maps`: [2][warps][32], `parts`: [2][ranks][32] in shared memory, used in turn.
-template <int N> struct Map { float a[N], b[N]; };
+// REVERSE: the last run comes first.  `maps`: [2][warps][32], `parts`: [2][ranks][32] in shared memory, used in turn.  The blocks of a
+// cluster send each other their part by asynchronous stores that count on the receiver's barrier (a cluster barrier waits for all
+// of a block's earlier stores to global memory: a fifth of the kernel's stalls).  A part's place is written again two turns later, after
+// this block's next part has been sent, which every warp precedes.
+template <int N> struct __align__(8 * N) Map { float a[N], b[N]; };
+__device__ __forceinline__ void send(unsigned to, unsigned bar, const Map<1>& m) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" :: "r"(to), "f"(m.a[0]), "f"(m.b[0]), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void send(unsigned to, unsigned bar, const Map<2>& m) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 :: "r"(to), "f"(m.a[0]), "f"(m.a[1]), "f"(m.b[0]), "f"(m.b[1]), "r"(bar) : "memory");
+}
 template <int N, bool REVERSE> struct Join {
     Map<N>*maps, *parts;
-    unsigned ranks, rank;
-    int turn, w, warps;
+    unsigned bars, ranks, rank;                                      // bars: a barrier for each turn
+    int w, warps;
+    int* err;
+    bool ok = true;
+    int turn = 0;
+    unsigned parity = 0;
+    // the whole cluster takes part; `pair`: shared memory of two barriers
+    __device__ __forceinline__ Join(Map<N>* at, uint64_t* pair, unsigned ranks, unsigned rank, int w, int warps, int* err)
+        : maps(at), parts(at + 2 * warps * 32), bars(smem_at(pair)), ranks(ranks), rank(rank), w(w), warps(warps), err(err) {
+        if (ranks == 1) return;
+        if (threadIdx.x == 0) {
+            tc::mbar_init(bars, 1);
+            tc::mbar_init(bars + 8, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cluster_sync();
+    }
     __device__ __forceinline__ void operator()(const Map<N>& mine, float (&carry)[N], float (&in)[N]) {
         const int lane = threadIdx.x & 31;
         Map<N>* m = maps + turn * warps * 32;
@@ -142,6 +167,7 @@ template <int N, bool REVERSE> struct Join {
         Map<N> pre, all;
 #pragma unroll
         for (int j = 0; j < N; ++j) { all.a[j] = 1.f; all.b[j] = 0.f; }
+        pre = all;
         for (int i = 0; i < warps; ++i) {
             const int k = REVERSE ? warps - 1 - i : i;
             if (k == w) pre = all;
@@ -154,15 +180,10 @@ template <int N, bool REVERSE> struct Join {
             for (int j = 0; j < N; ++j) { in[j] = fmaf(pre.a[j], carry[j], pre.b[j]); carry[j] = fmaf(all.a[j], carry[j], all.b[j]); }
         } else {
             Map<N>* p = parts + turn * ranks * 32;
-            for (unsigned r = w; r < ranks; r += warps) {            // every warp tells some of the blocks
-                const unsigned to = on_rank(smem_at(p + rank * 32 + lane), r);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(to + 4 * j), "f"(all.a[j]) : "memory");
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(to + 4 * N + 4 * j), "f"(all.b[j]) : "memory");
-                }
-            }
-            cluster_sync();
+            const unsigned bar = bars + 8 * turn;
+            if (threadIdx.x == 0) tc::mbar_expect_tx(bar, ranks * 32 * (unsigned)sizeof(Map<N>));
+            for (unsigned r = w; r < ranks; r += warps) send(on_rank(smem_at(p + rank * 32 + lane), r), on_rank(bar, r), all);   // every warp tells some of the blocks
+            ok = tc::mbar_wait(bar, parity, err, 0x500) && ok;
             for (unsigned i = 0; i < ranks; ++i) {
                 const unsigned k = REVERSE ? ranks - 1 - i : i;
                 if (k == rank)
@@ -172,6 +193,7 @@ template <int N, bool REVERSE> struct Join {
 #pragma unroll
                 for (int j = 0; j < N; ++j) carry[j] = fmaf(n.a[j], carry[j], n.b[j]);
             }
+            parity ^= turn;
         }
         turn ^= 1;
     }
@@ -232,21 +254,21 @@ template <typename T, bool VEC, int FORM> struct Forward {
 
 // A cluster per sequence and tile of channels; `ranks` blocks of `warps` runs each walk down the sequence.
 template <typename T, bool VEC, int FORM>
-__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a, int* err) {
     constexpr int N = LANES<T>;
-    __shared__ Map<N> maps[2 * WARPS * 32], parts[2 * 8 * 32];
+    __shared__ Map<N> maps[2 * (WARPS + 8) * 32];
+    __shared__ uint64_t pair[2];
     grid_dep_sync();
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
     const unsigned rank = cluster_rank();
-    if (ranks > 1) cluster_sync();                                   // the other blocks' shared memory is there
+    Join<N, false> join(maps, pair, ranks, rank, w, warps, err);
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const Lane<T, VEC> lane((int)(unit - b * a.tiles));
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
-    Join<N, false> join{maps, parts, ranks, rank, 0, w, warps};
     const int64_t stride = (int64_t)RUN * warps * ranks;
     for (int64_t t0 = (int64_t)RUN * (rank * warps + w), base = 0; base < seq.len; t0 += stride, base += stride) {
         const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
@@ -262,10 +284,12 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const
             r.template map<false>(a, n, all);
         }
         join(all, carry, h);
+        if (!join.ok) continue;
         if (a.states && n > 0) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h);
         if (n == RUN) r.template out<true>(a, row, n, lane, h); else r.template out<false>(a, row, n, lane, h);
     }
-    if (a.h1 && w == 0 && rank == 0) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+    if (a.h1 && w == 0 && rank == 0 && join.ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
 // ---- rows that start on 16 bytes: tiles through the copy engine ----
@@ -285,13 +309,13 @@ __device__ __forceinline__ void tiles_fence() { asm volatile("fence.proxy.async.
 
 struct Maps4 { CUtensorMap m[4]; };
 
-template <typename T, int FORM>
+template <typename T, int FORM, bool COUPLED>
 __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kernel(const __grid_constant__ Maps4 maps_in, const __grid_constant__ CUtensorMap map_y, const RecArgs a,
                                                                                   int* err) {
     constexpr int N = LANES<T>;
     extern __shared__ unsigned char dynamic[];                       // per warp two stages of three tiles (f, v, o: where y is put); the maps
     unsigned char* const smem = dynamic + (-smem_at(dynamic) & 127);
-    __shared__ uint64_t bars[WARPS][4];
+    __shared__ uint64_t bars[WARPS][4], pair[2];
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5, l = threadIdx.x & 31;
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
@@ -306,14 +330,13 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
     }
     __syncwarp();
     grid_dep_sync();
-    if (ranks > 1) cluster_sync();                                   // the other blocks' shared memory is there
+    Join<N, false> join(maps, pair, ranks, rank, w, warps, err);
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
     const Lane<T, true> lane(tile);
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
-    Join<N, false> join{maps, maps + 2 * warps * 32, ranks, rank, 0, w, warps};
     const int64_t stride = (int64_t)RUN * warps * ranks, own = (int64_t)RUN * (rank * warps + w);
     const auto load_fv = [&](int64_t t0, int s) {
         if (l || t0 >= seq.len) return;
@@ -344,8 +367,14 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
                 const Two<T> f = two_of<T>(*reinterpret_cast<const unsigned*>(at + 128 * i)), v = two_of<T>(*reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
                 Two<T> other;
                 gate2<T>(f, x[i], other);
-                d[i] = a.coupled ? mul2(other, v) : v;
-                if (i >= n) { x[i] = splat<T>(1.f); d[i] = splat<T>(0.f); }
+                d[i] = COUPLED ? mul2(other, v) : v;
+            }
+            if (n < RUN)
+#pragma unroll
+                for (int i = 0; i < RUN; ++i)
+                    if (i >= n) { x[i] = splat<T>(1.f); d[i] = splat<T>(0.f); }
+#pragma unroll
+            for (int i = 0; i < RUN; ++i) {
                 all_b = fma2(x[i], all_b, d[i]);
                 all_a = mul2(all_a, x[i]);
             }
@@ -359,6 +388,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
         to_floats<T>(all_b, all.b);
         float h0[N];
         join(all, carry, h0);
+        ok = ok && join.ok;
         if (n > 0) {
             if (a.states && ok) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h0);
             if (FORM) ok = tc::mbar_wait(bar + 16 + 8 * s, parity, err, 0x502) && ok;
@@ -391,18 +421,20 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
     }
     if (a.h1 && w == 0 && rank == 0 && ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
     if (l == 0) tiles_done();
+    __syncwarp();
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
-// The same backward.  Per step a thread keeps s, the smaller of a and 1 - a with the sign bit set where it is a (each of both is then exact to a
-// rounding), the gradient g that reaches h from its own output, and h_(t-1) - v (coupled) or h_(t-1).
+// The same backward.  Between its two walks a thread keeps, per step, a, 1 - a and the gradient g that reaches h from its own output in
+// registers, and (1 - a) (h_(t-1) - v) (coupled) or (1 - a) h_(t-1) in the words of the tiles of f and v that it has read.
 constexpr int BACK_WARPS = 4;
-template <typename T, int FORM>
+template <typename T, int FORM, bool COUPLED>
 __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream_kernel(const __grid_constant__ Maps4 maps_in, const __grid_constant__ Maps4 maps_out, const RecArgs a,
                                                                                         int* err) {
     constexpr int N = LANES<T>;
     extern __shared__ unsigned char dynamic[];                       // per warp two stages of four tiles (f, v, o, dy: df, dv, do replace them); the maps
     unsigned char* const smem = dynamic + (-smem_at(dynamic) & 127);
-    __shared__ uint64_t bars[BACK_WARPS][2];
+    __shared__ uint64_t bars[BACK_WARPS][2], pair[2];
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5, l = threadIdx.x & 31;
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
@@ -417,14 +449,13 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
     }
     __syncwarp();
     grid_dep_sync();
-    if (ranks > 1) cluster_sync();
+    Join<N, true> join(maps, pair, ranks, rank, w, warps, err);
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
     const Lane<T, true> lane(tile);
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.dh1 ? a.dh1 + b * a.cols : nullptr, a.cols, carry);
-    Join<N, true> join{maps, maps + 2 * warps * 32, ranks, rank, 0, w, warps};
     const int64_t stride = (int64_t)RUN * warps * ranks, own = (int64_t)RUN * (rank * warps + w), last = (seq.len + stride - 1) / stride * stride - stride;
     const auto load = [&](int64_t t0, int s) {
         if (l || t0 < 0 || t0 >= seq.len) return;
@@ -444,22 +475,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
     for (int64_t base = last; base >= 0; base -= stride, t0 -= stride) {
         const int n = (int)min((int64_t)RUN, max((int64_t)0, seq.len - t0));
         unsigned char* const at = mine + 4 * s * TILE_BYTES + 4 * l;
-        Two<T> k[RUN], g[RUN], d[RUN];
+        Two<T> x[RUN], other[RUN], g[RUN];
         Two<T> all_a = splat<T>(1.f), all_b = splat<T>(0.f);
-        // a and 1 - a of s
-        const auto both2 = [&](Two<T> v, Two<T>& x, Two<T>& other) {
-            const Two<T> small = each<T>(v, [](float q) { return fabsf(q); }), big = add2(splat<T>(1.f), mul2(small, splat<T>(-1.f)));
-            if constexpr (N == 1) {
-                const bool low = __float_as_uint(v) >> 31;
-                x = low ? small : big;
-                other = low ? big : small;
-            } else {
-                const float2 q = parts(v), sm = parts(small), bg = parts(big);
-                const bool l0 = __float_as_uint(q.x) >> 31, l1 = __float_as_uint(q.y) >> 31;
-                x = f2(l0 ? sm.x : bg.x, l1 ? sm.y : bg.y);
-                other = f2(l0 ? bg.x : sm.x, l1 ? bg.y : sm.y);
-            }
-        };
         if (n > 0) {
             float h0[N];
             lane.get_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h0);
@@ -469,30 +486,20 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
             for (int i = 0; i < RUN; ++i) {
                 const Two<T> f = two_of<T>(*reinterpret_cast<const unsigned*>(at + 128 * i)), v = two_of<T>(*reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
                 g[i] = two_of<T>(*reinterpret_cast<const unsigned*>(at + 3 * TILE_BYTES + 128 * i));
-                // e^-|f| / (1 + e^-|f|), with the sign of f
-                Two<T> p, e, x, other;
-                sigmoids<T>(each<T>(f, [](float q) { return fabsf(q) * -ffn::LOG2E; }), p, e);
-                p = mul2(p, e);
-                if constexpr (N == 1) k[i] = __uint_as_float(__float_as_uint(p) | (__float_as_uint(f) & 0x80000000u));
-                else {
-                    const float2 q = parts(p), r = parts(f);
-                    k[i] = f2(__uint_as_float(__float_as_uint(q.x) | (__float_as_uint(r.x) & 0x80000000u)), __uint_as_float(__float_as_uint(q.y) | (__float_as_uint(r.y) & 0x80000000u)));
-                }
-                both2(k[i], x, other);
-                d[i] = a.coupled ? fma2(v, splat<T>(-1.f), h) : h;
-                h = fma2(x, h, a.coupled ? mul2(other, v) : v);
+                gate2<T>(f, x[i], other[i]);
+                float keep[N];
+                to_floats<T>(mul2(other[i], COUPLED ? fma2(v, splat<T>(-1.f), h) : h), keep);
+#pragma unroll
+                for (int j = 0; j < N; ++j) *reinterpret_cast<float*>(at + j * TILE_BYTES + 128 * i) = keep[j];
+                h = fma2(x[i], h, COUPLED ? mul2(other[i], v) : v);
                 if (FORM) {
                     const Two<T> o = two_of<T>(*reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
                     Two<T> val, slope;
                     if (FORM == 1) {
-                        sigmoids<T>(mul2(o, splat<T>(-ffn::LOG2E)), p, e);
+                        Two<T> p, q;
+                        gate2<T>(o, p, q);
                         val = mul2(o, p);
-                        slope = fma2(mul2(val, e), p, p);            // p + o p (1 - p); 1 - p = e p
-                        if constexpr (N == 1) { if (p == 1.f) slope = 1.f; if (p == 0.f) slope = 0.f; }
-                        else {
-                            const float2 q = parts(p), r = parts(slope);
-                            slope = f2(q.x == 1.f || q.x == 0.f ? q.x : r.x, q.y == 1.f || q.y == 0.f ? q.y : r.y);
-                        }
+                        slope = fma2(val, q, p);
                     } else {
                         float oo[N], vv[N], ss[N];
                         to_floats<T>(o, oo);
@@ -504,14 +511,15 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
                     *reinterpret_cast<unsigned*>(at + 2 * TILE_BYTES + 128 * i) = word_of<T>(mul2(mul2(g[i], h), slope));
                     g[i] = mul2(g[i], val);
                 }
-                if (i >= n) { k[i] = splat<T>(0.f); g[i] = splat<T>(0.f); }
             }
+            if (n < RUN)
+#pragma unroll
+                for (int i = 0; i < RUN; ++i)
+                    if (i >= n) { x[i] = splat<T>(1.f); g[i] = splat<T>(0.f); }
 #pragma unroll
             for (int i = RUN - 1; i >= 0; --i) {
-                Two<T> x, other;
-                both2(k[i], x, other);
-                all_b = mul2(x, add2(g[i], all_b));
-                all_a = mul2(all_a, x);
+                all_b = mul2(x[i], add2(g[i], all_b));
+                all_a = mul2(all_a, x[i]);
             }
             if (FORM) tiles_fence();
         }
@@ -526,16 +534,18 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
         to_floats<T>(all_b, all.b);
         float q0[N];
         join(all, carry, q0);
+        ok = ok && join.ok;
         if (n > 0) {
             Two<T> q = join_floats<T>(q0);
 #pragma unroll
             for (int i = RUN - 1; i >= 0; --i) {
-                Two<T> x, other;
-                both2(k[i], x, other);
                 const Two<T> e = add2(g[i], q);
-                q = mul2(x, e);
-                *reinterpret_cast<unsigned*>(at + 128 * i) = word_of<T>(mul2(mul2(q, other), d[i]));
-                *reinterpret_cast<unsigned*>(at + TILE_BYTES + 128 * i) = word_of<T>(a.coupled ? mul2(e, other) : e);
+                q = mul2(x[i], e);
+                float keep[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) keep[j] = *reinterpret_cast<const float*>(at + j * TILE_BYTES + 128 * i);
+                *reinterpret_cast<unsigned*>(at + 128 * i) = word_of<T>(mul2(q, join_floats<T>(keep)));
+                *reinterpret_cast<unsigned*>(at + TILE_BYTES + 128 * i) = word_of<T>(COUPLED ? mul2(e, other[i]) : e);
             }
             if (n == RUN) {
                 tiles_fence();
@@ -558,6 +568,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
     }
     if (a.dh0 && w == 0 && rank == 0 && ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
     if (l == 0) tiles_done();
+    __syncwarp();
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
 // Sequences of at most one run, a warp each, a step at a time: a serving program's call.
@@ -664,9 +676,10 @@ template <typename T, bool VEC, int FORM> struct Backward {
 };
 
 template <typename T, bool VEC, int FORM>
-__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(const RecArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(const RecArgs a, int* err) {
     constexpr int N = LANES<T>;
-    __shared__ Map<N> maps[2 * WARPS * 32], parts[2 * 8 * 32];
+    __shared__ Map<N> maps[2 * (WARPS + 8) * 32];
+    __shared__ uint64_t pair[2];
     extern __shared__ float kept[];                                  // per step and channel of a thread one or two values
     grid_dep_sync();
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
@@ -674,13 +687,12 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(cons
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
     const unsigned rank = cluster_rank();
-    if (ranks > 1) cluster_sync();
+    Join<N, true> join(maps, pair, ranks, rank, w, warps, err);
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const Lane<T, VEC> lane((int)(unit - b * a.tiles));
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.dh1 ? a.dh1 + b * a.cols : nullptr, a.cols, carry);
-    Join<N, true> join{maps, parts, ranks, rank, 0, w, warps};
     const int64_t stride = (int64_t)RUN * warps * ranks;
     for (int64_t base = (seq.len + stride - 1) / stride * stride - stride; base >= 0; base -= stride) {
         const int64_t t0 = base + (int64_t)RUN * (rank * warps + w);
@@ -698,9 +710,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(cons
             r.template map<false>(a, row, n, lane, h, before, all);
         }
         join(all, carry, q);
+        if (!join.ok) continue;
         if (n == RUN) r.template out<true>(a, row, n, lane, before, q); else r.template out<false>(a, row, n, lane, before, q);
     }
-    if (a.dh0 && w == 0 && rank == 0) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
+    if (a.dh0 && w == 0 && rank == 0 && join.ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
 // ---- host ----
@@ -759,7 +773,8 @@ void shape(const RecArgs& a, int most, int per_sm, int* warps, int* ranks) {
     *ranks = 0;
     for (int s = 1; s <= 8; s *= 2) {
         if (s > 1 && (int64_t)s * *warps / 2 >= runs) break;
-        const double turns = (double)((units * s + SMS * per_sm - 1) / (SMS * per_sm)), steps = (double)((runs + s * *warps - 1) / (s * *warps));
+        const int slots = SMS * (s > 4 ? 2 : per_sm);                // the parts of eight blocks take the place of a third one
+        const double turns = (double)((units * s + slots - 1) / slots), steps = (double)((runs + s * *warps - 1) / (s * *warps));
         const double cost = turns * steps * (s > 1 ? 1.1 : 1.0);
         if (!*ranks || cost < best) { best = cost; *ranks = s; }
     }
@@ -775,7 +790,9 @@ template <typename T, bool VEC, int FORM> ftp_status forward_as(const RecArgs& a
     int warps, ranks;
     shape(a, WARPS, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
-    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, FORM>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a);
+    int* err = ffn::status_word();
+    FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, FORM>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
@@ -787,7 +804,9 @@ template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& 
     auto kern = recurrence_backward_kernel<T, VEC, FORM>;
     const size_t smem = (size_t)(a.coupled ? 2 : 1) * RUN * 32 * warps * LANES<T> * 4;
     FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RUN * 32 * WARPS * LANES<T> * 4) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
-    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, a);
+    int* err = ffn::status_word();
+    FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
@@ -802,7 +821,7 @@ template <typename T, int FORM> ftp_status forward_stream(const RecArgs& a, cuda
                 FTP_ECUDA, "%s: cannot describe a tensor to the copy engine", who);
     int* err = ffn::status_word();
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
-    auto kern = recurrence_forward_stream_kernel<T, FORM>;
+    auto kern = a.coupled ? recurrence_forward_stream_kernel<T, FORM, true> : recurrence_forward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 6 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
     FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + 8))) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, y, a, err);
@@ -820,7 +839,7 @@ template <typename T, int FORM> ftp_status backward_stream(const RecArgs& a, cud
                 FTP_ECUDA, "%s: cannot describe a tensor to the copy engine", who);
     int* err = ffn::status_word();
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
-    auto kern = recurrence_backward_stream_kernel<T, FORM>;
+    auto kern = a.coupled ? recurrence_backward_stream_kernel<T, FORM, true> : recurrence_backward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 8 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
     FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + 8))) == cudaSuccess, FTP_ECUDA,
                 "%s: no shared memory", who);
