@@ -56,46 +56,99 @@ template <typename T> struct Row {
     }
     __device__ __forceinline__ uint4 whole(int i) const { return reinterpret_cast<const uint4*>(p)[i]; }
     // any group; -infinity beyond the row
-    __device__ __forceinline__ void values(int i, float (&v)[V<T>]) const {
-        if (i >= first && i < end) { decode<T>(whole(i), v); return; }
+    __device__ __forceinline__ uint4 any(int i) const {
+        if (i >= first && i < end) return whole(i);
+        unsigned w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int j = 0; j < V<T>; ++j) {
             const int64_t c = (int64_t)i * V<T> + j - off;
-            v[j] = c >= 0 && c < vocab ? (float)p[(int64_t)i * V<T> + j] : -INFINITY;
+            w[j * (int)sizeof(T) / 4] |= (c >= 0 && c < vocab ? bits_of(p[(int64_t)i * V<T> + j]) : sizeof(T) == 4 ? 0xff800000u : 0xff80u) << (sizeof(T) == 4 ? 0 : 16 * (j & 1));
         }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ void values(int i, float (&v)[V<T>]) const { decode<T>(any(i), v); }
 };
 
+__device__ __forceinline__ unsigned max_bf2(unsigned a, unsigned b) { unsigned r; asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }   // NaN only if both are
+// Logits far below any that counts are raised to this, so that their distance to the largest stays finite where it meets the factor 0.
+constexpr float FAR = -1e18f;
+template <typename T> __device__ __forceinline__ uint4 raised(uint4 q) {   // a NaN stays one
+    if constexpr (sizeof(T) == 2)
+        asm("max.NaN.bf16x2 %0, %0, %4;\nmax.NaN.bf16x2 %1, %1, %4;\nmax.NaN.bf16x2 %2, %2, %4;\nmax.NaN.bf16x2 %3, %3, %4;"
+            : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w) : "r"(bf_pack(FAR, FAR)));
+    else
+        asm("{\n.reg .f32 f;\nmov.b32 f, %4;\n.reg .f32 a, b, c, d;\nmov.b32 a, %0;\nmov.b32 b, %1;\nmov.b32 c, %2;\nmov.b32 d, %3;\n"
+            "max.NaN.f32 a, a, f;\nmax.NaN.f32 b, b, f;\nmax.NaN.f32 c, c, f;\nmax.NaN.f32 d, d, f;\nmov.b32 %0, a;\nmov.b32 %1, b;\nmov.b32 %2, c;\nmov.b32 %3, d;\n}"
+            : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w) : "r"(__float_as_uint(FAR)));
+    return q;
+}
+template <typename T> __device__ __forceinline__ uint4 nothing() {         // a group of -infinity
+    const unsigned w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
 template <typename T, bool ENTROPY> struct Sums {
-    float m = -INFINITY, at = 0.f, s0 = 0.f, s1 = 0.f;               // at: m, or 0 while there is none
+    float m = -INFINITY, at = 0.f;                                   // at: m, or 0 while there is none
+    F2 s0 = 0ull, s1 = 0ull;
     __device__ __forceinline__ void rescale(float to, float c2) {
-        const float d = m == -INFINITY ? 0.f : (at - to) * c2, f = power<T>(d);                // no logit so far: the sums are 0
-        if (ENTROPY) s1 = f * fmaf(fmaxf(d, LOW), s0, s1);
-        s0 *= f;
+        const float d = m == -INFINITY ? 0.f : (at - to) * c2;       // no logit so far: the sums are 0
+        const F2 f = f2(power<T>(d));
+        if (ENTROPY) s1 = mul2(f, fma2(f2(fmaxf(d, LOW)), s0, s1));
+        s0 = mul2(s0, f);
         m = at = to;
     }
-    __device__ __forceinline__ void add(const float (&v)[V<T>], float c2) {
-        float top = v[0];
+    // N groups of logits; what is not there is -infinity
+    template <int N> __device__ __forceinline__ void add(const uint4 (&q)[N], float c2) {
+        float top;                                                   // the largest; with a NaN among them, that of the others
+        if constexpr (sizeof(T) == 2) {
+            unsigned w = max_bf2(max_bf2(q[0].x, q[0].y), max_bf2(q[0].z, q[0].w));
 #pragma unroll
-        for (int j = 1; j < V<T>; ++j) top = fmaxf(top, v[j]);
-        if (top > m) rescale(top, c2);
+            for (int u = 1; u < N; ++u) w = max_bf2(w, max_bf2(max_bf2(q[u].x, q[u].y), max_bf2(q[u].z, q[u].w)));
+            top = fmaxf(bf_lo(w), bf_hi(w));
+        } else {
+            top = __uint_as_float(q[0].x);
 #pragma unroll
-        for (int j = 0; j < V<T>; ++j) {
-            const float t = (v[j] - at) * c2, e = power<T>(t);
-            s0 += e;
-            if (ENTROPY) s1 = fmaf(e, fmaxf(t, LOW), s1);
+            for (int u = 0; u < N; ++u)
+                top = fmaxf(fmaxf(top, __uint_as_float(q[u].x)), fmaxf(__uint_as_float(q[u].y), fmaxf(__uint_as_float(q[u].z), __uint_as_float(q[u].w))));
         }
+        if (top > m) rescale(top, c2);
+        const F2 less = f2(-at), c = f2(c2);
+        if (!ENTROPY || at > 0.1f * FAR) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                F2 v[P<T>];
+                decode<T>(ENTROPY ? raised<T>(q[u]) : q[u], v);
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) {
+                    const F2 t = mul2(add2(v[j], less), c);
+                    const float2 p = parts(t);
+                    const F2 e = f2(power<T>(p.x), power<T>(p.y));
+                    s0 = add2(s0, e);
+                    if (ENTROPY) s1 = fma2(e, t, s1);
+                }
+            }
+        } else                                                       // even the largest logit is that far down
+            for (int u = 0; u < N; ++u) {
+                F2 v[P<T>];
+                decode<T>(q[u], v);
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) {
+                    const float2 p = parts(mul2(add2(v[j], less), c));
+                    const F2 e = f2(power<T>(p.x), power<T>(p.y));
+                    s0 = add2(s0, e);
+                    s1 = fma2(e, f2(fmaxf(p.x, LOW), fmaxf(p.y, LOW)), s1);
+                }
+            }
     }
 };
 
 template <typename T, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const LogpArgs a) {
-    extern __shared__ Key cand[];                                    // TOP: CAND candidates
+    extern __shared__ __align__(16) Key cand[];                      // TOP: CAND candidates
     __shared__ float red[3][16];
-    __shared__ float part[3];
+    __shared__ float part[3], total[3];
     __shared__ unsigned bound[32];
     __shared__ Key best[MOST_TOP], joined[8 * MOST_TOP];
-    __shared__ int hit[MOST_THREADS], hits, found;
+    __shared__ int found;
     grid_dep_sync();
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
@@ -105,33 +158,25 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
     const Row<T> x(a.x, row, a.ld, a.vocab);
     const int me = (int)rank * threads + tid, stride = (int)ranks * threads;
     Sums<T, ENTROPY> s;
+    // four groups in flight; the partial groups at both ends go to the first and the last thread
+    const bool head = me == 0 && x.first == 1, tail = me == stride - 1 && x.end < x.all && x.all - 1 >= x.first;
     int i = x.first + me;
     for (; i + 3 * stride < x.end; i += 4 * stride) {
         uint4 q[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
+        s.add(q, a.scale2);
+    }
+    {                                                                // what is left, with the partial groups
+        uint4 q[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float v[V<T>];
-            decode<T>(q[u], v);
-            s.add(v, a.scale2);
+        for (int u = 0; u < 3; ++u) q[u] = i + u * stride < x.end ? x.whole(i + u * stride) : nothing<T>();
+        q[3] = head ? x.any(0) : nothing<T>();
+        s.add(q, a.scale2);
+        if (tail) {
+            const uint4 r[1] = {x.any(x.all - 1)};
+            s.add(r, a.scale2);
         }
-    }
-    for (; i < x.end; i += stride) {
-        float v[V<T>];
-        decode<T>(x.whole(i), v);
-        s.add(v, a.scale2);
-    }
-    // the partial groups at both ends go to the first threads
-    if (me == 0 && x.first == 1) {
-        float v[V<T>];
-        x.values(0, v);
-        s.add(v, a.scale2);
-    }
-    if (me == stride - 1 && x.end < x.all && x.all - 1 >= x.first) {
-        float v[V<T>];
-        x.values(x.all - 1, v);
-        s.add(v, a.scale2);
     }
     const float mine = s.m;
     // the block's sums
@@ -139,13 +184,13 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if (lane == 0) red[0][w] = m;
-    if (TOP && tid == 0) { hits = 0; found = 0; }
+    if (TOP && tid == 0) found = 0;
     if (TOP && tid < MOST_TOP) best[tid] = 0;
     __syncthreads();
     m = red[0][0];
     for (int k = 1; k < warps; ++k) m = fmaxf(m, red[0][k]);
     if (m > s.m) s.rescale(m, a.scale2);
-    float s0 = s.s0, s1 = s.s1;
+    float s0 = sum2(s.s0), s1 = sum2(s.s1);
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
         s0 += __shfl_xor_sync(0xffffffffu, s0, d);
@@ -175,8 +220,6 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
 #pragma unroll
         for (int k = 0; k < 32; ++k) { const unsigned o = __shfl_sync(0xffffffffu, b, k); above += o > b || (o == b && k < lane); }
         const unsigned kth = __shfl_sync(0xffffffffu, b, __ffs(__ballot_sync(0xffffffffu, above == a.k - 1)) - 1);
-        if (order_of(mine) >= kth) hit[atomicAdd(&hits, 1)] = tid;
-        __syncthreads();
         const auto offer = [&](int g) {
             float v[V<T>];
             x.values(g, v);
@@ -189,19 +232,25 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
                 }
             }
         };
-        for (int h = w; h < hits; h += warps) {
-            const int owner = (int)rank * threads + hit[h];
+        // a warp reads its threads' groups again, 32 groups of one thread at a time
+        for (unsigned left = __ballot_sync(0xffffffffu, order_of(mine) >= kth); left; left &= left - 1) {
+            const int owner = (int)rank * threads + w * 32 + __ffs(left) - 1;
             for (int g = x.first + owner + lane * stride; g < x.end; g += 32 * stride) offer(g);
             if (lane == 0 && owner == 0 && x.first == 1) offer(0);
             if (lane == 0 && owner == stride - 1 && x.end < x.all && x.all - 1 >= x.first) offer(x.all - 1);
         }
         __syncthreads();
         const int n = found;
-        if (n <= CAND) {
+        if (n < CAND) {
+            if (tid == 0) cand[n] = 0;
+            __syncthreads();
             for (int k = tid; k < n; k += threads) {
                 const Key mykey = cand[k];
                 int rnk = 0;
-                for (int q = 0; q < n; ++q) rnk += cand[q] > mykey;
+                for (int q = 0; q < n; q += 2) {                     // an odd number has a 0 behind it
+                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(cand + q);
+                    rnk += (two.x > mykey) + (two.y > mykey);
+                }
                 if (rnk < a.k) best[rnk] = mykey;
             }
         } else {                                                     // too many equal ones: one after another, over the whole part of the row
@@ -232,31 +281,38 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
         }
     }
     if (ranks > 1) cluster_sync(); else __syncthreads();
-    if (rank == 0 && (TOP || w == 0)) {
-        float top = part[0], all0 = part[1], all1 = part[2];
+    if (rank == 0) {
         if (ranks > 1) {
-            float pm[8], p0[8], p1[8];
+            if (w == 0) {                                            // a lane per block
+                const unsigned from = on_rank(smem_at(part), min((unsigned)lane, ranks - 1));
+                float pm, p0, p1;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pm) : "r"(from) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p0) : "r"(from + 4) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p1) : "r"(from + 8) : "memory");
+                float top = pm;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const unsigned from = on_rank(smem_at(part), min((unsigned)r, ranks - 1));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pm[r]) : "r"(from) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p0[r]) : "r"(from + 4) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p1[r]) : "r"(from + 8) : "memory");
+                for (int d = 4; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                if (pm != -INFINITY) {                               // else p0 is 0, or NaN
+                    const float d = (pm - top) * a.scale2, f = power<T>(d);
+                    p1 = f * fmaf(fmaxf(d, LOW), p0, p1);
+                    p0 *= f;
+                }
+                if (lane >= (int)ranks) p0 = p1 = 0.f;
+#pragma unroll
+                for (int d = 4; d; d >>= 1) { p0 += __shfl_xor_sync(0xffffffffu, p0, d); p1 += __shfl_xor_sync(0xffffffffu, p1, d); }
+                if (lane == 0) { total[0] = top; total[1] = p0; total[2] = p1; }
             }
-#pragma unroll
-            for (int r = 1; r < 8; ++r) top = fmaxf(top, pm[r]);
-            all0 = all1 = 0.f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                if (r >= (int)ranks || pm[r] == -INFINITY) { if (r < (int)ranks) all0 += p0[r]; continue; }   // p0 is 0, or NaN
-                const float d = (pm[r] - top) * a.scale2, f = power<T>(d);
-                all1 += f * fmaf(fmaxf(d, LOW), p0[r], p1[r]);
-                all0 = fmaf(f, p0[r], all0);
-            }
+            if (TOP)
+                for (int k = tid; k < (int)ranks * a.k; k += threads) {
+                    const unsigned at = on_rank(smem_at(best), (unsigned)(k / a.k)) + 8u * (unsigned)(k % a.k);
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(joined[k]) : "r"(at) : "memory");
+                }
+            __syncthreads();
         }
+        const float top = ranks > 1 ? total[0] : part[0], all0 = ranks > 1 ? total[1] : part[1], all1 = ranks > 1 ? total[2] : part[2];
         const float log_sum = logf(all0);
+        const bool none = all0 == 0.f;                               // no token can occur
         if (tid == 0) {
-            const bool none = all0 == 0.f;                           // no token can occur
             if (a.logp) {
                 const int t = a.target[row];
                 float v = 0.f;
@@ -267,27 +323,20 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
             if (ENTROPY) a.entropy[row] = none ? 0.f : log_sum - all1 / all0 * 0.69314718055994531f;
         }
         if constexpr (TOP) {
-            Key* from = best;
+            const auto give = [&](int place, Key q) {
+                a.top[row * a.k + place] = (int32_t)~(unsigned)q;
+                if (a.top_logp) a.top_logp[row * a.k + place] = none ? -INFINITY : a.scale * (from_order((unsigned)(q >> 32)) - top) - log_sum;
+            };
             if (ranks > 1) {
-                for (int k = tid; k < (int)ranks * a.k; k += threads) {
-                    const unsigned at = on_rank(smem_at(best), (unsigned)(k / a.k)) + 8u * (unsigned)(k % a.k);
-                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(joined[k]) : "r"(at) : "memory");
-                }
-                __syncthreads();
                 for (int k = tid; k < (int)ranks * a.k; k += threads) {
                     const Key q = joined[k];
                     int rnk = 0;
+#pragma unroll 8
                     for (int z = 0; z < (int)ranks * a.k; ++z) rnk += joined[z] > q;
-                    if (q && rnk < a.k) {
-                        a.top[row * a.k + rnk] = (int32_t)~(unsigned)q;
-                        if (a.top_logp) { const float v = from_order((unsigned)(q >> 32)); a.top_logp[row * a.k + rnk] = all0 == 0.f ? -INFINITY : a.scale * (v - top) - log_sum; }
-                    }
+                    if (q && rnk < a.k) give(rnk, q);
                 }
-            } else if (tid < a.k) {
-                const Key q = from[tid];
-                a.top[row * a.k + tid] = (int32_t)~(unsigned)q;
-                if (a.top_logp) { const float v = from_order((unsigned)(q >> 32)); a.top_logp[row * a.k + tid] = all0 == 0.f ? -INFINITY : a.scale * (v - top) - log_sum; }
-            }
+            } else if (tid < a.k)
+                give(tid, best[tid]);
         }
     }
     if (ranks > 1) cluster_sync();                                   // nobody leaves while the first block reads its shared memory
@@ -304,7 +353,7 @@ struct LogpBack {
 };
 
 // d = scale (dlogp (1 at the target - p) - dentropy p (log p + H)).  A warp takes 128 groups of 16 bytes of a row, four to a lane.
-template <typename T>
+template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(256) logprob_backward_kernel(const LogpBack a) {
     grid_dep_sync();
     const int lane = threadIdx.x & 31;
@@ -314,43 +363,58 @@ __global__ void __launch_bounds__(256) logprob_backward_kernel(const LogpBack a)
         const Row<T> x(a.x, row, a.ld, a.vocab);
         T* out = static_cast<T*>(a.dx) + row * a.ldd - x.off;
         const bool same = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-        const int64_t g0 = (n - row * per_row) * 128 + lane;
+        const int g0 = (int)(n - row * per_row) * 128 + lane;
         uint4 q[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t g = g0 + 32 * u;
-            q[u] = g >= x.first && g < x.end ? x.whole((int)g) : make_uint4(0u, 0u, 0u, 0u);
+            const int g = g0 + 32 * u;
+            q[u] = g >= x.first && g < x.end ? x.whole(g) : nothing<T>();
         }
         const int t = a.target ? a.target[row] : -1;
         const float m = a.lse[2 * row], log_sum = a.lse[2 * row + 1];
-        const bool none = m == -INFINITY && log_sum == -INFINITY, given = t >= 0 && t < a.vocab && !none;
-        const float dl = given && a.dlogp ? a.dlogp[row] * a.scale : 0.f, dh = a.dentropy ? a.dentropy[row] * a.scale : 0.f, entropy = a.dentropy ? a.entropy[row] : 0.f;
-        const float plus = fmaf(dh, entropy, dl);
+        const bool none = m == -INFINITY && log_sum == -INFINITY, given = t >= 0 && t < a.vocab && !none, near = m > 0.1f * FAR;
+        const float dl = given && a.dlogp ? a.dlogp[row] * a.scale : 0.f, dh = ENTROPY ? a.dentropy[row] * a.scale : 0.f;
+        const float plus = ENTROPY ? -fmaf(dh, a.entropy[row], dl) : -dl;
+        const F2 less = f2(-m), c = f2(a.scale), sum = f2(-log_sum), b = f2(-dh), k = f2(plus);
+        const int at = given ? (t + x.off) / V<T> : -1, j_at = given ? (t + x.off) % V<T> : 0;     // the target's group, and its place in it
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t g = g0 + 32 * u;
+            const int g = g0 + 32 * u;
             if (g >= x.all) break;
             const bool whole = g >= x.first && g < x.end;
-            float v[V<T>];
-            if (whole) decode<T>(q[u], v); else x.values((int)g, v);
+            if (!whole) q[u] = x.any(g);
+            F2 v[P<T>];
+            decode<T>(ENTROPY && near ? raised<T>(q[u]) : q[u], v);
 #pragma unroll
-            for (int j = 0; j < V<T>; ++j) {
-                const float lp = (v[j] - m) * a.scale - log_sum;
-                const float p = sizeof(T) == 4 ? expf(lp) : ffn::ex2_fast(lp * ffn::LOG2E);
-                v[j] = none ? 0.f : -p * fmaf(dh, fmaxf(lp, LOW), plus);
+            for (int j = 0; j < P<T>; ++j) {
+                const F2 lp = fma2(add2(v[j], less), c, sum);
+                const float2 l = parts(lp);
+                F2 p;
+                if (sizeof(T) == 4) p = f2(expf(l.x), expf(l.y));
+                else {
+                    const float2 z = parts(mul2(lp, f2(ffn::LOG2E)));
+                    p = f2(ffn::ex2_fast(z.x), ffn::ex2_fast(z.y));
+                }
+                if (ENTROPY) v[j] = mul2(p, fma2(b, near ? lp : f2(fmaxf(l.x, LOW), fmaxf(l.y, LOW)), k));
+                else v[j] = mul2(p, k);
             }
-            const int64_t c0 = g * V<T> - x.off;
-            if (given && t >= c0 && t < c0 + V<T>) {
+            if (none)
 #pragma unroll
-                for (int j = 0; j < V<T>; ++j) if (t == c0 + j) v[j] += dl;
-            }
-            if (whole && same) reinterpret_cast<uint4*>(out)[g] = encode<T>(v);
+                for (int j = 0; j < P<T>; ++j) v[j] = 0ull;
+            if (g == at)
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) {
+                    if (j_at == 2 * j) v[j] = add2(v[j], f2(dl, 0.f));
+                    if (j_at == 2 * j + 1) v[j] = add2(v[j], f2(0.f, dl));
+                }
+            const uint4 r = encode<T>(v);
+            if (whole && same) reinterpret_cast<uint4*>(out)[g] = r;
             else {
-                const uint4 r = encode<T>(v);
-                const unsigned b[4] = {r.x, r.y, r.z, r.w};
+                const unsigned w[4] = {r.x, r.y, r.z, r.w};
+                const int64_t c0 = (int64_t)g * V<T> - x.off;
 #pragma unroll
                 for (int j = 0; j < V<T>; ++j)
-                    if (c0 + j >= 0 && c0 + j < a.vocab) from_bits(out + g * V<T> + j, b[j * (int)sizeof(T) / 4] >> (sizeof(T) == 4 ? 0 : 16 * (j & 1)));
+                    if (c0 + j >= 0 && c0 + j < a.vocab) from_bits(out + (int64_t)g * V<T> + j, w[j * (int)sizeof(T) / 4] >> (sizeof(T) == 4 ? 0 : 16 * (j & 1)));
             }
         }
     }
@@ -368,10 +432,11 @@ ftp_status check(const void* logits, int64_t rows, int32_t vocab, int64_t* ld, i
 }
 
 template <typename T> cudaError_t forward_of(const LogpArgs& a, cudaStream_t st) {
-    // a thread takes four groups and more; blocks of 512 share a row while that gives every multiprocessor no more than two
+    // a thread takes four groups and more, 16 where the rows fill the GPU (shorter turns between a block's sums: 4096 x 50021 bf16 takes
+    // 117 us with 512 threads a row, 256: see below); blocks of 512 share a row while that gives every multiprocessor no more than two
     const int groups = (a.vocab + V<T> - 1) / V<T>;
     int threads = 32, ranks = 1;
-    while (threads < MOST_THREADS && threads * 4 < groups) threads *= 2;
+    while (threads < MOST_THREADS && threads * (a.rows >= SMS ? 16 : 4) < groups) threads *= 2;
     while (ranks < 8 && a.rows * ranks * 2 <= 2 * SMS && ranks * 2 * threads * 2 <= groups) ranks *= 2;
     auto kern = a.k ? (a.entropy ? logprob_forward_kernel<T, true, true> : logprob_forward_kernel<T, false, true>)
                     : (a.entropy ? logprob_forward_kernel<T, true, false> : logprob_forward_kernel<T, false, false>);
@@ -422,8 +487,8 @@ ftp_status ftp_logprob_backward(const void* logits, int64_t rows, int32_t vocab,
     const int v = precision == FTP_FP32 ? 4 : 8;
     const int64_t pieces = rows * (((int64_t)vocab + 2 * v - 2) / v / 128 + 1);
     const dim3 grid((unsigned)std::min<int64_t>((pieces + 7) / 8, SMS * 64));
-    if (precision == FTP_FP32) launch(logprob_backward_kernel<float>, grid, dim3(256), 0, st, a);
-    else launch(logprob_backward_kernel<bf16>, grid, dim3(256), 0, st, a);
+    if (precision == FTP_FP32) launch(dentropy ? logprob_backward_kernel<float, true> : logprob_backward_kernel<float, false>, grid, dim3(256), 0, st, a);
+    else launch(dentropy ? logprob_backward_kernel<bf16, true> : logprob_backward_kernel<bf16, false>, grid, dim3(256), 0, st, a);
     return launched(who);
 }
 
