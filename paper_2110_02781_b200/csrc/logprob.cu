@@ -86,6 +86,14 @@ template <typename T> __device__ __forceinline__ uint4 nothing() {         // a 
     const unsigned w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
     return make_uint4(w, w, w, w);
 }
+// the largest of a group; with a NaN in it, that of the others
+template <typename T> __device__ __forceinline__ float top_of(const uint4& q) {
+    if constexpr (sizeof(T) == 4) return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+    else {
+        const unsigned w = max_bf2(max_bf2(q.x, q.y), max_bf2(q.z, q.w));
+        return fmaxf(bf_lo(w), bf_hi(w));
+    }
+}
 template <typename T, bool ENTROPY> struct Sums {
     float m = -INFINITY, at = 0.f;                                   // at: m, or 0 while there is none
     F2 s0 = 0ull, s1 = 0ull;
@@ -141,14 +149,28 @@ template <typename T, bool ENTROPY> struct Sums {
     }
 };
 
+// The 32 largest of two lists of 32 distinct keys (or 0), each in descending order along a warp, in descending order: the larger of
+// each pair from both ends, which rise and fall once, then sorted by halves.
+__device__ __forceinline__ Key merge(Key a, Key b) {
+    const int lane = threadIdx.x & 31;
+    b = __shfl_sync(0xffffffffu, b, 31 - lane);
+    a = a > b ? a : b;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const Key o = __shfl_xor_sync(0xffffffffu, a, d);
+        a = (a > o) == ((lane & d) == 0) ? a : o;
+    }
+    return a;
+}
+
 template <typename T, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const LogpArgs a) {
-    extern __shared__ __align__(16) Key cand[];                      // TOP: CAND candidates
+    extern __shared__ Key cand[];                                    // TOP: CAND candidates
     __shared__ float red[3][16];
     __shared__ float part[3], total[3];
     __shared__ unsigned bound[32];
-    __shared__ Key best[MOST_TOP], joined[8 * MOST_TOP];
-    __shared__ int found;
+    __shared__ Key best[MOST_TOP], joined[4][MOST_TOP];
+    __shared__ int hit[TOP ? MOST_THREADS : 1], hits, found;
     grid_dep_sync();
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
@@ -158,25 +180,37 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
     const Row<T> x(a.x, row, a.ld, a.vocab);
     const int me = (int)rank * threads + tid, stride = (int)ranks * threads;
     Sums<T, ENTROPY> s;
+    // the given token's logit, on its way meanwhile
+    int target = -1;
+    float given = 0.f;
+    if (me == 0 && a.logp) {
+        target = a.target[row];
+        if (target >= 0 && target < a.vocab) given = (float)x.p[x.off + (int64_t)target];
+    }
+    // The first groups of a thread stay in registers: with no more than these, nothing is read again for the likeliest tokens.
+    uint4 held[4];
     // four groups in flight; the partial groups at both ends go to the first and the last thread
     const bool head = me == 0 && x.first == 1, tail = me == stride - 1 && x.end < x.all && x.all - 1 >= x.first;
-    int i = x.first + me;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) held[u] = x.first + me + u * stride < x.end ? x.whole(x.first + me + u * stride) : nothing<T>();
+    s.add(held, a.scale2);
+    int i = x.first + me + 4 * stride;
     for (; i + 3 * stride < x.end; i += 4 * stride) {
         uint4 q[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
         s.add(q, a.scale2);
     }
-    {                                                                // what is left, with the partial groups
+    if (i < x.end) {
         uint4 q[4];
+        q[3] = nothing<T>();
 #pragma unroll
         for (int u = 0; u < 3; ++u) q[u] = i + u * stride < x.end ? x.whole(i + u * stride) : nothing<T>();
-        q[3] = head ? x.any(0) : nothing<T>();
         s.add(q, a.scale2);
-        if (tail) {
-            const uint4 r[1] = {x.any(x.all - 1)};
-            s.add(r, a.scale2);
-        }
+    }
+    if (head || tail) {
+        const uint4 ends[2] = {head ? x.any(0) : nothing<T>(), tail ? x.any(x.all - 1) : nothing<T>()};
+        s.add(ends, a.scale2);
     }
     const float mine = s.m;
     // the block's sums
@@ -184,11 +218,11 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if (lane == 0) red[0][w] = m;
-    if (TOP && tid == 0) found = 0;
+    if (TOP && tid == 0) hits = found = 0;
     if (TOP && tid < MOST_TOP) best[tid] = 0;
     __syncthreads();
-    m = red[0][0];
-    for (int k = 1; k < warps; ++k) m = fmaxf(m, red[0][k]);
+    m = red[0][lane & (warps - 1)];
+    for (int d = warps >> 1; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if (m > s.m) s.rescale(m, a.scale2);
     float s0 = sum2(s.s0), s1 = sum2(s.s1);
 #pragma unroll
@@ -209,10 +243,10 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
         }
     }
     __syncthreads();
-    if (tid == 0) {
-        s0 = red[1][0]; s1 = red[2][0];
-        for (int k = 1; k < warps; ++k) { s0 += red[1][k]; s1 += red[2][k]; }
-        part[0] = m; part[1] = s0; part[2] = s1;
+    if (w == 0) {
+        s0 = red[1][lane & (warps - 1)]; s1 = red[2][lane & (warps - 1)];
+        for (int d = warps >> 1; d; d >>= 1) { s0 += __shfl_xor_sync(0xffffffffu, s0, d); s1 += __shfl_xor_sync(0xffffffffu, s1, d); }
+        if (lane == 0) { part[0] = m; part[1] = s0; part[2] = s1; }
     }
     if constexpr (TOP) {
         const unsigned b = bound[lane];
@@ -220,38 +254,46 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
 #pragma unroll
         for (int k = 0; k < 32; ++k) { const unsigned o = __shfl_sync(0xffffffffu, b, k); above += o > b || (o == b && k < lane); }
         const unsigned kth = __shfl_sync(0xffffffffu, b, __ffs(__ballot_sync(0xffffffffu, above == a.k - 1)) - 1);
-        const auto offer = [&](int g) {
+        const float least = from_order(kth);                         // comparisons let a NaN pass
+        const auto offer = [&](int g, const uint4& q) {
+            if (top_of<T>(q) < least) return;
             float v[V<T>];
-            x.values(g, v);
+            decode<T>(q, v);
 #pragma unroll
             for (int j = 0; j < V<T>; ++j) {
+                if (v[j] < least) continue;
                 const int c = g * V<T> + j - x.off;
-                if (c >= 0 && c < a.vocab && order_of(v[j]) >= kth) {
-                    const int at = atomicAdd(&found, 1);
-                    if (at < CAND) cand[at] = key_of(v[j], c);
-                }
+                if (c < 0 || c >= a.vocab) continue;
+                const int at = atomicAdd(&found, 1);
+                if (at < CAND) cand[at] = key_of(v[j], c);
             }
         };
-        // a warp reads its threads' groups again, 32 groups of one thread at a time
-        for (unsigned left = __ballot_sync(0xffffffffu, order_of(mine) >= kth); left; left &= left - 1) {
-            const int owner = (int)rank * threads + w * 32 + __ffs(left) - 1;
-            for (int g = x.first + owner + lane * stride; g < x.end; g += 32 * stride) offer(g);
-            if (lane == 0 && owner == 0 && x.first == 1) offer(0);
-            if (lane == 0 && owner == stride - 1 && x.end < x.all && x.all - 1 >= x.first) offer(x.all - 1);
+        if (x.first + 4 * stride >= x.end) {
+            if (order_of(mine) >= kth) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (x.first + me + u * stride < x.end) offer(x.first + me + u * stride, held[u]);
+                if (head) offer(0, x.any(0));
+                if (tail) offer(x.all - 1, x.any(x.all - 1));
+            }
+        } else {
+            if (order_of(mine) >= kth) hit[atomicAdd(&hits, 1)] = tid;
+            __syncthreads();
+            for (int h = w; h < hits; h += warps) {                  // a thread's groups read again by a warp
+                const int owner = (int)rank * threads + hit[h];
+                for (int g = x.first + owner + lane * stride; g < x.end; g += 32 * stride) offer(g, x.whole(g));
+                if (lane == 0 && owner == 0 && x.first == 1) offer(0, x.any(0));
+                if (lane == 0 && owner == stride - 1 && x.end < x.all && x.all - 1 >= x.first) offer(x.all - 1, x.any(x.all - 1));
+            }
         }
         __syncthreads();
         const int n = found;
-        if (n < CAND) {
-            if (tid == 0) cand[n] = 0;
-            __syncthreads();
-            for (int k = tid; k < n; k += threads) {
+        if (n <= CAND) {                                             // how many are larger: a warp per candidate
+            for (int k = w; k < n; k += warps) {
                 const Key mykey = cand[k];
                 int rnk = 0;
-                for (int q = 0; q < n; q += 2) {                     // an odd number has a 0 behind it
-                    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(cand + q);
-                    rnk += (two.x > mykey) + (two.y > mykey);
-                }
-                if (rnk < a.k) best[rnk] = mykey;
+                for (int q = lane; q - lane < n; q += 32) rnk += __popc(__ballot_sync(0xffffffffu, q < n && cand[q] > mykey));
+                if (lane == 0 && rnk < a.k) best[rnk] = mykey;
             }
         } else {                                                     // too many equal ones: one after another, over the whole part of the row
             Key last = ~0ull;
@@ -302,23 +344,20 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
                 for (int d = 4; d; d >>= 1) { p0 += __shfl_xor_sync(0xffffffffu, p0, d); p1 += __shfl_xor_sync(0xffffffffu, p1, d); }
                 if (lane == 0) { total[0] = top; total[1] = p0; total[2] = p1; }
             }
-            if (TOP)
-                for (int k = tid; k < (int)ranks * a.k; k += threads) {
-                    const unsigned at = on_rank(smem_at(best), (unsigned)(k / a.k)) + 8u * (unsigned)(k % a.k);
-                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(joined[k]) : "r"(at) : "memory");
-                }
+            if (TOP && w < (int)ranks / 2) {                         // a warp for two blocks' tokens
+                Key two[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(two[i]) : "r"(on_rank(smem_at(best + lane), (unsigned)(2 * w + i))) : "memory");
+                joined[w][lane] = merge(two[0], two[1]);
+            }
             __syncthreads();
         }
         const float top = ranks > 1 ? total[0] : part[0], all0 = ranks > 1 ? total[1] : part[1], all1 = ranks > 1 ? total[2] : part[2];
         const float log_sum = logf(all0);
         const bool none = all0 == 0.f;                               // no token can occur
         if (tid == 0) {
-            if (a.logp) {
-                const int t = a.target[row];
-                float v = 0.f;
-                if (t >= 0 && t < a.vocab) v = none ? -INFINITY : a.scale * ((float)x.p[x.off + (int64_t)t] - top) - log_sum;
-                a.logp[row] = v;
-            }
+            if (a.logp) a.logp[row] = target < 0 || target >= a.vocab ? 0.f : none ? -INFINITY : a.scale * (given - top) - log_sum;
             if (a.lse) { a.lse[2 * row] = top; a.lse[2 * row + 1] = log_sum; }
             if (ENTROPY) a.entropy[row] = none ? 0.f : log_sum - all1 / all0 * 0.69314718055994531f;
         }
@@ -327,16 +366,12 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
                 a.top[row * a.k + place] = (int32_t)~(unsigned)q;
                 if (a.top_logp) a.top_logp[row * a.k + place] = none ? -INFINITY : a.scale * (from_order((unsigned)(q >> 32)) - top) - log_sum;
             };
-            if (ranks > 1) {
-                for (int k = tid; k < (int)ranks * a.k; k += threads) {
-                    const Key q = joined[k];
-                    int rnk = 0;
-#pragma unroll 8
-                    for (int z = 0; z < (int)ranks * a.k; ++z) rnk += joined[z] > q;
-                    if (q && rnk < a.k) give(rnk, q);
-                }
-            } else if (tid < a.k)
-                give(tid, best[tid]);
+            if (w == 0) {
+                Key q = ranks > 1 ? joined[0][lane] : best[lane];
+                if (ranks > 2) q = merge(q, joined[1][lane]);
+                if (ranks > 4) q = merge(q, merge(joined[2][lane], joined[3][lane]));
+                if (lane < a.k) give(lane, q);
+            }
         }
     }
     if (ranks > 1) cluster_sync();                                   // nobody leaves while the first block reads its shared memory
@@ -432,11 +467,11 @@ ftp_status check(const void* logits, int64_t rows, int32_t vocab, int64_t* ld, i
 }
 
 template <typename T> cudaError_t forward_of(const LogpArgs& a, cudaStream_t st) {
-    // a thread takes four groups and more, 16 where the rows fill the GPU (shorter turns between a block's sums: 4096 x 50021 bf16 takes
-    // 117 us with 512 threads a row, 256: see below); blocks of 512 share a row while that gives every multiprocessor no more than two
+    // a thread takes four groups and more, 64 where the rows fill the GPU (4096 x 50021 bf16: 101 us with 512 threads a row, 82 with
+    // 256, 77 with 128, 113 with 64); blocks of 512 share a row while that gives every multiprocessor no more than two
     const int groups = (a.vocab + V<T> - 1) / V<T>;
     int threads = 32, ranks = 1;
-    while (threads < MOST_THREADS && threads * (a.rows >= SMS ? 16 : 4) < groups) threads *= 2;
+    while (threads < MOST_THREADS && threads * (a.rows >= SMS ? 64 : 4) < groups) threads *= 2;
     while (ranks < 8 && a.rows * ranks * 2 <= 2 * SMS && ranks * 2 * threads * 2 <= groups) ranks *= 2;
     auto kern = a.k ? (a.entropy ? logprob_forward_kernel<T, true, true> : logprob_forward_kernel<T, false, true>)
                     : (a.entropy ? logprob_forward_kernel<T, true, false> : logprob_forward_kernel<T, false, false>);
