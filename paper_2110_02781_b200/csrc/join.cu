@@ -146,11 +146,15 @@ template <typename T, int G> __device__ __forceinline__ void decode_row(const ui
 
 // Threads resident on a multiprocessor, by the columns of a thread: what their registers leave (64, 80 and 128 a thread).
 constexpr int forward_threads(int columns) { return columns <= 8 ? 1024 : columns <= 16 ? 768 : 512; }
-constexpr int backward_threads(int columns) { return columns <= 8 ? 1024 : 512; }
+constexpr int BACKWARD_THREADS = 512;
+
+// Rows that the backward pass takes at a time where the usual gradients are asked for: the vectors that all rows share, and the running sums, are then
+// read half as often (with a row a time the first cache's bandwidth is three quarters used: 138 us instead of 127).
+constexpr int PAIR = 2;
 
 template <typename T, int G, bool VEC>
 __global__ void __launch_bounds__(forward_threads(G * V<T>)) join_forward_kernel(const JoinArgs a) {
-    __shared__ float2 red[32];
+    __shared__ float red[32];
     __shared__ Rounds keys;
     grid_dep_sync();
     const Dropping drop(a.drop, keys);
@@ -238,160 +242,274 @@ template <typename T> struct Running {
     }
 };
 
-// D = ds + r (g - mean(g) - x^ mean(g x^)), g = dy w_pre, x^ = (s - mean) r  (mean(g) with the layer norm only)
-// dx = alpha D;  dv = beta D gate mask / (1 - p);  du from dv w_post in the same way;  dgate = beta D drop(v)
-template <typename T, int G, bool VEC>
-__global__ void __launch_bounds__(backward_threads(G * V<T>)) join_backward_kernel(const JoinArgs a) {
+// With x^ and u^ the normalised rows of s and u, g = dy w_pre, K = beta gate mask / (1 - p), r the 1 / deviation of s and r' that of u:
+//
+//   e = ds + r g;   c1 = - r mean(g) (layer norm only), c2 = - r mean(g x^);   D = e + c1 + c2 x^
+//   dx = alpha D;   dv = K D;   du = r' (dv w_post - mean(dv w_post) - u^ mean(dv w_post u^));   dgate = (K / gate) D (u^ w_post + b_post)
+//
+// The sums over a row that du needs are sums of K w_post (e + c1 + c2 x^) and of that times u^: linear in c1 and c2, so all sums of a row
+// go through one exchange, and its values are decoded once.
+// USUAL: both norms with weights, biases beside them where one is a layer norm, all of their gradients asked for, a ds, dx and du: known
+// when compiled, because a question per group of columns costs three instructions.
+template <typename T, int G, bool VEC, bool LAYER, bool USUAL>
+__global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const JoinArgs a) {
+    constexpr int NS = LAYER ? 8 : 3, R = USUAL && G * V<T> <= 8 ? PAIR : 1;
+    const bool pre = USUAL || a.pre != FTP_NORM_NONE, post = USUAL || a.post != FTP_NORM_NONE, w_pre = USUAL || a.w_pre, w_post = USUAL || a.w_post;
+    const bool b_post = USUAL ? LAYER : a.b_post != nullptr, gated = a.gate, graded = a.dgate;
+    const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL ? (LAYER ? 1 : -1) : a.at[SUM_B_PRE], at_w_post = USUAL ? (LAYER ? 2 : 1) : a.at[SUM_W_POST],
+              at_b_post = USUAL ? (LAYER ? 3 : -1) : a.at[SUM_B_POST], at_gate = USUAL ? (LAYER ? 4 : 2) : a.at[SUM_GATE];
     extern __shared__ float4 dynamic[];
-    __shared__ float2 red[32];
+    __shared__ float red[2 * 16 * NS * R];
     __shared__ Rounds keys;
     grid_dep_sync();
     const Dropping drop(a.drop, keys);
-    RowSum sum{red, 0};
     const int t = threadIdx.x;
+    int turn = 0;
     Running<T> run{dynamic + t};
     if (G * V<T> >= 32 && a.spill) run.at = reinterpret_cast<float4*>(a.spill) + (size_t)blockIdx.x * a.nsums * (G * (V<T> / 4)) * blockDim.x + t;
     for (int i = 0; i < a.nsums * G; ++i) run.clear(i);
     const int64_t mine = blockIdx.x, first = mine * a.run, last = min(first + a.run, a.rows);
     int64_t group = a.gate_rows > 1 ? first / a.gate_rows : 0, next = a.gate_rows > 1 ? (group + 1) * a.gate_rows : 0;   // next: first row of the next group
     const F2 f = f2(drop.cut ? a.beta * a.drop.factor : a.beta), alpha = f2(a.alpha);
-    for (int64_t row = first; row < last; ++row) {
+    // USUAL: the next rows are on their way while these are worked on; a thread copies its own columns into shared memory and reads them itself
+    const unsigned staged = smem_at(dynamic) + a.nsums * (G * (V<T> / 4)) * blockDim.x * 16 + t * 16;
+    const int64_t lds[4] = {a.lds, a.ldy, a.ldds, a.ldu};
+    const void* const bases[4] = {a.s, a.dy, a.ds, a.u};
+    const auto ahead = [&](int64_t from) {
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+            if (from + q < last)
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(staged + ((q * 4 + n) * G + g) * blockDim.x * 16),
+                                     "l"(reinterpret_cast<const char*>(in_row<T>(bases[n], lds[n], from + q)) + (unsigned)column_in<T, true>(t, a.threads, g, 0, a.cols) * (unsigned)sizeof(T)) : "memory");
+    };
+    const auto arrived = [&](int q, int n, uint4 (&r)[G]) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[g].x), "=r"(r[g].y), "=r"(r[g].z), "=r"(r[g].w) : "r"(staged + ((q * 4 + n) * G + g) * blockDim.x * 16) : "memory");
+    };
+    if (USUAL) ahead(first);
+    for (int64_t row = first; row < last;) {
         if (a.gate_sums && row == next) {                            // another group: its predecessor's sum is complete as far as this run goes
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float v[V<T>];
-                run.get(a.at[SUM_GATE] * G + g, v);
+                run.get(at_gate * G + g, v);
                 put_vector<T, VEC>(a.gate_sums + (mine + group) * a.cols, t, a.threads, g, a.cols, v);
-                run.clear(a.at[SUM_GATE] * G + g);
+                run.clear(at_gate * G + g);
             }
             ++group;
             next += a.gate_rows;
         }
-        uint4 ru[G], rs[G], rdy[G], rds[G];
-        if (a.pre != FTP_NORM_NONE) fetch_row<T, G, VEC>(a, in_row<T>(a.s, a.lds, row), t, rs);
-        if (a.dy) fetch_row<T, G, VEC>(a, in_row<T>(a.dy, a.ldy, row), t, rdy);
-        if (a.ds) fetch_row<T, G, VEC>(a, in_row<T>(a.ds, a.ldds, row), t, rds);
-        if (a.u) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row), t, ru);
-        F2 d[G][P<T>], p[G][P<T>];
-        if (a.pre != FTP_NORM_NONE) {
-            const float m = a.stats[2 * a.rows + row], r = a.stats[3 * a.rows + row];
-            const F2 rp = f2(r), lp = f2(-m * r);
-            F2 p1 = 0ull, p2 = 0ull;
-            decode_row<T, G>(rdy, d);
-            clip_row<T, G, VEC>(a, t, d);
-            if (a.at[SUM_B_PRE] >= 0)
+        const int64_t end = a.gate_sums ? min(last, next) : last;    // the rows of an iteration share a group
+        bool on[R];
 #pragma unroll
-                for (int g = 0; g < G; ++g) run.add(a.at[SUM_B_PRE] * G + g, d[g]);
-            decode_row<T, G>(rs, p);
-            if (a.at[SUM_W_PRE] >= 0)
+        for (int q = 0; q < R; ++q) on[q] = row + q < end;
+        uint4 ru[R][G], rs[R][G], rdy[R][G], rds[R][G];
+        if (USUAL) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    F2 h[P<T>];
+        for (int q = 0; q < R; ++q) {
+            if (!on[q]) {                                            // zeros, which add nothing
 #pragma unroll
-                    for (int j = 0; j < P<T>; ++j) h[j] = mul2(fma2(p[g][j], rp, lp), d[g][j]);
-                    run.add(a.at[SUM_W_PRE] * G + g, h);
-                }
-            if (a.w_pre) scale_by<T, G, VEC>(a, a.w_pre, t, d);
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int j = 0; j < P<T>; ++j) {
-                    p[g][j] = fma2(p[g][j], rp, lp);
-                    p1 = add2(p1, d[g][j]);
-                    p2 = fma2(p[g][j], d[g][j], p2);
-                }
-            float2 c = make_float2(0.f, 0.f);
-            if (a.pre == FTP_NORM_LAYER) c = sum(sum2(p1), sum2(p2)); else c.y = sum(sum2(p2));
-            const F2 c1 = f2(-c.x * a.per_col), c2 = f2(-c.y * a.per_col);
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                F2 e[P<T>] = {};
-                if (a.ds) decode<T>(rds[g], e);
-#pragma unroll
-                for (int j = 0; j < P<T>; ++j) d[g][j] = fma2(rp, fma2(p[g][j], c2, add2(d[g][j], c1)), e[j]);
+                for (int g = 0; g < G; ++g) ru[q][g] = rs[q][g] = rdy[q][g] = rds[q][g] = make_uint4(0u, 0u, 0u, 0u);
+                continue;
             }
-        } else
-            decode_row<T, G>(rds, d);
-        clip_row<T, G, VEC>(a, t, d);
-        if (a.dx) {
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int j = 0; j < P<T>; ++j) p[g][j] = mul2(alpha, d[g][j]);
-            put_row<T, G, VEC>(a, out_row<T>(a.dx, a.lddx, row), t, p);
-        }
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int j = 0; j < P<T>; ++j) d[g][j] = mul2(d[g][j], f);
-        if (drop.cut) {
-            const unsigned long long n = drop.first_of(row, a.cols);
-#pragma unroll
-            for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(n, t, a.threads, g, d[g]);
-        }
-        float m = 0.f, r = 1.f;
-        if (a.post != FTP_NORM_NONE) { m = a.stats[row]; r = a.stats[a.rows + row]; }
-        const F2 rn = f2(r), ln = f2(-m * r);
-        if (a.dgate) {
-            decode_row<T, G>(ru, p);
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int j = 0; j < P<T>; ++j) p[g][j] = fma2(p[g][j], rn, ln);
-            if (a.w_post) scale_by<T, G, VEC>(a, a.w_post, t, p);
-            if (a.b_post) shift_by<T, G, VEC>(a, a.b_post, t, p);
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-#pragma unroll
-                for (int j = 0; j < P<T>; ++j) p[g][j] = mul2(p[g][j], d[g][j]);
-                if (a.gate_rows != 1) run.add(a.at[SUM_GATE] * G + g, p[g]);
+            if constexpr (USUAL) {
+                arrived(q, 0, rs[q]);
+                arrived(q, 1, rdy[q]);
+                arrived(q, 2, rds[q]);
+                arrived(q, 3, ru[q]);
+                continue;
             }
-            if (a.gate_rows == 1) put_row<T, G, VEC>(a, out_row<T>(a.dgate, a.lddg, row), t, p);
+            if (pre) fetch_row<T, G, VEC>(a, in_row<T>(a.s, a.lds, row + q), t, rs[q]);
+            if (USUAL || a.dy) fetch_row<T, G, VEC>(a, in_row<T>(a.dy, a.ldy, row + q), t, rdy[q]);
+            if (USUAL || a.ds) fetch_row<T, G, VEC>(a, in_row<T>(a.ds, a.ldds, row + q), t, rds[q]);
+            if (USUAL || a.u) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row + q), t, ru[q]);
         }
-        if (a.gate) gate_by<T, G, VEC>(a, row, t, d);
-        if (a.at[SUM_B_POST] >= 0)
+        if (USUAL) ahead(min(row + R, end));
+        float r[R];
+        F2 rp[R], lp[R], rn[R], ln[R];
 #pragma unroll
-            for (int g = 0; g < G; ++g) run.add(a.at[SUM_B_POST] * G + g, d[g]);
-        if (a.post != FTP_NORM_NONE) {
-            decode_row<T, G>(ru, p);
+        for (int q = 0; q < R; ++q) {
+            float ms = 0.f, mu = 0.f, ri = 1.f;
+            r[q] = 0.f;
+            if (pre && on[q]) { ms = a.stats[2 * a.rows + row + q]; r[q] = a.stats[3 * a.rows + row + q]; }
+            if (post && on[q]) { mu = a.stats[row + q]; ri = a.stats[a.rows + row + q]; }
+            rp[q] = f2(r[q]);
+            lp[q] = f2(-ms * r[q]);
+            rn[q] = f2(ri);
+            ln[q] = f2(-mu * ri);
+        }
+        F2 e[R][G][P<T>], xh[R][G][P<T>], mask[R][G][P<T>], uh[R][G][P<T>], sum[R][NS];   // mask: beta mask / (1 - p)
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) sum[q][i] = 0ull;
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int j = 0; j < P<T>; ++j) p[g][j] = fma2(p[g][j], rn, ln);
-            if (a.at[SUM_W_POST] >= 0)
+                for (int j = 0; j < P<T>; ++j) mask[q][g][j] = on[q] ? f : 0ull;
+            if (drop.cut) {
+                const unsigned long long n = drop.first_of(row + q, a.cols);
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    F2 h[P<T>];
-#pragma unroll
-                    for (int j = 0; j < P<T>; ++j) h[j] = mul2(p[g][j], d[g][j]);
-                    run.add(a.at[SUM_W_POST] * G + g, h);
-                }
-            if (a.w_post) scale_by<T, G, VEC>(a, a.w_post, t, d);
-            if (a.du) {
-                F2 q1 = 0ull, q2 = 0ull;
+                for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(n, t, a.threads, g, mask[q][g]);
+            }
+            clip_row<T, G, VEC>(a, t, mask[q]);
+            if (USUAL || a.ds) decode_row<T, G>(rds[q], e[q]);
+            else
 #pragma unroll
                 for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) e[q][g][j] = 0ull;
+        }
+        if (pre) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                F2 w[P<T>], h[P<T>], b[P<T>];
+                if (w_pre) fetch_vector<T, VEC>(a.w_pre, t, a.threads, g, a.cols, w);
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    F2 d[P<T>];
+                    decode<T>(rdy[q][g], d);
+                    if (!a.full) clip<T, VEC>(t, a.threads, g, a.cols, d);
+                    decode<T>(rs[q][g], xh[q][g]);
 #pragma unroll
                     for (int j = 0; j < P<T>; ++j) {
-                        q1 = add2(q1, d[g][j]);
-                        q2 = fma2(p[g][j], d[g][j], q2);
+                        xh[q][g][j] = fma2(xh[q][g][j], rp[q], lp[q]);
+                        h[j] = q ? fma2(xh[q][g][j], d[j], h[j]) : mul2(xh[q][g][j], d[j]);
+                        b[j] = q ? add2(b[j], d[j]) : d[j];
+                        if (w_pre) d[j] = mul2(d[j], w[j]);
+                        sum[q][0] = fma2(d[j], xh[q][g][j], sum[q][0]);
+                        if (LAYER) sum[q][3] = add2(sum[q][3], d[j]);
+                        e[q][g][j] = fma2(rp[q], d[j], e[q][g][j]);
                     }
-                float2 e = make_float2(0.f, 0.f);
-                if (a.post == FTP_NORM_LAYER) e = sum(sum2(q1), sum2(q2)); else e.y = sum(sum2(q2));
-                const F2 e1 = f2(-e.x * a.per_col), e2 = f2(-e.y * a.per_col);
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int j = 0; j < P<T>; ++j) d[g][j] = mul2(rn, fma2(p[g][j], e2, add2(d[g][j], e1)));
+                }
+                if (at_b_pre >= 0) run.add(at_b_pre * G + g, b);
+                if (at_w_pre >= 0) run.add(at_w_pre * G + g, h);
             }
         }
-        if (a.du) put_row<T, G, VEC>(a, out_row<T>(a.du, a.lddu, row), t, d);
+        if (USUAL || a.u) {
+#pragma unroll
+            for (int q = 0; q < R; ++q) decode_row<T, G>(ru[q], uh[q]);
+            if (post) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    F2 w[P<T>], gate[P<T>];
+                    if (w_post) fetch_vector<T, VEC>(a.w_post, t, a.threads, g, a.cols, w);
+#pragma unroll
+                    for (int q = 0; q < R; ++q) {
+                        if (gated && (q == 0 || (a.gate_rows && on[q]))) gate_of<T, VEC>(a, row + q, t, g, gate);
+#pragma unroll
+                        for (int j = 0; j < P<T>; ++j) {
+                            F2& x = uh[q][g][j];
+                            x = fma2(x, rn[q], ln[q]);
+                            F2 k = mask[q][g][j];
+                            if (gated) k = mul2(k, gate[j]);
+                            if (w_post) k = mul2(k, w[j]);
+                            const F2 z = mul2(k, x);
+                            sum[q][1] = fma2(z, e[q][g][j], sum[q][1]);
+                            if (pre) sum[q][2] = fma2(z, xh[q][g][j], sum[q][2]);
+                            if (LAYER) {
+                                sum[q][4] = add2(sum[q][4], z);
+                                sum[q][5] = fma2(k, e[q][g][j], sum[q][5]);
+                                if (pre) sum[q][6] = fma2(k, xh[q][g][j], sum[q][6]);
+                                sum[q][7] = add2(sum[q][7], k);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+        float all[R * NS];
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) all[q * NS + i] = sum2(sum[q][i]);
+        row_sums<R * NS>(all, red, turn);
+        F2 c1[R], c2[R], e1[R], e2[R];
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const float* s = all + q * NS;
+            const float c2f = -s[0] * a.per_col * r[q], c1f = LAYER && a.pre == FTP_NORM_LAYER ? -s[LAYER ? 3 : 0] * a.per_col * r[q] : 0.f;
+            c1[q] = f2(c1f);
+            c2[q] = f2(c2f);
+            e1[q] = e2[q] = 0ull;
+            if (post) {
+                e2[q] = f2(-fmaf(c2f, s[2], LAYER ? fmaf(c1f, s[LAYER ? 4 : 0], s[1]) : s[1]) * a.per_col);
+                if (LAYER && a.post == FTP_NORM_LAYER) e1[q] = f2(-fmaf(c2f, s[LAYER ? 6 : 0], fmaf(c1f, s[LAYER ? 7 : 0], s[LAYER ? 5 : 0])) * a.per_col);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            F2 w[P<T>], b[P<T>], gate[P<T>], of_gate[P<T>], of_w[P<T>], of_b[P<T>];
+            if (w_post) fetch_vector<T, VEC>(a.w_post, t, a.threads, g, a.cols, w);
+            if (graded && b_post) fetch_vector<T, VEC>(a.b_post, t, a.threads, g, a.cols, b);
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                F2 (&d)[P<T>] = e[q][g];
+                F2 (&x)[P<T>] = uh[q][g];
+                if (pre) {
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) {
+                        d[j] = fma2(c2[q], xh[q][g][j], d[j]);
+                        if (LAYER) d[j] = add2(d[j], c1[q]);
+                    }
+                }
+                if ((USUAL || a.dx) && on[q]) {
+                    F2 p[P<T>];
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) p[j] = mul2(alpha, d[j]);
+                    put<T, VEC>(out_row<T>(a.dx, a.lddx, row + q), t, a.threads, g, a.cols, encode<T>(p));
+                }
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) d[j] = mul2(d[j], mask[q][g][j]);
+                if (graded) {
+                    F2 p[P<T>];
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) {
+                        p[j] = w_post ? mul2(x[j], w[j]) : x[j];
+                        if (b_post) p[j] = add2(p[j], b[j]);
+                        p[j] = mul2(p[j], d[j]);
+                        of_gate[j] = q ? add2(of_gate[j], p[j]) : p[j];
+                    }
+                    if (a.gate_rows == 1 && on[q]) put<T, VEC>(out_row<T>(a.dgate, a.lddg, row + q), t, a.threads, g, a.cols, encode<T>(p));
+                }
+                if (gated) {
+                    if (q == 0 || (a.gate_rows && on[q])) gate_of<T, VEC>(a, row + q, t, g, gate);
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) d[j] = mul2(d[j], gate[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) {
+                    of_b[j] = q ? add2(of_b[j], d[j]) : d[j];
+                    of_w[j] = q ? fma2(d[j], x[j], of_w[j]) : mul2(d[j], x[j]);
+                }
+                if ((USUAL || a.du) && on[q]) {
+                    if (post) {
+#pragma unroll
+                        for (int j = 0; j < P<T>; ++j) {
+                            if (w_post) d[j] = mul2(d[j], w[j]);
+                            if (LAYER) d[j] = add2(d[j], e1[q]);
+                            d[j] = mul2(rn[q], fma2(e2[q], x[j], d[j]));
+                        }
+                    }
+                    put<T, VEC>(out_row<T>(a.du, a.lddu, row + q), t, a.threads, g, a.cols, encode<T>(d));
+                }
+            }
+            if (graded && a.gate_rows != 1) run.add(at_gate * G + g, of_gate);
+            if (at_b_post >= 0) run.add(at_b_post * G + g, of_b);
+            if (at_w_post >= 0) run.add(at_w_post * G + g, of_w);
+        }
+        row = min(row + R, end);
     }
     if (a.gate_sums && first < a.rows) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float v[V<T>];
-            run.get(a.at[SUM_GATE] * G + g, v);
+            run.get(at_gate * G + g, v);
             put_vector<T, VEC>(a.gate_sums + (mine + group) * a.cols, t, a.threads, g, a.cols, v);
         }
     }
@@ -411,21 +529,32 @@ __global__ void __launch_bounds__(backward_threads(G * V<T>)) join_backward_kern
     }
 }
 
-// Blocks' column sums joined in double, 16 threads a column.
+// Blocks' column sums joined in double: a warp per 32 columns and 32nd of the blocks, eight loads in flight.
 struct JoinSums { const float* part; float* out[SUMS]; int n, cols; int64_t blocks; };
-__global__ void __launch_bounds__(512) join_sums_kernel(const JoinSums a) {
-    __shared__ double part[16][33];
+__global__ void __launch_bounds__(1024) join_sums_kernel(const JoinSums a) {
+    constexpr int W = 32, U = 8;
+    __shared__ double part[W][33];
     grid_dep_sync();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     double s = 0.0;
-    if (c < a.cols)
-        for (int64_t b = w; b < a.blocks; b += 16) s += a.part[((size_t)b * a.n + blockIdx.y) * a.cols + c];
+    if (c < a.cols) {
+        const int64_t step = (int64_t)a.n * a.cols;
+        const float* p = a.part + (int64_t)blockIdx.y * a.cols + c;
+        for (int64_t b = w; b < a.blocks; b += W * U) {
+            float v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = b + u * W < a.blocks ? p[(b + u * W) * step] : 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += v[u];
+        }
+    }
     part[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < a.cols) {
-        for (int i = 1; i < 16; ++i) s += part[i][lane];
-        a.out[blockIdx.y][c] = (float)s;
+    for (int n = W / 2; n; n >>= 1) {
+        if (w < n) part[w][lane] = s += part[w + n][lane];
+        __syncthreads();
     }
+    if (w == 0 && c < a.cols) a.out[blockIdx.y][c] = (float)s;
 }
 // A group's gate gradient: the sums of the runs that hold rows of it.
 template <typename T>
@@ -544,13 +673,13 @@ JoinPlan plan_backward(const ftp_join_desc* d) {
     JoinPlan p;
     const int v = d->precision == FTP_FP32 ? 4 : 8;
     row_shape(d->cols, v, d->cols <= 512 * v ? 1 : 16 / v, &p.threads, &p.groups);
-    const int64_t each = (int64_t)SMS * std::min(16, backward_threads(p.groups * v) / p.threads);
+    const int64_t each = (int64_t)SMS * std::min(16, BACKWARD_THREADS / p.threads);
     p.run = (int)std::min<int64_t>(64, std::max<int64_t>(4, (d->rows + each - 1) / each));
     p.blocks = (d->rows + p.run - 1) / p.run;
     return p;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-constexpr size_t MOST_SMEM = 200 * 1024;
+constexpr size_t MOST_SMEM = 200 * 1024;                          // for the running sums
 struct JoinSpace { size_t sums, gate, spill, total; };
 JoinSpace space_of(const ftp_join_desc* d, const JoinPlan& p, int nsums) {
     const int v = d->precision == FTP_FP32 ? 4 : 8;
@@ -564,26 +693,40 @@ JoinSpace space_of(const ftp_join_desc* d, const JoinPlan& p, int nsums) {
 }
 
 template <typename T, int G>
-ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, cudaStream_t st, const char* who) {
-    const size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * p.threads * 4;
-    auto kern = vec ? join_backward_kernel<T, G, true> : join_backward_kernel<T, G, false>;
-    if (smem > 40 * 1024)                                            // 48 KB with what the kernel holds beside it
-        FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SMEM) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
+ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, bool usual, cudaStream_t st, const char* who) {
+    size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * p.threads * 4;
+    const bool layer = a.post == FTP_NORM_LAYER || a.pre == FTP_NORM_LAYER;
+    void (*kern)(JoinArgs) = nullptr;
+    size_t staged = 0;
+    if constexpr (G * V<T> <= 16)
+        if (usual) {
+            kern = layer ? join_backward_kernel<T, G, true, true, true> : join_backward_kernel<T, G, true, false, true>;
+            staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
+        }
+    if (!kern)
+        kern = layer ? (vec ? join_backward_kernel<T, G, true, true, false> : join_backward_kernel<T, G, false, true, false>)
+                     : (vec ? join_backward_kernel<T, G, true, false, false> : join_backward_kernel<T, G, false, false, false>);
+    smem += staged;
+    // 48 KB with what the kernel holds beside it
+    if (smem > 40 * 1024) FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 220 * 1024), FTP_ECUDA, "%s: no shared memory", who);
     launch(kern, dim3((unsigned)p.blocks), dim3(p.threads), smem, st, a);
     return FTP_OK;
 }
+template <typename T> bool wide_rows(const JoinArgs& a) {
+    return a.cols % V<T> == 0 && wide<T>(a.u, a.ldu, a.rows) && wide<T>(a.s, a.lds, a.rows) && wide<T>(a.dy, a.ldy, a.rows) && wide<T>(a.ds, a.ldds, a.rows) &&
+           wide<T>(a.du, a.lddu, a.rows) && wide<T>(a.dx, a.lddx, a.rows) && (a.gate_rows ? wide<T>(a.gate, a.ldg, 2) : on_bytes(a.gate, 16)) &&
+           (a.gate_rows != 1 || wide<T>(a.dgate, a.lddg, a.rows)) && wide_vectors({a.w_post, a.b_post, a.w_pre, a.out[0], a.out[1], a.out[2], a.out[3], a.out[4]});
+}
 template <typename T>
-ftp_status run_backward(JoinArgs& a, const JoinPlan& p, cudaStream_t st, const char* who) {
+ftp_status run_backward(JoinArgs& a, const JoinPlan& p, bool usual, cudaStream_t st, const char* who) {
     a.threads = p.threads;
     a.full = fills<T>(a, p.groups);
-    const bool vec = a.cols % V<T> == 0 && wide<T>(a.u, a.ldu, a.rows) && wide<T>(a.s, a.lds, a.rows) && wide<T>(a.dy, a.ldy, a.rows) && wide<T>(a.ds, a.ldds, a.rows) &&
-                     wide<T>(a.du, a.lddu, a.rows) && wide<T>(a.dx, a.lddx, a.rows) && (a.gate_rows ? wide<T>(a.gate, a.ldg, 2) : on_bytes(a.gate, 16)) &&
-                     (a.gate_rows != 1 || wide<T>(a.dgate, a.lddg, a.rows)) && wide_vectors({a.w_post, a.b_post, a.w_pre, a.out[0], a.out[1], a.out[2], a.out[3], a.out[4]});
+    const bool vec = wide_rows<T>(a);
     switch (p.groups) {
-        case 1: return backward_of<T, 1>(a, p, vec, st, who);
-        case 2: return backward_of<T, 2>(a, p, vec, st, who);
-        case 4: return backward_of<T, 4>(a, p, vec, st, who);
-        default: if constexpr (sizeof(T) == 4) return backward_of<T, 8>(a, p, vec, st, who);
+        case 1: return backward_of<T, 1>(a, p, vec, usual, st, who);
+        case 2: return backward_of<T, 2>(a, p, vec, usual, st, who);
+        case 4: return backward_of<T, 4>(a, p, vec, usual, st, who);
+        default: if constexpr (sizeof(T) == 4) return backward_of<T, 8>(a, p, vec, usual, st, who);
     }
     return FTP_OK;
 }
@@ -678,16 +821,21 @@ ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* 
         if (out[i]) j.out[a.nsums] = out[i];
         if (a.at[i] >= 0) ++a.nsums;
     }
+    const auto whole_groups = [&](const JoinArgs& q) { return d->precision == FTP_FP32 ? wide_rows<float>(q) : wide_rows<bf16>(q); };
+    // what the kernel for the usual call takes as known
+    const bool layer = d->post == FTP_NORM_LAYER || d->pre == FTP_NORM_LAYER;
+    const bool usual = d->post != FTP_NORM_NONE && d->pre != FTP_NORM_NONE && w_post && w_pre && dw_post && dw_pre && ds && dx && du && layer == (b_post != nullptr) &&
+                       layer == (db_post != nullptr) && layer == (db_pre != nullptr) && whole_groups(a);
     const JoinSpace sp = space_of(d, p, SUMS), now = space_of(d, p, a.nsums);
     char* base = static_cast<char*>(ws);
     a.sums = reinterpret_cast<float*>(base);
     if (shared_gate) a.gate_sums = reinterpret_cast<float*>(base + sp.sums);
     if (now.spill) a.spill = reinterpret_cast<float*>(base + sp.sums + sp.gate);
-    if (ftp_status r = d->precision == FTP_FP32 ? run_backward<float>(a, p, st, who) : run_backward<bf16>(a, p, st, who)) return r;
+    if (ftp_status r = d->precision == FTP_FP32 ? run_backward<float>(a, p, usual, st, who) : run_backward<bf16>(a, p, usual, st, who)) return r;
     const int n = a.nsums - shared_gate;
     if (n && p.blocks > 1) {
         j.part = a.sums; j.n = n; j.cols = d->cols; j.blocks = p.blocks;
-        launch(join_sums_kernel, dim3((d->cols + 31) / 32, n), dim3(512), 0, st, j);
+        launch(join_sums_kernel, dim3((d->cols + 31) / 32, n), dim3(1024), 0, st, j);
     }
     if (shared_gate) {
         const int64_t groups = (d->rows + d->gate_rows - 1) / d->gate_rows;

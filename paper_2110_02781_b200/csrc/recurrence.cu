@@ -803,7 +803,7 @@ template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& 
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     auto kern = recurrence_backward_kernel<T, VEC, FORM>;
     const size_t smem = (size_t)(a.coupled ? 2 : 1) * RUN * 32 * warps * LANES<T> * 4;
-    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * RUN * 32 * WARPS * LANES<T> * 4) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
+    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 2 * RUN * 32 * WARPS * LANES<T> * 4), FTP_ECUDA, "%s: no shared memory", who);
     int* err = ffn::status_word();
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, a, err);
@@ -823,7 +823,7 @@ template <typename T, int FORM> ftp_status forward_stream(const RecArgs& a, cuda
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     auto kern = a.coupled ? recurrence_forward_stream_kernel<T, FORM, true> : recurrence_forward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 6 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
-    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + 8))) == cudaSuccess, FTP_ECUDA, "%s: no shared memory", who);
+    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + 8)), FTP_ECUDA, "%s: no shared memory", who);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, y, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
@@ -841,7 +841,7 @@ template <typename T, int FORM> ftp_status backward_stream(const RecArgs& a, cud
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     auto kern = a.coupled ? recurrence_backward_stream_kernel<T, FORM, true> : recurrence_backward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 8 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
-    FTP_REQUIRE(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + 8))) == cudaSuccess, FTP_ECUDA,
+    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + 8)), FTP_ECUDA,
                 "%s: no shared memory", who);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, out, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

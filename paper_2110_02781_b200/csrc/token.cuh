@@ -48,6 +48,20 @@ __device__ __forceinline__ unsigned on_rank(unsigned at, unsigned rank) {
     return r;
 }
 
+// lets a kernel have `bytes` of dynamic shared memory; asked of the driver once per kernel and device (1.5 us a call otherwise)
+inline bool more_shared(const void* kern, size_t bytes) {
+    static thread_local const void* known[64] = {};
+    static thread_local int devices[64] = {};
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const size_t at = (reinterpret_cast<uintptr_t>(kern) >> 4) % 64;
+    if (known[at] == kern && devices[at] == dev) return true;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    known[at] = kern;
+    devices[at] = dev;
+    return true;
+}
+
 // ---- a row's columns on its threads ----
 // A thread holds groups of V columns (16 bytes).  VEC: V neighbours, one access (every row starts on 16 bytes and holds
 // whole groups).  Otherwise the V columns lie `threads` apart, so that a warp's accesses are still neighbours.
@@ -175,42 +189,44 @@ template <typename T, bool VEC> __device__ __forceinline__ void fetch_vector(con
 // Sums over the threads of a block (32 to 512, a power of two) that holds one row, through one place per warp; `red` holds two sets of
 // 16 places, used in turn, so that one barrier a sum is enough.  The order of additions depends on the thread alone.
 struct RowSum {
-    float2* red;
+    float* red;
     int turn;
     __device__ __forceinline__ float operator()(float a) {
 #pragma unroll
         for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
         const int n = blockDim.x >> 5, lane = threadIdx.x & 31;
         if (n == 1) return a;
-        float2* at = red + turn * 16;
+        float* at = red + turn * 16;
         turn ^= 1;
-        if (lane == 0) at[threadIdx.x >> 5].x = a;
+        if (lane == 0) at[threadIdx.x >> 5] = a;
         __syncthreads();
-        a = at[lane & (n - 1)].x;
+        a = at[lane & (n - 1)];
         for (int d = n >> 1; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
         return a;
     }
-    __device__ __forceinline__ float2 operator()(float a, float b) {
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, d);
-            b += __shfl_xor_sync(0xffffffffu, b, d);
-        }
-        const int n = blockDim.x >> 5, lane = threadIdx.x & 31;
-        if (n == 1) return make_float2(a, b);
-        float2* at = red + turn * 16;
-        turn ^= 1;
-        if (lane == 0) at[threadIdx.x >> 5] = make_float2(a, b);
-        __syncthreads();
-        const float2 q = at[lane & (n - 1)];
-        a = q.x; b = q.y;
-        for (int d = n >> 1; d; d >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, d);
-            b += __shfl_xor_sync(0xffffffffu, b, d);
-        }
-        return make_float2(a, b);
-    }
 };
+// N such sums at once; `red`: two sets of 16 N floats
+template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& turn) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int d = 16; d; d >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+    const int n = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (n == 1) return;
+    float* at = red + turn * 16 * N;
+    turn ^= 1;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[(threadIdx.x >> 5) * N + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = at[(lane & (n - 1)) * N + i];
+    for (int d = n >> 1; d; d >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+    }
+}
 
 // ---- dropout ----
 // Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; SC 2011).
