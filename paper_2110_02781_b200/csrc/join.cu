@@ -22,7 +22,7 @@ struct JoinArgs {
     const float *w_post, *b_post, *w_pre, *b_pre;
     float* stats;                            // four planes of `rows`: mean and 1 / deviation of u, of s
     int64_t rows, ldu, ldx, lds, ldy, ldg, lddu, ldds, lddx, lddg, gate_rows;
-    int cols, threads, post, pre, full;          // full: no thread has columns behind the last one
+    int cols, threads, groups, post, pre, full;  // full: no thread has columns behind the last one
     float eps, alpha, beta, per_col;         // per_col: 1 / cols
     Drop drop;
     // backward
@@ -219,8 +219,7 @@ __global__ void __launch_bounds__(forward_threads(G * V<T>)) join_forward_kernel
     }
 }
 
-// A thread's running sum number `i` (of V columns): float4s that lie a block's width apart.  Only the widest rows may have theirs in
-// global memory.
+// A thread's running sum number `i` (of V columns): float4s that lie a block's width apart.
 template <typename T> struct Running {
     float4* at;
     __device__ __forceinline__ float4& q(int i, int k) const { return at[(unsigned)(i * (V<T> / 4) + k) * blockDim.x]; }
@@ -266,7 +265,6 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
     const int t = threadIdx.x;
     int turn = 0;
     Running<T> run{dynamic + t};
-    if (G * V<T> >= 32 && a.spill) run.at = reinterpret_cast<float4*>(a.spill) + (size_t)blockIdx.x * a.nsums * (G * (V<T> / 4)) * blockDim.x + t;
     for (int i = 0; i < a.nsums * G; ++i) run.clear(i);
     const int64_t mine = blockIdx.x, first = mine * a.run, last = min(first + a.run, a.rows);
     int64_t group = a.gate_rows > 1 ? first / a.gate_rows : 0, next = a.gate_rows > 1 ? (group + 1) * a.gate_rows : 0;   // next: first row of the next group
@@ -529,6 +527,197 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
     }
 }
 
+// The same for rows of more than 16 columns a thread, whose values do not fit into registers: a group of columns at a time, every group read twice (the
+// second time from the second cache: 2000 x 16384 bf16 with all terms 1090 us with the values spilled to local memory, and less than half of that so).
+template <typename T, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(const JoinArgs a) {
+    constexpr int NS = LAYER ? 8 : 3;
+    extern __shared__ float4 dynamic[];
+    __shared__ float red[2 * 16 * NS];
+    __shared__ Rounds keys;
+    grid_dep_sync();
+    const Dropping drop(a.drop, keys);
+    const bool pre = a.pre != FTP_NORM_NONE, post = a.post != FTP_NORM_NONE;
+    const int t = threadIdx.x, G = a.groups;
+    int turn = 0;
+    Running<T> run{(a.spill ? reinterpret_cast<float4*>(a.spill) + (size_t)blockIdx.x * a.nsums * G * (V<T> / 4) * blockDim.x : dynamic) + t};
+    for (int i = 0; i < a.nsums * G; ++i) run.clear(i);
+    const int64_t mine = blockIdx.x, first = mine * a.run, last = min(first + a.run, a.rows);
+    int64_t group = a.gate_rows > 1 ? first / a.gate_rows : 0, next = a.gate_rows > 1 ? (group + 1) * a.gate_rows : 0;
+    const F2 f = f2(drop.cut ? a.beta * a.drop.factor : a.beta), alpha = f2(a.alpha);
+    const auto flush = [&](int64_t slot, bool again) {
+        for (int g = 0; g < G; ++g) {
+            float v[V<T>];
+            run.get(a.at[SUM_GATE] * G + g, v);
+            put_vector<T, VEC>(a.gate_sums + slot * a.cols, t, a.threads, g, a.cols, v);
+            if (again) run.clear(a.at[SUM_GATE] * G + g);
+        }
+    };
+    for (int64_t row = first; row < last; ++row) {
+        if (a.gate_sums && row == next) {
+            flush(mine + group, true);
+            ++group;
+            next += a.gate_rows;
+        }
+        float ms = 0.f, r = 0.f, mu = 0.f, ri = 1.f;
+        if (pre) { ms = a.stats[2 * a.rows + row]; r = a.stats[3 * a.rows + row]; }
+        if (post) { mu = a.stats[row]; ri = a.stats[a.rows + row]; }
+        const F2 rp = f2(r), lp = f2(-ms * r), rn = f2(ri), ln = f2(-mu * ri);
+        const unsigned long long number = drop.cut ? drop.first_of(row, a.cols) : 0;
+        // e, x^, beta mask / (1 - p), u^ and dy of a group
+        const auto load = [&](int g, F2 (&e)[P<T>], F2 (&xh)[P<T>], F2 (&mask)[P<T>], F2 (&uh)[P<T>], F2 (&dy)[P<T>]) {
+            uint4 rs, rdy, rds, ru;
+            if (pre) rs = fetch<T, VEC>(in_row<T>(a.s, a.lds, row), t, a.threads, g, a.cols);
+            if (a.dy) rdy = fetch<T, VEC>(in_row<T>(a.dy, a.ldy, row), t, a.threads, g, a.cols);
+            if (a.ds) rds = fetch<T, VEC>(in_row<T>(a.ds, a.ldds, row), t, a.threads, g, a.cols);
+            if (a.u) ru = fetch<T, VEC>(in_row<T>(a.u, a.ldu, row), t, a.threads, g, a.cols);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) { e[j] = xh[j] = uh[j] = dy[j] = 0ull; mask[j] = f; }
+            if (drop.cut) drop.template operator()<T, VEC>(number, t, a.threads, g, mask);
+            clip<T, VEC>(t, a.threads, g, a.cols, mask);
+            if (a.ds) decode<T>(rds, e);
+            if (a.u) decode<T>(ru, uh);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) uh[j] = fma2(uh[j], rn, ln);
+            if (!pre) return;
+            F2 w[P<T>];
+            decode<T>(rdy, dy);
+            clip<T, VEC>(t, a.threads, g, a.cols, dy);
+            decode<T>(rs, xh);
+            if (a.w_pre) fetch_vector<T, VEC>(a.w_pre, t, a.threads, g, a.cols, w);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) {
+                xh[j] = fma2(xh[j], rp, lp);
+                e[j] = fma2(rp, a.w_pre ? mul2(dy[j], w[j]) : dy[j], e[j]);
+            }
+        };
+        // K and K w_post
+        const auto factors = [&](int g, const F2 (&mask)[P<T>], F2 (&k)[P<T>], F2 (&kw)[P<T>]) {
+            F2 w[P<T>];
+            if (a.gate) gate_of<T, VEC>(a, row, t, g, w);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) k[j] = a.gate ? mul2(mask[j], w[j]) : mask[j];
+            if (a.w_post) fetch_vector<T, VEC>(a.w_post, t, a.threads, g, a.cols, w);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) kw[j] = a.w_post ? mul2(k[j], w[j]) : k[j];
+        };
+        F2 sum[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sum[i] = 0ull;
+        if (pre || post)
+#pragma unroll 1
+            for (int g = 0; g < G; ++g) {
+                F2 e[P<T>], xh[P<T>], mask[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
+                load(g, e, xh, mask, uh, dy);
+                if (a.at[SUM_B_PRE] >= 0) run.add(a.at[SUM_B_PRE] * G + g, dy);
+                if (a.at[SUM_W_PRE] >= 0) {
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) k[j] = mul2(xh[j], dy[j]);
+                    run.add(a.at[SUM_W_PRE] * G + g, k);
+                }
+                if (pre) {
+                    F2 w[P<T>];
+                    if (a.w_pre) fetch_vector<T, VEC>(a.w_pre, t, a.threads, g, a.cols, w);
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) {
+                        const F2 d = a.w_pre ? mul2(dy[j], w[j]) : dy[j];
+                        sum[0] = fma2(d, xh[j], sum[0]);
+                        if (LAYER) sum[3] = add2(sum[3], d);
+                    }
+                }
+                if (post) {
+                    factors(g, mask, k, kw);
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) {
+                        const F2 z = mul2(kw[j], uh[j]);
+                        sum[1] = fma2(z, e[j], sum[1]);
+                        sum[2] = fma2(z, xh[j], sum[2]);
+                        if (LAYER) {
+                            sum[4] = add2(sum[4], z);
+                            sum[5] = fma2(kw[j], e[j], sum[5]);
+                            sum[6] = fma2(kw[j], xh[j], sum[6]);
+                            sum[7] = add2(sum[7], kw[j]);
+                        }
+                    }
+                }
+            }
+        float s[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) s[i] = sum2(sum[i]);
+        row_sums<NS>(s, red, turn);
+        const float c2f = -s[0] * a.per_col * r, c1f = LAYER && a.pre == FTP_NORM_LAYER ? -s[LAYER ? 3 : 0] * a.per_col * r : 0.f;
+        float e1 = 0.f, e2 = 0.f;
+        if (post) {
+            e2 = -fmaf(c2f, s[2], LAYER ? fmaf(c1f, s[LAYER ? 4 : 0], s[1]) : s[1]) * a.per_col;
+            if (LAYER && a.post == FTP_NORM_LAYER) e1 = -fmaf(c2f, s[LAYER ? 6 : 0], fmaf(c1f, s[LAYER ? 7 : 0], s[LAYER ? 5 : 0])) * a.per_col;
+        }
+        // dx may lie on ds: a thread reads its columns of a group before it writes them
+#pragma unroll 1
+        for (int g = 0; g < G; ++g) {
+            F2 d[P<T>], xh[P<T>], mask[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
+            load(g, d, xh, mask, uh, dy);
+            factors(g, mask, k, kw);
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) {
+                d[j] = fma2(f2(c2f), xh[j], d[j]);
+                if (LAYER) d[j] = add2(d[j], f2(c1f));
+                dy[j] = mul2(alpha, d[j]);
+            }
+            if (a.dx) put<T, VEC>(out_row<T>(a.dx, a.lddx, row), t, a.threads, g, a.cols, encode<T>(dy));
+            if (a.dgate) {
+                F2 w[P<T>], p[P<T>];
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) p[j] = uh[j];
+                if (a.w_post) {
+                    fetch_vector<T, VEC>(a.w_post, t, a.threads, g, a.cols, w);
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) p[j] = mul2(p[j], w[j]);
+                }
+                if (a.b_post) {
+                    fetch_vector<T, VEC>(a.b_post, t, a.threads, g, a.cols, w);
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) p[j] = add2(p[j], w[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) p[j] = mul2(p[j], mul2(d[j], mask[j]));
+                if (a.gate_rows == 1) put<T, VEC>(out_row<T>(a.dgate, a.lddg, row), t, a.threads, g, a.cols, encode<T>(p));
+                else run.add(a.at[SUM_GATE] * G + g, p);
+            }
+#pragma unroll
+            for (int j = 0; j < P<T>; ++j) {
+                k[j] = mul2(k[j], d[j]);
+                d[j] = mul2(kw[j], d[j]);
+            }
+            if (a.at[SUM_B_POST] >= 0) run.add(a.at[SUM_B_POST] * G + g, k);
+            if (a.at[SUM_W_POST] >= 0) {
+#pragma unroll
+                for (int j = 0; j < P<T>; ++j) k[j] = mul2(k[j], uh[j]);
+                run.add(a.at[SUM_W_POST] * G + g, k);
+            }
+            if (a.du) {
+                if (post)
+#pragma unroll
+                    for (int j = 0; j < P<T>; ++j) d[j] = mul2(rn, fma2(f2(e2), uh[j], add2(d[j], f2(e1))));
+                put<T, VEC>(out_row<T>(a.du, a.lddu, row), t, a.threads, g, a.cols, encode<T>(d));
+            }
+        }
+    }
+    if (a.gate_sums && first < a.rows) flush(mine + group, false);
+    const int n = a.gate_sums ? a.nsums - 1 : a.nsums;
+    for (int k = 0; k < n; ++k) {
+        float* to = a.sums + ((size_t)blockIdx.x * n + k) * a.cols;
+        if (gridDim.x == 1) {
+#pragma unroll
+            for (int o = 0; o < SUMS; ++o) if (a.at[o] == k) to = a.out[o];
+        }
+        for (int g = 0; g < G; ++g) {
+            float v[V<T>];
+            run.get(k * G + g, v);
+            put_vector<T, VEC>(to, t, a.threads, g, a.cols, v);
+        }
+    }
+}
+
 // Blocks' column sums joined in double: a warp per 32 columns and 32nd of the blocks, eight loads in flight.
 struct JoinSums { const float* part; float* out[SUMS]; int n, cols; int64_t blocks; };
 __global__ void __launch_bounds__(1024) join_sums_kernel(const JoinSums a) {
@@ -720,13 +909,22 @@ template <typename T> bool wide_rows(const JoinArgs& a) {
 template <typename T>
 ftp_status run_backward(JoinArgs& a, const JoinPlan& p, bool usual, cudaStream_t st, const char* who) {
     a.threads = p.threads;
+    a.groups = p.groups;
     a.full = fills<T>(a, p.groups);
     const bool vec = wide_rows<T>(a);
+    if (p.groups * V<T> > 16) {
+        const bool layer = a.post == FTP_NORM_LAYER || a.pre == FTP_NORM_LAYER;
+        auto kern = layer ? (vec ? join_backward_wide_kernel<T, true, true> : join_backward_wide_kernel<T, false, true>)
+                          : (vec ? join_backward_wide_kernel<T, true, false> : join_backward_wide_kernel<T, false, false>);
+        const size_t smem = a.spill ? 0 : (size_t)a.nsums * p.groups * V<T> * p.threads * 4;
+        FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 220 * 1024), FTP_ECUDA, "%s: no shared memory", who);
+        launch(kern, dim3((unsigned)p.blocks), dim3(p.threads), smem, st, a);
+        return FTP_OK;
+    }
     switch (p.groups) {
         case 1: return backward_of<T, 1>(a, p, vec, usual, st, who);
         case 2: return backward_of<T, 2>(a, p, vec, usual, st, who);
-        case 4: return backward_of<T, 4>(a, p, vec, usual, st, who);
-        default: if constexpr (sizeof(T) == 4) return backward_of<T, 8>(a, p, vec, usual, st, who);
+        case 4: if constexpr (sizeof(T) == 4) return backward_of<T, 4>(a, p, vec, usual, st, who);
     }
     return FTP_OK;
 }

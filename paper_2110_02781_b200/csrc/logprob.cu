@@ -24,7 +24,7 @@ struct LogpArgs {
     float *logp, *entropy, *lse, *top_logp;
     int32_t* top;
     int64_t rows, ld;
-    int vocab, k;
+    int vocab, k, room;                                              // room: candidates that fit into shared memory
     float scale, scale2;                                             // scale2: scale * log2(e)
 };
 
@@ -164,19 +164,14 @@ __device__ __forceinline__ Key merge(Key a, Key b) {
 }
 
 template <typename T, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const LogpArgs a) {
-    extern __shared__ Key cand[];                                    // TOP: CAND candidates
+__device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsigned ranks, unsigned rank) {
+    extern __shared__ Key cand[];                                    // TOP: candidates
     __shared__ float red[3][16];
     __shared__ float part[3], total[3];
     __shared__ unsigned bound[32];
     __shared__ Key best[MOST_TOP], joined[4][MOST_TOP];
     __shared__ int hit[TOP ? MOST_THREADS : 1], hits, found;
-    grid_dep_sync();
-    unsigned ranks;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    const unsigned rank = cluster_rank();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, w = tid >> 5, warps = threads >> 5;
-    const int64_t row = blockIdx.x / ranks;
     const Row<T> x(a.x, row, a.ld, a.vocab);
     const int me = (int)rank * threads + tid, stride = (int)ranks * threads;
     Sums<T, ENTROPY> s;
@@ -235,7 +230,8 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
         // the warp's largest thread maxima
         unsigned o = order_of(mine);
         const int each = 32 / warps;
-        for (int k = 0; k < each; ++k) {
+        if (warps == 1) bound[lane] = o;
+        else for (int k = 0; k < each; ++k) {
             const unsigned top = __reduce_max_sync(0xffffffffu, o);
             const unsigned who = __ballot_sync(0xffffffffu, o == top);
             if (lane == __ffs(who) - 1) o = 0;
@@ -265,7 +261,7 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
                 const int c = g * V<T> + j - x.off;
                 if (c < 0 || c >= a.vocab) continue;
                 const int at = atomicAdd(&found, 1);
-                if (at < CAND) cand[at] = key_of(v[j], c);
+                if (at < a.room) cand[at] = key_of(v[j], c);
             }
         };
         if (x.first + 4 * stride >= x.end) {
@@ -288,7 +284,7 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
         }
         __syncthreads();
         const int n = found;
-        if (n <= CAND) {                                             // how many are larger: a warp per candidate
+        if (n <= a.room) {                                             // how many are larger: a warp per candidate
             for (int k = w; k < n; k += warps) {
                 const Key mykey = cand[k];
                 int rnk = 0;
@@ -375,6 +371,15 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
         }
     }
     if (ranks > 1) cluster_sync();                                   // nobody leaves while the first block reads its shared memory
+}
+
+// (A block that walks over several rows is slower, 85 instead of 78 us for 16000 x 120 bf16: nothing hides the end of a row.)
+template <typename T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const LogpArgs a) {
+    grid_dep_sync();
+    unsigned ranks;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    logprob_row<T, ENTROPY, TOP>(a, blockIdx.x / ranks, ranks, cluster_rank());
 }
 
 struct LogpBack {
@@ -467,15 +472,16 @@ ftp_status check(const void* logits, int64_t rows, int32_t vocab, int64_t* ld, i
 }
 
 template <typename T> cudaError_t forward_of(const LogpArgs& a, cudaStream_t st) {
-    // a thread takes four groups and more, 64 where the rows fill the GPU (4096 x 50021 bf16: 101 us with 512 threads a row, 82 with
-    // 256, 77 with 128, 113 with 64); blocks of 512 share a row while that gives every multiprocessor no more than two
+    // A thread takes four groups and more, about 50 where the rows fill the GPU (4096 x 50021 bf16: 101 us with 512 threads a row, 82 with 256, 77 with
+    // 128, 113 with 64; 4000 x 32000 with 20 top tokens 90, 83, 131 us with 256, 128, 64); blocks share a row while that gives every multiprocessor no more than two.
     const int groups = (a.vocab + V<T> - 1) / V<T>;
+    const int each = a.rows < SMS ? 4 : 50;                          // whatever k is, so that log probabilities do not depend on it
     int threads = 32, ranks = 1;
-    while (threads < MOST_THREADS && threads * (a.rows >= SMS ? 64 : 4) < groups) threads *= 2;
+    while (threads < MOST_THREADS && threads * each < groups) threads *= 2;
     while (ranks < 8 && a.rows * ranks * 2 <= 2 * SMS && ranks * 2 * threads * 2 <= groups) ranks *= 2;
     auto kern = a.k ? (a.entropy ? logprob_forward_kernel<T, true, true> : logprob_forward_kernel<T, false, true>)
                     : (a.entropy ? logprob_forward_kernel<T, true, false> : logprob_forward_kernel<T, false, false>);
-    return launch_cluster(kern, dim3((unsigned)(a.rows * ranks)), threads, a.k ? CAND * sizeof(Key) : 0, ranks, st, a);
+    return launch_cluster(kern, dim3((unsigned)(a.rows * ranks)), threads, a.k ? a.room * sizeof(Key) : 0, ranks, st, a);
 }
 
 }  // namespace
@@ -497,7 +503,7 @@ ftp_status ftp_logprob_forward(const void* logits, int64_t rows, int32_t vocab, 
     if (ftp_status s = check_elements({targets, logp, entropy, lse, top, top_logp}, 4, who)) return s;
     if (ftp_status s = check_addresses({logp, entropy, lse, top, top_logp}, {logits, targets}, who)) return s;
     if (rows == 0) return FTP_OK;
-    const LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, scale, scale * 1.44269504088896341f};
+    const LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, std::max(32, std::min(CAND, vocab)), scale, scale * 1.44269504088896341f};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = precision == FTP_FP32 ? forward_of<float>(a, st) : forward_of<bf16>(a, st);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

@@ -4,7 +4,7 @@
 // Bound by memory: one pass over f, v, o and y (backward: f, v, o, dy in, df, dv, do out).  A step is the map h -> a h + b, and the
 // maps of a run of steps compose to one, h -> A h + B.  A thread holds a run of 16 steps of two neighbouring channels (bf16; one
 // float channel) in registers, all its loads in flight at once; a warp 32 threads of one run; a block up to eight runs after one
-// another, and a cluster of up to eight blocks the runs after those, so that a long sequence of few channels still fills the GPU.
+// another, and a cluster of up to sixteen blocks the runs after those, so that a long sequence of few channels still fills the GPU.
 // The runs' maps go through shared memory, the blocks' through the cluster's, and are applied in the order of time, whatever
 // finishes first: one read of the data and the same bits every time.  The state and the maps are float.
 // The backward pass starts every run from the state that the forward pass kept in front of it, walks it forward once and then, with
@@ -18,7 +18,7 @@ namespace ftp {
 namespace token {
 namespace {
 
-constexpr int RUN = 16, WARPS = 8;
+constexpr int RUN = 16, WARPS = 8, BACK_WARPS = 4, MOST_RANKS = 16;   // runs of a block forward and backward; blocks of a cluster at most
 template <typename T> constexpr int LANES = 4 / (int)sizeof(T);      // channels of a thread
 template <typename T> constexpr int TILE = 32 * LANES<T>;            // of a block
 
@@ -256,7 +256,7 @@ template <typename T, bool VEC, int FORM> struct Forward {
 template <typename T, bool VEC, int FORM>
 __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const RecArgs a, int* err) {
     constexpr int N = LANES<T>;
-    __shared__ Map<N> maps[2 * (WARPS + 8) * 32];
+    __shared__ Map<N> maps[2 * (WARPS + MOST_RANKS) * 32];
     __shared__ uint64_t pair[2];
     grid_dep_sync();
     const int warps = blockDim.x >> 5, w = threadIdx.x >> 5;
@@ -427,7 +427,6 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
 
 // The same backward.  Between its two walks a thread keeps, per step, a, 1 - a and the gradient g that reaches h from its own output in
 // registers, and (1 - a) (h_(t-1) - v) (coupled) or (1 - a) h_(t-1) in the words of the tiles of f and v that it has read.
-constexpr int BACK_WARPS = 4;
 template <typename T, int FORM, bool COUPLED>
 __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream_kernel(const __grid_constant__ Maps4 maps_in, const __grid_constant__ Maps4 maps_out, const RecArgs a,
                                                                                         int* err) {
@@ -675,10 +674,11 @@ template <typename T, bool VEC, int FORM> struct Backward {
     }
 };
 
+template <typename T> constexpr int REG_WARPS = sizeof(T) == 2 ? BACK_WARPS : WARPS;   // as the registers allow: three blocks of four warps, two of eight
 template <typename T, bool VEC, int FORM>
-__global__ void __launch_bounds__(32 * WARPS, 2) recurrence_backward_kernel(const RecArgs a, int* err) {
+__global__ void __launch_bounds__(32 * REG_WARPS<T>, sizeof(T) == 2 ? 3 : 2) recurrence_backward_kernel(const RecArgs a, int* err) {
     constexpr int N = LANES<T>;
-    __shared__ Map<N> maps[2 * (WARPS + 8) * 32];
+    __shared__ Map<N> maps[2 * (WARPS + MOST_RANKS) * 32];
     __shared__ uint64_t pair[2];
     extern __shared__ float kept[];                                  // per step and channel of a thread one or two values
     grid_dep_sync();
@@ -771,9 +771,10 @@ void shape(const RecArgs& a, int most, int per_sm, int* warps, int* ranks) {
     while (*warps < most && *warps < runs) *warps *= 2;
     double best = 0;
     *ranks = 0;
-    for (int s = 1; s <= 8; s *= 2) {
+    for (int s = 1; s <= MOST_RANKS; s *= 2) {
         if (s > 1 && (int64_t)s * *warps / 2 >= runs) break;
-        const int slots = SMS * (s > 4 ? 2 : per_sm);                // the parts of eight blocks take the place of a third one
+        // the parts of eight blocks take the place of a third block, those of sixteen of a second one
+        const int slots = SMS * (s > 8 ? 1 : s > 4 ? 2 : per_sm);
         const double turns = (double)((units * s + slots - 1) / slots), steps = (double)((runs + s * *warps - 1) / (s * *warps));
         const double cost = turns * steps * (s > 1 ? 1.1 : 1.0);
         if (!*ranks || cost < best) { best = cost; *ranks = s; }
@@ -790,22 +791,25 @@ template <typename T, bool VEC, int FORM> ftp_status forward_as(const RecArgs& a
     int warps, ranks;
     shape(a, WARPS, 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
+    auto kern = recurrence_forward_kernel<T, VEC, FORM>;
     int* err = ffn::status_word();
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
-    const cudaError_t e = launch_cluster(recurrence_forward_kernel<T, VEC, FORM>, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a, err);
+    FTP_REQUIRE(ranks <= 8 || large_clusters(reinterpret_cast<const void*>(kern)), FTP_ECUDA, "%s: no clusters of %d blocks", who, ranks);
+    const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, 0, ranks, st, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
 }
 template <typename T, bool VEC, int FORM> ftp_status backward_as(const RecArgs& a, cudaStream_t st, const char* who) {
     const int64_t units = a.seqs * a.tiles;
     int warps, ranks;
-    shape(a, WARPS, 2, &warps, &ranks);
+    shape(a, REG_WARPS<T>, sizeof(T) == 2 ? 3 : 2, &warps, &ranks);
     FTP_REQUIRE(units * ranks < (1ll << 31), FTP_ERANGE, "%s: tensor too large", who);
     auto kern = recurrence_backward_kernel<T, VEC, FORM>;
     const size_t smem = (size_t)(a.coupled ? 2 : 1) * RUN * 32 * warps * LANES<T> * 4;
     FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 2 * RUN * 32 * WARPS * LANES<T> * 4), FTP_ECUDA, "%s: no shared memory", who);
     int* err = ffn::status_word();
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
+    FTP_REQUIRE(ranks <= 8 || large_clusters(reinterpret_cast<const void*>(kern)), FTP_ECUDA, "%s: no clusters of %d blocks", who, ranks);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
@@ -823,7 +827,8 @@ template <typename T, int FORM> ftp_status forward_stream(const RecArgs& a, cuda
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     auto kern = a.coupled ? recurrence_forward_stream_kernel<T, FORM, true> : recurrence_forward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 6 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
-    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + 8)), FTP_ECUDA, "%s: no shared memory", who);
+    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + WARPS * 6 * TILE_BYTES + maps * (WARPS + MOST_RANKS)), FTP_ECUDA, "%s: no shared memory", who);
+    FTP_REQUIRE(ranks <= 8 || large_clusters(reinterpret_cast<const void*>(kern)), FTP_ECUDA, "%s: no clusters of %d blocks", who, ranks);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, y, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;
@@ -841,8 +846,9 @@ template <typename T, int FORM> ftp_status backward_stream(const RecArgs& a, cud
     FTP_REQUIRE(err, FTP_ECUDA, "%s: no status word on this device", who);
     auto kern = a.coupled ? recurrence_backward_stream_kernel<T, FORM, true> : recurrence_backward_stream_kernel<T, FORM, false>;
     const size_t maps = 2 * 32 * sizeof(Map<LANES<T>>), smem = 128 + warps * 8 * TILE_BYTES + maps * (warps + (ranks > 1 ? ranks : 0));
-    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + 8)), FTP_ECUDA,
+    FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 128 + BACK_WARPS * 8 * TILE_BYTES + maps * (BACK_WARPS + MOST_RANKS)), FTP_ECUDA,
                 "%s: no shared memory", who);
+    FTP_REQUIRE(ranks <= 8 || large_clusters(reinterpret_cast<const void*>(kern)), FTP_ECUDA, "%s: no clusters of %d blocks", who, ranks);
     const cudaError_t e = launch_cluster(kern, dim3((unsigned)(units * ranks)), 32 * warps, smem, ranks, st, in, out, a, err);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return FTP_OK;

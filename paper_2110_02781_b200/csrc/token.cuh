@@ -48,19 +48,23 @@ __device__ __forceinline__ unsigned on_rank(unsigned at, unsigned rank) {
     return r;
 }
 
-// lets a kernel have `bytes` of dynamic shared memory; asked of the driver once per kernel and device (1.5 us a call otherwise)
-inline bool more_shared(const void* kern, size_t bytes) {
+// An attribute of a kernel, told to the driver once per kernel, device and thread (1.5 us a call otherwise)
+template <cudaFuncAttribute WHAT> bool kernel_may(const void* kern, int value) {
     static thread_local const void* known[64] = {};
     static thread_local int devices[64] = {};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
     const size_t at = (reinterpret_cast<uintptr_t>(kern) >> 4) % 64;
     if (known[at] == kern && devices[at] == dev) return true;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    if (cudaFuncSetAttribute(kern, WHAT, value) != cudaSuccess) return false;
     known[at] = kern;
     devices[at] = dev;
     return true;
 }
+// `bytes` of dynamic shared memory, the same for every call with a kernel
+inline bool more_shared(const void* kern, size_t bytes) { return kernel_may<cudaFuncAttributeMaxDynamicSharedMemorySize>(kern, (int)bytes); }
+// clusters of more than eight blocks
+inline bool large_clusters(const void* kern) { return kernel_may<cudaFuncAttributeNonPortableClusterSizeAllowed>(kern, 1); }
 
 // ---- a row's columns on its threads ----
 // A thread holds groups of V columns (16 bytes).  VEC: V neighbours, one access (every row starts on 16 bytes and holds
