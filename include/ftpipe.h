@@ -469,9 +469,9 @@ ftp_status ftp_checkpoint_pack(const void* x, int64_t rows, int32_t cols, int64_
 ftp_status ftp_checkpoint_unpack(const void* image, int32_t part, int64_t rows, int32_t cols, int32_t precision, void* x, int64_t ld,
                                  void* stream);
 
-/* Waits for the stream, reads the device word in which a feed-forward kernel leaves a code when one of its bounded waits
- * ran out, and clears it: FTP_OK or FTP_ETIMEOUT.  After a timeout the results of every feed-forward call on this device
- * since the last check are invalid.  FTP_ESTATE while the stream is being captured. */
+/* Waits for the stream, reads the device word in which a kernel of the feed-forward operators or of the recurrence leaves a
+ * code when one of its bounded waits ran out, and clears it: FTP_OK or FTP_ETIMEOUT.  After a timeout the results of every
+ * such call on this device since the last check are invalid.  FTP_ESTATE while the stream is being captured. */
 ftp_status ftp_check_op_status(void* stream);
 
 /* ---- operators around the feed-forward products ---------------------------------------------------------------------
@@ -553,7 +553,7 @@ ftp_status ftp_recurrence_forward(const ftp_recurrence_desc* d, const void* f, c
 ftp_status ftp_recurrence_backward(const ftp_recurrence_desc* d, const void* f, const void* v, const void* o, const float* states,
                                    const int32_t* offsets, const void* dy, const float* dh1, void* df, void* dv, void* dout, float* dh0, void* stream);
 
-/* Log probabilities of given tokens under rows of logits, z = scale x over `vocab` columns:
+/* Log probabilities of given tokens under rows of logits, z = scale x (0 < scale <= 1e18) over `vocab` columns:
  *
  *   logp = z_target - log sum e^z,   entropy = - sum p log p,   top: the k likeliest tokens, likeliest first (of equal ones the lowest)
  *

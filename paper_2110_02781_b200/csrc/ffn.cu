@@ -997,7 +997,7 @@ ftp_status ftp_check_op_status(void* stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e == cudaSuccess && code) e = cudaMemsetAsync(word, 0, sizeof code, st);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "check_op_status: %s", cudaGetErrorString(e));
-    FTP_REQUIRE(code == 0, FTP_ETIMEOUT, "a bounded wait of a feed-forward kernel ran out (code %d)", code);
+    FTP_REQUIRE(code == 0, FTP_ETIMEOUT, "a bounded wait of an operator's kernel ran out (code %d)", code);
     return FTP_OK;
 }
 

@@ -464,7 +464,7 @@ ftp_status check(const void* logits, int64_t rows, int32_t vocab, int64_t* ld, i
     FTP_REQUIRE(precision == FTP_FP32 || precision == FTP_BF16, FTP_EINVAL, "%s: unknown precision %d", who, precision);
     FTP_REQUIRE(rows >= 0 && vocab >= 1, FTP_EINVAL, "%s: rows must not be negative, vocab must be positive", who);
     FTP_REQUIRE(rows < (1ll << 28) && vocab < (1 << 30), FTP_ERANGE, "%s: tensor too large", who);
-    FTP_REQUIRE(scale > 0.f && scale <= 3e38f, FTP_EINVAL, "%s: scale must be positive and finite", who);
+    FTP_REQUIRE(scale > 0.f && scale <= 1e18f, FTP_EINVAL, "%s: scale must be positive, 1e18 at most", who);
     if (ftp_status s = check_pitches({*ld}, vocab, who)) return s;
     if (!*ld) *ld = vocab;
     FTP_REQUIRE(rows == 0 || logits, FTP_EINVAL, "%s: null buffer", who);

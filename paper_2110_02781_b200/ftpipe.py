@@ -693,7 +693,7 @@ def ftp_gated_backward(x, w_gate, w_up, dh, dx=None, dw_gate=None, dw_up=None, a
 
 
 def ftp_check_op_status(stream=None):
-    """Waits for the stream; raises FtpError if a bounded wait of a feed-forward kernel ran out since the last check."""
+    """Waits for the stream; raises FtpError if a bounded wait of an operator's kernel ran out since the last check."""
     _check(lib.ftp_check_op_status(_stream(stream)))
 
 

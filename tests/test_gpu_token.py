@@ -1,7 +1,10 @@
 """Operators around the feed-forward products on the GPU: block joins, dropout, gated recurrence, log probabilities of tokens."""
 import math
+import subprocess
+import sys
 import threading
 import zlib
+from pathlib import Path
 
 import pytest
 import torch
@@ -297,7 +300,7 @@ def rec_inputs(g, rows, cols, dt, gap=0, off=0, coupled=True):
 
 
 REC = [(1, 1, 1, 0, 0), (3, 1, 64, 0, 0), (70, 1, 130, 0, 0), (2, 16, 33, 0, 0), (1, 17, 64, 0, 0), (2, 31, 65, 3, 1), (5, 100, 96, 2, 0), (1, 129, 200, 0, 0), (3, 257, 31, 1, 1), (1, 1000, 64, 0, 8),
-       (1, 2500, 40, 0, 0), (2, 777, 300, 0, 0), (40, 40, 72, 0, 0), (300, 20, 64, 0, 0)]
+       (1, 2500, 40, 0, 0), (2, 777, 300, 0, 0), (40, 40, 72, 0, 0), (300, 20, 64, 0, 0), (1, 3000, 33, 1, 1), (1, 2100, 66, 1, 0)]
 
 
 @pytest.mark.parametrize("seqs,steps,cols,gap,off", REC)
@@ -726,6 +729,42 @@ def test_calls_on_other_streams_and_threads_at_once():
     assert not errors
     for net, w in zip(nets, want):
         assert torch.equal(net.logp, w[0]) and torch.equal(net.b["dx"], w[1]) and torch.equal(net.gn["post2"], w[2])
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    code = """
+import torch, paper_2110_02781_b200 as F
+dev = dict(device="cuda")
+f, v, o, y = (torch.randn(2, 300, 64, **dev).bfloat16() for _ in range(4))
+states, dy = torch.empty(F.ftp_recurrence_states(600, 2), 64, **dev), torch.randn(2, 300, 64, **dev).bfloat16()
+df, dv, do = (torch.empty_like(f) for _ in range(3))
+x, s, z, st = torch.randn(600, 4096, **dev).bfloat16(), torch.empty(600, 4096, **dev).bfloat16(), torch.empty(600, 4096, **dev).bfloat16(), torch.empty(4, 600, **dev)
+w, du, dx, dw, dw2 = torch.ones(4096, **dev), torch.empty_like(x), torch.empty_like(x), torch.empty(4096, **dev), torch.empty(4096, **dev)
+t, lp, lse, top = torch.zeros(600, dtype=torch.int32, **dev), torch.empty(600, **dev), torch.empty(600, 2, **dev), torch.empty(600, 5, dtype=torch.int32, **dev)
+rng = torch.tensor([1, 2], dtype=torch.int64, **dev)
+def step():
+    F.ftp_recurrence_forward(f, v, y, o=o, states=states)
+    F.ftp_recurrence_backward(f, v, dy, states, df, dv, o=o, do=do)
+    F.ftp_join_forward(x, x, s, z, w_post=w, w_pre=w, dropout=0.1, rng=rng, stats=st)
+    F.ftp_join_backward(x, s, z, x, st, du=du, dx=dx, dw_post=dw, dw_pre=dw2, w_post=w, w_pre=w, dropout=0.1, rng=rng)
+    F.ftp_logprob_forward(s, t, lp, lse=lse, top=top)
+    F.ftp_logprob_backward(s, t, lse, lp, du)
+    F.ftp_dropout(x, dx, 0.3, rng)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+g.replay()
+torch.cuda.synchronize()
+out = [y, df, do, dw, dw2, lp, top, du, dx]
+a = [q.clone() for q in out]
+step()
+assert all(torch.equal(p, q) for p, q in zip(a, out))
+F.ftp_check_op_status()
+print("same")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=str(Path(__file__).parent.parent))
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
 
 
 def test_no_rows():

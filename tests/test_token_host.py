@@ -108,7 +108,7 @@ def test_logprob_calls_that_are_refused():
         return L.ftp_logprob_backward(x, rows, vocab, ld, prec, scale, t, lse, ent, dl, dh, dx, ldd, None)
     for call in (f, b):
         assert call(prec=2) == 1 and call(rows=-1) == 1 and call(vocab=0) == 1 and call(ld=63) == 1 and call(scale=0.0) == 1 and call(scale=-1.0) == 1
-        assert call(scale=float("inf")) == 1 and call(scale=float("nan")) == 1 and call(x=None) == 1 and call(x=P + 1) == 2 and call(t=P + 2) == 2 and call(t=None) == 1
+        assert call(scale=float("inf")) == 1 and call(scale=2e18) == 1 and call(scale=float("nan")) == 1 and call(x=None) == 1 and call(x=P + 1) == 2 and call(t=P + 2) == 2 and call(t=None) == 1
         assert call(rows=1 << 28) == 2 and call(vocab=1 << 30) == 2 and call(ld=1 << 36) == 2 and call(rows=0, x=None) == 0
     assert f(k=33, top=R) == 1 and f(k=-1) == 1 and f(k=5) == 1 and f(top=R) == 1 and f(tl=R) == 1 and f(vocab=4, k=5, top=R) == 1
     assert f(logp=P) == 1 and f(ent=Q) == 1 and f(k=2, top=Q) == 1 and f(lse=Q + 2) == 2
