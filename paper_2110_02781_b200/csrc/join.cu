@@ -861,7 +861,7 @@ struct JoinPlan { int threads, groups, run; int64_t blocks; };
 JoinPlan plan_backward(const ftp_join_desc* d) {
     JoinPlan p;
     const int v = d->precision == FTP_FP32 ? 4 : 8;
-    row_shape(d->cols, v, d->cols <= 512 * v ? 1 : 16 / v, &p.threads, &p.groups);
+    row_shape(d->cols, v, (d->cols <= 512 * 8 ? 8 : 16) / v, &p.threads, &p.groups);
     const int64_t each = (int64_t)SMS * std::min(16, BACKWARD_THREADS / p.threads);
     p.run = (int)std::min<int64_t>(64, std::max<int64_t>(4, (d->rows + each - 1) / each));
     p.blocks = (d->rows + p.run - 1) / p.run;

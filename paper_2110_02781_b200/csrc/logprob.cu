@@ -188,13 +188,25 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
     const bool head = me == 0 && x.first == 1, tail = me == stride - 1 && x.end < x.all && x.all - 1 >= x.first;
 #pragma unroll
     for (int u = 0; u < 4; ++u) held[u] = x.first + me + u * stride < x.end ? x.whole(x.first + me + u * stride) : nothing<T>();
-    s.add(held, a.scale2);
     int i = x.first + me + 4 * stride;
-    for (; i + 3 * stride < x.end; i += 4 * stride) {
-        uint4 q[4];
+    if constexpr (TOP) {
+        s.add(held, a.scale2);
+        for (; i + 3 * stride < x.end; i += 4 * stride) {
+            uint4 q[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
-        s.add(q, a.scale2);
+            for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
+            s.add(q, a.scale2);
+        }
+    } else {                                                         // the next four are on their way meanwhile
+        for (; i + 3 * stride < x.end; i += 4 * stride) {
+            uint4 q[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
+            s.add(held, a.scale2);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) held[u] = q[u];
+        }
+        s.add(held, a.scale2);
     }
     if (i < x.end) {
         uint4 q[4];
