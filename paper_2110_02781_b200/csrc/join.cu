@@ -253,6 +253,7 @@ template <typename T> struct Running {
 template <typename T, int G, bool VEC, bool LAYER, bool USUAL>
 __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const JoinArgs a) {
     constexpr int NS = LAYER ? 8 : 3, R = USUAL && G * V<T> <= 8 ? PAIR : 1;
+    constexpr bool AHEAD = USUAL && VEC;
     const bool pre = USUAL || a.pre != FTP_NORM_NONE, post = USUAL || a.post != FTP_NORM_NONE, w_pre = USUAL || a.w_pre, w_post = USUAL || a.w_post;
     const bool b_post = USUAL ? LAYER : a.b_post != nullptr, gated = a.gate, graded = a.dgate;
     const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL ? (LAYER ? 1 : -1) : a.at[SUM_B_PRE], at_w_post = USUAL ? (LAYER ? 2 : 1) : a.at[SUM_W_POST],
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
     const int64_t mine = blockIdx.x, first = mine * a.run, last = min(first + a.run, a.rows);
     int64_t group = a.gate_rows > 1 ? first / a.gate_rows : 0, next = a.gate_rows > 1 ? (group + 1) * a.gate_rows : 0;   // next: first row of the next group
     const F2 f = f2(drop.cut ? a.beta * a.drop.factor : a.beta), alpha = f2(a.alpha);
-    // USUAL: the next rows are on their way while these are worked on; a thread copies its own columns into shared memory and reads them itself
+    // AHEAD: the next rows are on their way while these are worked on; a thread copies its own columns into shared memory and reads them itself
     const unsigned staged = smem_at(dynamic) + a.nsums * (G * (V<T> / 4)) * blockDim.x * 16 + t * 16;
     const int64_t lds[4] = {a.lds, a.ldy, a.ldds, a.ldu};
     const void* const bases[4] = {a.s, a.dy, a.ds, a.u};
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
         for (int g = 0; g < G; ++g)
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[g].x), "=r"(r[g].y), "=r"(r[g].z), "=r"(r[g].w) : "r"(staged + ((q * 4 + n) * G + g) * blockDim.x * 16) : "memory");
     };
-    if (USUAL) ahead(first);
+    if constexpr (AHEAD) ahead(first);
     for (int64_t row = first; row < last;) {
         if (a.gate_sums && row == next) {                            // another group: its predecessor's sum is complete as far as this run goes
 #pragma unroll
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
 #pragma unroll
         for (int q = 0; q < R; ++q) on[q] = row + q < end;
         uint4 ru[R][G], rs[R][G], rdy[R][G], rds[R][G];
-        if (USUAL) asm volatile("cp.async.wait_all;" ::: "memory");
+        if constexpr (AHEAD) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             if (!on[q]) {                                            // zeros, which add nothing
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
                 for (int g = 0; g < G; ++g) ru[q][g] = rs[q][g] = rdy[q][g] = rds[q][g] = make_uint4(0u, 0u, 0u, 0u);
                 continue;
             }
-            if constexpr (USUAL) {
+            if constexpr (AHEAD) {
                 arrived(q, 0, rs[q]);
                 arrived(q, 1, rdy[q]);
                 arrived(q, 2, rds[q]);
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
             if (USUAL || a.ds) fetch_row<T, G, VEC>(a, in_row<T>(a.ds, a.ldds, row + q), t, rds[q]);
             if (USUAL || a.u) fetch_row<T, G, VEC>(a, in_row<T>(a.u, a.ldu, row + q), t, ru[q]);
         }
-        if (USUAL) ahead(min(row + R, end));
+        if constexpr (AHEAD) ahead(min(row + R, end));
         float r[R];
         F2 rp[R], lp[R], rn[R], ln[R];
 #pragma unroll
@@ -889,8 +890,9 @@ ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, bool usual, cud
     size_t staged = 0;
     if constexpr (G * V<T> <= 16)
         if (usual) {
-            kern = layer ? join_backward_kernel<T, G, true, true, true> : join_backward_kernel<T, G, true, false, true>;
-            staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
+            kern = layer ? (vec ? join_backward_kernel<T, G, true, true, true> : join_backward_kernel<T, G, false, true, true>)
+                         : (vec ? join_backward_kernel<T, G, true, false, true> : join_backward_kernel<T, G, false, false, true>);
+            if (vec) staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
         }
     if (!kern)
         kern = layer ? (vec ? join_backward_kernel<T, G, true, true, false> : join_backward_kernel<T, G, false, true, false>)
@@ -1019,11 +1021,10 @@ ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* 
         if (out[i]) j.out[a.nsums] = out[i];
         if (a.at[i] >= 0) ++a.nsums;
     }
-    const auto whole_groups = [&](const JoinArgs& q) { return d->precision == FTP_FP32 ? wide_rows<float>(q) : wide_rows<bf16>(q); };
     // what the kernel for the usual call takes as known
     const bool layer = d->post == FTP_NORM_LAYER || d->pre == FTP_NORM_LAYER;
     const bool usual = d->post != FTP_NORM_NONE && d->pre != FTP_NORM_NONE && w_post && w_pre && dw_post && dw_pre && ds && dx && du && layer == (b_post != nullptr) &&
-                       layer == (db_post != nullptr) && layer == (db_pre != nullptr) && whole_groups(a);
+                       layer == (db_post != nullptr) && layer == (db_pre != nullptr);
     const JoinSpace sp = space_of(d, p, SUMS), now = space_of(d, p, a.nsums);
     char* base = static_cast<char*>(ws);
     a.sums = reinterpret_cast<float*>(base);
