@@ -248,16 +248,20 @@ template <typename T> struct Running {
 //
 // The sums over a row that du needs are sums of K w_post (e + c1 + c2 x^) and of that times u^: linear in c1 and c2, so all sums of a row
 // go through one exchange, and its values are decoded once.
-// USUAL: both norms with weights, biases beside them where one is a layer norm, all of their gradients asked for, a ds, dx and du: known
-// when compiled, because a question per group of columns costs three instructions.
-template <typename T, int G, bool VEC, bool LAYER, bool USUAL>
+// KIND: what is known when compiled, because a question per group of columns costs three instructions.  BOTH: both norms with weights; PRE_ONLY: the second
+// norm alone; either with biases beside the weights where a norm is a layer norm, all of their gradients asked for, a u, ds, dx and du.
+enum { ANY = 0, BOTH = 1, PRE_ONLY = 2 };
+template <typename T, int G, bool VEC, bool LAYER, int KIND>
 __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const JoinArgs a) {
+    constexpr bool USUAL = KIND != ANY, AHEAD = USUAL && VEC;
     constexpr int NS = LAYER ? 8 : 3, R = USUAL && G * V<T> <= 8 ? PAIR : 1;
-    constexpr bool AHEAD = USUAL && VEC;
-    const bool pre = USUAL || a.pre != FTP_NORM_NONE, post = USUAL || a.post != FTP_NORM_NONE, w_pre = USUAL || a.w_pre, w_post = USUAL || a.w_post;
-    const bool b_post = USUAL ? LAYER : a.b_post != nullptr, gated = a.gate, graded = a.dgate;
-    const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL ? (LAYER ? 1 : -1) : a.at[SUM_B_PRE], at_w_post = USUAL ? (LAYER ? 2 : 1) : a.at[SUM_W_POST],
-              at_b_post = USUAL ? (LAYER ? 3 : -1) : a.at[SUM_B_POST], at_gate = USUAL ? (LAYER ? 4 : 2) : a.at[SUM_GATE];
+    const bool pre = USUAL || a.pre != FTP_NORM_NONE, post = USUAL ? KIND == BOTH : a.post != FTP_NORM_NONE, w_pre = USUAL || a.w_pre,
+               w_post = USUAL ? KIND == BOTH : a.w_post != nullptr, b_post = USUAL ? LAYER && KIND == BOTH : a.b_post != nullptr;
+    const bool gated = a.gate, graded = a.dgate;
+    // places of the running sums
+    const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL ? (LAYER ? 1 : -1) : a.at[SUM_B_PRE],
+              at_w_post = USUAL ? (KIND == BOTH ? 1 + LAYER : -1) : a.at[SUM_W_POST], at_b_post = USUAL ? (LAYER && KIND == BOTH ? 3 : -1) : a.at[SUM_B_POST],
+              at_gate = USUAL ? (KIND == BOTH ? 2 : 1) * (1 + LAYER) : a.at[SUM_GATE];
     extern __shared__ float4 dynamic[];
     __shared__ float red[2 * 16 * NS * R];
     __shared__ Rounds keys;
@@ -882,21 +886,22 @@ JoinSpace space_of(const ftp_join_desc* d, const JoinPlan& p, int nsums) {
     return s;
 }
 
+template <typename T, int G, int KIND> void (*backward_kernel(bool vec, bool layer))(JoinArgs) {
+    return layer ? (vec ? join_backward_kernel<T, G, true, true, KIND> : join_backward_kernel<T, G, false, true, KIND>)
+                 : (vec ? join_backward_kernel<T, G, true, false, KIND> : join_backward_kernel<T, G, false, false, KIND>);
+}
 template <typename T, int G>
-ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, bool usual, cudaStream_t st, const char* who) {
+ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, int kind, cudaStream_t st, const char* who) {
     size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * p.threads * 4;
     const bool layer = a.post == FTP_NORM_LAYER || a.pre == FTP_NORM_LAYER;
     void (*kern)(JoinArgs) = nullptr;
     size_t staged = 0;
-    if constexpr (G * V<T> <= 16)
-        if (usual) {
-            kern = layer ? (vec ? join_backward_kernel<T, G, true, true, true> : join_backward_kernel<T, G, false, true, true>)
-                         : (vec ? join_backward_kernel<T, G, true, false, true> : join_backward_kernel<T, G, false, false, true>);
-            if (vec) staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
-        }
-    if (!kern)
-        kern = layer ? (vec ? join_backward_kernel<T, G, true, true, false> : join_backward_kernel<T, G, false, true, false>)
-                     : (vec ? join_backward_kernel<T, G, true, false, false> : join_backward_kernel<T, G, false, false, false>);
+    if constexpr (G * V<T> <= 16) {
+        if (kind == BOTH) kern = backward_kernel<T, G, BOTH>(vec, layer);
+        else if (kind == PRE_ONLY) kern = backward_kernel<T, G, PRE_ONLY>(vec, layer);
+        if (kern && vec) staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
+    }
+    if (!kern) kern = backward_kernel<T, G, ANY>(vec, layer);
     smem += staged;
     // 48 KB with what the kernel holds beside it
     if (smem > 40 * 1024) FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 220 * 1024), FTP_ECUDA, "%s: no shared memory", who);
@@ -909,7 +914,7 @@ template <typename T> bool wide_rows(const JoinArgs& a) {
            (a.gate_rows != 1 || wide<T>(a.dgate, a.lddg, a.rows)) && wide_vectors({a.w_post, a.b_post, a.w_pre, a.out[0], a.out[1], a.out[2], a.out[3], a.out[4]});
 }
 template <typename T>
-ftp_status run_backward(JoinArgs& a, const JoinPlan& p, bool usual, cudaStream_t st, const char* who) {
+ftp_status run_backward(JoinArgs& a, const JoinPlan& p, int kind, cudaStream_t st, const char* who) {
     a.threads = p.threads;
     a.groups = p.groups;
     a.full = fills<T>(a, p.groups);
@@ -924,9 +929,9 @@ ftp_status run_backward(JoinArgs& a, const JoinPlan& p, bool usual, cudaStream_t
         return FTP_OK;
     }
     switch (p.groups) {
-        case 1: return backward_of<T, 1>(a, p, vec, usual, st, who);
-        case 2: return backward_of<T, 2>(a, p, vec, usual, st, who);
-        case 4: if constexpr (sizeof(T) == 4) return backward_of<T, 4>(a, p, vec, usual, st, who);
+        case 1: return backward_of<T, 1>(a, p, vec, kind, st, who);
+        case 2: return backward_of<T, 2>(a, p, vec, kind, st, who);
+        case 4: if constexpr (sizeof(T) == 4) return backward_of<T, 4>(a, p, vec, kind, st, who);
     }
     return FTP_OK;
 }
@@ -1021,16 +1026,19 @@ ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* 
         if (out[i]) j.out[a.nsums] = out[i];
         if (a.at[i] >= 0) ++a.nsums;
     }
-    // what the kernel for the usual call takes as known
+    // what the kernels for the usual calls take as known
     const bool layer = d->post == FTP_NORM_LAYER || d->pre == FTP_NORM_LAYER;
-    const bool usual = d->post != FTP_NORM_NONE && d->pre != FTP_NORM_NONE && w_post && w_pre && dw_post && dw_pre && ds && dx && du && layer == (b_post != nullptr) &&
-                       layer == (db_post != nullptr) && layer == (db_pre != nullptr);
+    int kind = ANY;
+    if (d->pre != FTP_NORM_NONE && w_pre && dw_pre && layer == (db_pre != nullptr) && u && ds && dx && du) {
+        if (d->post == FTP_NORM_NONE) kind = PRE_ONLY;
+        else if (w_post && dw_post && layer == (b_post != nullptr) && layer == (db_post != nullptr)) kind = BOTH;
+    }
     const JoinSpace sp = space_of(d, p, SUMS), now = space_of(d, p, a.nsums);
     char* base = static_cast<char*>(ws);
     a.sums = reinterpret_cast<float*>(base);
     if (shared_gate) a.gate_sums = reinterpret_cast<float*>(base + sp.sums);
     if (now.spill) a.spill = reinterpret_cast<float*>(base + sp.sums + sp.gate);
-    if (ftp_status r = d->precision == FTP_FP32 ? run_backward<float>(a, p, usual, st, who) : run_backward<bf16>(a, p, usual, st, who)) return r;
+    if (ftp_status r = d->precision == FTP_FP32 ? run_backward<float>(a, p, kind, st, who) : run_backward<bf16>(a, p, kind, st, who)) return r;
     const int n = a.nsums - shared_gate;
     if (n && p.blocks > 1) {
         j.part = a.sums; j.n = n; j.cols = d->cols; j.blocks = p.blocks;
