@@ -1,12 +1,16 @@
 // A block's result joins the residual stream: s = alpha x + beta gate drop(post(u)), and the next block's input y = pre(s), in one
 // pass over the tokens each way; and dropout by itself.
 //
-// Bound by memory: the forward pass reads u, x and writes s, y; the backward pass reads u, s, dy, ds and writes du, dx.  A row lies
-// in the registers of 32 to 512 threads, which take 16 bytes of columns one to eight times; a sum over a row is five shuffles, one
-// exchange between its warps and up to four shuffles more.  Threads with many columns make these cheap and leave more rows in flight;
-// a single row is spread over more threads.  The column sums of the backward pass (gradients of the norms' weights and of a gate that many
-// rows share) grow in shared memory, each thread its own columns, over at most 64 rows, and a second kernel adds the blocks' sums in
-// double, in a fixed order.
+// Bound by memory in principle: the forward pass reads u, x and writes s, y; the backward pass reads u, s, dy, ds and writes du, dx.  A row lies in
+// the registers of a block of 32 to 512 threads, which take 16 bytes of columns one to eight times; a sum over a row is five shuffles, one exchange
+// between its warps and up to four shuffles more.  Forward: up to 32 columns a thread make these cheap and leave more rows in flight, the next row's
+// loads start as soon as a row's values are taken; a single row is spread over more threads.  The column sums of the backward pass (gradients of
+// the norms' weights and of a gate that many rows share) grow in shared memory, each thread its own columns, over at most 64 rows, and a second
+// kernel adds the blocks' sums in double, in a fixed order.
+// What sets the time is instructions (packed float arithmetic halves them; a dropout mask is 20 a column of eight): 8192 x 4096 bf16 forward with
+// dropout and a gate 65 us (4.1 TB/s), without dropout 55, 8192 x 8192 without both 93 (5.7 TB/s); backward 130 us with dropout, a gate and three
+// column sums (3.1 TB/s, 73 instructions an element, 2.2 a cycle), 120 without dropout, 84 for the second norm alone (4.8 TB/s).
+// Rows off 16 bytes: a thread's columns lie a block's width apart, single elements (8000 x 4001 bf16: 157 us forward, 233 backward).
 #include <algorithm>
 #include "token.cuh"
 
@@ -37,7 +41,7 @@ template <typename T> __device__ __forceinline__ T* out_row(void* base, int64_t 
 // a row of the gate: a float vector, or a row of the tensors' type for every gate_rows rows
 template <typename T, bool VEC> __device__ __forceinline__ void gate_of(const JoinArgs& a, int64_t row, int t, int g, F2 (&v)[P<T>]) {
     if (a.gate_rows == 0) fetch_vector<T, VEC>(static_cast<const float*>(a.gate), t, a.threads, g, a.cols, v);
-    else decode<T>(fetch<T, VEC>(static_cast<const T*>(a.gate) + row / a.gate_rows * a.ldg, t, a.threads, g, a.cols), v);
+    else decode<T>(fetch<T, VEC>(static_cast<const T*>(a.gate) + (int64_t)((unsigned)row / (unsigned)a.gate_rows) * a.ldg, t, a.threads, g, a.cols), v);
 }
 
 // What lies behind the last column becomes 0.
@@ -149,7 +153,8 @@ constexpr int forward_threads(int columns) { return columns <= 8 ? 1024 : column
 constexpr int BACKWARD_THREADS = 512;
 
 // Rows that the backward pass takes at a time where the usual gradients are asked for: the vectors that all rows share, and the running sums, are then
-// read half as often (with a row a time the first cache's bandwidth is three quarters used: 138 us instead of 127).
+// read half as often (8192 x 4096 bf16: 130 us; a row at a time 138, the first cache's bandwidth three quarters used).  With the eight sums of a layer norm a
+// row at a time is faster (8192 x 2048 float 171 instead of 206 us).
 constexpr int PAIR = 2;
 
 template <typename T, int G, bool VEC>
@@ -249,19 +254,19 @@ template <typename T> struct Running {
 // The sums over a row that du needs are sums of K w_post (e + c1 + c2 x^) and of that times u^: linear in c1 and c2, so all sums of a row
 // go through one exchange, and its values are decoded once.
 // KIND: what is known when compiled, because a question per group of columns costs three instructions.  BOTH: both norms with weights; PRE_ONLY: the second
-// norm alone; either with biases beside the weights where a norm is a layer norm, all of their gradients asked for, a u, ds, dx and du.
+// norm alone; with weights and their gradients, biases only where a norm is a layer norm, a u, ds, dx and du.
 enum { ANY = 0, BOTH = 1, PRE_ONLY = 2 };
 template <typename T, int G, bool VEC, bool LAYER, int KIND>
 __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const JoinArgs a) {
     constexpr bool USUAL = KIND != ANY, AHEAD = USUAL && VEC;
-    constexpr int NS = LAYER ? 8 : 3, R = USUAL && G * V<T> <= 8 ? PAIR : 1;
+    constexpr int NS = LAYER ? 8 : 3, R = USUAL && !LAYER && G * V<T> <= 8 ? PAIR : 1;
     const bool pre = USUAL || a.pre != FTP_NORM_NONE, post = USUAL ? KIND == BOTH : a.post != FTP_NORM_NONE, w_pre = USUAL || a.w_pre,
-               w_post = USUAL ? KIND == BOTH : a.w_post != nullptr, b_post = USUAL ? LAYER && KIND == BOTH : a.b_post != nullptr;
+               w_post = USUAL ? KIND == BOTH : a.w_post != nullptr, b_post = USUAL && (!LAYER || KIND != BOTH) ? false : a.b_post != nullptr;
     const bool gated = a.gate, graded = a.dgate;
     // places of the running sums
-    const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL ? (LAYER ? 1 : -1) : a.at[SUM_B_PRE],
-              at_w_post = USUAL ? (KIND == BOTH ? 1 + LAYER : -1) : a.at[SUM_W_POST], at_b_post = USUAL ? (LAYER && KIND == BOTH ? 3 : -1) : a.at[SUM_B_POST],
-              at_gate = USUAL ? (KIND == BOTH ? 2 : 1) * (1 + LAYER) : a.at[SUM_GATE];
+    const int at_w_pre = USUAL ? 0 : a.at[SUM_W_PRE], at_b_pre = USUAL && !LAYER ? -1 : a.at[SUM_B_PRE],
+              at_w_post = !USUAL || LAYER ? a.at[SUM_W_POST] : KIND == BOTH ? 1 : -1, at_b_post = USUAL && !LAYER ? -1 : a.at[SUM_B_POST],
+              at_gate = !USUAL || LAYER ? a.at[SUM_GATE] : KIND == BOTH ? 2 : 1;
     extern __shared__ float4 dynamic[];
     __shared__ float red[2 * 16 * NS * R];
     __shared__ Rounds keys;
@@ -765,6 +770,8 @@ __global__ void __launch_bounds__(128) join_gate_kernel(const float* part, int64
     }
 }
 
+// A warp per 32 V columns of a row, four such pieces in flight.  16384 x 4096 bf16: 60 us, 4.5 TB/s; bound by the generator's integer arithmetic (22
+// instructions an element, the integer pipe over half used); one piece in flight 69 us, two 60, eight 70.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) dropout_kernel(const T* x, T* y, int64_t rows, int cols, int64_t ldx, int64_t ldy, const Drop d) {
     __shared__ Rounds keys;
@@ -899,7 +906,7 @@ ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, int kind, cudaS
     if constexpr (G * V<T> <= 16) {
         if (kind == BOTH) kern = backward_kernel<T, G, BOTH>(vec, layer);
         else if (kind == PRE_ONLY) kern = backward_kernel<T, G, PRE_ONLY>(vec, layer);
-        if (kern && vec) staged = (size_t)(G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
+        if (kern && vec) staged = (size_t)(!layer && G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
     }
     if (!kern) kern = backward_kernel<T, G, ANY>(vec, layer);
     smem += staged;
@@ -1029,9 +1036,9 @@ ftp_status ftp_join_backward(const ftp_join_desc* d, const void* u, const void* 
     // what the kernels for the usual calls take as known
     const bool layer = d->post == FTP_NORM_LAYER || d->pre == FTP_NORM_LAYER;
     int kind = ANY;
-    if (d->pre != FTP_NORM_NONE && w_pre && dw_pre && layer == (db_pre != nullptr) && u && ds && dx && du) {
+    if (d->pre != FTP_NORM_NONE && w_pre && dw_pre && u && ds && dx && du && (layer || (!b_post && !db_post && !db_pre))) {
         if (d->post == FTP_NORM_NONE) kind = PRE_ONLY;
-        else if (w_post && dw_post && layer == (b_post != nullptr) && layer == (db_post != nullptr)) kind = BOTH;
+        else if (w_post && dw_post) kind = BOTH;
     }
     const JoinSpace sp = space_of(d, p, SUMS), now = space_of(d, p, a.nsums);
     char* base = static_cast<char*>(ws);

@@ -1,13 +1,14 @@
 // Log probabilities of given tokens under rows of logits, the rows' entropies and their likeliest tokens; and the logits' gradient.
 //
 // Bound by memory: the forward pass reads every logit once, the backward pass reads them once more and writes the gradient.
-// Forward: a block per row (a cluster of up to eight where there are few rows); a thread keeps the largest of its logits, m, and
-// with it sum e^(z - m) and sum e^(z - m) (z - m), from which the entropy is log sum - (second / first).  The sums are rescaled
-// only where a group of 16 bytes holds a new largest logit.  Rows that do not start on 16 bytes are read from the boundary before
-// them, the two partial groups element by element.
-// The k likeliest tokens come from the same pass: every warp gives its 32 / warps largest thread maxima, the k-th largest of
-// these 32 is a bound that k logits of the row reach, and only the groups of threads whose maximum reaches it are read again (about k
-// of up to 512 threads).  What reaches the bound is ranked by (value, lowest token) in shared memory.
+// Forward: a block per row (a cluster of up to eight where there are few rows); a thread keeps the largest of its logits, m, and with it sum e^(z - m) and
+// sum e^(z - m) (z - m), from which the entropy is log sum - (second / first).  The sums are rescaled only where four groups of 16 bytes hold a new
+// largest logit.  Rows that do not start on 16 bytes are read from the boundary before them, the two partial groups element by element.
+// The k likeliest tokens come from the same pass: every warp gives its 32 / warps largest thread maxima, the k-th largest of these 32 is a bound that k
+// logits of the row reach, and only the groups of threads whose maximum reaches it are looked at again (about k of up to 512 threads; in registers where a
+// thread has no more than four).  What reaches the bound is ranked by (value, lowest token).
+// 4096 x 50021 bf16 with entropies: 73-83 us (5.0-5.6 TB/s; the exponentials use two thirds of their pipe); 16 x 128000 with 20 top tokens: 9.1 us, a
+// chain of eight exchanges between threads, warps and blocks; backward, 8192 x 32000: 181-191 us (5.5-5.8 TB/s).
 #include <algorithm>
 #include "token.cuh"
 

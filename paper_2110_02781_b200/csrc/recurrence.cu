@@ -1,12 +1,15 @@
 // Gated linear recurrence over the steps of a sequence: h_t = a_t h_(t-1) + b_t with a = 1 / (1 + e^-f), b = (1 - a) v or v, and
 // y = act(o) h; every channel for itself.
 //
-// Bound by memory: one pass over f, v, o and y (backward: f, v, o, dy in, df, dv, do out).  A step is the map h -> a h + b, and the
-// maps of a run of steps compose to one, h -> A h + B.  A thread holds a run of 16 steps of two neighbouring channels (bf16; one
-// float channel) in registers, all its loads in flight at once; a warp 32 threads of one run; a block up to eight runs after one
-// another, and a cluster of up to sixteen blocks the runs after those, so that a long sequence of few channels still fills the GPU.
-// The runs' maps go through shared memory, the blocks' through the cluster's, and are applied in the order of time, whatever
-// finishes first: one read of the data and the same bits every time.  The state and the maps are float.
+// Bound by memory: one pass over f, v, o and y (backward: f, v, o, dy in, df, dv, do out).  A step is the map h -> a h + b, and the maps of a run of
+// steps compose to one, h -> A h + B.  A thread holds a run of 16 steps of two neighbouring channels (bf16; one float channel) in registers; a warp 32
+// threads of one run; a block up to eight runs after one another (four backward), and a cluster of up to sixteen blocks the runs after those, so that
+// a long sequence of few channels still fills the GPU.  The runs' maps go through shared memory, the blocks' through the cluster's, and are applied in
+// the order of time, whatever finishes first: one read of the data and the same bits every time.  The state and the maps are float.
+// Rows on 16 bytes come and go as tiles through the copy engine (below): 65536 x 2048 bf16 forward with a gate 279 us (4.0 TB/s; four
+// exponentials and reciprocals an element use half of their pipe, 256 blocks leave a seventh of the GPU idle), 24 ragged sequences of up to 4096 x 1536
+// backward 262 us (4.3 TB/s; latency at 12 warps a multiprocessor, which the registers allow).  Other rows through registers: 32000 x 2001 bf16 218 us
+// forward, 625 backward.
 // The backward pass starts every run from the state that the forward pass kept in front of it, walks it forward once and then, with
 // q_t = a_t (g_t + q_(t+1)) (g: dy act(o), q_(t+1): what reaches h_t from behind), backward in the same way.
 #include <algorithm>

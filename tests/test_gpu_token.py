@@ -89,7 +89,8 @@ JOIN = [(1, 1, 0, 0), (1, 64, 0, 0), (3, 7, 0, 0), (5, 40, 3, 1), (67, 96, 8, 0)
         (2, 12001, 1, 1), (70, 9000, 0, 0)]
 HOW = [dict(post="rms", pre="rms", gate="vector", p=0.1), dict(post="layer", pre="layer", gate=7, p=0.25, bias=1), dict(post="none", pre="layer", gate=None, p=0.0, bias=1),
        dict(post="rms", pre="none", gate=1, p=0.5), dict(post="layer", pre="rms", gate=50, p=0.0, bare=1), dict(post="none", pre="none", gate="vector", p=0.3),
-       dict(post="layer", pre="layer", gate=None, p=0.0), dict(post="layer", pre="layer", gate="vector", p=0.1, bias=1)]
+       dict(post="layer", pre="layer", gate=None, p=0.0), dict(post="layer", pre="layer", gate="vector", p=0.1, bias=1),
+       dict(post="none", pre="rms", gate=30, p=0.1), dict(post="none", pre="layer", gate="vector", p=0.2, bias=1), dict(post="layer", pre="rms", gate=9, p=0.1, bias=1)]
 
 
 def join_case(rows, cols, gap, off, dt, how):
