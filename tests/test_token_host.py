@@ -19,7 +19,7 @@ def fwd(d, u=P, x=P + 512, w_post=None, b_post=None, gate=None, w_pre=None, b_pr
     return L.ftp_join_forward(ref(d), u, x, w_post, b_post, gate, w_pre, b_pre, rng, s, y, stats, None)
 
 
-def bwd(d, u=P, s=P + 512, w_post=None, b_post=None, gate=None, w_pre=None, stats=P + 1024, rng=None, dy=P + 2048, ds=P + 3072, du=Q, dx=R, dw_post=None, db_post=None,
+def bwd(d, u=P, s=P + 512, w_post=None, b_post=None, gate=None, w_pre=None, stats=P + 1024, rng=None, dy=P + 2048, ds=P + 3584, du=Q, dx=R, dw_post=None, db_post=None,
         dw_pre=None, db_pre=None, dgate=None, ws=None, nws=0):
     return L.ftp_join_backward(ref(d), u, s, w_post, b_post, gate, w_pre, stats, rng, dy, ds, du, dx, dw_post, db_post, dw_pre, db_pre, dgate, ws, nws, None)
 
@@ -57,8 +57,8 @@ def test_join_calls_that_are_refused():
     assert bwd(ok, stats=None, **big) == 1 and bwd(join(pre=0), **big) == 1           # dy of a norm that is not there
     assert bwd(join(post=0), dw_post=P + 256, **big) == 1 and bwd(join(pre=0), dy=None, dw_pre=P + 256, **big) == 1
     assert bwd(ok, dgate=P + 256, **big) == 1 and bwd(join(gate_rows=2), **big) == 1
-    assert bwd(ok, du=P, **big) == 1 and bwd(ok, dx=P + 2048, **big) == 1 and bwd(ok, du=R, **big) == 1 and bwd(ok, du=P + 3072, **big) == 1
-    assert bwd(join(lddx=80), dx=P + 3072, **big) == 1                                # dx in place of ds with another pitch
+    assert bwd(ok, du=P, **big) == 1 and bwd(ok, dx=P + 2048, **big) == 1 and bwd(ok, du=R, **big) == 1 and bwd(ok, du=P + 3584, **big) == 1
+    assert bwd(join(lddx=80), dx=P + 3584, **big) == 1                                # dx in place of ds with another pitch
     assert bwd(ok, dw_post=Q + 2, **big) == 2 and bwd(ok, ds=P + 3, **big) == 2
     assert bwd(join(rows=5000)) == 3 and bwd(join(rows=5000), ws=P, nws=64) == 3 and bwd(join(rows=5000), ws=P + 16, nws=1 << 30) == 2
     assert bwd(join(rows=0), u=None, s=None, stats=None, dy=None, ds=None, du=None, dx=None) == 0
