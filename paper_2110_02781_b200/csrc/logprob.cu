@@ -1,14 +1,15 @@
 // Log probabilities of given tokens under rows of logits, the rows' entropies and their likeliest tokens; and the logits' gradient.
 //
 // Bound by memory: the forward pass reads every logit once, the backward pass reads them once more and writes the gradient.
-// Forward: a block per row (a cluster of up to eight where there are few rows); a thread keeps the largest of its logits, m, and with it sum e^(z - m) and
-// sum e^(z - m) (z - m), from which the entropy is log sum - (second / first).  The sums are rescaled only where four groups of 16 bytes hold a new
-// largest logit.  Rows that do not start on 16 bytes are read from the boundary before them, the two partial groups element by element.
+// Forward: a block per row, a cluster of up to eight where there are few rows, a warp where they are many and short; a thread keeps the largest of its
+// logits, m, and with it sum e^(z - m) and sum e^(z - m) (z - m), from which the entropy is log sum - (second / first).  The sums are rescaled only where
+// four groups of 16 bytes hold a new largest logit.  Rows that do not start on 16 bytes are read from the boundary before them, the two partial groups
+// element by element.
 // The k likeliest tokens come from the same pass: every warp gives its 32 / warps largest thread maxima, the k-th largest of these 32 is a bound that k
 // logits of the row reach, and only the groups of threads whose maximum reaches it are looked at again (about k of up to 512 threads; in registers where a
 // thread has no more than four).  What reaches the bound is ranked by (value, lowest token).
 // 4096 x 50021 bf16 with entropies: 73-83 us (5.0-5.6 TB/s; the exponentials use two thirds of their pipe); 16 x 128000 with 20 top tokens: 9.1 us, a
-// chain of eight exchanges between threads, warps and blocks; backward, 8192 x 32000: 181-191 us (5.5-5.8 TB/s).
+// chain of eight exchanges between threads, warps and blocks; 16000 x 12000 with a warp a row 64 us (6.0 TB/s); backward, 8192 x 32000: 181-191 us (5.5-5.8 TB/s).
 #include <algorithm>
 #include "token.cuh"
 
@@ -16,7 +17,7 @@ namespace ftp {
 namespace token {
 namespace {
 
-constexpr int MOST_THREADS = 512, MOST_TOP = 32, CAND = 2048;
+constexpr int MOST_THREADS = 512, MOST_TOP = 32, CAND = 2048, ROWS = 4, ROWS_CAND = 512;
 constexpr float LOW = -1e4f;                                         // stands for the logarithm of 0 where it meets a factor 0
 
 struct LogpArgs {
@@ -164,15 +165,24 @@ __device__ __forceinline__ Key merge(Key a, Key b) {
     return a;
 }
 
-template <typename T, bool ENTROPY, bool TOP>
+// What the threads of a row share
+template <bool TOP, bool WARP> struct Shared {
+    float red[3][16], part[3], total[3];
+    unsigned bound[32];
+    Key best[MOST_TOP], joined[WARP ? 1 : 4][MOST_TOP];
+    int hit[TOP ? (WARP ? 32 : MOST_THREADS) : 1], hits, found;
+};
+
+// WARP: a row to a warp instead of a block or a cluster
+template <typename T, bool ENTROPY, bool TOP, bool WARP>
 __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsigned ranks, unsigned rank) {
-    extern __shared__ Key cand[];                                    // TOP: candidates
-    __shared__ float red[3][16];
-    __shared__ float part[3], total[3];
-    __shared__ unsigned bound[32];
-    __shared__ Key best[MOST_TOP], joined[4][MOST_TOP];
-    __shared__ int hit[TOP ? MOST_THREADS : 1], hits, found;
-    const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, w = tid >> 5, warps = threads >> 5;
+    extern __shared__ Key candidates[];
+    __shared__ Shared<TOP, WARP> shared[WARP ? ROWS : 1];
+    const int threads = WARP ? 32 : blockDim.x, tid = WARP ? threadIdx.x & 31 : threadIdx.x, lane = tid & 31, w = tid >> 5, warps = threads >> 5;
+    const int mine_at = WARP ? threadIdx.x >> 5 : 0;
+    Shared<TOP, WARP>& sh = shared[mine_at];
+    Key* const cand = candidates + mine_at * a.room;
+    const auto sync = [] { if constexpr (WARP) __syncwarp(); else __syncthreads(); };
     const Row<T> x(a.x, row, a.ld, a.vocab);
     const int me = (int)rank * threads + tid, stride = (int)ranks * threads;
     Sums<T, ENTROPY> s;
@@ -225,12 +235,14 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
     float m = s.m;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) red[0][w] = m;
-    if (TOP && tid == 0) hits = found = 0;
-    if (TOP && tid < MOST_TOP) best[tid] = 0;
-    __syncthreads();
-    m = red[0][lane & (warps - 1)];
-    for (int d = warps >> 1; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    if (!WARP && lane == 0) sh.red[0][w] = m;
+    if (TOP && tid == 0) sh.hits = sh.found = 0;
+    if (TOP && tid < MOST_TOP) sh.best[tid] = 0;
+    if constexpr (!WARP) {
+        __syncthreads();
+        m = sh.red[0][lane & (warps - 1)];
+        for (int d = warps >> 1; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    }
     if (m > s.m) s.rescale(m, a.scale2);
     float s0 = sum2(s.s0), s1 = sum2(s.s1);
 #pragma unroll
@@ -238,27 +250,27 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
         s0 += __shfl_xor_sync(0xffffffffu, s0, d);
         s1 += __shfl_xor_sync(0xffffffffu, s1, d);
     }
-    if (lane == 0) { red[1][w] = s0; red[2][w] = s1; }
+    if (!WARP && lane == 0) { sh.red[1][w] = s0; sh.red[2][w] = s1; }
     if constexpr (TOP) {
         // the warp's largest thread maxima
         unsigned o = order_of(mine);
         const int each = 32 / warps;
-        if (warps == 1) bound[lane] = o;
+        if (warps == 1) sh.bound[lane] = o;
         else for (int k = 0; k < each; ++k) {
             const unsigned top = __reduce_max_sync(0xffffffffu, o);
             const unsigned who = __ballot_sync(0xffffffffu, o == top);
             if (lane == __ffs(who) - 1) o = 0;
-            if (lane == 0) bound[w * each + k] = top;
+            if (lane == 0) sh.bound[w * each + k] = top;
         }
     }
-    __syncthreads();
-    if (w == 0) {
-        s0 = red[1][lane & (warps - 1)]; s1 = red[2][lane & (warps - 1)];
+    if (TOP || !WARP) sync();
+    if (!WARP && w == 0) {
+        s0 = sh.red[1][lane & (warps - 1)]; s1 = sh.red[2][lane & (warps - 1)];
         for (int d = warps >> 1; d; d >>= 1) { s0 += __shfl_xor_sync(0xffffffffu, s0, d); s1 += __shfl_xor_sync(0xffffffffu, s1, d); }
-        if (lane == 0) { part[0] = m; part[1] = s0; part[2] = s1; }
+        if (lane == 0) { sh.part[0] = m; sh.part[1] = s0; sh.part[2] = s1; }
     }
     if constexpr (TOP) {
-        const unsigned b = bound[lane];
+        const unsigned b = sh.bound[lane];
         int above = 0;                                               // places are distinct: ties by lane
 #pragma unroll
         for (int k = 0; k < 32; ++k) { const unsigned o = __shfl_sync(0xffffffffu, b, k); above += o > b || (o == b && k < lane); }
@@ -273,7 +285,7 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
                 if (v[j] < least) continue;
                 const int c = g * V<T> + j - x.off;
                 if (c < 0 || c >= a.vocab) continue;
-                const int at = atomicAdd(&found, 1);
+                const int at = atomicAdd(&sh.found, 1);
                 if (at < a.room) cand[at] = key_of(v[j], c);
             }
         };
@@ -286,23 +298,23 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
                 if (tail) offer(x.all - 1, x.any(x.all - 1));
             }
         } else {
-            if (order_of(mine) >= kth) hit[atomicAdd(&hits, 1)] = tid;
-            __syncthreads();
-            for (int h = w; h < hits; h += warps) {                  // a thread's groups read again by a warp
-                const int owner = (int)rank * threads + hit[h];
+            if (order_of(mine) >= kth) sh.hit[atomicAdd(&sh.hits, 1)] = tid;
+            sync();
+            for (int h = w; h < sh.hits; h += warps) {               // a thread's groups read again by a warp
+                const int owner = (int)rank * threads + sh.hit[h];
                 for (int g = x.first + owner + lane * stride; g < x.end; g += 32 * stride) offer(g, x.whole(g));
                 if (lane == 0 && owner == 0 && x.first == 1) offer(0, x.any(0));
                 if (lane == 0 && owner == stride - 1 && x.end < x.all && x.all - 1 >= x.first) offer(x.all - 1, x.any(x.all - 1));
             }
         }
-        __syncthreads();
-        const int n = found;
+        sync();
+        const int n = sh.found;
         if (n <= a.room) {                                             // how many are larger: a warp per candidate
             for (int k = w; k < n; k += warps) {
                 const Key mykey = cand[k];
                 int rnk = 0;
                 for (int q = lane; q - lane < n; q += 32) rnk += __popc(__ballot_sync(0xffffffffu, q < n && cand[q] > mykey));
-                if (lane == 0 && rnk < a.k) best[rnk] = mykey;
+                if (lane == 0 && rnk < a.k) sh.best[rnk] = mykey;
             }
         } else {                                                     // too many equal ones: one after another, over the whole part of the row
             Key last = ~0ull;
@@ -320,22 +332,22 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
                 for (int g = x.first + me; g < x.end; g += stride) look(g);
                 if (me == 0 && x.first == 1) look(0);
                 if (me == stride - 1 && x.end < x.all && x.all - 1 >= x.first) look(x.all - 1);
-                __syncthreads();                                     // cand: the warps' largest
+                sync();                                              // cand: the warps' largest
 #pragma unroll
                 for (int d = 16; d; d >>= 1) { const Key q = __shfl_xor_sync(0xffffffffu, top, d); top = q > top ? q : top; }
                 if (lane == 0) cand[w] = top;
-                __syncthreads();
+                sync();
                 for (int q = 0; q < warps; ++q) top = cand[q] > top ? cand[q] : top;
-                if (tid == 0) best[k] = top;
+                if (tid == 0) sh.best[k] = top;
                 last = top;
             }
         }
     }
-    if (ranks > 1) cluster_sync(); else __syncthreads();
+    if (ranks > 1) cluster_sync(); else if (TOP || !WARP) sync();
     if (rank == 0) {
         if (ranks > 1) {
             if (w == 0) {                                            // a lane per block
-                const unsigned from = on_rank(smem_at(part), min((unsigned)lane, ranks - 1));
+                const unsigned from = on_rank(smem_at(sh.part), min((unsigned)lane, ranks - 1));
                 float pm, p0, p1;
                 asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pm) : "r"(from) : "memory");
                 asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p0) : "r"(from + 4) : "memory");
@@ -351,18 +363,19 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
                 if (lane >= (int)ranks) p0 = p1 = 0.f;
 #pragma unroll
                 for (int d = 4; d; d >>= 1) { p0 += __shfl_xor_sync(0xffffffffu, p0, d); p1 += __shfl_xor_sync(0xffffffffu, p1, d); }
-                if (lane == 0) { total[0] = top; total[1] = p0; total[2] = p1; }
+                if (lane == 0) { sh.total[0] = top; sh.total[1] = p0; sh.total[2] = p1; }
             }
             if (TOP && w < (int)ranks / 2) {                         // a warp for two blocks' tokens
                 Key two[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(two[i]) : "r"(on_rank(smem_at(best + lane), (unsigned)(2 * w + i))) : "memory");
-                joined[w][lane] = merge(two[0], two[1]);
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(two[i]) : "r"(on_rank(smem_at(sh.best + lane), (unsigned)(2 * w + i))) : "memory");
+                sh.joined[w][lane] = merge(two[0], two[1]);
             }
-            __syncthreads();
+            sync();
         }
-        const float top = ranks > 1 ? total[0] : part[0], all0 = ranks > 1 ? total[1] : part[1], all1 = ranks > 1 ? total[2] : part[2];
+        const float* const all = ranks > 1 ? sh.total : sh.part;
+        const float top = WARP ? m : all[0], all0 = WARP ? s0 : all[1], all1 = WARP ? s1 : all[2];
         const float log_sum = logf(all0);
         const bool none = all0 == 0.f;                               // no token can occur
         if (tid == 0) {
@@ -376,9 +389,9 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
                 if (a.top_logp) a.top_logp[row * a.k + place] = none ? -INFINITY : a.scale * (from_order((unsigned)(q >> 32)) - top) - log_sum;
             };
             if (w == 0) {
-                Key q = ranks > 1 ? joined[0][lane] : best[lane];
-                if (ranks > 2) q = merge(q, joined[1][lane]);
-                if (ranks > 4) q = merge(q, merge(joined[2][lane], joined[3][lane]));
+                Key q = ranks > 1 ? sh.joined[0][lane] : sh.best[lane];
+                if (ranks > 2) q = merge(q, sh.joined[1][lane]);
+                if (ranks > 4) q = merge(q, merge(sh.joined[2][lane], sh.joined[3][lane]));
                 if (lane < a.k) give(lane, q);
             }
         }
@@ -392,7 +405,14 @@ __global__ void __launch_bounds__(MOST_THREADS, 2) logprob_forward_kernel(const 
     grid_dep_sync();
     unsigned ranks;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    logprob_row<T, ENTROPY, TOP>(a, blockIdx.x / ranks, ranks, cluster_rank());
+    logprob_row<T, ENTROPY, TOP, false>(a, blockIdx.x / ranks, ranks, cluster_rank());
+}
+// Short rows, a warp each
+template <typename T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(32 * ROWS, 8) logprob_rows_kernel(const LogpArgs a) {
+    grid_dep_sync();
+    const int64_t row = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> 5);
+    if (row < a.rows) logprob_row<T, ENTROPY, TOP, true>(a, row, 1, 0);
 }
 
 struct LogpBack {
@@ -484,14 +504,26 @@ ftp_status check(const void* logits, int64_t rows, int32_t vocab, int64_t* ld, i
     return check_elements({logits}, precision == FTP_FP32 ? 4 : 2, who);
 }
 
-template <typename T> cudaError_t forward_of(const LogpArgs& a, cudaStream_t st) {
-    // A thread takes four groups and more, about 50 where the rows fill the GPU (4096 x 50021 bf16: 101 us with 512 threads a row, 82 with 256, 77 with
-    // 128, 113 with 64; 4000 x 32000 with 20 top tokens 90, 83, 131 us with 256, 128, 64); blocks share a row while that gives every multiprocessor no more than two.
+template <typename T> cudaError_t forward_of(LogpArgs& a, cudaStream_t st) {
+    // Few rows: four groups and more to a thread.  Otherwise a warp a row while that leaves enough warps (16000 x 20001 bf16: 104 us, 145 with 64 threads,
+    // 116 with 128; but 1500 x 20001: 29, 21, 16), and 128 threads above (8000 x 32000: 94, 102, 85 us; 4096 x 50021: 79, 85, 71, 101 with 512), or more while
+    // these do not fill the GPU (800 x 50000: 23 us with 128 threads, 19 with 256).  The choice does not depend on k, so that the log probabilities do not.
     const int groups = (a.vocab + V<T> - 1) / V<T>;
-    const int each = a.rows < SMS ? 4 : 50;                          // whatever k is, so that log probabilities do not depend on it
     int threads = 32, ranks = 1;
-    while (threads < MOST_THREADS && threads * each < groups) threads *= 2;
+    if (a.rows < SMS) while (threads < MOST_THREADS && threads * 4 < groups) threads *= 2;
+    else if (groups > (a.rows >= SMS * 64 ? 3200 : a.rows >= SMS * 16 ? 1600 : 128)) {
+        threads = 128;
+        while (threads < MOST_THREADS && a.rows * threads < SMS * 1024 && threads * 32 < groups) threads *= 2;
+    }
     while (ranks < 8 && a.rows * ranks * 2 <= 2 * SMS && ranks * 2 * threads * 2 <= groups) ranks *= 2;
+    // Rows of one warp: four to a block, because a multiprocessor starts a block every 0.27 us (8192 x 192 bf16: 16 us with a block a row, 4.6 here).
+    if (threads == 32 && ranks == 1 && a.rows >= SMS * ROWS) {
+        a.room = std::min(a.room, ROWS_CAND);
+        auto kern = a.k ? (a.entropy ? logprob_rows_kernel<T, true, true> : logprob_rows_kernel<T, false, true>)
+                        : (a.entropy ? logprob_rows_kernel<T, true, false> : logprob_rows_kernel<T, false, false>);
+        launch(kern, dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(32 * ROWS), a.k ? ROWS * a.room * sizeof(Key) : 0, st, a);
+        return cudaSuccess;
+    }
     auto kern = a.k ? (a.entropy ? logprob_forward_kernel<T, true, true> : logprob_forward_kernel<T, false, true>)
                     : (a.entropy ? logprob_forward_kernel<T, true, false> : logprob_forward_kernel<T, false, false>);
     return launch_cluster(kern, dim3((unsigned)(a.rows * ranks)), threads, a.k ? a.room * sizeof(Key) : 0, ranks, st, a);
@@ -516,7 +548,7 @@ ftp_status ftp_logprob_forward(const void* logits, int64_t rows, int32_t vocab, 
     if (ftp_status s = check_elements({targets, logp, entropy, lse, top, top_logp}, 4, who)) return s;
     if (ftp_status s = check_addresses({logp, entropy, lse, top, top_logp}, {logits, targets}, who)) return s;
     if (rows == 0) return FTP_OK;
-    const LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, std::max(32, std::min(CAND, vocab)), scale, scale * 1.44269504088896341f};
+    LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, std::max(32, std::min(CAND, vocab)), scale, scale * 1.44269504088896341f};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = precision == FTP_FP32 ? forward_of<float>(a, st) : forward_of<bf16>(a, st);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

@@ -545,6 +545,40 @@ def test_logprob_masks_ties_and_rows_of_nothing(vocab, dt, rows):
     close(d, H.logprob_backward(x64, t, 1.0, dl.double().cpu(), dh.double().cpu()), dt, "dlogits")
 
 
+@pytest.mark.parametrize("rows,vocab", [(592, 1), (593, 37), (595, 1025), (2371, 1500), (2370, 4500), (9475, 90)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("k", [1, 32])
+def test_logprob_many_short_rows(rows, vocab, dt, k):
+    """Rows enough to fill the GPU, of few tokens: random ones among masked ones, ties and rows of nothing, next to one another."""
+    g = gen("lp-short", rows, vocab, k, str(dt))
+    z = rnd(g, rows, vocab, scale=2.0)
+    z[1::5, ::2] = -math.inf
+    z[2::5] = 0.5
+    z[3::25] = -math.inf
+    z[4::5] = (torch.arange(vocab) % 4 == 1).double()
+    x, x64 = on_gpu(z, dt, 1, 1)
+    k, scale = min(k, vocab), 1.25
+    t = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    f32 = lambda *s: torch.full(s, -7.0, device="cuda")  # noqa: E731
+    logp, bare, ent, lse, tl = f32(rows), f32(rows), f32(rows), f32(rows, 2), f32(rows, k)
+    top = torch.full((rows, k), -7, dtype=torch.int32, device="cuda")
+    F.ftp_logprob_forward(x.t, t.cuda(), logp, entropy=ent, lse=lse, top=top, top_logp=tl, scale=scale)
+    F.ftp_logprob_forward(x.t, t.cuda(), bare, scale=scale)
+    assert torch.equal(bare, logp)
+    r_logp, r_ent, r_lse, lp, e1, e2 = H.logprob(x64, t, scale)
+    fin = torch.isfinite(r_logp)
+    assert bool((logp.cpu()[~fin] == -math.inf).all())
+    assert_within(logp.cpu()[fin], r_logp[fin], e1[fin], "logp")
+    assert_within(ent, r_ent, e2, "entropy")
+    assert torch.equal(lse[:, 0].double().cpu(), r_lse[:, 0])
+    want = torch.sort(x64, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(top.cpu().long(), want)
+    ref = lp.gather(1, want)
+    ok = torch.isfinite(ref)
+    assert bool((tl.cpu()[~ok] == -math.inf).all())
+    assert_within(tl.cpu()[ok], ref[ok], (e1[:, None] + 4 * H.U * ref.nan_to_num(0, 0, 0).abs())[ok], "top logp")
+
+
 def test_logprob_rows_with_nan_and_infinity():
     for dt in (BF, FP):
         for vocab in (50, 20001):
