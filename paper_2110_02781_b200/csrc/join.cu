@@ -867,20 +867,25 @@ void run_forward(JoinArgs& a, cudaStream_t st) {
     }
 }
 
-// The backward pass's work on its rows: runs of up to 64 rows (the float additions of a running sum), short ones while there are
-// fewer than two blocks for every multiprocessor.
+// The backward pass's work on its rows: runs of up to 64 rows (the float additions of a running sum), as long as give all blocks that the GPU
+// holds the same, once or more often (12000 x 3584 bf16 with runs of 64: 250 us, 173 with 41).  Eight columns a thread, two rows at a time, or
+// sixteen: of bf16 rows over 2048, 16 where only one block of the others would fit (16000 x 2560: 166 instead of 201 us), and where a row a time is taken
+// anyway or the second norm is alone (12000 x 4096: layer norms 235 instead of 267, the second norm alone 126 instead of 147; but both rms 144 and 130
+// for 8192 x 4096).  Float 8000 x 2560 rather 8: 130 instead of 156.
 struct JoinPlan { int threads, groups, run; int64_t blocks; };
 JoinPlan plan_backward(const ftp_join_desc* d) {
     JoinPlan p;
     const int v = d->precision == FTP_FP32 ? 4 : 8;
-    row_shape(d->cols, v, (d->cols <= 512 * 8 ? 8 : 16) / v, &p.threads, &p.groups);
+    const bool layer = d->post == FTP_NORM_LAYER || d->pre == FTP_NORM_LAYER, few = d->cols <= 2048 || (d->cols <= 4096 && (v == 4 || (d->post && !layer && d->cols > 2560)));
+    row_shape(d->cols, v, (few ? 8 : 16) / v, &p.threads, &p.groups);
     const int64_t each = (int64_t)SMS * std::min(16, BACKWARD_THREADS / p.threads);
-    p.run = (int)std::min<int64_t>(64, std::max<int64_t>(4, (d->rows + each - 1) / each));
+    const int64_t turns = std::max<int64_t>(1, (d->rows + 64 * each - 1) / (64 * each));                  // of the GPU's blocks: whole ones
+    p.run = (int)std::max<int64_t>(4, (d->rows + each * turns - 1) / (each * turns));
     p.blocks = (d->rows + p.run - 1) / p.run;
     return p;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-constexpr size_t MOST_SMEM = 200 * 1024;                          // for the running sums
+constexpr size_t MOST_SMEM = 200 * 1024, KERNEL_SMEM = 220 * 1024;  // for the running sums, and with the rows ahead
 struct JoinSpace { size_t sums, gate, spill, total; };
 JoinSpace space_of(const ftp_join_desc* d, const JoinPlan& p, int nsums) {
     const int v = d->precision == FTP_FP32 ? 4 : 8;
@@ -907,11 +912,12 @@ ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, int kind, cudaS
         if (kind == BOTH) kern = backward_kernel<T, G, BOTH>(vec, layer);
         else if (kind == PRE_ONLY) kern = backward_kernel<T, G, PRE_ONLY>(vec, layer);
         if (kern && vec) staged = (size_t)(!layer && G * V<T> <= 8 ? PAIR : 1) * 4 * G * 16 * p.threads;
+        if (smem + staged > KERNEL_SMEM) { kern = nullptr; staged = 0; }                                      // five sums beside the rows ahead: bf16 over 7680 columns, float over 6144
     }
     if (!kern) kern = backward_kernel<T, G, ANY>(vec, layer);
     smem += staged;
     // 48 KB with what the kernel holds beside it
-    if (smem > 40 * 1024) FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 220 * 1024), FTP_ECUDA, "%s: no shared memory", who);
+    if (smem > 40 * 1024) FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), KERNEL_SMEM), FTP_ECUDA, "%s: no shared memory", who);
     launch(kern, dim3((unsigned)p.blocks), dim3(p.threads), smem, st, a);
     return FTP_OK;
 }
@@ -931,7 +937,7 @@ ftp_status run_backward(JoinArgs& a, const JoinPlan& p, int kind, cudaStream_t s
         auto kern = layer ? (vec ? join_backward_wide_kernel<T, true, true> : join_backward_wide_kernel<T, false, true>)
                           : (vec ? join_backward_wide_kernel<T, true, false> : join_backward_wide_kernel<T, false, false>);
         const size_t smem = a.spill ? 0 : (size_t)a.nsums * p.groups * V<T> * p.threads * 4;
-        FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), 220 * 1024), FTP_ECUDA, "%s: no shared memory", who);
+        FTP_REQUIRE(more_shared(reinterpret_cast<const void*>(kern), KERNEL_SMEM), FTP_ECUDA, "%s: no shared memory", who);
         launch(kern, dim3((unsigned)p.blocks), dim3(p.threads), smem, st, a);
         return FTP_OK;
     }

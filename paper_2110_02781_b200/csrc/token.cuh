@@ -190,8 +190,9 @@ template <typename T, bool VEC> __device__ __forceinline__ void fetch_vector(con
     for (int j = 0; j < P<T>; ++j) v[j] = f2(f[2 * j], f[2 * j + 1]);
 }
 
-// Sums over the threads of a block (32 to 512, a power of two) that holds one row, through one place per warp; `red` holds two sets of
+// Sums over the threads of a block (32 to 512, whole warps) that holds one row, through one place per warp; `red` holds two sets of
 // 16 places, used in turn, so that one barrier a sum is enough.  The order of additions depends on the thread alone.
+__device__ __forceinline__ int halves(int warps) { return 1 << (31 - __clz(warps - 1)); }   // half of the power of two that holds 2 to 16 warps
 struct RowSum {
     float* red;
     int turn;
@@ -204,8 +205,9 @@ struct RowSum {
         turn ^= 1;
         if (lane == 0) at[threadIdx.x >> 5] = a;
         __syncthreads();
-        a = at[lane & (n - 1)];
-        for (int d = n >> 1; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+        const int h = halves(n), k = lane & (2 * h - 1);
+        a = k < n ? at[k] : 0.f;
+        for (int d = h; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
         return a;
     }
 };
@@ -224,9 +226,10 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
         for (int i = 0; i < N; ++i) at[(threadIdx.x >> 5) * N + i] = v[i];
     }
     __syncthreads();
+    const int h = halves(n), k = lane & (2 * h - 1);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = at[(lane & (n - 1)) * N + i];
-    for (int d = n >> 1; d; d >>= 1) {
+    for (int i = 0; i < N; ++i) v[i] = k < n ? at[k * N + i] : 0.f;
+    for (int d = h; d; d >>= 1) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
     }
@@ -333,12 +336,13 @@ inline ftp_status drop_of(Drop* d, double p, const void* rng, int32_t site, int6
     return FTP_OK;
 }
 
-// threads of a row (32..512) and groups per thread (a power of two, `most` at most while that needs no more than 512 threads)
+// threads of a row (whole warps, 512 at most) and groups per thread (a power of two, `most` at most while that needs no more than 512 threads)
 inline void row_shape(int cols, int v, int most, int* threads, int* groups) {
-    *threads = 32;
-    while (*threads < 512 && (int64_t)*threads * v * most < cols) *threads *= 2;
+    int t = 32;
+    while (t < 512 && (int64_t)t * v * most < cols) t *= 2;
     *groups = 1;
-    while ((int64_t)*threads * v * *groups < cols) *groups *= 2;
+    while ((int64_t)t * v * *groups < cols) *groups *= 2;
+    *threads = ((cols + v * *groups - 1) / (v * *groups) + 31) / 32 * 32;
 }
 
 }  // namespace token
