@@ -291,8 +291,8 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_kernel(const
         if (a.states && n > 0) lane.put_state(a.states + (seq.start / RUN + b + t0 / RUN) * a.cols, a.cols, h);
         if (n == RUN) r.template out<true>(a, row, n, lane, h); else r.template out<false>(a, row, n, lane, h);
     }
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it; every block has read h0, which may be h1
     if (a.h1 && w == 0 && rank == 0 && join.ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
-    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
 // ---- rows that start on 16 bytes: tiles through the copy engine ----
@@ -422,10 +422,10 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
         parity ^= s;
         s ^= 1;
     }
-    if (a.h1 && w == 0 && rank == 0 && ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
     if (l == 0) tiles_done();
     __syncwarp();
-    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it; every block has read h0, which may be h1
+    if (a.h1 && w == 0 && rank == 0 && ok) lane.put_state(a.h1 + b * a.cols, a.cols, carry);
 }
 
 // The same backward.  Between its two walks a thread keeps, per step, a, 1 - a and the gradient g that reaches h from its own output in
@@ -568,10 +568,10 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
             s ^= 1;
         }
     }
-    if (a.dh0 && w == 0 && rank == 0 && ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
     if (l == 0) tiles_done();
     __syncwarp();
-    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it; every block has read dh1, which may be dh0
+    if (a.dh0 && w == 0 && rank == 0 && ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
 }
 
 // Sequences of at most one run, a warp each, a step at a time: a serving program's call.
@@ -716,8 +716,8 @@ __global__ void __launch_bounds__(32 * REG_WARPS<T>, sizeof(T) == 2 ? 3 : 2) rec
         if (!join.ok) continue;
         if (n == RUN) r.template out<true>(a, row, n, lane, before, q); else r.template out<false>(a, row, n, lane, before, q);
     }
+    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it; every block has read dh1, which may be dh0
     if (a.dh0 && w == 0 && rank == 0 && join.ok) lane.put_state(a.dh0 + b * a.cols, a.cols, carry);
-    if (ranks > 1) cluster_sync();                                   // nobody leaves while another block may send to it
 }
 
 // ---- host ----

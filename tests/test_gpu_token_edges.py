@@ -1,0 +1,35 @@
+"""Operators around the feed-forward products on the GPU, where values or layouts are at their limits: states updated in place
+across a cluster, tails of runs, the float range's ends, what lies under a dropped element, gates far from 0."""
+import math
+
+import pytest
+import torch
+
+import token_helpers as H
+from ffn_helpers import HALF, assert_within
+from test_gpu_token import BF, FP, close, gen, on_gpu, rec_inputs, rnd, rng_of, vec
+
+F = pytest.importorskip("paper_2110_02781_b200")
+pytestmark = pytest.mark.gpu
+
+
+# ---- recurrence: one tensor for the states in front and behind --------------------------------------------------------
+@pytest.mark.parametrize("seqs,steps,cols", [(1, 2048, 64), (1, 1000, 128), (2, 600, 96), (1, 2047, 31), (3, 700, 65)])
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_states_in_place_of_one_another_in_one_turn_of_a_cluster(seqs, steps, cols, dt):
+    g = gen("place", seqs, steps, cols)
+    rows = seqs * steps
+    f, v, o, dy = (rnd(g, seqs, steps, cols).to(dt).cuda() for _ in range(4))
+    h0, dh1 = rnd(g, seqs, cols).float().cuda(), rnd(g, seqs, cols).float().cuda()
+    states = torch.empty(F.ftp_recurrence_states(rows, seqs), cols, device="cuda")
+    y, y2, h1 = torch.empty_like(f), torch.empty_like(f), torch.empty_like(h0)
+    F.ftp_recurrence_forward(f, v, y, o=o, h0=h0, h1=h1, states=states)
+    grads = [torch.empty_like(f) for _ in range(6)]
+    dh0 = torch.empty_like(h0)
+    F.ftp_recurrence_backward(f, v, dy, states, grads[0], grads[1], o=o, do=grads[2], dh1=dh1, dh0=dh0)
+    for _ in range(20):
+        h, dh = h0.clone(), dh1.clone()
+        F.ftp_recurrence_forward(f, v, y2, o=o, h0=h, h1=h)
+        F.ftp_recurrence_backward(f, v, dy, states, grads[3], grads[4], o=o, do=grads[5], dh1=dh, dh0=dh)
+        assert torch.equal(y, y2) and torch.equal(h, h1) and torch.equal(dh, dh0)
+        assert all(torch.equal(a, b) for a, b in zip(grads[:3], grads[3:]))
