@@ -557,13 +557,16 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
                     tile_out(&maps_out.m[1], c, seq.start + t0, tiles + (4 * s + 1) * TILE_BYTES);
                     tiles_commit();
                 }
-            } else if (ok)
-                for (int i = 0; i < n; ++i) {
-                    const int64_t row = seq.start + t0 + i;
-                    lane.put_word(static_cast<T*>(a.df) + row * a.lddf, a.cols, *reinterpret_cast<const unsigned*>(at + 128 * i));
-                    lane.put_word(static_cast<T*>(a.dv) + row * a.lddv, a.cols, *reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
-                    if (FORM) lane.put_word(static_cast<T*>(a.dout) + row * a.lddo, a.cols, *reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
-                }
+            } else {
+                tiles_fence();                                       // the copy engine fills these tiles again in the next turn
+                if (ok)
+                    for (int i = 0; i < n; ++i) {
+                        const int64_t row = seq.start + t0 + i;
+                        lane.put_word(static_cast<T*>(a.df) + row * a.lddf, a.cols, *reinterpret_cast<const unsigned*>(at + 128 * i));
+                        lane.put_word(static_cast<T*>(a.dv) + row * a.lddv, a.cols, *reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
+                        if (FORM) lane.put_word(static_cast<T*>(a.dout) + row * a.lddo, a.cols, *reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
+                    }
+            }
             parity ^= s;
             s ^= 1;
         }

@@ -33,3 +33,28 @@ def test_states_in_place_of_one_another_in_one_turn_of_a_cluster(seqs, steps, co
         F.ftp_recurrence_backward(f, v, dy, states, grads[3], grads[4], o=o, do=grads[5], dh1=dh, dh0=dh)
         assert torch.equal(y, y2) and torch.equal(h, h1) and torch.equal(dh, dh0)
         assert all(torch.equal(a, b) for a, b in zip(grads[:3], grads[3:]))
+
+
+# ---- recurrence: tails of runs -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("seqs,steps,cols", [(300, 391, 64), (320, 200, 32), (150, 1003, 128)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("coupled", [True, False])
+def test_backward_without_a_gate_walks_on_from_a_tail(seqs, steps, cols, dt, coupled):
+    """Enough sequences that a block walks one alone, in several turns of which the first has a partial run."""
+    g = gen("tail", seqs, steps, cols)
+    rows = seqs * steps
+    f, f64, v, v64, _, _ = rec_inputs(g, rows, cols, dt, coupled=coupled)
+    dy, dy64 = on_gpu(rnd(g, rows, cols), dt)
+    three = lambda t: t.view(seqs, steps, cols)  # noqa: E731
+    y, df, dv = (torch.full((rows, cols), -7.0, dtype=dt, device="cuda") for _ in range(3))
+    states = torch.empty(F.ftp_recurrence_states(rows, seqs), cols, device="cuda")
+    how = dict(coupled=coupled, act=F.ACT_NONE)
+    plain = lambda t: three(t.t.contiguous())  # noqa: E731
+    F.ftp_recurrence_forward(plain(f), plain(v), three(y), states=states, **how)
+    F.ftp_recurrence_backward(plain(f), plain(v), plain(dy), states, three(df), three(dv), **how)
+    zero = torch.zeros(cols, dtype=torch.float64)
+    for b in (0, seqs // 2, seqs - 1):
+        at = slice(b * steps, (b + 1) * steps)
+        want = H.recurrence_backward(f64[at], v64[at], None, zero, dy64[at], zero, None, coupled, dt)
+        close(df[at], want["df"], dt, f"df of {b}")
+        close(dv[at], want["dv"], dt, f"dv of {b}")
