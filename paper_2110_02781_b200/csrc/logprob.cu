@@ -27,7 +27,7 @@ struct LogpArgs {
     int32_t* top;
     int64_t rows, ld;
     int vocab, k, room;                                              // room: candidates that fit into shared memory
-    float scale, scale2;                                             // scale2: scale * log2(e)
+    float scale, scale2, near;                                       // scale2: scale * log2(e); near: see near_of
 };
 
 // a float's place in the order of floats (NaN above infinity)
@@ -72,8 +72,10 @@ template <typename T> struct Row {
 };
 
 __device__ __forceinline__ unsigned max_bf2(unsigned a, unsigned b) { unsigned r; asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }   // NaN only if both are
-// Logits far below any that counts are raised to this, so that their distance to the largest stays finite where it meets the factor 0.
+// Logits far below any that counts are raised to this, so that their distance to the largest stays finite where it meets the factor 0.  That holds while
+// the largest lies between FAR / 10 and `near_of`; other rows clamp the distances one by one.
 constexpr float FAR = -1e18f;
+inline float near_of(float scale2) { return (float)std::min(3.4e38, 3e38 / scale2 + FAR); }
 template <typename T> __device__ __forceinline__ uint4 raised(uint4 q) {   // a NaN stays one
     if constexpr (sizeof(T) == 2)
         asm("max.NaN.bf16x2 %0, %0, %4;\nmax.NaN.bf16x2 %1, %1, %4;\nmax.NaN.bf16x2 %2, %2, %4;\nmax.NaN.bf16x2 %3, %3, %4;"
@@ -107,7 +109,7 @@ template <typename T, bool ENTROPY> struct Sums {
         m = at = to;
     }
     // N groups of logits; what is not there is -infinity
-    template <int N> __device__ __forceinline__ void add(const uint4 (&q)[N], float c2) {
+    template <int N> __device__ __forceinline__ void add(const uint4 (&q)[N], float c2, float near) {
         float top;                                                   // the largest; with a NaN among them, that of the others
         if constexpr (sizeof(T) == 2) {
             unsigned w = max_bf2(max_bf2(q[0].x, q[0].y), max_bf2(q[0].z, q[0].w));
@@ -122,7 +124,7 @@ template <typename T, bool ENTROPY> struct Sums {
         }
         if (top > m) rescale(top, c2);
         const F2 less = f2(-at), c = f2(c2);
-        if (!ENTROPY || at > 0.1f * FAR) {
+        if (!ENTROPY || (at > 0.1f * FAR && at < near)) {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 F2 v[P<T>];
@@ -136,7 +138,7 @@ template <typename T, bool ENTROPY> struct Sums {
                     if (ENTROPY) s1 = fma2(e, t, s1);
                 }
             }
-        } else                                                       // even the largest logit is that far down
+        } else                                                       // even the largest logit is that far down, or it is that large
             for (int u = 0; u < N; ++u) {
                 F2 v[P<T>];
                 decode<T>(q[u], v);
@@ -201,34 +203,34 @@ __device__ __forceinline__ void logprob_row(const LogpArgs& a, int64_t row, unsi
     for (int u = 0; u < 4; ++u) held[u] = x.first + me + u * stride < x.end ? x.whole(x.first + me + u * stride) : nothing<T>();
     int i = x.first + me + 4 * stride;
     if constexpr (TOP) {
-        s.add(held, a.scale2);
+        s.add(held, a.scale2, a.near);
         for (; i + 3 * stride < x.end; i += 4 * stride) {
             uint4 q[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
-            s.add(q, a.scale2);
+            s.add(q, a.scale2, a.near);
         }
     } else {                                                         // the next four are on their way meanwhile
         for (; i + 3 * stride < x.end; i += 4 * stride) {
             uint4 q[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) q[u] = x.whole(i + u * stride);
-            s.add(held, a.scale2);
+            s.add(held, a.scale2, a.near);
 #pragma unroll
             for (int u = 0; u < 4; ++u) held[u] = q[u];
         }
-        s.add(held, a.scale2);
+        s.add(held, a.scale2, a.near);
     }
     if (i < x.end) {
         uint4 q[4];
         q[3] = nothing<T>();
 #pragma unroll
         for (int u = 0; u < 3; ++u) q[u] = i + u * stride < x.end ? x.whole(i + u * stride) : nothing<T>();
-        s.add(q, a.scale2);
+        s.add(q, a.scale2, a.near);
     }
     if (head || tail) {
         const uint4 ends[2] = {head ? x.any(0) : nothing<T>(), tail ? x.any(x.all - 1) : nothing<T>()};
-        s.add(ends, a.scale2);
+        s.add(ends, a.scale2, a.near);
     }
     const float mine = s.m;
     // the block's sums
@@ -548,7 +550,7 @@ ftp_status ftp_logprob_forward(const void* logits, int64_t rows, int32_t vocab, 
     if (ftp_status s = check_elements({targets, logp, entropy, lse, top, top_logp}, 4, who)) return s;
     if (ftp_status s = check_addresses({logp, entropy, lse, top, top_logp}, {logits, targets}, who)) return s;
     if (rows == 0) return FTP_OK;
-    LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, std::max(32, std::min(CAND, vocab)), scale, scale * 1.44269504088896341f};
+    LogpArgs a{logits, targets, logp, entropy, lse, top_logp, top, rows, ldl, vocab, k, std::max(32, std::min(CAND, vocab)), scale, scale * 1.44269504088896341f, near_of(scale * 1.44269504088896341f)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = precision == FTP_FP32 ? forward_of<float>(a, st) : forward_of<bf16>(a, st);
     FTP_REQUIRE(e == cudaSuccess, FTP_ECUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));

@@ -58,3 +58,55 @@ def test_backward_without_a_gate_walks_on_from_a_tail(seqs, steps, cols, dt, cou
         want = H.recurrence_backward(f64[at], v64[at], None, zero, dy64[at], zero, None, coupled, dt)
         close(df[at], want["df"], dt, f"df of {b}")
         close(dv[at], want["dv"], dt, f"dv of {b}")
+
+
+# ---- log probabilities: the float range's ends ---------------------------------------------------------------------------
+def logprob_both_ways(x, t, scale, dt):
+    """Forward with entropy, and the gradients of all three ways in, against 64 bits."""
+    xd, x64 = x.to(dt).cuda(), x.to(dt).double()
+    rows = x.shape[0]
+    logp, ent, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    F.ftp_logprob_forward(xd, t.cuda(), logp, entropy=ent, lse=lse, scale=scale)
+    r_logp, r_ent, r_lse, _, e1, e2 = H.logprob(x64, t, scale)
+    fin = torch.isfinite(r_logp.float())                                 # what a float can hold
+    assert bool((logp.cpu()[~fin] == -math.inf).all())
+    assert_within(logp.cpu()[fin], r_logp[fin], e1[fin], "logp")
+    assert_within(ent, r_ent, e2, "entropy")
+    assert torch.equal(lse[:, 0].double().cpu(), r_lse[:, 0])
+    g = gen("ends", rows, x.shape[1])
+    dl, dl64 = vec(rnd(g, rows))
+    dh, dh64 = vec(rnd(g, rows))
+    for a, b in ((dl, None), (None, dh), (dl, dh)):
+        d = torch.empty_like(xd)
+        F.ftp_logprob_backward(xd, t.cuda(), lse, a, d, entropy=ent, dentropy=b, scale=scale)
+        close(d, H.logprob_backward(x64, t, scale, dl64 if a is not None else None, dh64 if b is not None else None), dt, "dlogits")
+
+
+def rows_at_the_top(rows, vocab, dt):
+    low, high = torch.finfo(dt).min, torch.finfo(dt).max
+    x = torch.zeros(6, vocab, dtype=torch.float64)
+    x[0, vocab // 2] = high                                              # a token that is forced
+    x[1, 1] = x[1, vocab - 1] = high                                     # two of them
+    x[2] = -math.inf
+    x[2, vocab // 2], x[2, 3] = high, low                                # the whole range in one row
+    x[3, vocab // 2] = 2.0e38
+    x[4, vocab // 2], x[4, 2] = 2.5e38, 1.0e38
+    x[5] = high                                                          # uniform
+    return x[torch.arange(rows) % 6]
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 40), (6, 9000), (6, 70000), (600, 40), (606, 9000), (3, 70000)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("scale", [1.0, 0.5, 1.5, 1000.0])
+def test_logprob_of_logits_at_the_top_of_the_range(rows, vocab, dt, scale):
+    t = torch.full((rows,), vocab // 2, dtype=torch.int32)
+    t[1::2] = 1
+    x = rows_at_the_top(rows, vocab, dt)
+    logp, ent, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    F.ftp_logprob_forward(x.to(dt).cuda(), t.cuda(), logp, entropy=ent, lse=lse, scale=scale)
+    r_logp, r_ent, r_lse, _, e1, e2 = H.logprob(x.to(dt).double(), t, scale)
+    fin = torch.isfinite(r_logp.float())                                 # what a float can hold
+    assert bool((logp.cpu()[~fin] == -math.inf).all())
+    assert_within(logp.cpu()[fin], r_logp[fin], e1[fin], "logp")
+    assert_within(ent, r_ent, e2, "entropy")
+    assert torch.equal(lse[:, 0].double().cpu(), r_lse[:, 0])
