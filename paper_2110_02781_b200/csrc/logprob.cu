@@ -447,8 +447,10 @@ __global__ void __launch_bounds__(256) logprob_backward_kernel(const LogpBack a)
         }
         const int t = a.target ? a.target[row] : -1;
         const float m = a.lse[2 * row], log_sum = a.lse[2 * row + 1];
-        const bool none = m == -INFINITY && log_sum == -INFINITY, given = t >= 0 && t < a.vocab && !none, near = m > 0.1f * FAR;
+        const bool none = m == -INFINITY && log_sum == -INFINITY, given = t >= 0 && t < a.vocab && !none;
         const float dl = given && a.dlogp ? a.dlogp[row] * a.scale : 0.f, dh = ENTROPY ? a.dentropy[row] * a.scale : 0.f;
+        // log probabilities of raised logits, and dentropy times them, stay finite: elsewhere what meets the factor 0 is left out
+        const bool near = m > 0.1f * FAR && (m - FAR) * a.scale * fmaxf(1.f, fabsf(dh)) < 1e38f;
         const float plus = ENTROPY ? -fmaf(dh, a.entropy[row], dl) : -dl;
         const F2 less = f2(-m), c = f2(a.scale), sum = f2(-log_sum), b = f2(-dh), k = f2(plus);
         const int at = given ? (t + x.off) / V<T> : -1, j_at = given ? (t + x.off) % V<T> : 0;     // the target's group, and its place in it
@@ -470,8 +472,14 @@ __global__ void __launch_bounds__(256) logprob_backward_kernel(const LogpBack a)
                     const float2 z = parts(mul2(lp, f2(ffn::LOG2E)));
                     p = f2(ffn::ex2_fast(z.x), ffn::ex2_fast(z.y));
                 }
-                if (ENTROPY) v[j] = mul2(p, fma2(b, near ? lp : f2(fmaxf(l.x, LOW), fmaxf(l.y, LOW)), k));
-                else v[j] = mul2(p, k);
+                if (ENTROPY) {
+                    v[j] = mul2(p, fma2(b, lp, k));
+                    if (!near) {
+                        const float2 q = parts(p), d = parts(v[j]);
+                        v[j] = f2(q.x == 0.f ? 0.f : d.x, q.y == 0.f ? 0.f : d.y);
+                    }
+                } else
+                    v[j] = mul2(p, k);
             }
             if (none)
 #pragma unroll

@@ -110,3 +110,23 @@ def test_logprob_of_logits_at_the_top_of_the_range(rows, vocab, dt, scale):
     assert_within(logp.cpu()[fin], r_logp[fin], e1[fin], "logp")
     assert_within(ent, r_ent, e2, "entropy")
     assert torch.equal(lse[:, 0].double().cpu(), r_lse[:, 0])
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 40), (6, 9000), (606, 1001)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("scale", [1.0, 0.5, 1.5, 1000.0])
+def test_logprob_gradients_at_the_top_of_the_range(rows, vocab, dt, scale):
+    t = torch.full((rows,), vocab // 2, dtype=torch.int32)
+    t[1::2] = 1
+    logprob_both_ways(rows_at_the_top(rows, vocab, dt), t, scale, dt)
+
+
+@pytest.mark.parametrize("rows,vocab", [(5, 40), (7, 9001), (600, 300)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("scale", [1e9, 1e12, 1e18])
+def test_logprob_of_masked_rows_with_a_large_scale(rows, vocab, dt, scale):
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    x = rnd(gen("scale", rows, vocab), rows, vocab, scale=2.0) / scale
+    x[:, 1::3] = -math.inf
+    x[:, 2::5] = torch.finfo(dt).min
+    logprob_both_ways(x, torch.zeros(rows, dtype=torch.int32), scale, dt)
