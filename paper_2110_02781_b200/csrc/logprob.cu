@@ -11,6 +11,7 @@
 // 4096 x 50021 bf16 with entropies: 73-83 us (5.0-5.6 TB/s; the exponentials use two thirds of their pipe); 16 x 128000 with 20 top tokens: 9.1 us, a
 // chain of eight exchanges between threads, warps and blocks; 16000 x 12000 with a warp a row 64 us (6.0 TB/s); backward, 8192 x 32000: 181-191 us (5.5-5.8 TB/s).
 #include <algorithm>
+#include <type_traits>
 #include "token.cuh"
 
 namespace ftp {
@@ -461,26 +462,26 @@ __global__ void __launch_bounds__(256) logprob_backward_kernel(const LogpBack a)
             const bool whole = g >= x.first && g < x.end;
             if (!whole) q[u] = x.any(g);
             F2 v[P<T>];
-            decode<T>(ENTROPY && near ? raised<T>(q[u]) : q[u], v);
+            const auto gradient = [&](auto far) {
+                decode<T>(ENTROPY && !far.value ? raised<T>(q[u]) : q[u], v);
 #pragma unroll
-            for (int j = 0; j < P<T>; ++j) {
-                const F2 lp = fma2(add2(v[j], less), c, sum);
-                const float2 l = parts(lp);
-                F2 p;
-                if (sizeof(T) == 4) p = f2(expf(l.x), expf(l.y));
-                else {
-                    const float2 z = parts(mul2(lp, f2(ffn::LOG2E)));
-                    p = f2(ffn::ex2_fast(z.x), ffn::ex2_fast(z.y));
-                }
-                if (ENTROPY) {
-                    v[j] = mul2(p, fma2(b, lp, k));
-                    if (!near) {
-                        const float2 q = parts(p), d = parts(v[j]);
-                        v[j] = f2(q.x == 0.f ? 0.f : d.x, q.y == 0.f ? 0.f : d.y);
+                for (int j = 0; j < P<T>; ++j) {
+                    const F2 lp = fma2(add2(v[j], less), c, sum);
+                    const float2 l = parts(lp);
+                    F2 p;
+                    if (sizeof(T) == 4) p = f2(expf(l.x), expf(l.y));
+                    else {
+                        const float2 z = parts(mul2(lp, f2(ffn::LOG2E)));
+                        p = f2(ffn::ex2_fast(z.x), ffn::ex2_fast(z.y));
                     }
-                } else
-                    v[j] = mul2(p, k);
-            }
+                    v[j] = mul2(p, ENTROPY ? fma2(b, lp, k) : k);
+                    if (far.value) {
+                        const float2 e = parts(p), d = parts(v[j]);
+                        v[j] = f2(e.x == 0.f ? 0.f : d.x, e.y == 0.f ? 0.f : d.y);
+                    }
+                }
+            };
+            if (!ENTROPY || near) gradient(std::false_type{}); else gradient(std::true_type{});
             if (none)
 #pragma unroll
                 for (int j = 0; j < P<T>; ++j) v[j] = 0ull;
