@@ -499,7 +499,8 @@ ftp_status ftp_dropout(const void* x, void* y, int64_t rows, int32_t cols, int64
  * post, pre: FTP_NORM_NONE; FTP_NORM_RMS, v / sqrt(mean(v^2) + eps) * w + b; FTP_NORM_LAYER, (v - mean(v)) / sqrt(var(v) + eps) *
  * w + b, over a row; w and b nullable (1 and 0).  gate: NULL (1); with gate_rows 0 a float vector of cols; else a matrix of the
  * tensors' type with a row for every gate_rows tokens (the last may have fewer).  s is rounded to the tensors' type and y is
- * made of the rounded s.  Rows hold up to 16384 columns. */
+ * made of the rounded s.  A dropped element is 0 in s, and nothing goes back through it, whatever u (without post) or the
+ * gradients hold there; gates are finite.  Rows hold up to 16384 columns. */
 enum { FTP_NORM_NONE = 0, FTP_NORM_RMS = 1, FTP_NORM_LAYER = 2 };
 typedef struct {
     int64_t rows;

@@ -251,6 +251,8 @@ template <typename T> struct Running {
 //   e = ds + r g;   c1 = - r mean(g) (layer norm only), c2 = - r mean(g x^);   D = e + c1 + c2 x^
 //   dx = alpha D;   dv = K D;   du = r' (dv w_post - mean(dv w_post) - u^ mean(dv w_post u^));   dgate = (K / gate) D (u^ w_post + b_post)
 //
+// A dropped element adds nothing, whatever u and D hold there: its terms are cleared, where a product with 0 could be NaN (1 % of the time; a
+// gate, which multiplies what is left, has to be finite everywhere: clearing behind it too took 3 to 5 %).
 // The sums over a row that du needs are sums of K w_post (e + c1 + c2 x^) and of that times u^: linear in c1 and c2, so all sums of a row
 // go through one exchange, and its values are decoded once.
 // KIND: what is known when compiled, because a question per group of columns costs three instructions.  BOTH: both norms with weights; PRE_ONLY: the second
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
             rn[q] = f2(ri);
             ln[q] = f2(-mu * ri);
         }
-        F2 e[R][G][P<T>], xh[R][G][P<T>], mask[R][G][P<T>], uh[R][G][P<T>], sum[R][NS];   // mask: beta mask / (1 - p)
+        F2 e[R][G][P<T>], xh[R][G][P<T>], kept[R][G][P<T>], uh[R][G][P<T>], sum[R][NS];   // kept: all bits of what is not dropped
 #pragma unroll
         for (int q = 0; q < R; ++q) {
 #pragma unroll
@@ -359,13 +361,13 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int j = 0; j < P<T>; ++j) mask[q][g][j] = on[q] ? f : 0ull;
+                for (int j = 0; j < P<T>; ++j) kept[q][g][j] = on[q] ? ~0ull : 0ull;
             if (drop.cut) {
                 const unsigned long long n = drop.first_of(row + q, a.cols);
 #pragma unroll
-                for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(n, t, a.threads, g, mask[q][g]);
+                for (int g = 0; g < G; ++g) drop.template operator()<T, VEC>(n, t, a.threads, g, kept[q][g]);
             }
-            clip_row<T, G, VEC>(a, t, mask[q]);
+            clip_row<T, G, VEC>(a, t, kept[q]);
             if (USUAL || a.ds) decode_row<T, G>(rds[q], e[q]);
             else
 #pragma unroll
@@ -414,15 +416,16 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
                         for (int j = 0; j < P<T>; ++j) {
                             F2& x = uh[q][g][j];
                             x = fma2(x, rn[q], ln[q]);
-                            F2 k = mask[q][g][j];
+                            F2 k = f;
                             if (gated) k = mul2(k, gate[j]);
                             if (w_post) k = mul2(k, w[j]);
-                            const F2 z = mul2(k, x);
-                            sum[q][1] = fma2(z, e[q][g][j], sum[q][1]);
+                            const F2 z = mul2(k, x) & kept[q][g][j], d = e[q][g][j] & kept[q][g][j];
+                            if (LAYER) k &= kept[q][g][j];
+                            sum[q][1] = fma2(z, d, sum[q][1]);
                             if (pre) sum[q][2] = fma2(z, xh[q][g][j], sum[q][2]);
                             if (LAYER) {
                                 sum[q][4] = add2(sum[q][4], z);
-                                sum[q][5] = fma2(k, e[q][g][j], sum[q][5]);
+                                sum[q][5] = fma2(k, d, sum[q][5]);
                                 if (pre) sum[q][6] = fma2(k, xh[q][g][j], sum[q][6]);
                                 sum[q][7] = add2(sum[q][7], k);
                             }
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
                     put<T, VEC>(out_row<T>(a.dx, a.lddx, row + q), t, a.threads, g, a.cols, encode<T>(p));
                 }
 #pragma unroll
-                for (int j = 0; j < P<T>; ++j) d[j] = mul2(d[j], mask[q][g][j]);
+                for (int j = 0; j < P<T>; ++j) d[j] = mul2(d[j], f) & kept[q][g][j];
                 if (graded) {
                     F2 p[P<T>];
 #pragma unroll
@@ -481,6 +484,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
                         p[j] = w_post ? mul2(x[j], w[j]) : x[j];
                         if (b_post) p[j] = add2(p[j], b[j]);
                         p[j] = mul2(p[j], d[j]);
+                        if (!post) p[j] &= kept[q][g][j];            // u as it came
                         of_gate[j] = q ? add2(of_gate[j], p[j]) : p[j];
                     }
                     if (a.gate_rows == 1 && on[q]) put<T, VEC>(out_row<T>(a.dgate, a.lddg, row + q), t, a.threads, g, a.cols, encode<T>(p));
@@ -574,17 +578,17 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
         if (post) { mu = a.stats[row]; ri = a.stats[a.rows + row]; }
         const F2 rp = f2(r), lp = f2(-ms * r), rn = f2(ri), ln = f2(-mu * ri);
         const unsigned long long number = drop.cut ? drop.first_of(row, a.cols) : 0;
-        // e, x^, beta mask / (1 - p), u^ and dy of a group
-        const auto load = [&](int g, F2 (&e)[P<T>], F2 (&xh)[P<T>], F2 (&mask)[P<T>], F2 (&uh)[P<T>], F2 (&dy)[P<T>]) {
+        // e, x^, what is not dropped, u^ and dy of a group
+        const auto load = [&](int g, F2 (&e)[P<T>], F2 (&xh)[P<T>], F2 (&kept)[P<T>], F2 (&uh)[P<T>], F2 (&dy)[P<T>]) {
             uint4 rs, rdy, rds, ru;
             if (pre) rs = fetch<T, VEC>(in_row<T>(a.s, a.lds, row), t, a.threads, g, a.cols);
             if (a.dy) rdy = fetch<T, VEC>(in_row<T>(a.dy, a.ldy, row), t, a.threads, g, a.cols);
             if (a.ds) rds = fetch<T, VEC>(in_row<T>(a.ds, a.ldds, row), t, a.threads, g, a.cols);
             if (a.u) ru = fetch<T, VEC>(in_row<T>(a.u, a.ldu, row), t, a.threads, g, a.cols);
 #pragma unroll
-            for (int j = 0; j < P<T>; ++j) { e[j] = xh[j] = uh[j] = dy[j] = 0ull; mask[j] = f; }
-            if (drop.cut) drop.template operator()<T, VEC>(number, t, a.threads, g, mask);
-            clip<T, VEC>(t, a.threads, g, a.cols, mask);
+            for (int j = 0; j < P<T>; ++j) { e[j] = xh[j] = uh[j] = dy[j] = 0ull; kept[j] = ~0ull; }
+            if (drop.cut) drop.template operator()<T, VEC>(number, t, a.threads, g, kept);
+            clip<T, VEC>(t, a.threads, g, a.cols, kept);
             if (a.ds) decode<T>(rds, e);
             if (a.u) decode<T>(ru, uh);
 #pragma unroll
@@ -602,11 +606,11 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
             }
         };
         // K and K w_post
-        const auto factors = [&](int g, const F2 (&mask)[P<T>], F2 (&k)[P<T>], F2 (&kw)[P<T>]) {
+        const auto factors = [&](int g, const F2 (&kept)[P<T>], F2 (&k)[P<T>], F2 (&kw)[P<T>]) {
             F2 w[P<T>];
             if (a.gate) gate_of<T, VEC>(a, row, t, g, w);
 #pragma unroll
-            for (int j = 0; j < P<T>; ++j) k[j] = a.gate ? mul2(mask[j], w[j]) : mask[j];
+            for (int j = 0; j < P<T>; ++j) k[j] = (a.gate ? mul2(f, w[j]) : f) & kept[j];
             if (a.w_post) fetch_vector<T, VEC>(a.w_post, t, a.threads, g, a.cols, w);
 #pragma unroll
             for (int j = 0; j < P<T>; ++j) kw[j] = a.w_post ? mul2(k[j], w[j]) : k[j];
@@ -617,8 +621,8 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
         if (pre || post)
 #pragma unroll 1
             for (int g = 0; g < G; ++g) {
-                F2 e[P<T>], xh[P<T>], mask[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
-                load(g, e, xh, mask, uh, dy);
+                F2 e[P<T>], xh[P<T>], kept[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
+                load(g, e, xh, kept, uh, dy);
                 if (a.at[SUM_B_PRE] >= 0) run.add(a.at[SUM_B_PRE] * G + g, dy);
                 if (a.at[SUM_W_PRE] >= 0) {
 #pragma unroll
@@ -636,10 +640,11 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
                     }
                 }
                 if (post) {
-                    factors(g, mask, k, kw);
+                    factors(g, kept, k, kw);
 #pragma unroll
                     for (int j = 0; j < P<T>; ++j) {
                         const F2 z = mul2(kw[j], uh[j]);
+                        e[j] &= kept[j];
                         sum[1] = fma2(z, e[j], sum[1]);
                         sum[2] = fma2(z, xh[j], sum[2]);
                         if (LAYER) {
@@ -664,14 +669,15 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
         // dx may lie on ds: a thread reads its columns of a group before it writes them
 #pragma unroll 1
         for (int g = 0; g < G; ++g) {
-            F2 d[P<T>], xh[P<T>], mask[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
-            load(g, d, xh, mask, uh, dy);
-            factors(g, mask, k, kw);
+            F2 d[P<T>], xh[P<T>], kept[P<T>], uh[P<T>], dy[P<T>], k[P<T>], kw[P<T>];
+            load(g, d, xh, kept, uh, dy);
+            factors(g, kept, k, kw);
 #pragma unroll
             for (int j = 0; j < P<T>; ++j) {
                 d[j] = fma2(f2(c2f), xh[j], d[j]);
                 if (LAYER) d[j] = add2(d[j], f2(c1f));
                 dy[j] = mul2(alpha, d[j]);
+                d[j] &= kept[j];
             }
             if (a.dx) put<T, VEC>(out_row<T>(a.dx, a.lddx, row), t, a.threads, g, a.cols, encode<T>(dy));
             if (a.dgate) {
@@ -689,7 +695,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(co
                     for (int j = 0; j < P<T>; ++j) p[j] = add2(p[j], w[j]);
                 }
 #pragma unroll
-                for (int j = 0; j < P<T>; ++j) p[j] = mul2(p[j], mul2(d[j], mask[j]));
+                for (int j = 0; j < P<T>; ++j) p[j] = mul2(p[j], mul2(d[j], f)) & kept[j];
                 if (a.gate_rows == 1) put<T, VEC>(out_row<T>(a.dgate, a.lddg, row), t, a.threads, g, a.cols, encode<T>(p));
                 else run.add(a.at[SUM_GATE] * G + g, p);
             }

@@ -7,7 +7,7 @@ import torch
 
 import token_helpers as H
 from ffn_helpers import HALF, assert_within
-from test_gpu_token import BF, FP, close, gen, on_gpu, rec_inputs, rnd, rng_of, vec
+from test_gpu_token import BF, FP, close, gen, join_case, on_gpu, rec_inputs, rnd, rng_of, vec
 
 F = pytest.importorskip("paper_2110_02781_b200")
 pytestmark = pytest.mark.gpu
@@ -130,3 +130,47 @@ def test_logprob_of_masked_rows_with_a_large_scale(rows, vocab, dt, scale):
     x[:, 1::3] = -math.inf
     x[:, 2::5] = torch.finfo(dt).min
     logprob_both_ways(x, torch.zeros(rows, dtype=torch.int32), scale, dt)
+
+
+# ---- joins: what lies under a dropped element ------------------------------------------------------------------------------
+UNDER = [dict(post="none", pre="none", gate="vector"), dict(post="none", pre="rms", gate=None), dict(post="none", pre="layer", gate=7), dict(post="none", pre="rms", gate=1),
+         dict(post="rms", pre="rms", gate="vector"), dict(post="layer", pre="layer", gate=1, bias=1), dict(post="rms", pre="none", gate=50), dict(post="layer", pre="rms", gate=None, bare=1)]
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 64), (67, 133), (30, 520), (12, 4096), (11, 2560), (9, 8192), (5, 9000), (4, 9001)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("how", UNDER, ids=lambda h: f"{h['post']}-{h['pre']}-{h['gate']}")
+def test_whatever_lies_under_a_dropped_element_of_a_join(rows, cols, dt, how):
+    g, own, ref = join_case(rows, cols, 0, 0, dt, {"p": 0.25, **how})
+    own.pop("b_pre")
+    gone = ref["mask"] == 0
+    spoil = gone & (torch.rand(rows, cols, generator=g) < 0.2)
+    bad = torch.where(torch.rand(rows, cols, generator=g) < 0.5, math.nan, math.inf).double()
+    holes = lambda t: torch.where(spoil, bad, t)  # noqa: E731
+    u, u64 = on_gpu(rnd(g, rows, cols), dt)
+    s, s64 = on_gpu(rnd(g, rows, cols), dt)
+    ds, ds64 = on_gpu(rnd(g, rows, cols), dt)
+    dy, dy64 = on_gpu(rnd(g, rows, cols), dt)
+    stats = torch.zeros(4, rows, dtype=torch.float64)
+    for i, (kind, of) in enumerate(((how["post"], u64), (how["pre"], s64))):
+        if kind != "none":
+            mean, r = H.moments(of, kind, ref["eps"])
+            stats[2 * i], stats[2 * i + 1] = mean[:, 0], r[:, 0]
+    if how["post"] == "none":
+        u.t.copy_(holes(u64).to(dt))
+        out = torch.empty_like(u.t)
+        F.ftp_join_forward(u.t, s.t, out, None, **{**own, "pre": F.NORM_NONE, "w_pre": None})
+        close(out, H.join_forward(u64, s64, ref), dt, "s")
+    ds.t.copy_(holes(ds64).to(dt))
+    grads = {"d" + n: torch.empty(cols, device="cuda") for n in ("w_post", "b_post", "w_pre", "b_pre") if (how["post"] if "post" in n else how["pre"]) != "none"}
+    if own["gate"] is not None:
+        grads["dgate"] = torch.empty_like(own["gate"])
+    du, dx = torch.empty_like(u.t), torch.empty_like(u.t)
+    pre = how["pre"] != "none"
+    F.ftp_join_backward(u.t, s.t if pre else None, dy.t if pre else None, ds.t, stats.float().cuda(), du=du, dx=dx, **grads, **own)
+    want = H.join_backward(u64, s64, dy64, ds64, ref)
+    for name, t in {**grads, "du": du}.items():
+        close(t, want[name], t.dtype, name)
+    assert not torch.isfinite(dx.cpu()[spoil]).any()                     # the stream's gradient passes on what came in
+    dx.copy_(torch.where(spoil.cuda(), want["dx"][0].cuda(), dx.double()).to(dt))
+    close(dx, want["dx"], dt, "dx")
