@@ -72,12 +72,13 @@ template <typename T> __device__ __forceinline__ void split(unsigned w, float (&
     else { v[0] = bf_lo(w); v[1] = bf_hi(w); }
 }
 
-// a = 1 / (1 + e^-f) and 1 - a, each to a few roundings of itself, next to 1 and to 0 alike.  f below -79 counts as -79 (a 4e-35, 1 - a exactly
-// 1 in float), so that 0 times infinity does not arise.  bf16: hardware exponential and reciprocal, 2^-21 relative.
+// a = 1 / (1 + e^-f) and 1 - a, each to a few roundings of itself, next to 1 and to 0 alike.  f below -79 counts as -79 (a 5e-35, 1 - a exactly
+// 1 in float), so that 0 times infinity does not arise.  bf16: hardware exponential and reciprocal, 2^-21 relative, and 2^-24 |f| for the rounding of the
+// exponent (a gate of 20 in bf16 is itself known to 2^-9 of it).
+__device__ __forceinline__ float above(float f) { asm("max.NaN.f32 %0, %0, %1;" : "+f"(f) : "f"(-79.f)); return f; }
+template <typename T> __device__ __forceinline__ float exp_of_minus(float f) { return sizeof(T) == 4 ? expf(-f) : ffn::ex2_fast(f * -ffn::LOG2E); }
 template <typename T> __device__ __forceinline__ void gate(float f, float& a, float& other) {
-    float x = f * -ffn::LOG2E;
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(114.f));
-    const float e = sizeof(T) == 4 ? exp2f(x) : ffn::ex2_fast(x);
+    const float e = exp_of_minus<T>(above(f));
     a = sizeof(T) == 4 ? 1.f / (1.f + e) : ffn::rcp_fast(1.f + e);
     other = e * a;
 }
@@ -110,15 +111,15 @@ template <typename T> __device__ __forceinline__ void to_floats(Two<T> v, float 
     if constexpr (sizeof(T) == 4) o[0] = v;
     else { const float2 p = parts(v); o[0] = p.x; o[1] = p.y; }
 }
-// 1 / (1 + 2^x) and 2^x over the same
-template <typename T> __device__ __forceinline__ void sigmoids(Two<T> x, Two<T>& a, Two<T>& e) {
-    e = each<T>(x, [](float v) { return sizeof(T) == 4 ? exp2f(v) : ffn::ex2_fast(v); });
+// 1 / (1 + e^-f), and e^-f
+template <typename T> __device__ __forceinline__ void sigmoids(Two<T> f, Two<T>& a, Two<T>& e) {
+    if constexpr (sizeof(T) == 4) e = expf(-f);
+    else e = each<T>(mul2(f, splat<T>(-ffn::LOG2E)), [](float v) { return ffn::ex2_fast(v); });
     a = each<T>(add2(e, splat<T>(1.f)), [](float v) { return sizeof(T) == 4 ? 1.f / v : ffn::rcp_fast(v); });
 }
 template <typename T> __device__ __forceinline__ void gate2(Two<T> f, Two<T>& a, Two<T>& other) {
-    const Two<T> x = each<T>(mul2(f, splat<T>(-ffn::LOG2E)), [](float v) { asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(114.f)); return v; });
     Two<T> e;
-    sigmoids<T>(x, a, e);
+    sigmoids<T>(each<T>(f, [](float v) { return above(v); }), a, e);
     other = mul2(e, a);
 }
 
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
                     const Two<T> o = two_of<T>(*reinterpret_cast<const unsigned*>(to + 128 * i));
                     if (FORM == 1) {
                         Two<T> p, e;
-                        sigmoids<T>(mul2(o, splat<T>(-ffn::LOG2E)), p, e);
+                        sigmoids<T>(o, p, e);
                         y = mul2(mul2(o, p), h);
                     } else
                         y = mul2(each<T>(o, [&](float v) { return ffn::act_value<sizeof(T) == 2>(v, a.act); }), h);

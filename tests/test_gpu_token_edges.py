@@ -174,3 +174,42 @@ def test_whatever_lies_under_a_dropped_element_of_a_join(rows, cols, dt, how):
     assert not torch.isfinite(dx.cpu()[spoil]).any()                     # the stream's gradient passes on what came in
     dx.copy_(torch.where(spoil.cuda(), want["dx"][0].cuda(), dx.double()).to(dt))
     close(dx, want["dx"], dt, "dx")
+
+
+# ---- recurrence: gates far from 0 ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("steps,cols", [(1, 64), (17, 33), (40, 64)])
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("far", [20.0, 40.0, 75.0])
+def test_recurrence_gates_far_from_zero(steps, cols, dt, far):
+    """a next to 0 and 1 - a next to 0, each relative to itself: the exponential (float: 2 units in the last place, 4 roundings; bf16: 2^-22 and a rounding of
+    the exponent, |f| roundings of the value), an addition, a reciprocal and a product, then at most 8 more products."""
+    g = gen("far", steps, cols, far)
+    f64 = (far * (1.0 + torch.linspace(0, 0.05, cols, dtype=torch.float64))).expand(steps, cols).to(dt).double().clone()
+    rel = (16 * H.U if dt == FP else 2.0 ** -21 + far * 1.05 * H.U + 12 * H.U)
+    sign = torch.where(torch.arange(steps) % 2 == 0, 1.0, -1.0).double()[:, None]
+    one = (1.0 + torch.rand(1, cols, generator=g, dtype=torch.float64)).to(dt).double()
+    gpu = lambda t, d=dt: t.to(d).cuda()  # noqa: E731
+    states = torch.empty(F.ftp_recurrence_states(steps, 1), cols, device="cuda")
+    y, df, dv = (torch.empty(steps, cols, dtype=dt, device="cuda") for _ in range(3))
+    h1, dh0 = torch.empty(1, cols, device="cuda"), torch.empty(1, cols, device="cuda")
+
+    def both_ways(f, v, h0, dy, dh1):
+        F.ftp_recurrence_forward(gpu(f), gpu(v), y, h0=gpu(h0, FP), h1=h1, states=states)
+        F.ftp_recurrence_backward(gpu(f), gpu(v), gpu(dy), states, df, dv, dh1=gpu(dh1, FP), dh0=dh0)
+    near = lambda got, want, what: assert_within(got, want, (rel + HALF[got.dtype]) * want.abs(), what)  # noqa: E731
+    nothing = torch.zeros(steps, cols, dtype=torch.float64)
+    # 1 - a: a first value that nothing adds to and nothing forgets (a is 1), and a gradient that reaches every step
+    a, b = H.gates(f64)
+    v = nothing.clone()
+    v[0] = one
+    both_ways(f64, v, nothing[:1], nothing, one)
+    near(y, (b[0] * one).expand(steps, cols), "y")
+    near(h1, b[:1] * one, "h1")
+    near(dv, b * one, "dv")
+    # a: every state is the step's own value, of the other sign than the last
+    a, b = H.gates(-f64)
+    v = sign * one
+    both_ways(-f64, v, -v[:1], one.expand(steps, cols), nothing[:1])
+    near(y, v, "y")
+    near(df, a * b * one * (-2 * v), "df")
+    near(dh0, a[:1] * one, "dh0")
