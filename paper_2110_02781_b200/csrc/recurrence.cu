@@ -499,9 +499,12 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
                     const Two<T> o = two_of<T>(*reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
                     Two<T> val, slope;
                     if (FORM == 1) {
+                        // o below -79 counts as -79 in the product too: o times a's floor would not be small
+                        const Two<T> oo = each<T>(o, [](float v) { return above(v); });
                         Two<T> p, q;
-                        gate2<T>(o, p, q);
-                        val = mul2(o, p);
+                        sigmoids<T>(oo, p, q);
+                        q = mul2(q, p);
+                        val = mul2(oo, p);
                         slope = fma2(val, q, p);
                     } else {
                         float oo[N], vv[N], ss[N];

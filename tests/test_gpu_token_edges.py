@@ -213,3 +213,26 @@ def test_recurrence_gates_far_from_zero(steps, cols, dt, far):
     near(y, v, "y")
     near(df, a * b * one * (-2 * v), "df")
     near(dh0, a[:1] * one, "dh0")
+
+
+def test_recurrence_output_gates_closed_by_the_lowest_value():
+    """silu(o) and its slope are 0 far below 0: what reaches the states does not come through such an output."""
+    for dt in (BF, FP):
+        for cols in (64, 65):
+            g = gen("closed", cols, str(dt))
+            f, v, dy = (rnd(g, 50, cols).to(dt).cuda() for _ in range(3))
+            dh1 = rnd(g, 1, cols).float().cuda()
+            states = torch.empty(F.ftp_recurrence_states(50, 1), cols, device="cuda")
+            res = []
+            for value in (0.0, torch.finfo(dt).min, -1e35, -1e30, -200.0):
+                o = torch.full_like(f, value)
+                y, df, dv, do, dh0 = (*(torch.empty_like(f) for _ in range(4)), torch.empty_like(dh1))
+                F.ftp_recurrence_forward(f, v, y, o=o, states=states)
+                F.ftp_recurrence_backward(f, v, dy, states, df, dv, o=o, do=do, dh1=dh1, dh0=dh0)
+                assert not y.float().abs().max() > 1e-30
+                if value:
+                    assert do.float().abs().max() < 1e-30
+                res.append((df.float(), dv.float(), dh0))
+            for other in res[1:]:
+                for a, b in zip(res[0], other):
+                    assert torch.allclose(a, b, rtol=1e-6, atol=1e-30)
