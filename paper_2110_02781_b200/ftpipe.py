@@ -852,7 +852,7 @@ def _recurrence_desc(who, cur, f, act, coupled, offsets, max_len, named, states,
         if offsets.get_device() != cur or offsets.dtype is not torch.int32 or not offsets.is_contiguous() or offsets.dim() != 1 or offsets.numel() < 1:
             _bad(who, "offsets must be a contiguous int32 vector of sequences + 1 values on the current CUDA device")
         seqs, rows = offsets.numel() - 1, f.shape[0]
-        n = rows if max_len is None else max_len
+        n = rows if max_len is None else min(max_len, rows)
     pitches = [0 if t is None else _steps(who, name, t, f.shape, dt, cur) for name, t in named]
     d = RecurrenceDesc(seqs, n, rows, cols, prec, act, int(coupled), *pitches)
     for name, t in vectors:

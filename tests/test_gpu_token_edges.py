@@ -236,3 +236,15 @@ def test_recurrence_output_gates_closed_by_the_lowest_value():
             for other in res[1:]:
                 for a, b in zip(res[0], other):
                     assert torch.allclose(a, b, rtol=1e-6, atol=1e-30)
+
+
+def test_recurrence_packed_sequences_of_no_rows():
+    for max_len in (None, 0, 40, 1000):
+        e = lambda: torch.empty(0, 8, dtype=BF, device="cuda")  # noqa: E731
+        off = torch.zeros(4, dtype=torch.int32, device="cuda")
+        h0, h1 = torch.randn(3, 8, device="cuda"), torch.empty(3, 8, device="cuda")
+        states = torch.full((F.ftp_recurrence_states(0, 3), 8), -7.0, device="cuda")
+        F.ftp_recurrence_forward(e(), e(), e(), h0=h0, h1=h1, states=states, offsets=off, max_len=max_len)
+        assert torch.equal(h0, h1) and bool((states == -7.0).all())
+        F.ftp_recurrence_backward(e(), e(), e(), states, e(), e(), dh1=h0, dh0=h1.zero_(), offsets=off, max_len=max_len)
+        assert torch.equal(h0, h1)
