@@ -910,7 +910,7 @@ template <typename T, int G, int KIND> void (*backward_kernel(bool vec, bool lay
 }
 template <typename T, int G>
 ftp_status backward_of(JoinArgs& a, const JoinPlan& p, bool vec, int kind, cudaStream_t st, const char* who) {
-    size_t smem = a.spill ? 0 : (size_t)a.nsums * G * V<T> * p.threads * 4;
+    size_t smem = (size_t)a.nsums * G * V<T> * p.threads * 4;           // 160 KB at most: only rows of more columns a thread spill their sums
     const bool layer = a.post == FTP_NORM_LAYER || a.pre == FTP_NORM_LAYER;
     void (*kern)(JoinArgs) = nullptr;
     size_t staged = 0;
