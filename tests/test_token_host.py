@@ -100,6 +100,13 @@ def test_recurrence_calls_that_are_refused():
     assert F.ftp_recurrence_states(100, 3) == 9
 
 
+def test_recurrence_rows_that_are_not_those_of_its_sequences_are_refused():
+    for seqs, n, rows, status in ((0, 40, 80, 1), (2, 40, 81, 1), (2, 0, 80, 1), (0, 40, 0, 0)):
+        d = rec(seqs=seqs, n=n, rows=rows)
+        assert L.ftp_recurrence_forward(ref(d), P, P + 256, P + 512, None, None, Q, None, None, None) == status
+        assert L.ftp_recurrence_backward(ref(d), P, P + 256, P + 512, P + 768, None, P + 1024, None, Q, Q + 256, Q + 512, None, None) == status
+
+
 def test_logprob_calls_that_are_refused():
     def f(x=P, rows=4, vocab=64, ld=0, prec=1, scale=1.0, t=P + 2048, logp=Q, ent=None, lse=None, top=None, tl=None, k=0):
         return L.ftp_logprob_forward(x, rows, vocab, ld, prec, scale, t, logp, ent, lse, top, tl, k, None)
