@@ -957,7 +957,7 @@ ftp_status run_backward(JoinArgs& a, const JoinPlan& p, int kind, cudaStream_t s
 
 ftp_status zero_vectors(std::initializer_list<float*> all, int cols, cudaStream_t st, const char* who) {
     for (float* p : all)
-        if (p) FTP_REQUIRE(cudaMemsetAsync(p, 0, (size_t)cols * 4, st) == cudaSuccess, FTP_ECUDA, "%s: memset failed", who);
+        if (p) FTP_REQUIRE(told(cudaMemsetAsync(p, 0, (size_t)cols * 4, st)) == cudaSuccess, FTP_ECUDA, "%s: memset failed", who);
     return FTP_OK;
 }
 

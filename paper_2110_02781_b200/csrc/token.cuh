@@ -21,6 +21,11 @@ template <typename... A> void launch(A&&... args) {
     ++ffn::launches();
     ftp::launch(std::forward<A>(args)...);
 }
+// An error that the caller reports by itself: not left behind for the next call's check of its own launches.
+inline cudaError_t told(cudaError_t e) {
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+}
 template <typename... KA, typename... A>
 cudaError_t launch_cluster(void (*kern)(KA...), dim3 grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t st, A&&... args) {
     ++ffn::launches();
@@ -36,7 +41,7 @@ cudaError_t launch_cluster(void (*kern)(KA...), dim3 grid, unsigned block, size_
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
+    return told(cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...));
 }
 
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -53,10 +58,10 @@ template <cudaFuncAttribute WHAT> bool kernel_may(const void* kern, int value) {
     static thread_local const void* known[64] = {};
     static thread_local int devices[64] = {};
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (told(cudaGetDevice(&dev)) != cudaSuccess) return false;
     const size_t at = (reinterpret_cast<uintptr_t>(kern) >> 4) % 64;
     if (known[at] == kern && devices[at] == dev) return true;
-    if (cudaFuncSetAttribute(kern, WHAT, value) != cudaSuccess) return false;
+    if (told(cudaFuncSetAttribute(kern, WHAT, value)) != cudaSuccess) return false;
     known[at] = kern;
     devices[at] = dev;
     return true;

@@ -1,6 +1,9 @@
 """Operators around the feed-forward products on the GPU, where values or layouts are at their limits: states updated in place
 across a cluster, tails of runs, the float range's ends, what lies under a dropped element, gates far from 0."""
 import math
+import subprocess
+import sys
+from pathlib import Path
 
 import pytest
 import torch
@@ -248,3 +251,42 @@ def test_recurrence_packed_sequences_of_no_rows():
         assert torch.equal(h0, h1) and bool((states == -7.0).all())
         F.ftp_recurrence_backward(e(), e(), e(), states, e(), e(), dh1=h0, dh0=h1.zero_(), offsets=off, max_len=max_len)
         assert torch.equal(h0, h1)
+
+
+# ---- a launch that the runtime refuses -------------------------------------------------------------------------------------
+def test_a_refused_launch_is_reported_once():
+    """A launch into the legacy stream while a blocking stream of this thread is captured is an error of the host; the next call, outside the capture, is a
+    call like any other."""
+    code = """
+import ctypes as C
+import torch, paper_2110_02781_b200 as F
+f32 = lambda *s: torch.randn(*s, device="cuda")
+x, y, t, lp = f32(64, 256), f32(64, 256), torch.zeros(64, dtype=torch.int32, device="cuda"), f32(64)
+f, v, h = f32(1, 300, 64), f32(1, 300, 64), f32(1, 300, 64)
+calls = [lambda **k: F.ftp_logprob_forward(x, t, lp, **k), lambda **k: F.ftp_recurrence_forward(f, v, h, **k), lambda **k: F.ftp_dropout(x, y, 0.0, None, **k),
+         lambda **k: F.ftp_join_forward(None, x, None, y, post=F.NORM_NONE, **k)]
+for c in calls:
+    c()
+torch.cuda.synchronize()
+cu = C.CDLL("libcuda.so.1")
+def ok(r):
+    assert r == 0, r
+for bad in calls:
+    st, graph = C.c_void_p(), C.c_void_p()
+    ok(cu.cuStreamCreate(C.byref(st), 0))
+    ok(cu.cuStreamBeginCapture_v2(st, 0))
+    try:
+        bad(stream=0)
+        refused = False
+    except F.FtpError as e:
+        refused = "launch failed" in str(e)
+    cu.cuStreamEndCapture(st, C.byref(graph))
+    ok(cu.cuStreamDestroy_v2(st))
+    assert refused
+    for c in calls:
+        c()
+torch.cuda.synchronize()
+print("reported once")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=str(Path(__file__).parent.parent))
+    assert r.returncode == 0 and "reported once" in r.stdout, r.stdout + r.stderr
