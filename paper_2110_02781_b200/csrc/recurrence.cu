@@ -306,6 +306,8 @@ __device__ __forceinline__ void tile_in(unsigned to, const CUtensorMap* map, int
 __device__ __forceinline__ void tile_out(const CUtensorMap* map, int c, int64_t row, unsigned from) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" :: "l"(map), "r"(c), "r"((int)row), "r"(from) : "memory");
 }
+// Tiles are stored by the copy engine in whole 16 bytes: where the last columns are not (a pitch may be all the same), it would write what lies behind them.
+template <typename T> __device__ __forceinline__ bool whole_tile(int c, int cols) { return c + TILE<T> <= cols || cols % V<T> == 0; }
 __device__ __forceinline__ void tiles_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void tiles_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }       // shared memory may be written again
 __device__ __forceinline__ void tiles_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
@@ -338,6 +340,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
     const Lane<T, true> lane(tile);
+    const bool storable = whole_tile<T>(c, a.cols);
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.h0 ? a.h0 + b * a.cols : nullptr, a.cols, carry);
@@ -413,8 +416,8 @@ __global__ void __launch_bounds__(32 * WARPS, 2) recurrence_forward_stream_kerne
                 }
                 *reinterpret_cast<unsigned*>(to + 128 * i) = word_of<T>(y);
             }
-            if (n == RUN) {
-                tiles_fence();
+            tiles_fence();                                           // the copy engine reads this tile, or fills it again
+            if (n == RUN && storable) {
                 __syncwarp();
                 if (l == 0 && ok) { tile_out(&map_y, c, seq.start + t0, tiles + (3 * s + 2) * TILE_BYTES); tiles_commit(); }
             } else if (ok)
@@ -456,6 +459,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
     const int64_t unit = blockIdx.x / ranks, b = unit / a.tiles;
     const int tile = (int)(unit - b * a.tiles), c = tile * TILE<T>;
     const Lane<T, true> lane(tile);
+    const bool storable = whole_tile<T>(c, a.cols);
     const Where seq = where(a, b);
     float carry[N];
     lane.get_state(a.dh1 ? a.dh1 + b * a.cols : nullptr, a.cols, carry);
@@ -533,7 +537,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
         if (l == 0) {
             tiles_read();                                            // the other stage's results have left
             if (base < last - (skip ? stride : 0)) load(t0 - stride, s ^ 1);
-            if (FORM && n == RUN && ok) { tile_out(&maps_out.m[2], c, seq.start + t0, tiles + (4 * s + 2) * TILE_BYTES); tiles_commit(); }
+            if (FORM && n == RUN && storable && ok) { tile_out(&maps_out.m[2], c, seq.start + t0, tiles + (4 * s + 2) * TILE_BYTES); tiles_commit(); }
         }
         Map<N> all;
         to_floats<T>(all_a, all.a);
@@ -553,24 +557,21 @@ __global__ void __launch_bounds__(32 * BACK_WARPS, 3) recurrence_backward_stream
                 *reinterpret_cast<unsigned*>(at + 128 * i) = word_of<T>(mul2(q, join_floats<T>(keep)));
                 *reinterpret_cast<unsigned*>(at + TILE_BYTES + 128 * i) = word_of<T>(COUPLED ? mul2(e, other[i]) : e);
             }
-            if (n == RUN) {
-                tiles_fence();
+            tiles_fence();                                           // the copy engine reads these tiles, or fills them again in the next turn
+            if (n == RUN && storable) {
                 __syncwarp();
                 if (l == 0 && ok) {
                     tile_out(&maps_out.m[0], c, seq.start + t0, tiles + (4 * s) * TILE_BYTES);
                     tile_out(&maps_out.m[1], c, seq.start + t0, tiles + (4 * s + 1) * TILE_BYTES);
                     tiles_commit();
                 }
-            } else {
-                tiles_fence();                                       // the copy engine fills these tiles again in the next turn
-                if (ok)
-                    for (int i = 0; i < n; ++i) {
-                        const int64_t row = seq.start + t0 + i;
-                        lane.put_word(static_cast<T*>(a.df) + row * a.lddf, a.cols, *reinterpret_cast<const unsigned*>(at + 128 * i));
-                        lane.put_word(static_cast<T*>(a.dv) + row * a.lddv, a.cols, *reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
-                        if (FORM) lane.put_word(static_cast<T*>(a.dout) + row * a.lddo, a.cols, *reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
-                    }
-            }
+            } else if (ok)
+                for (int i = 0; i < n; ++i) {
+                    const int64_t row = seq.start + t0 + i;
+                    lane.put_word(static_cast<T*>(a.df) + row * a.lddf, a.cols, *reinterpret_cast<const unsigned*>(at + 128 * i));
+                    lane.put_word(static_cast<T*>(a.dv) + row * a.lddv, a.cols, *reinterpret_cast<const unsigned*>(at + TILE_BYTES + 128 * i));
+                    if (FORM) lane.put_word(static_cast<T*>(a.dout) + row * a.lddo, a.cols, *reinterpret_cast<const unsigned*>(at + 2 * TILE_BYTES + 128 * i));
+                }
             parity ^= s;
             s ^= 1;
         }

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import token_helpers as H
-from ffn_helpers import HALF, assert_within
+from ffn_helpers import HALF, Guarded, assert_within
 from test_gpu_token import BF, FP, close, gen, join_case, on_gpu, rec_inputs, rnd, rng_of, vec
 
 F = pytest.importorskip("paper_2110_02781_b200")
@@ -290,3 +290,33 @@ print("reported once")
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=str(Path(__file__).parent.parent))
     assert r.returncode == 0 and "reported once" in r.stdout, r.stdout + r.stderr
+
+
+# ---- recurrence: columns of a wider tensor -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("cols,gap", [(63, 1), (7, 1), (1, 7), (33, 7), (66, 6), (130, 6), (61, 3), (5, 3)])
+@pytest.mark.parametrize("lengths", [[700], [33] * 20, [64, 0, 5, 257, 16, 1], [100] * 300])
+@pytest.mark.parametrize("dt,name", [(BF, "silu"), (BF, None), (FP, "silu"), (FP, None)])
+def test_recurrence_over_rows_on_16_bytes_of_columns_that_are_not(cols, gap, lengths, dt, name):
+    """Rows of every tensor start on 16 bytes, and the last columns do not fill theirs: what lies behind them is another's."""
+    g = gen("slices", cols, str(lengths), name)
+    rows, seqs = sum(lengths), len(lengths)
+    f, f64, v, v64, o, o64 = rec_inputs(g, rows, cols, dt, gap)
+    dy, dy64 = on_gpu(rnd(g, rows, cols), dt, gap)
+    starts = [0] + torch.tensor(lengths).cumsum(0).tolist()
+    y, df, dv, do = (Guarded(rows, cols, dt, gap) for _ in range(4))
+    states = torch.empty(F.ftp_recurrence_states(rows, seqs), cols, device="cuda")
+    how = dict(act=F.ACT_SILU if name else F.ACT_NONE, offsets=torch.tensor(starts, dtype=torch.int32, device="cuda"), max_len=max(lengths), o=o.t if name else None)
+    F.ftp_recurrence_forward(f.t, v.t, y.t, states=states, **how)
+    F.ftp_recurrence_backward(f.t, v.t, dy.t, states, df.t, dv.t, do=do.t if name else None, **how)
+    assert y.untouched() and df.untouched() and dv.untouched() and do.untouched()
+    zero = torch.zeros(cols, dtype=torch.float64)
+    for b in sorted({0, seqs // 2, seqs - 1}):
+        at = slice(starts[b], starts[b + 1])
+        o1 = o64[at] if name else None
+        _, _, ys, ey = H.recurrence(f64[at], v64[at], o1, zero, name, True, dt)
+        want = H.recurrence_backward(f64[at], v64[at], o1, zero, dy64[at], zero, name, True, dt)
+        close(y.t[at], (ys, ey), dt, f"y of {b}")
+        close(df.t[at], want["df"], dt, f"df of {b}")
+        close(dv.t[at], want["dv"], dt, f"dv of {b}")
+        if name:
+            close(do.t[at], want["do"], dt, f"do of {b}")
