@@ -320,3 +320,29 @@ def test_recurrence_over_rows_on_16_bytes_of_columns_that_are_not(cols, gap, len
         close(dv.t[at], want["dv"], dt, f"dv of {b}")
         if name:
             close(do.t[at], want["do"], dt, f"do of {b}")
+
+
+# ---- tensors of more than 2^31 elements ---------------------------------------------------------------------------------------
+def test_wide_offsets_through_the_copy_engine_and_backward():
+    """Rows whose elements lie beyond 2^31: long sequences, and the backward passes."""
+    rows, cols, ld = 45, 96, 50_000_000
+    buf = torch.zeros((rows - 1) * ld + 16 * cols, dtype=BF, device="cuda")
+    far = [torch.as_strided(buf, (rows, cols), (ld, 1), i * cols) for i in range(12)]
+    near = [torch.randn(rows, cols, device="cuda").to(BF) for _ in range(12)]
+    for a, b in zip(far, near):
+        a.copy_(b)
+
+    def run(t):
+        f, v, o, dy, y, df, dv, do, dl, du, dx, dg = t
+        states, h1, dh0 = torch.empty(F.ftp_recurrence_states(rows, 1), cols, device="cuda"), torch.empty(1, cols, device="cuda"), torch.empty(1, cols, device="cuda")
+        F.ftp_recurrence_forward(f, v, y, o=o, h1=h1, states=states)
+        F.ftp_recurrence_backward(f, v, dy, states, df, dv, o=o, do=do, dh0=dh0)
+        lse, lp = torch.empty(rows, 2, device="cuda"), torch.empty(rows, device="cuda")
+        token = torch.arange(rows, dtype=torch.int32, device="cuda")
+        F.ftp_logprob_forward(f, token, lp, lse=lse)
+        F.ftp_logprob_backward(f, token, lse, lp, dl)
+        stats, w, dw = torch.rand(4, rows, device="cuda", generator=torch.Generator("cuda").manual_seed(1)), torch.ones(cols, device="cuda"), torch.empty(2, cols, device="cuda")
+        F.ftp_join_backward(f, v, o, dy, stats, du=du, dx=dx, dgate=dg, dw_post=dw[0], dw_pre=dw[1], gate=y, gate_rows=1, w_post=w, w_pre=w, dropout=0.2, rng=rng_of(3, 4))
+        return [y, df, dv, do, dl, du, dx, dg, h1, dh0, lse, dw]
+    for a, b in zip(run(far), run(near)):
+        assert torch.equal(a, b)
