@@ -477,8 +477,8 @@ ftp_status ftp_check_op_status(void* stream);
 /* ---- operators around the feed-forward products ---------------------------------------------------------------------
  * (The paper's networks have no counterpart: these are what a stage of a language model needs beside its token-wise products.)
  * Conventions as above: tokens are rows, vectors of weights and their gradients are float, everything else has the type
- * `precision` names, pitches are elements between rows (0: no gap), sums, statistics and states are float or double.  The same
- * inputs laid out alike give the same bits.  Outputs may not overlap inputs or each other but where a call says so. */
+ * `precision` names, pitches are elements between rows (0: no gap), sums, statistics and states are float or double; of bf16
+ * tensors their exponentials are known to 2^-21 (gates f of the recurrence: and 2^-24 |f|).  The same inputs laid out alike give the same bits.  Outputs may not overlap inputs or each other but where a call says so. */
 
 /* Dropout.  A mask is never stored: whether an element stays is a function of two 64-bit words in device memory, rng[0] (key) and
  * rng[1] (step), read when the kernel runs (a replayed graph takes the words of that moment), of `site` (0..2^24-1: which dropout
@@ -498,7 +498,8 @@ ftp_status ftp_dropout(const void* x, void* y, int64_t rows, int32_t cols, int64
  *
  * post, pre: FTP_NORM_NONE; FTP_NORM_RMS, v / sqrt(mean(v^2) + eps) * w + b; FTP_NORM_LAYER, (v - mean(v)) / sqrt(var(v) + eps) *
  * w + b, over a row; w and b nullable (1 and 0).  gate: NULL (1); with gate_rows 0 a float vector of cols; else a matrix of the
- * tensors' type with a row for every gate_rows tokens (the last may have fewer).  s is rounded to the tensors' type and y is
+ * tensors' type with a row for every gate_rows tokens (the last may have fewer).  Squares and their sums are floats: a row with
+ * values beyond 1e18 may have 1 / deviation 0, and values below 1e-19 add nothing to it.  s is rounded to the tensors' type and y is
  * made of the rounded s.  A dropped element is 0 in s, and nothing goes back through it, whatever u (without post) or the
  * gradients hold there; gates are finite.  Rows hold up to 16384 columns. */
 enum { FTP_NORM_NONE = 0, FTP_NORM_RMS = 1, FTP_NORM_LAYER = 2 };

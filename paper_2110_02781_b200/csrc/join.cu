@@ -7,10 +7,12 @@
 // loads start as soon as a row's values are taken; a single row is spread over more threads.  The column sums of the backward pass (gradients of
 // the norms' weights and of a gate that many rows share) grow in shared memory, each thread its own columns, over at most 64 rows, and a second
 // kernel adds the blocks' sums in double, in a fixed order.
-// What sets the time is instructions (packed float arithmetic halves them; a dropout mask is 20 a column of eight): 8192 x 4096 bf16 forward with
-// dropout and a gate 65 us (4.1 TB/s), without dropout 55, 8192 x 8192 without both 93 (5.7 TB/s); backward 130 us with dropout, a gate and three
-// column sums (3.1 TB/s, 73 instructions an element, 2.2 a cycle), 120 without dropout, 84 for the second norm alone (4.8 TB/s).
-// Rows off 16 bytes: a thread's columns lie a block's width apart, single elements (8000 x 4001 bf16: 157 us forward, 233 backward).
+// What sets the time is latency at 16 warps a multiprocessor, which the registers allow, over as many instructions as there are: 1.8 of 4 a cycle forward
+// (34 an element), 2.2 backward (76), no pipe over 39 %; packed float arithmetic halved them.  8192 x 4096 bf16 forward with dropout and a gate
+// 65 us (4.1 TB/s), without both 46, 8192 x 8192 without both 93 (5.7 TB/s); backward 131 us with dropout, a gate and three column sums (3.1 TB/s), 118
+// without dropout, 106 without the gate too, 88-91 for the second norm alone.  8192 x 2048 float: 48 forward, 90 backward, without both.
+// A call that leaves out u, ds or a weight's gradient goes through the kernel for any (8192 x 4096 bf16: 140-162 us, floors 31 to 62).
+// Rows off 16 bytes: a thread's columns lie a block's width apart, single elements (8000 x 4001 bf16: 157 us forward, 247 backward).
 #include <algorithm>
 #include "token.cuh"
 
@@ -542,7 +544,7 @@ __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_kernel(const J
 }
 
 // The same for rows of more than 16 columns a thread, whose values do not fit into registers: a group of columns at a time, every group read twice (the
-// second time from the second cache: 2000 x 16384 bf16 with all terms 1090 us with the values spilled to local memory, and less than half of that so).
+// second time from the second cache: 2000 x 16384 bf16 with all terms 1090 us with the values spilled to local memory, and 500 so).
 template <typename T, bool VEC, bool LAYER>
 __global__ void __launch_bounds__(BACKWARD_THREADS) join_backward_wide_kernel(const JoinArgs a) {
     constexpr int NS = LAYER ? 8 : 3;
@@ -761,7 +763,8 @@ __global__ void __launch_bounds__(1024) join_sums_kernel(const JoinSums a) {
     }
     if (w == 0 && c < a.cols) a.out[blockIdx.y][c] = (float)s;
 }
-// A group's gate gradient: the sums of the runs that hold rows of it.
+// A group's gate gradient: the sums of the runs that hold rows of it, one after another (long groups take long: 8192 x 512 bf16 with 4096 rows a group 78 us
+// for the whole call, 31 with a gate vector).
 template <typename T>
 __global__ void __launch_bounds__(128) join_gate_kernel(const float* part, int64_t groups, int64_t gate_rows, int64_t rows, int run, int cols, T* out, int64_t ld) {
     grid_dep_sync();
@@ -776,8 +779,9 @@ __global__ void __launch_bounds__(128) join_gate_kernel(const float* part, int64
     }
 }
 
-// A warp per 32 V columns of a row, four such pieces in flight.  16384 x 4096 bf16: 60 us, 4.5 TB/s; bound by the generator's integer arithmetic (22
-// instructions an element, the integer pipe over half used); one piece in flight 69 us, two 60, eight 70.
+// A warp per 32 V columns of a row, four such pieces in flight.  16384 x 4096 bf16: 61 us, 4.4 TB/s, 2.6 instructions a cycle and the integer pipe over half
+// used: 22 instructions an element, a quarter of them the generator's products and exclusive ors, the others masks, conversions and 64-bit indexes; one
+// piece in flight 69 us, two 60, eight 70.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) dropout_kernel(const T* x, T* y, int64_t rows, int cols, int64_t ldx, int64_t ldy, const Drop d) {
     __shared__ Rounds keys;
@@ -875,9 +879,11 @@ void run_forward(JoinArgs& a, cudaStream_t st) {
 
 // The backward pass's work on its rows: runs of up to 64 rows (the float additions of a running sum), as long as give all blocks that the GPU
 // holds the same, once or more often (12000 x 3584 bf16 with runs of 64: 250 us, 173 with 41).  Eight columns a thread, two rows at a time, or
-// sixteen: of bf16 rows over 2048, 16 where only one block of the others would fit (16000 x 2560: 166 instead of 201 us), and where a row a time is taken
-// anyway or the second norm is alone (12000 x 4096: layer norms 235 instead of 267, the second norm alone 126 instead of 147; but both rms 144 and 130
-// for 8192 x 4096).  Float 8000 x 2560 rather 8: 130 instead of 156.
+// sixteen.  Up to 2048 columns eight (12000 x 2048 bf16, 8 and 16: both rms 95 and 107 us, layer norms 146 and 196, the second norm alone 67 and 71).  bf16
+// above: sixteen, except for both rms over 2560.  Up to 2560 columns these are 160 threads, of which three blocks fit and of the other kind one (12000 x 2560
+// 140 and 127 us); from there on two and one (2568: 144 and 153, 2624: 147 and 156, 3328: 175 and 177, 4096: 193 and 195).  Layer norms take a row
+// at a time anyway (2176: 226 and 172, 3328: 278 and 247; but 4096 with gate and dropout 310 and 332), the second norm alone is bound by memory sooner (2176: 89 and
+// 75, 4096: 130 and 126).  Float up to 4096: eight (8000 x 2176 both rms 128 and 154, 4096 212 and 237, layer norms 220 and 251).
 struct JoinPlan { int threads, groups, run; int64_t blocks; };
 JoinPlan plan_backward(const ftp_join_desc* d) {
     JoinPlan p;

@@ -9,7 +9,7 @@
 // logits of the row reach, and only the groups of threads whose maximum reaches it are looked at again (about k of up to 512 threads; in registers where a
 // thread has no more than four).  What reaches the bound is ranked by (value, lowest token).
 // 4096 x 50021 bf16 with entropies: 73-83 us (5.0-5.6 TB/s; the exponentials use two thirds of their pipe); 16 x 128000 with 20 top tokens: 9.1 us, a
-// chain of eight exchanges between threads, warps and blocks; 16000 x 12000 with a warp a row 64 us (6.0 TB/s); backward, 8192 x 32000: 181-191 us (5.5-5.8 TB/s).
+// chain of eight exchanges between threads, warps and blocks; 16000 x 12000 with a warp a row 64 us (6.0 TB/s); backward, 8192 x 32000: 182-191 us (5.5-5.8 TB/s).
 #include <algorithm>
 #include <type_traits>
 #include "token.cuh"

@@ -8,8 +8,8 @@
 // the order of time, whatever finishes first: one read of the data and the same bits every time.  The state and the maps are float.
 // Rows on 16 bytes come and go as tiles through the copy engine (below): 65536 x 2048 bf16 forward with a gate 279 us (4.0 TB/s; four
 // exponentials and reciprocals an element use half of their pipe, 256 blocks leave a seventh of the GPU idle), 24 ragged sequences of up to 4096 x 1536
-// backward 262 us (4.3 TB/s; latency at 12 warps a multiprocessor, which the registers allow).  Other rows through registers: 32000 x 2001 bf16 218 us
-// forward, 625 backward.
+// 166 forward and 262 us backward (4.3 TB/s; latency at 12 warps a multiprocessor, which the registers allow).  Float, 32000 x 1000: 137 and
+// 315 us, without a gate 91 and 203.  Other rows through registers: 32000 x 2001 bf16 209 us forward, 599 backward.
 // The backward pass starts every run from the state that the forward pass kept in front of it, walks it forward once and then, with
 // q_t = a_t (g_t + q_(t+1)) (g: dy act(o), q_(t+1): what reaches h_t from behind), backward in the same way.
 #include <algorithm>
@@ -611,8 +611,8 @@ __global__ void __launch_bounds__(128) recurrence_short_kernel(const RecArgs a) 
     if (a.h1) lane.put_state(a.h1 + b * a.cols, a.cols, h);
 }
 
-// One run backward.  Between its two walks it keeps, per step, a and 1 - a's partner s (the smaller of both, sign bit set where it is a), the gradient g that
-// reaches h from its own output, and in shared memory h_(t-1) - v (coupled) or h_(t-1).
+// One run backward.  Between its two walks it keeps, per step, a and the gradient g that reaches h from its own output in registers, and in shared memory
+// (1 - a) (h_(t-1) - v) and 1 - a (coupled), or (1 - a) h_(t-1).
 template <typename T, bool VEC, int FORM> struct Backward {
     static constexpr int N = LANES<T>;
     unsigned f[RUN], v[RUN], o[RUN], dy[RUN];
