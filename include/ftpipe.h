@@ -478,7 +478,8 @@ ftp_status ftp_check_op_status(void* stream);
  * (The paper's networks have no counterpart: these are what a stage of a language model needs beside its token-wise products.)
  * Conventions as above: tokens are rows, vectors of weights and their gradients are float, everything else has the type
  * `precision` names, pitches are elements between rows (0: no gap), sums, statistics and states are float or double; of bf16
- * tensors their exponentials are known to 2^-21 (gates f of the recurrence: and 2^-24 |f|).  The same inputs laid out alike give the same bits.  Outputs may not overlap inputs or each other but where a call says so. */
+ * tensors their exponentials are known to 2^-21 (gates f of the recurrence: and 2^-24 |f|).  The same inputs laid out alike
+ * give the same bits.  Outputs may not overlap inputs or each other but where a call says so. */
 
 /* Dropout.  A mask is never stored: whether an element stays is a function of two 64-bit words in device memory, rng[0] (key) and
  * rng[1] (step), read when the kernel runs (a replayed graph takes the words of that moment), of `site` (0..2^24-1: which dropout
